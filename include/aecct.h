@@ -240,6 +240,66 @@ int aecct_spe_table(const uint8_t *H, int32_t n, int32_t k, int32_t d_spe, int32
                     const double *wq, const double *wk, const double *wv, const double *wo, float *spe_out,
                     double *lam_out, double *U_out, double *spe64_out);
 
+/*
+ * Operators of AAP layers of any width (no counterpart in the paper beyond eqs. Quant, Ternary and
+ * AAPLinear, Sec. 4.1): what a network that is built from AAP linear layers trains and answers with,
+ * outside the fused decoder.  All pointers DEVICE unless said otherwise; asynchronous on cuda_stream;
+ * element types of activations and gradients are AECCT_F32, AECCT_F16 and AECCT_BF16, sums and statistics
+ * are 32-bit or wider.  A row is a token.  A leading dimension (ld...) is the distance from one row to the
+ * next, in elements, at least the row's width.  Pointers are aligned to their element; rows that are
+ * 16-byte aligned and a multiple of 16 bytes apart are read fastest.  Outputs do not overlap inputs unless
+ * said otherwise.  A workspace is used from the call's start on the stream to its end.  Every result is the
+ * same bits on every run.
+ */
+#define AECCT_F32 0
+#define AECCT_F16 1
+#define AECCT_BF16 2
+
+/* Root-mean-square norm with the residual's addition, quantised to 8 bits (eq. Quant):
+ *   h = x + residual, rounded to its type; r = 1 / sqrt(mean_i h_i^2 + eps); z_i = h_i gain_i in 32 bits;
+ *   alpha = max(max_i |z_i|, 2^-100); codes_i = rint(z_i (127 / alpha)); scale = alpha r / 127,
+ * so that codes_i scale is the norm's output h_i r gain_i, rounded to 255 steps.  The codes take no part of
+ * a sum, and are the same bits on every device and batch.
+ *   x, residual  [rows][d] of dtype, ldx and ldr apart; residual NULL: h = x, and sum is not written.
+ *   gain         fp32 [d].
+ *   sum          [rows][d] of dtype: h (it may be x or residual itself, where those are d apart).
+ *   codes        int8 [rows][d];  scale  fp32 [rows].
+ *   values       [rows][d] of dtype: codes_i scale, or NULL.
+ * A row that holds a NaN or an infinity gets a scale that is not a number, and codes without meaning.
+ * rows == 0 is a no-op.  Errors: INVALID_ARG (rows < 0, d < 1, a leading dimension under d, a dtype not
+ * named above, eps < 0 or not finite, a NULL or misaligned pointer), UNSUPPORTED (d > 32768), CUDA. */
+int aecct_rms_quant(const void *x, int64_t ldx, const void *residual, int64_t ldr, const float *gain, int64_t rows,
+                    int32_t d, int32_t dtype, float eps, void *sum, int8_t *codes, float *scale, void *values,
+                    void *cuda_stream);
+
+/* Its gradients, the rounding passed straight through (dy is the gradient of codes_i scale):
+ *   t_i = dy_i gain_i; dx_i = r t_i - h_i r^3 mean_j(t_j h_j) + dsum_i; dgain_i = sum over rows of dy_i h_i r.
+ * dx is the gradient of x and of residual alike.
+ *   dy, h, dsum  [rows][d] of dtype (h: the sum of the forward pass, or x without a residual; dsum: the
+ *                gradient that reaches h by another way, or NULL).
+ *   dx           [rows][d] of dtype;  dgain  fp32 [d] (zero for no rows).
+ *   workspace    aecct_rms_quant_backward_workspace bytes, 16-byte aligned.
+ * Errors: as above, and INVALID_ARG for a workspace that is too small. */
+int aecct_rms_quant_backward_workspace(int64_t rows, int32_t d, int64_t *bytes);
+int aecct_rms_quant_backward(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *dsum, int64_t ldd,
+                             const float *gain, int64_t rows, int32_t d, int32_t dtype, float eps, void *dx,
+                             float *dgain, void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
+/* The global norm over many gradients, and the gradients scaled down to it:
+ *   norm = sqrt(sum over tensors and elements of g^2); out = g min(1, max_norm / (norm + eps)).
+ *   grad, out    HOST arrays of n_tensors DEVICE pointers; out[j] may be grad[j] (in place: not written
+ *                where the factor is 1), and no other tensor.
+ *   len, dtype   HOST [n_tensors]: elements (0 is allowed, with any pointer) and type of each tensor.
+ *   norm         DEVICE fp32 scalar (0 for no tensors).
+ *   workspace    aecct_clip_workspace bytes, 8-byte aligned.
+ * Squares are 32-bit products: elements past 1.8e19 make the norm infinite and the factor 0; a NaN makes
+ * every gradient one.  Errors: INVALID_ARG (n_tensors or a length < 0, a dtype not named above, max_norm <= 0,
+ * eps < 0 or either not finite, a NULL or misaligned pointer, a workspace that is too small), CUDA. */
+int aecct_clip_workspace(int32_t n_tensors, int64_t *bytes);
+int aecct_clip_gradients(int32_t n_tensors, const void *const *grad, const int64_t *len, const int32_t *dtype,
+                         void *const *out, float max_norm, float eps, float *norm, void *workspace,
+                         int64_t workspace_bytes, void *cuda_stream);
+
 /* Wait for the handle's last decode and report whether its kernel stopped on a
  * device-side timeout (AECCT_ERR_TIMEOUT) or a CUDA error occurred. */
 int aecct_synchronize(aecct_handle *h);

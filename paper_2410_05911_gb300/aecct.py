@@ -26,7 +26,8 @@ EXPORTED_SYMBOLS = (
     "aecct_create", "aecct_decode", "aecct_decode_host", "aecct_synchronize", "aecct_set_capture",
     "aecct_query", "aecct_destroy", "aecct_status_string", "aecct_last_error", "aecct_selftest_mma",
     "aecct_selftest_timeout", "aecct_decode_host_noalloc", "aecct_selftest_fma_rate", "aecct_aap_ternarize",
-    "aecct_aap_ternarize_list", "aecct_spe_table",
+    "aecct_aap_ternarize_list", "aecct_spe_table", "aecct_rms_quant", "aecct_rms_quant_backward",
+    "aecct_rms_quant_backward_workspace", "aecct_clip_gradients", "aecct_clip_workspace",
 )
 
 
@@ -88,6 +89,12 @@ def load(build_if_missing: bool = True):
     L.aecct_aap_ternarize.argtypes = [P, I32, P, P, ctypes.c_float, P, P, P, P]
     L.aecct_aap_ternarize_list.argtypes = [P, I32, P, P, ctypes.c_float, P, P, P, P]
     L.aecct_spe_table.argtypes = [P, I32, I32, I32, I32, P, P, P, P, P, P, P, P, P]
+    F32 = ctypes.c_float
+    L.aecct_rms_quant.argtypes = [P, I64, P, I64, P, I64, I32, I32, F32, P, P, P, P, P]
+    L.aecct_rms_quant_backward.argtypes = [P, I64, P, I64, P, I64, P, I64, I32, I32, F32, P, P, P, I64, P]
+    L.aecct_rms_quant_backward_workspace.argtypes = [I64, I32, ctypes.POINTER(I64)]
+    L.aecct_clip_gradients.argtypes = [I32, P, P, P, P, F32, F32, P, P, I64, P]
+    L.aecct_clip_workspace.argtypes = [I32, ctypes.POINTER(I64)]
     for name in EXPORTED_SYMBOLS:
         fn = getattr(L, name)
         if fn.restype is None or fn.restype is ctypes.c_int:
@@ -404,3 +411,139 @@ def spe_table(H: np.ndarray, params, want_eigen: bool = False):
     _check(load().aecct_spe_table(H.ctypes.data, n, n - m, d_spe, heads, *[w.ctypes.data for w in ws], out.ctypes.data,
                                   ptr(lam), ptr(U), ptr(t64)), "aecct_spe_table")
     return (out, t64, lam, U) if want_eigen else out
+
+
+# ------------------------------------------------------------------------------------------
+# operators of AAP layers of any width
+# ------------------------------------------------------------------------------------------
+_ELEMENT = {}  # torch type -> the C ABI's number
+
+
+def _element(dtype):
+    """The C ABI's number of an activation or gradient type, None for another type."""
+    if not _ELEMENT:
+        import torch
+
+        _ELEMENT.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
+    return _ELEMENT.get(dtype)
+
+
+def _rows(t):
+    """(tensor, elements from row to row): rows of the last dimension, read where they lie if they are an
+    equal distance apart, else from a contiguous copy."""
+    if t.is_contiguous():
+        return t, t.shape[-1]
+    if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]:
+        return t, t.stride(0)
+    return t.contiguous(), t.shape[-1]
+
+
+def _check_like(name, t, x, dtype=None):
+    if t.device != x.device or t.dtype != (dtype or x.dtype) or t.shape != x.shape:
+        raise ValueError(f"{name} must be a {dtype or x.dtype} tensor of shape {tuple(x.shape)} on {x.device}")
+
+
+def _check_rows(name, t, gain):
+    """`t` holds rows of a known type on the GPU, and `gain` one float32 for each element of a row."""
+    import torch
+
+    if not t.is_cuda or _element(t.dtype) is None or t.dim() < 1:
+        raise ValueError(f"{name} must be a float32, float16 or bfloat16 CUDA tensor of rows")
+    if gain.device != t.device or gain.dtype != torch.float32 or gain.dim() != 1 or gain.shape[0] != t.shape[-1]:
+        raise ValueError(f"gain must be a float32 tensor of shape ({t.shape[-1]},) on {t.device}")
+
+
+def rms_quant(x, gain, residual=None, eps: float = 1e-6, want_values: bool = False, stream=None):
+    """aecct_rms_quant: h = x + residual, its root-mean-square norm times gain, and eq. Quant of that, a
+    row (the last dimension) at a time, on `stream` after what is queued on the current one.
+
+    Returns (codes int8 like x, scale float32 x.shape[:-1], total, values): codes * scale is the norm's output;
+    total is h in x's type (x itself without a residual); values is codes * scale in x's type, or None."""
+    import torch
+
+    _check_rows("x", x, gain)
+    if residual is not None:
+        _check_like("residual", residual, x)
+    dev, d = x.device, x.shape[-1]
+    src, ldx = _rows(x)
+    res, ldr = _rows(residual) if residual is not None else (None, 0)
+    gain = gain.contiguous()
+    codes = torch.empty(x.shape, dtype=torch.int8, device=dev)
+    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev)
+    total = torch.empty(x.shape, dtype=x.dtype, device=dev) if residual is not None else x
+    values = torch.empty(x.shape, dtype=x.dtype, device=dev) if want_values else None
+    s = _stream_of(stream, dev, (src, res, gain, codes, scale, total, values))
+    st = load().aecct_rms_quant(src.data_ptr(), ldx, res.data_ptr() if res is not None else None, ldr, gain.data_ptr(),
+                                scale.numel(), d, _element(x.dtype), eps,
+                                total.data_ptr() if res is not None else None, codes.data_ptr(), scale.data_ptr(),
+                                values.data_ptr() if values is not None else None, s.cuda_stream)
+    _check(st, "aecct_rms_quant")
+    return codes, scale, total, values
+
+
+def rms_quant_backward(dy, total, gain, dtotal=None, eps: float = 1e-6, stream=None):
+    """aecct_rms_quant_backward: the gradients of rms_quant, the rounding passed straight through.  dy is
+    the gradient of codes * scale, total the sum that the forward pass returned, dtotal the gradient that
+    reaches it by another way (the residual stream's own).  Returns (dx, dgain): dx is the gradient of x and
+    of residual alike, in their type; dgain is float32."""
+    import torch
+
+    _check_rows("dy", dy, gain)
+    _check_like("total", total, dy)
+    if dtotal is not None:
+        _check_like("dtotal", dtotal, dy)
+    dev, d = dy.device, dy.shape[-1]
+    rows = dy.numel() // d if d else 0
+    g, lddy = _rows(dy)
+    h, ldh = _rows(total)
+    dt, ldd = _rows(dtotal) if dtotal is not None else (None, 0)
+    gain = gain.contiguous()
+    L = load()
+    size = ctypes.c_int64()
+    _check(L.aecct_rms_quant_backward_workspace(rows, d, ctypes.byref(size)), "aecct_rms_quant_backward")
+    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dev)
+    dgain = torch.empty(d, dtype=torch.float32, device=dev)
+    work = torch.empty(max(1, size.value), dtype=torch.uint8, device=dev)
+    s = _stream_of(stream, dev, (g, h, dt, gain, dx, dgain, work))
+    st = L.aecct_rms_quant_backward(g.data_ptr(), lddy, h.data_ptr(), ldh, dt.data_ptr() if dt is not None else None, ldd,
+                                    gain.data_ptr(), rows, d, _element(dy.dtype), eps, dx.data_ptr(), dgain.data_ptr(),
+                                    work.data_ptr(), size.value, s.cuda_stream)
+    _check(st, "aecct_rms_quant_backward")
+    return dx, dgain
+
+
+def clip_gradients(grads, max_norm: float, eps: float = 1e-6, out=None, stream=None):
+    """aecct_clip_gradients: scales the tensors `grads` by min(1, max_norm / (norm + eps)), norm the 2-norm over
+    all of their elements, in place or into the tensors `out`.  Returns norm, a float32 scalar on the GPU."""
+    import torch
+
+    grads = list(grads)
+    outs = grads if out is None else list(out)
+    if len(outs) != len(grads):
+        raise ValueError(f"out must have {len(grads)} tensors")
+    n = len(grads)
+    dev = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
+    if dev.type != "cuda":
+        raise ValueError("clip_gradients takes CUDA tensors")
+    kinds = []
+    for g, o in zip(grads, outs):
+        k = _element(g.dtype)
+        if k is None or g.device != dev or not g.is_contiguous():
+            raise ValueError("gradients must be contiguous float32, float16 or bfloat16 tensors on one device")
+        if o is not g and (o.dtype != g.dtype or o.shape != g.shape or o.device != dev or not o.is_contiguous()):
+            raise ValueError("out must hold contiguous tensors like the gradients")
+        kinds.append(k)
+    L = load()
+    size = ctypes.c_int64()
+    _check(L.aecct_clip_workspace(n, ctypes.byref(size)), "aecct_clip_gradients")
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    work = torch.empty(size.value, dtype=torch.uint8, device=dev)
+    src = np.array([g.data_ptr() for g in grads], np.uintp)
+    dst = src if out is None else np.array([o.data_ptr() for o in outs], np.uintp)
+    lens = np.array([g.numel() for g in grads], np.int64)
+    types = np.array(kinds, np.int32)
+    s = _stream_of(stream, dev, (*grads, *(outs if out is not None else ()), norm, work))
+    st = L.aecct_clip_gradients(n, src.ctypes.data, lens.ctypes.data, types.ctypes.data, dst.ctypes.data, max_norm, eps,
+                                norm.data_ptr(), work.data_ptr(), size.value, s.cuda_stream)
+    _check(st, "aecct_clip_gradients")
+    return norm

@@ -282,6 +282,43 @@ cudaError_t launch_aap_ternarize(const float *const *w, int n, const int64_t *le
 cudaError_t launch_unpack_weights(const uint8_t *packed, int n_layers, int D, const ChunkDesc *chunks, int n_chunks,
                                   uint32_t layer_bytes, uint8_t *wstream, cudaStream_t stream);
 
+// norm.cu: root-mean-square norm with the residual's addition and eq. Quant, and its gradients.
+// dtype: 0 = float, 1 = half, 2 = bfloat16 (the types of aecct.h)
+constexpr int kNormMaxWidth = 32 * 1024;
+struct RmsQuantCall {
+  int64_t rows;
+  int d, dtype;
+  const void *x, *res;  // res: NULL without a residual
+  int64_t ldx, ldr;     // elements from one row to the next
+  const float *gain;
+  float eps;
+  void *sum;  // [rows][d] x + res; NULL without a residual
+  int8_t *codes;
+  float *scale;
+  void *values;  // or NULL
+};
+struct RmsQuantGradCall {
+  int64_t rows;
+  int d, dtype;
+  const void *dy, *h, *dsum;  // dsum: NULL where nothing else reads the sum
+  int64_t lddy, ldh, ldd;
+  const float *gain;
+  float eps;
+  void *dx;
+  float *dgain;
+  float *partial;  // rms_quant_grad_partials(rows, d) floats
+};
+cudaError_t launch_rms_quant(const RmsQuantCall &c, cudaStream_t stream);
+int64_t rms_quant_grad_partials(int64_t rows, int d);
+cudaError_t launch_rms_quant_grad(const RmsQuantGradCall &c, cudaStream_t stream);
+
+// clip.cu: the global norm over many tensors, and clipping
+constexpr int kClipMaxTensors = 512;  // tensors of a launch (the launcher splits larger calls)
+constexpr int kClipMaxBlocks = 2048;  // partial sums of a launch's CTAs
+int64_t clip_partials(int n_tensors);
+cudaError_t launch_clip_gradients(int n, const void *const *g, const int64_t *len, const int32_t *dtype, void *const *out,
+                                  float max_norm, float eps, float *norm, double *partial, cudaStream_t stream);
+
 // spe.cu: the spectral positional encoding (Sec. 4.3) on the GPU
 constexpr int kSpeMaxHeads = 8;
 constexpr int kSpeMaxTokens = 1024;

@@ -28,6 +28,12 @@ int cuda_fail(cudaError_t e, const char *what) {
   return AECCT_ERR_CUDA;
 }
 
+// the element types of the operators, and a pointer to elements of one
+bool element_type(int32_t dtype) { return dtype >= AECCT_F32 && dtype <= AECCT_BF16; }
+bool is_array(const void *p, int32_t dtype) {
+  return p && (reinterpret_cast<uintptr_t>(p) & (dtype == AECCT_F32 ? 3u : 1u)) == 0;
+}
+
 }  // namespace
 
 struct aecct_handle {
@@ -1250,6 +1256,71 @@ int aecct_aap_ternarize(const float *w_dev, int32_t n_tensors, const int64_t *le
   }
   return aecct_aap_ternarize_list(w.data(), n_tensors, len_host, delta_host, eps, packed_dev, scale_dev, wq_dev,
                                   cuda_stream);
+}
+
+int aecct_rms_quant(const void *x, int64_t ldx, const void *residual, int64_t ldr, const float *gain, int64_t rows,
+                    int32_t d, int32_t dtype, float eps, void *sum, int8_t *codes, float *scale, void *values,
+                    void *cuda_stream) {
+  if (rows < 0 || d < 1 || !element_type(dtype) || !(eps >= 0.0f) || !std::isfinite(eps)) return AECCT_ERR_INVALID_ARG;
+  if (d > kNormMaxWidth) return AECCT_ERR_UNSUPPORTED;
+  if (rows == 0) return AECCT_OK;
+  if (!is_array(x, dtype) || !is_array(gain, AECCT_F32) || !codes || !is_array(scale, AECCT_F32) || ldx < d)
+    return AECCT_ERR_INVALID_ARG;
+  if (residual && (!is_array(residual, dtype) || !is_array(sum, dtype) || ldr < d)) return AECCT_ERR_INVALID_ARG;
+  if (values && !is_array(values, dtype)) return AECCT_ERR_INVALID_ARG;
+  const RmsQuantCall c = {rows, d, dtype, x, residual, ldx, residual ? ldr : 0, gain, eps, residual ? sum : nullptr,
+                          codes, scale, values};
+  const cudaError_t e = launch_rms_quant(c, static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "rms_quant launch");
+}
+
+int aecct_rms_quant_backward_workspace(int64_t rows, int32_t d, int64_t *bytes) {
+  if (!bytes || rows < 0 || d < 1) return AECCT_ERR_INVALID_ARG;
+  if (d > kNormMaxWidth) return AECCT_ERR_UNSUPPORTED;
+  *bytes = rms_quant_grad_partials(rows, d) * static_cast<int64_t>(sizeof(float));
+  return AECCT_OK;
+}
+
+int aecct_rms_quant_backward(const void *dy, int64_t lddy, const void *h, int64_t ldh, const void *dsum, int64_t ldd,
+                             const float *gain, int64_t rows, int32_t d, int32_t dtype, float eps, void *dx,
+                             float *dgain, void *workspace, int64_t workspace_bytes, void *cuda_stream) {
+  if (rows < 0 || d < 1 || !element_type(dtype) || !(eps >= 0.0f) || !std::isfinite(eps)) return AECCT_ERR_INVALID_ARG;
+  if (d > kNormMaxWidth) return AECCT_ERR_UNSUPPORTED;
+  if (!is_array(gain, AECCT_F32) || !is_array(dgain, AECCT_F32)) return AECCT_ERR_INVALID_ARG;
+  if (rows > 0) {
+    if (!is_array(dy, dtype) || !is_array(h, dtype) || !is_array(dx, dtype) || lddy < d || ldh < d) return AECCT_ERR_INVALID_ARG;
+    if (dsum && (!is_array(dsum, dtype) || ldd < d)) return AECCT_ERR_INVALID_ARG;
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 15u) ||
+        workspace_bytes < rms_quant_grad_partials(rows, d) * static_cast<int64_t>(sizeof(float)))
+      return AECCT_ERR_INVALID_ARG;
+  }
+  const RmsQuantGradCall c = {rows, d, dtype, dy, h, dsum, lddy, ldh, dsum ? ldd : 0, gain, eps, dx, dgain,
+                              static_cast<float *>(workspace)};
+  const cudaError_t e = launch_rms_quant_grad(c, static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "rms_quant_backward launch");
+}
+
+int aecct_clip_workspace(int32_t n_tensors, int64_t *bytes) {
+  if (!bytes || n_tensors < 0) return AECCT_ERR_INVALID_ARG;
+  *bytes = clip_partials(n_tensors) * static_cast<int64_t>(sizeof(double));
+  return AECCT_OK;
+}
+
+int aecct_clip_gradients(int32_t n_tensors, const void *const *grad, const int64_t *len, const int32_t *dtype,
+                         void *const *out, float max_norm, float eps, float *norm, void *workspace,
+                         int64_t workspace_bytes, void *cuda_stream) {
+  if (n_tensors < 0 || (n_tensors > 0 && (!grad || !len || !dtype || !out))) return AECCT_ERR_INVALID_ARG;
+  if (!(max_norm > 0.0f) || !std::isfinite(max_norm) || !(eps >= 0.0f) || !std::isfinite(eps)) return AECCT_ERR_INVALID_ARG;
+  if (!is_array(norm, AECCT_F32) || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 7u) ||
+      workspace_bytes < clip_partials(n_tensors) * static_cast<int64_t>(sizeof(double)))
+    return AECCT_ERR_INVALID_ARG;
+  for (int j = 0; j < n_tensors; ++j) {
+    if (len[j] < 0 || !element_type(dtype[j])) return AECCT_ERR_INVALID_ARG;
+    if (len[j] > 0 && (!is_array(grad[j], dtype[j]) || !is_array(out[j], dtype[j]))) return AECCT_ERR_INVALID_ARG;
+  }
+  const cudaError_t e = launch_clip_gradients(n_tensors, grad, len, dtype, out, max_norm, eps, norm,
+                                              static_cast<double *>(workspace), static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "clip_gradients launch");
 }
 
 int aecct_selftest_fma_rate(int32_t paired, double *fma_per_s) {
