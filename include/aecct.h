@@ -285,6 +285,37 @@ int aecct_rms_quant_backward(const void *dy, int64_t lddy, const void *h, int64_
                              const float *gain, int64_t rows, int32_t d, int32_t dtype, float eps, void *dx,
                              float *dgain, void *workspace, int64_t workspace_bytes, void *cuda_stream);
 
+/* The AAP linear layer (eq. AAPLinear) on the codes of aecct_rms_quant (or any int8 rows with a scale) and
+ * the 2-bit weights of aecct_aap_ternarize:
+ *   y[m][n] = scale[m] w_scale sum_k codes[m][k] T[n][k] + bias[n].
+ * The sum is one of integers and exact; it is multiplied by scale[m] w_scale, and bias added, in 32 bits.
+ *   codes    int8 [M][K], ldc apart;  scale  fp32 [M].
+ *   packed   [N][K / 4] bytes, the 2-bit format of w_packed above (K a multiple of 4; the invalid code 10 counts as 0).
+ *   w_scale  DEVICE fp32 scalar (gamma delta);  bias  fp32 [N] or NULL.
+ *   y        [M][N] of dtype.
+ *   workspace  aecct_aap_linear_workspace bytes, 16-byte aligned (NULL where that is 0).
+ * M == 0 or N == 0 is a no-op.  Errors: INVALID_ARG (a size < 0, K < 4 or not a multiple of 4, ldc < K, a
+ * dtype not named above, a NULL or misaligned pointer, a workspace that is too small), UNSUPPORTED (K > 65536, N or
+ * M >= 2^31), CUDA. */
+int aecct_aap_linear_workspace(int64_t M, int64_t K, int64_t N, int64_t *bytes);
+int aecct_aap_linear(const int8_t *codes, int64_t ldc, const float *scale, const uint8_t *packed, const float *w_scale,
+                     const float *bias, int64_t M, int64_t K, int64_t N, int32_t dtype, void *y, void *workspace,
+                     int64_t workspace_bytes, void *cuda_stream);
+
+/* Its gradients; that of the weights is passed straight through Ternary:
+ *   dx[m][k] = w_scale sum_n dy[m][n] T[n][k]             (the gradient of codes[m][k] scale[m])
+ *   dw[n][k] = sum_m dy[m][n] scale[m] codes[m][k]        (the gradient of w_scale T[n][k], and so of W)
+ *   db[n]    = sum_m dy[m][n].
+ *   dy  [M][N] of dtype, lddy apart;  dx  [M][K] of dtype;  dw  [N][K] of wdtype;  db  fp32 [N].
+ * dx, dw and db may be NULL where they are not wanted.  Products are of dy's own values with the integers;
+ * dy scale[m] is rounded to 8 bits for a dw in AECCT_BF16, to 16 for one in AECCT_F16 and to 24 for one in
+ * AECCT_F32.  Sums are in 32 bits.  M == 0 makes dw and db zero.  Errors: as above. */
+int aecct_aap_linear_backward_workspace(int64_t M, int64_t K, int64_t N, int32_t dtype, int32_t wdtype, int64_t *bytes);
+int aecct_aap_linear_backward(const void *dy, int64_t lddy, const int8_t *codes, int64_t ldc, const float *scale,
+                              const uint8_t *packed, const float *w_scale, int64_t M, int64_t K, int64_t N,
+                              int32_t dtype, int32_t wdtype, void *dx, void *dw, float *db, void *workspace,
+                              int64_t workspace_bytes, void *cuda_stream);
+
 /* The global norm over many gradients, and the gradients scaled down to it:
  *   norm = sqrt(sum over tensors and elements of g^2); out = g min(1, max_norm / (norm + eps)).
  *   grad, out    HOST arrays of n_tensors DEVICE pointers; out[j] may be grad[j] (in place: not written

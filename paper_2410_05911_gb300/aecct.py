@@ -28,6 +28,8 @@ EXPORTED_SYMBOLS = (
     "aecct_selftest_timeout", "aecct_decode_host_noalloc", "aecct_selftest_fma_rate", "aecct_aap_ternarize",
     "aecct_aap_ternarize_list", "aecct_spe_table", "aecct_rms_quant", "aecct_rms_quant_backward",
     "aecct_rms_quant_backward_workspace", "aecct_clip_gradients", "aecct_clip_workspace",
+    "aecct_aap_linear", "aecct_aap_linear_workspace", "aecct_aap_linear_backward",
+    "aecct_aap_linear_backward_workspace",
 )
 
 
@@ -93,6 +95,10 @@ def load(build_if_missing: bool = True):
     L.aecct_rms_quant.argtypes = [P, I64, P, I64, P, I64, I32, I32, F32, P, P, P, P, P]
     L.aecct_rms_quant_backward.argtypes = [P, I64, P, I64, P, I64, P, I64, I32, I32, F32, P, P, P, I64, P]
     L.aecct_rms_quant_backward_workspace.argtypes = [I64, I32, ctypes.POINTER(I64)]
+    L.aecct_aap_linear_workspace.argtypes = [I64, I64, I64, ctypes.POINTER(I64)]
+    L.aecct_aap_linear.argtypes = [P, I64, P, P, P, P, I64, I64, I64, I32, P, P, I64, P]
+    L.aecct_aap_linear_backward_workspace.argtypes = [I64, I64, I64, I32, I32, ctypes.POINTER(I64)]
+    L.aecct_aap_linear_backward.argtypes = [P, I64, P, I64, P, P, P, I64, I64, I64, I32, I32, P, P, P, P, I64, P]
     L.aecct_clip_gradients.argtypes = [I32, P, P, P, P, F32, F32, P, P, I64, P]
     L.aecct_clip_workspace.argtypes = [I32, ctypes.POINTER(I64)]
     for name in EXPORTED_SYMBOLS:
@@ -510,6 +516,90 @@ def rms_quant_backward(dy, total, gain, dtotal=None, eps: float = 1e-6, stream=N
                                     work.data_ptr(), size.value, s.cuda_stream)
     _check(st, "aecct_rms_quant_backward")
     return dx, dgain
+
+
+def _check_linear(codes, scale, packed, w_scale):
+    """(tokens, K, N) of an AAP linear layer's operands."""
+    import torch
+
+    dev = codes.device
+    if not codes.is_cuda or codes.dtype != torch.int8 or codes.dim() < 1:
+        raise ValueError("codes must be an int8 CUDA tensor of rows")
+    K = codes.shape[-1]
+    if scale.device != dev or scale.dtype != torch.float32 or scale.shape != codes.shape[:-1]:
+        raise ValueError(f"scale must be a float32 tensor of shape {tuple(codes.shape[:-1])} on {dev}")
+    if packed.device != dev or packed.dtype != torch.uint8 or not packed.is_contiguous():
+        raise ValueError(f"packed must be a contiguous uint8 tensor on {dev}")
+    if K < 4 or K % 4 or packed.numel() % (K // 4):
+        raise ValueError(f"rows of {K} codes do not divide weights of {4 * packed.numel()}: K is a multiple of 4")
+    if w_scale.device != dev or w_scale.dtype != torch.float32 or w_scale.numel() != 1:
+        raise ValueError(f"w_scale must be a float32 tensor of one element on {dev}")
+    return scale.numel(), K, packed.numel() // (K // 4)
+
+
+def aap_linear(codes, scale, packed, w_scale, bias=None, dtype=None, stream=None):
+    """aecct_aap_linear: scale * w_scale * (codes @ T^T) + bias for int8 rows `codes` [..., K] with one float32
+    scale each (those of rms_quant), and the 2-bit ternary weights T [N, K] of aap_ternarize: packed uint8
+    (N * K / 4 bytes) and their scale, a float32 tensor of one element.  bias is float32 [N] or None.  Returns
+    y [..., N] of `dtype` (float32 unless given)."""
+    import torch
+
+    M, K, N = _check_linear(codes, scale, packed, w_scale)
+    dtype = torch.float32 if dtype is None else dtype
+    if _element(dtype) is None:
+        raise ValueError("dtype must be float32, float16 or bfloat16")
+    dev = codes.device
+    if bias is not None:
+        if bias.device != dev or bias.dtype != torch.float32 or bias.shape != (N,):
+            raise ValueError(f"bias must be a float32 tensor of shape ({N},) on {dev}")
+        bias = bias.contiguous()
+    q, ldc = _rows(codes)
+    scale = scale.contiguous()
+    L = load()
+    size = ctypes.c_int64()
+    _check(L.aecct_aap_linear_workspace(M, K, N, ctypes.byref(size)), "aecct_aap_linear")
+    y = torch.empty(codes.shape[:-1] + (N,), dtype=dtype, device=dev)
+    work = torch.empty(size.value, dtype=torch.uint8, device=dev) if size.value else None
+    s = _stream_of(stream, dev, (q, scale, packed, w_scale, bias, y, work))
+    st = L.aecct_aap_linear(q.data_ptr(), ldc, scale.data_ptr(), packed.data_ptr(), w_scale.data_ptr(),
+                            bias.data_ptr() if bias is not None else None, M, K, N, _element(dtype), y.data_ptr(),
+                            work.data_ptr() if work is not None else None, size.value, s.cuda_stream)
+    _check(st, "aecct_aap_linear")
+    return y
+
+
+def aap_linear_backward(dy, codes, scale, packed, w_scale, weight_dtype=None, want=(True, True, True), stream=None):
+    """aecct_aap_linear_backward: the gradients of aap_linear for dy [..., N] (float32, float16 or bfloat16).  Returns
+    (dx, dw, db), None where `want` says that one is not wanted: dx [..., K] in dy's type is the gradient of
+    codes * scale (rms_quant_backward takes it), dw [N, K] in weight_dtype (float32 unless given) that of the
+    weights behind aap_ternarize, passed straight through, db [N] float32 that of the bias."""
+    import torch
+
+    M, K, N = _check_linear(codes, scale, packed, w_scale)
+    weight_dtype = torch.float32 if weight_dtype is None else weight_dtype
+    dev = codes.device
+    if _element(weight_dtype) is None:
+        raise ValueError("weight_dtype must be float32, float16 or bfloat16")
+    if dy.device != dev or _element(dy.dtype) is None or dy.shape != codes.shape[:-1] + (N,):
+        raise ValueError(f"dy must be a float32, float16 or bfloat16 tensor of shape {tuple(codes.shape[:-1]) + (N,)} on {dev}")
+    g, lddy = _rows(dy)
+    q, ldc = _rows(codes)
+    scale = scale.contiguous()
+    L = load()
+    size = ctypes.c_int64()
+    kinds = _element(dy.dtype), _element(weight_dtype)
+    _check(L.aecct_aap_linear_backward_workspace(M, K, N, *kinds, ctypes.byref(size)), "aecct_aap_linear_backward")
+    dx = torch.empty(codes.shape, dtype=dy.dtype, device=dev) if want[0] else None
+    dw = torch.empty((N, K), dtype=weight_dtype, device=dev) if want[1] else None
+    db = torch.empty(N, dtype=torch.float32, device=dev) if want[2] else None
+    work = torch.empty(size.value, dtype=torch.uint8, device=dev) if size.value else None
+    s = _stream_of(stream, dev, (g, q, scale, packed, w_scale, dx, dw, db, work))
+    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
+    st = L.aecct_aap_linear_backward(g.data_ptr(), lddy, q.data_ptr(), ldc, scale.data_ptr(), packed.data_ptr(),
+                                     w_scale.data_ptr(), M, K, N, *kinds, ptr(dx), ptr(dw), ptr(db), ptr(work), size.value,
+                                     s.cuda_stream)
+    _check(st, "aecct_aap_linear_backward")
+    return dx, dw, db
 
 
 def clip_gradients(grads, max_norm: float, eps: float = 1e-6, out=None, stream=None):

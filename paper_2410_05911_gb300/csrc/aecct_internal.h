@@ -312,6 +312,41 @@ cudaError_t launch_rms_quant(const RmsQuantCall &c, cudaStream_t stream);
 int64_t rms_quant_grad_partials(int64_t rows, int d);
 cudaError_t launch_rms_quant_grad(const RmsQuantGradCall &c, cudaStream_t stream);
 
+// linear.cu: the AAP linear layer on int8 codes and 2-bit weights, and its gradients
+constexpr int64_t kLinearMaxRows = int64_t(1) << 31;  // tokens; widths are 32-bit, K at most 65536
+constexpr int kLinearMaxK = 65536;                    // |sum of codes| <= 127 K < 2^24: exact in 32 bits
+struct AapLinearCall {
+  int64_t M, K, N;
+  int dtype;
+  const int8_t *codes;  // [M][K], ldc apart
+  int64_t ldc;
+  const float *scale;     // [M]
+  const uint8_t *packed;  // [N][K / 4]
+  const float *w_scale;   // scalar
+  const float *bias;      // [N] or NULL
+  void *y;                // [M][N]
+  void *workspace;        // aap_linear_workspace bytes
+};
+struct AapLinearGradCall {
+  int64_t M, K, N;
+  int dtype, wdtype;
+  const void *dy;  // [M][N], lddy apart
+  int64_t lddy;
+  const int8_t *codes;
+  int64_t ldc;
+  const float *scale;
+  const uint8_t *packed;
+  const float *w_scale;
+  void *dx;  // [M][K] or NULL
+  void *dw;  // [N][K] of wdtype, or NULL
+  float *db;  // [N] or NULL
+  void *workspace;
+};
+int64_t aap_linear_workspace(int64_t M, int64_t K, int64_t N);
+cudaError_t launch_aap_linear(const AapLinearCall &c, cudaStream_t stream);
+int64_t aap_linear_grad_workspace(int64_t M, int64_t K, int64_t N, int dtype, int wdtype);
+cudaError_t launch_aap_linear_grad(const AapLinearGradCall &c, cudaStream_t stream);
+
 // clip.cu: the global norm over many tensors, and clipping
 constexpr int kClipMaxTensors = 512;  // tensors of a launch (the launcher splits larger calls)
 constexpr int kClipMaxBlocks = 2048;  // partial sums of a launch's CTAs

@@ -34,6 +34,15 @@ bool is_array(const void *p, int32_t dtype) {
   return p && (reinterpret_cast<uintptr_t>(p) & (dtype == AECCT_F32 ? 3u : 1u)) == 0;
 }
 
+bool is_workspace(const void *p, int64_t bytes, int64_t need) {
+  return need == 0 || (p && (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && bytes >= need);
+}
+// the sizes of an AAP linear layer: M tokens, K inputs, N outputs
+int linear_sizes(int64_t M, int64_t K, int64_t N) {
+  if (M < 0 || N < 0 || K < 4 || K % 4 != 0) return AECCT_ERR_INVALID_ARG;
+  return K > kLinearMaxK || M >= kLinearMaxRows || N >= kLinearMaxRows ? AECCT_ERR_UNSUPPORTED : AECCT_OK;
+}
+
 }  // namespace
 
 struct aecct_handle {
@@ -1298,6 +1307,63 @@ int aecct_rms_quant_backward(const void *dy, int64_t lddy, const void *h, int64_
                               static_cast<float *>(workspace)};
   const cudaError_t e = launch_rms_quant_grad(c, static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "rms_quant_backward launch");
+}
+
+int aecct_aap_linear_workspace(int64_t M, int64_t K, int64_t N, int64_t *bytes) {
+  const int st = linear_sizes(M, K, N);
+  if (st != AECCT_OK || !bytes) return st != AECCT_OK ? st : AECCT_ERR_INVALID_ARG;
+  *bytes = M > 0 && N > 0 ? aap_linear_workspace(M, K, N) : 0;
+  return AECCT_OK;
+}
+
+int aecct_aap_linear(const int8_t *codes, int64_t ldc, const float *scale, const uint8_t *packed, const float *w_scale,
+                     const float *bias, int64_t M, int64_t K, int64_t N, int32_t dtype, void *y, void *workspace,
+                     int64_t workspace_bytes, void *cuda_stream) {
+  const int sizes = linear_sizes(M, K, N);
+  if (sizes != AECCT_OK) return sizes;
+  if (!element_type(dtype)) return AECCT_ERR_INVALID_ARG;
+  if (M == 0 || N == 0) return AECCT_OK;
+  if (!codes || ldc < K || !is_array(scale, AECCT_F32) || !packed || !is_array(w_scale, AECCT_F32) || !is_array(y, dtype))
+    return AECCT_ERR_INVALID_ARG;
+  if (bias && !is_array(bias, AECCT_F32)) return AECCT_ERR_INVALID_ARG;
+  if (!is_workspace(workspace, workspace_bytes, aap_linear_workspace(M, K, N))) return AECCT_ERR_INVALID_ARG;
+  const AapLinearCall c = {M, K, N, dtype, codes, ldc, scale, packed, w_scale, bias, y, workspace};
+  const cudaError_t e = launch_aap_linear(c, static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "aap_linear launch");
+}
+
+int aecct_aap_linear_backward_workspace(int64_t M, int64_t K, int64_t N, int32_t dtype, int32_t wdtype, int64_t *bytes) {
+  const int st = linear_sizes(M, K, N);
+  if (st != AECCT_OK || !bytes) return st != AECCT_OK ? st : AECCT_ERR_INVALID_ARG;
+  if (!element_type(dtype) || !element_type(wdtype)) return AECCT_ERR_INVALID_ARG;
+  *bytes = N > 0 ? aap_linear_grad_workspace(M, K, N, dtype, wdtype) : 0;
+  return AECCT_OK;
+}
+
+int aecct_aap_linear_backward(const void *dy, int64_t lddy, const int8_t *codes, int64_t ldc, const float *scale,
+                              const uint8_t *packed, const float *w_scale, int64_t M, int64_t K, int64_t N,
+                              int32_t dtype, int32_t wdtype, void *dx, void *dw, float *db, void *workspace,
+                              int64_t workspace_bytes, void *cuda_stream) {
+  const int sizes = linear_sizes(M, K, N);
+  if (sizes != AECCT_OK) return sizes;
+  if (!element_type(dtype) || !element_type(wdtype)) return AECCT_ERR_INVALID_ARG;
+  if (M > 0 && N > 0 && (!is_array(dy, dtype) || lddy < N)) return AECCT_ERR_INVALID_ARG;
+  if (M == 0) dx = nullptr;
+  if (N == 0) dw = nullptr, db = nullptr;
+  if (dx && (!is_array(dx, dtype) || (N > 0 && (!packed || !is_array(w_scale, AECCT_F32))))) return AECCT_ERR_INVALID_ARG;
+  if (dw && (!is_array(dw, wdtype) || (M > 0 && (!codes || ldc < K || !is_array(scale, AECCT_F32))))) return AECCT_ERR_INVALID_ARG;
+  if (db && !is_array(db, AECCT_F32)) return AECCT_ERR_INVALID_ARG;
+  if (!is_workspace(workspace, workspace_bytes, N > 0 ? aap_linear_grad_workspace(M, K, N, dtype, wdtype) : 0))
+    return AECCT_ERR_INVALID_ARG;
+  const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
+  if (N == 0) {  // an empty sum
+    if (!dx) return AECCT_OK;
+    const cudaError_t e = cudaMemsetAsync(dx, 0, static_cast<size_t>(M) * K * (dtype == AECCT_F32 ? 4 : 2), stream);
+    return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "aap_linear_backward memset");
+  }
+  const AapLinearGradCall c = {M, K, N, dtype, wdtype, dy, lddy, codes, ldc, scale, packed, w_scale, dx, dw, db, workspace};
+  const cudaError_t e = launch_aap_linear_grad(c, stream);
+  return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "aap_linear_backward launch");
 }
 
 int aecct_clip_workspace(int32_t n_tensors, int64_t *bytes) {
