@@ -282,6 +282,8 @@ cudaError_t launch_aap_ternarize(const float *const *w, int n, const int64_t *le
 cudaError_t launch_unpack_weights(const uint8_t *packed, int n_layers, int D, const ChunkDesc *chunks, int n_chunks,
                                   uint32_t layer_bytes, uint8_t *wstream, cudaStream_t stream);
 
+int sm_count();  // SMs of the current device (norm.cu)
+
 // norm.cu: root-mean-square norm with the residual's addition and eq. Quant, and its gradients.
 // dtype: 0 = float, 1 = half, 2 = bfloat16 (the types of aecct.h)
 constexpr int kNormMaxWidth = 32 * 1024;
@@ -344,6 +346,9 @@ struct AapLinearGradCall {
 };
 int64_t aap_linear_workspace(int64_t M, int64_t K, int64_t N);
 cudaError_t launch_aap_linear(const AapLinearCall &c, cudaStream_t stream);
+int *linear_status();  // host memory: 1 once a wait in a kernel of these has given up; NULL without memory
+int64_t weight_grad_workspace(int64_t M, int64_t K, int64_t N, int wdtype);  // floats
+cudaError_t launch_weight_grad(const AapLinearGradCall &c, float *work, cudaStream_t stream);
 int64_t aap_linear_grad_workspace(int64_t M, int64_t K, int64_t N, int dtype, int wdtype);
 cudaError_t launch_aap_linear_grad(const AapLinearGradCall &c, cudaStream_t stream);
 

@@ -37,6 +37,15 @@ bool is_array(const void *p, int32_t dtype) {
 bool is_workspace(const void *p, int64_t bytes, int64_t need) {
   return need == 0 || (p && (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && bytes >= need);
 }
+// a wait that gave up in a kernel of an earlier call, reported once
+int linear_gave_up() {
+  int *word = linear_status();
+  if (!word) return AECCT_ERR_OUT_OF_MEMORY;
+  if (*static_cast<volatile int *>(word) == 0) return AECCT_OK;
+  *static_cast<volatile int *>(word) = 0;
+  g_last_error = "aap_linear: a device-side wait of an earlier call exceeded its limit";
+  return AECCT_ERR_TIMEOUT;
+}
 // the sizes of an AAP linear layer: M tokens, K inputs, N outputs
 int linear_sizes(int64_t M, int64_t K, int64_t N) {
   if (M < 0 || N < 0 || K < 4 || K % 4 != 0) return AECCT_ERR_INVALID_ARG;
@@ -1327,6 +1336,8 @@ int aecct_aap_linear(const int8_t *codes, int64_t ldc, const float *scale, const
     return AECCT_ERR_INVALID_ARG;
   if (bias && !is_array(bias, AECCT_F32)) return AECCT_ERR_INVALID_ARG;
   if (!is_workspace(workspace, workspace_bytes, aap_linear_workspace(M, K, N))) return AECCT_ERR_INVALID_ARG;
+  const int earlier = linear_gave_up();
+  if (earlier != AECCT_OK) return earlier;
   const AapLinearCall c = {M, K, N, dtype, codes, ldc, scale, packed, w_scale, bias, y, workspace};
   const cudaError_t e = launch_aap_linear(c, static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "aap_linear launch");
@@ -1336,7 +1347,7 @@ int aecct_aap_linear_backward_workspace(int64_t M, int64_t K, int64_t N, int32_t
   const int st = linear_sizes(M, K, N);
   if (st != AECCT_OK || !bytes) return st != AECCT_OK ? st : AECCT_ERR_INVALID_ARG;
   if (!element_type(dtype) || !element_type(wdtype)) return AECCT_ERR_INVALID_ARG;
-  *bytes = N > 0 ? aap_linear_grad_workspace(M, K, N, dtype, wdtype) : 0;
+  *bytes = M > 0 && N > 0 ? aap_linear_grad_workspace(M, K, N, dtype, wdtype) : 0;
   return AECCT_OK;
 }
 
@@ -1353,14 +1364,18 @@ int aecct_aap_linear_backward(const void *dy, int64_t lddy, const int8_t *codes,
   if (dx && (!is_array(dx, dtype) || (N > 0 && (!packed || !is_array(w_scale, AECCT_F32))))) return AECCT_ERR_INVALID_ARG;
   if (dw && (!is_array(dw, wdtype) || (M > 0 && (!codes || ldc < K || !is_array(scale, AECCT_F32))))) return AECCT_ERR_INVALID_ARG;
   if (db && !is_array(db, AECCT_F32)) return AECCT_ERR_INVALID_ARG;
-  if (!is_workspace(workspace, workspace_bytes, N > 0 ? aap_linear_grad_workspace(M, K, N, dtype, wdtype) : 0))
+  if (!is_workspace(workspace, workspace_bytes, M > 0 && N > 0 ? aap_linear_grad_workspace(M, K, N, dtype, wdtype) : 0))
     return AECCT_ERR_INVALID_ARG;
   const cudaStream_t stream = static_cast<cudaStream_t>(cuda_stream);
-  if (N == 0) {  // an empty sum
-    if (!dx) return AECCT_OK;
-    const cudaError_t e = cudaMemsetAsync(dx, 0, static_cast<size_t>(M) * K * (dtype == AECCT_F32 ? 4 : 2), stream);
+  if (M == 0 || N == 0) {  // empty sums
+    cudaError_t e = cudaSuccess;
+    if (dx) e = cudaMemsetAsync(dx, 0, static_cast<size_t>(M) * K * (dtype == AECCT_F32 ? 4 : 2), stream);
+    if (e == cudaSuccess && dw) e = cudaMemsetAsync(dw, 0, static_cast<size_t>(N) * K * (wdtype == AECCT_F32 ? 4 : 2), stream);
+    if (e == cudaSuccess && db) e = cudaMemsetAsync(db, 0, static_cast<size_t>(N) * sizeof(float), stream);
     return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "aap_linear_backward memset");
   }
+  const int earlier = linear_gave_up();
+  if (earlier != AECCT_OK) return earlier;
   const AapLinearGradCall c = {M, K, N, dtype, wdtype, dy, lddy, codes, ldc, scale, packed, w_scale, dx, dw, db, workspace};
   const cudaError_t e = launch_aap_linear_grad(c, stream);
   return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "aap_linear_backward launch");

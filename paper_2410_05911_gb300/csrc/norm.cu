@@ -14,6 +14,7 @@
 // and dx = dres = dh.  Squares, products and sums are in 32 bits.
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cstdint>
 
 #include "aecct_internal.h"
@@ -282,12 +283,6 @@ int row_threads(int d, int E) {
   return G * E >= d ? G : 32 * ((d + 32 * E - 1) / (32 * E));
 }
 
-int sm_count() {
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 1;
-  return n;
-}
-
 template <typename T, int V, int E>
 cudaError_t launch_quant(QuantArgs<T> a, cudaStream_t st) {
   a.s.G = row_threads(a.s.d, E);
@@ -358,6 +353,16 @@ cudaError_t grad_of(const RmsQuantGradCall &c, cudaStream_t st) {
 }
 
 }  // namespace
+
+int sm_count() {
+  static std::atomic<int> known[64];  // by device
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev < 0 || dev >= 64) return 1;
+  if ((n = known[dev].load(std::memory_order_relaxed)) > 0) return n;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 1;
+  known[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
 
 cudaError_t launch_rms_quant(const RmsQuantCall &c, cudaStream_t st) {
   return c.dtype == 0 ? quant_of<float>(c, st) : c.dtype == 1 ? quant_of<__half>(c, st) : quant_of<__nv_bfloat16>(c, st);
