@@ -20,33 +20,34 @@ namespace aecct {
 
 namespace {
 
-// rows of the tile along the tokens: no more than there are, in steps of what the kernel is built for
+// the tile: few tokens take a narrow one, whose rest would be converted zeros
 template <class F>
-auto with_tile(int64_t M, const F &f) {
-  if (M <= 16) return f(std::integral_constant<int, 16>());
-  if (M <= 64) return f(std::integral_constant<int, 64>());
-  return f(std::integral_constant<int, 256>());
+auto with_forward_tile(int64_t M, int64_t N, const F &f) {
+  if (M <= 16) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
+  if (M > 64 && M <= 128) return f(std::integral_constant<int, 128>(), std::integral_constant<int, 1>());
+  return with_tile<256>(N, M, f);
 }
 
 }  // namespace
 
 int64_t aap_linear_workspace(int64_t M, int64_t K, int64_t N) {
   const int sms = sm_count();
-  return with_tile(M, [&](auto tb) {
-    const GemmPlan p = gemm_plan<decltype(tb)::value, 1>(N, M, K, sms);
+  return with_forward_tile(M, N, [&](auto tb, auto cg) {
+    constexpr int TB = decltype(tb)::value, CG = decltype(cg)::value;
+    const GemmPlan p = gemm_plan<WeightsK, CodesK<TB / CG>, TB, CG>(N, M, K, sms);
     return p.splits > 1 ? p.splits * M * N * static_cast<int64_t>(sizeof(float)) : int64_t(0);
   });
 }
 
 cudaError_t launch_aap_linear(const AapLinearCall &c, cudaStream_t st) {
-  const bool vec = c.K % 32 == 0 && (reinterpret_cast<uintptr_t>(c.packed) & 7u) == 0;
-  const WeightsK a = {c.packed, c.N, c.K, vec};
+  const WeightsK a = {c.packed, c.N, c.K, weights_unit(c.packed, c.K)};
   const OutY out = {c.y, c.dtype, c.N, c.scale, c.w_scale, c.bias};
-  return with_tile(c.M, [&](auto tb) {
-    constexpr int TB = decltype(tb)::value;
-    const CodesK<TB> b = {c.codes, c.M, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
-    return launch_gemm<WeightsK, CodesK<TB>, OutY, TB>(c.N, c.M, c.K, a, b, out, static_cast<float *>(c.workspace), sm_count(),
-                                                       linear_status(), st);
+  return with_forward_tile(c.M, c.N, [&](auto tb, auto cg) {
+    constexpr int TB = decltype(tb)::value, CG = decltype(cg)::value;
+    using B = CodesK<TB / CG>;
+    const B b = {c.codes, c.M, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
+    return launch_gemm<WeightsK, B, OutY, TB, CG>(c.N, c.M, c.K, a, b, out, static_cast<float *>(c.workspace), sm_count(),
+                                                  linear_status(), st);
   });
 }
 

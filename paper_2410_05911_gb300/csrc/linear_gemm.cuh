@@ -8,16 +8,19 @@
 // a quarter of one a weight keeps L2 traffic under what 16-bit operands would need, and no pass over memory
 // lays operands out before the product.
 //
-// One CTA makes a tile of 128 i by TB j.  Eight producer warps load kStep = 64 of r a step ahead, convert and
-// store; a ninth warp issues the MMAs.  Lanes hold consecutive i in tensor memory, so that the epilogue's
-// stores of one j are 32 neighbouring elements.  Two CTAs share an SM where their operands fit, one's
-// epilogue behind the other's products.
+// A CTA makes a tile of 128 i by TB j; from 256 of both on, a cluster of two makes 256 by 256 (cta_group::2),
+// each CTA with its own 128 rows of A and half of B in shared memory, so that a B is converted and stored by one
+// of two SMs.  Eight producer warps load a step ahead, convert and store; a ninth warp (of the first
+// CTA) issues the MMAs.  Lanes hold consecutive i in tensor memory, so that the epilogue's stores of one j are 32
+// neighbouring elements.  Two CTAs share an SM where their operands fit, one's epilogue behind the other's
+// products.
 //
-// Operand tiles are 8 x 16-byte core matrices without swizzle: element (x, r) of a K-major tile (16 bytes
-// along r) at (x / 8) 1024 + (r / 8) 128 + (x % 8) 16 + (r % 8) 2, of an MN-major tile (16 bytes along x) at
-// (x / 8) 1024 + (r / 8) 128 + (r % 8) 16 + (x % 8) 2.  In both, core matrices along r are 128 bytes
-// apart and those along x 1024, and eight lanes that hold eight consecutive rows of the source store
-// 128 consecutive bytes.
+// Operand tiles are 8 x 16-byte core matrices without swizzle.  Element (x, r) of a K-major tile (16 bytes
+// along r) is at (x / 8) 1152 + (r / 8) 144 + (x % 8) 16 + (r % 8) 2, of an MN-major tile (16 bytes along x)
+// at (x / 8) 1040 + (r / 8) 128 + (r % 8) 16 + (x % 8) 2.  The 16 bytes of padding between core matrices along
+// the source's contiguous dimension let eight lanes read one 128-byte line of a row and store their eight
+// pieces to eight different bank groups.  (Eight lanes on eight rows store without padding, but their loads take
+// a wavefront per row: 1,330 a step of 256 rows, where the tensor cores need 512 cycles.)
 #pragma once
 #include <cuda_runtime.h>
 
@@ -34,14 +37,17 @@ constexpr int kTileI = 128;         // i per CTA: the lanes of tensor memory
 constexpr int kProducerWarps = 8;
 constexpr int kProducers = kProducerWarps * 32;
 constexpr int kGemmThreads = kProducers + 32;
-constexpr uint32_t kTileABytes = kTileI * kStep * 2;
+// a tile of x rows, and its descriptor's strides
+__host__ __device__ constexpr uint32_t tile_bytes(bool mn, int x) { return x / 8 * (mn ? 1040u : 1152u); }
+__host__ __device__ constexpr uint32_t tile_lbo(bool mn) { return mn ? 128u : 144u; }
+__host__ __device__ constexpr uint32_t tile_sbo(bool mn) { return mn ? 1040u : 1152u; }
 constexpr long long kGemmWaitCycles = 1ll << 32;  // a wait that takes longer (about 2 s) has lost its arrival
 
 // instruction descriptor of kind::f16: 32-bit accumulators; BF: bfloat16 operands, else half; MN: both
 // operands' 16-byte rows run along i and j
-__host__ __device__ constexpr uint32_t gemm_idesc(bool bf, bool mn_a, bool mn_b, uint32_t n) {
+__host__ __device__ constexpr uint32_t gemm_idesc(bool bf, bool mn_a, bool mn_b, uint32_t m, uint32_t n) {
   return (1u << 4) | (bf ? (1u << 7) | (1u << 10) : 0u) | (mn_a ? 1u << 15 : 0u) | (mn_b ? 1u << 16 : 0u) | ((n >> 3) << 17) |
-         ((128u >> 4) << 24);
+         ((m >> 4) << 24);
 }
 
 __device__ __forceinline__ void st_shared16(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
@@ -49,31 +55,30 @@ __device__ __forceinline__ void st_shared16(uint32_t addr, uint32_t a, uint32_t 
 }
 
 // ----------------------------------------------------------------------------- conversions
-// 16 weights of 2 bits (00 = 0, 01 = +1, 11 = -1) as 16-bit floats of twice their value, 0 and +-2: their
-// low bytes are zero in half and in bfloat16 alike, so that one byte permutation makes two of them, with
-// the codes as selectors into a table of high bytes.  Position 4 p + b of the 16 holds weight 4 b + p
-// (field p of byte b); mix16 is that order.
-__host__ __device__ constexpr int mix16(int pos) { return ((pos & 3) << 2) | (pos >> 2); }
-__device__ __forceinline__ void weights16(uint32_t w, uint32_t (&o)[8]) {
+// 2-bit weights (00 = 0, 01 = +1, 11 = -1) as 16-bit floats of twice their value, 0 and +-2: their low bytes
+// are zero in half and in bfloat16 alike, so that one byte permutation makes two of them, with the codes as
+// selectors into a table of high bytes.  The two come from one field of neighbouring bytes, so position
+// 2 p + h of 8 weights holds weight 4 h + p; mix8 is that order.
+__host__ __device__ constexpr int mix8(int pos) { return ((pos & 1) << 2) | (pos >> 1); }
+// weights 0 .. 7 (the low half) or 8 .. 15 of a word
+__device__ __forceinline__ void weights8(uint32_t w, bool high, uint32_t (&o)[4]) {
   constexpr uint32_t table = 0xC0004000u;
 #pragma unroll
   for (int p = 0; p < 4; ++p) {
-    const uint32_t s = (p < 2 ? w << (4 - 2 * p) : w >> (2 * p - 4)) & 0x30303030u;
-    o[2 * p] = __byte_perm(table, 0, s & 0xFFFFu);
-    o[2 * p + 1] = __byte_perm(table, 0, s >> 16);
+    const int by = (high ? 16 : 0) + 2 * p - 4;  // to selector bits 4, 5 and 12, 13
+    const uint32_t s = (by < 0 ? w << -by : w >> by) & 0x3030u;
+    o[p] = __byte_perm(table, 0, s);
   }
 }
-// 16 int8 codes as halves in the order of mix16: (code + 128) in the low byte of 1024, less 1152
-__device__ __forceinline__ void codes16_half_mixed(const uint32_t (&b)[4], uint32_t (&o)[8]) {
+// 8 int8 codes as halves in the order of mix8: (code + 128) in the low byte of 1024, less 1152
+__device__ __forceinline__ void codes8_half_mixed(uint32_t b0, uint32_t b1, uint32_t (&o)[4]) {
 #pragma unroll
-  for (int p = 0; p < 4; ++p)
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const uint32_t t = __byte_perm(b[2 * h], b[2 * h + 1], 0x0400u + 0x0101u * p);
-      const uint32_t u = (t & 0x00FF00FFu) ^ 0x64806480u;
-      const __half2 v = __hsub2(*reinterpret_cast<const __half2 *>(&u), __half2{__ushort_as_half(0x6480), __ushort_as_half(0x6480)});
-      o[2 * p + h] = *reinterpret_cast<const uint32_t *>(&v);
-    }
+  for (int p = 0; p < 4; ++p) {
+    const uint32_t t = __byte_perm(b0, b1, 0x0400u + 0x0101u * p);
+    const uint32_t u = (t & 0x00FF00FFu) ^ 0x64806480u;
+    const __half2 v = __hsub2(*reinterpret_cast<const __half2 *>(&u), __half2{__ushort_as_half(0x6480), __ushort_as_half(0x6480)});
+    o[p] = *reinterpret_cast<const uint32_t *>(&v);
+  }
 }
 // 4 int8 codes as bfloat16, in order: the low 7 bits in the mantissa of 128, less 128, or 256 for a negative one
 __device__ __forceinline__ void codes4_bf16(uint32_t b, uint32_t &o0, uint32_t &o1) {
@@ -113,17 +118,39 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint32_t addr, uint3
 }
 
 // ----------------------------------------------------------------------------- operands
-// Each has kMN (16-byte rows run along x), kRegs (a thread's registers of one step), init(x0, tid),
-// load(r0, r1, regs) for r0 .. r0 + 63, zeros from r1 on, and store(regs, tile); a B also kBf (bfloat16 or
-// half) and P (pieces of an element).
+// Each has kMN (16-byte rows run along x), kSpan (steps that one load feeds), kRegs (a thread's registers
+// of them), init(x0, tid), load(r0, r1, regs) for r0 .. r0 + 64 kSpan - 1, zeros from r1 on, and
+// store(regs, step of the span, tile); a B also kBf (bfloat16 or half) and P (pieces of an element).
+// The forward product's operands span two steps: the first takes the low 8 of every 16 k, the second the
+// high 8, so that a load is 16 bytes of codes and a row's 128 bytes are one line.
 
-// A(i = n, r = k): 2-bit weights, K-major, mixed order along k.  A thread holds 32 weights of one row.
+// 16 bytes of 2-bit weights at p, `left` weights in range (a multiple of 4).  unit: 16 or 4 bytes that every
+// row is a multiple of, or 1
+__device__ __forceinline__ void load_weights(const uint8_t *p, int64_t left, int unit, uint32_t (&w)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) w[i] = 0;
+  if (left <= 0) return;
+  if (unit == 16) {
+    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p));
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+  } else if (unit == 4) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (16 * i < left) w[i] = __ldg(reinterpret_cast<const uint32_t *>(p) + i);
+  } else {
+#pragma unroll
+    for (int b = 0; b < 16; ++b)
+      if (4 * b < left) w[b >> 2] |= static_cast<uint32_t>(__ldg(p + b)) << (8 * (b & 3));
+  }
+}
+
+// A(i = n, r = k): 2-bit weights, K-major, mixed order along k.  A thread holds 64 weights of one row.
 struct WeightsK {
   static constexpr bool kMN = false;
-  static constexpr int kRegs = 2;
+  static constexpr int kSpan = 2, kRegs = 4;
   const uint8_t *packed;
   int64_t N, K;
-  bool vec;  // rows are whole 8-byte words
+  int unit;
   struct Thread {
     const uint8_t *p;
     uint32_t off;
@@ -133,38 +160,26 @@ struct WeightsK {
   __device__ __forceinline__ Thread init(int64_t x0, int tid) const {
     const int lane = tid & 31, row = (tid >> 5) * 16 + ((lane >> 4) << 3) + (lane & 7), half = (lane >> 3) & 1;
     const int64_t n = x0 + row;
-    return {packed + (n * K >> 2) + half * 8, (row >> 3) * 1024u + half * 512u + (row & 7) * 16u, half * 32, n < N};
+    return {packed + (n * K >> 2) + half * 16, (row >> 3) * 1152u + half * 576u + (row & 7) * 16u, half * 64, n < N};
   }
   __device__ __forceinline__ void load(const Thread &t, int64_t r0, int64_t r1, uint32_t (&w)[kRegs]) const {
-    const uint8_t *p = t.p + (r0 >> 2);
-    const int64_t left = r1 - r0 - t.k;  // weights of this thread's row that are left
-    w[0] = w[1] = 0;
-    if (!t.live || left <= 0) return;
-    if (vec) {
-      const uint2 v = __ldg(reinterpret_cast<const uint2 *>(p));
-      w[0] = v.x, w[1] = v.y;
-    } else {
-#pragma unroll
-      for (int b = 0; b < 8; ++b)
-        if (4 * b < left) w[b >> 2] |= static_cast<uint32_t>(__ldg(p + b)) << (8 * (b & 3));
-    }
+    load_weights(t.p + (r0 >> 2), t.live ? r1 - r0 - t.k : 0, unit, w);
   }
-  __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], uint32_t tile) const {
+  __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool second, uint32_t tile) const {
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      uint32_t o[8];
-      weights16(w[g], o);
-      st_shared16(tile + t.off + g * 256u, o[0], o[1], o[2], o[3]);
-      st_shared16(tile + t.off + g * 256u + 128u, o[4], o[5], o[6], o[7]);
+    for (int g = 0; g < 4; ++g) {
+      uint32_t o[4];
+      weights8(w[g], second, o);
+      st_shared16(tile + t.off + g * 144u, o[0], o[1], o[2], o[3]);
     }
   }
 };
 
-// A(i = k, r = n): the same weights, MN-major; row i of the tile is k = i with its low 4 bits mixed.
-// A thread holds 32 k of one n.
+// A(i = k, r = n): the same weights, MN-major; row i of the tile is k = i with its low 3 bits mixed.
+// A thread holds 32 k of one n.  vec: rows are whole 8-byte words.
 struct WeightsT {
   static constexpr bool kMN = true;
-  static constexpr int kRegs = 2;
+  static constexpr int kSpan = 1, kRegs = 2;
   const uint8_t *packed;
   int64_t N, K;
   bool vec;
@@ -176,7 +191,7 @@ struct WeightsT {
   __device__ __forceinline__ Thread init(int64_t x0, int tid) const {
     const int lane = tid & 31, n = (tid >> 5) * 8 + (lane & 7), q = lane >> 3;
     const int64_t k = x0 + 32 * q, left = K - k;
-    return {packed + (k >> 2), q * 4096u + (n >> 3) * 128u + (n & 7) * 16u, n, static_cast<int>(left < 32 ? left : 32)};
+    return {packed + (k >> 2), q * 4160u + (n >> 3) * 128u + (n & 7) * 16u, n, static_cast<int>(left < 32 ? left : 32)};
   }
   __device__ __forceinline__ void load(const Thread &t, int64_t r0, int64_t r1, uint32_t (&w)[kRegs]) const {
     w[0] = w[1] = 0;
@@ -191,13 +206,12 @@ struct WeightsT {
         if (4 * b < t.left) w[b >> 2] |= static_cast<uint32_t>(__ldg(p + b)) << (8 * (b & 3));
     }
   }
-  __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], uint32_t tile) const {
+  __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool, uint32_t tile) const {
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
-      uint32_t o[8];
-      weights16(w[g], o);
-      st_shared16(tile + t.off + g * 2048u, o[0], o[1], o[2], o[3]);
-      st_shared16(tile + t.off + g * 2048u + 1024u, o[4], o[5], o[6], o[7]);
+    for (int g = 0; g < 4; ++g) {
+      uint32_t o[4];
+      weights8(w[g >> 1], g & 1, o);
+      st_shared16(tile + t.off + g * 1040u, o[0], o[1], o[2], o[3]);
     }
   }
 };
@@ -220,13 +234,13 @@ __device__ __forceinline__ void load_codes(const int8_t *p, int left, int unit, 
 }
 
 // B(j = m, r = k): int8 codes as halves, K-major, mixed order along k.  A thread holds 16 codes of each of
-// TB / 64 rows.
-template <int TB>
+// X / 32 rows.
+template <int X>
 struct CodesK {
   static constexpr bool kMN = false, kBf = false;
   static constexpr int P = 1;
-  static constexpr int kUnits = TB >= 64 ? TB / 64 : 1;
-  static constexpr int kRegs = 4 * kUnits;
+  static constexpr int kUnits = X >= 32 ? X / 32 : 1;
+  static constexpr int kSpan = 2, kRegs = 4 * kUnits;
   const int8_t *codes;
   int64_t M, ld;
   int unit;
@@ -237,67 +251,67 @@ struct CodesK {
     int64_t left;  // rows from this thread's first on
   };
   __device__ __forceinline__ Thread init(int64_t x0, int tid) const {
-    const int lane = tid & 31, row = (tid >> 5) * 8 + (lane & 7), q = lane >> 3;
+    const int lane = tid & 31, row = (tid >> 5) * 4 + (lane >> 3), q = lane & 7;
     const int64_t m = x0 + row;
-    return {codes + m * ld + 16 * q, (row >> 3) * 1024u + q * 256u + (row & 7) * 16u, 16 * q, row < TB ? M - m : 0};
+    return {codes + m * ld + 16 * q, (row >> 3) * 1152u + q * 144u + (row & 7) * 16u, 16 * q, row < X ? M - m : 0};
   }
   __device__ __forceinline__ void load(const Thread &t, int64_t r0, int64_t r1, uint32_t (&w)[kRegs]) const {
     const int64_t left = r1 - r0 - t.k;
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       w[4 * u] = w[4 * u + 1] = w[4 * u + 2] = w[4 * u + 3] = 0;
-      if (left > 0 && t.left > 64 * u)
-        load_codes(t.p + r0 + 64 * u * ld, static_cast<int>(left < 16 ? left : 16), unit, w + 4 * u);
+      if (left > 0 && t.left > 32 * u)
+        load_codes(t.p + r0 + 32 * u * ld, static_cast<int>(left < 16 ? left : 16), unit, w + 4 * u);
     }
   }
-  __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], uint32_t tile) const {
-    if (TB < 64 && t.off >= TB * 128u) return;
+  __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool second, uint32_t tile) const {
+    if (X < 32 && t.off >= tile_bytes(false, X)) return;
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-      const uint32_t b[4] = {w[4 * u], w[4 * u + 1], w[4 * u + 2], w[4 * u + 3]};
-      uint32_t o[8];
-      codes16_half_mixed(b, o);
-      st_shared16(tile + t.off + u * 8192u, o[0], o[1], o[2], o[3]);
-      st_shared16(tile + t.off + u * 8192u + 128u, o[4], o[5], o[6], o[7]);
+      uint32_t o[4];
+      codes8_half_mixed(second ? w[4 * u + 2] : w[4 * u], second ? w[4 * u + 3] : w[4 * u + 1], o);
+      st_shared16(tile + t.off + u * 4608u, o[0], o[1], o[2], o[3]);
     }
   }
 };
 
-// A(i = k, r = m): int8 codes as bfloat16, MN-major.  A thread holds 2 x 16 codes of one m.
+// A(i = k, r = m): int8 codes as bfloat16, MN-major.  A thread holds 16 codes of each of 2 m, and stores their
+// two pieces in an order that gives eight lanes eight bank groups.
 struct CodesT {
   static constexpr bool kMN = true;
-  static constexpr int kRegs = 8;
+  static constexpr int kSpan = 1, kRegs = 8;
   const int8_t *codes;
   int64_t K, ld;
   int unit;
   struct Thread {
     const int8_t *p;
-    uint32_t off;
+    uint32_t off, turn;
     int m;
     int64_t left;
   };
   __device__ __forceinline__ Thread init(int64_t x0, int tid) const {
-    const int lane = tid & 31, m = (tid >> 5) * 8 + (lane & 7), q = lane >> 3;
-    return {codes + x0 + 16 * q, q * 2048u + (m >> 3) * 128u + (m & 7) * 16u, m, K - x0 - 16 * q};
+    const int lane = tid & 31, m = (tid >> 5) * 4 + (lane >> 3), q = lane & 7;
+    return {codes + x0 + 16 * q, q * 2080u + (m >> 3) * 128u + (m & 7) * 16u, static_cast<uint32_t>(q >> 2), m, K - x0 - 16 * q};
   }
   __device__ __forceinline__ void load(const Thread &t, int64_t r0, int64_t r1, uint32_t (&w)[kRegs]) const {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       w[4 * u] = w[4 * u + 1] = w[4 * u + 2] = w[4 * u + 3] = 0;
-      const int64_t left = t.left - 64 * u;
-      if (r0 + t.m < r1 && left > 0)
-        load_codes(t.p + (r0 + t.m) * ld + 64 * u, static_cast<int>(left < 16 ? left : 16), unit, w + 4 * u);
+      if (r0 + t.m + 32 * u < r1 && t.left > 0)
+        load_codes(t.p + (r0 + t.m + 32 * u) * ld, static_cast<int>(t.left < 16 ? t.left : 16), unit, w + 4 * u);
     }
   }
-  __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], uint32_t tile) const {
+  __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool, uint32_t tile) const {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      uint32_t o[8];
+    for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) codes4_bf16(w[4 * u + i], o[2 * i], o[2 * i + 1]);
-      st_shared16(tile + t.off + u * 8192u, o[0], o[1], o[2], o[3]);
-      st_shared16(tile + t.off + u * 8192u + 1024u, o[4], o[5], o[6], o[7]);
-    }
+      for (int h = 0; h < 2; ++h) {
+        const bool high = (h ^ t.turn) != 0;
+        uint32_t o[4];
+        codes4_bf16(high ? w[4 * u + 2] : w[4 * u], o[0], o[1]);
+        codes4_bf16(high ? w[4 * u + 3] : w[4 * u + 1], o[2], o[3]);
+        st_shared16(tile + t.off + (high ? 1040u : 0u) + u * 512u, o[0], o[1], o[2], o[3]);
+      }
   }
 };
 
@@ -336,13 +350,13 @@ __device__ __forceinline__ void grad8_f32(const uint32_t *w, float (&v)[8]) {
 }
 
 // B(j = m, r = n): gradients, K-major: 16-bit ones as they are, 32-bit ones in three pieces.  A thread holds
-// 8 elements of each of TB / 32 places: 4 groups of 8 columns, 2 of them a thread, of TB / 64 rows.
-template <typename T, int TB>
+// 8 elements of each of X / 32 rows.
+template <typename T, int X>
 struct GradK {
   static constexpr bool kMN = false, kBf = !std::is_same_v<T, __half>;
   static constexpr int P = sizeof(T) == 4 ? 3 : 1;
-  static constexpr int kRows = TB >= 64 ? TB / 64 : 1, kUnits = 2 * kRows;
-  static constexpr int kRegs = kWords8<T> * kUnits;
+  static constexpr int kUnits = X / 32;
+  static constexpr int kSpan = 1, kRegs = kWords8<T> * kUnits;
   const T *dy;
   int64_t M, ld;
   bool vec;
@@ -353,46 +367,43 @@ struct GradK {
     int64_t left;
   };
   __device__ __forceinline__ Thread init(int64_t x0, int tid) const {
-    const int lane = tid & 31, row = (tid >> 5) * 8 + (lane & 7), q = lane >> 3;
+    const int lane = tid & 31, row = (tid >> 5) * 4 + (lane >> 3), q = lane & 7;
     const int64_t m = x0 + row;
-    return {dy + m * ld + 8 * q, (row >> 3) * 1024u + q * 128u + (row & 7) * 16u, 8 * q, row < TB ? M - m : 0};
+    return {dy + m * ld + 8 * q, (row >> 3) * 1152u + q * 144u + (row & 7) * 16u, 8 * q, M - m};
   }
   __device__ __forceinline__ void load(const Thread &t, int64_t r0, int64_t r1, uint32_t (&w)[kRegs]) const {
+    const int64_t left = r1 - r0 - t.n;
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       uint32_t *o = w + kWords8<T> * u;
 #pragma unroll
       for (int i = 0; i < kWords8<T>; ++i) o[i] = 0;
-      const int64_t left = r1 - r0 - t.n - 32 * (u & 1);
-      if (left > 0 && t.left > 64 * (u >> 1))
-        load_grad8<T>(t.p + r0 + 32 * (u & 1) + 64 * (u >> 1) * ld, static_cast<int>(left < 8 ? left : 8), vec, o);
+      if (left > 0 && t.left > 32 * u) load_grad8<T>(t.p + r0 + 32 * u * ld, static_cast<int>(left < 8 ? left : 8), vec, o);
     }
   }
-  __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], uint32_t tile) const {
-    if (TB < 64 && t.off >= TB * 128u) return;
+  __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool, uint32_t tile) const {
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-      const uint32_t at = tile + t.off + (u & 1) * 512u + (u >> 1) * 8192u;
       const uint32_t *o = w + kWords8<T> * u;
       if constexpr (P == 1) {
-        st_shared16(at, o[0], o[1], o[2], o[3]);
+        st_shared16(tile + t.off + u * 4608u, o[0], o[1], o[2], o[3]);
       } else {
         float v[8];
         grad8_f32<T>(o, v);
-        split8<P>(v, at, TB * kStep * 2);
+        split8<P>(v, tile + t.off + u * 4608u, tile_bytes(false, X));
       }
     }
   }
 };
 
-// B(j = n, r = m): gradients times their row's scale, in P bfloat16 pieces, MN-major.  A thread holds TB / 32
-// groups of 8 columns of one m, and its scale.
-template <typename T, int TB, int P_>
+// B(j = n, r = m): gradients times their row's scale, in P bfloat16 pieces, MN-major.  A thread holds X / 64
+// groups of 8 columns of each of 2 m, and their scales.
+template <typename T, int X, int P_>
 struct GradT {
   static constexpr bool kMN = true, kBf = true;
   static constexpr int P = P_;
-  static constexpr int kUnits = TB / 32;
-  static constexpr int kRegs = kWords8<T> * kUnits + 1;
+  static constexpr int kGroups = X / 64;
+  static constexpr int kSpan = 1, kRegs = 2 * kWords8<T> * kGroups + 2;
   const T *dy;
   int64_t N, ld;
   const float *scale;
@@ -404,31 +415,36 @@ struct GradT {
     int64_t left;
   };
   __device__ __forceinline__ Thread init(int64_t x0, int tid) const {
-    const int lane = tid & 31, m = (tid >> 5) * 8 + (lane & 7), q = lane >> 3;
-    return {dy + x0 + 8 * q, q * 1024u + (m >> 3) * 128u + (m & 7) * 16u, m, N - x0 - 8 * q};
+    const int lane = tid & 31, m = (tid >> 5) * 4 + (lane >> 3), q = lane & 7;
+    return {dy + x0 + 8 * q, q * 1040u + (m >> 3) * 128u + (m & 7) * 16u, m, N - x0 - 8 * q};
   }
   __device__ __forceinline__ void load(const Thread &t, int64_t r0, int64_t r1, uint32_t (&w)[kRegs]) const {
-    const bool live = r0 + t.m < r1;
-    w[kRegs - 1] = live ? __float_as_uint(__ldg(scale + r0 + t.m)) : 0u;
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      uint32_t *o = w + kWords8<T> * u;
+    for (int h = 0; h < 2; ++h) {
+      const int64_t m = r0 + t.m + 32 * h;
+      const bool live = m < r1;
+      w[kRegs - 2 + h] = live ? __float_as_uint(__ldg(scale + m)) : 0u;
 #pragma unroll
-      for (int i = 0; i < kWords8<T>; ++i) o[i] = 0;
-      const int64_t left = t.left - 32 * u;
-      if (live && left > 0) load_grad8<T>(t.p + (r0 + t.m) * ld + 32 * u, static_cast<int>(left < 8 ? left : 8), vec, o);
+      for (int u = 0; u < kGroups; ++u) {
+        uint32_t *o = w + kWords8<T> * (h * kGroups + u);
+#pragma unroll
+        for (int i = 0; i < kWords8<T>; ++i) o[i] = 0;
+        const int64_t left = t.left - 64 * u;
+        if (live && left > 0) load_grad8<T>(t.p + m * ld + 64 * u, static_cast<int>(left < 8 ? left : 8), vec, o);
+      }
     }
   }
-  __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], uint32_t tile) const {
-    const float s = __uint_as_float(w[kRegs - 1]);
+  __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool, uint32_t tile) const {
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      float v[8];
-      grad8_f32<T>(w + kWords8<T> * u, v);
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= s;
-      split8<P>(v, tile + t.off + u * 4096u, TB * kStep * 2);
-    }
+      for (int u = 0; u < kGroups; ++u) {
+        float v[8];
+        grad8_f32<T>(w + kWords8<T> * (h * kGroups + u), v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= __uint_as_float(w[kRegs - 2 + h]);
+        split8<P>(v, tile + t.off + u * 8320u + h * 512u, tile_bytes(true, X));
+      }
   }
 };
 
@@ -471,56 +487,66 @@ struct GemmArgs {
   A a;
   B b;
   Out out;
-  int tiles_i, steps;  // tiles along i; steps of a split
+  int tiles_i, steps;  // tiles along i (whole clusters); steps of a split
   float *partial;      // [splits][J][I] where there are several, else NULL
   int *err;            // set to 1 by a wait that gave up
 };
 
-template <int TB, int P>
+// CG CTAs on a tile of 128 CG i by TB j; a B operand of X = TB / CG rows each
+template <class A, class B, int TB, int CG>
 struct GemmShape {
-  static constexpr uint32_t kPieceBytes = TB * kStep * 2;
-  static constexpr uint32_t kStageBytes = kTileABytes + P * kPieceBytes;
-  static constexpr int kStages = P == 3 ? 3 : TB >= 128 ? 2 : 4;
-  static constexpr uint32_t kSmem = kStages * kStageBytes + 256;
-  static constexpr int kCtasPerSm = kSmem * 2 <= kSmemPerSm - 2048 ? 2 : 1;
+  static constexpr uint32_t kABytes = tile_bytes(A::kMN, kTileI), kPieceBytes = tile_bytes(B::kMN, TB / CG);
+  static constexpr uint32_t kStageBytes = kABytes + B::P * kPieceBytes;
+  static constexpr uint32_t kBars = 256;
+  static constexpr int fit(uint32_t room) { return static_cast<int>((room - kBars) / kStageBytes); }
+  static constexpr uint32_t kHalfSm = kSmemPerSm / 2 - 1024;
+  static constexpr int kCtasPerSm = fit(kHalfSm) >= 2 ? 2 : 1;
+  static constexpr int kAll = kCtasPerSm == 2 ? fit(kHalfSm) : fit(kMaxDynSmem);
+  static constexpr int kStages = kAll > 4 ? 4 : kAll;
+  static constexpr uint32_t kSmem = kStages * kStageBytes + kBars;
   static constexpr uint32_t kTmemCols = TB < 32 ? 32 : TB;
+  static_assert(kStages >= 2 && kStageBytes % 16 == 0 && kCtasPerSm * kTmemCols <= 512, "stages and accumulators");
+  static_assert(A::kSpan == B::kSpan, "operands load together");
 };
 
-template <class A, class B, class Out, int TB>
-__global__ void __launch_bounds__(kGemmThreads, GemmShape<TB, B::P>::kCtasPerSm)
+template <class A, class B, class Out, int TB, int CG>
+__global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPerSm)
     gemm_kernel(const __grid_constant__ GemmArgs<A, B, Out> g) {
-  constexpr int P = B::P;
-  using S = GemmShape<TB, P>;
+  constexpr int P = B::P, kSpan = A::kSpan;
+  using S = GemmShape<A, B, TB, CG>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t base = smem_u32(smem);
   const uint32_t bars = base + S::kStages * S::kStageBytes;  // full[stages], empty[stages], done; then 2 words
   const uint32_t full = bars, empty = bars + 8 * S::kStages, done = bars + 16 * S::kStages;
   volatile uint32_t *word = reinterpret_cast<volatile uint32_t *>(smem + S::kStages * S::kStageBytes + 16 * S::kStages + 8);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  const uint32_t rank = CG == 2 ? cluster_ctarank() : 0;
   const int64_t i0 = static_cast<int64_t>(blockIdx.x % g.tiles_i) * kTileI, j0 = static_cast<int64_t>(blockIdx.x / g.tiles_i) * TB;
   const int64_t first = static_cast<int64_t>(blockIdx.y) * g.steps * kStep;
   const int64_t end = first + static_cast<int64_t>(g.steps) * kStep < g.R ? first + static_cast<int64_t>(g.steps) * kStep : g.R;
-  const int steps = static_cast<int>((end - first + kStep - 1) / kStep);
+  const int steps = kSpan * static_cast<int>((end - first + kSpan * kStep - 1) / (kSpan * kStep));
 
   if (tid == 0) {
-    for (int s = 0; s < S::kStages; ++s) mbar_init(full + 8 * s, kProducerWarps), mbar_init(empty + 8 * s, 1);
+    for (int s = 0; s < S::kStages; ++s) mbar_init(full + 8 * s, CG * kProducerWarps), mbar_init(empty + 8 * s, 1);
     mbar_init(done, 1);
     fence_mbar_init_cluster();
     word[1] = 0;
   }
   if (warp == kProducerWarps) {
-    tmem_alloc(smem_u32(const_cast<uint32_t *>(word)), S::kTmemCols);
-    tmem_relinquish();
+    tmem_alloc_cg<CG>(smem_u32(const_cast<uint32_t *>(word)), S::kTmemCols);
+    tmem_relinquish_cg<CG>();
   }
   tc_fence_before();
-  __syncthreads();
+  if constexpr (CG == 2) cluster_sync_all();  // (the other CTA's barriers too)
+  else __syncthreads();
   tc_fence_after();
   const uint32_t tmem = word[0];
   // a wait with an end: one that gives up stops the CTA's others too
   auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
-    if (mbar_try_wait(bar, parity)) return true;
+    auto try_wait = [&] { return CG == 2 ? mbar_try_wait_acq_cluster(bar, parity) : mbar_try_wait(bar, parity); };
+    if (try_wait()) return true;
     const long long t0 = clock64();
-    while (!mbar_try_wait(bar, parity)) {
+    while (!try_wait()) {
       if (word[1]) return false;
       if (clock64() - t0 > kGemmWaitCycles) {
         word[1] = 1;
@@ -533,48 +559,62 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<TB, B::P>::kCtasPerSm)
 
   if (warp < kProducerWarps) {
     const typename A::Thread ta = g.a.init(i0, tid);
-    const typename B::Thread tb = g.b.init(j0, tid);
+    const typename B::Thread tb = g.b.init(j0 + rank * (TB / CG), tid);
     uint32_t ra[A::kRegs], rb[B::kRegs];
     g.a.load(ta, first, end, ra);
     g.b.load(tb, first, end, rb);
-    for (int it = 0; it < steps; ++it) {
-      const int s = it % S::kStages;
-      const bool free = it < S::kStages || wait(empty + 8 * s, (it / S::kStages - 1) & 1);
-      if (!__all_sync(0xffffffffu, free)) break;
-      const uint32_t stage = base + s * S::kStageBytes;
-      g.a.store(ta, ra, stage);
-      g.b.store(tb, rb, stage + kTileABytes);
-      fence_proxy_async_smem();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(full + 8 * s);
-      if (it + 1 < steps) {  // the next step's, in flight while the tensor cores work through the stages
-        g.a.load(ta, first + static_cast<int64_t>(it + 1) * kStep, end, ra);
-        g.b.load(tb, first + static_cast<int64_t>(it + 1) * kStep, end, rb);
+    const uint32_t full0 = CG == 2 ? mapa_cluster(full, 0) : full;
+    int s = 0, parity = 1;
+    for (int it = 0; it < steps; it += kSpan) {
+#pragma unroll
+      for (int h = 0; h < kSpan; ++h) {
+        const bool free = it + h < S::kStages || wait(empty + 8 * s, parity);
+        if (!__all_sync(0xffffffffu, free)) {
+          it = steps;
+          break;
+        }
+        const uint32_t stage = base + s * S::kStageBytes;
+        g.a.store(ta, ra, h == 1, stage);
+        g.b.store(tb, rb, h == 1, stage + S::kABytes);
+        fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          if constexpr (CG == 2) mbar_arrive_cluster(full0 + 8 * s);
+          else mbar_arrive(full + 8 * s);
+        }
+        if (++s == S::kStages) s = 0, parity ^= 1;
+      }
+      if (it + kSpan < steps) {  // the next span's, in flight while the tensor cores work through the stages
+        g.a.load(ta, first + static_cast<int64_t>(it + kSpan) * kStep, end, ra);
+        g.b.load(tb, first + static_cast<int64_t>(it + kSpan) * kStep, end, rb);
       }
     }
-  } else {
-    constexpr uint32_t idesc = gemm_idesc(B::kBf, A::kMN, B::kMN, TB);
+  } else if (rank == 0) {
+    constexpr uint32_t idesc = gemm_idesc(B::kBf, A::kMN, B::kMN, 128 * CG, TB);
+    constexpr uint32_t la = tile_lbo(A::kMN), lb = tile_lbo(B::kMN);
+    int s = 0, parity = 0;
     for (int it = 0; it < steps; ++it) {
-      const int s = it % S::kStages;
-      if (!__all_sync(0xffffffffu, wait(full + 8 * s, (it / S::kStages) & 1))) break;
+      if (!__all_sync(0xffffffffu, wait(full + 8 * s, parity))) break;
       tc_fence_after();
-      const uint32_t at = base + s * S::kStageBytes, bt = at + kTileABytes;
+      const uint32_t at = base + s * S::kStageBytes, bt = at + S::kABytes;
 #pragma unroll
       for (int p = 0; p < P; ++p)
 #pragma unroll
         for (int ks = 0; ks < kStep / 16; ++ks)
-          mma_bf16_warp(tmem, make_sdesc(at + ks * 256, 128, 1024), make_sdesc(bt + p * S::kPieceBytes + ks * 256, 128, 1024), idesc,
-                        it > 0 || p > 0 || ks > 0 ? 1u : 0u);
-      mma_commit_warp(empty + 8 * s);
+          mma_f16_cg_warp<CG>(tmem, make_sdesc(at + ks * 2 * la, la, tile_sbo(A::kMN)),
+                              make_sdesc(bt + p * S::kPieceBytes + ks * 2 * lb, lb, tile_sbo(B::kMN)), idesc,
+                              it > 0 || p > 0 || ks > 0 ? 1u : 0u);
+      mma_commit_cg_warp<CG>(empty + 8 * s);
+      if (++s == S::kStages) s = 0, parity ^= 1;
     }
-    mma_commit_warp(done);
+    mma_commit_cg_warp<CG>(done);
   }
   __syncwarp();
   const bool ready = __all_sync(0xffffffffu, wait(done, 0) && !word[1]);
   tc_fence_after();
   if (warp < kProducerWarps) {
     const int64_t row = 32 * (warp & 3) + lane;  // of the tile, and the lane of tensor memory
-    const int64_t i = i0 + (std::is_same_v<A, WeightsT> ? (row & ~15) | mix16(row & 15) : row);
+    const int64_t i = i0 + (std::is_same_v<A, WeightsT> ? (row & ~7) | mix8(row & 7) : row);
     const uint32_t tl = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16);
     constexpr int kHalf = TB / 2;  // columns of each of the two warps of a lane quadrant
     constexpr int kGroup = kHalf < 16 ? 8 : 16;
@@ -603,10 +643,11 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<TB, B::P>::kCtasPerSm)
     }
   }
   tc_fence_before();
-  __syncthreads();
+  if constexpr (CG == 2) cluster_sync_all();
+  else __syncthreads();
   if (warp == kProducerWarps) {
     tc_fence_after();
-    tmem_dealloc(tmem, S::kTmemCols);
+    tmem_dealloc_cg<CG>(tmem, S::kTmemCols);
   }
 }
 
@@ -628,6 +669,10 @@ inline int codes_unit(const int8_t *codes, int64_t ld, int64_t K) {
   const uintptr_t all = reinterpret_cast<uintptr_t>(codes) | static_cast<uintptr_t>(ld) | static_cast<uintptr_t>(K);
   return (all & 15u) == 0 ? 16 : (all & 3u) == 0 ? 4 : 1;
 }
+inline int weights_unit(const uint8_t *packed, int64_t K) {
+  const uintptr_t p = reinterpret_cast<uintptr_t>(packed);
+  return K % 64 == 0 && (p & 15u) == 0 ? 16 : K % 16 == 0 && (p & 3u) == 0 ? 4 : 1;
+}
 template <typename T>
 bool grads_vec(const void *dy, int64_t ld, int64_t N) {
   return (reinterpret_cast<uintptr_t>(dy) & 15u) == 0 && ld * static_cast<int64_t>(sizeof(T)) % 16 == 0 && N % 8 == 0;
@@ -639,35 +684,52 @@ struct GemmPlan {
   int splits, steps;
 };
 constexpr int kMinSteps = 4;
-template <int TB, int P>
+template <class A, class B, int TB, int CG>
 GemmPlan gemm_plan(int64_t I, int64_t J, int64_t R, int sms) {
   GemmPlan p;
-  p.tiles_i = (I + kTileI - 1) / kTileI, p.tiles_j = (J + TB - 1) / TB;
-  const int64_t all = (R + kStep - 1) / kStep, room = static_cast<int64_t>(sms) * GemmShape<TB, P>::kCtasPerSm;
+  p.tiles_i = (I + CG * kTileI - 1) / (CG * kTileI) * CG, p.tiles_j = (J + TB - 1) / TB;
+  const int64_t all = (R + kStep - 1) / kStep, room = static_cast<int64_t>(sms) * GemmShape<A, B, TB, CG>::kCtasPerSm;
   int64_t splits = room / (p.tiles_i * p.tiles_j);
   if (splits > all / kMinSteps) splits = all / kMinSteps;
   if (splits < 1) splits = 1;
-  p.steps = static_cast<int>((all + splits - 1) / splits);
-  p.splits = p.steps > 0 ? static_cast<int>((all + p.steps - 1) / p.steps) : 1;
-  if (p.splits < 1) p.splits = 1;
+  const int64_t steps = (all + splits - 1) / splits;
+  p.steps = static_cast<int>((steps + A::kSpan - 1) / A::kSpan * A::kSpan);
+  p.splits = static_cast<int>((all + p.steps - 1) / p.steps);
   return p;
 }
 
-template <class A, class B, class Out, int TB>
+template <class A, class B, class Out, int TB, int CG>
 cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b, const Out &out, float *partial, int sms, int *err,
                         cudaStream_t st) {
-  constexpr int P = B::P;
-  using S = GemmShape<TB, P>;
-  const GemmPlan p = gemm_plan<TB, P>(I, J, R, sms);
+  using S = GemmShape<A, B, TB, CG>;
+  const GemmPlan p = gemm_plan<A, B, TB, CG>(I, J, R, sms);
   const GemmArgs<A, B, Out> g = {I, J, R, a, b, out, static_cast<int>(p.tiles_i), p.steps, p.splits > 1 ? partial : nullptr, err};
-  auto *kernel = gemm_kernel<A, B, Out, TB>;
+  auto *kernel = gemm_kernel<A, B, Out, TB, CG>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
   if (e != cudaSuccess) return e;
-  kernel<<<dim3(static_cast<unsigned>(p.tiles_i * p.tiles_j), p.splits), kGemmThreads, S::kSmem, st>>>(g);
-  if ((e = cudaGetLastError()) != cudaSuccess || p.splits == 1) return e;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = CG, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(p.tiles_i * p.tiles_j), p.splits);
+  cfg.blockDim = dim3(kGemmThreads);
+  cfg.dynamicSmemBytes = S::kSmem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if ((e = cudaLaunchKernelEx(&cfg, kernel, g)) != cudaSuccess || p.splits == 1) return e;
   gemm_join_kernel<Out><<<dim3(static_cast<unsigned>((I + 255) / 256), static_cast<unsigned>(J < 65535 ? J : 65535)), 256, 0, st>>>(
       partial, p.splits, I, J, out);
   return cudaGetLastError();
+}
+
+// The tile of a product: f(TB, CG).  At most 64 j: 64 (the rest of a tile would be converted zeros); one row
+// of tiles along i: a single CTA's; else a pair's.
+template <int SINGLE, class F>
+auto with_tile(int64_t I, int64_t J, const F &f) {
+  if (J <= 64) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
+  if (I <= kTileI) return f(std::integral_constant<int, SINGLE>(), std::integral_constant<int, 1>());
+  return f(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
 }
 
 }  // namespace aecct

@@ -41,24 +41,29 @@ int bias_parts(int64_t M, int64_t N) {
   return static_cast<int>(p < 1 ? 1 : p > 65535 ? 65535 : p);
 }
 
-template <class F>
-auto with_tile(int64_t M, bool pieces, const F &f) {
-  if (M <= 64) return f(std::integral_constant<int, 64>());
-  return pieces ? f(std::integral_constant<int, 128>()) : f(std::integral_constant<int, 256>());
-}
+// j of a single CTA's tile: three pieces of 256 rows would leave room for one stage
+template <typename T>
+constexpr int kSingle = sizeof(T) == 4 ? 128 : 256;
 
 template <typename T>
 cudaError_t input_grad(const AapLinearGradCall &c, float *work, cudaStream_t st) {
   const WeightsT a = {c.packed, c.N, c.K, c.K % 32 == 0 && (reinterpret_cast<uintptr_t>(c.packed) & 7u) == 0};
   const OutX out = {c.dx, c.dtype, c.K, c.w_scale};
-  auto run = [&](auto tb) {
-    constexpr int TB = decltype(tb)::value;
-    const GradK<T, TB> b = {static_cast<const T *>(c.dy), c.M, c.lddy, grads_vec<T>(c.dy, c.lddy, c.N)};
-    return launch_gemm<WeightsT, GradK<T, TB>, OutX, TB>(c.K, c.M, c.N, a, b, out, work, sm_count(), linear_status(), st);
-  };
-  if (c.M <= 64) return run(std::integral_constant<int, 64>());
-  if constexpr (sizeof(T) == 4) return run(std::integral_constant<int, 128>());
-  else return run(std::integral_constant<int, 256>());
+  return with_tile<kSingle<T>>(c.K, c.M, [&](auto tb, auto cg) {
+    constexpr int TB = decltype(tb)::value, CG = decltype(cg)::value;
+    using B = GradK<T, TB / CG>;
+    const B b = {static_cast<const T *>(c.dy), c.M, c.lddy, grads_vec<T>(c.dy, c.lddy, c.N)};
+    return launch_gemm<WeightsT, B, OutX, TB, CG>(c.K, c.M, c.N, a, b, out, work, sm_count(), linear_status(), st);
+  });
+}
+
+template <typename T>
+int64_t input_grad_workspace(int64_t M, int64_t K, int64_t N) {
+  return with_tile<kSingle<T>>(K, M, [&](auto tb, auto cg) {
+    constexpr int TB = decltype(tb)::value, CG = decltype(cg)::value;
+    const GemmPlan p = gemm_plan<WeightsT, GradK<T, TB / CG>, TB, CG>(K, M, N, sm_count());
+    return p.splits > 1 ? p.splits * M * K : int64_t(0);
+  });
 }
 
 template <typename T>
@@ -75,12 +80,7 @@ cudaError_t bias_grad(const AapLinearGradCall &c, float *work, cudaStream_t st) 
 
 // the three products run one after the other and share the workspace
 int64_t aap_linear_grad_workspace(int64_t M, int64_t K, int64_t N, int dtype, int wdtype) {
-  const int sms = sm_count();
-  const int64_t x = with_tile(M, dtype == 0, [&](auto tb) {
-    constexpr int TB = decltype(tb)::value;
-    const GemmPlan p = dtype == 0 ? gemm_plan<TB == 256 ? 128 : TB, 3>(K, M, N, sms) : gemm_plan<TB, 1>(K, M, N, sms);
-    return p.splits > 1 ? p.splits * M * K : int64_t(0);
-  });
+  const int64_t x = dtype == 0 ? input_grad_workspace<float>(M, K, N) : input_grad_workspace<__half>(M, K, N);
   const int64_t w = weight_grad_workspace(M, K, N, wdtype), b = static_cast<int64_t>(bias_parts(M, N)) * N;
   const int64_t most = x > w ? (x > b ? x : b) : (w > b ? w : b);
   return most * static_cast<int64_t>(sizeof(float));

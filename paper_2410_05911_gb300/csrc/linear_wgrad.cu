@@ -21,13 +21,21 @@ template <typename T, int P>
 cudaError_t weight_grad(const AapLinearGradCall &c, float *work, cudaStream_t st) {
   const CodesT a = {c.codes, c.K, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
   const OutW out = {c.dw, c.wdtype, c.K};
-  auto run = [&](auto tb) {
-    constexpr int TB = decltype(tb)::value;
-    const GradT<T, TB, P> b = {static_cast<const T *>(c.dy), c.N, c.lddy, c.scale, grads_vec<T>(c.dy, c.lddy, c.N)};
-    return launch_gemm<CodesT, GradT<T, TB, P>, OutW, TB>(c.K, c.N, c.M, a, b, out, work, sm_count(), linear_status(), st);
-  };
-  if (c.N <= 64) return run(std::integral_constant<int, 64>());
-  return run(std::integral_constant<int, P == 1 ? 256 : 128>());
+  return with_tile<P == 1 ? 256 : 128>(c.K, c.N, [&](auto tb, auto cg) {
+    constexpr int TB = decltype(tb)::value, CG = decltype(cg)::value;
+    using B = GradT<T, TB / CG, P>;
+    const B b = {static_cast<const T *>(c.dy), c.N, c.lddy, c.scale, grads_vec<T>(c.dy, c.lddy, c.N)};
+    return launch_gemm<CodesT, B, OutW, TB, CG>(c.K, c.N, c.M, a, b, out, work, sm_count(), linear_status(), st);
+  });
+}
+
+template <int P>
+int64_t workspace_of(int64_t M, int64_t K, int64_t N) {
+  return with_tile<P == 1 ? 256 : 128>(K, N, [&](auto tb, auto cg) {
+    constexpr int TB = decltype(tb)::value, CG = decltype(cg)::value;
+    const GemmPlan p = gemm_plan<CodesT, GradT<float, TB / CG, P>, TB, CG>(K, N, M, sm_count());
+    return p.splits > 1 ? p.splits * K * N : int64_t(0);
+  });
 }
 
 template <typename T>
@@ -39,12 +47,8 @@ cudaError_t weight_grad(const AapLinearGradCall &c, float *work, cudaStream_t st
 }  // namespace
 
 int64_t weight_grad_workspace(int64_t M, int64_t K, int64_t N, int wdtype) {
-  const int sms = sm_count();
-  const int pieces = pieces_of(M, wdtype);
-  const GemmPlan p = pieces == 3   ? (N <= 64 ? gemm_plan<64, 3>(K, N, M, sms) : gemm_plan<128, 3>(K, N, M, sms))
-                     : pieces == 2 ? (N <= 64 ? gemm_plan<64, 2>(K, N, M, sms) : gemm_plan<128, 2>(K, N, M, sms))
-                                   : (N <= 64 ? gemm_plan<64, 1>(K, N, M, sms) : gemm_plan<256, 1>(K, N, M, sms));
-  return p.splits > 1 ? p.splits * K * N : 0;
+  const int p = pieces_of(M, wdtype);
+  return p == 3 ? workspace_of<3>(M, K, N) : p == 2 ? workspace_of<2>(M, K, N) : workspace_of<1>(M, K, N);
 }
 
 cudaError_t launch_weight_grad(const AapLinearGradCall &c, float *work, cudaStream_t st) {
