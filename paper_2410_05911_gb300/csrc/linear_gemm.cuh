@@ -10,7 +10,7 @@
 //
 // A CTA makes a tile of 128 i by TB j; from 256 of both on, a cluster of two makes 256 by 256 (cta_group::2),
 // each CTA with its own 128 rows of A and half of B in shared memory, so that a B is converted and stored by one
-// of two SMs.  Eight producer warps load a step ahead, convert and store; a ninth warp (of the first
+// of two SMs.  Sixteen producer warps load ahead, convert and store; another warp (of the first
 // CTA) issues the MMAs.  Lanes hold consecutive i in tensor memory, so that the epilogue's stores of one j are 32
 // neighbouring elements.  Two CTAs share an SM where their operands fit, one's epilogue behind the other's
 // products.
@@ -34,9 +34,10 @@ namespace aecct {
 
 constexpr int kStep = 64;           // r per stage
 constexpr int kTileI = 128;         // i per CTA: the lanes of tensor memory
-constexpr int kProducerWarps = 8;
+constexpr int kProducerWarps = 16;
 constexpr int kProducers = kProducerWarps * 32;
 constexpr int kGemmThreads = kProducers + 32;
+constexpr int kPass = kProducerWarps * 4;  // rows of 8 lanes that the producers hold at a time
 // a tile of x rows, and its descriptor's strides
 __host__ __device__ constexpr uint32_t tile_bytes(bool mn, int x) { return x / 8 * (mn ? 1040u : 1152u); }
 __host__ __device__ constexpr uint32_t tile_lbo(bool mn) { return mn ? 128u : 144u; }
@@ -119,14 +120,102 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint32_t addr, uint3
 
 // ----------------------------------------------------------------------------- operands
 // Each has kMN (16-byte rows run along x), kSpan (steps that one load feeds), kRegs (a thread's registers
-// of them), init(x0, tid), load(r0, r1, regs) for r0 .. r0 + 64 kSpan - 1, zeros from r1 on, and
-// store(regs, step of the span, tile); a B also kBf (bfloat16 or half) and P (pieces of an element).
-// The forward product's operands span two steps: the first takes the low 8 of every 16 k, the second the
-// high 8, so that a load is 16 bytes of codes and a row's 128 bytes are one line.
+// of them), init(x0, r0, tid), load(thread, left, regs): the next span, of `left` r that are in range, zeros
+// beyond; and store(thread, regs, step of the span, tile).  A B also has kBf (bfloat16 or half) and P
+// (pieces of an element).  The forward product's operands span two steps: the first takes the low 8 of every
+// 16 k, the second the high 8, so that a load is 16 bytes of codes and a row's 128 bytes are one line.
 
-// 16 bytes of 2-bit weights at p, `left` weights in range (a multiple of 4).  unit: 16 or 4 bytes that every
+// 2-bit weights at p, 4 W bytes, `left` weights in range (a multiple of 4).  unit: 8 or 4 bytes that every
 // row is a multiple of, or 1
-__device__ __forceinline__ void load_weights(const uint8_t *p, int64_t left, int unit, uint32_t (&w)[4]) {
+template <int W>
+__device__ __forceinline__ void load_weights(const uint8_t *p, int left, int unit, uint32_t (&w)[W]) {
+#pragma unroll
+  for (int i = 0; i < W; ++i) w[i] = 0;
+  if (left <= 0) return;
+  if (unit == 8) {
+    if constexpr (W == 2) {
+      const uint2 v = __ldg(reinterpret_cast<const uint2 *>(p));
+      w[0] = v.x, w[1] = v.y;
+    } else {
+      w[0] = __ldg(reinterpret_cast<const uint32_t *>(p));
+    }
+  } else if (unit == 4) {
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+      if (16 * i < left) w[i] = __ldg(reinterpret_cast<const uint32_t *>(p) + i);
+  } else {
+#pragma unroll
+    for (int b = 0; b < 4 * W; ++b)
+      if (4 * b < left) w[b >> 2] |= static_cast<uint32_t>(__ldg(p + b)) << (8 * (b & 3));
+  }
+}
+
+// A(i = n, r = k): 2-bit weights, K-major, mixed order along k.  A thread holds 32 weights of one row.
+struct WeightsK {
+  static constexpr bool kMN = false;
+  static constexpr int kSpan = 2, kRegs = 2;
+  const uint8_t *packed;
+  int64_t N, K;
+  int unit;
+  struct Thread {
+    const uint8_t *p;
+    uint32_t off;
+    int k;
+  };
+  __device__ __forceinline__ Thread init(int64_t x0, int64_t r0, int tid) const {
+    const int lane = tid & 31, row = (tid >> 5) * 8 + (lane & 7), q = lane >> 3;
+    const int64_t n = x0 + row;  // (a row past the last one holds nothing in range)
+    return {packed + (n * K + r0 >> 2) + q * 8, (row >> 3) * 1152u + q * 288u + (row & 7) * 16u, n < N ? q * 32 : 1 << 30};
+  }
+  __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
+    load_weights<2>(t.p, left - t.k, unit, w);
+    t.p += kSpan * kStep / 4;
+  }
+  __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool second, uint32_t tile) const {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      uint32_t o[4];
+      weights8(w[g], second, o);
+      st_shared16(tile + t.off + g * 144u, o[0], o[1], o[2], o[3]);
+    }
+  }
+};
+
+// A(i = k, r = n): the same weights, MN-major; row i of the tile is k = i with its low 3 bits mixed.
+// A thread holds 16 k of one n.
+struct WeightsT {
+  static constexpr bool kMN = true;
+  static constexpr int kSpan = 1, kRegs = 1;
+  const uint8_t *packed;
+  int64_t N, K;
+  int unit;
+  struct Thread {
+    const uint8_t *p;
+    uint32_t off;
+    int n, k;  // k: how many of the 16 are in range
+  };
+  __device__ __forceinline__ Thread init(int64_t x0, int64_t r0, int tid) const {
+    const int lane = tid & 31, warp = tid >> 5, n = (warp >> 1) * 8 + (lane & 7), q = (warp & 1) * 4 + (lane >> 3);
+    const int64_t k = x0 + 16 * q, left = K - k;
+    return {packed + ((r0 + n) * K + k >> 2), q * 2080u + (n >> 3) * 128u + (n & 7) * 16u, n,
+            static_cast<int>(left < 16 ? left : 16)};
+  }
+  __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
+    load_weights<1>(t.p, t.n < left ? t.k : 0, unit, w);
+    t.p += kStep / 4 * K;
+  }
+  __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool, uint32_t tile) const {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      uint32_t o[4];
+      weights8(w[0], g, o);
+      st_shared16(tile + t.off + g * 1040u, o[0], o[1], o[2], o[3]);
+    }
+  }
+};
+
+// 16 codes at p, `left` of them in range.  unit: 16 or 4 bytes that every row is a multiple of, or 1
+__device__ __forceinline__ void load_codes(const int8_t *p, int left, int unit, uint32_t *w) {
 #pragma unroll
   for (int i = 0; i < 4; ++i) w[i] = 0;
   if (left <= 0) return;
@@ -136,110 +225,26 @@ __device__ __forceinline__ void load_weights(const uint8_t *p, int64_t left, int
   } else if (unit == 4) {
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (16 * i < left) w[i] = __ldg(reinterpret_cast<const uint32_t *>(p) + i);
+      if (4 * i < left) w[i] = __ldg(reinterpret_cast<const uint32_t *>(p) + i);
   } else {
-#pragma unroll
-    for (int b = 0; b < 16; ++b)
-      if (4 * b < left) w[b >> 2] |= static_cast<uint32_t>(__ldg(p + b)) << (8 * (b & 3));
-  }
-}
-
-// A(i = n, r = k): 2-bit weights, K-major, mixed order along k.  A thread holds 64 weights of one row.
-struct WeightsK {
-  static constexpr bool kMN = false;
-  static constexpr int kSpan = 2, kRegs = 4;
-  const uint8_t *packed;
-  int64_t N, K;
-  int unit;
-  struct Thread {
-    const uint8_t *p;
-    uint32_t off;
-    int k;
-    bool live;
-  };
-  __device__ __forceinline__ Thread init(int64_t x0, int tid) const {
-    const int lane = tid & 31, row = (tid >> 5) * 16 + ((lane >> 4) << 3) + (lane & 7), half = (lane >> 3) & 1;
-    const int64_t n = x0 + row;
-    return {packed + (n * K >> 2) + half * 16, (row >> 3) * 1152u + half * 576u + (row & 7) * 16u, half * 64, n < N};
-  }
-  __device__ __forceinline__ void load(const Thread &t, int64_t r0, int64_t r1, uint32_t (&w)[kRegs]) const {
-    load_weights(t.p + (r0 >> 2), t.live ? r1 - r0 - t.k : 0, unit, w);
-  }
-  __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool second, uint32_t tile) const {
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      uint32_t o[4];
-      weights8(w[g], second, o);
-      st_shared16(tile + t.off + g * 144u, o[0], o[1], o[2], o[3]);
-    }
-  }
-};
-
-// A(i = k, r = n): the same weights, MN-major; row i of the tile is k = i with its low 3 bits mixed.
-// A thread holds 32 k of one n.  vec: rows are whole 8-byte words.
-struct WeightsT {
-  static constexpr bool kMN = true;
-  static constexpr int kSpan = 1, kRegs = 2;
-  const uint8_t *packed;
-  int64_t N, K;
-  bool vec;
-  struct Thread {
-    const uint8_t *p;
-    uint32_t off;
-    int n, left;
-  };
-  __device__ __forceinline__ Thread init(int64_t x0, int tid) const {
-    const int lane = tid & 31, n = (tid >> 5) * 8 + (lane & 7), q = lane >> 3;
-    const int64_t k = x0 + 32 * q, left = K - k;
-    return {packed + (k >> 2), q * 4160u + (n >> 3) * 128u + (n & 7) * 16u, n, static_cast<int>(left < 32 ? left : 32)};
-  }
-  __device__ __forceinline__ void load(const Thread &t, int64_t r0, int64_t r1, uint32_t (&w)[kRegs]) const {
-    w[0] = w[1] = 0;
-    if (r0 + t.n >= r1 || t.left <= 0) return;
-    const uint8_t *p = t.p + ((r0 + t.n) * K >> 2);
-    if (vec) {
-      const uint2 v = __ldg(reinterpret_cast<const uint2 *>(p));
-      w[0] = v.x, w[1] = v.y;
-    } else {
-#pragma unroll
-      for (int b = 0; b < 8; ++b)
-        if (4 * b < t.left) w[b >> 2] |= static_cast<uint32_t>(__ldg(p + b)) << (8 * (b & 3));
-    }
-  }
-  __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool, uint32_t tile) const {
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      uint32_t o[4];
-      weights8(w[g >> 1], g & 1, o);
-      st_shared16(tile + t.off + g * 1040u, o[0], o[1], o[2], o[3]);
-    }
-  }
-};
-
-// 16 codes at p, `left` of them in range (1 .. 16).  unit: 16 or 4 bytes that every row is a multiple of, or 1
-__device__ __forceinline__ void load_codes(const int8_t *p, int left, int unit, uint32_t *w) {
-  if (unit == 16) {
-    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p));
-    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-  } else if (unit == 4) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = 4 * i < left ? __ldg(reinterpret_cast<const uint32_t *>(p) + i) : 0u;
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = 0;
 #pragma unroll
     for (int i = 0; i < 16; ++i)
       if (i < left) w[i >> 2] |= (static_cast<uint32_t>(__ldg(p + i)) & 0xFFu) << (8 * (i & 3));
   }
 }
 
+// rows of `have` from the first one on that x rows of a tile may read, as an int
+__device__ __forceinline__ int rows_left(int64_t have) {
+  return static_cast<int>(have < 0 ? 0 : have < 1024 ? have : 1024);
+}
+
 // B(j = m, r = k): int8 codes as halves, K-major, mixed order along k.  A thread holds 16 codes of each of
-// X / 32 rows.
+// X / kPass rows.
 template <int X>
 struct CodesK {
   static constexpr bool kMN = false, kBf = false;
   static constexpr int P = 1;
-  static constexpr int kUnits = X >= 32 ? X / 32 : 1;
+  static constexpr int kUnits = X >= kPass ? X / kPass : 1;
   static constexpr int kSpan = 2, kRegs = 4 * kUnits;
   const int8_t *codes;
   int64_t M, ld;
@@ -247,79 +252,73 @@ struct CodesK {
   struct Thread {
     const int8_t *p;
     uint32_t off;
-    int k;
-    int64_t left;  // rows from this thread's first on
+    int k, rows;
   };
-  __device__ __forceinline__ Thread init(int64_t x0, int tid) const {
+  __device__ __forceinline__ Thread init(int64_t x0, int64_t r0, int tid) const {
     const int lane = tid & 31, row = (tid >> 5) * 4 + (lane >> 3), q = lane & 7;
     const int64_t m = x0 + row;
-    return {codes + m * ld + 16 * q, (row >> 3) * 1152u + q * 144u + (row & 7) * 16u, 16 * q, row < X ? M - m : 0};
+    return {codes + m * ld + r0 + 16 * q, (row >> 3) * 1152u + q * 144u + (row & 7) * 16u, 16 * q, row < X ? rows_left(M - m) : 0};
   }
-  __device__ __forceinline__ void load(const Thread &t, int64_t r0, int64_t r1, uint32_t (&w)[kRegs]) const {
-    const int64_t left = r1 - r0 - t.k;
+  __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      w[4 * u] = w[4 * u + 1] = w[4 * u + 2] = w[4 * u + 3] = 0;
-      if (left > 0 && t.left > 32 * u)
-        load_codes(t.p + r0 + 32 * u * ld, static_cast<int>(left < 16 ? left : 16), unit, w + 4 * u);
-    }
+    for (int u = 0; u < kUnits; ++u) load_codes(t.p + u * kPass * ld, t.rows > kPass * u ? left - t.k : 0, unit, w + 4 * u);
+    t.p += kSpan * kStep;
   }
   __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool second, uint32_t tile) const {
-    if (X < 32 && t.off >= tile_bytes(false, X)) return;
+    if (X < kPass && t.off >= tile_bytes(false, X)) return;
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       uint32_t o[4];
       codes8_half_mixed(second ? w[4 * u + 2] : w[4 * u], second ? w[4 * u + 3] : w[4 * u + 1], o);
-      st_shared16(tile + t.off + u * 4608u, o[0], o[1], o[2], o[3]);
+      st_shared16(tile + t.off + u * (kPass / 8 * 1152u), o[0], o[1], o[2], o[3]);
     }
   }
 };
 
-// A(i = k, r = m): int8 codes as bfloat16, MN-major.  A thread holds 16 codes of each of 2 m, and stores their
-// two pieces in an order that gives eight lanes eight bank groups.
+// A(i = k, r = m): int8 codes as bfloat16, MN-major.  A thread holds 16 codes of one m, and stores their two
+// pieces in an order that gives eight lanes eight bank groups.
 struct CodesT {
   static constexpr bool kMN = true;
-  static constexpr int kSpan = 1, kRegs = 8;
+  static constexpr int kSpan = 1, kRegs = 4;
+  static_assert(kPass == kStep, "a pass is a step's tokens");
   const int8_t *codes;
   int64_t K, ld;
   int unit;
   struct Thread {
     const int8_t *p;
     uint32_t off, turn;
-    int m;
-    int64_t left;
+    int m, k;  // k: how many of the 16 are in range
   };
-  __device__ __forceinline__ Thread init(int64_t x0, int tid) const {
+  __device__ __forceinline__ Thread init(int64_t x0, int64_t r0, int tid) const {
     const int lane = tid & 31, m = (tid >> 5) * 4 + (lane >> 3), q = lane & 7;
-    return {codes + x0 + 16 * q, q * 2080u + (m >> 3) * 128u + (m & 7) * 16u, static_cast<uint32_t>(q >> 2), m, K - x0 - 16 * q};
+    const int64_t left = K - x0 - 16 * q;
+    return {codes + (r0 + m) * ld + x0 + 16 * q, q * 2080u + (m >> 3) * 128u + (m & 7) * 16u, static_cast<uint32_t>(q >> 2), m,
+            static_cast<int>(left < 16 ? left : 16)};
   }
-  __device__ __forceinline__ void load(const Thread &t, int64_t r0, int64_t r1, uint32_t (&w)[kRegs]) const {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      w[4 * u] = w[4 * u + 1] = w[4 * u + 2] = w[4 * u + 3] = 0;
-      if (r0 + t.m + 32 * u < r1 && t.left > 0)
-        load_codes(t.p + (r0 + t.m + 32 * u) * ld, static_cast<int>(t.left < 16 ? t.left : 16), unit, w + 4 * u);
-    }
+  __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
+    load_codes(t.p, t.m < left ? t.k : 0, unit, w);
+    t.p += kStep * ld;
   }
   __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool, uint32_t tile) const {
 #pragma unroll
-    for (int u = 0; u < 2; ++u)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const bool high = (h ^ t.turn) != 0;
-        uint32_t o[4];
-        codes4_bf16(high ? w[4 * u + 2] : w[4 * u], o[0], o[1]);
-        codes4_bf16(high ? w[4 * u + 3] : w[4 * u + 1], o[2], o[3]);
-        st_shared16(tile + t.off + (high ? 1040u : 0u) + u * 512u, o[0], o[1], o[2], o[3]);
-      }
+    for (int h = 0; h < 2; ++h) {
+      const bool high = (h ^ t.turn) != 0;
+      uint32_t o[4];
+      codes4_bf16(high ? w[2] : w[0], o[0], o[1]);
+      codes4_bf16(high ? w[3] : w[1], o[2], o[3]);
+      st_shared16(tile + t.off + (high ? 1040u : 0u), o[0], o[1], o[2], o[3]);
+    }
   }
 };
 
-// 8 elements at p as loaded words (4 of two 16-bit elements, or 8 of one), `left` of them in range (1 .. 8)
+// 8 elements at p as loaded words (4 of two 16-bit elements, or 8 of one), `left` of them in range
 template <typename T>
 constexpr int kWords8 = sizeof(T) == 4 ? 8 : 4;
 template <typename T>
 __device__ __forceinline__ void load_grad8(const T *p, int left, bool vec, uint32_t *w) {
+#pragma unroll
+  for (int i = 0; i < kWords8<T>; ++i) w[i] = 0;
+  if (left <= 0) return;
   if (vec) {
     const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p));
     w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
@@ -329,13 +328,12 @@ __device__ __forceinline__ void load_grad8(const T *p, int left, bool vec, uint3
     }
   } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = i < left ? __ldg(reinterpret_cast<const uint32_t *>(p) + i) : 0u;
+    for (int i = 0; i < 8; ++i)
+      if (i < left) w[i] = __ldg(reinterpret_cast<const uint32_t *>(p) + i);
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint16_t *h = reinterpret_cast<const uint16_t *>(p) + 2 * i;
-      w[i] = (2 * i < left ? static_cast<uint32_t>(__ldg(h)) : 0u) | (2 * i + 1 < left ? static_cast<uint32_t>(__ldg(h + 1)) << 16 : 0u);
-    }
+    for (int i = 0; i < 8; ++i)
+      if (i < left) w[i >> 1] |= static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t *>(p) + i)) << (16 * (i & 1));
   }
 }
 template <typename T>
@@ -350,12 +348,12 @@ __device__ __forceinline__ void grad8_f32(const uint32_t *w, float (&v)[8]) {
 }
 
 // B(j = m, r = n): gradients, K-major: 16-bit ones as they are, 32-bit ones in three pieces.  A thread holds
-// 8 elements of each of X / 32 rows.
+// 8 elements of each of X / kPass rows.
 template <typename T, int X>
 struct GradK {
   static constexpr bool kMN = false, kBf = !std::is_same_v<T, __half>;
   static constexpr int P = sizeof(T) == 4 ? 3 : 1;
-  static constexpr int kUnits = X / 32;
+  static constexpr int kUnits = X / kPass;
   static constexpr int kSpan = 1, kRegs = kWords8<T> * kUnits;
   const T *dy;
   int64_t M, ld;
@@ -363,94 +361,77 @@ struct GradK {
   struct Thread {
     const T *p;
     uint32_t off;
-    int n;
-    int64_t left;
+    int n, rows;
   };
-  __device__ __forceinline__ Thread init(int64_t x0, int tid) const {
+  __device__ __forceinline__ Thread init(int64_t x0, int64_t r0, int tid) const {
     const int lane = tid & 31, row = (tid >> 5) * 4 + (lane >> 3), q = lane & 7;
     const int64_t m = x0 + row;
-    return {dy + m * ld + 8 * q, (row >> 3) * 1152u + q * 144u + (row & 7) * 16u, 8 * q, M - m};
+    return {dy + m * ld + r0 + 8 * q, (row >> 3) * 1152u + q * 144u + (row & 7) * 16u, 8 * q, rows_left(M - m)};
   }
-  __device__ __forceinline__ void load(const Thread &t, int64_t r0, int64_t r1, uint32_t (&w)[kRegs]) const {
-    const int64_t left = r1 - r0 - t.n;
+  __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) {
-      uint32_t *o = w + kWords8<T> * u;
-#pragma unroll
-      for (int i = 0; i < kWords8<T>; ++i) o[i] = 0;
-      if (left > 0 && t.left > 32 * u) load_grad8<T>(t.p + r0 + 32 * u * ld, static_cast<int>(left < 8 ? left : 8), vec, o);
-    }
+    for (int u = 0; u < kUnits; ++u)
+      load_grad8<T>(t.p + u * kPass * ld, t.rows > kPass * u ? left - t.n : 0, vec, w + kWords8<T> * u);
+    t.p += kStep;
   }
   __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool, uint32_t tile) const {
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-      const uint32_t *o = w + kWords8<T> * u;
+      const uint32_t *o = w + kWords8<T> * u, at = tile + t.off + u * (kPass / 8 * 1152u);
       if constexpr (P == 1) {
-        st_shared16(tile + t.off + u * 4608u, o[0], o[1], o[2], o[3]);
+        st_shared16(at, o[0], o[1], o[2], o[3]);
       } else {
         float v[8];
         grad8_f32<T>(o, v);
-        split8<P>(v, tile + t.off + u * 4608u, tile_bytes(false, X));
+        split8<P>(v, at, tile_bytes(false, X));
       }
     }
   }
 };
 
 // B(j = n, r = m): gradients times their row's scale, in P bfloat16 pieces, MN-major.  A thread holds X / 64
-// groups of 8 columns of each of 2 m, and their scales.
+// groups of 8 columns of one m, and its scale.
 template <typename T, int X, int P_>
 struct GradT {
   static constexpr bool kMN = true, kBf = true;
   static constexpr int P = P_;
   static constexpr int kGroups = X / 64;
-  static constexpr int kSpan = 1, kRegs = 2 * kWords8<T> * kGroups + 2;
+  static constexpr int kSpan = 1, kRegs = kWords8<T> * kGroups + 1;
   const T *dy;
   int64_t N, ld;
   const float *scale;
   bool vec;
   struct Thread {
     const T *p;
+    const float *s;
     uint32_t off;
-    int m;
-    int64_t left;
+    int m, columns;
   };
-  __device__ __forceinline__ Thread init(int64_t x0, int tid) const {
+  __device__ __forceinline__ Thread init(int64_t x0, int64_t r0, int tid) const {
     const int lane = tid & 31, m = (tid >> 5) * 4 + (lane >> 3), q = lane & 7;
-    return {dy + x0 + 8 * q, q * 1040u + (m >> 3) * 128u + (m & 7) * 16u, m, N - x0 - 8 * q};
+    return {dy + (r0 + m) * ld + x0 + 8 * q, scale + r0 + m, q * 1040u + (m >> 3) * 128u + (m & 7) * 16u, m, rows_left(N - x0 - 8 * q)};
   }
-  __device__ __forceinline__ void load(const Thread &t, int64_t r0, int64_t r1, uint32_t (&w)[kRegs]) const {
+  __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
+    const bool live = t.m < left;
+    w[kRegs - 1] = live ? __float_as_uint(__ldg(t.s)) : 0u;
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int64_t m = r0 + t.m + 32 * h;
-      const bool live = m < r1;
-      w[kRegs - 2 + h] = live ? __float_as_uint(__ldg(scale + m)) : 0u;
-#pragma unroll
-      for (int u = 0; u < kGroups; ++u) {
-        uint32_t *o = w + kWords8<T> * (h * kGroups + u);
-#pragma unroll
-        for (int i = 0; i < kWords8<T>; ++i) o[i] = 0;
-        const int64_t left = t.left - 64 * u;
-        if (live && left > 0) load_grad8<T>(t.p + m * ld + 64 * u, static_cast<int>(left < 8 ? left : 8), vec, o);
-      }
-    }
+    for (int u = 0; u < kGroups; ++u) load_grad8<T>(t.p + 64 * u, live ? t.columns - 64 * u : 0, vec, w + kWords8<T> * u);
+    t.p += kStep * ld, t.s += kStep;
   }
   __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool, uint32_t tile) const {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int u = 0; u < kGroups; ++u) {
+      float v[8];
+      grad8_f32<T>(w + kWords8<T> * u, v);
 #pragma unroll
-      for (int u = 0; u < kGroups; ++u) {
-        float v[8];
-        grad8_f32<T>(w + kWords8<T> * (h * kGroups + u), v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] *= __uint_as_float(w[kRegs - 2 + h]);
-        split8<P>(v, tile + t.off + u * 8320u + h * 512u, tile_bytes(true, X));
-      }
+      for (int e = 0; e < 8; ++e) v[e] *= __uint_as_float(w[kRegs - 1]);
+      split8<P>(v, tile + t.off + u * 8320u, tile_bytes(true, X));
+    }
   }
 };
 
 // ----------------------------------------------------------------------------- epilogues
-// put(j, i, v): one element of the product; consecutive lanes hold consecutive i (in mixed order for
-// weights that run along i: `i` is the true one).
+// out(j, i) = product factor(j) + add(i)
 struct OutY {  // y[m][n] = v / 2 scale_m w_scale + b_n
   void *y;
   int dtype;
@@ -474,6 +455,25 @@ struct OutW {  // dW[n][k] = v
   __device__ __forceinline__ float factor(int64_t) const { return 1.0f; }
   __device__ __forceinline__ float add(int64_t) const { return 0.0f; }
 };
+// The CTA's accumulators, 32 lanes of i by kColumns of j a warp: to y (rows of j, `ld` apart), times the
+// column's factor, plus the lane's `add`
+template <typename T, int kColumns>
+__device__ __forceinline__ void put_tile(T *y, int64_t ld, int columns, bool live, uint32_t tmem, const float *factor, float add) {
+  constexpr int kGroup = kColumns < 16 ? kColumns : 16;
+  static_assert(kColumns % kGroup == 0 && kGroup >= 4, "columns of a warp");
+#pragma unroll 1
+  for (int c = 0; c < kColumns && c < columns; c += kGroup) {
+    float v[kGroup];
+    tmem_ld<kGroup>(tmem + c, v);
+    tmem_wait_ld();
+    if (!live) continue;
+#pragma unroll
+    for (int e = 0; e < kGroup; ++e) {
+      if (c + e < columns) *y = from_f32<T>(fmaf(v[e], factor[c + e], add));
+      y += ld;
+    }
+  }
+}
 __device__ __forceinline__ void put_element(void *y, int dtype, int64_t at, float v) {
   if (dtype == 0) static_cast<float *>(y)[at] = v;
   else if (dtype == 1) static_cast<__half *>(y)[at] = __float2half_rn(v);
@@ -497,7 +497,7 @@ template <class A, class B, int TB, int CG>
 struct GemmShape {
   static constexpr uint32_t kABytes = tile_bytes(A::kMN, kTileI), kPieceBytes = tile_bytes(B::kMN, TB / CG);
   static constexpr uint32_t kStageBytes = kABytes + B::P * kPieceBytes;
-  static constexpr uint32_t kBars = 256;
+  static constexpr uint32_t kBars = 256 + TB * 4;  // barriers and two words; the columns' factors
   static constexpr int fit(uint32_t room) { return static_cast<int>((room - kBars) / kStageBytes); }
   static constexpr uint32_t kHalfSm = kSmemPerSm / 2 - 1024;
   static constexpr int kCtasPerSm = fit(kHalfSm) >= 2 ? 2 : 1;
@@ -557,38 +557,44 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     return true;
   };
 
+  float *factor = reinterpret_cast<float *>(smem + S::kStages * S::kStageBytes + 256);
+  for (int c = tid; c < TB; c += kGemmThreads) factor[c] = g.partial ? 1.0f : j0 + c < g.J ? g.out.factor(j0 + c) : 0.0f;
   if (warp < kProducerWarps) {
-    const typename A::Thread ta = g.a.init(i0, tid);
-    const typename B::Thread tb = g.b.init(j0 + rank * (TB / CG), tid);
-    uint32_t ra[A::kRegs], rb[B::kRegs];
-    g.a.load(ta, first, end, ra);
-    g.b.load(tb, first, end, rb);
+    typename A::Thread ta = g.a.init(i0, first, tid);
+    typename B::Thread tb = g.b.init(j0 + rank * (TB / CG), first, tid);
     const uint32_t full0 = CG == 2 ? mapa_cluster(full, 0) : full;
-    int s = 0, parity = 1;
-    for (int it = 0; it < steps; it += kSpan) {
+    // kAhead spans in registers, in flight while the tensor cores work through the stages
+    constexpr int kAhead = A::kRegs + B::kRegs <= 12 ? 2 : 1;
+    uint32_t ra[kAhead][A::kRegs], rb[kAhead][B::kRegs];
+    int left = static_cast<int>(end - first);
 #pragma unroll
-      for (int h = 0; h < kSpan; ++h) {
-        const bool free = it + h < S::kStages || wait(empty + 8 * s, parity);
-        if (!__all_sync(0xffffffffu, free)) {
-          it = steps;
-          break;
+    for (int a = 0; a < kAhead; ++a, left -= kSpan * kStep) g.a.load(ta, left, ra[a]), g.b.load(tb, left, rb[a]);
+    int s = 0, parity = 1;
+    bool ok = true;
+    for (int it = 0; ok && it < steps; it += kAhead * kSpan) {
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) {
+        if (it + a * kSpan >= steps) break;
+#pragma unroll
+        for (int h = 0; h < kSpan; ++h) {
+          ok = ok && __all_sync(0xffffffffu, it + a * kSpan + h < S::kStages || wait(empty + 8 * s, parity));
+          if (!ok) break;
+          const uint32_t stage = base + s * S::kStageBytes;
+          g.a.store(ta, ra[a], h == 1, stage);
+          g.b.store(tb, rb[a], h == 1, stage + S::kABytes);
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            if constexpr (CG == 2) mbar_arrive_cluster(full0 + 8 * s);
+            else mbar_arrive(full + 8 * s);
+          }
+          if (++s == S::kStages) s = 0, parity ^= 1;
         }
-        const uint32_t stage = base + s * S::kStageBytes;
-        g.a.store(ta, ra, h == 1, stage);
-        g.b.store(tb, rb, h == 1, stage + S::kABytes);
-        fence_proxy_async_smem();
-        __syncwarp();
-        if (lane == 0) {
-          if constexpr (CG == 2) mbar_arrive_cluster(full0 + 8 * s);
-          else mbar_arrive(full + 8 * s);
-        }
-        if (++s == S::kStages) s = 0, parity ^= 1;
-      }
-      if (it + kSpan < steps) {  // the next span's, in flight while the tensor cores work through the stages
-        g.a.load(ta, first + static_cast<int64_t>(it + kSpan) * kStep, end, ra);
-        g.b.load(tb, first + static_cast<int64_t>(it + kSpan) * kStep, end, rb);
+        g.a.load(ta, left, ra[a]), g.b.load(tb, left, rb[a]);
+        left -= kSpan * kStep;
       }
     }
+    named_bar_sync(1, kProducers);  // (the factors)
   } else if (rank == 0) {
     constexpr uint32_t idesc = gemm_idesc(B::kBf, A::kMN, B::kMN, 128 * CG, TB);
     constexpr uint32_t la = tile_lbo(A::kMN), lb = tile_lbo(B::kMN);
@@ -612,35 +618,20 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   __syncwarp();
   const bool ready = __all_sync(0xffffffffu, wait(done, 0) && !word[1]);
   tc_fence_after();
-  if (warp < kProducerWarps) {
-    const int64_t row = 32 * (warp & 3) + lane;  // of the tile, and the lane of tensor memory
+  if (warp < kProducerWarps && ready) {
+    const int row = 32 * (warp & 3) + lane;  // of the tile, and the lane of tensor memory
     const int64_t i = i0 + (std::is_same_v<A, WeightsT> ? (row & ~7) | mix8(row & 7) : row);
-    const uint32_t tl = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16);
-    constexpr int kHalf = TB / 2;  // columns of each of the two warps of a lane quadrant
-    constexpr int kGroup = kHalf < 16 ? 8 : 16;
-    const int c0 = (warp >> 2) * kHalf;
-    const float add = !g.partial && i < g.I ? g.out.add(i) : 0.0f;
-    if (ready) {
-#pragma unroll 1
-      for (int c = c0; c < c0 + kHalf; c += kGroup) {
-        if (j0 + c >= g.J) break;
-        float v[kGroup];
-        tmem_ld<kGroup>(tl + c, v);
-        tmem_wait_ld();
-        if (i < g.I) {
-          if (g.partial) {
-            float *o = g.partial + (static_cast<int64_t>(blockIdx.y) * g.J + j0 + c) * g.I + i;
-#pragma unroll
-            for (int e = 0; e < kGroup; ++e)
-              if (j0 + c + e < g.J) o[e * g.I] = v[e];
-          } else {
-#pragma unroll
-            for (int e = 0; e < kGroup; ++e)
-              if (j0 + c + e < g.J) put_element(g.out.y, g.out.dtype, (j0 + c + e) * g.out.ld + i, v[e] * g.out.factor(j0 + c + e) + add);
-          }
-        }
-      }
-    }
+    constexpr int kColumns = TB / (kProducerWarps / 4);  // of each of the warps of a lane quadrant
+    const int c0 = (warp >> 2) * kColumns, columns = rows_left(g.J - j0 - c0);
+    const uint32_t tl = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + c0;
+    const bool live = i < g.I;
+    const float add = !g.partial && live ? g.out.add(i) : 0.0f;
+    const int64_t at = (j0 + c0) * g.out.ld + i;
+    if (g.partial)
+      put_tile<float, kColumns>(g.partial + (static_cast<int64_t>(blockIdx.y) * g.J + j0 + c0) * g.I + i, g.I, columns, live, tl, factor + c0, 0.0f);
+    else if (g.out.dtype == 0) put_tile<float, kColumns>(static_cast<float *>(g.out.y) + at, g.out.ld, columns, live, tl, factor + c0, add);
+    else if (g.out.dtype == 1) put_tile<__half, kColumns>(static_cast<__half *>(g.out.y) + at, g.out.ld, columns, live, tl, factor + c0, add);
+    else put_tile<__nv_bfloat16, kColumns>(static_cast<__nv_bfloat16 *>(g.out.y) + at, g.out.ld, columns, live, tl, factor + c0, add);
   }
   tc_fence_before();
   if constexpr (CG == 2) cluster_sync_all();
@@ -663,15 +654,15 @@ __global__ void __launch_bounds__(256) gemm_join_kernel(const float *partial, in
   }
 }
 
-// what every row of codes is a multiple of and starts on, for load_codes; and whether rows of gradients are
-// whole 16-byte pieces
+// the bytes that every row of codes or weights is a multiple of and starts on (load_codes, load_weights), and
+// whether rows of gradients are whole 16-byte pieces
 inline int codes_unit(const int8_t *codes, int64_t ld, int64_t K) {
   const uintptr_t all = reinterpret_cast<uintptr_t>(codes) | static_cast<uintptr_t>(ld) | static_cast<uintptr_t>(K);
   return (all & 15u) == 0 ? 16 : (all & 3u) == 0 ? 4 : 1;
 }
 inline int weights_unit(const uint8_t *packed, int64_t K) {
   const uintptr_t p = reinterpret_cast<uintptr_t>(packed);
-  return K % 64 == 0 && (p & 15u) == 0 ? 16 : K % 16 == 0 && (p & 3u) == 0 ? 4 : 1;
+  return K % 32 == 0 && (p & 7u) == 0 ? 8 : K % 16 == 0 && (p & 3u) == 0 ? 4 : 1;
 }
 template <typename T>
 bool grads_vec(const void *dy, int64_t ld, int64_t N) {

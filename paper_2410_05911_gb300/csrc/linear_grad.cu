@@ -47,7 +47,7 @@ constexpr int kSingle = sizeof(T) == 4 ? 128 : 256;
 
 template <typename T>
 cudaError_t input_grad(const AapLinearGradCall &c, float *work, cudaStream_t st) {
-  const WeightsT a = {c.packed, c.N, c.K, c.K % 32 == 0 && (reinterpret_cast<uintptr_t>(c.packed) & 7u) == 0};
+  const WeightsT a = {c.packed, c.N, c.K, weights_unit(c.packed, c.K)};
   const OutX out = {c.dx, c.dtype, c.K, c.w_scale};
   return with_tile<kSingle<T>>(c.K, c.M, [&](auto tb, auto cg) {
     constexpr int TB = decltype(tb)::value, CG = decltype(cg)::value;
