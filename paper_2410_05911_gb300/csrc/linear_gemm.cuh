@@ -516,9 +516,10 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   using S = GemmShape<A, B, TB, CG>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t base = smem_u32(smem);
-  const uint32_t bars = base + S::kStages * S::kStageBytes;  // full[stages], empty[stages], done; then 2 words
-  const uint32_t full = bars, empty = bars + 8 * S::kStages, done = bars + 16 * S::kStages;
-  volatile uint32_t *word = reinterpret_cast<volatile uint32_t *>(smem + S::kStages * S::kStageBytes + 16 * S::kStages + 8);
+  // full[stages] (this CTA's producers), peer[stages] (the other CTA's stage), empty[stages], done; 2 words
+  const uint32_t full = base + S::kStages * S::kStageBytes, peer = full + 8 * S::kStages, empty = peer + 8 * S::kStages,
+                 done = empty + 8 * S::kStages;
+  volatile uint32_t *word = reinterpret_cast<volatile uint32_t *>(smem + S::kStages * S::kStageBytes + 24 * S::kStages + 8);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = CG == 2 ? cluster_ctarank() : 0;
   const int64_t i0 = static_cast<int64_t>(blockIdx.x % g.tiles_i) * kTileI, j0 = static_cast<int64_t>(blockIdx.x / g.tiles_i) * TB;
@@ -527,7 +528,7 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   const int steps = kSpan * static_cast<int>((end - first + kSpan * kStep - 1) / (kSpan * kStep));
 
   if (tid == 0) {
-    for (int s = 0; s < S::kStages; ++s) mbar_init(full + 8 * s, CG * kProducerWarps), mbar_init(empty + 8 * s, 1);
+    for (int s = 0; s < S::kStages; ++s) mbar_init(full + 8 * s, kProducerWarps), mbar_init(peer + 8 * s, 1), mbar_init(empty + 8 * s, 1);
     mbar_init(done, 1);
     fence_mbar_init_cluster();
     word[1] = 0;
@@ -562,7 +563,6 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   if (warp < kProducerWarps) {
     typename A::Thread ta = g.a.init(i0, first, tid);
     typename B::Thread tb = g.b.init(j0 + rank * (TB / CG), first, tid);
-    const uint32_t full0 = CG == 2 ? mapa_cluster(full, 0) : full;
     // kAhead spans in registers, in flight while the tensor cores work through the stages
     constexpr int kAhead = A::kRegs + B::kRegs <= 12 ? 2 : 1;
     uint32_t ra[kAhead][A::kRegs], rb[kAhead][B::kRegs];
@@ -582,12 +582,8 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
           const uint32_t stage = base + s * S::kStageBytes;
           g.a.store(ta, ra[a], h == 1, stage);
           g.b.store(tb, rb[a], h == 1, stage + S::kABytes);
-          fence_proxy_async_smem();
           __syncwarp();
-          if (lane == 0) {
-            if constexpr (CG == 2) mbar_arrive_cluster(full0 + 8 * s);
-            else mbar_arrive(full + 8 * s);
-          }
+          if (lane == 0) mbar_arrive(full + 8 * s);
           if (++s == S::kStages) s = 0, parity ^= 1;
         }
         g.a.load(ta, left, ra[a]), g.b.load(tb, left, rb[a]);
@@ -595,25 +591,36 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
       }
     }
     named_bar_sync(1, kProducers);  // (the factors)
-  } else if (rank == 0) {
+  } else {
+    // A stage that the producers have written becomes the tensor cores' with one fence between the proxies, here,
+    // and not one in every producer, where it would also wait for the loads in flight.  In the second CTA
+    // that is all; it tells the first.
     constexpr uint32_t idesc = gemm_idesc(B::kBf, A::kMN, B::kMN, 128 * CG, TB);
     constexpr uint32_t la = tile_lbo(A::kMN), lb = tile_lbo(B::kMN);
+    const uint32_t peer0 = CG == 2 ? mapa_cluster(peer, 0) : peer;
     int s = 0, parity = 0;
     for (int it = 0; it < steps; ++it) {
       if (!__all_sync(0xffffffffu, wait(full + 8 * s, parity))) break;
-      tc_fence_after();
-      const uint32_t at = base + s * S::kStageBytes, bt = at + S::kABytes;
+      fence_proxy_async_smem();
+      if (rank == 0) {
+        if (CG == 2 && !__all_sync(0xffffffffu, wait(peer + 8 * s, parity))) break;
+        tc_fence_after();
+        const uint32_t at = base + s * S::kStageBytes, bt = at + S::kABytes;
 #pragma unroll
-      for (int p = 0; p < P; ++p)
+        for (int p = 0; p < P; ++p)
 #pragma unroll
-        for (int ks = 0; ks < kStep / 16; ++ks)
-          mma_f16_cg_warp<CG>(tmem, make_sdesc(at + ks * 2 * la, la, tile_sbo(A::kMN)),
-                              make_sdesc(bt + p * S::kPieceBytes + ks * 2 * lb, lb, tile_sbo(B::kMN)), idesc,
-                              it > 0 || p > 0 || ks > 0 ? 1u : 0u);
-      mma_commit_cg_warp<CG>(empty + 8 * s);
+          for (int ks = 0; ks < kStep / 16; ++ks)
+            mma_f16_cg_warp<CG>(tmem, make_sdesc(at + ks * 2 * la, la, tile_sbo(A::kMN)),
+                                make_sdesc(bt + p * S::kPieceBytes + ks * 2 * lb, lb, tile_sbo(B::kMN)), idesc,
+                                it > 0 || p > 0 || ks > 0 ? 1u : 0u);
+        mma_commit_cg_warp<CG>(empty + 8 * s);
+      } else {
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(peer0 + 8 * s);
+      }
       if (++s == S::kStages) s = 0, parity ^= 1;
     }
-    mma_commit_cg_warp<CG>(done);
+    if (rank == 0) mma_commit_cg_warp<CG>(done);
   }
   __syncwarp();
   const bool ready = __all_sync(0xffffffffu, wait(done, 0) && !word[1]);
