@@ -7,7 +7,7 @@
 //   db[n]    = sum_m dy[m, n]
 //
 // The three products run on the tensor cores (linear_gemm.cuh).  The forward sum is one of integers up to
-// 2 * 127 * 65536 < 2^24: exact in 32 bits, and the same however it is split.
+// 127 * 65536 < 2^23: exact in 32 bits, and the same however it is split.
 #include <cuda_runtime.h>
 
 #include <atomic>

@@ -56,23 +56,34 @@ __device__ __forceinline__ void st_shared16(uint32_t addr, uint32_t a, uint32_t 
 }
 
 // ----------------------------------------------------------------------------- conversions
-// 2-bit weights (00 = 0, 01 = +1, 11 = -1) as 16-bit floats of twice their value, 0 and +-2: their low bytes
-// are zero in half and in bfloat16 alike, so that one byte permutation makes two of them, with the codes as
-// selectors into a table of high bytes.  The two come from one field of neighbouring bytes, so position
-// 2 p + h of 8 weights holds weight 4 h + p; mix8 is that order.
-__host__ __device__ constexpr int mix8(int pos) { return ((pos & 1) << 2) | (pos >> 1); }
-// weights 0 .. 7 (the low half) or 8 .. 15 of a word
-__device__ __forceinline__ void weights8(uint32_t w, bool high, uint32_t (&o)[4]) {
-  constexpr uint32_t table = 0xC0004000u;
+// 16 2-bit weights (00 = 0, 01 = +1, 11 = -1, 10 = 0) of a word as 16-bit floats, two at a time: fields f and f + 8
+// sit at the same place of the word's halves, in the low bits of a mantissa where the exponent makes them
+// integers (1024 + x: 10 bits of a half; 128 + x: 7 bits of a bfloat16), so that one logical operation takes both
+// fields, with their high bit turned over (0, 1, -1 become 2, 3, 1), and one multiply-add brings them down by
+// 4^f and subtracts 2.  No shift until the mantissa's bits run out.  o[p] holds
+// weights f and f + 8 for f = p, or f = 4 + p where `high`; mix16 is the order of both in a row.
+__host__ __device__ constexpr int mix16(int pos) { return ((pos & 1) << 3) | ((pos >> 3) << 2) | ((pos >> 1) & 3); }
+template <bool BF>
+__device__ __forceinline__ void weights4(uint32_t w, bool high, uint32_t (&o)[4]) {
+  w &= 0x55555555u | (w + w);  // 10 is 00
+  constexpr int kFields = BF ? 3 : 5;
 #pragma unroll
   for (int p = 0; p < 4; ++p) {
-    const int by = (high ? 16 : 0) + 2 * p - 4;  // to selector bits 4, 5 and 12, 13
-    const uint32_t s = (by < 0 ? w << -by : w >> by) & 0x3030u;
-    o[p] = __byte_perm(table, 0, s);
+    const int f = (high ? 4 : 0) + p, g = f % kFields;
+    const uint32_t x = w >> (2 * (f - g));
+    const uint32_t u = (x & (0x00030003u << (2 * g))) ^ ((BF ? 0x43004300u : 0x64006400u) | (0x00020002u << (2 * g)));
+    const float by = 1.0f / static_cast<float>(1 << (2 * g)), less = -((BF ? 128.0f : 1024.0f) * by + 2.0f);
+    if constexpr (BF) {
+      const __nv_bfloat162 v = __hfma2(*reinterpret_cast<const __nv_bfloat162 *>(&u), __float2bfloat162_rn(by), __float2bfloat162_rn(less));
+      o[p] = *reinterpret_cast<const uint32_t *>(&v);
+    } else {
+      const __half2 v = __hfma2(*reinterpret_cast<const __half2 *>(&u), __float2half2_rn(by), __float2half2_rn(less));
+      o[p] = *reinterpret_cast<const uint32_t *>(&v);
+    }
   }
 }
-// 8 int8 codes as halves in the order of mix8: (code + 128) in the low byte of 1024, less 1152
-__device__ __forceinline__ void codes8_half_mixed(uint32_t b0, uint32_t b1, uint32_t (&o)[4]) {
+// 4 + 4 int8 codes of two words as halves, codes p of both in o[p]: (code + 128) in the low byte of 1024, less 1152
+__device__ __forceinline__ void codes8_half(uint32_t b0, uint32_t b1, uint32_t (&o)[4]) {
 #pragma unroll
   for (int p = 0; p < 4; ++p) {
     const uint32_t t = __byte_perm(b0, b1, 0x0400u + 0x0101u * p);
@@ -122,8 +133,9 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint32_t addr, uint3
 // Each has kMN (16-byte rows run along x), kSpan (steps that one load feeds), kRegs (a thread's registers
 // of them), init(x0, r0, tid), load(thread, left, regs): the next span, of `left` r that are in range, zeros
 // beyond; and store(thread, regs, step of the span, tile).  A B also has kBf (bfloat16 or half) and P
-// (pieces of an element).  The forward product's operands span two steps: the first takes the low 8 of every
-// 16 k, the second the high 8, so that a load is 16 bytes of codes and a row's 128 bytes are one line.
+// (pieces of an element), an A kMixed (its rows are in the order of mix16).  The forward product's operands span two steps: the first takes k = 0 .. 3 and
+// 8 .. 11 of every 16 k, the second the others, so that a load is 16 bytes of codes and a row's 128 bytes are
+// one line.
 
 // 2-bit weights at p, 4 W bytes, `left` weights in range (a multiple of 4).  unit: 8 or 4 bytes that every
 // row is a multiple of, or 1
@@ -152,7 +164,7 @@ __device__ __forceinline__ void load_weights(const uint8_t *p, int left, int uni
 
 // A(i = n, r = k): 2-bit weights, K-major, mixed order along k.  A thread holds 32 weights of one row.
 struct WeightsK {
-  static constexpr bool kMN = false;
+  static constexpr bool kMN = false, kMixed = false;
   static constexpr int kSpan = 2, kRegs = 2;
   const uint8_t *packed;
   int64_t N, K;
@@ -175,16 +187,17 @@ struct WeightsK {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       uint32_t o[4];
-      weights8(w[g], second, o);
+      weights4<false>(w[g], second, o);
       st_shared16(tile + t.off + g * 144u, o[0], o[1], o[2], o[3]);
     }
   }
 };
 
-// A(i = k, r = n): the same weights, MN-major; row i of the tile is k = i with its low 3 bits mixed.
-// A thread holds 16 k of one n.
+// A(i = k, r = n): the same weights as bfloat16 or half, MN-major; row i of the tile is k = i with its low 4
+// bits mixed.  A thread holds 16 k of one n.
+template <bool BF>
 struct WeightsT {
-  static constexpr bool kMN = true;
+  static constexpr bool kMN = true, kMixed = true;
   static constexpr int kSpan = 1, kRegs = 1;
   const uint8_t *packed;
   int64_t N, K;
@@ -208,7 +221,7 @@ struct WeightsT {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       uint32_t o[4];
-      weights8(w[0], g, o);
+      weights4<BF>(w[0], g == 1, o);
       st_shared16(tile + t.off + g * 1040u, o[0], o[1], o[2], o[3]);
     }
   }
@@ -269,7 +282,7 @@ struct CodesK {
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
       uint32_t o[4];
-      codes8_half_mixed(second ? w[4 * u + 2] : w[4 * u], second ? w[4 * u + 3] : w[4 * u + 1], o);
+      codes8_half(second ? w[4 * u + 1] : w[4 * u], second ? w[4 * u + 3] : w[4 * u + 2], o);
       st_shared16(tile + t.off + u * (kPass / 8 * 1152u), o[0], o[1], o[2], o[3]);
     }
   }
@@ -278,7 +291,7 @@ struct CodesK {
 // A(i = k, r = m): int8 codes as bfloat16, MN-major.  A thread holds 16 codes of one m, and stores their two
 // pieces in an order that gives eight lanes eight bank groups.
 struct CodesT {
-  static constexpr bool kMN = true;
+  static constexpr bool kMN = true, kMixed = false;
   static constexpr int kSpan = 1, kRegs = 4;
   static_assert(kPass == kStep, "a pass is a step's tokens");
   const int8_t *codes;
@@ -432,20 +445,20 @@ struct GradT {
 
 // ----------------------------------------------------------------------------- epilogues
 // out(j, i) = product factor(j) + add(i)
-struct OutY {  // y[m][n] = v / 2 scale_m w_scale + b_n
+struct OutY {  // y[m][n] = v scale_m w_scale + b_n
   void *y;
   int dtype;
   int64_t ld;
   const float *scale, *w_scale, *bias;
-  __device__ __forceinline__ float factor(int64_t j) const { return __ldg(scale + j) * __ldg(w_scale) * 0.5f; }
+  __device__ __forceinline__ float factor(int64_t j) const { return __ldg(scale + j) * __ldg(w_scale); }
   __device__ __forceinline__ float add(int64_t i) const { return bias ? __ldg(bias + i) : 0.0f; }
 };
-struct OutX {  // dx[m][k] = v / 2 w_scale
+struct OutX {  // dx[m][k] = v w_scale
   void *y;
   int dtype;
   int64_t ld;
   const float *w_scale;
-  __device__ __forceinline__ float factor(int64_t) const { return __ldg(w_scale) * 0.5f; }
+  __device__ __forceinline__ float factor(int64_t) const { return __ldg(w_scale); }
   __device__ __forceinline__ float add(int64_t) const { return 0.0f; }
 };
 struct OutW {  // dW[n][k] = v
@@ -627,7 +640,7 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   tc_fence_after();
   if (warp < kProducerWarps && ready) {
     const int row = 32 * (warp & 3) + lane;  // of the tile, and the lane of tensor memory
-    const int64_t i = i0 + (std::is_same_v<A, WeightsT> ? (row & ~7) | mix8(row & 7) : row);
+    const int64_t i = i0 + (A::kMixed ? (row & ~15) | mix16(row & 15) : row);
     constexpr int kColumns = TB / (kProducerWarps / 4);  // of each of the warps of a lane quadrant
     const int c0 = (warp >> 2) * kColumns, columns = rows_left(g.J - j0 - c0);
     const uint32_t tl = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + c0;

@@ -47,13 +47,14 @@ constexpr int kSingle = sizeof(T) == 4 ? 128 : 256;
 
 template <typename T>
 cudaError_t input_grad(const AapLinearGradCall &c, float *work, cudaStream_t st) {
-  const WeightsT a = {c.packed, c.N, c.K, weights_unit(c.packed, c.K)};
+  using A = WeightsT<GradK<T, 64>::kBf>;
+  const A a = {c.packed, c.N, c.K, weights_unit(c.packed, c.K)};
   const OutX out = {c.dx, c.dtype, c.K, c.w_scale};
   return with_tile<kSingle<T>>(c.K, c.M, [&](auto tb, auto cg) {
     constexpr int TB = decltype(tb)::value, CG = decltype(cg)::value;
     using B = GradK<T, TB / CG>;
     const B b = {static_cast<const T *>(c.dy), c.M, c.lddy, grads_vec<T>(c.dy, c.lddy, c.N)};
-    return launch_gemm<WeightsT, B, OutX, TB, CG>(c.K, c.M, c.N, a, b, out, work, sm_count(), linear_status(), st);
+    return launch_gemm<A, B, OutX, TB, CG>(c.K, c.M, c.N, a, b, out, work, sm_count(), linear_status(), st);
   });
 }
 
@@ -61,7 +62,8 @@ template <typename T>
 int64_t input_grad_workspace(int64_t M, int64_t K, int64_t N) {
   return with_tile<kSingle<T>>(K, M, [&](auto tb, auto cg) {
     constexpr int TB = decltype(tb)::value, CG = decltype(cg)::value;
-    const GemmPlan p = gemm_plan<WeightsT, GradK<T, TB / CG>, TB, CG>(K, M, N, sm_count());
+    using B = GradK<T, TB / CG>;
+    const GemmPlan p = gemm_plan<WeightsT<B::kBf>, B, TB, CG>(K, M, N, sm_count());
     return p.splits > 1 ? p.splits * M * K : int64_t(0);
   });
 }
