@@ -347,8 +347,8 @@ struct AapLinearGradCall {
 int64_t aap_linear_workspace(int64_t M, int64_t K, int64_t N);
 cudaError_t launch_aap_linear(const AapLinearCall &c, cudaStream_t stream);
 int *linear_status();  // host memory: 1 once a wait in a kernel of these has given up; NULL without memory
-int64_t weight_grad_workspace(int64_t M, int64_t K, int64_t N, int wdtype);  // floats
-cudaError_t launch_weight_grad(const AapLinearGradCall &c, float *work, cudaStream_t stream);
+int64_t weight_grad_workspace(int64_t M, int64_t K, int64_t N, int wdtype);
+cudaError_t launch_weight_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t stream);
 int64_t aap_linear_grad_workspace(int64_t M, int64_t K, int64_t N, int dtype, int wdtype);
 cudaError_t launch_aap_linear_grad(const AapLinearGradCall &c, cudaStream_t stream);
 

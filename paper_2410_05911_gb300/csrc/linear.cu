@@ -20,34 +20,48 @@ namespace aecct {
 
 namespace {
 
-// the tile: few tokens take a narrow one, whose rest would be converted zeros
+using Staged = Tiled<128, false, false, 1, WeightsK::kSpan>;
+
+// a single CTA's tile: 16 tokens where there are no more
 template <class F>
-auto with_forward_tile(int64_t M, int64_t N, const F &f) {
-  if (M <= 16) return f(std::integral_constant<int, 16>(), std::integral_constant<int, 1>());
-  if (M > 64 && M <= 128) return f(std::integral_constant<int, 128>(), std::integral_constant<int, 1>());
-  return with_tile<256>(N, M, f);
+auto with_forward_tile(int64_t M, const F &f) {
+  if (M <= 16) return f(std::integral_constant<int, 16>());
+  return with_single_tile(M, f);
+}
+
+int64_t partial_bytes(const GemmPlan &p, int64_t M, int64_t N) {
+  return p.splits > 1 ? p.splits * M * N * static_cast<int64_t>(sizeof(float)) : 0;
 }
 
 }  // namespace
 
+// the splits' sums, and before them the staged codes
 int64_t aap_linear_workspace(int64_t M, int64_t K, int64_t N) {
   const int sms = sm_count();
-  return with_forward_tile(M, N, [&](auto tb, auto cg) {
-    constexpr int TB = decltype(tb)::value, CG = decltype(cg)::value;
-    const GemmPlan p = gemm_plan<WeightsK, CodesK<TB / CG>, TB, CG>(N, M, K, sms);
-    return p.splits > 1 ? p.splits * M * N * static_cast<int64_t>(sizeof(float)) : int64_t(0);
+  if (pair_tiles(N, M)) return partial_bytes(gemm_plan<WeightsK, Staged, 256, 2>(N, M, K, sms), M, N) + 2 * M * staged_k(K);
+  return with_forward_tile(M, [&](auto tb) {
+    constexpr int TB = decltype(tb)::value;
+    return partial_bytes(gemm_plan<WeightsK, CodesK<TB>, TB, 1>(N, M, K, sms), M, N);
   });
 }
 
 cudaError_t launch_aap_linear(const AapLinearCall &c, cudaStream_t st) {
   const WeightsK a = {c.packed, c.N, c.K, weights_unit(c.packed, c.K)};
   const OutY out = {c.y, c.dtype, c.N, c.scale, c.w_scale, c.bias};
-  return with_forward_tile(c.M, c.N, [&](auto tb, auto cg) {
-    constexpr int TB = decltype(tb)::value, CG = decltype(cg)::value;
-    using B = CodesK<TB / CG>;
-    const B b = {c.codes, c.M, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
-    return launch_gemm<WeightsK, B, OutY, TB, CG>(c.N, c.M, c.K, a, b, out, static_cast<float *>(c.workspace), sm_count(),
-                                                  linear_status(), st);
+  const int sms = sm_count();
+  if (pair_tiles(c.N, c.M)) {
+    cudaError_t e = launch_stage_codes(c.codes, c.ldc, c.M, c.K, c.workspace, st);
+    if (e != cudaSuccess) return e;
+    Staged b;
+    if ((e = tensor_map(&b.map, c.workspace, false, staged_k(c.K), c.M, staged_k(c.K), 1, Staged::X)) != cudaSuccess) return e;
+    float *partial = reinterpret_cast<float *>(static_cast<uint8_t *>(c.workspace) + 2 * c.M * staged_k(c.K));
+    return launch_gemm<WeightsK, Staged, OutY, 256, 2>(c.N, c.M, c.K, a, b, out, partial, sms, linear_status(), st);
+  }
+  return with_forward_tile(c.M, [&](auto tb) {
+    constexpr int TB = decltype(tb)::value;
+    const CodesK<TB> b = {c.codes, c.M, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
+    return launch_gemm<WeightsK, CodesK<TB>, OutY, TB, 1>(c.N, c.M, c.K, a, b, out, static_cast<float *>(c.workspace), sms,
+                                                         linear_status(), st);
   });
 }
 

@@ -10,8 +10,9 @@
 //
 // A CTA makes a tile of 128 i by TB j; from 256 of both on, a cluster of two makes 256 by 256 (cta_group::2),
 // each CTA with its own 128 rows of A and half of B in shared memory, so that a B is converted and stored by one
-// of two SMs.  Sixteen producer warps load ahead, convert and store; another warp (of the first
-// CTA) issues the MMAs.  Lanes hold consecutive i in tensor memory, so that the epilogue's stores of one j are 32
+// of two SMs.  Two groups of eight producer warps take the spans of r in turn (a warp's waits and its
+// arrivals cost it some 700 cycles a stage, whatever it stores in between): each loads its next span while the
+// other stores, converts and stores; another warp (of the first CTA) issues the MMAs.  Lanes hold consecutive i in tensor memory, so that the epilogue's stores of one j are 32
 // neighbouring elements.  Two CTAs share an SM where their operands fit, one's epilogue behind the other's
 // products.
 //
@@ -24,7 +25,10 @@
 #pragma once
 #include <cuda_runtime.h>
 
+#include <climits>
 #include <cstdint>
+
+#include <cuda.h>
 
 #include "aecct_internal.h"
 #include "rowtypes.cuh"
@@ -34,15 +38,18 @@ namespace aecct {
 
 constexpr int kStep = 64;           // r per stage
 constexpr int kTileI = 128;         // i per CTA: the lanes of tensor memory
-constexpr int kProducerWarps = 16;
+constexpr int kGroups = 2;          // of producers, which take the spans of r in turn
+constexpr int kGroupWarps = 8;
+constexpr int kProducerWarps = kGroups * kGroupWarps;
 constexpr int kProducers = kProducerWarps * 32;
-constexpr int kGemmThreads = kProducers + 32;
-constexpr int kPass = kProducerWarps * 4;  // rows of 8 lanes that the producers hold at a time
+constexpr int kGemmThreads = kProducers + 64;  // and the warps of the MMAs and of the copies
+constexpr int kPass = kGroupWarps * 4;  // rows of 8 lanes that a group holds at a time
 // a tile of x rows, and its descriptor's strides
 __host__ __device__ constexpr uint32_t tile_bytes(bool mn, int x) { return x / 8 * (mn ? 1040u : 1152u); }
 __host__ __device__ constexpr uint32_t tile_lbo(bool mn) { return mn ? 128u : 144u; }
 __host__ __device__ constexpr uint32_t tile_sbo(bool mn) { return mn ? 1040u : 1152u; }
-constexpr long long kGemmWaitCycles = 1ll << 32;  // a wait that takes longer (about 2 s) has lost its arrival
+constexpr uint32_t kGemmWaitNs = 10000;   // a wait looks again after this long at the latest
+constexpr int kGemmWaitTries = 1 << 20;   // and has lost its arrival after so many looks (tenths of a second at least)
 
 // instruction descriptor of kind::f16: 32-bit accumulators; BF: bfloat16 operands, else half; MN: both
 // operands' 16-byte rows run along i and j
@@ -106,18 +113,18 @@ __device__ __forceinline__ void codes4_bf16(uint32_t b, uint32_t &o0, uint32_t &
 // cuts off 8 bits and the next takes what is left, so that three hold a 32-bit value exactly.  An infinity
 // stays one in its first piece, and its others are zero.
 template <int P>
-__device__ __forceinline__ void split8(const float (&v)[8], uint32_t addr, uint32_t piece_bytes) {
+__device__ __forceinline__ void split8(const float (&v)[8], uint32_t (&o)[P][4]) {
   if constexpr (P == 1) {
-    st_shared16(addr, pack2<__nv_bfloat16>(v[0], v[1]), pack2<__nv_bfloat16>(v[2], v[3]), pack2<__nv_bfloat16>(v[4], v[5]),
-                pack2<__nv_bfloat16>(v[6], v[7]));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[0][i] = pack2<__nv_bfloat16>(v[2 * i], v[2 * i + 1]);
   } else {
     uint32_t x[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) x[e] = v[e] == v[e] ? __float_as_uint(v[e]) : 0x7FC00000u;
 #pragma unroll
     for (int p = 0; p < P; ++p) {
-      st_shared16(addr + p * piece_bytes, __byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632),
-                  __byte_perm(x[4], x[5], 0x7632), __byte_perm(x[6], x[7], 0x7632));
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[p][i] = __byte_perm(x[2 * i], x[2 * i + 1], 0x7632);
       if (p + 1 < P) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -128,30 +135,31 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint32_t addr, uint3
     }
   }
 }
+template <int P>
+__device__ __forceinline__ void store_split8(const float (&v)[8], uint32_t addr, uint32_t piece_bytes) {
+  uint32_t o[P][4];
+  split8<P>(v, o);
+#pragma unroll
+  for (int p = 0; p < P; ++p) st_shared16(addr + p * piece_bytes, o[p][0], o[p][1], o[p][2], o[p][3]);
+}
 
 // ----------------------------------------------------------------------------- operands
 // Each has kMN (16-byte rows run along x), kSpan (steps that one load feeds), kRegs (a thread's registers
-// of them), init(x0, r0, tid), load(thread, left, regs): the next span, of `left` r that are in range, zeros
-// beyond; and store(thread, regs, step of the span, tile).  A B also has kBf (bfloat16 or half) and P
-// (pieces of an element), an A kMixed (its rows are in the order of mix16).  The forward product's operands span two steps: the first takes k = 0 .. 3 and
-// 8 .. 11 of every 16 k, the second the others, so that a load is 16 bytes of codes and a row's 128 bytes are
-// one line.
+// of them), init(x0, r0, tid), full(thread, regs): the next span, every r in range and every row whole 16-byte
+// (weights: 8-byte) pieces, in plain loads; load(thread, left, regs): the same where only `left` r are in range,
+// or rows are not such, zeros beyond; aligned(): rows are; and store(thread, regs, step of the span, tile).
+// A row or column of the tile past the operand's last one reads that one again: its products are dropped.
+// A B also has kBf (bfloat16 or half) and P (pieces of an element), an A kMixed (its rows are in the order of
+// mix16).  The forward product's operands span two steps: the first takes k = 0 .. 3 and 8 .. 11 of every 16 k, the
+// second the others, so that a load is 16 bytes of codes and a row's 128 bytes are one line.
 
-// 2-bit weights at p, 4 W bytes, `left` weights in range (a multiple of 4).  unit: 8 or 4 bytes that every
+// 2-bit weights at p, 4 W bytes, `left` weights in range (a multiple of 4).  unit: 16, 8 or 4 bytes that every
 // row is a multiple of, or 1
 template <int W>
 __device__ __forceinline__ void load_weights(const uint8_t *p, int left, int unit, uint32_t (&w)[W]) {
 #pragma unroll
   for (int i = 0; i < W; ++i) w[i] = 0;
-  if (left <= 0) return;
-  if (unit == 8) {
-    if constexpr (W == 2) {
-      const uint2 v = __ldg(reinterpret_cast<const uint2 *>(p));
-      w[0] = v.x, w[1] = v.y;
-    } else {
-      w[0] = __ldg(reinterpret_cast<const uint32_t *>(p));
-    }
-  } else if (unit == 4) {
+  if (unit >= 4) {
 #pragma unroll
     for (int i = 0; i < W; ++i)
       if (16 * i < left) w[i] = __ldg(reinterpret_cast<const uint32_t *>(p) + i);
@@ -162,10 +170,10 @@ __device__ __forceinline__ void load_weights(const uint8_t *p, int left, int uni
   }
 }
 
-// A(i = n, r = k): 2-bit weights, K-major, mixed order along k.  A thread holds 32 weights of one row.
+// A(i = n, r = k): 2-bit weights, K-major, mixed order along k.  A thread holds 64 weights of one row.
 struct WeightsK {
   static constexpr bool kMN = false, kMixed = false;
-  static constexpr int kSpan = 2, kRegs = 2;
+  static constexpr int kSpan = 2, kRegs = 4;
   const uint8_t *packed;
   int64_t N, K;
   int unit;
@@ -174,18 +182,24 @@ struct WeightsK {
     uint32_t off;
     int k;
   };
+  bool aligned() const { return unit == 16; }
   __device__ __forceinline__ Thread init(int64_t x0, int64_t r0, int tid) const {
-    const int lane = tid & 31, row = (tid >> 5) * 8 + (lane & 7), q = lane >> 3;
-    const int64_t n = x0 + row;  // (a row past the last one holds nothing in range)
-    return {packed + (n * K + r0 >> 2) + q * 8, (row >> 3) * 1152u + q * 288u + (row & 7) * 16u, n < N ? q * 32 : 1 << 30};
+    const int lane = tid & 31, row = (tid >> 5) * 16 + ((lane >> 4) << 3) + (lane & 7), half = (lane >> 3) & 1;
+    const int64_t n = x0 + row < N ? x0 + row : N - 1;
+    return {packed + ((n * K + r0) >> 2) + half * 16, (row >> 3) * 1152u + half * 576u + (row & 7) * 16u, half * 64};
+  }
+  __device__ __forceinline__ void full(Thread &t, uint32_t (&w)[kRegs]) const {
+    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(t.p));
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    t.p += kGroups * kSpan * kStep / 4;
   }
   __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
-    load_weights<2>(t.p, left - t.k, unit, w);
-    t.p += kSpan * kStep / 4;
+    load_weights<4>(t.p, left - t.k, unit, w);
+    t.p += kGroups * kSpan * kStep / 4;
   }
   __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool second, uint32_t tile) const {
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
+    for (int g = 0; g < 4; ++g) {
       uint32_t o[4];
       weights4<false>(w[g], second, o);
       st_shared16(tile + t.off + g * 144u, o[0], o[1], o[2], o[3]);
@@ -194,34 +208,40 @@ struct WeightsK {
 };
 
 // A(i = k, r = n): the same weights as bfloat16 or half, MN-major; row i of the tile is k = i with its low 4
-// bits mixed.  A thread holds 16 k of one n.
+// bits mixed.  A thread holds 32 k of one n.
 template <bool BF>
 struct WeightsT {
   static constexpr bool kMN = true, kMixed = true;
-  static constexpr int kSpan = 1, kRegs = 1;
+  static constexpr int kSpan = 1, kRegs = 2;
   const uint8_t *packed;
   int64_t N, K;
   int unit;
   struct Thread {
     const uint8_t *p;
     uint32_t off;
-    int n, k;  // k: how many of the 16 are in range
+    int n, k;  // k: how many of the 32 are in range
   };
+  bool aligned() const { return unit >= 8; }
   __device__ __forceinline__ Thread init(int64_t x0, int64_t r0, int tid) const {
-    const int lane = tid & 31, warp = tid >> 5, n = (warp >> 1) * 8 + (lane & 7), q = (warp & 1) * 4 + (lane >> 3);
-    const int64_t k = x0 + 16 * q, left = K - k;
-    return {packed + ((r0 + n) * K + k >> 2), q * 2080u + (n >> 3) * 128u + (n & 7) * 16u, n,
-            static_cast<int>(left < 16 ? left : 16)};
+    const int lane = tid & 31, n = (tid >> 5) * 8 + (lane & 7), q = lane >> 3;
+    const int64_t left = K - x0 - 32 * q, k = left > 0 ? x0 + 32 * q : K - (K < 32 ? K : 32);
+    return {packed + (((r0 + n) * K + k) >> 2), q * 4160u + (n >> 3) * 128u + (n & 7) * 16u, n,
+            static_cast<int>(left < 32 ? left : 32)};
+  }
+  __device__ __forceinline__ void full(Thread &t, uint32_t (&w)[kRegs]) const {
+    const uint2 v = __ldg(reinterpret_cast<const uint2 *>(t.p));
+    w[0] = v.x, w[1] = v.y;
+    t.p += kGroups * kStep / 4 * K;
   }
   __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
-    load_weights<1>(t.p, t.n < left ? t.k : 0, unit, w);
-    t.p += kStep / 4 * K;
+    load_weights<2>(t.p, t.n < left ? t.k : 0, unit, w);
+    t.p += kGroups * kStep / 4 * K;
   }
   __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool, uint32_t tile) const {
 #pragma unroll
-    for (int g = 0; g < 2; ++g) {
+    for (int g = 0; g < 4; ++g) {
       uint32_t o[4];
-      weights4<BF>(w[0], g == 1, o);
+      weights4<BF>(w[g >> 1], g & 1, o);
       st_shared16(tile + t.off + g * 1040u, o[0], o[1], o[2], o[3]);
     }
   }
@@ -255,7 +275,7 @@ __device__ __forceinline__ int rows_left(int64_t have) {
 // X / kPass rows.
 template <int X>
 struct CodesK {
-  static constexpr bool kMN = false, kBf = false;
+  static constexpr bool kTma = false, kMN = false, kBf = false;
   static constexpr int P = 1;
   static constexpr int kUnits = X >= kPass ? X / kPass : 1;
   static constexpr int kSpan = 2, kRegs = 4 * kUnits;
@@ -263,19 +283,35 @@ struct CodesK {
   int64_t M, ld;
   int unit;
   struct Thread {
-    const int8_t *p;
+    const int8_t *p[kUnits];
     uint32_t off;
-    int k, rows;
+    int k;
   };
+  bool aligned() const { return unit == 16; }
   __device__ __forceinline__ Thread init(int64_t x0, int64_t r0, int tid) const {
     const int lane = tid & 31, row = (tid >> 5) * 4 + (lane >> 3), q = lane & 7;
-    const int64_t m = x0 + row;
-    return {codes + m * ld + r0 + 16 * q, (row >> 3) * 1152u + q * 144u + (row & 7) * 16u, 16 * q, row < X ? rows_left(M - m) : 0};
+    Thread t = {{}, (row >> 3) * 1152u + q * 144u + (row & 7) * 16u, 16 * q};
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int64_t m = x0 + row + u * kPass;
+      t.p[u] = codes + (m < M ? m : M - 1) * ld + r0 + 16 * q;
+    }
+    return t;
+  }
+  __device__ __forceinline__ void full(Thread &t, uint32_t (&w)[kRegs]) const {
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const uint4 v = __ldg(reinterpret_cast<const uint4 *>(t.p[u]));
+      w[4 * u] = v.x, w[4 * u + 1] = v.y, w[4 * u + 2] = v.z, w[4 * u + 3] = v.w;
+      t.p[u] += kGroups * kSpan * kStep;
+    }
   }
   __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u) load_codes(t.p + u * kPass * ld, t.rows > kPass * u ? left - t.k : 0, unit, w + 4 * u);
-    t.p += kSpan * kStep;
+    for (int u = 0; u < kUnits; ++u) {
+      load_codes(t.p[u], left - t.k, unit, w + 4 * u);
+      t.p[u] += kGroups * kSpan * kStep;
+    }
   }
   __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool second, uint32_t tile) const {
     if (X < kPass && t.off >= tile_bytes(false, X)) return;
@@ -288,12 +324,12 @@ struct CodesK {
   }
 };
 
-// A(i = k, r = m): int8 codes as bfloat16, MN-major.  A thread holds 16 codes of one m, and stores their two
-// pieces in an order that gives eight lanes eight bank groups.
+// A(i = k, r = m): int8 codes as bfloat16, MN-major.  A thread holds 16 codes of each of 2 m, and stores their
+// two pieces in an order that gives eight lanes eight bank groups.
 struct CodesT {
   static constexpr bool kMN = true, kMixed = false;
-  static constexpr int kSpan = 1, kRegs = 4;
-  static_assert(kPass == kStep, "a pass is a step's tokens");
+  static constexpr int kSpan = 1, kRegs = 8;
+  static_assert(2 * kPass == kStep, "two passes are a step's tokens");
   const int8_t *codes;
   int64_t K, ld;
   int unit;
@@ -302,25 +338,37 @@ struct CodesT {
     uint32_t off, turn;
     int m, k;  // k: how many of the 16 are in range
   };
+  bool aligned() const { return unit == 16; }
   __device__ __forceinline__ Thread init(int64_t x0, int64_t r0, int tid) const {
     const int lane = tid & 31, m = (tid >> 5) * 4 + (lane >> 3), q = lane & 7;
-    const int64_t left = K - x0 - 16 * q;
-    return {codes + (r0 + m) * ld + x0 + 16 * q, q * 2080u + (m >> 3) * 128u + (m & 7) * 16u, static_cast<uint32_t>(q >> 2), m,
+    const int64_t left = K - x0 - 16 * q, k = left > 0 ? x0 + 16 * q : K - (K < 16 ? K : 16);
+    return {codes + (r0 + m) * ld + k, q * 2080u + (m >> 3) * 128u + (m & 7) * 16u, static_cast<uint32_t>(q >> 2), m,
             static_cast<int>(left < 16 ? left : 16)};
   }
+  __device__ __forceinline__ void full(Thread &t, uint32_t (&w)[kRegs]) const {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const uint4 v = __ldg(reinterpret_cast<const uint4 *>(t.p + u * kPass * ld));
+      w[4 * u] = v.x, w[4 * u + 1] = v.y, w[4 * u + 2] = v.z, w[4 * u + 3] = v.w;
+    }
+    t.p += kGroups * kStep * ld;
+  }
   __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
-    load_codes(t.p, t.m < left ? t.k : 0, unit, w);
-    t.p += kStep * ld;
+#pragma unroll
+    for (int u = 0; u < 2; ++u) load_codes(t.p + u * kPass * ld, t.m + u * kPass < left ? t.k : 0, unit, w + 4 * u);
+    t.p += kGroups * kStep * ld;
   }
   __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool, uint32_t tile) const {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const bool high = (h ^ t.turn) != 0;
-      uint32_t o[4];
-      codes4_bf16(high ? w[2] : w[0], o[0], o[1]);
-      codes4_bf16(high ? w[3] : w[1], o[2], o[3]);
-      st_shared16(tile + t.off + (high ? 1040u : 0u), o[0], o[1], o[2], o[3]);
-    }
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const bool high = (h ^ t.turn) != 0;
+        uint32_t o[4];
+        codes4_bf16(high ? w[4 * u + 2] : w[4 * u], o[0], o[1]);
+        codes4_bf16(high ? w[4 * u + 3] : w[4 * u + 1], o[2], o[3]);
+        st_shared16(tile + t.off + (high ? 1040u : 0u) + u * (kPass / 8 * 128u), o[0], o[1], o[2], o[3]);
+      }
   }
 };
 
@@ -350,6 +398,14 @@ __device__ __forceinline__ void load_grad8(const T *p, int left, bool vec, uint3
   }
 }
 template <typename T>
+__device__ __forceinline__ void full_grad8(const T *p, uint32_t *w) {
+#pragma unroll
+  for (int i = 0; i < kWords8<T> / 4; ++i) {
+    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+    w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
+  }
+}
+template <typename T>
 __device__ __forceinline__ void grad8_f32(const uint32_t *w, float (&v)[8]) {
   if constexpr (sizeof(T) == 4) {
 #pragma unroll
@@ -364,7 +420,7 @@ __device__ __forceinline__ void grad8_f32(const uint32_t *w, float (&v)[8]) {
 // 8 elements of each of X / kPass rows.
 template <typename T, int X>
 struct GradK {
-  static constexpr bool kMN = false, kBf = !std::is_same_v<T, __half>;
+  static constexpr bool kTma = false, kMN = false, kBf = !std::is_same_v<T, __half>;
   static constexpr int P = sizeof(T) == 4 ? 3 : 1;
   static constexpr int kUnits = X / kPass;
   static constexpr int kSpan = 1, kRegs = kWords8<T> * kUnits;
@@ -372,20 +428,34 @@ struct GradK {
   int64_t M, ld;
   bool vec;
   struct Thread {
-    const T *p;
+    const T *p[kUnits];
     uint32_t off;
-    int n, rows;
+    int n;
   };
+  bool aligned() const { return vec; }
   __device__ __forceinline__ Thread init(int64_t x0, int64_t r0, int tid) const {
     const int lane = tid & 31, row = (tid >> 5) * 4 + (lane >> 3), q = lane & 7;
-    const int64_t m = x0 + row;
-    return {dy + m * ld + r0 + 8 * q, (row >> 3) * 1152u + q * 144u + (row & 7) * 16u, 8 * q, rows_left(M - m)};
+    Thread t = {{}, (row >> 3) * 1152u + q * 144u + (row & 7) * 16u, 8 * q};
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      const int64_t m = x0 + row + u * kPass;
+      t.p[u] = dy + (m < M ? m : M - 1) * ld + r0 + 8 * q;
+    }
+    return t;
+  }
+  __device__ __forceinline__ void full(Thread &t, uint32_t (&w)[kRegs]) const {
+#pragma unroll
+    for (int u = 0; u < kUnits; ++u) {
+      full_grad8<T>(t.p[u], w + kWords8<T> * u);
+      t.p[u] += kGroups * kStep;
+    }
   }
   __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
 #pragma unroll
-    for (int u = 0; u < kUnits; ++u)
-      load_grad8<T>(t.p + u * kPass * ld, t.rows > kPass * u ? left - t.n : 0, vec, w + kWords8<T> * u);
-    t.p += kStep;
+    for (int u = 0; u < kUnits; ++u) {
+      load_grad8<T>(t.p[u], left - t.n, vec, w + kWords8<T> * u);
+      t.p[u] += kGroups * kStep;
+    }
   }
   __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool, uint32_t tile) const {
 #pragma unroll
@@ -396,20 +466,20 @@ struct GradK {
       } else {
         float v[8];
         grad8_f32<T>(o, v);
-        split8<P>(v, at, tile_bytes(false, X));
+        store_split8<P>(v, at, tile_bytes(false, X));
       }
     }
   }
 };
 
 // B(j = n, r = m): gradients times their row's scale, in P bfloat16 pieces, MN-major.  A thread holds X / 64
-// groups of 8 columns of one m, and its scale.
+// pieces of 8 columns of each of 2 m, and their scales.
 template <typename T, int X, int P_>
 struct GradT {
-  static constexpr bool kMN = true, kBf = true;
+  static constexpr bool kTma = false, kMN = true, kBf = true;
   static constexpr int P = P_;
-  static constexpr int kGroups = X / 64;
-  static constexpr int kSpan = 1, kRegs = kWords8<T> * kGroups + 1;
+  static constexpr int kPieces = X / 64;
+  static constexpr int kSpan = 1, kRegs = 2 * kWords8<T> * kPieces + 2;
   const T *dy;
   int64_t N, ld;
   const float *scale;
@@ -418,27 +488,70 @@ struct GradT {
     const T *p;
     const float *s;
     uint32_t off;
-    int m, columns;
+    int m, columns, last;  // last: the furthest piece that starts in range
   };
+  bool aligned() const { return vec; }
   __device__ __forceinline__ Thread init(int64_t x0, int64_t r0, int tid) const {
     const int lane = tid & 31, m = (tid >> 5) * 4 + (lane >> 3), q = lane & 7;
-    return {dy + (r0 + m) * ld + x0 + 8 * q, scale + r0 + m, q * 1040u + (m >> 3) * 128u + (m & 7) * 16u, m, rows_left(N - x0 - 8 * q)};
+    const int columns = rows_left(N - x0 - 8 * q);  // (none: back to the last 8)
+    return {dy + (r0 + m) * ld + x0 + 8 * q, scale + r0 + m, q * 1040u + (m >> 3) * 128u + (m & 7) * 16u, m, columns,
+            columns > 0 ? (columns - 1) / 64 * 64 : static_cast<int>(N - x0 - 8 * q) - 8};
+  }
+  __device__ __forceinline__ void full(Thread &t, uint32_t (&w)[kRegs]) const {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      w[kRegs - 2 + h] = __float_as_uint(__ldg(t.s + h * kPass));
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u)
+        full_grad8<T>(t.p + h * kPass * ld + (64 * u < t.last ? 64 * u : t.last), w + kWords8<T> * (h * kPieces + u));
+    }
+    t.p += kGroups * kStep * ld, t.s += kGroups * kStep;
   }
   __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
-    const bool live = t.m < left;
-    w[kRegs - 1] = live ? __float_as_uint(__ldg(t.s)) : 0u;
 #pragma unroll
-    for (int u = 0; u < kGroups; ++u) load_grad8<T>(t.p + 64 * u, live ? t.columns - 64 * u : 0, vec, w + kWords8<T> * u);
-    t.p += kStep * ld, t.s += kStep;
+    for (int h = 0; h < 2; ++h) {
+      const bool live = t.m + h * kPass < left;
+      w[kRegs - 2 + h] = live ? __float_as_uint(__ldg(t.s + h * kPass)) : 0u;
+#pragma unroll
+      for (int u = 0; u < kPieces; ++u)
+        load_grad8<T>(t.p + h * kPass * ld + 64 * u, live ? t.columns - 64 * u : 0, vec, w + kWords8<T> * (h * kPieces + u));
+    }
+    t.p += kGroups * kStep * ld, t.s += kGroups * kStep;
   }
   __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool, uint32_t tile) const {
 #pragma unroll
-    for (int u = 0; u < kGroups; ++u) {
-      float v[8];
-      grad8_f32<T>(w + kWords8<T> * u, v);
+    for (int h = 0; h < 2; ++h)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[e] *= __uint_as_float(w[kRegs - 1]);
-      split8<P>(v, tile + t.off + u * 8320u, tile_bytes(true, X));
+      for (int u = 0; u < kPieces; ++u) {
+        float v[8];
+        grad8_f32<T>(w + kWords8<T> * (h * kPieces + u), v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] *= __uint_as_float(w[kRegs - 2 + h]);
+        store_split8<P>(v, tile + t.off + u * 8320u + h * (kPass / 8 * 128u), tile_bytes(true, X));
+      }
+  }
+};
+
+// B from 16-bit rows in memory, copied by TMA with a 128-byte swizzle: `map` has the dimensions (contiguous,
+// rows, pieces); elements out of range are zeros.  MN: the contiguous dimension runs along j, and a step is 64 of
+// its rows; else it runs along r.
+template <int X_, bool MN, bool BF, int P_, int SPAN>
+struct Tiled {
+  static constexpr bool kTma = true, kMN = MN, kBf = BF;
+  static constexpr int P = P_, X = X_, kSpan = SPAN;
+  CUtensorMap map;
+  bool aligned() const { return true; }
+  // the copies of one step into `tile` (P pieces of X rows of 64): j from x0, r from r0
+  __device__ __forceinline__ void copy(int64_t x0, int64_t r0, uint32_t tile, uint32_t bar) const {
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      if constexpr (MN) {
+#pragma unroll
+        for (int b = 0; b < X / 64; ++b)
+          tensor_g2s(tile + p * X * 128 + b * 8192, &map, static_cast<int>(x0) + 64 * b, static_cast<int>(r0), p, bar);
+      } else {
+        tensor_g2s(tile + p * X * 128, &map, static_cast<int>(r0), static_cast<int>(x0), p, bar);
+      }
     }
   }
 };
@@ -501,15 +614,19 @@ struct GemmArgs {
   B b;
   Out out;
   int tiles_i, steps;  // tiles along i (whole clusters); steps of a split
+  int full;            // r that are left for a span to be loaded by full(), more than there are without alignment
   float *partial;      // [splits][J][I] where there are several, else NULL
   int *err;            // set to 1 by a wait that gave up
 };
 
-// CG CTAs on a tile of 128 CG i by TB j; a B operand of X = TB / CG rows each
+// CG CTAs on a tile of 128 CG i by TB j; a B operand of X = TB / CG rows each.  A stage is B's pieces, then A
+// (on 1024 bytes where B is swizzled)
 template <class A, class B, int TB, int CG>
 struct GemmShape {
-  static constexpr uint32_t kABytes = tile_bytes(A::kMN, kTileI), kPieceBytes = tile_bytes(B::kMN, TB / CG);
-  static constexpr uint32_t kStageBytes = kABytes + B::P * kPieceBytes;
+  static constexpr uint32_t kABytes = tile_bytes(A::kMN, kTileI);
+  static constexpr uint32_t kPieceBytes = B::kTma ? TB / CG * 128u : tile_bytes(B::kMN, TB / CG);
+  static constexpr uint32_t kOperands = kABytes + B::P * kPieceBytes;
+  static constexpr uint32_t kStageBytes = B::kTma ? (kOperands + 1023u) & ~1023u : kOperands;
   static constexpr uint32_t kBars = 256 + TB * 4;  // barriers and two words; the columns' factors
   static constexpr int fit(uint32_t room) { return static_cast<int>((room - kBars) / kStageBytes); }
   static constexpr uint32_t kHalfSm = kSmemPerSm / 2 - 1024;
@@ -529,10 +646,11 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   using S = GemmShape<A, B, TB, CG>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t base = smem_u32(smem);
-  // full[stages] (this CTA's producers), peer[stages] (the other CTA's stage), empty[stages], done; 2 words
-  const uint32_t full = base + S::kStages * S::kStageBytes, peer = full + 8 * S::kStages, empty = peer + 8 * S::kStages,
-                 done = empty + 8 * S::kStages;
-  volatile uint32_t *word = reinterpret_cast<volatile uint32_t *>(smem + S::kStages * S::kStageBytes + 24 * S::kStages + 8);
+  // full[stages] (this CTA's producers), copied[stages] (its copies), peer[stages] (the other CTA's stage),
+  // empty[stages], done; 2 words
+  constexpr uint32_t kB = 8 * S::kStages;
+  const uint32_t full = base + S::kStages * S::kStageBytes, copied = full + kB, peer = copied + kB, empty = peer + kB, done = empty + kB;
+  volatile uint32_t *word = reinterpret_cast<volatile uint32_t *>(smem + S::kStages * S::kStageBytes + 4 * kB + 8);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = CG == 2 ? cluster_ctarank() : 0;
   const int64_t i0 = static_cast<int64_t>(blockIdx.x % g.tiles_i) * kTileI, j0 = static_cast<int64_t>(blockIdx.x / g.tiles_i) * TB;
@@ -541,7 +659,7 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   const int steps = kSpan * static_cast<int>((end - first + kSpan * kStep - 1) / (kSpan * kStep));
 
   if (tid == 0) {
-    for (int s = 0; s < S::kStages; ++s) mbar_init(full + 8 * s, kProducerWarps), mbar_init(peer + 8 * s, 1), mbar_init(empty + 8 * s, 1);
+    for (int s = 0; s < S::kStages; ++s) mbar_init(full + 8 * s, kGroupWarps), mbar_init(copied + 8 * s, 1), mbar_init(peer + 8 * s, 1), mbar_init(empty + 8 * s, 1);
     mbar_init(done, 1);
     fence_mbar_init_cluster();
     word[1] = 0;
@@ -555,14 +673,12 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   else __syncthreads();
   tc_fence_after();
   const uint32_t tmem = word[0];
-  // a wait with an end: one that gives up stops the CTA's others too
+  // A wait with an end: one that gives up stops the CTA's others too.  The hardware suspends a waiting warp for
+  // up to kGemmWaitNs at a time, so that it takes no issue slots from the ones that convert.
   auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
-    auto try_wait = [&] { return CG == 2 ? mbar_try_wait_acq_cluster(bar, parity) : mbar_try_wait(bar, parity); };
-    if (try_wait()) return true;
-    const long long t0 = clock64();
-    while (!try_wait()) {
+    for (int tries = 0; !mbar_try_wait_for(bar, parity, kGemmWaitNs); ++tries) {
       if (word[1]) return false;
-      if (clock64() - t0 > kGemmWaitCycles) {
+      if (tries > kGemmWaitTries) {
         word[1] = 1;
         *g.err = 1;
         return false;
@@ -574,58 +690,80 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   float *factor = reinterpret_cast<float *>(smem + S::kStages * S::kStageBytes + 256);
   for (int c = tid; c < TB; c += kGemmThreads) factor[c] = g.partial ? 1.0f : j0 + c < g.J ? g.out.factor(j0 + c) : 0.0f;
   if (warp < kProducerWarps) {
-    typename A::Thread ta = g.a.init(i0, first, tid);
-    typename B::Thread tb = g.b.init(j0 + rank * (TB / CG), first, tid);
-    // kAhead spans in registers, in flight while the tensor cores work through the stages
-    constexpr int kAhead = A::kRegs + B::kRegs <= 12 ? 2 : 1;
-    uint32_t ra[kAhead][A::kRegs], rb[kAhead][B::kRegs];
-    int left = static_cast<int>(end - first);
-#pragma unroll
-    for (int a = 0; a < kAhead; ++a, left -= kSpan * kStep) g.a.load(ta, left, ra[a]), g.b.load(tb, left, rb[a]);
-    int s = 0, parity = 1;
-    bool ok = true;
-    for (int it = 0; ok && it < steps; it += kAhead * kSpan) {
-#pragma unroll
-      for (int a = 0; a < kAhead; ++a) {
-        if (it + a * kSpan >= steps) break;
+    const int group = warp / kGroupWarps, at = tid - group * kGroupWarps * 32;
+    constexpr int kSpanR = kSpan * kStep;
+    typename A::Thread ta = g.a.init(i0, first + group * kSpanR, at);
+    uint32_t ra[A::kRegs];
+    int left = static_cast<int>(end - first) - group * kSpanR;
+    const auto load_a = [&] {
+      if (left >= g.full) g.a.full(ta, ra);
+      else g.a.load(ta, left, ra);
+    };
+    const auto skip = [](int &s, uint32_t &parity, int by) {
+      s += by;
+      if (s >= S::kStages) s -= S::kStages, parity ^= 1;
+    };
+    int s = 0;
+    uint32_t parity = 1;  // (a stage's first wait is for the phase before its first, and over at once)
+    skip(s, parity, group * kSpan);
+    // the group's spans: `load` the next one's B, `store` the step's
+    const auto produce = [&](const auto &load_b, const auto &store_b) {
+      load_a(), load_b(left);
+      left -= kGroups * kSpanR;
+      for (int it = group * kSpan; it < steps; it += kGroups * kSpan) {
 #pragma unroll
         for (int h = 0; h < kSpan; ++h) {
-          ok = ok && __all_sync(0xffffffffu, it + a * kSpan + h < S::kStages || wait(empty + 8 * s, parity));
-          if (!ok) break;
+          if (!__all_sync(0xffffffffu, wait(empty + 8 * s, parity))) return;
           const uint32_t stage = base + s * S::kStageBytes;
-          g.a.store(ta, ra[a], h == 1, stage);
-          g.b.store(tb, rb[a], h == 1, stage + S::kABytes);
+          g.a.store(ta, ra, h == 1, stage + B::P * S::kPieceBytes);
+          store_b(h == 1, stage);
           __syncwarp();
           if (lane == 0) mbar_arrive(full + 8 * s);
-          if (++s == S::kStages) s = 0, parity ^= 1;
+          skip(s, parity, 1);
         }
-        g.a.load(ta, left, ra[a]), g.b.load(tb, left, rb[a]);
-        left -= kSpan * kStep;
+        load_a(), load_b(left);
+        left -= kGroups * kSpanR;
+        skip(s, parity, (kGroups - 1) * kSpan);
       }
+    };
+    if constexpr (B::kTma) {
+      produce([](int) {}, [](bool, uint32_t) {});
+    } else {
+      typename B::Thread tb = g.b.init(j0 + rank * (TB / CG), first + group * kSpanR, at);
+      uint32_t rb[B::kRegs];
+      produce([&](int left) {
+        if (left >= g.full) g.b.full(tb, rb);
+        else g.b.load(tb, left, rb);
+      }, [&](bool second, uint32_t tile) { g.b.store(tb, rb, second, tile); });
     }
     named_bar_sync(1, kProducers);  // (the factors)
-  } else {
+  } else if (warp == kProducerWarps) {
     // A stage that the producers have written becomes the tensor cores' with one fence between the proxies, here,
-    // and not one in every producer, where it would also wait for the loads in flight.  In the second CTA
-    // that is all; it tells the first.
+    // on the way from their writes to the MMA, and not one in every producer, where it would also wait for
+    // the loads in flight.  In the second CTA that is all; it tells the first.
     constexpr uint32_t idesc = gemm_idesc(B::kBf, A::kMN, B::kMN, 128 * CG, TB);
     constexpr uint32_t la = tile_lbo(A::kMN), lb = tile_lbo(B::kMN);
     const uint32_t peer0 = CG == 2 ? mapa_cluster(peer, 0) : peer;
-    int s = 0, parity = 0;
+    int s = 0;
+    uint32_t parity = 0;
     for (int it = 0; it < steps; ++it) {
-      if (!__all_sync(0xffffffffu, wait(full + 8 * s, parity))) break;
+      if (!__all_sync(0xffffffffu, wait(full + 8 * s, parity) && (!B::kTma || wait(copied + 8 * s, parity)))) break;
       fence_proxy_async_smem();
       if (rank == 0) {
         if (CG == 2 && !__all_sync(0xffffffffu, wait(peer + 8 * s, parity))) break;
         tc_fence_after();
-        const uint32_t at = base + s * S::kStageBytes, bt = at + S::kABytes;
+        const uint32_t bt = base + s * S::kStageBytes, at = bt + P * S::kPieceBytes;
 #pragma unroll
         for (int p = 0; p < P; ++p)
 #pragma unroll
-          for (int ks = 0; ks < kStep / 16; ++ks)
-            mma_f16_cg_warp<CG>(tmem, make_sdesc(at + ks * 2 * la, la, tile_sbo(A::kMN)),
-                                make_sdesc(bt + p * S::kPieceBytes + ks * 2 * lb, lb, tile_sbo(B::kMN)), idesc,
+          for (int ks = 0; ks < kStep / 16; ++ks) {
+            const uint32_t b = bt + p * S::kPieceBytes;
+            const uint64_t bdesc = !B::kTma  ? make_sdesc(b + ks * 2 * lb, lb, tile_sbo(B::kMN))
+                                   : B::kMN ? make_sdesc_sw128(b + ks * 2048, 8192, 1024)
+                                            : make_sdesc_sw128(b + ks * 32, 16, 1024);
+            mma_f16_cg_warp<CG>(tmem, make_sdesc(at + ks * 2 * la, la, tile_sbo(A::kMN)), bdesc, idesc,
                                 it > 0 || p > 0 || ks > 0 ? 1u : 0u);
+          }
         mma_commit_cg_warp<CG>(empty + 8 * s);
       } else {
         __syncwarp();
@@ -634,6 +772,22 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
       if (++s == S::kStages) s = 0, parity ^= 1;
     }
     if (rank == 0) mma_commit_cg_warp<CG>(done);
+  } else if constexpr (B::kTma) {
+    const int64_t x0 = j0 + rank * (TB / CG);
+    int s = 0, it = 0;
+    uint32_t parity = 1;
+    for (; it < steps; ++it) {
+      if (!__all_sync(0xffffffffu, wait(empty + 8 * s, parity))) break;
+      if (lane == 0) {
+        mbar_arrive_expect_tx(copied + 8 * s, P * S::kPieceBytes);
+        g.b.copy(x0, first + static_cast<int64_t>(it) * kStep, base + s * S::kStageBytes, copied + 8 * s);
+      }
+      __syncwarp();
+      if (++s == S::kStages) s = 0, parity ^= 1;
+    }
+    // a CTA that gives up still waits for the copies it has begun
+    for (int k = it < S::kStages ? 0 : it - S::kStages; k < it; ++k)
+      for (int tries = 0; !mbar_try_wait_for(copied + 8 * (k % S::kStages), (k / S::kStages) & 1, kGemmWaitNs) && tries < 1024; ++tries) {}
   }
   __syncwarp();
   const bool ready = __all_sync(0xffffffffu, wait(done, 0) && !word[1]);
@@ -682,7 +836,7 @@ inline int codes_unit(const int8_t *codes, int64_t ld, int64_t K) {
 }
 inline int weights_unit(const uint8_t *packed, int64_t K) {
   const uintptr_t p = reinterpret_cast<uintptr_t>(packed);
-  return K % 32 == 0 && (p & 7u) == 0 ? 8 : K % 16 == 0 && (p & 3u) == 0 ? 4 : 1;
+  return K % 64 == 0 && (p & 15u) == 0 ? 16 : K % 32 == 0 && (p & 7u) == 0 ? 8 : K % 16 == 0 && (p & 3u) == 0 ? 4 : 1;
 }
 template <typename T>
 bool grads_vec(const void *dy, int64_t ld, int64_t N) {
@@ -714,7 +868,8 @@ cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b,
                         cudaStream_t st) {
   using S = GemmShape<A, B, TB, CG>;
   const GemmPlan p = gemm_plan<A, B, TB, CG>(I, J, R, sms);
-  const GemmArgs<A, B, Out> g = {I, J, R, a, b, out, static_cast<int>(p.tiles_i), p.steps, p.splits > 1 ? partial : nullptr, err};
+  const GemmArgs<A, B, Out> g = {I, J, R, a, b, out, static_cast<int>(p.tiles_i), p.steps,
+                                   a.aligned() && b.aligned() ? A::kSpan * kStep : INT_MAX, p.splits > 1 ? partial : nullptr, err};
   auto *kernel = gemm_kernel<A, B, Out, TB, CG>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
   if (e != cudaSuccess) return e;
@@ -734,13 +889,32 @@ cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b,
   return cudaGetLastError();
 }
 
-// The tile of a product: f(TB, CG).  At most 64 j: 64 (the rest of a tile would be converted zeros); one row
-// of tiles along i: a single CTA's; else a pair's.
-template <int SINGLE, class F>
-auto with_tile(int64_t I, int64_t J, const F &f) {
-  if (J <= 64) return f(std::integral_constant<int, 64>(), std::integral_constant<int, 1>());
-  if (I <= kTileI) return f(std::integral_constant<int, SINGLE>(), std::integral_constant<int, 1>());
-  return f(std::integral_constant<int, 256>(), std::integral_constant<int, 2>());
+// The tile of a product: f(TB, CG).  More than one tile of 128 of both i and j: a pair's, whose B is copied by
+// TMA (staged first where memory does not hold it in 16 bits).  Else a single CTA's, which converts B itself:
+// of 64 j at most where there are no more (the rest of a tile would be converted zeros), of 128.
+inline bool pair_tiles(int64_t I, int64_t J) { return I > kTileI && J > kTileI; }
+template <class F>
+auto with_single_tile(int64_t J, const F &f) {
+  return J <= 64 ? f(std::integral_constant<int, 64>()) : f(std::integral_constant<int, 128>());
 }
+
+// linear_stage.cu
+constexpr int64_t staged_k(int64_t K) { return (K + 127) / 128 * 128; }
+struct StageGrads {
+  const void *dy;  // [M][N], ld apart
+  int64_t ld, M, N;
+  int dtype;
+  const float *scale;  // [M] or NULL
+  int pieces;          // bfloat16 pieces; 0: 16-bit gradients as they are
+  void *out;           // [pieces][M][N up to a multiple of 8] 16-bit, or NULL
+  float *db;           // [N] column sums, or NULL
+  float *partial;      // [stage_parts(M, N)][N] with db
+};
+int stage_parts(int64_t M, int64_t N);
+cudaError_t launch_stage_codes(const int8_t *codes, int64_t ld, int64_t M, int64_t K, void *out, cudaStream_t st);
+cudaError_t launch_stage_grads(const StageGrads &c, cudaStream_t st);
+// the map of 16-bit rows [pieces][rows][width], ld apart, in boxes of 64 by box_rows
+cudaError_t tensor_map(CUtensorMap *map, const void *base, bool bf, int64_t width, int64_t rows, int64_t ld, int pieces, int box_rows);
+constexpr int64_t up16(int64_t bytes) { return (bytes + 15) / 16 * 16; }
 
 }  // namespace aecct

@@ -1,6 +1,6 @@
-// linear_wgrad.cu -- the gradient of the AAP linear layer's weights, dW = sum over tokens of dy scale codes
-// (linear.cu has the formulas).  dy scale is no 16-bit number: it goes through the tensor cores in as many
-// bfloat16 pieces as the gradient's own type has room for (1: bfloat16, 2: half, 3: float, exact).  One
+// linear_wgrad.cu -- the gradient of the AAP linear layer's weights, dW = sum over tokens of dy scale codes, and
+// of its bias (linear.cu has the formulas).  dy scale is no 16-bit number: it goes through the tensor cores in as
+// many bfloat16 pieces as the gradient's own type has room for (1: bfloat16, 2: half, 3: float, exact).  One
 // piece rounds each term to 8 bits, which many tokens average out; the few terms of up to kFewTokens are
 // taken in two pieces, where the product is bound by writing dW and the second one costs nothing.
 #include <cuda_runtime.h>
@@ -17,42 +17,76 @@ constexpr int64_t kFewTokens = 64;
 
 int pieces_of(int64_t M, int wdtype) { return wdtype == 0 ? 3 : wdtype == 1 || M <= kFewTokens ? 2 : 1; }
 
-template <typename T, int P>
-cudaError_t weight_grad(const AapLinearGradCall &c, float *work, cudaStream_t st) {
-  const CodesT a = {c.codes, c.K, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
-  const OutW out = {c.dw, c.wdtype, c.K};
-  return with_tile<P == 1 ? 256 : 128>(c.K, c.N, [&](auto tb, auto cg) {
-    constexpr int TB = decltype(tb)::value, CG = decltype(cg)::value;
-    using B = GradT<T, TB / CG, P>;
-    const B b = {static_cast<const T *>(c.dy), c.N, c.lddy, c.scale, grads_vec<T>(c.dy, c.lddy, c.N)};
-    return launch_gemm<CodesT, B, OutW, TB, CG>(c.K, c.N, c.M, a, b, out, work, sm_count(), linear_status(), st);
-  });
+int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
+
+int64_t partial_bytes(const GemmPlan &p, int64_t N, int64_t K) {
+  return p.splits > 1 ? p.splits * N * K * static_cast<int64_t>(sizeof(float)) : 0;
 }
 
+int64_t sums_bytes(int64_t M, int64_t N) { return up16(static_cast<int64_t>(stage_parts(M, N)) * N * sizeof(float)); }
+
 template <int P>
-int64_t workspace_of(int64_t M, int64_t K, int64_t N) {
-  return with_tile<P == 1 ? 256 : 128>(K, N, [&](auto tb, auto cg) {
-    constexpr int TB = decltype(tb)::value, CG = decltype(cg)::value;
-    const GemmPlan p = gemm_plan<CodesT, GradT<float, TB / CG, P>, TB, CG>(K, N, M, sm_count());
-    return p.splits > 1 ? p.splits * K * N : int64_t(0);
+using Staged = Tiled<128, true, true, P, 1>;
+
+template <int P>
+cudaError_t staged_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t st) {
+  Staged<P> b;
+  const cudaError_t e = tensor_map(&b.map, work, true, c.N, c.M, padded(c.N), P, kStep);
+  if (e != cudaSuccess) return e;
+  const CodesT a = {c.codes, c.K, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
+  const OutW out = {c.dw, c.wdtype, c.K};
+  float *partial = reinterpret_cast<float *>(work + 2 * P * c.M * padded(c.N));
+  return launch_gemm<CodesT, Staged<P>, OutW, 256, 2>(c.K, c.N, c.M, a, b, out, partial, sm_count(), linear_status(), st);
+}
+
+template <typename T, int P>
+cudaError_t weight_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t st) {
+  const CodesT a = {c.codes, c.K, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
+  const OutW out = {c.dw, c.wdtype, c.K};
+  return with_single_tile(c.N, [&](auto tb) {
+    constexpr int TB = decltype(tb)::value;
+    using B = GradT<T, TB, P>;
+    const B b = {static_cast<const T *>(c.dy), c.N, c.lddy, c.scale, grads_vec<T>(c.dy, c.lddy, c.N)};
+    return launch_gemm<CodesT, B, OutW, TB, 1>(c.K, c.N, c.M, a, b, out, reinterpret_cast<float *>(work), sm_count(), linear_status(), st);
   });
 }
 
 template <typename T>
-cudaError_t weight_grad(const AapLinearGradCall &c, float *work, cudaStream_t st) {
+cudaError_t weight_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t st) {
   const int p = pieces_of(c.M, c.wdtype);
   return p == 3 ? weight_grad<T, 3>(c, work, st) : p == 2 ? weight_grad<T, 2>(c, work, st) : weight_grad<T, 1>(c, work, st);
 }
 
-}  // namespace
-
-int64_t weight_grad_workspace(int64_t M, int64_t K, int64_t N, int wdtype) {
-  const int p = pieces_of(M, wdtype);
-  return p == 3 ? workspace_of<3>(M, K, N) : p == 2 ? workspace_of<2>(M, K, N) : workspace_of<1>(M, K, N);
+template <int P>
+int64_t workspace_of(int64_t M, int64_t K, int64_t N) {
+  const int sms = sm_count();
+  if (pair_tiles(K, N)) return partial_bytes(gemm_plan<CodesT, Staged<P>, 256, 2>(K, N, M, sms), N, K) + 2 * P * M * padded(N);
+  return with_single_tile(N, [&](auto tb) {
+    constexpr int TB = decltype(tb)::value;
+    return partial_bytes(gemm_plan<CodesT, GradT<float, TB, P>, TB, 1>(K, N, M, sms), N, K);
+  });
 }
 
-cudaError_t launch_weight_grad(const AapLinearGradCall &c, float *work, cudaStream_t st) {
-  return c.dtype == 0 ? weight_grad<float>(c, work, st) : c.dtype == 1 ? weight_grad<__half>(c, work, st) : weight_grad<__nv_bfloat16>(c, work, st);
+}  // namespace
+
+// the column sums, and after them the staged pieces and the splits' sums
+int64_t weight_grad_workspace(int64_t M, int64_t K, int64_t N, int wdtype) {
+  const int p = pieces_of(M, wdtype);
+  return sums_bytes(M, N) + (p == 3 ? workspace_of<3>(M, K, N) : p == 2 ? workspace_of<2>(M, K, N) : workspace_of<1>(M, K, N));
+}
+
+cudaError_t launch_weight_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t st) {
+  const int p = pieces_of(c.M, c.wdtype);
+  uint8_t *rest = work + sums_bytes(c.M, c.N);
+  const bool staged = c.dw && pair_tiles(c.K, c.N);
+  if (staged || c.db) {
+    const StageGrads s = {c.dy, c.lddy, c.M, c.N, c.dtype, c.scale, staged ? p : 1, staged ? rest : nullptr, c.db, reinterpret_cast<float *>(work)};
+    const cudaError_t e = launch_stage_grads(s, st);
+    if (e != cudaSuccess) return e;
+  }
+  if (!c.dw) return cudaSuccess;
+  if (staged) return p == 3 ? staged_grad<3>(c, rest, st) : p == 2 ? staged_grad<2>(c, rest, st) : staged_grad<1>(c, rest, st);
+  return c.dtype == 0 ? weight_grad<float>(c, rest, st) : c.dtype == 1 ? weight_grad<__half>(c, rest, st) : weight_grad<__nv_bfloat16>(c, rest, st);
 }
 
 }  // namespace aecct

@@ -64,6 +64,18 @@ __device__ __forceinline__ bool mbar_try_wait_acq_cluster(uint32_t bar, uint32_t
   return ok != 0;
 }
 
+// the same, suspended for up to about `ns` while the phase is not over
+__device__ __forceinline__ bool mbar_try_wait_for(uint32_t bar, uint32_t parity, uint32_t ns) {
+  uint32_t ok;
+  asm volatile(
+      "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, %3;\n\t"
+      "selp.u32 %0, 1, 0, p;\n\t}"
+      : "=r"(ok)
+      : "r"(bar), "r"(parity), "r"(ns)
+      : "memory");
+  return ok != 0;
+}
+
 __device__ __forceinline__ void fence_acq_rel_cluster() { asm volatile("fence.acq_rel.cluster;" ::: "memory"); }
 
 // ----------------------------------------------------------------------------- cluster
@@ -115,6 +127,15 @@ __device__ __forceinline__ void bulk_g2s(uint32_t dst_smem, const void *src, uin
                    dst_smem),
                "l"(src), "r"(bytes), "r"(bar)
                : "memory");
+}
+
+// a box of a rank-3 tensor (TMA engine) into shared memory, at element coordinates x (contiguous), y, z
+__device__ __forceinline__ void tensor_g2s(uint32_t dst_smem, const void *map, int x, int y, int z, uint32_t bar) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(
+          dst_smem),
+      "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar)
+      : "memory");
 }
 
 // shared -> global bulk copy (TMA engine), tracked by the issuing thread's bulk groups
@@ -232,6 +253,12 @@ __device__ __forceinline__ uint64_t make_sdesc(uint32_t saddr, uint32_t lbo, uin
   d |= (uint64_t)((sbo & 0x3FFFFu) >> 4) << 32;
   d |= (uint64_t)1 << 46;  // descriptor version for tcgen05
   return d;                // base offset 0, relative LBO, layout type 0 = no swizzle
+}
+// The same for tiles that TMA wrote with a 128-byte swizzle (8 rows of 128 bytes, on 1024 bytes): K-major, 64 elements
+// of K a row, sbo between groups of 8 rows of M/N (lbo is not read); MN-major, 64 elements of M/N a row, sbo between
+// groups of 8 K, lbo between blocks of 64 M/N.
+__device__ __forceinline__ uint64_t make_sdesc_sw128(uint32_t saddr, uint32_t lbo, uint32_t sbo) {
+  return make_sdesc(saddr, lbo, sbo) | (uint64_t)2 << 61;
 }
 // Instruction descriptor for kind::f16: bf16 A and B, fp32 accumulator, both K-major.
 __host__ __device__ constexpr uint32_t make_idesc_bf16(uint32_t M, uint32_t N) {
