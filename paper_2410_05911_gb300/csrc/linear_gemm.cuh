@@ -48,8 +48,7 @@ constexpr int kPass = kGroupWarps * 4;  // rows of 8 lanes that a group holds at
 __host__ __device__ constexpr uint32_t tile_bytes(bool mn, int x) { return x / 8 * (mn ? 1040u : 1152u); }
 __host__ __device__ constexpr uint32_t tile_lbo(bool mn) { return mn ? 128u : 144u; }
 __host__ __device__ constexpr uint32_t tile_sbo(bool mn) { return mn ? 1040u : 1152u; }
-constexpr uint32_t kGemmWaitNs = 10000;   // a wait looks again after this long at the latest
-constexpr int kGemmWaitTries = 1 << 20;   // and has lost its arrival after so many looks (tenths of a second at least)
+constexpr int kGemmWaitTries = 1 << 24;  // a wait that has looked so often (seconds) has lost its arrival
 
 // instruction descriptor of kind::f16: 32-bit accumulators; BF: bfloat16 operands, else half; MN: both
 // operands' 16-byte rows run along i and j
@@ -673,10 +672,9 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   else __syncthreads();
   tc_fence_after();
   const uint32_t tmem = word[0];
-  // A wait with an end: one that gives up stops the CTA's others too.  The hardware suspends a waiting warp for
-  // up to kGemmWaitNs at a time, so that it takes no issue slots from the ones that convert.
+  // a wait with an end: one that gives up stops the CTA's others too
   auto wait = [&](uint32_t bar, uint32_t parity) -> bool {
-    for (int tries = 0; !mbar_try_wait_for(bar, parity, kGemmWaitNs); ++tries) {
+    for (int tries = 0; !mbar_try_wait(bar, parity); ++tries) {
       if (word[1]) return false;
       if (tries > kGemmWaitTries) {
         word[1] = 1;
@@ -767,7 +765,7 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
         mma_commit_cg_warp<CG>(empty + 8 * s);
       } else {
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(peer0 + 8 * s);
+        if (lane == 0) mbar_arrive_peer(peer0 + 8 * s);
       }
       if (++s == S::kStages) s = 0, parity ^= 1;
     }
@@ -787,7 +785,7 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     }
     // a CTA that gives up still waits for the copies it has begun
     for (int k = it < S::kStages ? 0 : it - S::kStages; k < it; ++k)
-      for (int tries = 0; !mbar_try_wait_for(copied + 8 * (k % S::kStages), (k / S::kStages) & 1, kGemmWaitNs) && tries < 1024; ++tries) {}
+      for (int tries = 0; !mbar_try_wait(copied + 8 * (k % S::kStages), (k / S::kStages) & 1) && tries < kGemmWaitTries; ++tries) {}
   }
   __syncwarp();
   const bool ready = __all_sync(0xffffffffu, wait(done, 0) && !word[1]);

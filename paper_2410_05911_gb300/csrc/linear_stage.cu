@@ -142,7 +142,7 @@ cudaError_t tensor_map(CUtensorMap *map, const void *base, bool bf, int64_t widt
   static const Encode encode = [] {
     void *f = nullptr;
     cudaDriverEntryPointQueryResult found;
-    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &f, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess)
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess || found != cudaDriverEntryPointSuccess)
       f = nullptr;
     return reinterpret_cast<Encode>(f);
   }();
