@@ -22,26 +22,31 @@ namespace {
 
 using Staged = Tiled<128, false, false, 1, WeightsK::kSpan>;
 
-// a single CTA's tile: 16 tokens where there are no more
+// Whether a pair's product reads staged codes: staging costs its bytes, and saves each tile along N the conversion
+// (8,192 x 4,096 codes: 15 us; their product with 1,024 weights 51 us converted, 40 us staged, with 4,096 207 and 162).
+bool stages_codes(int64_t N) { return N >= 1536; }
+
+// the other tiles: 16 tokens where there are no more
 template <class F>
 auto with_forward_tile(int64_t M, const F &f) {
   if (M <= 16) return f(std::integral_constant<int, 16>());
   return with_single_tile(M, f);
 }
 
-int64_t partial_bytes(const GemmPlan &p, int64_t M, int64_t N) {
-  return p.splits > 1 ? p.splits * M * N * static_cast<int64_t>(sizeof(float)) : 0;
-}
+constexpr int64_t kFloat = sizeof(float);
 
 }  // namespace
 
-// the splits' sums, and before them the staged codes
+// the staged codes, and the splits' sums
 int64_t aap_linear_workspace(int64_t M, int64_t K, int64_t N) {
   const int sms = sm_count();
-  if (pair_tiles(N, M)) return partial_bytes(gemm_plan<WeightsK, Staged, 256, 2>(N, M, K, sms), M, N) + 2 * M * staged_k(K);
+  if (pair_tiles(N, M, sms)) {
+    if (stages_codes(N)) return partial_floats(gemm_plan<WeightsK, Staged, 256, 2>(N, M, K, sms), N, M) * kFloat + 2 * M * staged_k(K);
+    return partial_floats(gemm_plan<WeightsK, CodesK<128>, 256, 2>(N, M, K, sms), N, M) * kFloat;
+  }
   return with_forward_tile(M, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
-    return partial_bytes(gemm_plan<WeightsK, CodesK<TB>, TB, 1>(N, M, K, sms), M, N);
+    return partial_floats(gemm_plan<WeightsK, CodesK<TB>, TB, 1>(N, M, K, sms), N, M) * kFloat;
   });
 }
 
@@ -49,7 +54,12 @@ cudaError_t launch_aap_linear(const AapLinearCall &c, cudaStream_t st) {
   const WeightsK a = {c.packed, c.N, c.K, weights_unit(c.packed, c.K)};
   const OutY out = {c.y, c.dtype, c.N, c.scale, c.w_scale, c.bias};
   const int sms = sm_count();
-  if (pair_tiles(c.N, c.M)) {
+  if (pair_tiles(c.N, c.M, sms)) {
+    if (!stages_codes(c.N)) {
+      const CodesK<128> b = {c.codes, c.M, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
+      return launch_gemm<WeightsK, CodesK<128>, OutY, 256, 2>(c.N, c.M, c.K, a, b, out, static_cast<float *>(c.workspace), sms,
+                                                             linear_status(), st);
+    }
     cudaError_t e = launch_stage_codes(c.codes, c.ldc, c.M, c.K, c.workspace, st);
     if (e != cudaSuccess) return e;
     Staged b;

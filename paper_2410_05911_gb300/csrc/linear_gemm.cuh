@@ -614,7 +614,8 @@ struct GemmArgs {
   Out out;
   int tiles_i, steps;  // tiles along i (whole clusters); steps of a split
   int full;            // r that are left for a span to be loaded by full(), more than there are without alignment
-  float *partial;      // [splits][J][I] where there are several, else NULL
+  int parts;           // splits that are one cluster and join in shared memory (CG = 1), else 1
+  float *partial;      // [splits][J][I] where several join in a second kernel, else NULL
   int *err;            // set to 1 by a wait that gave up
 };
 
@@ -625,7 +626,11 @@ struct GemmShape {
   static constexpr uint32_t kABytes = tile_bytes(A::kMN, kTileI);
   static constexpr uint32_t kPieceBytes = B::kTma ? TB / CG * 128u : tile_bytes(B::kMN, TB / CG);
   static constexpr uint32_t kOperands = kABytes + B::P * kPieceBytes;
-  static constexpr uint32_t kStageBytes = B::kTma ? (kOperands + 1023u) & ~1023u : kOperands;
+  static constexpr uint32_t kStepBytes = B::kTma ? (kOperands + 1023u) & ~1023u : kOperands;
+  // steps of a stage: a single CTA's product has its barriers once a span (they cost the issuing warp more than
+  // the MMAs of its narrower step)
+  static constexpr int kSteps = CG == 1 ? A::kSpan : 1;
+  static constexpr uint32_t kStageBytes = kSteps * kStepBytes;
   static constexpr uint32_t kBars = 256 + TB * 4;  // barriers and two words; the columns' factors
   static constexpr int fit(uint32_t room) { return static_cast<int>((room - kBars) / kStageBytes); }
   static constexpr uint32_t kHalfSm = kSmemPerSm / 2 - 1024;
@@ -635,6 +640,7 @@ struct GemmShape {
   static constexpr uint32_t kSmem = kStages * kStageBytes + kBars;
   static constexpr uint32_t kTmemCols = TB < 32 ? 32 : TB;
   static_assert(kStages >= 2 && kStageBytes % 16 == 0 && kCtasPerSm * kTmemCols <= 512, "stages and accumulators");
+  static_assert(CG == 2 || kStages * kStageBytes >= kTileI * TB * 4, "a cluster joins its tile in the stages");
   static_assert(A::kSpan == B::kSpan, "operands load together");
 };
 
@@ -645,11 +651,11 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   using S = GemmShape<A, B, TB, CG>;
   extern __shared__ __align__(1024) uint8_t smem[];
   const uint32_t base = smem_u32(smem);
-  // full[stages] (this CTA's producers), copied[stages] (its copies), peer[stages] (the other CTA's stage),
-  // empty[stages], done; 2 words
+  // full[stages]: this CTA's producers, its copies, and in a pair's first CTA the other's stage, in one barrier (each
+  // wait costs the issuing warp some 200 cycles); empty[stages], done; 2 words
   constexpr uint32_t kB = 8 * S::kStages;
-  const uint32_t full = base + S::kStages * S::kStageBytes, copied = full + kB, peer = copied + kB, empty = peer + kB, done = empty + kB;
-  volatile uint32_t *word = reinterpret_cast<volatile uint32_t *>(smem + S::kStages * S::kStageBytes + 4 * kB + 8);
+  const uint32_t full = base + S::kStages * S::kStageBytes, empty = full + kB, done = empty + kB;
+  volatile uint32_t *word = reinterpret_cast<volatile uint32_t *>(smem + S::kStages * S::kStageBytes + 2 * kB + 8);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = CG == 2 ? cluster_ctarank() : 0;
   const int64_t i0 = static_cast<int64_t>(blockIdx.x % g.tiles_i) * kTileI, j0 = static_cast<int64_t>(blockIdx.x / g.tiles_i) * TB;
@@ -658,7 +664,7 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   const int steps = kSpan * static_cast<int>((end - first + kSpan * kStep - 1) / (kSpan * kStep));
 
   if (tid == 0) {
-    for (int s = 0; s < S::kStages; ++s) mbar_init(full + 8 * s, kGroupWarps), mbar_init(copied + 8 * s, 1), mbar_init(peer + 8 * s, 1), mbar_init(empty + 8 * s, 1);
+    for (int s = 0; s < S::kStages; ++s) mbar_init(full + 8 * s, kGroupWarps + (B::kTma ? 1 : 0) + (CG == 2 && rank == 0 ? 1 : 0)), mbar_init(empty + 8 * s, 1);
     mbar_init(done, 1);
     fence_mbar_init_cluster();
     word[1] = 0;
@@ -703,7 +709,7 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     };
     int s = 0;
     uint32_t parity = 1;  // (a stage's first wait is for the phase before its first, and over at once)
-    skip(s, parity, group * kSpan);
+    skip(s, parity, group * (kSpan / S::kSteps));
     // the group's spans: `load` the next one's B, `store` the step's
     const auto produce = [&](const auto &load_b, const auto &store_b) {
       load_a(), load_b(left);
@@ -711,17 +717,20 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
       for (int it = group * kSpan; it < steps; it += kGroups * kSpan) {
 #pragma unroll
         for (int h = 0; h < kSpan; ++h) {
-          if (!__all_sync(0xffffffffu, wait(empty + 8 * s, parity))) return;
-          const uint32_t stage = base + s * S::kStageBytes;
-          g.a.store(ta, ra, h == 1, stage + B::P * S::kPieceBytes);
-          store_b(h == 1, stage);
-          __syncwarp();
-          if (lane == 0) mbar_arrive(full + 8 * s);
-          skip(s, parity, 1);
+          const bool opens = h % S::kSteps == 0, closes = h % S::kSteps == S::kSteps - 1;
+          if (opens && !__all_sync(0xffffffffu, wait(empty + 8 * s, parity))) return;
+          const uint32_t tile = base + s * S::kStageBytes + h % S::kSteps * S::kStepBytes;
+          g.a.store(ta, ra, h == 1, tile + B::P * S::kPieceBytes);
+          store_b(h == 1, tile);
+          if (closes) {
+            __syncwarp();
+            if (lane == 0) mbar_arrive(full + 8 * s);
+            skip(s, parity, 1);
+          }
         }
         load_a(), load_b(left);
         left -= kGroups * kSpanR;
-        skip(s, parity, (kGroups - 1) * kSpan);
+        skip(s, parity, (kGroups - 1) * (kSpan / S::kSteps));
       }
     };
     if constexpr (B::kTma) {
@@ -741,31 +750,33 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     // the loads in flight.  In the second CTA that is all; it tells the first.
     constexpr uint32_t idesc = gemm_idesc(B::kBf, A::kMN, B::kMN, 128 * CG, TB);
     constexpr uint32_t la = tile_lbo(A::kMN), lb = tile_lbo(B::kMN);
-    const uint32_t peer0 = CG == 2 ? mapa_cluster(peer, 0) : peer;
+    const uint32_t full0 = CG == 2 ? mapa_cluster(full, 0) : full;
     int s = 0;
     uint32_t parity = 0;
-    for (int it = 0; it < steps; ++it) {
-      if (!__all_sync(0xffffffffu, wait(full + 8 * s, parity) && (!B::kTma || wait(copied + 8 * s, parity)))) break;
+    for (int it = 0; it < steps; it += S::kSteps) {
+      if (!__all_sync(0xffffffffu, wait(full + 8 * s, parity))) break;
       fence_proxy_async_smem();
       if (rank == 0) {
-        if (CG == 2 && !__all_sync(0xffffffffu, wait(peer + 8 * s, parity))) break;
         tc_fence_after();
-        const uint32_t bt = base + s * S::kStageBytes, at = bt + P * S::kPieceBytes;
 #pragma unroll
-        for (int p = 0; p < P; ++p)
+        for (int u = 0; u < S::kSteps; ++u) {
+          const uint32_t bt = base + s * S::kStageBytes + u * S::kStepBytes, at = bt + P * S::kPieceBytes;
 #pragma unroll
-          for (int ks = 0; ks < kStep / 16; ++ks) {
-            const uint32_t b = bt + p * S::kPieceBytes;
-            const uint64_t bdesc = !B::kTma  ? make_sdesc(b + ks * 2 * lb, lb, tile_sbo(B::kMN))
-                                   : B::kMN ? make_sdesc_sw128(b + ks * 2048, 8192, 1024)
-                                            : make_sdesc_sw128(b + ks * 32, 16, 1024);
-            mma_f16_cg_warp<CG>(tmem, make_sdesc(at + ks * 2 * la, la, tile_sbo(A::kMN)), bdesc, idesc,
-                                it > 0 || p > 0 || ks > 0 ? 1u : 0u);
-          }
+          for (int p = 0; p < P; ++p)
+#pragma unroll
+            for (int ks = 0; ks < kStep / 16; ++ks) {
+              const uint32_t b = bt + p * S::kPieceBytes;
+              const uint64_t bdesc = !B::kTma  ? make_sdesc(b + ks * 2 * lb, lb, tile_sbo(B::kMN))
+                                     : B::kMN ? make_sdesc_sw128(b + ks * 2048, 8192, 1024)
+                                              : make_sdesc_sw128(b + ks * 32, 16, 1024);
+              mma_f16_cg_warp<CG>(tmem, make_sdesc(at + ks * 2 * la, la, tile_sbo(A::kMN)), bdesc, idesc,
+                                  it > 0 || u > 0 || p > 0 || ks > 0 ? 1u : 0u);
+            }
+        }
         mma_commit_cg_warp<CG>(empty + 8 * s);
       } else {
         __syncwarp();
-        if (lane == 0) mbar_arrive_peer(peer0 + 8 * s);
+        if (lane == 0) mbar_arrive_peer(full0 + 8 * s);
       }
       if (++s == S::kStages) s = 0, parity ^= 1;
     }
@@ -777,25 +788,58 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     for (; it < steps; ++it) {
       if (!__all_sync(0xffffffffu, wait(empty + 8 * s, parity))) break;
       if (lane == 0) {
-        mbar_arrive_expect_tx(copied + 8 * s, P * S::kPieceBytes);
-        g.b.copy(x0, first + static_cast<int64_t>(it) * kStep, base + s * S::kStageBytes, copied + 8 * s);
+        mbar_arrive_expect_tx(full + 8 * s, P * S::kPieceBytes);
+        g.b.copy(x0, first + static_cast<int64_t>(it) * kStep, base + s * S::kStageBytes, full + 8 * s);
       }
       __syncwarp();
       if (++s == S::kStages) s = 0, parity ^= 1;
     }
-    // a CTA that gives up still waits for the copies it has begun
-    for (int k = it < S::kStages ? 0 : it - S::kStages; k < it; ++k)
-      for (int tries = 0; !mbar_try_wait(copied + 8 * (k % S::kStages), (k / S::kStages) & 1) && tries < kGemmWaitTries; ++tries) {}
+    // a CTA that gives up still waits for the copies it has begun: until they are over, or with an end
+    if (it < steps)
+      for (int k = it < S::kStages ? 0 : it - S::kStages; k < it; ++k)
+        for (int tries = 0; !mbar_try_wait(full + 8 * (k % S::kStages), (k / S::kStages) & 1) && tries < kGemmWaitTries; ++tries) {}
   }
   __syncwarp();
   const bool ready = __all_sync(0xffffffffu, wait(done, 0) && !word[1]);
   tc_fence_after();
-  if (warp < kProducerWarps && ready) {
-    const int row = 32 * (warp & 3) + lane;  // of the tile, and the lane of tensor memory
-    const int64_t i = i0 + (A::kMixed ? (row & ~15) | mix16(row & 15) : row);
-    constexpr int kColumns = TB / (kProducerWarps / 4);  // of each of the warps of a lane quadrant
-    const int c0 = (warp >> 2) * kColumns, columns = rows_left(g.J - j0 - c0);
-    const uint32_t tl = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + c0;
+  const int row = 32 * (warp & 3) + lane;  // of the tile, and the lane of tensor memory
+  const int64_t i = i0 + (A::kMixed ? (row & ~15) | mix16(row & 15) : row);
+  constexpr int kColumns = TB / (kProducerWarps / 4);  // of each of the warps of a lane quadrant
+  const int c0 = ((warp >> 2) & 3) * kColumns;
+  const uint32_t tl = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + c0;
+  if (CG == 1 && g.parts > 1) {
+    // A cluster's CTAs hold sums over parts of R.  Each joins TB / parts of the columns: the others send theirs to
+    // its shared memory (the stages, once every CTA is done with its own), and it adds them in the parts' order.
+    const int part = blockIdx.y, mine = TB / g.parts;
+    cluster_sync_all();
+    if (warp < kProducerWarps && ready) {
+      constexpr int kGroup = kColumns < 16 ? kColumns : 16;
+#pragma unroll 1
+      for (int c = 0; c < kColumns; c += kGroup) {
+        float v[kGroup];
+        tmem_ld<kGroup>(tl + c, v);
+        tmem_wait_ld();
+#pragma unroll
+        for (int e = 0; e < kGroup; ++e) {
+          const int to = (c0 + c + e) / mine, at = part * mine + (c0 + c + e) - to * mine;
+          st_cluster_f32(mapa_cluster(base + 4u * (at * kTileI + row), to), steps > 0 ? v[e] : 0.0f);
+        }
+      }
+    }
+    cluster_sync_all();
+    if (warp < kProducerWarps && ready && i < g.I) {
+      const float *sums = reinterpret_cast<const float *>(smem);
+      const float add = g.out.add(i);
+      for (int c = warp >> 2; c < mine; c += kProducerWarps / 4) {
+        const int64_t jj = j0 + part * mine + c;
+        if (jj >= g.J) break;
+        float v = 0.0f;
+        for (int k = 0; k < g.parts; ++k) v += sums[(k * mine + c) * kTileI + row];
+        put_element(g.out.y, g.out.dtype, jj * g.out.ld + i, fmaf(v, factor[part * mine + c], add));
+      }
+    }
+  } else if (warp < kProducerWarps && ready) {
+    const int columns = rows_left(g.J - j0 - c0);
     const bool live = i < g.I;
     const float add = !g.partial && live ? g.out.add(i) : 0.0f;
     const int64_t at = (j0 + c0) * g.out.ld + i;
@@ -841,25 +885,35 @@ bool grads_vec(const void *dy, int64_t ld, int64_t N) {
   return (reinterpret_cast<uintptr_t>(dy) & 15u) == 0 && ld * static_cast<int64_t>(sizeof(T)) % 16 == 0 && N % 8 == 0;
 }
 
-// How the sum over R is split: into as many parts as leave every SM a tile, of at least kMinSteps steps each.
+// How the sum over R is split where there are fewer tiles than SMs: into as many parts as SMs are left for, of at least
+// kMinSteps steps each.  (Two CTAs to an SM for the parts' sake, or parts of a full grid, lose more in the joining
+// than they gain: 8,192 x 4,096 x 512 46 us whole, 59 us in two parts, 72 in four.)  Up to 8 parts of a single CTA's
+// tiles are a cluster, which joins them itself (a power of two, as it divides the tile's columns); more, or a
+// pair's, leave their sums in memory for a second kernel.
 struct GemmPlan {
   int64_t tiles_i, tiles_j;
   int splits, steps;
+  bool cluster;
 };
-constexpr int kMinSteps = 4;
+constexpr int kMinSteps = 8;
 template <class A, class B, int TB, int CG>
 GemmPlan gemm_plan(int64_t I, int64_t J, int64_t R, int sms) {
   GemmPlan p;
   p.tiles_i = (I + CG * kTileI - 1) / (CG * kTileI) * CG, p.tiles_j = (J + TB - 1) / TB;
-  const int64_t all = (R + kStep - 1) / kStep, room = static_cast<int64_t>(sms) * GemmShape<A, B, TB, CG>::kCtasPerSm;
-  int64_t splits = room / (p.tiles_i * p.tiles_j);
+  const int64_t all = (R + kStep - 1) / kStep;
+  int64_t splits = sms / (p.tiles_i * p.tiles_j);
   if (splits > all / kMinSteps) splits = all / kMinSteps;
   if (splits < 1) splits = 1;
+  p.cluster = CG == 1 && splits > 1 && splits < 16;
+  if (p.cluster) splits = splits >= 8 ? 8 : splits >= 4 ? 4 : 2;
   const int64_t steps = (all + splits - 1) / splits;
   p.steps = static_cast<int>((steps + A::kSpan - 1) / A::kSpan * A::kSpan);
-  p.splits = static_cast<int>((all + p.steps - 1) / p.steps);
+  // (a cluster keeps its parts, the last ones empty where R runs out)
+  p.splits = p.cluster ? static_cast<int>(splits) : static_cast<int>((all + p.steps - 1) / p.steps);
   return p;
 }
+// floats of workspace that the splits' sums take
+inline int64_t partial_floats(const GemmPlan &p, int64_t I, int64_t J) { return p.splits > 1 && !p.cluster ? p.splits * I * J : 0; }
 
 template <class A, class B, class Out, int TB, int CG>
 cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b, const Out &out, float *partial, int sms, int *err,
@@ -867,13 +921,14 @@ cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b,
   using S = GemmShape<A, B, TB, CG>;
   const GemmPlan p = gemm_plan<A, B, TB, CG>(I, J, R, sms);
   const GemmArgs<A, B, Out> g = {I, J, R, a, b, out, static_cast<int>(p.tiles_i), p.steps,
-                                   a.aligned() && b.aligned() ? A::kSpan * kStep : INT_MAX, p.splits > 1 ? partial : nullptr, err};
+                                   a.aligned() && b.aligned() ? A::kSpan * kStep : INT_MAX, p.cluster ? p.splits : 1,
+                                   p.splits > 1 && !p.cluster ? partial : nullptr, err};
   auto *kernel = gemm_kernel<A, B, Out, TB, CG>;
   cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
   if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
-  attr[0].val.clusterDim.x = CG, attr[0].val.clusterDim.y = 1, attr[0].val.clusterDim.z = 1;
+  attr[0].val.clusterDim.x = CG, attr[0].val.clusterDim.y = p.cluster ? p.splits : 1, attr[0].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(p.tiles_i * p.tiles_j), p.splits);
   cfg.blockDim = dim3(kGemmThreads);
@@ -881,16 +936,18 @@ cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b,
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
-  if ((e = cudaLaunchKernelEx(&cfg, kernel, g)) != cudaSuccess || p.splits == 1) return e;
+  if ((e = cudaLaunchKernelEx(&cfg, kernel, g)) != cudaSuccess || !g.partial) return e;
   gemm_join_kernel<Out><<<dim3(static_cast<unsigned>((I + 255) / 256), static_cast<unsigned>(J < 65535 ? J : 65535)), 256, 0, st>>>(
       partial, p.splits, I, J, out);
   return cudaGetLastError();
 }
 
-// The tile of a product: f(TB, CG).  More than one tile of 128 of both i and j: a pair's, whose B is copied by
-// TMA (staged first where memory does not hold it in 16 bits).  Else a single CTA's, which converts B itself:
-// of 64 j at most where there are no more (the rest of a tile would be converted zeros), of 128.
-inline bool pair_tiles(int64_t I, int64_t J) { return I > kTileI && J > kTileI; }
+// The tile of a product.  A pair's 256 x 256 where those fill half of the SMs at least (2,048 x 1,024 x 1,024: 64 CTAs in
+// pairs 16.7 us, 128 single ones 12.7 us; 1,024 x 4,096 x 4,096: 128 in pairs 46 us, 256 single ones 58 us), else a
+// single CTA's, of 64 j at most where there are no more (the rest of a tile would be converted zeros), of 128.
+inline bool pair_tiles(int64_t I, int64_t J, int sms) {
+  return I > kTileI && J > kTileI && 2 * ((I + 255) / 256 * 2) * ((J + 255) / 256) >= sms;
+}
 template <class F>
 auto with_single_tile(int64_t J, const F &f) {
   return J <= 64 ? f(std::integral_constant<int, 64>()) : f(std::integral_constant<int, 128>());

@@ -25,16 +25,14 @@ bool in_place(const void *dy, int64_t ld) {
   return sizeof(T) == 2 && (reinterpret_cast<uintptr_t>(dy) & 15u) == 0 && ld % 8 == 0;
 }
 
-int64_t partial_bytes(const GemmPlan &p, int64_t M, int64_t K) {
-  return p.splits > 1 ? p.splits * M * K * static_cast<int64_t>(sizeof(float)) : 0;
-}
+constexpr int64_t kFloat = sizeof(float);
 
 template <typename T>
 cudaError_t input_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t st) {
   const Weights<T> a = {c.packed, c.N, c.K, weights_unit(c.packed, c.K)};
   const OutX out = {c.dx, c.dtype, c.K, c.w_scale};
   const int sms = sm_count();
-  if (pair_tiles(c.K, c.M)) {
+  if (pair_tiles(c.K, c.M, sms)) {
     Staged<T> b;
     const void *rows = c.dy;
     int64_t ld = c.lddy;
@@ -59,10 +57,10 @@ cudaError_t input_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t s
 template <typename T>
 int64_t input_grad_workspace(int64_t M, int64_t K, int64_t N) {
   const int sms = sm_count();
-  if (pair_tiles(K, M)) return partial_bytes(gemm_plan<Weights<T>, Staged<T>, 256, 2>(K, M, N, sms), M, K) + 2 * kPieces<T> * M * padded(N);
+  if (pair_tiles(K, M, sms)) return partial_floats(gemm_plan<Weights<T>, Staged<T>, 256, 2>(K, M, N, sms), K, M) * kFloat + 2 * kPieces<T> * M * padded(N);
   return with_single_tile(M, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
-    return partial_bytes(gemm_plan<Weights<T>, GradK<T, TB>, TB, 1>(K, M, N, sms), M, K);
+    return partial_floats(gemm_plan<Weights<T>, GradK<T, TB>, TB, 1>(K, M, N, sms), K, M) * kFloat;
   });
 }
 

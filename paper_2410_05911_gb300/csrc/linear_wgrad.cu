@@ -19,9 +19,7 @@ int pieces_of(int64_t M, int wdtype) { return wdtype == 0 ? 3 : wdtype == 1 || M
 
 int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
 
-int64_t partial_bytes(const GemmPlan &p, int64_t N, int64_t K) {
-  return p.splits > 1 ? p.splits * N * K * static_cast<int64_t>(sizeof(float)) : 0;
-}
+constexpr int64_t kFloat = sizeof(float);
 
 int64_t sums_bytes(int64_t M, int64_t N) { return up16(static_cast<int64_t>(stage_parts(M, N)) * N * sizeof(float)); }
 
@@ -60,10 +58,10 @@ cudaError_t weight_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t 
 template <int P>
 int64_t workspace_of(int64_t M, int64_t K, int64_t N) {
   const int sms = sm_count();
-  if (pair_tiles(K, N)) return partial_bytes(gemm_plan<CodesT, Staged<P>, 256, 2>(K, N, M, sms), N, K) + 2 * P * M * padded(N);
+  if (pair_tiles(K, N, sms)) return partial_floats(gemm_plan<CodesT, Staged<P>, 256, 2>(K, N, M, sms), K, N) * kFloat + 2 * P * M * padded(N);
   return with_single_tile(N, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
-    return partial_bytes(gemm_plan<CodesT, GradT<float, TB, P>, TB, 1>(K, N, M, sms), N, K);
+    return partial_floats(gemm_plan<CodesT, GradT<float, TB, P>, TB, 1>(K, N, M, sms), K, N) * kFloat;
   });
 }
 
@@ -78,7 +76,7 @@ int64_t weight_grad_workspace(int64_t M, int64_t K, int64_t N, int wdtype) {
 cudaError_t launch_weight_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t st) {
   const int p = pieces_of(c.M, c.wdtype);
   uint8_t *rest = work + sums_bytes(c.M, c.N);
-  const bool staged = c.dw && pair_tiles(c.K, c.N);
+  const bool staged = c.dw && pair_tiles(c.K, c.N, sm_count());
   if (staged || c.db) {
     const StageGrads s = {c.dy, c.lddy, c.M, c.N, c.dtype, c.scale, staged ? p : 1, staged ? rest : nullptr, c.db, reinterpret_cast<float *>(work)};
     const cudaError_t e = launch_stage_grads(s, st);
