@@ -423,68 +423,38 @@ def spe_table(H: np.ndarray, params, want_eigen: bool = False):
 # operators of AAP layers of any width
 # ------------------------------------------------------------------------------------------
 _ELEMENT = {}  # torch type -> the C ABI's number
+_binding = None
 
 
-def _element(dtype):
-    """The C ABI's number of an activation or gradient type, None for another type."""
-    if not _ELEMENT:
+def _operators():
+    """The compiled tensor side of the operators (csrc/torch_binding.cpp)."""
+    global _binding
+    if _binding is None:
+        import importlib.machinery
+        import importlib.util
+
         import torch
 
+        load()
+        if not os.path.exists(build_lib.BINDING_PATH):
+            raise OSError(f"aecct_torch.so not built at {build_lib.BINDING_PATH}")
+        loader = importlib.machinery.ExtensionFileLoader("aecct_torch", build_lib.BINDING_PATH)
+        m = importlib.util.module_from_spec(importlib.util.spec_from_loader("aecct_torch", loader))
+        loader.exec_module(m)
+        m.setup(_stream_of, _check)
         _ELEMENT.update({torch.float32: 0, torch.float16: 1, torch.bfloat16: 2})
-    return _ELEMENT.get(dtype)
-
-
-def _rows(t):
-    """(tensor, elements from row to row): rows of the last dimension, read where they lie if they are an
-    equal distance apart, else from a contiguous copy."""
-    if t.is_contiguous():
-        return t, t.shape[-1]
-    if t.dim() == 2 and t.stride(1) == 1 and t.stride(0) >= t.shape[1]:
-        return t, t.stride(0)
-    return t.contiguous(), t.shape[-1]
-
-
-def _check_like(name, t, x, dtype=None):
-    if t.device != x.device or t.dtype != (dtype or x.dtype) or t.shape != x.shape:
-        raise ValueError(f"{name} must be a {dtype or x.dtype} tensor of shape {tuple(x.shape)} on {x.device}")
-
-
-def _check_rows(name, t, gain):
-    """`t` holds rows of a known type on the GPU, and `gain` one float32 for each element of a row."""
-    import torch
-
-    if not t.is_cuda or _element(t.dtype) is None or t.dim() < 1:
-        raise ValueError(f"{name} must be a float32, float16 or bfloat16 CUDA tensor of rows")
-    if gain.device != t.device or gain.dtype != torch.float32 or gain.dim() != 1 or gain.shape[0] != t.shape[-1]:
-        raise ValueError(f"gain must be a float32 tensor of shape ({t.shape[-1]},) on {t.device}")
+        _binding = m
+    return _binding
 
 
 def rms_quant(x, gain, residual=None, eps: float = 1e-6, want_values: bool = False, stream=None):
     """aecct_rms_quant: h = x + residual, its root-mean-square norm times gain, and eq. Quant of that, a
     row (the last dimension) at a time, on `stream` after what is queued on the current one.
 
-    Returns (codes int8 like x, scale float32 x.shape[:-1], total, values): codes * scale is the norm's output;
-    total is h in x's type (x itself without a residual); values is codes * scale in x's type, or None."""
-    import torch
-
-    _check_rows("x", x, gain)
-    if residual is not None:
-        _check_like("residual", residual, x)
-    dev, d = x.device, x.shape[-1]
-    src, ldx = _rows(x)
-    res, ldr = _rows(residual) if residual is not None else (None, 0)
-    gain = gain.contiguous()
-    codes = torch.empty(x.shape, dtype=torch.int8, device=dev)
-    scale = torch.empty(x.shape[:-1], dtype=torch.float32, device=dev)
-    total = torch.empty(x.shape, dtype=x.dtype, device=dev) if residual is not None else x
-    values = torch.empty(x.shape, dtype=x.dtype, device=dev) if want_values else None
-    s = _stream_of(stream, dev, (src, res, gain, codes, scale, total, values))
-    st = load().aecct_rms_quant(src.data_ptr(), ldx, res.data_ptr() if res is not None else None, ldr, gain.data_ptr(),
-                                scale.numel(), d, _element(x.dtype), eps,
-                                total.data_ptr() if res is not None else None, codes.data_ptr(), scale.data_ptr(),
-                                values.data_ptr() if values is not None else None, s.cuda_stream)
-    _check(st, "aecct_rms_quant")
-    return codes, scale, total, values
+    x and residual are float32, float16 or bfloat16, gain is float32 [d].  Returns (codes int8 like x, scale float32
+    x.shape[:-1], total, values): codes * scale is the norm's output; total is h in x's type (x itself
+    without a residual); values is codes * scale in x's type, or None."""
+    return (_binding or _operators()).rms_quant(x, gain, residual, eps, bool(want_values), stream)
 
 
 def rms_quant_backward(dy, total, gain, dtotal=None, eps: float = 1e-6, stream=None):
@@ -492,49 +462,7 @@ def rms_quant_backward(dy, total, gain, dtotal=None, eps: float = 1e-6, stream=N
     the gradient of codes * scale, total the sum that the forward pass returned, dtotal the gradient that
     reaches it by another way (the residual stream's own).  Returns (dx, dgain): dx is the gradient of x and
     of residual alike, in their type; dgain is float32."""
-    import torch
-
-    _check_rows("dy", dy, gain)
-    _check_like("total", total, dy)
-    if dtotal is not None:
-        _check_like("dtotal", dtotal, dy)
-    dev, d = dy.device, dy.shape[-1]
-    rows = dy.numel() // d if d else 0
-    g, lddy = _rows(dy)
-    h, ldh = _rows(total)
-    dt, ldd = _rows(dtotal) if dtotal is not None else (None, 0)
-    gain = gain.contiguous()
-    L = load()
-    size = ctypes.c_int64()
-    _check(L.aecct_rms_quant_backward_workspace(rows, d, ctypes.byref(size)), "aecct_rms_quant_backward")
-    dx = torch.empty(dy.shape, dtype=dy.dtype, device=dev)
-    dgain = torch.empty(d, dtype=torch.float32, device=dev)
-    work = torch.empty(max(1, size.value), dtype=torch.uint8, device=dev)
-    s = _stream_of(stream, dev, (g, h, dt, gain, dx, dgain, work))
-    st = L.aecct_rms_quant_backward(g.data_ptr(), lddy, h.data_ptr(), ldh, dt.data_ptr() if dt is not None else None, ldd,
-                                    gain.data_ptr(), rows, d, _element(dy.dtype), eps, dx.data_ptr(), dgain.data_ptr(),
-                                    work.data_ptr(), size.value, s.cuda_stream)
-    _check(st, "aecct_rms_quant_backward")
-    return dx, dgain
-
-
-def _check_linear(codes, scale, packed, w_scale):
-    """(tokens, K, N) of an AAP linear layer's operands."""
-    import torch
-
-    dev = codes.device
-    if not codes.is_cuda or codes.dtype != torch.int8 or codes.dim() < 1:
-        raise ValueError("codes must be an int8 CUDA tensor of rows")
-    K = codes.shape[-1]
-    if scale.device != dev or scale.dtype != torch.float32 or scale.shape != codes.shape[:-1]:
-        raise ValueError(f"scale must be a float32 tensor of shape {tuple(codes.shape[:-1])} on {dev}")
-    if packed.device != dev or packed.dtype != torch.uint8 or not packed.is_contiguous():
-        raise ValueError(f"packed must be a contiguous uint8 tensor on {dev}")
-    if K < 4 or K % 4 or packed.numel() % (K // 4):
-        raise ValueError(f"rows of {K} codes do not divide weights of {4 * packed.numel()}: K is a multiple of 4")
-    if w_scale.device != dev or w_scale.dtype != torch.float32 or w_scale.numel() != 1:
-        raise ValueError(f"w_scale must be a float32 tensor of one element on {dev}")
-    return scale.numel(), K, packed.numel() // (K // 4)
+    return (_binding or _operators()).rms_quant_backward(dy, total, gain, dtotal, eps, stream)
 
 
 def aap_linear(codes, scale, packed, w_scale, bias=None, dtype=None, stream=None):
@@ -542,30 +470,8 @@ def aap_linear(codes, scale, packed, w_scale, bias=None, dtype=None, stream=None
     scale each (those of rms_quant), and the 2-bit ternary weights T [N, K] of aap_ternarize: packed uint8
     (N * K / 4 bytes) and their scale, a float32 tensor of one element.  bias is float32 [N] or None.  Returns
     y [..., N] of `dtype` (float32 unless given)."""
-    import torch
-
-    M, K, N = _check_linear(codes, scale, packed, w_scale)
-    dtype = torch.float32 if dtype is None else dtype
-    if _element(dtype) is None:
-        raise ValueError("dtype must be float32, float16 or bfloat16")
-    dev = codes.device
-    if bias is not None:
-        if bias.device != dev or bias.dtype != torch.float32 or bias.shape != (N,):
-            raise ValueError(f"bias must be a float32 tensor of shape ({N},) on {dev}")
-        bias = bias.contiguous()
-    q, ldc = _rows(codes)
-    scale = scale.contiguous()
-    L = load()
-    size = ctypes.c_int64()
-    _check(L.aecct_aap_linear_workspace(M, K, N, ctypes.byref(size)), "aecct_aap_linear")
-    y = torch.empty(codes.shape[:-1] + (N,), dtype=dtype, device=dev)
-    work = torch.empty(size.value, dtype=torch.uint8, device=dev) if size.value else None
-    s = _stream_of(stream, dev, (q, scale, packed, w_scale, bias, y, work))
-    st = L.aecct_aap_linear(q.data_ptr(), ldc, scale.data_ptr(), packed.data_ptr(), w_scale.data_ptr(),
-                            bias.data_ptr() if bias is not None else None, M, K, N, _element(dtype), y.data_ptr(),
-                            work.data_ptr() if work is not None else None, size.value, s.cuda_stream)
-    _check(st, "aecct_aap_linear")
-    return y
+    ops = _binding or _operators()
+    return ops.aap_linear(codes, scale, packed, w_scale, bias, 0 if dtype is None else _ELEMENT.get(dtype), stream)
 
 
 def aap_linear_backward(dy, codes, scale, packed, w_scale, weight_dtype=None, want=(True, True, True), stream=None):
@@ -573,67 +479,16 @@ def aap_linear_backward(dy, codes, scale, packed, w_scale, weight_dtype=None, wa
     (dx, dw, db), None where `want` says that one is not wanted: dx [..., K] in dy's type is the gradient of
     codes * scale (rms_quant_backward takes it), dw [N, K] in weight_dtype (float32 unless given) that of the
     weights behind aap_ternarize, passed straight through, db [N] float32 that of the bias."""
-    import torch
-
-    M, K, N = _check_linear(codes, scale, packed, w_scale)
-    weight_dtype = torch.float32 if weight_dtype is None else weight_dtype
-    dev = codes.device
-    if _element(weight_dtype) is None:
-        raise ValueError("weight_dtype must be float32, float16 or bfloat16")
-    if dy.device != dev or _element(dy.dtype) is None or dy.shape != codes.shape[:-1] + (N,):
-        raise ValueError(f"dy must be a float32, float16 or bfloat16 tensor of shape {tuple(codes.shape[:-1]) + (N,)} on {dev}")
-    g, lddy = _rows(dy)
-    q, ldc = _rows(codes)
-    scale = scale.contiguous()
-    L = load()
-    size = ctypes.c_int64()
-    kinds = _element(dy.dtype), _element(weight_dtype)
-    _check(L.aecct_aap_linear_backward_workspace(M, K, N, *kinds, ctypes.byref(size)), "aecct_aap_linear_backward")
-    dx = torch.empty(codes.shape, dtype=dy.dtype, device=dev) if want[0] else None
-    dw = torch.empty((N, K), dtype=weight_dtype, device=dev) if want[1] else None
-    db = torch.empty(N, dtype=torch.float32, device=dev) if want[2] else None
-    work = torch.empty(size.value, dtype=torch.uint8, device=dev) if size.value else None
-    s = _stream_of(stream, dev, (g, q, scale, packed, w_scale, dx, dw, db, work))
-    ptr = lambda t: t.data_ptr() if t is not None else None  # noqa: E731
-    st = L.aecct_aap_linear_backward(g.data_ptr(), lddy, q.data_ptr(), ldc, scale.data_ptr(), packed.data_ptr(),
-                                     w_scale.data_ptr(), M, K, N, *kinds, ptr(dx), ptr(dw), ptr(db), ptr(work), size.value,
-                                     s.cuda_stream)
-    _check(st, "aecct_aap_linear_backward")
-    return dx, dw, db
+    ops = _binding or _operators()
+    return ops.aap_linear_backward(codes, scale, packed, w_scale, dy, 0 if weight_dtype is None else _ELEMENT.get(weight_dtype),
+                                   want[0], want[1], want[2], stream)
 
 
 def clip_gradients(grads, max_norm: float, eps: float = 1e-6, out=None, stream=None):
     """aecct_clip_gradients: scales the tensors `grads` by min(1, max_norm / (norm + eps)), norm the 2-norm over
-    all of their elements, in place or into the tensors `out`.  Returns norm, a float32 scalar on the GPU."""
+    all of their elements, in place or into the tensors `out`.  They are contiguous float32, float16 and bfloat16
+    tensors on one GPU.  Returns norm, a float32 scalar there."""
     import torch
 
-    grads = list(grads)
-    outs = grads if out is None else list(out)
-    if len(outs) != len(grads):
-        raise ValueError(f"out must have {len(grads)} tensors")
-    n = len(grads)
-    dev = grads[0].device if n else torch.device("cuda", torch.cuda.current_device())
-    if dev.type != "cuda":
-        raise ValueError("clip_gradients takes CUDA tensors")
-    kinds = []
-    for g, o in zip(grads, outs):
-        k = _element(g.dtype)
-        if k is None or g.device != dev or not g.is_contiguous():
-            raise ValueError("gradients must be contiguous float32, float16 or bfloat16 tensors on one device")
-        if o is not g and (o.dtype != g.dtype or o.shape != g.shape or o.device != dev or not o.is_contiguous()):
-            raise ValueError("out must hold contiguous tensors like the gradients")
-        kinds.append(k)
-    L = load()
-    size = ctypes.c_int64()
-    _check(L.aecct_clip_workspace(n, ctypes.byref(size)), "aecct_clip_gradients")
-    norm = torch.empty((), dtype=torch.float32, device=dev)
-    work = torch.empty(size.value, dtype=torch.uint8, device=dev)
-    src = np.array([g.data_ptr() for g in grads], np.uintp)
-    dst = src if out is None else np.array([o.data_ptr() for o in outs], np.uintp)
-    lens = np.array([g.numel() for g in grads], np.int64)
-    types = np.array(kinds, np.int32)
-    s = _stream_of(stream, dev, (*grads, *(outs if out is not None else ()), norm, work))
-    st = L.aecct_clip_gradients(n, src.ctypes.data, lens.ctypes.data, types.ctypes.data, dst.ctypes.data, max_norm, eps,
-                                norm.data_ptr(), work.data_ptr(), size.value, s.cuda_stream)
-    _check(st, "aecct_clip_gradients")
-    return norm
+    device = 0 if grads or stream is not None else torch.cuda.current_device()
+    return (_binding or _operators()).clip_gradients(grads, max_norm, eps, out, device, stream)

@@ -1,7 +1,7 @@
-"""Build libaecct.so in-tree with nvcc for sm_103a (GB300).
+"""Build libaecct.so in-tree with nvcc for sm_103a (GB300), and its binding to torch's tensors with g++.
 
 The CUDA sources are compiled in parallel (one nvcc per translation unit) and linked into
-paper_2410_05911_gb300/_build/libaecct.so.  The decoder's translation unit is built with
+paper_2410_05911_gb300/_build/libaecct.so; aecct_torch.so beside it links against it and torch.  The decoder's translation unit is built with
 --fmad=false so that no multiply-add is contracted behind the explicit fp32 operation order.
 """
 from __future__ import annotations
@@ -14,6 +14,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OUT_DIR = os.path.join(HERE, "_build")
 LIB_PATH = os.path.join(OUT_DIR, "libaecct.so")
+BINDING_PATH = os.path.join(OUT_DIR, "aecct_torch.so")
+BINDING_SOURCE = "torch_binding.cpp"
 SOURCES = ["api.cu", "decoder_kernel.cu", "decoder_kernel_gelu.cu", "decoder_kernel_fp.cu", "decoder_kernel_fp_gelu.cu",
            "decoder_kernel_cap.cu", "decoder_kernel_cap_fp.cu", "selftest.cu", "aap.cu", "spe.cu",
            "norm.cu", "clip.cu", "linear.cu", "linear_grad.cu", "linear_wgrad.cu",
@@ -30,11 +32,34 @@ def nvcc() -> str:
 
 
 def _stale() -> bool:
-    if not os.path.exists(LIB_PATH):
+    if not os.path.exists(LIB_PATH) or not os.path.exists(BINDING_PATH):
         return True
-    t = os.path.getmtime(LIB_PATH)
-    deps = [os.path.join(CSRC, s) for s in SOURCES + HEADERS] + [os.path.abspath(__file__)]
+    t = min(os.path.getmtime(LIB_PATH), os.path.getmtime(BINDING_PATH))
+    deps = [os.path.join(CSRC, s) for s in SOURCES + HEADERS + [BINDING_SOURCE]] + [os.path.abspath(__file__)]
     return any(os.path.getmtime(p) > t for p in deps if os.path.exists(p))
+
+
+def _binding_command(obj: str):
+    """g++ on the binding's source: torch's and Python's headers."""
+    import sysconfig
+
+    import torch
+
+    inc = os.path.join(os.path.dirname(torch.__file__), "include")
+    dirs = [inc, os.path.join(inc, "torch", "csrc", "api", "include"), sysconfig.get_paths()["include"],
+            os.path.join(os.path.dirname(os.path.dirname(nvcc())) or "/usr/local/cuda", "include")]
+    return ["g++", "-O2", "-std=c++17", "-fPIC", "-c", os.path.join(CSRC, BINDING_SOURCE), "-o", obj,
+            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *[a for d in dirs for a in ("-isystem", d)]]
+
+
+def _link_binding(obj: str) -> None:
+    import torch
+
+    lib = os.path.join(os.path.dirname(torch.__file__), "lib")
+    tmp = BINDING_PATH + f".tmp{os.getpid()}"
+    subprocess.check_call(["g++", "-shared", "-o", tmp, obj, "-L" + OUT_DIR, "-l:libaecct.so", "-L" + lib, "-ltorch_python",
+                           "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + lib])
+    os.replace(tmp, BINDING_PATH)
 
 
 def build(force: bool = False, verbose_ptxas: bool = False) -> str:
@@ -51,6 +76,9 @@ def build(force: bool = False, verbose_ptxas: bool = False) -> str:
         if verbose_ptxas:
             cmd.insert(1, "-Xptxas=-v")
         procs.append((src, subprocess.Popen(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)))
+    binding = os.path.join(OUT_DIR, "torch_binding.o")
+    procs.append((BINDING_SOURCE, subprocess.Popen(_binding_command(binding), stdout=subprocess.PIPE, stderr=subprocess.STDOUT,
+                                                   text=True)))
     failed = []
     for src, pr in procs:
         out, _ = pr.communicate()
@@ -59,10 +87,11 @@ def build(force: bool = False, verbose_ptxas: bool = False) -> str:
         if pr.returncode:
             failed.append(src)
     if failed:
-        raise RuntimeError(f"nvcc failed for {failed}")
+        raise RuntimeError(f"compilation failed for {failed}")
     tmp = LIB_PATH + f".tmp{os.getpid()}"
     subprocess.check_call([nvcc(), *ARCH, "-shared", "-o", tmp, *objs])
     os.replace(tmp, LIB_PATH)
+    _link_binding(binding)
     return LIB_PATH
 
 

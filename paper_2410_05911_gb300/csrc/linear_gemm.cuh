@@ -25,6 +25,7 @@
 #pragma once
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <climits>
 #include <cstdint>
 
@@ -924,8 +925,15 @@ cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b,
                                    a.aligned() && b.aligned() ? A::kSpan * kStep : INT_MAX, p.cluster ? p.splits : 1,
                                    p.splits > 1 && !p.cluster ? partial : nullptr, err};
   auto *kernel = gemm_kernel<A, B, Out, TB, CG>;
-  cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+  static std::atomic<uint64_t> allowed{0};  // devices on which the kernel may use its shared memory
+  int dev = 0;
+  cudaError_t e = cudaGetDevice(&dev);
   if (e != cudaSuccess) return e;
+  const uint64_t bit = uint64_t(1) << (dev & 63);
+  if (dev >= 64 || !(allowed.load(std::memory_order_relaxed) & bit)) {
+    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem)) != cudaSuccess) return e;
+    if (dev < 64) allowed.fetch_or(bit, std::memory_order_relaxed);
+  }
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = CG, attr[0].val.clusterDim.y = p.cluster ? p.splits : 1, attr[0].val.clusterDim.z = 1;
