@@ -283,6 +283,9 @@ cudaError_t launch_unpack_weights(const uint8_t *packed, int n_layers, int D, co
                                   uint32_t layer_bytes, uint8_t *wstream, cudaStream_t stream);
 
 int sm_count();  // SMs of the current device (norm.cu)
+// Host memory that the operators' kernels see: 1 once a wait in one of them has given up (linear.cu).  NULL where it could not be
+// allocated.
+int *wait_status();
 
 // norm.cu: root-mean-square norm with the residual's addition and eq. Quant, and its gradients.
 // dtype: 0 = float, 1 = half, 2 = bfloat16 (the types of aecct.h)
@@ -346,7 +349,6 @@ struct AapLinearGradCall {
 };
 int64_t aap_linear_workspace(int64_t M, int64_t K, int64_t N);
 cudaError_t launch_aap_linear(const AapLinearCall &c, cudaStream_t stream);
-int *linear_status();  // host memory: 1 once a wait in a kernel of these has given up; NULL without memory
 int64_t weight_grad_workspace(int64_t M, int64_t K, int64_t N, int wdtype);
 cudaError_t launch_weight_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t stream);
 int64_t aap_linear_grad_workspace(int64_t M, int64_t K, int64_t N, int dtype, int wdtype);

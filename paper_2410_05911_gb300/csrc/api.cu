@@ -38,12 +38,12 @@ bool is_workspace(const void *p, int64_t bytes, int64_t need) {
   return need == 0 || (p && (reinterpret_cast<uintptr_t>(p) & 15u) == 0 && bytes >= need);
 }
 // a wait that gave up in a kernel of an earlier call, reported once
-int linear_gave_up() {
-  int *word = linear_status();
+int wait_gave_up() {
+  int *word = wait_status();
   if (!word) return AECCT_ERR_OUT_OF_MEMORY;
   if (*static_cast<volatile int *>(word) == 0) return AECCT_OK;
   *static_cast<volatile int *>(word) = 0;
-  g_last_error = "aap_linear: a device-side wait of an earlier call exceeded its limit";
+  g_last_error = "a device-side wait of an earlier call of an operator exceeded its limit";
   return AECCT_ERR_TIMEOUT;
 }
 // the sizes of an AAP linear layer: M tokens, K inputs, N outputs
@@ -1286,6 +1286,8 @@ int aecct_rms_quant(const void *x, int64_t ldx, const void *residual, int64_t ld
     return AECCT_ERR_INVALID_ARG;
   if (residual && (!is_array(residual, dtype) || !is_array(sum, dtype) || ldr < d)) return AECCT_ERR_INVALID_ARG;
   if (values && !is_array(values, dtype)) return AECCT_ERR_INVALID_ARG;
+  const int earlier = wait_gave_up();
+  if (earlier != AECCT_OK) return earlier;
   const RmsQuantCall c = {rows, d, dtype, x, residual, ldx, residual ? ldr : 0, gain, eps, residual ? sum : nullptr,
                           codes, scale, values};
   const cudaError_t e = launch_rms_quant(c, static_cast<cudaStream_t>(cuda_stream));
@@ -1312,6 +1314,8 @@ int aecct_rms_quant_backward(const void *dy, int64_t lddy, const void *h, int64_
         workspace_bytes < rms_quant_grad_partials(rows, d) * static_cast<int64_t>(sizeof(float)))
       return AECCT_ERR_INVALID_ARG;
   }
+  const int earlier = wait_gave_up();
+  if (earlier != AECCT_OK) return earlier;
   const RmsQuantGradCall c = {rows, d, dtype, dy, h, dsum, lddy, ldh, dsum ? ldd : 0, gain, eps, dx, dgain,
                               static_cast<float *>(workspace)};
   const cudaError_t e = launch_rms_quant_grad(c, static_cast<cudaStream_t>(cuda_stream));
@@ -1336,7 +1340,7 @@ int aecct_aap_linear(const int8_t *codes, int64_t ldc, const float *scale, const
     return AECCT_ERR_INVALID_ARG;
   if (bias && !is_array(bias, AECCT_F32)) return AECCT_ERR_INVALID_ARG;
   if (!is_workspace(workspace, workspace_bytes, aap_linear_workspace(M, K, N))) return AECCT_ERR_INVALID_ARG;
-  const int earlier = linear_gave_up();
+  const int earlier = wait_gave_up();
   if (earlier != AECCT_OK) return earlier;
   const AapLinearCall c = {M, K, N, dtype, codes, ldc, scale, packed, w_scale, bias, y, workspace};
   const cudaError_t e = launch_aap_linear(c, static_cast<cudaStream_t>(cuda_stream));
@@ -1374,7 +1378,7 @@ int aecct_aap_linear_backward(const void *dy, int64_t lddy, const int8_t *codes,
     if (e == cudaSuccess && db) e = cudaMemsetAsync(db, 0, static_cast<size_t>(N) * sizeof(float), stream);
     return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "aap_linear_backward memset");
   }
-  const int earlier = linear_gave_up();
+  const int earlier = wait_gave_up();
   if (earlier != AECCT_OK) return earlier;
   const AapLinearGradCall c = {M, K, N, dtype, wdtype, dy, lddy, codes, ldc, scale, packed, w_scale, dx, dw, db, workspace};
   const cudaError_t e = launch_aap_linear_grad(c, stream);

@@ -44,13 +44,13 @@ cudaError_t input_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t s
     }
     if ((e = tensor_map(&b.map, rows, Staged<T>::kBf, c.N, c.M, ld, kPieces<T>, Staged<T>::X)) != cudaSuccess) return e;
     float *partial = reinterpret_cast<float *>(work + 2 * kPieces<T> * c.M * padded(c.N));
-    return launch_gemm<Weights<T>, Staged<T>, OutX, 256, 2>(c.K, c.M, c.N, a, b, out, partial, sms, linear_status(), st);
+    return launch_gemm<Weights<T>, Staged<T>, OutX, 256, 2>(c.K, c.M, c.N, a, b, out, partial, sms, wait_status(), st);
   }
   return with_single_tile(c.M, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
     using B = GradK<T, TB>;
     const B b = {static_cast<const T *>(c.dy), c.M, c.lddy, grads_vec<T>(c.dy, c.lddy, c.N)};
-    return launch_gemm<Weights<T>, B, OutX, TB, 1>(c.K, c.M, c.N, a, b, out, reinterpret_cast<float *>(work), sms, linear_status(), st);
+    return launch_gemm<Weights<T>, B, OutX, TB, 1>(c.K, c.M, c.N, a, b, out, reinterpret_cast<float *>(work), sms, wait_status(), st);
   });
 }
 

@@ -34,7 +34,7 @@ cudaError_t staged_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t 
   const CodesT a = {c.codes, c.K, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
   const OutW out = {c.dw, c.wdtype, c.K};
   float *partial = reinterpret_cast<float *>(work + 2 * P * c.M * padded(c.N));
-  return launch_gemm<CodesT, Staged<P>, OutW, 256, 2>(c.K, c.N, c.M, a, b, out, partial, sm_count(), linear_status(), st);
+  return launch_gemm<CodesT, Staged<P>, OutW, 256, 2>(c.K, c.N, c.M, a, b, out, partial, sm_count(), wait_status(), st);
 }
 
 template <typename T, int P>
@@ -45,7 +45,7 @@ cudaError_t weight_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t 
     constexpr int TB = decltype(tb)::value;
     using B = GradT<T, TB, P>;
     const B b = {static_cast<const T *>(c.dy), c.N, c.lddy, c.scale, grads_vec<T>(c.dy, c.lddy, c.N)};
-    return launch_gemm<CodesT, B, OutW, TB, 1>(c.K, c.N, c.M, a, b, out, reinterpret_cast<float *>(work), sm_count(), linear_status(), st);
+    return launch_gemm<CodesT, B, OutW, TB, 1>(c.K, c.N, c.M, a, b, out, reinterpret_cast<float *>(work), sm_count(), wait_status(), st);
   });
 }
 

@@ -19,6 +19,7 @@
 
 #include "aecct_internal.h"
 #include "rowtypes.cuh"
+#include "sm103_ptx.cuh"
 
 namespace aecct {
 
@@ -26,9 +27,10 @@ namespace {
 
 constexpr float kAlphaMin = 0x1p-100f;  // 127 / alpha stays finite, and a row of zeros gets codes of zero
 constexpr int kSmallThreads = 256;      // CTA of rows that fit a warp
-constexpr int kPerThread = 16;          // elements of a row that a thread holds (kNormMaxWidth: twice that)
-constexpr int kPerThreadWide = 32;
-static_assert(kNormMaxWidth == 1024 * kPerThreadWide, "the widest row is a CTA of 1024 threads");
+// Elements of a row that a thread holds: few, so that many threads' loads are in flight; as many as it takes for a
+// CTA of 1024 threads to hold the row (kNormMaxWidth: 32).
+constexpr int kFew = 8, kSome = 16, kMany = 32;
+static_assert(kNormMaxWidth == 1024 * kMany, "the widest row is a CTA of 1024 threads");
 
 // The threads of a row: G consecutive lanes of a warp (d <= 32 E; BLOCK = 0), or a CTA of whole warps, at
 // most BLOCK threads.  Thread t of
@@ -152,6 +154,34 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : kSmallThreads) rms_quant_kerne
   }
 }
 
+// E elements of a row as they lie in memory: V at a time (16 bytes, or one)
+template <typename T, int V, int E>
+struct RawRow {
+  uint4 w[V == 1 ? 1 : E / V];
+  T e[V == 1 ? E : 1];
+  // elements (j G + t) V ... of the row at p, of d; what lies past its end, or in no row, is not read
+  __device__ __forceinline__ void load(const T *p, bool live, int t, int G, int d) {
+#pragma unroll
+    for (int j = 0; j < E / V; ++j) {
+      const int i = (j * G + t) * V;
+      if (live && i < d) {
+        if constexpr (V == 1) e[j] = p[i];
+        else w[j] = *reinterpret_cast<const uint4 *>(p + i);
+      } else {
+        if constexpr (V == 1) e[j] = from_f32<T>(0.0f);
+        else w[j] = make_uint4(0, 0, 0, 0);
+      }
+    }
+  }
+  __device__ __forceinline__ void get(int j, float (&v)[V]) const {
+    if constexpr (V == 1) v[0] = to_f32(e[j]);
+    else if constexpr (sizeof(T) == 4)
+      v[0] = __uint_as_float(w[j].x), v[1] = __uint_as_float(w[j].y), v[2] = __uint_as_float(w[j].z), v[3] = __uint_as_float(w[j].w);
+    else
+      unpack2<T>(w[j].x, v[0], v[1]), unpack2<T>(w[j].y, v[2], v[3]), unpack2<T>(w[j].z, v[4], v[5]), unpack2<T>(w[j].w, v[6], v[7]);
+  }
+};
+
 template <typename T>
 struct GradArgs {
   RowShape s;
@@ -163,6 +193,9 @@ struct GradArgs {
   float *partial;  // [CTAs][d]: each CTA's sum of dy h r over its rows
 };
 
+// A CTA takes every gridDim-th row (or group of rows) and holds the next one's elements, in flight, while it works
+// on one: the sums over a row and their barrier would otherwise stand between its loads and the next row's.
+// Bound by memory: rows of 4,096 in bfloat16 with `dsum` (8 bytes an element).
 template <typename T, int V, int E, int BLOCK>
 __global__ void __launch_bounds__(BLOCK ? BLOCK : kSmallThreads) rms_quant_grad_kernel(const __grid_constant__ GradArgs<T> a) {
   __shared__ float2 buf[2][32];
@@ -171,6 +204,7 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : kSmallThreads) rms_quant_grad_
   const int d = a.s.d, G = a.s.G;
   const int t = BLOCK ? threadIdx.x : threadIdx.x & (G - 1);
   const int per = BLOCK ? 1 : kSmallThreads / G;
+  const int64_t step = static_cast<int64_t>(gridDim.x) * per;
   float dg[E], g[E];
 #pragma unroll
   for (int j = 0; j < C; ++j) {
@@ -178,26 +212,32 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : kSmallThreads) rms_quant_grad_
 #pragma unroll
     for (int e = 0; e < V; ++e) dg[j * V + e] = 0.0f, g[j * V + e] = i < d ? __ldg(a.gain + i + e) : 0.0f;
   }
+  const float by = __fdiv_rn(1.0f, static_cast<float>(d));
   int parity = 0;
-  for (int64_t first = static_cast<int64_t>(blockIdx.x) * per; first < a.s.rows; first += static_cast<int64_t>(gridDim.x) * per) {
-    const int64_t row = first + (BLOCK ? 0 : threadIdx.x / G);
-    const bool live = row < a.s.rows;
-    float h[E], dy[E];
-    float ss = 0.0f, th = 0.0f;
+  int64_t row = static_cast<int64_t>(blockIdx.x) * per + (BLOCK ? 0 : threadIdx.x / G);
+  RawRow<T, V, E> h, dy, ds;
+  const auto load = [&](int64_t r) {
+    const bool live = r < a.s.rows;
+    h.load(a.h + r * a.ldh, live, t, G, d);
+    dy.load(a.dy + r * a.lddy, live, t, G, d);
+    if (a.dsum) ds.load(a.dsum + r * a.ldd, live, t, G, d);
+  };
+  load(row);
+  for (int64_t first = static_cast<int64_t>(blockIdx.x) * per; first < a.s.rows; first += step, row += step) {
+    float hv[E], tv[E], ss = 0.0f, th = 0.0f;  // tv: dy gain
 #pragma unroll
     for (int j = 0; j < C; ++j) {
-      const int i = (j * G + t) * V;
-      if (live && i < d) {
-        load_v<T, V>(a.h + row * a.ldh + i, h + j * V);
-        load_v<T, V>(a.dy + row * a.lddy + i, dy + j * V);
-      } else {
+      float x[V], y[V];
+      h.get(j, x), dy.get(j, y);
 #pragma unroll
-        for (int e = 0; e < V; ++e) h[j * V + e] = 0.0f, dy[j * V + e] = 0.0f;
+      for (int e = 0; e < V; ++e) {
+        const int k = j * V + e;
+        hv[k] = x[e], tv[k] = y[e] * g[k];
+        ss = fmaf(x[e], x[e], ss), th = fmaf(tv[k], x[e], th);
       }
     }
-#pragma unroll
-    for (int e = 0; e < E; ++e) ss = fmaf(h[e], h[e], ss), th = fmaf(dy[e] * g[e], h[e], th);
-    // (both sums: the maximum's place is not used)
+    const RawRow<T, V, E> own = dy, sum = ds;
+    load(row + step);
     for (int o = (BLOCK ? 32 : G) >> 1; o > 0; o >>= 1) {
       ss += __shfl_xor_sync(0xffffffffu, ss, o);
       th += __shfl_xor_sync(0xffffffffu, th, o);
@@ -215,20 +255,21 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : kSmallThreads) rms_quant_grad_
       parity ^= 1;
     }
     const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(ss, static_cast<float>(d)) + a.eps));
-    const float c = r * r * r * __fdiv_rn(th, static_cast<float>(d));
-    if (live) {
+    const float c = r * r * r * (th * by);
+    if (row < a.s.rows) {
 #pragma unroll
       for (int j = 0; j < C; ++j) {
         const int i = (j * G + t) * V;
         if (i < d) {
-          float o[V];
-          if (a.dsum) load_v<T, V>(a.dsum + row * a.ldd + i, o);
+          float o[V], y[V];
+          own.get(j, y);
+          if (a.dsum) sum.get(j, o);
 #pragma unroll
           for (int e = 0; e < V; ++e) {
             const int k = j * V + e;
-            const float v = fmaf(-h[k], c, r * (dy[k] * g[k]));
+            const float v = fmaf(-hv[k], c, r * tv[k]);
             o[e] = a.dsum ? v + o[e] : v;
-            dg[k] = fmaf(dy[k], h[k] * r, dg[k]);
+            dg[k] = fmaf(y[e], hv[k] * r, dg[k]);
           }
           store_v<T, V>(a.dx + row * d + i, o);
         }
@@ -259,19 +300,301 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : kSmallThreads) rms_quant_grad_
   }
 }
 
-// dgain[i] = sum over the CTAs' partial sums, in a fixed order: 32 columns a CTA, 8 rows of them at a time
-__global__ void __launch_bounds__(256) rms_quant_dgain_kernel(const float *partial, int parts, int d, float *dgain) {
-  __shared__ float s[8][32];
-  const int i = blockIdx.x * 32 + (threadIdx.x & 31), k0 = threadIdx.x >> 5;
+// ----------------------------------------------------------------------------- rows through shared memory
+// Rows of more than a warp's lanes hold come to shared memory by bulk copies, kRing rows ahead of the one that is
+// worked on: what is in flight then does not hang on registers or threads, and a row that does not start on 16
+// bytes is copied from the 16 bytes that it starts in, to the same place of a 16-byte line.  Copies stay within the
+// tensor: at its very first and last row, elements outside of whole 16-byte lines are copied by threads.
+constexpr int kRing = 4;  // rows in flight, fewer (two at least) where that many do not fit
+constexpr int kNormWaitTries = 1 << 24;  // a wait that has looked so often (seconds) has lost its copy
+
+template <typename T>
+struct RowSource {
+  const T *p;  // NULL: none
+  int64_t ld;
+};
+
+// the bytes of a row of d elements at p that a bulk copy takes: [first, last)
+template <typename T>
+__device__ __forceinline__ void copy_range(const T *p, int d, bool first_row, bool last_row, uintptr_t &first, uintptr_t &last) {
+  const uintptr_t a = reinterpret_cast<uintptr_t>(p), b = a + d * sizeof(T);
+  first = first_row ? (a + 15) & ~uintptr_t(15) : a & ~uintptr_t(15);
+  last = last_row ? b & ~uintptr_t(15) : (b + 15) & ~uintptr_t(15);
+  if (last < first) last = first;
+}
+// bytes of shared memory of a row
+template <typename T>
+__host__ __device__ constexpr int row_bytes(int d) { return (d * static_cast<int>(sizeof(T)) + 31) / 16 * 16; }
+
+// one thread: the copies of a row's N sources into `stage`
+template <typename T, int N>
+__device__ __forceinline__ void copy_rows(const RowSource<T> (&src)[N], int64_t row, int64_t rows, int d, uint32_t stage, uint32_t bar) {
+  uintptr_t first[N], last[N];
+  uint32_t bytes = 0;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    if (src[k].p) {
+      copy_range(src[k].p + row * src[k].ld, d, row == 0, row == rows - 1, first[k], last[k]);
+      bytes += static_cast<uint32_t>(last[k] - first[k]);
+    }
+  mbar_arrive_expect_tx(bar, bytes);
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    if (src[k].p && last[k] > first[k]) {
+      const uintptr_t line = reinterpret_cast<uintptr_t>(src[k].p + row * src[k].ld) & ~uintptr_t(15);
+      bulk_g2s(stage + k * row_bytes<T>(d) + static_cast<uint32_t>(first[k] - line), reinterpret_cast<const void *>(first[k]),
+               static_cast<uint32_t>(last[k] - first[k]), bar);
+    }
+}
+// where source k's row lies in its stage
+template <typename T>
+__device__ __forceinline__ T *row_in(uint8_t *stage, const RowSource<T> &src, int k, int64_t row, int d) {
+  return reinterpret_cast<T *>(stage + k * row_bytes<T>(d) + (reinterpret_cast<uintptr_t>(src.p + row * src.ld) & 15));
+}
+// all threads: the elements of the first and last row that no copy takes
+template <typename T, int N>
+__device__ __forceinline__ void patch_rows(const RowSource<T> (&src)[N], int64_t row, int64_t rows, int d, uint8_t *stage) {
+  if (row != 0 && row != rows - 1) return;
+#pragma unroll
+  for (int k = 0; k < N; ++k)
+    if (src[k].p) {
+      const T *p = src[k].p + row * src[k].ld;
+      T *s = row_in(stage, src[k], k, row, d);
+      uintptr_t first, last;
+      copy_range(p, d, row == 0, row == rows - 1, first, last);
+      const int from = static_cast<int>((static_cast<intptr_t>(first) - reinterpret_cast<intptr_t>(p)) / static_cast<int>(sizeof(T)));
+      const int to = static_cast<int>((static_cast<intptr_t>(last) - reinterpret_cast<intptr_t>(p)) / static_cast<int>(sizeof(T)));
+      // (no copy at all where the row lies within a line: from >= to)
+      for (int i = threadIdx.x; i < d; i += blockDim.x)
+        if (i < from || i >= to) s[i] = p[i];
+    }
+  __syncthreads();
+}
+// a wait for a copy, with an end: its rows are then wrong, and err says so
+__device__ __forceinline__ void wait_copy(uint32_t bar, uint32_t parity, int *err) {
+  for (int tries = 0; !mbar_try_wait(bar, parity); ++tries)
+    if (tries > kNormWaitTries) {
+      *err = 1;
+      return;
+    }
+}
+
+template <typename T>
+struct RingGradArgs {
+  RowSource<T> src[3];  // h, dy, dsum
+  int64_t rows;
+  int d;
+  int ring;  // rows of the ring
+  const float *gain;
+  float eps;
+  T *dx;
+  float *partial;
+  int *err;  // set to 1 by a wait that gave up
+};
+
+// One row a CTA at a time; thread t holds the sums of dgain of elements (j blockDim + t) V ... (V = 1 where a row or its
+// outputs do not start on 16 bytes).
+template <typename T, int V, int E>
+__global__ void __launch_bounds__(512) ring_grad_kernel(const __grid_constant__ RingGradArgs<T> a) {
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ uint64_t bars[kRing];
+  __shared__ float2 buf[2][16];
+  constexpr int C = E / V;
+  const int d = a.d, t = threadIdx.x, G = blockDim.x;
+  const int stage_bytes = (a.src[2].p ? 3 : 2) * row_bytes<T>(d);
+  const uint32_t bar = smem_u32(bars), base = smem_u32(ring);
+  if (t == 0) {
+    for (int s = 0; s < a.ring; ++s) mbar_init(bar + 8 * s, 1);
+    fence_mbar_init_cluster();
+    for (int s = 0; s < a.ring; ++s) {
+      const int64_t row = blockIdx.x + static_cast<int64_t>(s) * gridDim.x;
+      if (row < a.rows) copy_rows(a.src, row, a.rows, d, base + s * stage_bytes, bar + 8 * s);
+    }
+  }
+  float dg[E], g[E];
+#pragma unroll
+  for (int j = 0; j < C; ++j)
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const int i = (j * G + t) * V;
+      dg[j * V + e] = 0.0f, g[j * V + e] = i < d ? __ldg(a.gain + i + e) : 0.0f;
+    }
+  __syncthreads();
+  int s = 0, parity = 0;
+  int64_t n = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, ++n) {
+    uint8_t *stage = ring + s * stage_bytes;
+    wait_copy(bar + 8 * s, parity, a.err);
+    patch_rows(a.src, row, a.rows, d, stage);
+    const T *h = row_in(stage, a.src[0], 0, row, d), *dy = row_in(stage, a.src[1], 1, row, d);
+    float ss = 0.0f, th = 0.0f;
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      const int i = (j * G + t) * V;
+      if (i < d) {
+        float x[V], y[V];
+        load_v<T, V>(h + i, x), load_v<T, V>(dy + i, y);
+#pragma unroll
+        for (int e = 0; e < V; ++e) ss = fmaf(x[e], x[e], ss), th = fmaf(y[e] * g[j * V + e], x[e], th);
+      }
+    }
+    for (int o = 16; o > 0; o >>= 1) {
+      ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      th += __shfl_xor_sync(0xffffffffu, th, o);
+    }
+    float2 *b = buf[n & 1];
+    if ((t & 31) == 0) b[t >> 5] = make_float2(ss, th);
+    __syncthreads();
+    // (every thread is done with the row before: its place takes the next row but ring - 1)
+    if (t == 0 && n > 0) {
+      const int64_t next = row + static_cast<int64_t>(a.ring - 1) * gridDim.x;
+      const int place = s == 0 ? a.ring - 1 : s - 1;
+      if (next < a.rows) copy_rows(a.src, next, a.rows, d, base + place * stage_bytes, bar + 8 * place);
+    }
+    float2 v = (t & 31) < (G >> 5) ? b[t & 31] : make_float2(0.0f, 0.0f);
+    for (int o = 8; o > 0; o >>= 1) {
+      v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+      v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
+    }
+    v.x = __shfl_sync(0xffffffffu, v.x, 0), v.y = __shfl_sync(0xffffffffu, v.y, 0);  // (16 warps at most)
+    const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(v.x, static_cast<float>(d)) + a.eps));
+    const float c = r * r * r * __fdiv_rn(v.y, static_cast<float>(d));
+    const T *ds = a.src[2].p ? row_in(stage, a.src[2], 2, row, d) : nullptr;
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      const int i = (j * G + t) * V;
+      if (i < d) {
+        float x[V], y[V], o[V];
+        load_v<T, V>(h + i, x), load_v<T, V>(dy + i, y);
+        if (ds) load_v<T, V>(ds + i, o);
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          const float w = fmaf(-x[e], c, r * (y[e] * g[j * V + e]));
+          o[e] = ds ? w + o[e] : w;
+          dg[j * V + e] = fmaf(y[e], x[e] * r, dg[j * V + e]);
+        }
+        store_v<T, V>(a.dx + row * d + i, o);
+      }
+    }
+    if (++s == a.ring) s = 0, parity ^= 1;
+  }
+#pragma unroll
+  for (int j = 0; j < C; ++j) {
+    const int i = (j * G + t) * V;
+    if (i < d)
+#pragma unroll
+      for (int e = 0; e < V; ++e) a.partial[static_cast<int64_t>(blockIdx.x) * d + i + e] = dg[j * V + e];
+  }
+}
+
+template <typename T>
+struct RingQuantArgs {
+  RowSource<T> src[2];  // x, residual
+  int64_t rows;
+  int d, ring;
+  const float *gain;
+  float eps;
+  T *sum;
+  int8_t *codes;
+  float *scale;
+  T *values;
+  int *err;
+};
+
+// The forward pass of rows that do not start on 16 bytes, or that its outputs' do not: an element at a time from shared
+// memory, where aligned rows are read from global memory in 16-byte pieces (rms_quant_kernel).
+template <typename T, int E>
+__global__ void __launch_bounds__(512) ring_quant_kernel(const __grid_constant__ RingQuantArgs<T> a) {
+  extern __shared__ __align__(16) uint8_t ring[];
+  __shared__ uint64_t bars[kRing];
+  __shared__ float2 buf[2][16];
+  const int d = a.d, t = threadIdx.x, G = blockDim.x;
+  const int stage_bytes = (a.src[1].p ? 2 : 1) * row_bytes<T>(d);
+  const uint32_t bar = smem_u32(bars), base = smem_u32(ring);
+  if (t == 0) {
+    for (int s = 0; s < a.ring; ++s) mbar_init(bar + 8 * s, 1);
+    fence_mbar_init_cluster();
+    for (int s = 0; s < a.ring; ++s) {
+      const int64_t row = blockIdx.x + static_cast<int64_t>(s) * gridDim.x;
+      if (row < a.rows) copy_rows(a.src, row, a.rows, d, base + s * stage_bytes, bar + 8 * s);
+    }
+  }
+  float g[E];
+#pragma unroll
+  for (int j = 0; j < E; ++j) g[j] = j * G + t < d ? __ldg(a.gain + j * G + t) : 0.0f;
+  __syncthreads();
+  int s = 0, parity = 0;
+  int64_t n = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, ++n) {
+    uint8_t *stage = ring + s * stage_bytes;
+    wait_copy(bar + 8 * s, parity, a.err);
+    patch_rows(a.src, row, a.rows, d, stage);
+    const T *x = row_in(stage, a.src[0], 0, row, d);
+    const T *res = a.src[1].p ? row_in(stage, a.src[1], 1, row, d) : nullptr;
+    float z[E], ss = 0.0f, top = 0.0f;
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      const int i = j * G + t;
+      z[j] = 0.0f;
+      if (i < d) {
+        float h = to_f32(x[i]);
+        if (res) {
+          const T sum = from_f32<T>(h + to_f32(res[i]));
+          a.sum[row * d + i] = sum;
+          h = to_f32(sum);
+        }
+        ss = fmaf(h, h, ss);
+        z[j] = h * g[j];
+        top = fmaxf(top, fabsf(z[j]));
+      }
+    }
+    for (int o = 16; o > 0; o >>= 1) {
+      ss += __shfl_xor_sync(0xffffffffu, ss, o);
+      top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    }
+    float2 *b = buf[n & 1];
+    if ((t & 31) == 0) b[t >> 5] = make_float2(ss, top);
+    __syncthreads();
+    if (t == 0) {  // (every thread has read the row: its place takes another)
+      const int64_t next = row + static_cast<int64_t>(a.ring) * gridDim.x;
+      if (next < a.rows) copy_rows(a.src, next, a.rows, d, base + s * stage_bytes, bar + 8 * s);
+    }
+    float2 v = (t & 31) < (G >> 5) ? b[t & 31] : make_float2(0.0f, 0.0f);
+    for (int o = 8; o > 0; o >>= 1) {
+      v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
+      v.y = fmaxf(v.y, __shfl_xor_sync(0xffffffffu, v.y, o));
+    }
+    v.x = __shfl_sync(0xffffffffu, v.x, 0), v.y = __shfl_sync(0xffffffffu, v.y, 0);  // (16 warps at most)
+    const float alpha = fmaxf(v.y, kAlphaMin), inv = __fdiv_rn(127.0f, alpha);
+    const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(v.x, static_cast<float>(d)) + a.eps));
+    const float sc = __fdiv_rn(alpha * r, 127.0f);
+    if (t == 0) a.scale[row] = sc;
+#pragma unroll
+    for (int j = 0; j < E; ++j) {
+      const int i = j * G + t;
+      if (i < d) {
+        const int q = __float2int_rn(z[j] * inv);  // (a NaN gives 0)
+        a.codes[row * d + i] = static_cast<int8_t>(q);
+        if (a.values) a.values[row * d + i] = from_f32<T>(static_cast<float>(q) * sc);
+      }
+    }
+    if (++s == a.ring) s = 0, parity ^= 1;
+  }
+}
+
+// dgain[i] = sum over the CTAs' partial sums, in a fixed order: 32 columns a CTA, 32 rows of them at a time
+__global__ void __launch_bounds__(1024) rms_quant_dgain_kernel(const float *partial, int parts, int d, float *dgain) {
+  __shared__ float s[32][33];
+  const int c = threadIdx.x & 31, k0 = threadIdx.x >> 5, i = blockIdx.x * 32 + c;
   float v = 0.0f;
   if (i < d)
-    for (int k = k0; k < parts; k += 8) v += partial[static_cast<int64_t>(k) * d + i];
-  s[k0][threadIdx.x & 31] = v;
+#pragma unroll 4
+    for (int k = k0; k < parts; k += 32) v += partial[static_cast<int64_t>(k) * d + i];
+  s[k0][c] = v;
   __syncthreads();
-  if (k0 == 0 && i < d) {
-    for (int k = 1; k < 8; ++k) v += s[k][threadIdx.x];
-    dgain[i] = v;
-  }
+  v = s[c][k0];  // column k0 of the CTA, a row a lane
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (c == 0 && blockIdx.x * 32 + k0 < d) dgain[blockIdx.x * 32 + k0] = v;
 }
 
 bool on16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
@@ -283,6 +606,37 @@ int row_threads(int d, int E) {
   return G * E >= d ? G : 32 * ((d + 32 * E - 1) / (32 * E));
 }
 
+// How rows go through shared memory: threads of a CTA, elements that each holds, rows of the ring, CTAs.  ring = 0:
+// not at all, as two rows do not fit.
+struct RingPlan {
+  int threads, E, ring, blocks, smem;
+};
+constexpr int kRingSmem = 200 * 1024;  // of an SM
+RingPlan ring_plan(int64_t rows, int d, int element_bytes, int sources) {
+  RingPlan p = {};
+  p.threads = (d + kFew * 32 - 1) / (kFew * 32) * 32;
+  p.threads = p.threads < 64 ? 64 : p.threads > 512 ? 512 : p.threads;
+  for (p.E = kFew; p.E * p.threads < d; p.E *= 2) {}
+  const int stage = sources * ((d * element_bytes + 31) / 16 * 16);
+  int ctas = 1024 / p.threads;
+  while (ctas > 1 && ctas * 2 * stage > kRingSmem) --ctas;
+  p.ring = kRingSmem / ctas / stage;
+  if (p.ring > kRing) p.ring = kRing;
+  if (p.ring < 2 || p.E > kMany) p.ring = 0;
+  p.smem = p.ring * stage;
+  const int64_t most = static_cast<int64_t>(sm_count()) * ctas;
+  p.blocks = static_cast<int>(rows < most ? rows : most);
+  return p;
+}
+
+template <class K, class A>
+cudaError_t launch_ring(K *kernel, const A &a, const RingPlan &p, cudaStream_t st) {
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kRingSmem);
+  if (e != cudaSuccess) return e;
+  kernel<<<p.blocks, p.threads, p.smem, st>>>(a);
+  return cudaGetLastError();
+}
+
 template <typename T, int V, int E>
 cudaError_t launch_quant(QuantArgs<T> a, cudaStream_t st) {
   a.s.G = row_threads(a.s.d, E);
@@ -290,7 +644,9 @@ cudaError_t launch_quant(QuantArgs<T> a, cudaStream_t st) {
   const int64_t per = block ? 1 : kSmallThreads / a.s.G;
   const int64_t grid = (a.s.rows + per - 1) / per;
   const unsigned blocks = static_cast<unsigned>(grid < (int64_t(1) << 30) ? grid : (int64_t(1) << 30));
-  if constexpr (E == kPerThread) {
+  if constexpr (E == kFew) {
+    rms_quant_kernel<T, V, E, 0><<<blocks, kSmallThreads, 0, st>>>(a);
+  } else if constexpr (E == kSome) {
     if (!block) rms_quant_kernel<T, V, E, 0><<<blocks, kSmallThreads, 0, st>>>(a);
     else if (a.s.G <= 512) rms_quant_kernel<T, V, E, 512><<<blocks, a.s.G, 0, st>>>(a);
     else rms_quant_kernel<T, V, E, 1024><<<blocks, a.s.G, 0, st>>>(a);
@@ -307,49 +663,54 @@ cudaError_t quant_of(const RmsQuantCall &c, cudaStream_t st) {
   constexpr int V = kVec<T>;
   const bool vec = on16(c.x) && on16(c.res) && on16(c.sum) && on16(c.codes) && on16(c.values) && on16(c.gain) && c.d % V == 0 &&
                    c.ldx % V == 0 && c.ldr % V == 0;
-  if (c.d <= 1024 * kPerThread) return vec ? launch_quant<T, V, kPerThread>(a, st) : launch_quant<T, 1, kPerThread>(a, st);
-  return vec ? launch_quant<T, V, kPerThreadWide>(a, st) : launch_quant<T, 1, kPerThreadWide>(a, st);
+  if (vec) return c.d <= 1024 * kSome ? launch_quant<T, V, kSome>(a, st) : launch_quant<T, V, kMany>(a, st);
+  if (c.d <= 32 * kFew) return launch_quant<T, 1, kFew>(a, st);
+  const RingPlan p = ring_plan(c.rows, c.d, sizeof(T), c.res ? 2 : 1);
+  if (!p.ring) return launch_quant<T, 1, kMany>(a, st);
+  const RingQuantArgs<T> r = {{{a.x, a.ldx}, {a.res, a.ldr}}, c.rows, c.d, p.ring, c.gain, c.eps, a.sum, c.codes, c.scale, a.values, wait_status()};
+  return p.E == kFew    ? launch_ring(ring_quant_kernel<T, kFew>, r, p, st)
+         : p.E == kSome ? launch_ring(ring_quant_kernel<T, kSome>, r, p, st)
+                        : launch_ring(ring_quant_kernel<T, kMany>, r, p, st);
 }
 
-// CTAs of the backward kernel: what the GPU holds at once, no more than there are rows for
-int grad_blocks(int64_t rows, int d, int E) {
-  const int G = row_threads(d, E);
-  const int threads = G > 32 ? G : kSmallThreads;
+// CTAs of the backward kernel that holds rows in registers: 1,024 threads an SM, no more than there are rows for
+int grad_blocks(int64_t rows, int d) {
+  const int G = row_threads(d, d <= 32 * kFew ? kFew : kMany), threads = G > 32 ? G : kSmallThreads;
   const int64_t per = G > 32 ? 1 : kSmallThreads / G;
   const int64_t most = static_cast<int64_t>(sm_count()) * (threads > 512 ? 1 : 1024 / threads);
   const int64_t need = (rows + per - 1) / per;
   return static_cast<int>(need < most ? need : most);
 }
 
-template <typename T, int V, int E>
-cudaError_t launch_grad(GradArgs<T> a, float *dgain, cudaStream_t st) {
-  a.s.G = row_threads(a.s.d, E);
-  const int blocks = grad_blocks(a.s.rows, a.s.d, E);
-  if (blocks > 0) {
-    if constexpr (E == kPerThread) {
-      if (a.s.G <= 32) rms_quant_grad_kernel<T, V, E, 0><<<blocks, kSmallThreads, 0, st>>>(a);
-      else if (a.s.G <= 512) rms_quant_grad_kernel<T, V, E, 512><<<blocks, a.s.G, 0, st>>>(a);
-      else rms_quant_grad_kernel<T, V, E, 1024><<<blocks, a.s.G, 0, st>>>(a);
-    } else {
-      rms_quant_grad_kernel<T, V, E, 1024><<<blocks, a.s.G, 0, st>>>(a);
-    }
-    const cudaError_t e = cudaGetLastError();
-    if (e != cudaSuccess) return e;
+template <typename T, int V>
+cudaError_t launch_grad(const RmsQuantGradCall &c, cudaStream_t st) {
+  const T *h = static_cast<const T *>(c.h), *dy = static_cast<const T *>(c.dy), *ds = static_cast<const T *>(c.dsum);
+  T *dx = static_cast<T *>(c.dx);
+  const RingPlan p = c.d <= 32 * kFew ? RingPlan{} : ring_plan(c.rows, c.d, sizeof(T), ds ? 3 : 2);
+  int blocks = p.ring ? p.blocks : grad_blocks(c.rows, c.d);
+  cudaError_t e = cudaSuccess;
+  if (blocks > 0 && p.ring) {
+    const RingGradArgs<T> r = {{{h, c.ldh}, {dy, c.lddy}, {ds, c.ldd}}, c.rows, c.d, p.ring, c.gain, c.eps, dx, c.partial, wait_status()};
+    e = p.E == kFew    ? launch_ring(ring_grad_kernel<T, V, kFew>, r, p, st)
+        : p.E == kSome ? launch_ring(ring_grad_kernel<T, V, kSome>, r, p, st)
+                       : launch_ring(ring_grad_kernel<T, V, kMany>, r, p, st);
+  } else if (blocks > 0) {
+    GradArgs<T> a = {{c.rows, c.d, row_threads(c.d, c.d <= 32 * kFew ? kFew : kMany)}, dy, h, ds, c.lddy, c.ldh, c.ldd, c.gain, c.eps, dx, c.partial};
+    if (c.d <= 32 * kFew) rms_quant_grad_kernel<T, V, kFew, 0><<<blocks, kSmallThreads, 0, st>>>(a);
+    else rms_quant_grad_kernel<T, V, kMany, 1024><<<blocks, a.s.G, 0, st>>>(a);
+    e = cudaGetLastError();
   }
-  rms_quant_dgain_kernel<<<(a.s.d + 31) / 32, 256, 0, st>>>(a.partial, blocks, a.s.d, dgain);
+  if (e != cudaSuccess) return e;
+  rms_quant_dgain_kernel<<<(c.d + 31) / 32, 1024, 0, st>>>(c.partial, blocks, c.d, c.dgain);
   return cudaGetLastError();
 }
 
 template <typename T>
 cudaError_t grad_of(const RmsQuantGradCall &c, cudaStream_t st) {
-  GradArgs<T> a = {{c.rows, c.d, 0}, static_cast<const T *>(c.dy), static_cast<const T *>(c.h), static_cast<const T *>(c.dsum),
-                   c.lddy, c.ldh, c.ldd, c.gain, c.eps, static_cast<T *>(c.dx), c.partial};
   constexpr int V = kVec<T>;
   const bool vec = on16(c.dy) && on16(c.h) && on16(c.dsum) && on16(c.dx) && c.d % V == 0 && c.lddy % V == 0 && c.ldh % V == 0 &&
                    c.ldd % V == 0;
-  if (c.d <= 1024 * kPerThread)
-    return vec ? launch_grad<T, V, kPerThread>(a, c.dgain, st) : launch_grad<T, 1, kPerThread>(a, c.dgain, st);
-  return vec ? launch_grad<T, V, kPerThreadWide>(a, c.dgain, st) : launch_grad<T, 1, kPerThreadWide>(a, c.dgain, st);
+  return vec ? launch_grad<T, V>(c, st) : launch_grad<T, 1>(c, st);
 }
 
 }  // namespace
@@ -368,8 +729,15 @@ cudaError_t launch_rms_quant(const RmsQuantCall &c, cudaStream_t st) {
   return c.dtype == 0 ? quant_of<float>(c, st) : c.dtype == 1 ? quant_of<__half>(c, st) : quant_of<__nv_bfloat16>(c, st);
 }
 
+// (for any type, and with a dsum or without)
 int64_t rms_quant_grad_partials(int64_t rows, int d) {
-  return static_cast<int64_t>(grad_blocks(rows, d, d <= 1024 * kPerThread ? kPerThread : kPerThreadWide)) * d;
+  int most = grad_blocks(rows, d);
+  for (int bytes = 2; bytes <= 4; bytes += 2)
+    for (int sources = 2; sources <= 3; ++sources) {
+      const RingPlan p = ring_plan(rows, d, bytes, sources);
+      if (p.ring && p.blocks > most) most = p.blocks;
+    }
+  return static_cast<int64_t>(most) * d;
 }
 
 cudaError_t launch_rms_quant_grad(const RmsQuantGradCall &c, cudaStream_t st) {
