@@ -282,6 +282,23 @@ cudaError_t launch_aap_ternarize(const float *const *w, int n, const int64_t *le
 cudaError_t launch_unpack_weights(const uint8_t *packed, int n_layers, int D, const ChunkDesc *chunks, int n_chunks,
                                   uint32_t layer_bytes, uint8_t *wstream, cudaStream_t stream);
 
+// A launch that may begin before the kernel before it on the stream is over, up to its own grid_wait: the second kernels of
+// operators, whose launch and first instructions would otherwise add some 2 us to a call.
+template <class... P, class... A>
+cudaError_t launch_dependent(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t stream, const A &...args) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[0].val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = grid;
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
+  cfg.dynamicSmemBytes = smem;
+  cfg.stream = stream;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, P(args)...);
+}
+
 int sm_count();  // SMs of the current device (norm.cu)
 // Host memory that the operators' kernels see: 1 once a wait in one of them has given up (linear.cu).  NULL where it could not be
 // allocated.

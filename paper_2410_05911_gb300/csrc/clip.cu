@@ -14,6 +14,7 @@
 
 #include "aecct_internal.h"
 #include "rowtypes.cuh"
+#include "sm103_ptx.cuh"
 
 namespace aecct {
 
@@ -107,6 +108,7 @@ __device__ __forceinline__ void scale_piece(const T *p, T *o, int n, float c) {
 template <int N>
 __global__ void __launch_bounds__(kThreads1) clip_norm_kernel(const __grid_constant__ ClipTable<N> t, double *partial) {
   __shared__ double buf[kThreads1 / 32];
+  grid_trigger();
   double sum = 0.0;
   for (int64_t piece = blockIdx.x; piece < t.first[t.n]; piece += gridDim.x) {
     const int j = tensor_of(t, piece);
@@ -125,6 +127,7 @@ template <int N>
 __global__ void __launch_bounds__(kThreads1) clip_scale_kernel(const __grid_constant__ ClipTable<N> t, const double *partial,
                                                                int parts, float max_norm, float eps, float *norm) {
   __shared__ double buf[kThreads1 / 32];
+  grid_wait();
   double v = 0.0;
   for (int i = threadIdx.x; i < parts; i += kThreads1) v += partial[i];
   const float nm = static_cast<float>(sqrt(cta_sum(v, buf)));
@@ -164,9 +167,15 @@ cudaError_t run_clip(int n, const void *const *g, const int64_t *len, const int3
   for (int pass = 0; pass < 2; ++pass)
     for (int j0 = 0; j0 < n || (j0 == 0 && n == 0); j0 += N) {
       const int blocks = fill(t, j0, n - j0 < N ? n - j0 : N, g, len, dtype, out);
-      if (pass == 0) clip_norm_kernel<N><<<blocks, kThreads1, 0, st>>>(t, partial + parts), parts += blocks;
-      else clip_scale_kernel<N><<<blocks, kThreads1, 0, st>>>(t, partial, parts, max_norm, eps, j0 == 0 ? norm : nullptr);
-      const cudaError_t e = cudaGetLastError();
+      cudaError_t e;
+      if (pass == 0) {
+        clip_norm_kernel<N><<<blocks, kThreads1, 0, st>>>(t, partial + parts);
+        e = cudaGetLastError();
+        parts += blocks;
+      } else {
+        e = launch_dependent(clip_scale_kernel<N>, dim3(blocks), kThreads1, 0, st, t, partial, parts, max_norm, eps,
+                             j0 == 0 ? norm : static_cast<float *>(nullptr));
+      }
       if (e != cudaSuccess) return e;
     }
   return cudaSuccess;

@@ -205,6 +205,7 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : kSmallThreads) rms_quant_grad_
   const int t = BLOCK ? threadIdx.x : threadIdx.x & (G - 1);
   const int per = BLOCK ? 1 : kSmallThreads / G;
   const int64_t step = static_cast<int64_t>(gridDim.x) * per;
+  grid_trigger();
   float dg[E], g[E];
 #pragma unroll
   for (int j = 0; j < C; ++j) {
@@ -326,9 +327,17 @@ __device__ __forceinline__ void copy_range(const T *p, int d, bool first_row, bo
 template <typename T>
 __host__ __device__ constexpr int row_bytes(int d) { return (d * static_cast<int>(sizeof(T)) + 31) / 16 * 16; }
 
-// one thread: the copies of a row's N sources into `stage`
-template <typename T, int N>
+// one thread: the copies of a row's N sources into `stage`.  ALIGNED: every row starts and ends on 16 bytes
+template <typename T, int N, bool ALIGNED = false>
 __device__ __forceinline__ void copy_rows(const RowSource<T> (&src)[N], int64_t row, int64_t rows, int d, uint32_t stage, uint32_t bar) {
+  if constexpr (ALIGNED) {
+    const uint32_t bytes = d * sizeof(T);
+    mbar_arrive_expect_tx(bar, (src[N - 1].p ? N : N - 1) * bytes);
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+      if (src[k].p) bulk_g2s(stage + k * row_bytes<T>(d), src[k].p + row * src[k].ld, bytes, bar);
+    return;
+  }
   uintptr_t first[N], last[N];
   uint32_t bytes = 0;
 #pragma unroll
@@ -347,8 +356,9 @@ __device__ __forceinline__ void copy_rows(const RowSource<T> (&src)[N], int64_t 
     }
 }
 // where source k's row lies in its stage
-template <typename T>
+template <typename T, bool ALIGNED = false>
 __device__ __forceinline__ T *row_in(uint8_t *stage, const RowSource<T> &src, int k, int64_t row, int d) {
+  if constexpr (ALIGNED) return reinterpret_cast<T *>(stage + k * row_bytes<T>(d));
   return reinterpret_cast<T *>(stage + k * row_bytes<T>(d) + (reinterpret_cast<uintptr_t>(src.p + row * src.ld) & 15));
 }
 // all threads: the elements of the first and last row that no copy takes
@@ -393,13 +403,15 @@ struct RingGradArgs {
 };
 
 // One row a CTA at a time; thread t holds the sums of dgain of elements (j blockDim + t) V ... (V = 1 where a row or its
-// outputs do not start on 16 bytes).
+// outputs do not start on 16 bytes).  A row is read from shared memory once, its products kept in pairs: with two
+// passes over it in single operations (328 instructions of a thread for 8 elements of 4,096) the instructions were
+// the bound, 56 us for 8,192 bfloat16 rows.
 template <typename T, int V, int E>
-__global__ void __launch_bounds__(512) ring_grad_kernel(const __grid_constant__ RingGradArgs<T> a) {
+__global__ void __launch_bounds__(512, E == kFew ? 2 : 1) ring_grad_kernel(const __grid_constant__ RingGradArgs<T> a) {
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ uint64_t bars[kRing];
-  __shared__ float2 buf[2][16];
-  constexpr int C = E / V;
+  __shared__ __align__(16) f32x2 buf[2][16];  // a warp's sums, zeros where there is no warp
+  constexpr int C = E / V, H = E / 2;
   const int d = a.d, t = threadIdx.x, G = blockDim.x;
   const int stage_bytes = (a.src[2].p ? 3 : 2) * row_bytes<T>(d);
   const uint32_t bar = smem_u32(bars), base = smem_u32(ring);
@@ -408,82 +420,116 @@ __global__ void __launch_bounds__(512) ring_grad_kernel(const __grid_constant__ 
     fence_mbar_init_cluster();
     for (int s = 0; s < a.ring; ++s) {
       const int64_t row = blockIdx.x + static_cast<int64_t>(s) * gridDim.x;
-      if (row < a.rows) copy_rows(a.src, row, a.rows, d, base + s * stage_bytes, bar + 8 * s);
+      if (row < a.rows) copy_rows<T, 3, (V > 1)>(a.src, row, a.rows, d, base + s * stage_bytes, bar + 8 * s);
     }
   }
-  float dg[E], g[E];
+  grid_trigger();
+  if (t < 32) buf[t >> 4][t & 15] = 0;
+  f32x2 dg[H], g[H];
+  const float by = __fdiv_rn(1.0f, static_cast<float>(d));
 #pragma unroll
-  for (int j = 0; j < C; ++j)
+  for (int k = 0; k < H; ++k) {
+    float v[2];
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const int i = (j * G + t) * V;
-      dg[j * V + e] = 0.0f, g[j * V + e] = i < d ? __ldg(a.gain + i + e) : 0.0f;
+    for (int e = 0; e < 2; ++e) {
+      const int j = (2 * k + e) / V, i = (j * G + t) * V + (2 * k + e) % V;
+      v[e] = i < d ? __ldg(a.gain + i) : 0.0f;
     }
+    dg[k] = 0, g[k] = pair(v[0], v[1]);
+  }
   __syncthreads();
-  int s = 0, parity = 0;
-  int64_t n = 0;
-  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, ++n) {
+  int s = 0, parity = 0, n = 0;
+  T *out = a.dx + static_cast<int64_t>(blockIdx.x) * d;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x, n ^= 1, out += static_cast<int64_t>(gridDim.x) * d) {
     uint8_t *stage = ring + s * stage_bytes;
     wait_copy(bar + 8 * s, parity, a.err);
-    patch_rows(a.src, row, a.rows, d, stage);
-    const T *h = row_in(stage, a.src[0], 0, row, d), *dy = row_in(stage, a.src[1], 1, row, d);
-    float ss = 0.0f, th = 0.0f;
+    if constexpr (V == 1) patch_rows(a.src, row, a.rows, d, stage);
+    f32x2 h[H], t2[H], p[H];  // h, dy gain, dy h
+    f32x2 ss = 0, th = 0;
+    {
+      const T *hs = row_in<T, (V > 1)>(stage, a.src[0], 0, row, d), *ys = row_in<T, (V > 1)>(stage, a.src[1], 1, row, d);
+      float x[E], y[E];
 #pragma unroll
-    for (int j = 0; j < C; ++j) {
-      const int i = (j * G + t) * V;
-      if (i < d) {
-        float x[V], y[V];
-        load_v<T, V>(h + i, x), load_v<T, V>(dy + i, y);
+      for (int j = 0; j < C; ++j) {
+        const int i = (j * G + t) * V;
+        if (i < d) {
+          load_v<T, V>(hs + i, x + j * V), load_v<T, V>(ys + i, y + j * V);
+        } else {
 #pragma unroll
-        for (int e = 0; e < V; ++e) ss = fmaf(x[e], x[e], ss), th = fmaf(y[e] * g[j * V + e], x[e], th);
-      }
-    }
-    for (int o = 16; o > 0; o >>= 1) {
-      ss += __shfl_xor_sync(0xffffffffu, ss, o);
-      th += __shfl_xor_sync(0xffffffffu, th, o);
-    }
-    float2 *b = buf[n & 1];
-    if ((t & 31) == 0) b[t >> 5] = make_float2(ss, th);
-    __syncthreads();
-    // (every thread is done with the row before: its place takes the next row but ring - 1)
-    if (t == 0 && n > 0) {
-      const int64_t next = row + static_cast<int64_t>(a.ring - 1) * gridDim.x;
-      const int place = s == 0 ? a.ring - 1 : s - 1;
-      if (next < a.rows) copy_rows(a.src, next, a.rows, d, base + place * stage_bytes, bar + 8 * place);
-    }
-    float2 v = (t & 31) < (G >> 5) ? b[t & 31] : make_float2(0.0f, 0.0f);
-    for (int o = 8; o > 0; o >>= 1) {
-      v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-      v.y += __shfl_xor_sync(0xffffffffu, v.y, o);
-    }
-    v.x = __shfl_sync(0xffffffffu, v.x, 0), v.y = __shfl_sync(0xffffffffu, v.y, 0);  // (16 warps at most)
-    const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(v.x, static_cast<float>(d)) + a.eps));
-    const float c = r * r * r * __fdiv_rn(v.y, static_cast<float>(d));
-    const T *ds = a.src[2].p ? row_in(stage, a.src[2], 2, row, d) : nullptr;
-#pragma unroll
-    for (int j = 0; j < C; ++j) {
-      const int i = (j * G + t) * V;
-      if (i < d) {
-        float x[V], y[V], o[V];
-        load_v<T, V>(h + i, x), load_v<T, V>(dy + i, y);
-        if (ds) load_v<T, V>(ds + i, o);
-#pragma unroll
-        for (int e = 0; e < V; ++e) {
-          const float w = fmaf(-x[e], c, r * (y[e] * g[j * V + e]));
-          o[e] = ds ? w + o[e] : w;
-          dg[j * V + e] = fmaf(y[e], x[e] * r, dg[j * V + e]);
+          for (int e = 0; e < V; ++e) x[j * V + e] = y[j * V + e] = 0.0f;
         }
-        store_v<T, V>(a.dx + row * d + i, o);
       }
+#pragma unroll
+      for (int k = 0; k < H; ++k) {
+        const f32x2 yy = pair(y[2 * k], y[2 * k + 1]);
+        h[k] = pair(x[2 * k], x[2 * k + 1]);
+        t2[k] = mul2(yy, g[k]), p[k] = mul2(yy, h[k]);
+        ss = fma2(h[k], h[k], ss), th = fma2(p[k], g[k], th);
+      }
+    }
+    // both sums side by side in a pair
+    float s0, s1, h0, h1;
+    unpair(ss, s0, s1), unpair(th, h0, h1);
+    f32x2 sum = add2(pair(s0, h0), pair(s1, h1));
+    for (int o = 16; o > 0; o >>= 1) sum = add2(sum, __shfl_xor_sync(0xffffffffu, sum, o));
+    f32x2 *b = buf[n];
+    if ((t & 31) == 0) b[t >> 5] = sum;
+    __syncthreads();
+    sum = 0;
+#pragma unroll
+    for (int w = 0; w < 16; w += 2) {
+      const ulonglong2 v = *reinterpret_cast<const ulonglong2 *>(b + w);
+      sum = add2(add2(sum, v.x), v.y);
+    }
+    float sq, dot;
+    unpair(sum, sq, dot);
+    const float r = rsqrtf(fmaf(sq, by, a.eps)), c = -r * r * r * (dot * by);
+    const f32x2 r2 = pair(r, r), c2 = pair(c, c);
+    const T *ds = a.src[2].p ? row_in<T, (V > 1)>(stage, a.src[2], 2, row, d) : nullptr;
+#pragma unroll
+    for (int k = 0; k < H; ++k) dg[k] = fma2(p[k], r2, dg[k]);
+#pragma unroll
+    for (int j = 0; j < C; ++j) {
+      const int i = (j * G + t) * V;
+      if (i < d) {
+        float o[V];
+        if (ds) {
+          load_v<T, V>(ds + i, o);
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; ++e) o[e] = 0.0f;
+        }
+        if constexpr (V == 1) {
+          float hh[2], tt[2];
+          unpair(h[j / 2], hh[0], hh[1]), unpair(t2[j / 2], tt[0], tt[1]);
+          o[0] = fmaf(tt[j & 1], r, fmaf(hh[j & 1], c, o[0]));
+        } else {
+#pragma unroll
+          for (int e = 0; e < V; e += 2) {
+            const int k = (j * V + e) / 2;
+            unpair(fma2(t2[k], r2, fma2(h[k], c2, pair(o[e], o[e + 1]))), o[e], o[e + 1]);
+          }
+        }
+        store_v<T, V>(out + i, o);
+      }
+    }
+    __syncthreads();
+    // (every thread is done with the row: its place takes another)
+    if (t == 0) {
+      const int64_t next = row + static_cast<int64_t>(a.ring) * gridDim.x;
+      if (next < a.rows) copy_rows<T, 3, (V > 1)>(a.src, next, a.rows, d, base + s * stage_bytes, bar + 8 * s);
     }
     if (++s == a.ring) s = 0, parity ^= 1;
   }
 #pragma unroll
-  for (int j = 0; j < C; ++j) {
-    const int i = (j * G + t) * V;
-    if (i < d)
+  for (int k = 0; k < H; ++k) {
+    float v[2];
+    unpair(dg[k], v[0], v[1]);
 #pragma unroll
-      for (int e = 0; e < V; ++e) a.partial[static_cast<int64_t>(blockIdx.x) * d + i + e] = dg[j * V + e];
+    for (int e = 0; e < 2; ++e) {
+      const int j = (2 * k + e) / V, i = (j * G + t) * V + (2 * k + e) % V;
+      if (i < d) a.partial[static_cast<int64_t>(blockIdx.x) * d + i] = v[e];
+    }
   }
 }
 
@@ -507,7 +553,7 @@ template <typename T, int E>
 __global__ void __launch_bounds__(512) ring_quant_kernel(const __grid_constant__ RingQuantArgs<T> a) {
   extern __shared__ __align__(16) uint8_t ring[];
   __shared__ uint64_t bars[kRing];
-  __shared__ float2 buf[2][16];
+  __shared__ __align__(16) float2 buf[2][16];  // a warp's sum and maximum, zeros where there is no warp
   const int d = a.d, t = threadIdx.x, G = blockDim.x;
   const int stage_bytes = (a.src[1].p ? 2 : 1) * row_bytes<T>(d);
   const uint32_t bar = smem_u32(bars), base = smem_u32(ring);
@@ -519,6 +565,7 @@ __global__ void __launch_bounds__(512) ring_quant_kernel(const __grid_constant__
       if (row < a.rows) copy_rows(a.src, row, a.rows, d, base + s * stage_bytes, bar + 8 * s);
     }
   }
+  if (t < 32) buf[t >> 4][t & 15] = make_float2(0.0f, 0.0f);
   float g[E];
 #pragma unroll
   for (int j = 0; j < E; ++j) g[j] = j * G + t < d ? __ldg(a.gain + j * G + t) : 0.0f;
@@ -559,12 +606,12 @@ __global__ void __launch_bounds__(512) ring_quant_kernel(const __grid_constant__
       const int64_t next = row + static_cast<int64_t>(a.ring) * gridDim.x;
       if (next < a.rows) copy_rows(a.src, next, a.rows, d, base + s * stage_bytes, bar + 8 * s);
     }
-    float2 v = (t & 31) < (G >> 5) ? b[t & 31] : make_float2(0.0f, 0.0f);
-    for (int o = 8; o > 0; o >>= 1) {
-      v.x += __shfl_xor_sync(0xffffffffu, v.x, o);
-      v.y = fmaxf(v.y, __shfl_xor_sync(0xffffffffu, v.y, o));
+    float2 v = make_float2(0.0f, 0.0f);
+#pragma unroll
+    for (int w = 0; w < 16; w += 2) {
+      const float4 u = *reinterpret_cast<const float4 *>(b + w);
+      v.x += u.x + u.z, v.y = fmaxf(v.y, fmaxf(u.y, u.w));
     }
-    v.x = __shfl_sync(0xffffffffu, v.x, 0), v.y = __shfl_sync(0xffffffffu, v.y, 0);  // (16 warps at most)
     const float alpha = fmaxf(v.y, kAlphaMin), inv = __fdiv_rn(127.0f, alpha);
     const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(v.x, static_cast<float>(d)) + a.eps));
     const float sc = __fdiv_rn(alpha * r, 127.0f);
@@ -587,6 +634,7 @@ __global__ void __launch_bounds__(1024) rms_quant_dgain_kernel(const float *part
   __shared__ float s[32][33];
   const int c = threadIdx.x & 31, k0 = threadIdx.x >> 5, i = blockIdx.x * 32 + c;
   float v = 0.0f;
+  grid_wait();
   if (i < d)
 #pragma unroll 4
     for (int k = k0; k < parts; k += 32) v += partial[static_cast<int64_t>(k) * d + i];
@@ -701,8 +749,7 @@ cudaError_t launch_grad(const RmsQuantGradCall &c, cudaStream_t st) {
     e = cudaGetLastError();
   }
   if (e != cudaSuccess) return e;
-  rms_quant_dgain_kernel<<<(c.d + 31) / 32, 1024, 0, st>>>(c.partial, blocks, c.d, c.dgain);
-  return cudaGetLastError();
+  return launch_dependent(rms_quant_dgain_kernel, dim3((c.d + 31) / 32), 1024, 0, st, c.partial, blocks, c.d, c.dgain);
 }
 
 template <typename T>
