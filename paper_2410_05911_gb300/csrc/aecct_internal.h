@@ -373,10 +373,10 @@ cudaError_t launch_aap_linear_grad(const AapLinearGradCall &c, cudaStream_t stre
 
 // clip.cu: the global norm over many tensors, and clipping
 constexpr int kClipMaxTensors = 512;  // tensors of a launch (the launcher splits larger calls)
-constexpr int kClipMaxBlocks = 2048;  // partial sums of a launch's CTAs
+constexpr int kClipMaxBlocks = 2048;  // partial sums of a launch's CTAs, 8 bytes each
 int64_t clip_partials(int n_tensors);
 cudaError_t launch_clip_gradients(int n, const void *const *g, const int64_t *len, const int32_t *dtype, void *const *out,
-                                  float max_norm, float eps, float *norm, double *partial, cudaStream_t stream);
+                                  float max_norm, float eps, float *norm, float2 *partial, cudaStream_t stream);
 
 // spe.cu: the spectral positional encoding (Sec. 4.3) on the GPU
 constexpr int kSpeMaxHeads = 8;

@@ -1387,7 +1387,7 @@ int aecct_aap_linear_backward(const void *dy, int64_t lddy, const int8_t *codes,
 
 int aecct_clip_workspace(int32_t n_tensors, int64_t *bytes) {
   if (!bytes || n_tensors < 0) return AECCT_ERR_INVALID_ARG;
-  *bytes = clip_partials(n_tensors) * static_cast<int64_t>(sizeof(double));
+  *bytes = clip_partials(n_tensors) * static_cast<int64_t>(sizeof(float2));
   return AECCT_OK;
 }
 
@@ -1397,14 +1397,14 @@ int aecct_clip_gradients(int32_t n_tensors, const void *const *grad, const int64
   if (n_tensors < 0 || (n_tensors > 0 && (!grad || !len || !dtype || !out))) return AECCT_ERR_INVALID_ARG;
   if (!(max_norm > 0.0f) || !std::isfinite(max_norm) || !(eps >= 0.0f) || !std::isfinite(eps)) return AECCT_ERR_INVALID_ARG;
   if (!is_array(norm, AECCT_F32) || !workspace || (reinterpret_cast<uintptr_t>(workspace) & 7u) ||
-      workspace_bytes < clip_partials(n_tensors) * static_cast<int64_t>(sizeof(double)))
+      workspace_bytes < clip_partials(n_tensors) * static_cast<int64_t>(sizeof(float2)))
     return AECCT_ERR_INVALID_ARG;
   for (int j = 0; j < n_tensors; ++j) {
     if (len[j] < 0 || !element_type(dtype[j])) return AECCT_ERR_INVALID_ARG;
     if (len[j] > 0 && (!is_array(grad[j], dtype[j]) || !is_array(out[j], dtype[j]))) return AECCT_ERR_INVALID_ARG;
   }
   const cudaError_t e = launch_clip_gradients(n_tensors, grad, len, dtype, out, max_norm, eps, norm,
-                                              static_cast<double *>(workspace), static_cast<cudaStream_t>(cuda_stream));
+                                              static_cast<float2 *>(workspace), static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "clip_gradients launch");
 }
 

@@ -30,7 +30,7 @@ bool stages_codes(int64_t N) { return N >= 1536; }
 template <class F>
 auto with_forward_tile(int64_t M, const F &f) {
   if (M <= 16) return f(std::integral_constant<int, 16>());
-  return with_single_tile(M, f);
+  return with_single_tile<1>(M, f);
 }
 
 constexpr int64_t kFloat = sizeof(float);

@@ -670,6 +670,7 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     fence_mbar_init_cluster();
     word[1] = 0;
   }
+  grid_trigger();
   if (warp == kProducerWarps) {
     tmem_alloc_cg<CG>(smem_u32(const_cast<uint32_t *>(word)), S::kTmemCols);
     tmem_relinquish_cg<CG>();
@@ -751,6 +752,9 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     // the loads in flight.  In the second CTA that is all; it tells the first.
     constexpr uint32_t idesc = gemm_idesc(B::kBf, A::kMN, B::kMN, 128 * CG, TB);
     constexpr uint32_t la = tile_lbo(A::kMN), lb = tile_lbo(B::kMN);
+    constexpr uint32_t ka = 2 * la / 16, kb = (!B::kTma ? 2 * lb : B::kMN ? 2048u : 32u) / 16;  // 16 of r on, in 16-byte units
+    const uint64_t a0 = make_sdesc(base + P * S::kPieceBytes, la, tile_sbo(A::kMN));
+    const uint64_t b0 = !B::kTma ? make_sdesc(base, lb, tile_sbo(B::kMN)) : make_sdesc_sw128(base, B::kMN ? 8192 : 16, 1024);
     const uint32_t full0 = CG == 2 ? mapa_cluster(full, 0) : full;
     int s = 0;
     uint32_t parity = 0;
@@ -759,20 +763,15 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
       fence_proxy_async_smem();
       if (rank == 0) {
         tc_fence_after();
+        // descriptors of stage 0 moved on: an address is in 16-byte units in a descriptor's low word
 #pragma unroll
         for (int u = 0; u < S::kSteps; ++u) {
-          const uint32_t bt = base + s * S::kStageBytes + u * S::kStepBytes, at = bt + P * S::kPieceBytes;
+          const uint32_t off = (s * S::kStageBytes + u * S::kStepBytes) >> 4;
 #pragma unroll
           for (int p = 0; p < P; ++p)
-#pragma unroll
-            for (int ks = 0; ks < kStep / 16; ++ks) {
-              const uint32_t b = bt + p * S::kPieceBytes;
-              const uint64_t bdesc = !B::kTma  ? make_sdesc(b + ks * 2 * lb, lb, tile_sbo(B::kMN))
-                                     : B::kMN ? make_sdesc_sw128(b + ks * 2048, 8192, 1024)
-                                              : make_sdesc_sw128(b + ks * 32, 16, 1024);
-              mma_f16_cg_warp<CG>(tmem, make_sdesc(at + ks * 2 * la, la, tile_sbo(A::kMN)), bdesc, idesc,
-                                  it > 0 || u > 0 || p > 0 || ks > 0 ? 1u : 0u);
-            }
+            mma_f16_x4_warp<CG, ka, kb>(tmem, static_cast<uint32_t>(a0) + off, static_cast<uint32_t>(a0 >> 32),
+                                                   static_cast<uint32_t>(b0) + off + (p * S::kPieceBytes >> 4),
+                                                   static_cast<uint32_t>(b0 >> 32), idesc, it > 0 || u > 0 || p > 0 ? 1u : 0u);
         }
         mma_commit_cg_warp<CG>(empty + 8 * s);
       } else {
@@ -859,15 +858,17 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   }
 }
 
-// the splits' sums, added in order, and the epilogue
+// the splits' sums, added in order, and the epilogue: an element a thread
 template <class Out>
 __global__ void __launch_bounds__(256) gemm_join_kernel(const float *partial, int splits, int64_t I, int64_t J, const Out out) {
-  const int64_t i = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x, j = blockIdx.y;
-  for (int64_t jj = j; jj < J; jj += gridDim.y) {
-    if (i >= I) return;
+  grid_wait();
+  const int64_t all = I * J;
+  for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < all; at += static_cast<int64_t>(gridDim.x) * 256) {
+    const int64_t j = at / I, i = at - j * I;
     float v = 0.0f;
-    for (int s = 0; s < splits; ++s) v += partial[(s * J + jj) * I + i];
-    put_element(out.y, out.dtype, jj * out.ld + i, v * out.factor(jj) + out.add(i));
+#pragma unroll 8
+    for (int s = 0; s < splits; ++s) v += partial[s * all + at];
+    put_element(out.y, out.dtype, j * out.ld + i, fmaf(v, out.factor(j), out.add(i)));
   }
 }
 
@@ -945,20 +946,21 @@ cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b,
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   if ((e = cudaLaunchKernelEx(&cfg, kernel, g)) != cudaSuccess || !g.partial) return e;
-  gemm_join_kernel<Out><<<dim3(static_cast<unsigned>((I + 255) / 256), static_cast<unsigned>(J < 65535 ? J : 65535)), 256, 0, st>>>(
-      partial, p.splits, I, J, out);
-  return cudaGetLastError();
+  const int64_t blocks = (I * J + 255) / 256, most = static_cast<int64_t>(sms) * 32;
+  return launch_dependent(gemm_join_kernel<Out>, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), 256, 0, st,
+                          static_cast<const float *>(partial), p.splits, I, J, out);
 }
 
 // The tile of a product.  A pair's 256 x 256 where those fill half of the SMs at least (2,048 x 1,024 x 1,024: 64 CTAs in
 // pairs 16.7 us, 128 single ones 12.7 us; 1,024 x 4,096 x 4,096: 128 in pairs 46 us, 256 single ones 58 us), else a
-// single CTA's, of 64 j at most where there are no more (the rest of a tile would be converted zeros), of 128.
+// single CTA's, of 64 j at most where there are no more (the rest of a tile would be converted zeros) or three pieces of
+// more would leave an SM one CTA, of 128.
 inline bool pair_tiles(int64_t I, int64_t J, int sms) {
   return I > kTileI && J > kTileI && 2 * ((I + 255) / 256 * 2) * ((J + 255) / 256) >= sms;
 }
-template <class F>
+template <int P, class F>
 auto with_single_tile(int64_t J, const F &f) {
-  return J <= 64 ? f(std::integral_constant<int, 64>()) : f(std::integral_constant<int, 128>());
+  return J <= 64 || P == 3 ? f(std::integral_constant<int, 64>()) : f(std::integral_constant<int, 128>());
 }
 
 // linear_stage.cu

@@ -46,7 +46,7 @@ cudaError_t input_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t s
     float *partial = reinterpret_cast<float *>(work + 2 * kPieces<T> * c.M * padded(c.N));
     return launch_gemm<Weights<T>, Staged<T>, OutX, 256, 2>(c.K, c.M, c.N, a, b, out, partial, sms, wait_status(), st);
   }
-  return with_single_tile(c.M, [&](auto tb) {
+  return with_single_tile<kPieces<T>>(c.M, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
     using B = GradK<T, TB>;
     const B b = {static_cast<const T *>(c.dy), c.M, c.lddy, grads_vec<T>(c.dy, c.lddy, c.N)};
@@ -58,7 +58,7 @@ template <typename T>
 int64_t input_grad_workspace(int64_t M, int64_t K, int64_t N) {
   const int sms = sm_count();
   if (pair_tiles(K, M, sms)) return partial_floats(gemm_plan<Weights<T>, Staged<T>, 256, 2>(K, M, N, sms), K, M) * kFloat + 2 * kPieces<T> * M * padded(N);
-  return with_single_tile(M, [&](auto tb) {
+  return with_single_tile<kPieces<T>>(M, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
     return partial_floats(gemm_plan<Weights<T>, GradK<T, TB>, TB, 1>(K, M, N, sms), K, M) * kFloat;
   });

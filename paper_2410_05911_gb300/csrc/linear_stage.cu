@@ -39,6 +39,7 @@ template <typename T, int P>
 __global__ void __launch_bounds__(kStageThreads) stage_grads_kernel(const T *dy, int64_t ld, bool vec, int64_t M, int64_t N, int64_t Np,
                                                                     const float *scale, uint16_t *out, float *partial) {
   __shared__ float sums[8][256];
+  grid_trigger();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + 8 * lane;
   const int left = static_cast<int>(N - n < 8 ? N - n : 8);
@@ -80,19 +81,21 @@ __global__ void __launch_bounds__(kStageThreads) stage_grads_kernel(const T *dy,
   }
 }
 
-__global__ void __launch_bounds__(kStageThreads) join_sums_kernel(const float *partial, int parts, int64_t N, float *db) {
-  __shared__ float s[8][32];
-  const int64_t n = static_cast<int64_t>(blockIdx.x) * 32 + (threadIdx.x & 31);
-  const int k0 = threadIdx.x >> 5;
+// db[n] = the sum over the CTAs' partial sums, in a fixed order: 32 columns a CTA, 32 rows of them at a time
+__global__ void __launch_bounds__(1024) join_sums_kernel(const float *partial, int parts, int64_t N, float *db) {
+  __shared__ float s[32][33];
+  const int c = threadIdx.x & 31, k0 = threadIdx.x >> 5;
+  const int64_t n = static_cast<int64_t>(blockIdx.x) * 32;
   float v = 0.0f;
-  if (n < N)
-    for (int k = k0; k < parts; k += 8) v += partial[k * N + n];
-  s[k0][threadIdx.x & 31] = v;
+  grid_wait();
+  if (n + c < N)
+#pragma unroll 4
+    for (int k = k0; k < parts; k += 32) v += partial[k * N + n + c];
+  s[k0][c] = v;
   __syncthreads();
-  if (k0 == 0 && n < N) {
-    for (int k = 1; k < 8; ++k) v += s[k][threadIdx.x];
-    db[n] = v;
-  }
+  v = s[c][k0];  // column k0 of the CTA, a row a lane
+  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+  if (c == 0 && n + k0 < N) db[n + k0] = v;
 }
 
 template <typename T, int P>
@@ -102,8 +105,7 @@ cudaError_t stage_of(const StageGrads &c, cudaStream_t st) {
                                                            (c.N + 7) / 8 * 8, c.scale, static_cast<uint16_t *>(c.out), c.db ? c.partial : nullptr);
   cudaError_t e = cudaGetLastError();
   if (e != cudaSuccess || !c.db) return e;
-  join_sums_kernel<<<static_cast<unsigned>((c.N + 31) / 32), kStageThreads, 0, st>>>(c.partial, static_cast<int>(grid.y), c.N, c.db);
-  return cudaGetLastError();
+  return launch_dependent(join_sums_kernel, dim3(static_cast<unsigned>((c.N + 31) / 32)), 1024, 0, st, c.partial, static_cast<int>(grid.y), c.N, c.db);
 }
 
 template <typename T>

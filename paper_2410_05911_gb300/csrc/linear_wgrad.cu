@@ -41,7 +41,7 @@ template <typename T, int P>
 cudaError_t weight_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t st) {
   const CodesT a = {c.codes, c.K, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
   const OutW out = {c.dw, c.wdtype, c.K};
-  return with_single_tile(c.N, [&](auto tb) {
+  return with_single_tile<P>(c.N, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
     using B = GradT<T, TB, P>;
     const B b = {static_cast<const T *>(c.dy), c.N, c.lddy, c.scale, grads_vec<T>(c.dy, c.lddy, c.N)};
@@ -59,7 +59,7 @@ template <int P>
 int64_t workspace_of(int64_t M, int64_t K, int64_t N) {
   const int sms = sm_count();
   if (pair_tiles(K, N, sms)) return partial_floats(gemm_plan<CodesT, Staged<P>, 256, 2>(K, N, M, sms), K, N) * kFloat + 2 * P * M * padded(N);
-  return with_single_tile(N, [&](auto tb) {
+  return with_single_tile<P>(N, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
     return partial_floats(gemm_plan<CodesT, GradT<float, TB, P>, TB, 1>(K, N, M, sms), K, N) * kFloat;
   });

@@ -87,5 +87,12 @@ __device__ __forceinline__ void store_v(T *p, const float *v) {
     *reinterpret_cast<uint4 *>(p) = make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]),
                                                pack2<T>(v[6], v[7]));
 }
+// the 16-byte store of values that nothing reads soon
+template <typename T>
+__device__ __forceinline__ void store_stream(T *p, const float *v) {
+  if constexpr (sizeof(T) == 4) __stcs(reinterpret_cast<float4 *>(p), make_float4(v[0], v[1], v[2], v[3]));
+  else
+    __stcs(reinterpret_cast<uint4 *>(p), make_uint4(pack2<T>(v[0], v[1]), pack2<T>(v[2], v[3]), pack2<T>(v[4], v[5]), pack2<T>(v[6], v[7])));
+}
 
 }  // namespace aecct

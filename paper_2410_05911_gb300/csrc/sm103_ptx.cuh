@@ -345,16 +345,28 @@ __device__ __forceinline__ void tmem_dealloc_cg(uint32_t taddr, uint32_t ncols) 
   if constexpr (CG == 1) tmem_dealloc(taddr, ncols);
   else asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(taddr), "r"(ncols) : "memory");
 }
-template <int CG>
-__device__ __forceinline__ void mma_f16_cg_warp(uint32_t tmem_d, uint64_t adesc, uint64_t bdesc, uint32_t idesc, uint32_t accumulate) {
-  if constexpr (CG == 1) mma_bf16_warp(tmem_d, adesc, bdesc, idesc, accumulate);
-  else
-    asm volatile(
-        "{\n\t.reg .pred p, e;\n\t.reg .b32 r;\n\tsetp.ne.b32 p, %4, 0;\n\t"
-        "elect.sync r|e, 0xffffffff;\n\t"
-        "@e tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(tmem_d),
-        "l"(adesc), "l"(bdesc), "r"(idesc), "r"(accumulate)
-        : "memory");
+// Four MMAs along K (64 elements), operands' descriptors `a` and `b` plus ka and kb (in 16-byte units) a step; the first one
+// overwrites D where `accumulate` is 0.  Descriptors come as low and high words: the address is in the low one.
+template <int CG, uint32_t KA, uint32_t KB>
+__device__ __forceinline__ void mma_f16_x4_warp(uint32_t tmem_d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc,
+                                                uint32_t accumulate) {
+#define AECCT_MMA_X4(G)                                                                                              \
+  asm volatile(                                                                                                      \
+      "{\n\t.reg .pred p, e, t;\n\t.reg .b32 r, al, bl;\n\t.reg .b64 a, b;\n\tsetp.ne.b32 p, %6, 0;\n\tsetp.eq.b32 t, %5, %5;\n\t" \
+      "elect.sync r|e, 0xffffffff;\n\t"                                                                              \
+      "mov.b64 a, {%1, %2};\n\tmov.b64 b, {%3, %4};\n\t"                                                            \
+      "@e tcgen05.mma.cta_group::" G ".kind::f16 [%0], a, b, %5, p;\n\t"                                             \
+      "add.u32 al, %1, %7;\n\tadd.u32 bl, %3, %8;\n\tmov.b64 a, {al, %2};\n\tmov.b64 b, {bl, %4};\n\t"              \
+      "@e tcgen05.mma.cta_group::" G ".kind::f16 [%0], a, b, %5, t;\n\t"                                             \
+      "add.u32 al, al, %7;\n\tadd.u32 bl, bl, %8;\n\tmov.b64 a, {al, %2};\n\tmov.b64 b, {bl, %4};\n\t"              \
+      "@e tcgen05.mma.cta_group::" G ".kind::f16 [%0], a, b, %5, t;\n\t"                                             \
+      "add.u32 al, al, %7;\n\tadd.u32 bl, bl, %8;\n\tmov.b64 a, {al, %2};\n\tmov.b64 b, {bl, %4};\n\t"              \
+      "@e tcgen05.mma.cta_group::" G ".kind::f16 [%0], a, b, %5, t;\n\t}" ::"r"(tmem_d),                             \
+      "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate), "n"(KA), "n"(KB)                      \
+      : "memory")
+  if constexpr (CG == 1) AECCT_MMA_X4("1");
+  else AECCT_MMA_X4("2");
+#undef AECCT_MMA_X4
 }
 template <int CG>
 __device__ __forceinline__ void mma_commit_cg_warp(uint32_t bar) {
