@@ -615,6 +615,7 @@ struct GemmArgs {
   Out out;
   int tiles_i, steps;  // tiles along i (whole clusters); steps of a split
   int full;            // r that are left for a span to be loaded by full(), more than there are without alignment
+  int stages;
   int parts;           // splits that are one cluster and join in shared memory (CG = 1), else 1
   float *partial;      // [splits][J][I] where several join in a second kernel, else NULL
   int *err;            // set to 1 by a wait that gave up
@@ -633,15 +634,19 @@ struct GemmShape {
   static constexpr int kSteps = CG == 1 ? A::kSpan : 1;
   static constexpr uint32_t kStageBytes = kSteps * kStepBytes;
   static constexpr uint32_t kBars = 256 + TB * 4;  // barriers and two words; the columns' factors
+  static constexpr int kMaxStages = 8;
   static constexpr int fit(uint32_t room) { return static_cast<int>((room - kBars) / kStageBytes); }
   static constexpr uint32_t kHalfSm = kSmemPerSm / 2 - 1024;
   static constexpr int kCtasPerSm = fit(kHalfSm) >= 2 ? 2 : 1;
-  static constexpr int kAll = kCtasPerSm == 2 ? fit(kHalfSm) : fit(kMaxDynSmem);
-  static constexpr int kStages = kAll > 4 ? 4 : kAll;
-  static constexpr uint32_t kSmem = kStages * kStageBytes + kBars;
+  // stages of a CTA that has half of an SM, or all of one
+  static constexpr int stages(bool half) {
+    const int n = half ? fit(kHalfSm) : fit(kMaxDynSmem);
+    return n < kMaxStages ? n : kMaxStages;
+  }
+  static constexpr uint32_t smem(int stages) { return stages * kStageBytes + kBars; }
   static constexpr uint32_t kTmemCols = TB < 32 ? 32 : TB;
-  static_assert(kStages >= 2 && kStageBytes % 16 == 0 && kCtasPerSm * kTmemCols <= 512, "stages and accumulators");
-  static_assert(CG == 2 || kStages * kStageBytes >= kTileI * TB * 4, "a cluster joins its tile in the stages");
+  static_assert(stages(kCtasPerSm == 2) >= 2 && kStageBytes % 16 == 0 && kCtasPerSm * kTmemCols <= 512, "stages and accumulators");
+  static_assert(CG == 2 || stages(kCtasPerSm == 2) * kStageBytes >= kTileI * TB * 4, "a cluster joins its tile in the stages");
   static_assert(A::kSpan == B::kSpan, "operands load together");
 };
 
@@ -654,9 +659,10 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   const uint32_t base = smem_u32(smem);
   // full[stages]: this CTA's producers, its copies, and in a pair's first CTA the other's stage, in one barrier (each
   // wait costs the issuing warp some 200 cycles); empty[stages], done; 2 words
-  constexpr uint32_t kB = 8 * S::kStages;
-  const uint32_t full = base + S::kStages * S::kStageBytes, empty = full + kB, done = empty + kB;
-  volatile uint32_t *word = reinterpret_cast<volatile uint32_t *>(smem + S::kStages * S::kStageBytes + 2 * kB + 8);
+  constexpr uint32_t kB = 8 * S::kMaxStages;
+  uint8_t *tail = smem + g.stages * S::kStageBytes;
+  const uint32_t full = smem_u32(tail), empty = full + kB, done = empty + kB;
+  volatile uint32_t *word = reinterpret_cast<volatile uint32_t *>(tail + 2 * kB + 8);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = CG == 2 ? cluster_ctarank() : 0;
   const int64_t i0 = static_cast<int64_t>(blockIdx.x % g.tiles_i) * kTileI, j0 = static_cast<int64_t>(blockIdx.x / g.tiles_i) * TB;
@@ -665,7 +671,7 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   const int steps = kSpan * static_cast<int>((end - first + kSpan * kStep - 1) / (kSpan * kStep));
 
   if (tid == 0) {
-    for (int s = 0; s < S::kStages; ++s) mbar_init(full + 8 * s, kGroupWarps + (B::kTma ? 1 : 0) + (CG == 2 && rank == 0 ? 1 : 0)), mbar_init(empty + 8 * s, 1);
+    for (int s = 0; s < g.stages; ++s) mbar_init(full + 8 * s, kGroupWarps + (B::kTma ? 1 : 0) + (CG == 2 && rank == 0 ? 1 : 0)), mbar_init(empty + 8 * s, 1);
     mbar_init(done, 1);
     fence_mbar_init_cluster();
     word[1] = 0;
@@ -693,7 +699,7 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     return true;
   };
 
-  float *factor = reinterpret_cast<float *>(smem + S::kStages * S::kStageBytes + 256);
+  float *factor = reinterpret_cast<float *>(tail + 256);
   for (int c = tid; c < TB; c += kGemmThreads) factor[c] = g.partial ? 1.0f : j0 + c < g.J ? g.out.factor(j0 + c) : 0.0f;
   if (warp < kProducerWarps) {
     const int group = warp / kGroupWarps, at = tid - group * kGroupWarps * 32;
@@ -705,9 +711,9 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
       if (left >= g.full) g.a.full(ta, ra);
       else g.a.load(ta, left, ra);
     };
-    const auto skip = [](int &s, uint32_t &parity, int by) {
+    const auto skip = [&](int &s, uint32_t &parity, int by) {
       s += by;
-      if (s >= S::kStages) s -= S::kStages, parity ^= 1;
+      if (s >= g.stages) s -= g.stages, parity ^= 1;
     };
     int s = 0;
     uint32_t parity = 1;  // (a stage's first wait is for the phase before its first, and over at once)
@@ -778,7 +784,7 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
         __syncwarp();
         if (lane == 0) mbar_arrive_peer(full0 + 8 * s);
       }
-      if (++s == S::kStages) s = 0, parity ^= 1;
+      if (++s == g.stages) s = 0, parity ^= 1;
     }
     if (rank == 0) mma_commit_cg_warp<CG>(done);
   } else if constexpr (B::kTma) {
@@ -792,12 +798,12 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
         g.b.copy(x0, first + static_cast<int64_t>(it) * kStep, base + s * S::kStageBytes, full + 8 * s);
       }
       __syncwarp();
-      if (++s == S::kStages) s = 0, parity ^= 1;
+      if (++s == g.stages) s = 0, parity ^= 1;
     }
     // a CTA that gives up still waits for the copies it has begun: until they are over, or with an end
     if (it < steps)
-      for (int k = it < S::kStages ? 0 : it - S::kStages; k < it; ++k)
-        for (int tries = 0; !mbar_try_wait(full + 8 * (k % S::kStages), (k / S::kStages) & 1) && tries < kGemmWaitTries; ++tries) {}
+      for (int k = it < g.stages ? 0 : it - g.stages; k < it; ++k)
+        for (int tries = 0; !mbar_try_wait(full + 8 * (k % g.stages), (k / g.stages) & 1) && tries < kGemmWaitTries; ++tries) {}
   }
   __syncwarp();
   const bool ready = __all_sync(0xffffffffu, wait(done, 0) && !word[1]);
@@ -922,8 +928,10 @@ cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b,
                         cudaStream_t st) {
   using S = GemmShape<A, B, TB, CG>;
   const GemmPlan p = gemm_plan<A, B, TB, CG>(I, J, R, sms);
+  const int64_t ctas = p.tiles_i * p.tiles_j * p.splits;
+  const int stages = S::stages(S::kCtasPerSm == 2 && ctas > sms);
   const GemmArgs<A, B, Out> g = {I, J, R, a, b, out, static_cast<int>(p.tiles_i), p.steps,
-                                   a.aligned() && b.aligned() ? A::kSpan * kStep : INT_MAX, p.cluster ? p.splits : 1,
+                                   a.aligned() && b.aligned() ? A::kSpan * kStep : INT_MAX, stages, p.cluster ? p.splits : 1,
                                    p.splits > 1 && !p.cluster ? partial : nullptr, err};
   auto *kernel = gemm_kernel<A, B, Out, TB, CG>;
   static std::atomic<uint64_t> allowed{0};  // devices on which the kernel may use its shared memory
@@ -932,7 +940,7 @@ cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b,
   if (e != cudaSuccess) return e;
   const uint64_t bit = uint64_t(1) << (dev & 63);
   if (dev >= 64 || !(allowed.load(std::memory_order_relaxed) & bit)) {
-    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem)) != cudaSuccess) return e;
+    if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynSmem)) != cudaSuccess) return e;
     if (dev < 64) allowed.fetch_or(bit, std::memory_order_relaxed);
   }
   cudaLaunchAttribute attr[1];
@@ -941,7 +949,7 @@ cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b,
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(p.tiles_i * p.tiles_j), p.splits);
   cfg.blockDim = dim3(kGemmThreads);
-  cfg.dynamicSmemBytes = S::kSmem;
+  cfg.dynamicSmemBytes = S::smem(stages);
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
