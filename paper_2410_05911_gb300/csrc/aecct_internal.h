@@ -367,7 +367,8 @@ struct AapLinearGradCall {
 int64_t aap_linear_workspace(int64_t M, int64_t K, int64_t N);
 cudaError_t launch_aap_linear(const AapLinearCall &c, cudaStream_t stream);
 int64_t weight_grad_workspace(int64_t M, int64_t K, int64_t N, int wdtype);
-cudaError_t launch_weight_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t stream);
+// dependent: after a kernel of the same call
+cudaError_t launch_weight_grad(const AapLinearGradCall &c, uint8_t *work, bool dependent, cudaStream_t stream);
 int64_t aap_linear_grad_workspace(int64_t M, int64_t K, int64_t N, int dtype, int wdtype);
 cudaError_t launch_aap_linear_grad(const AapLinearGradCall &c, cudaStream_t stream);
 

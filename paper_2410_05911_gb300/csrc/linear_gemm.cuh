@@ -616,6 +616,7 @@ struct GemmArgs {
   int tiles_i, steps;  // tiles along i (whole clusters); steps of a split
   int full;            // r that are left for a span to be loaded by full(), more than there are without alignment
   int stages;
+  int dependent;       // launched before the kernel before it was over
   int parts;           // splits that are one cluster and join in shared memory (CG = 1), else 1
   float *partial;      // [splits][J][I] where several join in a second kernel, else NULL
   int *err;            // set to 1 by a wait that gave up
@@ -681,6 +682,7 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     tmem_alloc_cg<CG>(smem_u32(const_cast<uint32_t *>(word)), S::kTmemCols);
     tmem_relinquish_cg<CG>();
   }
+  if (g.dependent) grid_wait();
   tc_fence_before();
   if constexpr (CG == 2) cluster_sync_all();  // (the other CTA's barriers too)
   else __syncthreads();
@@ -867,6 +869,7 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
 // the splits' sums, added in order, and the epilogue: an element a thread
 template <class Out>
 __global__ void __launch_bounds__(256) gemm_join_kernel(const float *partial, int splits, int64_t I, int64_t J, const Out out) {
+  grid_trigger();
   grid_wait();
   const int64_t all = I * J;
   for (int64_t at = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; at < all; at += static_cast<int64_t>(gridDim.x) * 256) {
@@ -925,13 +928,13 @@ inline int64_t partial_floats(const GemmPlan &p, int64_t I, int64_t J) { return 
 
 template <class A, class B, class Out, int TB, int CG>
 cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b, const Out &out, float *partial, int sms, int *err,
-                        cudaStream_t st) {
+                        bool dependent, cudaStream_t st) {
   using S = GemmShape<A, B, TB, CG>;
   const GemmPlan p = gemm_plan<A, B, TB, CG>(I, J, R, sms);
   const int64_t ctas = p.tiles_i * p.tiles_j * p.splits;
   const int stages = S::stages(S::kCtasPerSm == 2 && ctas > sms);
   const GemmArgs<A, B, Out> g = {I, J, R, a, b, out, static_cast<int>(p.tiles_i), p.steps,
-                                   a.aligned() && b.aligned() ? A::kSpan * kStep : INT_MAX, stages, p.cluster ? p.splits : 1,
+                                   a.aligned() && b.aligned() ? A::kSpan * kStep : INT_MAX, stages, dependent ? 1 : 0, p.cluster ? p.splits : 1,
                                    p.splits > 1 && !p.cluster ? partial : nullptr, err};
   auto *kernel = gemm_kernel<A, B, Out, TB, CG>;
   static std::atomic<uint64_t> allowed{0};  // devices on which the kernel may use its shared memory
@@ -943,7 +946,9 @@ cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b,
     if ((e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDynSmem)) != cudaSuccess) return e;
     if (dev < 64) allowed.fetch_or(bit, std::memory_order_relaxed);
   }
-  cudaLaunchAttribute attr[1];
+  cudaLaunchAttribute attr[2];
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = CG, attr[0].val.clusterDim.y = p.cluster ? p.splits : 1, attr[0].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
@@ -952,7 +957,7 @@ cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b,
   cfg.dynamicSmemBytes = S::smem(stages);
   cfg.stream = st;
   cfg.attrs = attr;
-  cfg.numAttrs = 1;
+  cfg.numAttrs = dependent ? 2 : 1;
   if ((e = cudaLaunchKernelEx(&cfg, kernel, g)) != cudaSuccess || !g.partial) return e;
   const int64_t blocks = (I * J + 255) / 256, most = static_cast<int64_t>(sms) * 32;
   return launch_dependent(gemm_join_kernel<Out>, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), 256, 0, st,
@@ -982,6 +987,7 @@ struct StageGrads {
   void *out;           // [pieces][M][N up to a multiple of 8] 16-bit, or NULL
   float *db;           // [N] column sums, or NULL
   float *partial;      // [stage_parts(M, N)][N] with db
+  bool dependent;      // launched before the kernel before it is over
 };
 int stage_parts(int64_t M, int64_t N);
 cudaError_t launch_stage_codes(const int8_t *codes, int64_t ld, int64_t M, int64_t K, void *out, cudaStream_t st);

@@ -36,21 +36,22 @@ cudaError_t input_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t s
     Staged<T> b;
     const void *rows = c.dy;
     int64_t ld = c.lddy;
+    const bool staged = !in_place<T>(c.dy, c.lddy);
     cudaError_t e = cudaSuccess;
-    if (!in_place<T>(c.dy, c.lddy)) {
+    if (staged) {
       rows = work, ld = padded(c.N);
-      const StageGrads s = {c.dy, c.lddy, c.M, c.N, c.dtype, nullptr, sizeof(T) == 4 ? 3 : 0, work, nullptr, nullptr};
+      const StageGrads s = {c.dy, c.lddy, c.M, c.N, c.dtype, nullptr, sizeof(T) == 4 ? 3 : 0, work, nullptr, nullptr, false};
       if ((e = launch_stage_grads(s, st)) != cudaSuccess) return e;
     }
     if ((e = tensor_map(&b.map, rows, Staged<T>::kBf, c.N, c.M, ld, kPieces<T>, Staged<T>::X)) != cudaSuccess) return e;
     float *partial = reinterpret_cast<float *>(work + 2 * kPieces<T> * c.M * padded(c.N));
-    return launch_gemm<Weights<T>, Staged<T>, OutX, 256, 2>(c.K, c.M, c.N, a, b, out, partial, sms, wait_status(), st);
+    return launch_gemm<Weights<T>, Staged<T>, OutX, 256, 2>(c.K, c.M, c.N, a, b, out, partial, sms, wait_status(), staged, st);
   }
   return with_single_tile<kPieces<T>>(c.M, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
     using B = GradK<T, TB>;
     const B b = {static_cast<const T *>(c.dy), c.M, c.lddy, grads_vec<T>(c.dy, c.lddy, c.N)};
-    return launch_gemm<Weights<T>, B, OutX, TB, 1>(c.K, c.M, c.N, a, b, out, reinterpret_cast<float *>(work), sms, wait_status(), st);
+    return launch_gemm<Weights<T>, B, OutX, TB, 1>(c.K, c.M, c.N, a, b, out, reinterpret_cast<float *>(work), sms, wait_status(), false, st);
   });
 }
 
@@ -77,7 +78,7 @@ cudaError_t launch_aap_linear_grad(const AapLinearGradCall &c, cudaStream_t st) 
   uint8_t *work = static_cast<uint8_t *>(c.workspace);
   cudaError_t e = cudaSuccess;
   if (c.dx) e = c.dtype == 0 ? input_grad<float>(c, work, st) : c.dtype == 1 ? input_grad<__half>(c, work, st) : input_grad<__nv_bfloat16>(c, work, st);
-  if (e == cudaSuccess && (c.dw || c.db)) e = launch_weight_grad(c, work, st);
+  if (e == cudaSuccess && (c.dw || c.db)) e = launch_weight_grad(c, work, c.dx != nullptr, st);
   return e;
 }
 

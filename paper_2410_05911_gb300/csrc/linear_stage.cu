@@ -17,6 +17,7 @@ constexpr int kStageThreads = 256;
 // codes [M][ld] to halves [M][Kp], Kp a multiple of 128: 64 k of a block's first step, then those of its second
 __global__ void __launch_bounds__(kStageThreads) stage_codes_kernel(const int8_t *codes, int64_t ld, int unit, int64_t M, int K, int Kp,
                                                                     __half *out) {
+  grid_trigger();
   const int pieces = Kp / 16;  // of 16 codes, 8 to a block
   const int64_t all = M * pieces;
   for (int64_t i = static_cast<int64_t>(blockIdx.x) * kStageThreads + threadIdx.x; i < all; i += static_cast<int64_t>(gridDim.x) * kStageThreads) {
@@ -40,6 +41,7 @@ __global__ void __launch_bounds__(kStageThreads) stage_grads_kernel(const T *dy,
                                                                     const float *scale, uint16_t *out, float *partial) {
   __shared__ float sums[8][256];
   grid_trigger();
+  grid_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + 8 * lane;
   const int left = static_cast<int>(N - n < 8 ? N - n : 8);
@@ -87,6 +89,7 @@ __global__ void __launch_bounds__(1024) join_sums_kernel(const float *partial, i
   const int c = threadIdx.x & 31, k0 = threadIdx.x >> 5;
   const int64_t n = static_cast<int64_t>(blockIdx.x) * 32;
   float v = 0.0f;
+  grid_trigger();
   grid_wait();
   if (n + c < N)
 #pragma unroll 4
@@ -101,9 +104,18 @@ __global__ void __launch_bounds__(1024) join_sums_kernel(const float *partial, i
 template <typename T, int P>
 cudaError_t stage_of(const StageGrads &c, cudaStream_t st) {
   const dim3 grid(static_cast<unsigned>((c.N + 255) / 256), static_cast<unsigned>(stage_parts(c.M, c.N)));
-  stage_grads_kernel<T, P><<<grid, kStageThreads, 0, st>>>(static_cast<const T *>(c.dy), c.ld, grads_vec<T>(c.dy, c.ld, c.N), c.M, c.N,
-                                                           (c.N + 7) / 8 * 8, c.scale, static_cast<uint16_t *>(c.out), c.db ? c.partial : nullptr);
-  cudaError_t e = cudaGetLastError();
+  const bool vec = grads_vec<T>(c.dy, c.ld, c.N);
+  const int64_t Np = (c.N + 7) / 8 * 8;
+  float *partial = c.db ? c.partial : nullptr;
+  cudaError_t e;
+  if (c.dependent) {
+    e = launch_dependent(stage_grads_kernel<T, P>, grid, kStageThreads, 0, st, static_cast<const T *>(c.dy), c.ld, vec, c.M, c.N, Np,
+                         c.scale, static_cast<uint16_t *>(c.out), partial);
+  } else {
+    stage_grads_kernel<T, P><<<grid, kStageThreads, 0, st>>>(static_cast<const T *>(c.dy), c.ld, vec, c.M, c.N, Np, c.scale,
+                                                             static_cast<uint16_t *>(c.out), partial);
+    e = cudaGetLastError();
+  }
   if (e != cudaSuccess || !c.db) return e;
   return launch_dependent(join_sums_kernel, dim3(static_cast<unsigned>((c.N + 31) / 32)), 1024, 0, st, c.partial, static_cast<int>(grid.y), c.N, c.db);
 }
