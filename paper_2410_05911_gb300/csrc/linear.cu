@@ -41,12 +41,12 @@ constexpr int64_t kFloat = sizeof(float);
 int64_t aap_linear_workspace(int64_t M, int64_t K, int64_t N) {
   const int sms = sm_count();
   if (pair_tiles(N, M, sms)) {
-    if (stages_codes(N)) return partial_floats(gemm_plan<WeightsK, Staged, 256, 2>(N, M, K, sms), N, M) * kFloat + 2 * M * staged_k(K);
-    return partial_floats(gemm_plan<WeightsK, CodesK<128>, 256, 2>(N, M, K, sms), N, M) * kFloat;
+    if (stages_codes(N)) return partial_floats<WeightsK, Staged, 256, 2>(N, M, K, sms) * kFloat + 2 * M * staged_k(K);
+    return partial_floats<WeightsK, CodesK<128>, 256, 2>(N, M, K, sms) * kFloat;
   }
   return with_forward_tile(M, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
-    return partial_floats(gemm_plan<WeightsK, CodesK<TB>, TB, 1>(N, M, K, sms), N, M) * kFloat;
+    return partial_floats<WeightsK, CodesK<TB>, TB, 1>(N, M, K, sms) * kFloat;
   });
 }
 
@@ -56,7 +56,7 @@ cudaError_t launch_aap_linear(const AapLinearCall &c, cudaStream_t st) {
   const int sms = sm_count();
   if (pair_tiles(c.N, c.M, sms)) {
     if (!stages_codes(c.N)) {
-      const CodesK<128> b = {c.codes, c.M, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
+      const CodesK<128> b = {c.codes, c.M, c.K, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
       return launch_gemm<WeightsK, CodesK<128>, OutY, 256, 2>(c.N, c.M, c.K, a, b, out, static_cast<float *>(c.workspace), sms,
                                                              wait_status(), false, st);
     }
@@ -69,7 +69,7 @@ cudaError_t launch_aap_linear(const AapLinearCall &c, cudaStream_t st) {
   }
   return with_forward_tile(c.M, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
-    const CodesK<TB> b = {c.codes, c.M, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
+    const CodesK<TB> b = {c.codes, c.M, c.K, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
     return launch_gemm<WeightsK, CodesK<TB>, OutY, TB, 1>(c.N, c.M, c.K, a, b, out, static_cast<float *>(c.workspace), sms,
                                                          wait_status(), false, st);
   });

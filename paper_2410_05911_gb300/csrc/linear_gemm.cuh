@@ -112,11 +112,14 @@ __device__ __forceinline__ void codes4_bf16(uint32_t b, uint32_t &o0, uint32_t &
 // 8 values in 32 bits as P bfloat16 pieces each, the largest first: rounded where there is one; else each piece
 // cuts off 8 bits and the next takes what is left, so that three hold a 32-bit value exactly.  An infinity
 // stays one in its first piece, and its others are zero.
-template <int P>
-__device__ __forceinline__ void split8(const float (&v)[8], uint32_t (&o)[P][4]) {
+// put(p, words) takes a piece at a time.
+template <int P, class Put>
+__device__ __forceinline__ void split8(const float (&v)[8], const Put &put) {
+  uint32_t o[4];
   if constexpr (P == 1) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[0][i] = pack2<__nv_bfloat16>(v[2 * i], v[2 * i + 1]);
+    for (int i = 0; i < 4; ++i) o[i] = pack2<__nv_bfloat16>(v[2 * i], v[2 * i + 1]);
+    put(0, o);
   } else {
     uint32_t x[8];
 #pragma unroll
@@ -124,7 +127,8 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint32_t (&o)[P][4])
 #pragma unroll
     for (int p = 0; p < P; ++p) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[p][i] = __byte_perm(x[2 * i], x[2 * i + 1], 0x7632);
+      for (int i = 0; i < 4; ++i) o[i] = __byte_perm(x[2 * i], x[2 * i + 1], 0x7632);
+      put(p, o);
       if (p + 1 < P) {
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -137,10 +141,7 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint32_t (&o)[P][4])
 }
 template <int P>
 __device__ __forceinline__ void store_split8(const float (&v)[8], uint32_t addr, uint32_t piece_bytes) {
-  uint32_t o[P][4];
-  split8<P>(v, o);
-#pragma unroll
-  for (int p = 0; p < P; ++p) st_shared16(addr + p * piece_bytes, o[p][0], o[p][1], o[p][2], o[p][3]);
+  split8<P>(v, [&](int p, const uint32_t (&o)[4]) { st_shared16(addr + p * piece_bytes, o[0], o[1], o[2], o[3]); });
 }
 
 // ----------------------------------------------------------------------------- operands
@@ -153,20 +154,42 @@ __device__ __forceinline__ void store_split8(const float (&v)[8], uint32_t addr,
 // mix16).  The forward product's operands span two steps: the first takes k = 0 .. 3 and 8 .. 11 of every 16 k, the
 // second the others, so that a load is 16 bytes of codes and a row's 128 bytes are one line.
 
-// 2-bit weights at p, 4 W bytes, `left` weights in range (a multiple of 4).  unit: 16, 8 or 4 bytes that every
-// row is a multiple of, or 1
+// 4 W bytes at any p, of which the first `left` are in range, the others zeros: aligned words that hold any of them, shifted.
+// An array lies in [base, limit): a word that reaches out of it (at its very ends) is read byte by byte.
 template <int W>
-__device__ __forceinline__ void load_weights(const uint8_t *p, int left, int unit, uint32_t (&w)[W]) {
+__device__ __forceinline__ void load_bytes(const void *at, int left, const void *base, const void *limit, uint32_t *w) {
 #pragma unroll
   for (int i = 0; i < W; ++i) w[i] = 0;
-  if (unit >= 4) {
+  if (left <= 0) return;
+  const uint8_t *p = static_cast<const uint8_t *>(at);
+  const int n = left < 4 * W ? left : 4 * W, off = static_cast<int>(reinterpret_cast<uintptr_t>(p) & 3);
+  const uint8_t *a = p - off;
+  if (a >= static_cast<const uint8_t *>(base) && a + ((off + n + 3) & ~3) <= static_cast<const uint8_t *>(limit)) {
+    uint32_t v[W + 1];
 #pragma unroll
-    for (int i = 0; i < W; ++i)
-      if (16 * i < left) w[i] = __ldg(reinterpret_cast<const uint32_t *>(p) + i);
+    for (int i = 0; i <= W; ++i) v[i] = 4 * i < off + n ? __ldg(reinterpret_cast<const uint32_t *>(a) + i) : 0u;
+#pragma unroll
+    for (int i = 0; i < W; ++i) {
+      w[i] = __funnelshift_r(v[i], v[i + 1], 8 * off);
+      if (4 * i + 4 > n) w[i] = 4 * i < n ? w[i] & (0xFFFFFFFFu >> (8 * (4 * i + 4 - n))) : 0u;
+    }
   } else {
 #pragma unroll
     for (int b = 0; b < 4 * W; ++b)
-      if (4 * b < left) w[b >> 2] |= static_cast<uint32_t>(__ldg(p + b)) << (8 * (b & 3));
+      if (b < n) w[b >> 2] |= static_cast<uint32_t>(__ldg(p + b)) << (8 * (b & 3));
+  }
+}
+
+// 2-bit weights at p, 4 W bytes, `left` weights in range (a multiple of 4).  unit: 16, 8 or 4 bytes that every
+// row is a multiple of, or 1
+template <int W>
+__device__ __forceinline__ void load_weights(const uint8_t *p, int left, int unit, const uint8_t *base, const uint8_t *limit,
+                                             uint32_t (&w)[W]) {
+  if (unit >= 4) {
+#pragma unroll
+    for (int i = 0; i < W; ++i) w[i] = 16 * i < left ? __ldg(reinterpret_cast<const uint32_t *>(p) + i) : 0u;
+  } else {
+    load_bytes<W>(p, left / 4, base, limit, w);
   }
 }
 
@@ -194,7 +217,7 @@ struct WeightsK {
     t.p += kGroups * kSpan * kStep / 4;
   }
   __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
-    load_weights<4>(t.p, left - t.k, unit, w);
+    load_weights<4>(t.p, left - t.k, unit, packed, packed + (N * K >> 2), w);
     t.p += kGroups * kSpan * kStep / 4;
   }
   __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool second, uint32_t tile) const {
@@ -234,7 +257,7 @@ struct WeightsT {
     t.p += kGroups * kStep / 4 * K;
   }
   __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
-    load_weights<2>(t.p, t.n < left ? t.k : 0, unit, w);
+    load_weights<2>(t.p, t.n < left ? t.k : 0, unit, packed, packed + (N * K >> 2), w);
     t.p += kGroups * kStep / 4 * K;
   }
   __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool, uint32_t tile) const {
@@ -247,22 +270,14 @@ struct WeightsT {
   }
 };
 
-// 16 codes at p, `left` of them in range.  unit: 16 or 4 bytes that every row is a multiple of, or 1
-__device__ __forceinline__ void load_codes(const int8_t *p, int left, int unit, uint32_t *w) {
+// 16 codes at p, `left` of them in range.  unit: 16 or 4 bytes that every row is a multiple of, or 1; the rows lie in
+// [base, limit)
+__device__ __forceinline__ void load_codes(const int8_t *p, int left, int unit, const int8_t *base, const int8_t *limit, uint32_t *w) {
+  if (unit >= 4) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) w[i] = 0;
-  if (left <= 0) return;
-  if (unit == 16) {
-    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p));
-    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-  } else if (unit == 4) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (4 * i < left) w[i] = __ldg(reinterpret_cast<const uint32_t *>(p) + i);
+    for (int i = 0; i < 4; ++i) w[i] = 4 * i < left ? __ldg(reinterpret_cast<const uint32_t *>(p) + i) : 0u;
   } else {
-#pragma unroll
-    for (int i = 0; i < 16; ++i)
-      if (i < left) w[i >> 2] |= (static_cast<uint32_t>(__ldg(p + i)) & 0xFFu) << (8 * (i & 3));
+    load_bytes<4>(p, left, base, limit, w);
   }
 }
 
@@ -280,7 +295,7 @@ struct CodesK {
   static constexpr int kUnits = X >= kPass ? X / kPass : 1;
   static constexpr int kSpan = 2, kRegs = 4 * kUnits;
   const int8_t *codes;
-  int64_t M, ld;
+  int64_t M, K, ld;
   int unit;
   struct Thread {
     const int8_t *p[kUnits];
@@ -309,7 +324,7 @@ struct CodesK {
   __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-      load_codes(t.p[u], left - t.k, unit, w + 4 * u);
+      load_codes(t.p[u], left - t.k, unit, codes, codes + (M - 1) * ld + K, w + 4 * u);
       t.p[u] += kGroups * kSpan * kStep;
     }
   }
@@ -331,7 +346,7 @@ struct CodesT {
   static constexpr int kSpan = 1, kRegs = 8;
   static_assert(2 * kPass == kStep, "two passes are a step's tokens");
   const int8_t *codes;
-  int64_t K, ld;
+  int64_t M, K, ld;
   int unit;
   struct Thread {
     const int8_t *p;
@@ -355,7 +370,7 @@ struct CodesT {
   }
   __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) load_codes(t.p + u * kPass * ld, t.m + u * kPass < left ? t.k : 0, unit, w + 4 * u);
+    for (int u = 0; u < 2; ++u) load_codes(t.p + u * kPass * ld, t.m + u * kPass < left ? t.k : 0, unit, codes, codes + (M - 1) * ld + K, w + 4 * u);
     t.p += kGroups * kStep * ld;
   }
   __device__ __forceinline__ void store(const Thread &t, const uint32_t (&w)[kRegs], bool, uint32_t tile) const {
@@ -376,25 +391,21 @@ struct CodesT {
 template <typename T>
 constexpr int kWords8 = sizeof(T) == 4 ? 8 : 4;
 template <typename T>
-__device__ __forceinline__ void load_grad8(const T *p, int left, bool vec, uint32_t *w) {
-#pragma unroll
-  for (int i = 0; i < kWords8<T>; ++i) w[i] = 0;
-  if (left <= 0) return;
+__device__ __forceinline__ void load_grad8(const T *p, int left, bool vec, const T *base, const T *limit, uint32_t *w) {
   if (vec) {
-    const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p));
-    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
-    if constexpr (sizeof(T) == 4) {
-      const uint4 u = __ldg(reinterpret_cast<const uint4 *>(p) + 1);
-      w[4] = u.x, w[5] = u.y, w[6] = u.z, w[7] = u.w;
+#pragma unroll
+    for (int i = 0; i < kWords8<T>; ++i) w[i] = 0;
+    if (left <= 0) return;
+#pragma unroll
+    for (int i = 0; i < kWords8<T> / 4; ++i) {
+      const uint4 v = __ldg(reinterpret_cast<const uint4 *>(p) + i);
+      w[4 * i] = v.x, w[4 * i + 1] = v.y, w[4 * i + 2] = v.z, w[4 * i + 3] = v.w;
     }
   } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < left) w[i] = __ldg(reinterpret_cast<const uint32_t *>(p) + i);
+    for (int i = 0; i < 8; ++i) w[i] = i < left ? __ldg(reinterpret_cast<const uint32_t *>(p) + i) : 0u;
   } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < left) w[i >> 1] |= static_cast<uint32_t>(__ldg(reinterpret_cast<const uint16_t *>(p) + i)) << (16 * (i & 1));
+    load_bytes<4>(p, left < 8 ? 2 * left : 16, base, limit, w);
   }
 }
 template <typename T>
@@ -425,7 +436,7 @@ struct GradK {
   static constexpr int kUnits = X / kPass;
   static constexpr int kSpan = 1, kRegs = kWords8<T> * kUnits;
   const T *dy;
-  int64_t M, ld;
+  int64_t M, N, ld;
   bool vec;
   struct Thread {
     const T *p[kUnits];
@@ -453,7 +464,7 @@ struct GradK {
   __device__ __forceinline__ void load(Thread &t, int left, uint32_t (&w)[kRegs]) const {
 #pragma unroll
     for (int u = 0; u < kUnits; ++u) {
-      load_grad8<T>(t.p[u], left - t.n, vec, w + kWords8<T> * u);
+      load_grad8<T>(t.p[u], left - t.n, vec, dy, dy + (M - 1) * ld + N, w + kWords8<T> * u);
       t.p[u] += kGroups * kStep;
     }
   }
@@ -481,7 +492,7 @@ struct GradT {
   static constexpr int kPieces = X / 64;
   static constexpr int kSpan = 1, kRegs = 2 * kWords8<T> * kPieces + 2;
   const T *dy;
-  int64_t N, ld;
+  int64_t M, N, ld;
   const float *scale;
   bool vec;
   struct Thread {
@@ -514,7 +525,8 @@ struct GradT {
       w[kRegs - 2 + h] = live ? __float_as_uint(__ldg(t.s + h * kPass)) : 0u;
 #pragma unroll
       for (int u = 0; u < kPieces; ++u)
-        load_grad8<T>(t.p + h * kPass * ld + 64 * u, live ? t.columns - 64 * u : 0, vec, w + kWords8<T> * (h * kPieces + u));
+        load_grad8<T>(t.p + h * kPass * ld + 64 * u, live ? t.columns - 64 * u : 0, vec, dy, dy + (M - 1) * ld + N,
+                      w + kWords8<T> * (h * kPieces + u));
     }
     t.p += kGroups * kStep * ld, t.s += kGroups * kStep;
   }
@@ -581,17 +593,17 @@ struct OutW {  // dW[n][k] = v
   __device__ __forceinline__ float factor(int64_t) const { return 1.0f; }
   __device__ __forceinline__ float add(int64_t) const { return 0.0f; }
 };
-// The CTA's accumulators, 32 lanes of i by kColumns of j a warp: to y (rows of j, `ld` apart), times the
+// The CTA's sums (get(c, v): columns c .. of a lane), 32 lanes of i by kColumns of j a warp: to y (rows of j, `ld` apart), times the
 // column's factor, plus the lane's `add`
-template <typename T, int kColumns>
-__device__ __forceinline__ void put_tile(T *y, int64_t ld, int columns, bool live, uint32_t tmem, const float *factor, float add) {
+template <typename T, int kColumns, bool REGISTERS, class Get>
+__device__ __forceinline__ void put_tile(T *y, int64_t ld, int columns, bool live, const Get &get, const float *factor, float add) {
   constexpr int kGroup = kColumns < 16 ? kColumns : 16;
   static_assert(kColumns % kGroup == 0 && kGroup >= 4, "columns of a warp");
-#pragma unroll 1
-  for (int c = 0; c < kColumns && c < columns; c += kGroup) {
+#pragma unroll(REGISTERS ? kColumns : 1)
+  for (int c = 0; c < kColumns; c += kGroup) {
+    if (c >= columns) break;
     float v[kGroup];
-    tmem_ld<kGroup>(tmem + c, v);
-    tmem_wait_ld();
+    get(c, v);
     if (!live) continue;
 #pragma unroll
     for (int e = 0; e < kGroup; ++e) {
@@ -618,7 +630,8 @@ struct GemmArgs {
   int stages;
   int dependent;       // launched before the kernel before it was over
   int parts;           // splits that are one cluster and join in shared memory (CG = 1), else 1
-  float *partial;      // [splits][J][I] where several join in a second kernel, else NULL
+  bool joins;          // the splits' sums join in a second kernel
+  float *partial;      // [splits][J][I] where they do, or where a part of R is in chunks (kCarry)
   int *err;            // set to 1 by a wait that gave up
 };
 
@@ -634,18 +647,24 @@ struct GemmShape {
   // the MMAs of its narrower step)
   static constexpr int kSteps = CG == 1 ? A::kSpan : 1;
   static constexpr uint32_t kStageBytes = kSteps * kStepBytes;
+  // Three pieces carry 32-bit operands, and the tensor cores' 32-bit additions cut off what does not fit: each one
+  // loses up to 2^-23 of the sum (4e-6 in all over 96 of them, measured).  So such sums are kept in parts: the lower
+  // pieces' in one (2^-8 of the size), the first pieces' in kSets - 1 in turn, each over kChunk steps at most, then
+  // added in registers: 28 additions to a part at most.
+  static constexpr int kSets = B::P == 3 ? 4 : 1;
+  static constexpr int kChunk = 20;  // a multiple of the producers' groups
+  static constexpr uint32_t kTmemCols = TB * kSets < 32 ? 32 : TB * kSets;
   static constexpr uint32_t kBars = 256 + TB * 4;  // barriers and two words; the columns' factors
   static constexpr int kMaxStages = 8;
   static constexpr int fit(uint32_t room) { return static_cast<int>((room - kBars) / kStageBytes); }
   static constexpr uint32_t kHalfSm = kSmemPerSm / 2 - 1024;
-  static constexpr int kCtasPerSm = fit(kHalfSm) >= 2 ? 2 : 1;
+  static constexpr int kCtasPerSm = fit(kHalfSm) >= 2 && 2 * kTmemCols <= 512 ? 2 : 1;
   // stages of a CTA that has half of an SM, or all of one
   static constexpr int stages(bool half) {
     const int n = half ? fit(kHalfSm) : fit(kMaxDynSmem);
     return n < kMaxStages ? n : kMaxStages;
   }
   static constexpr uint32_t smem(int stages) { return stages * kStageBytes + kBars; }
-  static constexpr uint32_t kTmemCols = TB < 32 ? 32 : TB;
   static_assert(stages(kCtasPerSm == 2) >= 2 && kStageBytes % 16 == 0 && kCtasPerSm * kTmemCols <= 512, "stages and accumulators");
   static_assert(CG == 2 || stages(kCtasPerSm == 2) * kStageBytes >= kTileI * TB * 4, "a cluster joins its tile in the stages");
   static_assert(A::kSpan == B::kSpan, "operands load together");
@@ -662,20 +681,30 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   // wait costs the issuing warp some 200 cycles); empty[stages], done; 2 words
   constexpr uint32_t kB = 8 * S::kMaxStages;
   uint8_t *tail = smem + g.stages * S::kStageBytes;
-  const uint32_t full = smem_u32(tail), empty = full + kB, done = empty + kB;
-  volatile uint32_t *word = reinterpret_cast<volatile uint32_t *>(tail + 2 * kB + 8);
+  const uint32_t full = smem_u32(tail), empty = full + kB, done = empty + kB, drained = done + 8;
+  volatile uint32_t *word = reinterpret_cast<volatile uint32_t *>(tail + 2 * kB + 16);
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
   const uint32_t rank = CG == 2 ? cluster_ctarank() : 0;
-  const int64_t i0 = static_cast<int64_t>(blockIdx.x % g.tiles_i) * kTileI, j0 = static_cast<int64_t>(blockIdx.x / g.tiles_i) * TB;
-  const int64_t first = static_cast<int64_t>(blockIdx.y) * g.steps * kStep;
-  const int64_t end = first + static_cast<int64_t>(g.steps) * kStep < g.R ? first + static_cast<int64_t>(g.steps) * kStep : g.R;
-  const int steps = kSpan * static_cast<int>((end - first + kSpan * kStep - 1) / (kSpan * kStep));
+  // this CTA's tile and part of R.  (In shared memory, and read where they are used: the main loop has no registers
+  // to spare for them.)
+  volatile int64_t *place = reinterpret_cast<volatile int64_t *>(tail + 2 * kB + 24);
+  const auto i0_of = [&]() -> int64_t { return place[0]; };
+  const auto j0_of = [&]() -> int64_t { return place[1]; };
+  const auto first_of = [&]() -> int64_t { return place[2]; };
+  const auto end_of = [&]() -> int64_t { return place[3]; };
+  const auto steps_of = [&] { return static_cast<int>(place[4]); };
 
   if (tid == 0) {
     for (int s = 0; s < g.stages; ++s) mbar_init(full + 8 * s, kGroupWarps + (B::kTma ? 1 : 0) + (CG == 2 && rank == 0 ? 1 : 0)), mbar_init(empty + 8 * s, 1);
     mbar_init(done, 1);
+    mbar_init(drained, CG * kProducerWarps);
     fence_mbar_init_cluster();
     word[1] = 0;
+    const int64_t first = static_cast<int64_t>(blockIdx.y) * g.steps * kStep, whole = static_cast<int64_t>(g.steps) * kStep;
+    const int64_t end = first + whole < g.R ? first + whole : g.R;
+    place[0] = static_cast<int64_t>(blockIdx.x % g.tiles_i) * kTileI, place[1] = static_cast<int64_t>(blockIdx.x / g.tiles_i) * TB;
+    place[2] = first, place[3] = end;
+    place[4] = kSpan * ((end - first + kSpan * kStep - 1) / (kSpan * kStep));
   }
   grid_trigger();
   if (warp == kProducerWarps) {
@@ -701,18 +730,72 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     return true;
   };
 
+  constexpr int kColumns = TB / (kProducerWarps / 4);  // of each of the warps of a lane quadrant
+  // this thread's place in the tile: its row (lane of tensor memory), its warp's first column, i, the columns'
+  // address.  (Computed where it is used: the main loop has no registers to spare for it.)
+  const auto row_of = [] { return static_cast<int>(threadIdx.x & 127); };
+  const auto column_of = [] { return static_cast<int>((threadIdx.x >> 7) & 3) * kColumns; };
+  const auto i_of = [&] {
+    const int r = row_of();
+    return i0_of() + (A::kMixed ? (r & ~15) | mix16(r & 15) : r);
+  };
+  const auto tmem_of = [&] { return tmem + (static_cast<uint32_t>(threadIdx.x & 96) << 16) + column_of(); };
+  const auto carry_of = [&](int c) { return g.partial + (static_cast<int64_t>(blockIdx.y) * g.J + j0_of() + column_of() + c) * g.I + i_of(); };
+  // Three pieces: the sums over the chunks that are over stay in this thread's registers (a pair's CTA, alone on its
+  // SM), or in the part's place of `partial` (half of an SM's registers are too few).
+  constexpr bool kKeep = P == 3 && CG == 2, kCarry = P == 3 && CG == 1;
+  float acc[kKeep ? kColumns : 1];
+  const auto chunks_of = [&] { return P == 3 ? (steps_of() + S::kChunk - 1) / S::kChunk : 1; };
+  bool ready = true;
+  // the n columns from c on of this warp's: the parts of the chunk in tensor memory
+  const auto parts_of = [&](int chunk, int c, auto &v) {
+    constexpr int n = sizeof(v) / sizeof(float);
+    const uint32_t tl = tmem_of();
+    const int left = P == 3 ? steps_of() - chunk * S::kChunk : 0;
+    tmem_ld<n>(tl + c, v);
+    tmem_wait_ld();
+#pragma unroll
+    for (int set = 1; set < S::kSets; ++set) {
+      float u[n];
+      tmem_ld<n>(tl + set * TB + c, u);
+      tmem_wait_ld();
+      // (a chunk of fewer steps than parts has not written them all)
+      const bool used = set == S::kSets - 1 || left > set;
+#pragma unroll
+      for (int e = 0; e < n; ++e) v[e] += used ? u[e] : 0.0f;
+    }
+  };
+  const auto drain = [&](int chunk) {  // (a whole warp)
+    ready = __all_sync(0xffffffffu, wait(done, chunk & 1) && !word[1]);
+    if (!ready) return;
+    tc_fence_after();
+    constexpr int kGroup = kColumns < 16 ? kColumns : 16;
+#pragma unroll(kKeep ? kColumns : 1)
+    for (int c = 0; c < kColumns; c += kGroup) {
+      float v[kGroup];
+      parts_of(chunk, c, v);
+#pragma unroll
+      for (int e = 0; e < kGroup; ++e) {
+        if constexpr (kKeep) {
+          acc[c + e] = chunk == 0 ? v[e] : acc[c + e] + v[e];
+        } else if (i_of() < g.I && j0_of() + column_of() + c + e < g.J) {
+          float *o = carry_of(c + e);
+          *o = chunk == 0 ? v[e] : *o + v[e];
+        }
+      }
+    }
+    tc_fence_before();
+    __syncwarp();
+    if (lane == 0) {
+      if constexpr (CG == 2) mbar_arrive_peer(mapa_cluster(drained, 0));
+      else mbar_arrive(drained);
+    }
+  };
   float *factor = reinterpret_cast<float *>(tail + 256);
-  for (int c = tid; c < TB; c += kGemmThreads) factor[c] = g.partial ? 1.0f : j0 + c < g.J ? g.out.factor(j0 + c) : 0.0f;
+  for (int c = tid; c < TB; c += kGemmThreads) factor[c] = g.joins ? 1.0f : j0_of() + c < g.J ? g.out.factor(j0_of() + c) : 0.0f;
   if (warp < kProducerWarps) {
     const int group = warp / kGroupWarps, at = tid - group * kGroupWarps * 32;
     constexpr int kSpanR = kSpan * kStep;
-    typename A::Thread ta = g.a.init(i0, first + group * kSpanR, at);
-    uint32_t ra[A::kRegs];
-    int left = static_cast<int>(end - first) - group * kSpanR;
-    const auto load_a = [&] {
-      if (left >= g.full) g.a.full(ta, ra);
-      else g.a.load(ta, left, ra);
-    };
     const auto skip = [&](int &s, uint32_t &parity, int by) {
       s += by;
       if (s >= g.stages) s -= g.stages, parity ^= 1;
@@ -720,38 +803,69 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     int s = 0;
     uint32_t parity = 1;  // (a stage's first wait is for the phase before its first, and over at once)
     skip(s, parity, group * (kSpan / S::kSteps));
-    // the group's spans: `load` the next one's B, `store` the step's
-    const auto produce = [&](const auto &load_b, const auto &store_b) {
-      load_a(), load_b(left);
-      left -= kGroups * kSpanR;
-      for (int it = group * kSpan; it < steps; it += kGroups * kSpan) {
-#pragma unroll
-        for (int h = 0; h < kSpan; ++h) {
-          const bool opens = h % S::kSteps == 0, closes = h % S::kSteps == S::kSteps - 1;
-          if (opens && !__all_sync(0xffffffffu, wait(empty + 8 * s, parity))) return;
-          const uint32_t tile = base + s * S::kStageBytes + h % S::kSteps * S::kStepBytes;
-          g.a.store(ta, ra, h == 1, tile + B::P * S::kPieceBytes);
-          store_b(h == 1, tile);
-          if (closes) {
-            __syncwarp();
-            if (lane == 0) mbar_arrive(full + 8 * s);
-            skip(s, parity, 1);
+    int chunk = 0;
+    // the group's spans among `steps` from `first` on: `load` the next one's, `store` the step's
+    const auto produce = [&](int64_t first, int64_t end, int steps) {
+      typename A::Thread ta = g.a.init(i0_of(), first + group * kSpanR, at);
+      uint32_t ra[A::kRegs];
+      int left = static_cast<int>(end - first) - group * kSpanR;
+      const auto spans = [&](const auto &load_b, const auto &store_b) {
+        const auto load = [&] {
+          if (left >= g.full) g.a.full(ta, ra);
+          else g.a.load(ta, left, ra);
+          load_b(left);
+          left -= kGroups * kSpanR;
+        };
+        load();
+        for (int it = group * kSpan; it < steps; it += kGroups * kSpan) {
+          if (kKeep && it >= (chunk + 1) * S::kChunk) {
+            drain(chunk++);
+            if (!ready) return;
           }
+#pragma unroll
+          for (int h = 0; h < kSpan; ++h) {
+            const bool opens = h % S::kSteps == 0, closes = h % S::kSteps == S::kSteps - 1;
+            if (opens && !__all_sync(0xffffffffu, wait(empty + 8 * s, parity))) return;
+            const uint32_t tile = base + s * S::kStageBytes + h % S::kSteps * S::kStepBytes;
+            g.a.store(ta, ra, h == 1, tile + B::P * S::kPieceBytes);
+            store_b(h == 1, tile);
+            if (closes) {
+              __syncwarp();
+              if (lane == 0) mbar_arrive(full + 8 * s);
+              skip(s, parity, 1);
+            }
+          }
+          load();
+          skip(s, parity, (kGroups - 1) * (kSpan / S::kSteps));
         }
-        load_a(), load_b(left);
-        left -= kGroups * kSpanR;
-        skip(s, parity, (kGroups - 1) * (kSpan / S::kSteps));
+      };
+      if constexpr (B::kTma) {
+        spans([](int) {}, [](bool, uint32_t) {});
+      } else {
+        typename B::Thread tb = g.b.init(j0_of() + rank * (TB / CG), first + group * kSpanR, at);
+        uint32_t rb[B::kRegs];
+        spans([&](int left) {
+          if (left >= g.full) g.b.full(tb, rb);
+          else g.b.load(tb, left, rb);
+        }, [&](bool second, uint32_t tile) { g.b.store(tb, rb, second, tile); });
       }
     };
-    if constexpr (B::kTma) {
-      produce([](int) {}, [](bool, uint32_t) {});
+    if constexpr (kCarry) {
+      // a chunk at a time, from its own first loads on: the other CTA of the SM has the meantime
+      for (;; drain(chunk++)) {
+        if (!ready) break;
+        const int64_t from = first_of() + static_cast<int64_t>(chunk) * (S::kChunk * kStep), to = from + S::kChunk * kStep;
+        const int64_t end = end_of();
+        const int steps = steps_of() - chunk * S::kChunk;
+        produce(from, to < end ? to : end, steps < S::kChunk ? steps : S::kChunk);
+        if (chunk + 1 >= chunks_of()) break;
+      }
     } else {
-      typename B::Thread tb = g.b.init(j0 + rank * (TB / CG), first + group * kSpanR, at);
-      uint32_t rb[B::kRegs];
-      produce([&](int left) {
-        if (left >= g.full) g.b.full(tb, rb);
-        else g.b.load(tb, left, rb);
-      }, [&](bool second, uint32_t tile) { g.b.store(tb, rb, second, tile); });
+      produce(first_of(), end_of(), steps_of());
+    }
+    if constexpr (kKeep) {
+      // (a group's last step may lie in an earlier chunk than the other's)
+      while (ready && chunk < chunks_of()) drain(chunk++);
     }
     named_bar_sync(1, kProducers);  // (the factors)
   } else if (warp == kProducerWarps) {
@@ -766,7 +880,17 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     const uint32_t full0 = CG == 2 ? mapa_cluster(full, 0) : full;
     int s = 0;
     uint32_t parity = 0;
-    for (int it = 0; it < steps; it += S::kSteps) {
+    const int steps = steps_of();
+    for (int it = 0, in = 0, chunk = 0; it < steps; it += S::kSteps, ++in) {  // in: steps of the chunk
+      if (P == 3 && in == S::kChunk) {
+        in = 0;
+        if (rank == 0) {
+          mma_commit_cg_warp<CG>(done);
+          if (!__all_sync(0xffffffffu, wait(drained, chunk & 1))) break;
+          tc_fence_after();
+        }
+        ++chunk;
+      }
       if (!__all_sync(0xffffffffu, wait(full + 8 * s, parity))) break;
       fence_proxy_async_smem();
       if (rank == 0) {
@@ -776,10 +900,13 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
         for (int u = 0; u < S::kSteps; ++u) {
           const uint32_t off = (s * S::kStageBytes + u * S::kStepBytes) >> 4;
 #pragma unroll
-          for (int p = 0; p < P; ++p)
-            mma_f16_x4_warp<CG, ka, kb>(tmem, static_cast<uint32_t>(a0) + off, static_cast<uint32_t>(a0 >> 32),
-                                                   static_cast<uint32_t>(b0) + off + (p * S::kPieceBytes >> 4),
-                                                   static_cast<uint32_t>(b0 >> 32), idesc, it > 0 || u > 0 || p > 0 ? 1u : 0u);
+          for (int p = 0; p < P; ++p) {
+            const uint32_t set = P != 3 ? 0u : p > 0 ? S::kSets - 1u : static_cast<uint32_t>(in) % (S::kSets - 1u);
+            const bool first = P != 3 ? it == 0 && u == 0 && p == 0 : p == 1 ? in == 0 : p == 0 && in < S::kSets - 1;
+            mma_f16_x4_warp<CG, ka, kb>(tmem + set * TB, static_cast<uint32_t>(a0) + off, static_cast<uint32_t>(a0 >> 32),
+                                        static_cast<uint32_t>(b0) + off + (p * S::kPieceBytes >> 4), static_cast<uint32_t>(b0 >> 32), idesc,
+                                        first ? 0u : 1u);
+          }
         }
         mma_commit_cg_warp<CG>(empty + 8 * s);
       } else {
@@ -790,7 +917,8 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     }
     if (rank == 0) mma_commit_cg_warp<CG>(done);
   } else if constexpr (B::kTma) {
-    const int64_t x0 = j0 + rank * (TB / CG);
+    const int64_t x0 = j0_of() + rank * (TB / CG), first = first_of();
+    const int steps = steps_of();
     int s = 0, it = 0;
     uint32_t parity = 1;
     for (; it < steps; ++it) {
@@ -808,29 +936,41 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
         for (int tries = 0; !mbar_try_wait(full + 8 * (k % g.stages), (k / g.stages) & 1) && tries < kGemmWaitTries; ++tries) {}
   }
   __syncwarp();
-  const bool ready = __all_sync(0xffffffffu, wait(done, 0) && !word[1]);
+  if constexpr (!kKeep) ready = __all_sync(0xffffffffu, ready && wait(done, (chunks_of() - 1) & 1) && !word[1]);
   tc_fence_after();
-  const int row = 32 * (warp & 3) + lane;  // of the tile, and the lane of tensor memory
-  const int64_t i = i0 + (A::kMixed ? (row & ~15) | mix16(row & 15) : row);
-  constexpr int kColumns = TB / (kProducerWarps / 4);  // of each of the warps of a lane quadrant
-  const int c0 = ((warp >> 2) & 3) * kColumns;
-  const uint32_t tl = tmem + (static_cast<uint32_t>(32 * (warp & 3)) << 16) + c0;
+  const int64_t i = i_of(), j0 = j0_of();
+  const int row = row_of(), c0 = column_of(), chunks = chunks_of();
+  // columns c .. of this warp's, whole
+  const auto columns_of = [&](int c, auto &v) {
+    constexpr int n = sizeof(v) / sizeof(float);
+    if constexpr (kKeep) {
+#pragma unroll
+      for (int e = 0; e < n; ++e) v[e] = acc[c + e];
+    } else {
+      parts_of(chunks - 1, c, v);
+      if (kCarry && chunks > 1 && i < g.I) {
+#pragma unroll
+        for (int e = 0; e < n; ++e)
+          if (j0 + c0 + c + e < g.J) v[e] += *carry_of(c + e);
+      }
+    }
+  };
   if (CG == 1 && g.parts > 1) {
     // A cluster's CTAs hold sums over parts of R.  Each joins TB / parts of the columns: the others send theirs to
     // its shared memory (the stages, once every CTA is done with its own), and it adds them in the parts' order.
     const int part = blockIdx.y, mine = TB / g.parts;
+    const bool any = steps_of() > 0;
     cluster_sync_all();
     if (warp < kProducerWarps && ready) {
       constexpr int kGroup = kColumns < 16 ? kColumns : 16;
-#pragma unroll 1
+#pragma unroll(kKeep ? kColumns : 1)
       for (int c = 0; c < kColumns; c += kGroup) {
         float v[kGroup];
-        tmem_ld<kGroup>(tl + c, v);
-        tmem_wait_ld();
+        columns_of(c, v);
 #pragma unroll
         for (int e = 0; e < kGroup; ++e) {
           const int to = (c0 + c + e) / mine, at = part * mine + (c0 + c + e) - to * mine;
-          st_cluster_f32(mapa_cluster(base + 4u * (at * kTileI + row), to), steps > 0 ? v[e] : 0.0f);
+          st_cluster_f32(mapa_cluster(base + 4u * (at * kTileI + row), to), any ? v[e] : 0.0f);
         }
       }
     }
@@ -849,13 +989,13 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
   } else if (warp < kProducerWarps && ready) {
     const int columns = rows_left(g.J - j0 - c0);
     const bool live = i < g.I;
-    const float add = !g.partial && live ? g.out.add(i) : 0.0f;
+    const float add = !g.joins && live ? g.out.add(i) : 0.0f;
     const int64_t at = (j0 + c0) * g.out.ld + i;
-    if (g.partial)
-      put_tile<float, kColumns>(g.partial + (static_cast<int64_t>(blockIdx.y) * g.J + j0 + c0) * g.I + i, g.I, columns, live, tl, factor + c0, 0.0f);
-    else if (g.out.dtype == 0) put_tile<float, kColumns>(static_cast<float *>(g.out.y) + at, g.out.ld, columns, live, tl, factor + c0, add);
-    else if (g.out.dtype == 1) put_tile<__half, kColumns>(static_cast<__half *>(g.out.y) + at, g.out.ld, columns, live, tl, factor + c0, add);
-    else put_tile<__nv_bfloat16, kColumns>(static_cast<__nv_bfloat16 *>(g.out.y) + at, g.out.ld, columns, live, tl, factor + c0, add);
+    if (g.joins)
+      put_tile<float, kColumns, kKeep>(carry_of(0), g.I, columns, live, columns_of, factor + c0, 0.0f);
+    else if (g.out.dtype == 0) put_tile<float, kColumns, kKeep>(static_cast<float *>(g.out.y) + at, g.out.ld, columns, live, columns_of, factor + c0, add);
+    else if (g.out.dtype == 1) put_tile<__half, kColumns, kKeep>(static_cast<__half *>(g.out.y) + at, g.out.ld, columns, live, columns_of, factor + c0, add);
+    else put_tile<__nv_bfloat16, kColumns, kKeep>(static_cast<__nv_bfloat16 *>(g.out.y) + at, g.out.ld, columns, live, columns_of, factor + c0, add);
   }
   tc_fence_before();
   if constexpr (CG == 2) cluster_sync_all();
@@ -923,8 +1063,13 @@ GemmPlan gemm_plan(int64_t I, int64_t J, int64_t R, int sms) {
   p.splits = p.cluster ? static_cast<int>(splits) : static_cast<int>((all + p.steps - 1) / p.steps);
   return p;
 }
-// floats of workspace that the splits' sums take
-inline int64_t partial_floats(const GemmPlan &p, int64_t I, int64_t J) { return p.splits > 1 && !p.cluster ? p.splits * I * J : 0; }
+// floats of workspace that the splits' sums take, or those of their chunks
+template <class A, class B, int TB, int CG>
+int64_t partial_floats(int64_t I, int64_t J, int64_t R, int sms) {
+  const GemmPlan p = gemm_plan<A, B, TB, CG>(I, J, R, sms);
+  const bool carries = B::P == 3 && CG == 1 && p.steps > GemmShape<A, B, TB, CG>::kChunk;
+  return (p.splits > 1 && !p.cluster) || carries ? p.splits * I * J : 0;
+}
 
 template <class A, class B, class Out, int TB, int CG>
 cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b, const Out &out, float *partial, int sms, int *err,
@@ -935,7 +1080,7 @@ cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b,
   const int stages = S::stages(S::kCtasPerSm == 2 && ctas > sms);
   const GemmArgs<A, B, Out> g = {I, J, R, a, b, out, static_cast<int>(p.tiles_i), p.steps,
                                    a.aligned() && b.aligned() ? A::kSpan * kStep : INT_MAX, stages, dependent ? 1 : 0, p.cluster ? p.splits : 1,
-                                   p.splits > 1 && !p.cluster ? partial : nullptr, err};
+                                   p.splits > 1 && !p.cluster, partial, err};
   auto *kernel = gemm_kernel<A, B, Out, TB, CG>;
   static std::atomic<uint64_t> allowed{0};  // devices on which the kernel may use its shared memory
   int dev = 0;
@@ -958,7 +1103,7 @@ cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b,
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = dependent ? 2 : 1;
-  if ((e = cudaLaunchKernelEx(&cfg, kernel, g)) != cudaSuccess || !g.partial) return e;
+  if ((e = cudaLaunchKernelEx(&cfg, kernel, g)) != cudaSuccess || !g.joins) return e;
   const int64_t blocks = (I * J + 255) / 256, most = static_cast<int64_t>(sms) * 32;
   return launch_dependent(gemm_join_kernel<Out>, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), 256, 0, st,
                           static_cast<const float *>(partial), p.splits, I, J, out);
@@ -968,6 +1113,8 @@ cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b,
 // pairs 16.7 us, 128 single ones 12.7 us; 1,024 x 4,096 x 4,096: 128 in pairs 46 us, 256 single ones 58 us), else a
 // single CTA's, of 64 j at most where there are no more (the rest of a tile would be converted zeros) or three pieces of
 // more would leave an SM one CTA, of 128.
+template <int P>
+constexpr int kPairTile = P == 3 ? 128 : 256;  // j of a pair's tile: three pieces' sums take four parts of tensor memory
 inline bool pair_tiles(int64_t I, int64_t J, int sms) {
   return I > kTileI && J > kTileI && 2 * ((I + 255) / 256 * 2) * ((J + 255) / 256) >= sms;
 }

@@ -13,7 +13,7 @@ namespace {
 template <typename T>
 constexpr int kPieces = sizeof(T) == 4 ? 3 : 1;
 template <typename T>
-using Staged = Tiled<128, false, !std::is_same_v<T, __half>, kPieces<T>, 1>;
+using Staged = Tiled<kPairTile<kPieces<T>> / 2, false, !std::is_same_v<T, __half>, kPieces<T>, 1>;
 template <typename T>
 using Weights = WeightsT<!std::is_same_v<T, __half>>;
 
@@ -45,12 +45,12 @@ cudaError_t input_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t s
     }
     if ((e = tensor_map(&b.map, rows, Staged<T>::kBf, c.N, c.M, ld, kPieces<T>, Staged<T>::X)) != cudaSuccess) return e;
     float *partial = reinterpret_cast<float *>(work + 2 * kPieces<T> * c.M * padded(c.N));
-    return launch_gemm<Weights<T>, Staged<T>, OutX, 256, 2>(c.K, c.M, c.N, a, b, out, partial, sms, wait_status(), staged, st);
+    return launch_gemm<Weights<T>, Staged<T>, OutX, kPairTile<kPieces<T>>, 2>(c.K, c.M, c.N, a, b, out, partial, sms, wait_status(), staged, st);
   }
   return with_single_tile<kPieces<T>>(c.M, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
     using B = GradK<T, TB>;
-    const B b = {static_cast<const T *>(c.dy), c.M, c.lddy, grads_vec<T>(c.dy, c.lddy, c.N)};
+    const B b = {static_cast<const T *>(c.dy), c.M, c.N, c.lddy, grads_vec<T>(c.dy, c.lddy, c.N)};
     return launch_gemm<Weights<T>, B, OutX, TB, 1>(c.K, c.M, c.N, a, b, out, reinterpret_cast<float *>(work), sms, wait_status(), false, st);
   });
 }
@@ -58,10 +58,10 @@ cudaError_t input_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t s
 template <typename T>
 int64_t input_grad_workspace(int64_t M, int64_t K, int64_t N) {
   const int sms = sm_count();
-  if (pair_tiles(K, M, sms)) return partial_floats(gemm_plan<Weights<T>, Staged<T>, 256, 2>(K, M, N, sms), K, M) * kFloat + 2 * kPieces<T> * M * padded(N);
+  if (pair_tiles(K, M, sms)) return partial_floats<Weights<T>, Staged<T>, kPairTile<kPieces<T>>, 2>(K, M, N, sms) * kFloat + 2 * kPieces<T> * M * padded(N);
   return with_single_tile<kPieces<T>>(M, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
-    return partial_floats(gemm_plan<Weights<T>, GradK<T, TB>, TB, 1>(K, M, N, sms), K, M) * kFloat;
+    return partial_floats<Weights<T>, GradK<T, TB>, TB, 1>(K, M, N, sms) * kFloat;
   });
 }
 

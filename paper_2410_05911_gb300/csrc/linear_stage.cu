@@ -24,7 +24,7 @@ __global__ void __launch_bounds__(kStageThreads) stage_codes_kernel(const int8_t
     const int64_t m = i / pieces;
     const int c = static_cast<int>(i - m * pieces), left = K - 16 * c;
     uint32_t w[4], o[4];
-    load_codes(codes + m * ld + 16 * c, left, left < 16 && unit == 16 ? 4 : unit, w);
+    load_codes(codes + m * ld + 16 * c, left, unit, codes, codes + (M - 1) * ld + K, w);
     __half *to = out + m * Kp + (c >> 3) * 128 + (c & 7) * 8;
     codes8_half(w[0], w[2], o);
     *reinterpret_cast<uint4 *>(to) = make_uint4(o[0], o[1], o[2], o[3]);
@@ -50,7 +50,7 @@ __global__ void __launch_bounds__(kStageThreads) stage_grads_kernel(const T *dy,
   for (int64_t m = static_cast<int64_t>(blockIdx.y) * 8 + warp; m < M; m += 8 * static_cast<int64_t>(gridDim.y)) {
     uint32_t w[kWords8<T>];
     float v[8];
-    load_grad8<T>(dy + m * ld + n, left, vec, w);
+    load_grad8<T>(dy + m * ld + n, left, vec, dy, dy + (M - 1) * ld + N, w);
     grad8_f32<T>(w, v);
 #pragma unroll
     for (int e = 0; e < 8; ++e) sum[e] += v[e];
@@ -64,10 +64,7 @@ __global__ void __launch_bounds__(kStageThreads) stage_grads_kernel(const T *dy,
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[e] *= s;
         }
-        uint32_t o[P][4];
-        split8<P>(v, o);
-#pragma unroll
-        for (int p = 0; p < P; ++p) *reinterpret_cast<uint4 *>(to + p * M * Np) = make_uint4(o[p][0], o[p][1], o[p][2], o[p][3]);
+        split8<P>(v, [&](int p, const uint32_t (&o)[4]) { *reinterpret_cast<uint4 *>(to + p * M * Np) = make_uint4(o[0], o[1], o[2], o[3]); });
       }
     }
   }

@@ -24,27 +24,27 @@ constexpr int64_t kFloat = sizeof(float);
 int64_t sums_bytes(int64_t M, int64_t N) { return up16(static_cast<int64_t>(stage_parts(M, N)) * N * sizeof(float)); }
 
 template <int P>
-using Staged = Tiled<128, true, true, P, 1>;
+using Staged = Tiled<kPairTile<P> / 2, true, true, P, 1>;
 
 template <int P>
 cudaError_t staged_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t st) {
   Staged<P> b;
   const cudaError_t e = tensor_map(&b.map, work, true, c.N, c.M, padded(c.N), P, kStep);
   if (e != cudaSuccess) return e;
-  const CodesT a = {c.codes, c.K, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
+  const CodesT a = {c.codes, c.M, c.K, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
   const OutW out = {c.dw, c.wdtype, c.K};
   float *partial = reinterpret_cast<float *>(work + 2 * P * c.M * padded(c.N));
-  return launch_gemm<CodesT, Staged<P>, OutW, 256, 2>(c.K, c.N, c.M, a, b, out, partial, sm_count(), wait_status(), true, st);
+  return launch_gemm<CodesT, Staged<P>, OutW, kPairTile<P>, 2>(c.K, c.N, c.M, a, b, out, partial, sm_count(), wait_status(), true, st);
 }
 
 template <typename T, int P>
 cudaError_t weight_grad(const AapLinearGradCall &c, uint8_t *work, bool dependent, cudaStream_t st) {
-  const CodesT a = {c.codes, c.K, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
+  const CodesT a = {c.codes, c.M, c.K, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
   const OutW out = {c.dw, c.wdtype, c.K};
   return with_single_tile<P>(c.N, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
     using B = GradT<T, TB, P>;
-    const B b = {static_cast<const T *>(c.dy), c.N, c.lddy, c.scale, grads_vec<T>(c.dy, c.lddy, c.N)};
+    const B b = {static_cast<const T *>(c.dy), c.M, c.N, c.lddy, c.scale, grads_vec<T>(c.dy, c.lddy, c.N)};
     return launch_gemm<CodesT, B, OutW, TB, 1>(c.K, c.N, c.M, a, b, out, reinterpret_cast<float *>(work), sm_count(), wait_status(), dependent, st);
   });
 }
@@ -58,10 +58,10 @@ cudaError_t weight_grad(const AapLinearGradCall &c, uint8_t *work, bool dependen
 template <int P>
 int64_t workspace_of(int64_t M, int64_t K, int64_t N) {
   const int sms = sm_count();
-  if (pair_tiles(K, N, sms)) return partial_floats(gemm_plan<CodesT, Staged<P>, 256, 2>(K, N, M, sms), K, N) * kFloat + 2 * P * M * padded(N);
+  if (pair_tiles(K, N, sms)) return partial_floats<CodesT, Staged<P>, kPairTile<P>, 2>(K, N, M, sms) * kFloat + 2 * P * M * padded(N);
   return with_single_tile<P>(N, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
-    return partial_floats(gemm_plan<CodesT, GradT<float, TB, P>, TB, 1>(K, N, M, sms), K, N) * kFloat;
+    return partial_floats<CodesT, GradT<float, TB, P>, TB, 1>(K, N, M, sms) * kFloat;
   });
 }
 
