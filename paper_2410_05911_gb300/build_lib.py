@@ -19,7 +19,7 @@ BINDING_SOURCE = "torch_binding.cpp"
 SOURCES = ["api.cu", "decoder_kernel.cu", "decoder_kernel_gelu.cu", "decoder_kernel_fp.cu", "decoder_kernel_fp_gelu.cu",
            "decoder_kernel_cap.cu", "decoder_kernel_cap_fp.cu", "selftest.cu", "aap.cu", "spe.cu",
            "norm.cu", "clip.cu", "linear.cu", "linear_grad.cu", "linear_wgrad.cu",
-           "linear_stage.cu"]
+           "linear_stage.cu", "linear_few.cu"]
 HEADERS = ["aecct_internal.h", "sm103_ptx.cuh", "rowtypes.cuh", "linear_gemm.cuh", "decoder_kernel.cuh", os.path.join("..", "..", "include", "aecct.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--fmad=false",
