@@ -629,7 +629,7 @@ struct GemmArgs {
   int full;            // r that are left for a span to be loaded by full(), more than there are without alignment
   int stages;
   int dependent;       // launched before the kernel before it was over
-  int parts;           // splits that are one cluster and join in shared memory (CG = 1), else 1
+  int parts;           // splits that are one cluster and join in shared memory, else 1
   bool joins;          // the splits' sums join in a second kernel
   float *partial;      // [splits][J][I] where they do, or where a part of R is in chunks (kCarry)
   int *err;            // set to 1 by a wait that gave up
@@ -666,7 +666,8 @@ struct GemmShape {
   }
   static constexpr uint32_t smem(int stages) { return stages * kStageBytes + kBars; }
   static_assert(stages(kCtasPerSm == 2) >= 2 && kStageBytes % 16 == 0 && kCtasPerSm * kTmemCols <= 512, "stages and accumulators");
-  static_assert(CG == 2 || stages(kCtasPerSm == 2) * kStageBytes >= kTileI * TB * 4, "a cluster joins its tile in the stages");
+  static constexpr bool kClusters = CG == 1 && TB == 16;  // parts of R may join in a cluster (gemm_plan)
+  static_assert(!kClusters || stages(kCtasPerSm == 2) * kStageBytes >= kTileI * TB * 4, "a cluster joins its tile in the stages");
   static_assert(A::kSpan == B::kSpan, "operands load together");
 };
 
@@ -955,7 +956,7 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
       }
     }
   };
-  if (CG == 1 && g.parts > 1) {
+  if (S::kClusters && g.parts > 1) {
     // A cluster's CTAs hold sums over parts of R.  Each joins TB / parts of the columns: the others send theirs to
     // its shared memory (the stages, once every CTA is done with its own), and it adds them in the parts' order.
     const int part = blockIdx.y, mine = TB / g.parts;
@@ -1037,10 +1038,15 @@ bool grads_vec(const void *dy, int64_t ld, int64_t N) {
 }
 
 // How the sum over R is split where there are fewer tiles than SMs: into as many parts as SMs are left for, of at least
-// kMinSteps steps each.  (Two CTAs to an SM for the parts' sake, or parts of a full grid, lose more in the joining
-// than they gain: 8,192 x 4,096 x 512 46 us whole, 59 us in two parts, 72 in four.)  Up to 8 parts of a single CTA's
-// tiles are a cluster, which joins them itself (a power of two, as it divides the tile's columns); more, or a
-// pair's, leave their sums in memory for a second kernel.
+// kMinSteps steps each, whose sums a second kernel joins.  Two CTAs to an SM for the parts' sake lose more in the joining
+// than they gain (8,192 x 4,096 x 512 46 us whole, 59 us in two parts; 37 x 4,096 x 16,384 20 and 27 us), but not where
+// parts of 32-bit sums are longer than a chunk and stop at its end (dX of 300 x 1,024 x 4,096: 26 us in 3 parts, 23 us in 7;
+// dW of 100,000 x 512 x 512: 445 and 384 us; shorter parts, 23,040 x 128 x 512: 23 us in 19, 26 us in 38).
+//
+// Up to 4 parts of a tile of 16 j are a cluster, which joins them itself: there the second kernel would be an eighth of the time
+// (16 x 4,096 x 4,096: 8.4 and 9.4 us).  Wider tiles are slower so (64 x 4,096 x 4,096: 11.7 us in clusters, 11.1 us without;
+// 300 x 2,048 x 2,048: 17.7 and 13.2 us), and so are clusters of 8, which wait for 8 SMs of one kind
+// (16 x 16,384 x 2,048: 21.9 and 13.0 us).
 struct GemmPlan {
   int64_t tiles_i, tiles_j;
   int splits, steps;
@@ -1052,11 +1058,14 @@ GemmPlan gemm_plan(int64_t I, int64_t J, int64_t R, int sms) {
   GemmPlan p;
   p.tiles_i = (I + CG * kTileI - 1) / (CG * kTileI) * CG, p.tiles_j = (J + TB - 1) / TB;
   const int64_t all = (R + kStep - 1) / kStep;
-  int64_t splits = sms / (p.tiles_i * p.tiles_j);
+  using S = GemmShape<A, B, TB, CG>;
+  const int64_t tiles = p.tiles_i * p.tiles_j;
+  int64_t splits = sms / tiles;
+  if (B::P == 3 && CG == 1 && all > S::kChunk * (splits < 1 ? 1 : splits)) splits = S::kCtasPerSm * static_cast<int64_t>(sms) / tiles;
   if (splits > all / kMinSteps) splits = all / kMinSteps;
   if (splits < 1) splits = 1;
-  p.cluster = CG == 1 && splits > 1 && splits < 16;
-  if (p.cluster) splits = splits >= 8 ? 8 : splits >= 4 ? 4 : 2;
+  p.cluster = S::kClusters && splits > 1 && splits < 8;
+  if (p.cluster) splits = splits >= 4 ? 4 : 2;  // (a power of two, as it divides the tile's columns)
   const int64_t steps = (all + splits - 1) / splits;
   p.steps = static_cast<int>((steps + A::kSpan - 1) / A::kSpan * A::kSpan);
   // (a cluster keeps its parts, the last ones empty where R runs out)
