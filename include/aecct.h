@@ -249,7 +249,9 @@ int aecct_spe_table(const uint8_t *H, int32_t n, int32_t k, int32_t d_spe, int32
  * next, in elements, at least the row's width.  Pointers are aligned to their element; rows that are
  * 16-byte aligned and a multiple of 16 bytes apart are read fastest.  Outputs do not overlap inputs unless
  * said otherwise.  A workspace is used from the call's start on the stream to its end.  Every result is the
- * same bits on every run.
+ * same bits on every run.  All but aecct_clip_gradients have kernels with waits on the device, each with a
+ * limit: OUT_OF_MEMORY where the first call could not allocate their status word on the host, and TIMEOUT, once,
+ * where a wait of an earlier call exceeded its limit (that call's outputs are incomplete).
  */
 #define AECCT_F32 0
 #define AECCT_F16 1
@@ -267,7 +269,8 @@ int aecct_spe_table(const uint8_t *H, int32_t n, int32_t k, int32_t d_spe, int32
  *   values       [rows][d] of dtype: codes_i scale, or NULL.
  * A row that holds a NaN or an infinity gets a scale that is not a number, and codes without meaning.
  * rows == 0 is a no-op.  Errors: INVALID_ARG (rows < 0, d < 1, a leading dimension under d, a dtype not
- * named above, eps < 0 or not finite, a NULL or misaligned pointer), UNSUPPORTED (d > 32768), CUDA. */
+ * named above, eps < 0 or not finite, a NULL or misaligned pointer), UNSUPPORTED (d > 32768), CUDA,
+ * OUT_OF_MEMORY and TIMEOUT. */
 int aecct_rms_quant(const void *x, int64_t ldx, const void *residual, int64_t ldr, const float *gain, int64_t rows,
                     int32_t d, int32_t dtype, float eps, void *sum, int8_t *codes, float *scale, void *values,
                     void *cuda_stream);
@@ -296,8 +299,7 @@ int aecct_rms_quant_backward(const void *dy, int64_t lddy, const void *h, int64_
  *   workspace  aecct_aap_linear_workspace bytes, 16-byte aligned (NULL where that is 0).
  * M == 0 or N == 0 is a no-op.  Errors: INVALID_ARG (a size < 0, K < 4 or not a multiple of 4, ldc < K, a
  * dtype not named above, a NULL or misaligned pointer, a workspace that is too small), UNSUPPORTED (K > 65536, N or
- * M >= 2^31), CUDA, OUT_OF_MEMORY (the first call allocates a status word on the host), and TIMEOUT, once, where a
- * device-side wait of an earlier call exceeded its limit (that call's outputs are incomplete). */
+ * M >= 2^31), CUDA, OUT_OF_MEMORY and TIMEOUT. */
 int aecct_aap_linear_workspace(int64_t M, int64_t K, int64_t N, int64_t *bytes);
 int aecct_aap_linear(const int8_t *codes, int64_t ldc, const float *scale, const uint8_t *packed, const float *w_scale,
                      const float *bias, int64_t M, int64_t K, int64_t N, int32_t dtype, void *y, void *workspace,

@@ -6,7 +6,8 @@
 //   dW[n, k] = sum_m dy[m, n] scale_m q[m, k]      (straight through Ternary)
 //   db[n]    = sum_m dy[m, n]
 //
-// The three products run on the tensor cores (linear_gemm.cuh).  The forward sum is one of integers up to
+// The three products run on the tensor cores (linear_gemm.cuh), a few tokens' forward product in integers
+// (linear_few.cu).  The forward sum is one of integers up to
 // 127 * 65536 < 2^23: exact in 32 bits, and the same however it is split.
 #include <cuda_runtime.h>
 
@@ -29,7 +30,7 @@ bool stages_codes(int64_t N) { return N >= 1536; }
 // The products of so few tokens that reading the weights is the work (linear_few.cu): 1 token 3.6 us, 8.4 us on the
 // tensor cores, 4 tokens 5.3 and 8.6 us at 4,096 x 4,096, 13.6 and 17 us at 16,384 x 4,096; a token more costs 1.5 us there,
 // and next to nothing on the tensor cores.
-constexpr int64_t kFewTokens = 4;
+constexpr int64_t kIntegerTokens = 4;
 
 // the other tiles: 16 tokens where there are no more
 template <class F>
@@ -45,7 +46,7 @@ constexpr int64_t kFloat = sizeof(float);
 // the staged codes, and the splits' sums
 int64_t aap_linear_workspace(int64_t M, int64_t K, int64_t N) {
   const int sms = sm_count();
-  if (M <= kFewTokens) return 0;
+  if (M <= kIntegerTokens) return 0;
   if (pair_tiles(N, M, sms)) {
     if (stages_codes(N)) return partial_floats<WeightsK, Staged, 256, 2>(N, M, K, sms) * kFloat + 2 * M * staged_k(K);
     return partial_floats<WeightsK, CodesK<128>, 256, 2>(N, M, K, sms) * kFloat;
@@ -57,7 +58,7 @@ int64_t aap_linear_workspace(int64_t M, int64_t K, int64_t N) {
 }
 
 cudaError_t launch_aap_linear(const AapLinearCall &c, cudaStream_t st) {
-  if (c.M <= kFewTokens) return launch_aap_linear_few(c, st);
+  if (c.M <= kIntegerTokens) return launch_aap_linear_few(c, st);
   const WeightsK a = {c.packed, c.N, c.K, weights_unit(c.packed, c.K)};
   const OutY out = {c.y, c.dtype, c.N, c.scale, c.w_scale, c.bias};
   const int sms = sm_count();
