@@ -58,7 +58,7 @@ def _link_binding(obj: str) -> None:
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
     tmp = BINDING_PATH + f".tmp{os.getpid()}"
     subprocess.check_call(["g++", "-shared", "-o", tmp, obj, "-L" + OUT_DIR, "-l:libaecct.so", "-L" + lib, "-ltorch_python",
-                           "-ltorch_cpu", "-ltorch", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + lib])
+                           "-ltorch_cpu", "-ltorch_cuda", "-ltorch", "-lc10", "-lc10_cuda", "-Wl,-rpath,$ORIGIN", "-Wl,-rpath," + lib])
     os.replace(tmp, BINDING_PATH)
 
 
