@@ -1053,10 +1053,11 @@ bool grads_vec(const void *dy, int64_t ld, int64_t N) {
 }
 
 // How the sum over R is split where there are fewer tiles than SMs: into as many parts as SMs are left for, of at least
-// kMinSteps steps each, whose sums a second kernel joins.  Two CTAs to an SM for the parts' sake lose more in the joining
-// than they gain (8,192 x 4,096 x 512 46 us whole, 59 us in two parts; 37 x 4,096 x 16,384 20 and 27 us), but not where
-// parts of 32-bit sums are longer than a chunk and stop at its end (dX of 300 x 1,024 x 4,096: 26 us in 3 parts, 23 us in 7;
-// dW of 100,000 x 512 x 512: 445 and 384 us; shorter parts, 23,040 x 128 x 512: 23 us in 19, 26 us in 38).
+// kMinSteps steps each (a pair's, with four times the sums of a single tile: twice as many; dX of 2,048 x 1,024 x 1,024
+// whole 11.4 us, in two parts of 8 steps 18.1 us), whose sums a second kernel joins.  Two CTAs to an SM for the parts'
+// sake lose more in the joining than they gain (8,192 x 4,096 x 512 46 us whole, 59 us in two parts; 37 x 4,096 x 16,384
+// 20 and 27 us), but not where parts of 32-bit sums are longer than a chunk and stop at its end (dX of 2,048 x 512 x
+// 16,384 in single tiles: 249 and 219 us; shorter parts, dW of 23,040 x 128 x 512: 23 us in 19, 26 us in 38).
 //
 // Up to 4 parts of a tile of 16 j are a cluster, which joins them itself: there the second kernel would be an eighth of the time
 // (16 x 4,096 x 4,096: 8.4 and 9.4 us).  Wider tiles are slower so (64 x 4,096 x 4,096: 11.7 us in clusters, 11.1 us without;
@@ -1077,7 +1078,7 @@ GemmPlan gemm_plan(int64_t I, int64_t J, int64_t R, int sms) {
   const int64_t tiles = p.tiles_i * p.tiles_j;
   int64_t splits = sms / tiles;
   if (B::P == 3 && CG == 1 && all > S::kChunk * (splits < 1 ? 1 : splits)) splits = S::kCtasPerSm * static_cast<int64_t>(sms) / tiles;
-  if (splits > all / kMinSteps) splits = all / kMinSteps;
+  if (splits > all / (CG * kMinSteps)) splits = all / (CG * kMinSteps);
   if (splits < 1) splits = 1;
   p.cluster = S::kClusters && splits > 1 && splits < 8;
   if (p.cluster) splits = splits >= 4 ? 4 : 2;  // (a power of two, as it divides the tile's columns)
@@ -1141,6 +1142,16 @@ template <int P>
 constexpr int kPairTile = P == 3 ? 128 : 256;  // j of a pair's tile: three pieces' sums take four parts of tensor memory
 inline bool pair_tiles(int64_t I, int64_t J, int sms) {
   return I > kTileI && J > kTileI && 2 * ((I + 255) / 256 * 2) * ((J + 255) / 256) >= sms;
+}
+// The gradients' products, of any R, also where single tiles would take each SM through many steps: they convert dy for
+// every 128 k, a pair's once for 256, from rows that lie there or are laid out once (kLongSteps single steps an SM: dW of
+// 20,000 x 1,088 x 784 (tokens, K, N) 130 steps, 102 us in single tiles, 65 us in pairs, in 32 bits 292 and 142 us; dX of
+// 1,500 x 1,088 x 784 9 steps, 12.8 and 10.1 us; dW of 5,000 x 512 x 512 8 steps, 13.5 and 17.6 us).  With up to 256 k dy is
+// not read often enough to be laid out (dW of 20,000 x 256 x 1,024: 28 us in single tiles, 36 us in pairs).
+constexpr int64_t kLongSteps = 9;
+inline bool grad_pairs(int64_t I, int64_t J, int64_t R, int sms) {
+  const int64_t steps = ((I + kTileI - 1) / kTileI) * ((J + 127) / 128) * ((R + kStep - 1) / kStep);
+  return pair_tiles(I, J, sms) || (I > 2 * kTileI && J > kTileI && steps >= kLongSteps * sms);
 }
 template <int P, class F>
 auto with_single_tile(int64_t J, const F &f) {

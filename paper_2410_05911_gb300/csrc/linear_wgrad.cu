@@ -58,7 +58,7 @@ cudaError_t weight_grad(const AapLinearGradCall &c, uint8_t *work, bool dependen
 template <int P>
 int64_t workspace_of(int64_t M, int64_t K, int64_t N) {
   const int sms = sm_count();
-  if (pair_tiles(K, N, sms)) return partial_floats<CodesT, Staged<P>, kPairTile<P>, 2>(K, N, M, sms) * kFloat + 2 * P * M * padded(N);
+  if (grad_pairs(K, N, M, sms)) return partial_floats<CodesT, Staged<P>, kPairTile<P>, 2>(K, N, M, sms) * kFloat + 2 * P * M * padded(N);
   return with_single_tile<P>(N, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
     return partial_floats<CodesT, GradT<float, TB, P>, TB, 1>(K, N, M, sms) * kFloat;
@@ -76,7 +76,7 @@ int64_t weight_grad_workspace(int64_t M, int64_t K, int64_t N, int wdtype) {
 cudaError_t launch_weight_grad(const AapLinearGradCall &c, uint8_t *work, bool dependent, cudaStream_t st) {
   const int p = pieces_of(c.M, c.wdtype);
   uint8_t *rest = work + sums_bytes(c.M, c.N);
-  const bool staged = c.dw && pair_tiles(c.K, c.N, sm_count());
+  const bool staged = c.dw && grad_pairs(c.K, c.N, c.M, sm_count());
   if (staged || c.db) {
     const StageGrads s = {c.dy, c.lddy, c.M, c.N, c.dtype, c.scale, staged ? p : 1, staged ? rest : nullptr, c.db, reinterpret_cast<float *>(work), dependent};
     const cudaError_t e = launch_stage_grads(s, st);
