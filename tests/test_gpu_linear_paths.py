@@ -131,3 +131,21 @@ def test_first_call_under_capture_and_on_another_stream():
         assert torch.equal(few, y[:2])
         for got, ref in zip((dx, dw, db), aecct.aap_linear_backward(dy, codes, scale, packed, w_scale)):
             assert torch.equal(got, ref)
+
+
+@pytest.mark.parametrize("M,K,N", [(9000, 388, 261), (9000, 516, 264), (200, 4100, 2100), (260, 2052, 4097)])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_gradients_in_pairs_of_few_tiles(dtype, M, K, N):
+    """Long products of few tiles are split among pairs.  In 32 bits within LONG as above; with 16-bit gradients each
+    factor dy scale of dW is rounded to 8 bits, and R additions lose up to 2^-23 each."""
+    gen = generator(M + K)
+    codes, scale, packed, w_scale, t = random_layer(M, K, N, gen, K + 1)
+    dy = torch.randn((M, N), device="cuda", generator=gen).to(dtype)
+    dx, dw, db = aecct.aap_linear_backward(dy, codes, scale, packed, w_scale, weight_dtype=dtype)
+    d64, q64 = dy.double(), codes.double() * scale.double()[:, None]
+    half = dtype == torch.bfloat16
+    for got, ref, size, R, factor in [(dx, d64 @ t * w_scale.double(), d64.abs() @ t.abs() * w_scale.double(), N, 0.0),
+                                      (dw, d64.T @ q64, d64.abs().T @ q64.abs(), M, 2.0 ** -8)]:
+        bound = (factor + (R + 4) * U32) * size + 2.0 ** -8 * ref.abs() if half else LONG * size
+        assert ((got.double() - ref).abs() <= bound).all()
+    assert ((db.double() - d64.sum(0)).abs() <= 1e-5 * d64.abs().sum(0)).all()
