@@ -368,8 +368,8 @@ int64_t aap_linear_workspace(int64_t M, int64_t K, int64_t N);
 cudaError_t launch_aap_linear(const AapLinearCall &c, cudaStream_t stream);
 cudaError_t launch_aap_linear_few(const AapLinearCall &c, cudaStream_t stream);  // up to 4 tokens
 int64_t weight_grad_workspace(int64_t M, int64_t K, int64_t N, int wdtype);
-// dependent: after a kernel of the same call
-cudaError_t launch_weight_grad(const AapLinearGradCall &c, uint8_t *work, bool dependent, cudaStream_t stream);
+// beside: a kernel of the same call has been launched, in a workspace of its own
+cudaError_t launch_weight_grad(const AapLinearGradCall &c, uint8_t *work, bool beside, cudaStream_t stream);
 int64_t aap_linear_grad_workspace(int64_t M, int64_t K, int64_t N, int dtype, int wdtype);
 cudaError_t launch_aap_linear_grad(const AapLinearGradCall &c, cudaStream_t stream);
 

@@ -66,20 +66,20 @@ cudaError_t launch_aap_linear(const AapLinearCall &c, cudaStream_t st) {
     if (!stages_codes(c.N)) {
       const CodesK<128> b = {c.codes, c.M, c.K, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
       return launch_gemm<WeightsK, CodesK<128>, OutY, 256, 2>(c.N, c.M, c.K, a, b, out, static_cast<float *>(c.workspace), sms,
-                                                             wait_status(), false, st);
+                                                             wait_status(), Order::kFirst, st);
     }
     cudaError_t e = launch_stage_codes(c.codes, c.ldc, c.M, c.K, c.workspace, st);
     if (e != cudaSuccess) return e;
     Staged b;
     if ((e = tensor_map(&b.map, c.workspace, false, staged_k(c.K), c.M, staged_k(c.K), 1, Staged::X)) != cudaSuccess) return e;
     float *partial = reinterpret_cast<float *>(static_cast<uint8_t *>(c.workspace) + 2 * c.M * staged_k(c.K));
-    return launch_gemm<WeightsK, Staged, OutY, 256, 2>(c.N, c.M, c.K, a, b, out, partial, sms, wait_status(), true, st);
+    return launch_gemm<WeightsK, Staged, OutY, 256, 2>(c.N, c.M, c.K, a, b, out, partial, sms, wait_status(), Order::kAfter, st);
   }
   return with_forward_tile(c.M, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
     const CodesK<TB> b = {c.codes, c.M, c.K, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
     return launch_gemm<WeightsK, CodesK<TB>, OutY, TB, 1>(c.N, c.M, c.K, a, b, out, static_cast<float *>(c.workspace), sms,
-                                                         wait_status(), false, st);
+                                                         wait_status(), Order::kFirst, st);
   });
 }
 

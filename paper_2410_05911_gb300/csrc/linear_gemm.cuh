@@ -627,6 +627,12 @@ __device__ __forceinline__ void put_element(void *y, int dtype, int64_t at, floa
 }
 
 // ----------------------------------------------------------------------------- the kernel
+// A kernel's order to the one before it on the stream.  kFirst: the first of a call, which begins when all before is over.
+// kAfter: it reads what the kernel before it writes, and waits for that one's end at its start.  kBeside: it neither reads nor
+// writes what the call's kernels before it write, as the gradients of one call in workspaces of their own, and waits for
+// the one before it at its own end, so that what follows on the stream follows both.  (All that the call reads was there when its
+// first kernel began.)
+enum class Order { kFirst, kAfter, kBeside };
 template <class A, class B, class Out>
 struct GemmArgs {
   int64_t I, J, R;
@@ -636,7 +642,7 @@ struct GemmArgs {
   int tiles_i, steps;  // tiles along i (whole clusters); steps of a split
   int full;            // r that are left for a span to be loaded by full(), more than there are without alignment
   int stages;
-  int dependent;       // launched before the kernel before it was over
+  Order order;         // to the kernel before it on the stream
   int parts;           // splits that are one cluster and join in shared memory, else 1
   bool joins;          // the splits' sums join in a second kernel
   float *partial;      // [splits][J][I] where they do, or where a part of R is in chunks (kCarry)
@@ -723,7 +729,7 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     tmem_alloc_cg<CG>(smem_u32(const_cast<uint32_t *>(word)), S::kTmemCols);
     tmem_relinquish_cg<CG>();
   }
-  if (g.dependent) grid_wait();
+  if (g.order == Order::kAfter) grid_wait();
   tc_fence_before();
   if constexpr (CG == 2) cluster_sync_all();  // (the other CTA's barriers too)
   else __syncthreads();
@@ -1020,6 +1026,7 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     tc_fence_after();
     tmem_dealloc_cg<CG>(tmem, S::kTmemCols);
   }
+  if (g.order == Order::kBeside) grid_wait();
 }
 
 // the splits' sums, added in order, and the epilogue: an element a thread
@@ -1098,13 +1105,13 @@ int64_t partial_floats(int64_t I, int64_t J, int64_t R, int sms) {
 
 template <class A, class B, class Out, int TB, int CG>
 cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b, const Out &out, float *partial, int sms, int *err,
-                        bool dependent, cudaStream_t st) {
+                        Order order, cudaStream_t st) {
   using S = GemmShape<A, B, TB, CG>;
   const GemmPlan p = gemm_plan<A, B, TB, CG>(I, J, R, sms);
   const int64_t ctas = p.tiles_i * p.tiles_j * p.splits;
   const int stages = S::stages(S::kCtasPerSm == 2 && ctas > sms);
   const GemmArgs<A, B, Out> g = {I, J, R, a, b, out, static_cast<int>(p.tiles_i), p.steps,
-                                   a.aligned() && b.aligned() ? A::kSpan * kStep : INT_MAX, stages, dependent ? 1 : 0, p.cluster ? p.splits : 1,
+                                   a.aligned() && b.aligned() ? A::kSpan * kStep : INT_MAX, stages, order, p.cluster ? p.splits : 1,
                                    p.splits > 1 && !p.cluster, partial, err};
   auto *kernel = gemm_kernel<A, B, Out, TB, CG>;
   static std::atomic<uint64_t> allowed{0};  // devices on which the kernel may use its shared memory
@@ -1127,7 +1134,7 @@ cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b,
   cfg.dynamicSmemBytes = S::smem(stages);
   cfg.stream = st;
   cfg.attrs = attr;
-  cfg.numAttrs = dependent ? 2 : 1;
+  cfg.numAttrs = order == Order::kFirst ? 1 : 2;
   if ((e = cudaLaunchKernelEx(&cfg, kernel, g)) != cudaSuccess || !g.joins) return e;
   const int64_t blocks = (I * J + 255) / 256, most = static_cast<int64_t>(sms) * 32;
   return launch_dependent(gemm_join_kernel<Out>, dim3(static_cast<unsigned>(blocks < most ? blocks : most)), 256, 0, st,
@@ -1169,7 +1176,7 @@ struct StageGrads {
   void *out;           // [pieces][M][N up to a multiple of 8] 16-bit, or NULL
   float *db;           // [N] column sums, or NULL
   float *partial;      // [stage_parts(M, N)][N] with db
-  bool dependent;      // launched before the kernel before it is over
+  Order order;         // to the kernel before it on the stream
 };
 int stage_parts(int64_t M, int64_t N);
 cudaError_t launch_stage_codes(const int8_t *codes, int64_t ld, int64_t M, int64_t K, void *out, cudaStream_t st);

@@ -47,18 +47,18 @@ cudaError_t input_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t s
     cudaError_t e = cudaSuccess;
     if (staged) {
       rows = work, ld = padded(c.N);
-      const StageGrads s = {c.dy, c.lddy, c.M, c.N, c.dtype, nullptr, sizeof(T) == 4 ? 3 : 0, work, nullptr, nullptr, false};
+      const StageGrads s = {c.dy, c.lddy, c.M, c.N, c.dtype, nullptr, sizeof(T) == 4 ? 3 : 0, work, nullptr, nullptr, Order::kFirst};
       if ((e = launch_stage_grads(s, st)) != cudaSuccess) return e;
     }
     if ((e = tensor_map(&b.map, rows, Staged<T>::kBf, c.N, c.M, ld, kPieces<T>, Staged<T>::X)) != cudaSuccess) return e;
     float *partial = reinterpret_cast<float *>(work + 2 * kPieces<T> * c.M * padded(c.N));
-    return launch_gemm<Weights<T>, Staged<T>, OutX, kPairTile<kPieces<T>>, 2>(c.K, c.M, c.N, a, b, out, partial, sms, wait_status(), staged, st);
+    return launch_gemm<Weights<T>, Staged<T>, OutX, kPairTile<kPieces<T>>, 2>(c.K, c.M, c.N, a, b, out, partial, sms, wait_status(), staged ? Order::kAfter : Order::kFirst, st);
   }
   const void *dy = c.dy;
   int64_t ld = c.lddy, width = c.N;
   const bool staged = stages_rows<T>(c.K) && !grads_vec<T>(dy, ld, width);
   if (staged) {
-    const StageGrads s = {dy, ld, c.M, c.N, c.dtype, nullptr, 0, work, nullptr, nullptr, false};
+    const StageGrads s = {dy, ld, c.M, c.N, c.dtype, nullptr, 0, work, nullptr, nullptr, Order::kFirst};
     const cudaError_t e = launch_stage_grads(s, st);
     if (e != cudaSuccess) return e;
     dy = work, ld = width = padded(c.N), work += up16(2 * c.M * ld);
@@ -67,7 +67,7 @@ cudaError_t input_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t s
     constexpr int TB = decltype(tb)::value;
     using B = GradK<T, TB>;
     const B b = {static_cast<const T *>(dy), c.M, width, ld, grads_vec<T>(dy, ld, width)};
-    return launch_gemm<Weights<T>, B, OutX, TB, 1>(c.K, c.M, c.N, a, b, out, reinterpret_cast<float *>(work), sms, wait_status(), staged, st);
+    return launch_gemm<Weights<T>, B, OutX, TB, 1>(c.K, c.M, c.N, a, b, out, reinterpret_cast<float *>(work), sms, wait_status(), staged ? Order::kAfter : Order::kFirst, st);
   });
 }
 
@@ -81,20 +81,22 @@ int64_t input_grad_workspace(int64_t M, int64_t K, int64_t N) {
   });
 }
 
+int64_t input_part(int64_t M, int64_t K, int64_t N, int dtype) {
+  return up16(dtype == 0 ? input_grad_workspace<float>(M, K, N) : input_grad_workspace<__half>(M, K, N));
+}
+
 }  // namespace
 
-// the three gradients run one after the other and share the workspace
+// dX's part, and that of dW and db beside it
 int64_t aap_linear_grad_workspace(int64_t M, int64_t K, int64_t N, int dtype, int wdtype) {
-  const int64_t x = dtype == 0 ? input_grad_workspace<float>(M, K, N) : input_grad_workspace<__half>(M, K, N);
-  const int64_t w = weight_grad_workspace(M, K, N, wdtype);
-  return x > w ? x : w;
+  return input_part(M, K, N, dtype) + weight_grad_workspace(M, K, N, wdtype);
 }
 
 cudaError_t launch_aap_linear_grad(const AapLinearGradCall &c, cudaStream_t st) {
   uint8_t *work = static_cast<uint8_t *>(c.workspace);
   cudaError_t e = cudaSuccess;
   if (c.dx) e = c.dtype == 0 ? input_grad<float>(c, work, st) : c.dtype == 1 ? input_grad<__half>(c, work, st) : input_grad<__nv_bfloat16>(c, work, st);
-  if (e == cudaSuccess && (c.dw || c.db)) e = launch_weight_grad(c, work, c.dx != nullptr, st);
+  if (e == cudaSuccess && (c.dw || c.db)) e = launch_weight_grad(c, work + input_part(c.M, c.K, c.N, c.dtype), c.dx != nullptr, st);
   return e;
 }
 

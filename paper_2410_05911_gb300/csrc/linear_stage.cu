@@ -38,10 +38,10 @@ __global__ void __launch_bounds__(kStageThreads) stage_codes_kernel(const int8_t
 // sums alone.  A CTA takes 256 columns, 8 a thread, of every gridDim.y-th group of 8 rows.
 template <typename T, int P>
 __global__ void __launch_bounds__(kStageThreads) stage_grads_kernel(const T *dy, int64_t ld, bool vec, int64_t M, int64_t N, int64_t Np,
-                                                                    const float *scale, uint16_t *out, float *partial) {
+                                                                    const float *scale, uint16_t *out, float *partial, Order order) {
   __shared__ float sums[8][256];
   grid_trigger();
-  grid_wait();
+  if (order == Order::kAfter) grid_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + 8 * lane;
   const int left = static_cast<int>(N - n < 8 ? N - n : 8);
@@ -68,16 +68,18 @@ __global__ void __launch_bounds__(kStageThreads) stage_grads_kernel(const T *dy,
       }
     }
   }
-  if (!partial) return;
+  if (partial) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) sums[warp][8 * lane + e] = sum[e];
-  __syncthreads();
-  const int64_t c = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  if (c < N) {
-    float s = 0.0f;
-    for (int k = 0; k < 8; ++k) s += sums[k][threadIdx.x];
-    partial[blockIdx.y * N + c] = s;
+    for (int e = 0; e < 8; ++e) sums[warp][8 * lane + e] = sum[e];
+    __syncthreads();
+    const int64_t c = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
+    if (c < N) {
+      float s = 0.0f;
+      for (int k = 0; k < 8; ++k) s += sums[k][threadIdx.x];
+      partial[blockIdx.y * N + c] = s;
+    }
   }
+  if (order == Order::kBeside) grid_wait();
 }
 
 // db[n] = the sum over the CTAs' partial sums, in a fixed order: 32 columns a CTA, 32 rows of them at a time
@@ -103,18 +105,19 @@ cudaError_t stage_of(const StageGrads &c, cudaStream_t st) {
   const dim3 grid(static_cast<unsigned>((c.N + 255) / 256), static_cast<unsigned>(stage_parts(c.M, c.N)));
   const bool vec = grads_vec<T>(c.dy, c.ld, c.N);
   const int64_t Np = (c.N + 7) / 8 * 8;
-  float *partial = c.db ? c.partial : nullptr;
+  float *partial = !c.db ? nullptr : grid.y == 1 ? c.db : c.partial;
   cudaError_t e;
-  if (c.dependent) {
+  if (c.order != Order::kFirst) {
     e = launch_dependent(stage_grads_kernel<T, P>, grid, kStageThreads, 0, st, static_cast<const T *>(c.dy), c.ld, vec, c.M, c.N, Np,
-                         c.scale, static_cast<uint16_t *>(c.out), partial);
+                         c.scale, static_cast<uint16_t *>(c.out), partial, c.order);
   } else {
     stage_grads_kernel<T, P><<<grid, kStageThreads, 0, st>>>(static_cast<const T *>(c.dy), c.ld, vec, c.M, c.N, Np, c.scale,
-                                                             static_cast<uint16_t *>(c.out), partial);
+                                                             static_cast<uint16_t *>(c.out), partial, c.order);
     e = cudaGetLastError();
   }
-  if (e != cudaSuccess || !c.db) return e;
-  return launch_dependent(join_sums_kernel, dim3(static_cast<unsigned>((c.N + 31) / 32)), 1024, 0, st, c.partial, static_cast<int>(grid.y), c.N, c.db);
+  if (e != cudaSuccess || !c.db || grid.y == 1) return e;  // (one part is the sum)
+  return launch_dependent(join_sums_kernel, dim3(static_cast<unsigned>((c.N + 31) / 32)), 1024, 0, st, c.partial,
+                          static_cast<int>(grid.y), c.N, c.db);
 }
 
 template <typename T>
@@ -129,7 +132,7 @@ cudaError_t stage_of(const StageGrads &c, cudaStream_t st) {
 
 // row groups of a CTA column: eight CTAs an SM, no more than there are rows for
 int stage_parts(int64_t M, int64_t N) {
-  const int64_t groups = (M + 31) / 32, columns = (N + 255) / 256, most = (8 * static_cast<int64_t>(sm_count()) + columns - 1) / columns;
+  const int64_t groups = (M + 63) / 64, columns = (N + 255) / 256, most = (8 * static_cast<int64_t>(sm_count()) + columns - 1) / columns;
   const int64_t p = groups < most ? groups : most;
   return static_cast<int>(p < 1 ? 1 : p);
 }

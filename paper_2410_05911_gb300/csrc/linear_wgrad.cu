@@ -34,25 +34,25 @@ cudaError_t staged_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t 
   const CodesT a = {c.codes, c.M, c.K, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
   const OutW out = {c.dw, c.wdtype, c.K};
   float *partial = reinterpret_cast<float *>(work + 2 * P * c.M * padded(c.N));
-  return launch_gemm<CodesT, Staged<P>, OutW, kPairTile<P>, 2>(c.K, c.N, c.M, a, b, out, partial, sm_count(), wait_status(), true, st);
+  return launch_gemm<CodesT, Staged<P>, OutW, kPairTile<P>, 2>(c.K, c.N, c.M, a, b, out, partial, sm_count(), wait_status(), Order::kAfter, st);
 }
 
 template <typename T, int P>
-cudaError_t weight_grad(const AapLinearGradCall &c, uint8_t *work, bool dependent, cudaStream_t st) {
+cudaError_t weight_grad(const AapLinearGradCall &c, uint8_t *work, Order order, cudaStream_t st) {
   const CodesT a = {c.codes, c.M, c.K, c.ldc, codes_unit(c.codes, c.ldc, c.K)};
   const OutW out = {c.dw, c.wdtype, c.K};
   return with_single_tile<P>(c.N, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
     using B = GradT<T, TB, P>;
     const B b = {static_cast<const T *>(c.dy), c.M, c.N, c.lddy, c.scale, grads_vec<T>(c.dy, c.lddy, c.N)};
-    return launch_gemm<CodesT, B, OutW, TB, 1>(c.K, c.N, c.M, a, b, out, reinterpret_cast<float *>(work), sm_count(), wait_status(), dependent, st);
+    return launch_gemm<CodesT, B, OutW, TB, 1>(c.K, c.N, c.M, a, b, out, reinterpret_cast<float *>(work), sm_count(), wait_status(), order, st);
   });
 }
 
 template <typename T>
-cudaError_t weight_grad(const AapLinearGradCall &c, uint8_t *work, bool dependent, cudaStream_t st) {
+cudaError_t weight_grad(const AapLinearGradCall &c, uint8_t *work, Order order, cudaStream_t st) {
   const int p = pieces_of(c.M, c.wdtype);
-  return p == 3 ? weight_grad<T, 3>(c, work, dependent, st) : p == 2 ? weight_grad<T, 2>(c, work, dependent, st) : weight_grad<T, 1>(c, work, dependent, st);
+  return p == 3 ? weight_grad<T, 3>(c, work, order, st) : p == 2 ? weight_grad<T, 2>(c, work, order, st) : weight_grad<T, 1>(c, work, order, st);
 }
 
 template <int P>
@@ -73,19 +73,23 @@ int64_t weight_grad_workspace(int64_t M, int64_t K, int64_t N, int wdtype) {
   return sums_bytes(M, N) + (p == 3 ? workspace_of<3>(M, K, N) : p == 2 ? workspace_of<2>(M, K, N) : workspace_of<1>(M, K, N));
 }
 
-cudaError_t launch_weight_grad(const AapLinearGradCall &c, uint8_t *work, bool dependent, cudaStream_t st) {
+cudaError_t launch_weight_grad(const AapLinearGradCall &c, uint8_t *work, bool beside, cudaStream_t st) {
+  Order order = beside ? Order::kBeside : Order::kFirst;
   const int p = pieces_of(c.M, c.wdtype);
   uint8_t *rest = work + sums_bytes(c.M, c.N);
   const bool staged = c.dw && grad_pairs(c.K, c.N, c.M, sm_count());
   if (staged || c.db) {
-    const StageGrads s = {c.dy, c.lddy, c.M, c.N, c.dtype, c.scale, staged ? p : 1, staged ? rest : nullptr, c.db, reinterpret_cast<float *>(work), dependent};
+    const StageGrads s = {c.dy, c.lddy, c.M, c.N, c.dtype, c.scale, staged ? p : 1, staged ? rest : nullptr, c.db,
+                          reinterpret_cast<float *>(work), order};
     const cudaError_t e = launch_stage_grads(s, st);
     if (e != cudaSuccess) return e;
-    dependent = true;
+    order = Order::kBeside;
   }
   if (!c.dw) return cudaSuccess;
   if (staged) return p == 3 ? staged_grad<3>(c, rest, st) : p == 2 ? staged_grad<2>(c, rest, st) : staged_grad<1>(c, rest, st);
-  return c.dtype == 0 ? weight_grad<float>(c, rest, dependent, st) : c.dtype == 1 ? weight_grad<__half>(c, rest, dependent, st) : weight_grad<__nv_bfloat16>(c, rest, dependent, st);
+  return c.dtype == 0   ? weight_grad<float>(c, rest, order, st)
+         : c.dtype == 1 ? weight_grad<__half>(c, rest, order, st)
+                        : weight_grad<__nv_bfloat16>(c, rest, order, st);
 }
 
 }  // namespace aecct
