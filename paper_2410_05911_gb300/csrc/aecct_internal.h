@@ -330,6 +330,8 @@ struct RmsQuantGradCall {
   float *dgain;
   float *partial;  // rms_quant_grad_partials(rows, d) floats
 };
+// out[i] = sum over k < parts of partial[k][i], after the kernel before it (norm.cu)
+cudaError_t launch_join_columns(const float *partial, int parts, int64_t n, float *out, cudaStream_t stream);
 cudaError_t launch_rms_quant(const RmsQuantCall &c, cudaStream_t stream);
 int64_t rms_quant_grad_partials(int64_t rows, int d);
 cudaError_t launch_rms_quant_grad(const RmsQuantGradCall &c, cudaStream_t stream);

@@ -82,24 +82,6 @@ __global__ void __launch_bounds__(kStageThreads) stage_grads_kernel(const T *dy,
   if (order == Order::kBeside) grid_wait();
 }
 
-// db[n] = the sum over the CTAs' partial sums, in a fixed order: 32 columns a CTA, 32 rows of them at a time
-__global__ void __launch_bounds__(1024) join_sums_kernel(const float *partial, int parts, int64_t N, float *db) {
-  __shared__ float s[32][33];
-  const int c = threadIdx.x & 31, k0 = threadIdx.x >> 5;
-  const int64_t n = static_cast<int64_t>(blockIdx.x) * 32;
-  float v = 0.0f;
-  grid_trigger();
-  grid_wait();
-  if (n + c < N)
-#pragma unroll 4
-    for (int k = k0; k < parts; k += 32) v += partial[k * N + n + c];
-  s[k0][c] = v;
-  __syncthreads();
-  v = s[c][k0];  // column k0 of the CTA, a row a lane
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  if (c == 0 && n + k0 < N) db[n + k0] = v;
-}
-
 template <typename T, int P>
 cudaError_t stage_of(const StageGrads &c, cudaStream_t st) {
   const dim3 grid(static_cast<unsigned>((c.N + 255) / 256), static_cast<unsigned>(stage_parts(c.M, c.N)));
@@ -116,8 +98,7 @@ cudaError_t stage_of(const StageGrads &c, cudaStream_t st) {
     e = cudaGetLastError();
   }
   if (e != cudaSuccess || !c.db || grid.y == 1) return e;  // (one part is the sum)
-  return launch_dependent(join_sums_kernel, dim3(static_cast<unsigned>((c.N + 31) / 32)), 1024, 0, st, c.partial,
-                          static_cast<int>(grid.y), c.N, c.db);
+  return launch_join_columns(c.partial, static_cast<int>(grid.y), c.N, c.db, st);
 }
 
 template <typename T>
