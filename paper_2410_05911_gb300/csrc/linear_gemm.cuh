@@ -667,6 +667,8 @@ struct GemmShape {
   // added in registers: 28 additions to a part at most.
   static constexpr int kSets = B::P == 3 ? 4 : 1;
   static constexpr int kChunk = 20;  // a multiple of the producers' groups
+  // (Pairs wait for each other's tensor memory, so no mix of these products, of any streams, may run short of it: one of
+  // more than half has an SM's shared memory to itself, and of the others a third CTA does not fit that.)
   static constexpr uint32_t kTmemCols = TB * kSets < 32 ? 32 : TB * kSets;
   static constexpr uint32_t kBars = 256 + TB * 4;  // barriers and two words; the columns' factors
   static constexpr int kMaxStages = 8;
@@ -680,6 +682,8 @@ struct GemmShape {
   }
   static constexpr uint32_t smem(int stages) { return stages * kStageBytes + kBars; }
   static_assert(stages(kCtasPerSm == 2) >= 2 && kStageBytes % 16 == 0 && kCtasPerSm * kTmemCols <= 512, "stages and accumulators");
+  static_assert(stages(kCtasPerSm == 2) * kStageBytes > kSmemPerSm / 3 && (kTmemCols <= 256 || stages(false) * kStageBytes > kSmemPerSm * 2 / 3),
+                "CTAs of an SM and its tensor memory");
   static constexpr bool kClusters = CG == 1 && TB == 16;  // parts of R may join in a cluster (gemm_plan)
   static_assert(!kClusters || stages(kCtasPerSm == 2) * kStageBytes >= kTileI * TB * 4, "a cluster joins its tile in the stages");
   static_assert(A::kSpan == B::kSpan, "operands load together");
@@ -725,11 +729,12 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     place[4] = kSpan * ((end - first + kSpan * kStep - 1) / (kSpan * kStep));
   }
   grid_trigger();
+  // (before the allocation: a pair that held tensor memory while it waited could keep it from a pair that it waits for)
+  if (g.order == Order::kAfter) grid_wait();
   if (warp == kProducerWarps) {
     tmem_alloc_cg<CG>(smem_u32(const_cast<uint32_t *>(word)), S::kTmemCols);
     tmem_relinquish_cg<CG>();
   }
-  if (g.order == Order::kAfter) grid_wait();
   tc_fence_before();
   if constexpr (CG == 2) cluster_sync_all();  // (the other CTA's barriers too)
   else __syncthreads();
@@ -1103,6 +1108,7 @@ int64_t partial_floats(int64_t I, int64_t J, int64_t R, int sms) {
   return (p.splits > 1 && !p.cluster) || carries ? p.splits * I * J : 0;
 }
 
+// (A pair is never kBeside: two kernels of pairs at a time could each hold the tensor memory that the other's pairs lack.)
 template <class A, class B, class Out, int TB, int CG>
 cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b, const Out &out, float *partial, int sms, int *err,
                         Order order, cudaStream_t st) {
