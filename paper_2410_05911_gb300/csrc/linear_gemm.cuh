@@ -682,8 +682,8 @@ struct GemmShape {
   }
   static constexpr uint32_t smem(int stages) { return stages * kStageBytes + kBars; }
   static_assert(stages(kCtasPerSm == 2) >= 2 && kStageBytes % 16 == 0 && kCtasPerSm * kTmemCols <= 512, "stages and accumulators");
-  static_assert(stages(kCtasPerSm == 2) * kStageBytes > kSmemPerSm / 3 && (kTmemCols <= 256 || stages(false) * kStageBytes > kSmemPerSm * 2 / 3),
-                "CTAs of an SM and its tensor memory");
+  static_assert(stages(kCtasPerSm == 2) * kStageBytes > kSmemPerSm / 3, "at most two CTAs on an SM");
+  static_assert(kTmemCols <= 256 || stages(false) * kStageBytes > kSmemPerSm * 2 / 3, "one CTA on an SM");
   static constexpr bool kClusters = CG == 1 && TB == 16;  // parts of R may join in a cluster (gemm_plan)
   static_assert(!kClusters || stages(kCtasPerSm == 2) * kStageBytes >= kTileI * TB * 4, "a cluster joins its tile in the stages");
   static_assert(A::kSpan == B::kSpan, "operands load together");
@@ -763,7 +763,9 @@ __global__ void __launch_bounds__(kGemmThreads, GemmShape<A, B, TB, CG>::kCtasPe
     return i0_of() + (A::kMixed ? (r & ~15) | mix16(r & 15) : r);
   };
   const auto tmem_of = [&] { return tmem + (static_cast<uint32_t>(threadIdx.x & 96) << 16) + column_of(); };
-  const auto carry_of = [&](int c) { return g.partial + (static_cast<int64_t>(blockIdx.y) * g.J + j0_of() + column_of() + c) * g.I + i_of(); };
+  const auto carry_of = [&](int c) {
+    return g.partial + (static_cast<int64_t>(blockIdx.y) * g.J + j0_of() + column_of() + c) * g.I + i_of();
+  };
   // Three pieces: the sums over the chunks that are over stay in this thread's registers (a pair's CTA, alone on its
   // SM), or in the part's place of `partial` (half of an SM's registers are too few).
   constexpr bool kKeep = P == 3 && CG == 2, kCarry = P == 3 && CG == 1;
