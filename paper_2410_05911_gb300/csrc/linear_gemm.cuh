@@ -116,32 +116,24 @@ __device__ __forceinline__ void codes4_bf16(uint32_t b, uint32_t &o0, uint32_t &
   };
   o0 = sub(t0), o1 = sub(t1);
 }
-// 8 values in 32 bits as P bfloat16 pieces each, the largest first: rounded where there is one; else each piece
-// cuts off 8 bits and the next takes what is left, so that three hold a 32-bit value exactly.  An infinity
-// stays one in its first piece, and its others are zero.
-// put(p, words) takes a piece at a time.
+// 8 values in 32 bits as P bfloat16 pieces each, the largest first: each piece cuts off 8 bits and the next takes what is
+// left, so that two hold 16 bits and three a 32-bit value exactly.  An infinity stays one in its first piece, and its others
+// are zero.  put(p, words) takes a piece at a time.
 template <int P, class Put>
 __device__ __forceinline__ void split8(const float (&v)[8], const Put &put) {
-  uint32_t o[4];
-  if constexpr (P == 1) {
+  uint32_t o[4], x[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = pack2<__nv_bfloat16>(v[2 * i], v[2 * i + 1]);
-    put(0, o);
-  } else {
-    uint32_t x[8];
+  for (int e = 0; e < 8; ++e) x[e] = v[e] == v[e] ? __float_as_uint(v[e]) : 0x7FC00000u;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x[e] = v[e] == v[e] ? __float_as_uint(v[e]) : 0x7FC00000u;
+  for (int p = 0; p < P; ++p) {
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
+    for (int i = 0; i < 4; ++i) o[i] = __byte_perm(x[2 * i], x[2 * i + 1], 0x7632);
+    put(p, o);
+    if (p + 1 < P) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) o[i] = __byte_perm(x[2 * i], x[2 * i + 1], 0x7632);
-      put(p, o);
-      if (p + 1 < P) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const float top = __uint_as_float(x[e] & 0xFFFF0000u);
-          x[e] = fabsf(top) < INFINITY ? __float_as_uint(__uint_as_float(x[e]) - top) : 0u;
-        }
+      for (int e = 0; e < 8; ++e) {
+        const float top = __uint_as_float(x[e] & 0xFFFF0000u);
+        x[e] = fabsf(top) < INFINITY ? __float_as_uint(__uint_as_float(x[e]) - top) : 0u;
       }
     }
   }
@@ -1180,7 +1172,7 @@ struct StageGrads {
   int64_t ld, M, N;
   int dtype;
   const float *scale;  // [M] or NULL
-  int pieces;          // bfloat16 pieces; 0: 16-bit gradients as they are
+  int pieces;          // bfloat16 pieces; 0: 16-bit gradients as they are, or the sums alone
   void *out;           // [pieces][M][N up to a multiple of 8] 16-bit, or NULL
   float *db;           // [N] column sums, or NULL
   float *partial;      // [stage_parts(M, N)][N] with db

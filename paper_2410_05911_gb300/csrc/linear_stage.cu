@@ -33,7 +33,7 @@ __global__ void __launch_bounds__(kStageThreads) stage_codes_kernel(const int8_t
   }
 }
 
-// dy [M][ld] to P pieces [P][M][Np] (Np a multiple of 8): dy times scale (NULL: 1) in bfloat16, or as it is
+// dy [M][ld] to P pieces [P][M][Np] (Np a multiple of 8): dy times scale (NULL: 1) in bfloat16, or 16-bit dy as it is
 // (P = 0); and the sums of dy's columns over the CTA's rows to partial[blockIdx.y][N] (NULL: none).  out NULL: the
 // sums alone.  A CTA takes 256 columns, 8 a thread, of every gridDim.y-th group of 8 rows.
 template <typename T, int P>
@@ -103,10 +103,7 @@ cudaError_t stage_of(const StageGrads &c, cudaStream_t st) {
 
 template <typename T>
 cudaError_t stage_of(const StageGrads &c, cudaStream_t st) {
-  if constexpr (sizeof(T) == 2) {
-    if (c.pieces == 0) return stage_of<T, 0>(c, st);
-  }
-  return c.pieces == 3 ? stage_of<T, 3>(c, st) : c.pieces == 2 ? stage_of<T, 2>(c, st) : stage_of<T, 1>(c, st);
+  return c.pieces == 3 ? stage_of<T, 3>(c, st) : c.pieces == 2 ? stage_of<T, 2>(c, st) : stage_of<T, 0>(c, st);
 }
 
 }  // namespace

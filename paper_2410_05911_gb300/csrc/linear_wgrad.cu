@@ -1,8 +1,10 @@
 // linear_wgrad.cu -- the gradient of the AAP linear layer's weights, dW = sum over tokens of dy scale codes, and
-// of its bias (linear.cu has the formulas).  dy scale is no 16-bit number: it goes through the tensor cores in as
-// many bfloat16 pieces as the gradient's own type has room for (1: bfloat16, 2: half, 3: float, exact).  One
-// piece rounds each term to 8 bits, which many tokens average out; the few terms of up to kFewTokens are
-// taken in two pieces, where the product is bound by writing dW and the second one costs nothing.
+// of its bias (linear.cu has the formulas).  dy scale is no 16-bit number: it goes through the tensor cores in
+// bfloat16 pieces, two (16 bits) for a gradient of 16 bits, three (exact) for one of 32.  Two, so that what is cut off
+// a term stays under the rounding of the gradient itself, to 8 bits in bfloat16 and 11 in half.  With one piece
+// for bfloat16 each term would lose as much as the result: the error of 8,192 x 4,096 x 4,096 in the 2-norm was 2.3e-3 of
+// it, where the rounding of the result alone is 1.7e-3, and terms alike kept all of their own 2^-8.  (dW then took 188 us,
+// and takes 326 us: the second piece is as much work again.)
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -13,9 +15,7 @@ namespace aecct {
 
 namespace {
 
-constexpr int64_t kFewTokens = 64;
-
-int pieces_of(int64_t M, int wdtype) { return wdtype == 0 ? 3 : wdtype == 1 || M <= kFewTokens ? 2 : 1; }
+int pieces_of(int wdtype) { return wdtype == 0 ? 3 : 2; }
 
 int64_t padded(int64_t n) { return (n + 7) / 8 * 8; }
 
@@ -51,8 +51,7 @@ cudaError_t weight_grad(const AapLinearGradCall &c, uint8_t *work, Order order, 
 
 template <typename T>
 cudaError_t weight_grad(const AapLinearGradCall &c, uint8_t *work, Order order, cudaStream_t st) {
-  const int p = pieces_of(c.M, c.wdtype);
-  return p == 3 ? weight_grad<T, 3>(c, work, order, st) : p == 2 ? weight_grad<T, 2>(c, work, order, st) : weight_grad<T, 1>(c, work, order, st);
+  return pieces_of(c.wdtype) == 3 ? weight_grad<T, 3>(c, work, order, st) : weight_grad<T, 2>(c, work, order, st);
 }
 
 template <int P>
@@ -69,24 +68,23 @@ int64_t workspace_of(int64_t M, int64_t K, int64_t N) {
 
 // the column sums, and after them the staged pieces and the splits' sums
 int64_t weight_grad_workspace(int64_t M, int64_t K, int64_t N, int wdtype) {
-  const int p = pieces_of(M, wdtype);
-  return sums_bytes(M, N) + (p == 3 ? workspace_of<3>(M, K, N) : p == 2 ? workspace_of<2>(M, K, N) : workspace_of<1>(M, K, N));
+  return sums_bytes(M, N) + (pieces_of(wdtype) == 3 ? workspace_of<3>(M, K, N) : workspace_of<2>(M, K, N));
 }
 
 cudaError_t launch_weight_grad(const AapLinearGradCall &c, uint8_t *work, bool beside, cudaStream_t st) {
   Order order = beside ? Order::kBeside : Order::kFirst;
-  const int p = pieces_of(c.M, c.wdtype);
+  const int p = pieces_of(c.wdtype);
   uint8_t *rest = work + sums_bytes(c.M, c.N);
   const bool staged = c.dw && grad_pairs(c.K, c.N, c.M, sm_count());
   if (staged || c.db) {
-    const StageGrads s = {c.dy, c.lddy, c.M, c.N, c.dtype, c.scale, staged ? p : 1, staged ? rest : nullptr, c.db,
+    const StageGrads s = {c.dy, c.lddy, c.M, c.N, c.dtype, c.scale, staged ? p : 0, staged ? rest : nullptr, c.db,
                           reinterpret_cast<float *>(work), order};
     const cudaError_t e = launch_stage_grads(s, st);
     if (e != cudaSuccess) return e;
     order = Order::kBeside;
   }
   if (!c.dw) return cudaSuccess;
-  if (staged) return p == 3 ? staged_grad<3>(c, rest, st) : p == 2 ? staged_grad<2>(c, rest, st) : staged_grad<1>(c, rest, st);
+  if (staged) return p == 3 ? staged_grad<3>(c, rest, st) : staged_grad<2>(c, rest, st);
   return c.dtype == 0   ? weight_grad<float>(c, rest, order, st)
          : c.dtype == 1 ? weight_grad<__half>(c, rest, order, st)
                         : weight_grad<__nv_bfloat16>(c, rest, order, st);
