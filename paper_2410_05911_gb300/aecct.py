@@ -420,7 +420,7 @@ def spe_table(H: np.ndarray, params, want_eigen: bool = False):
 
 
 # ------------------------------------------------------------------------------------------
-# operators of AAP layers of any width
+# operators of AAP layers of any width: on tensors of the current CUDA device
 # ------------------------------------------------------------------------------------------
 _ELEMENT = {}  # torch type -> the C ABI's number
 _binding = None
@@ -451,7 +451,8 @@ def rms_quant(x, gain, residual=None, eps: float = 1e-6, want_values: bool = Fal
     """aecct_rms_quant: h = x + residual, its root-mean-square norm times gain, and eq. Quant of that, a
     row (the last dimension) at a time, on `stream` after what is queued on the current one.
 
-    x and residual are float32, float16 or bfloat16, gain is float32 [d].  Returns (codes int8 like x, scale float32
+    x and residual are float32, float16 or bfloat16, gain is float32 [d], all on the current CUDA device (as
+    are the tensors of the functions below; others are refused).  Returns (codes int8 like x, scale float32
     x.shape[:-1], total, values): codes * scale is the norm's output; total is h in x's type (x itself
     without a residual); values is codes * scale in x's type, or None."""
     return (_binding or _operators()).rms_quant(x, gain, residual, eps, bool(want_values), stream)
@@ -487,8 +488,8 @@ def aap_linear_backward(dy, codes, scale, packed, w_scale, weight_dtype=None, wa
 def clip_gradients(grads, max_norm: float, eps: float = 1e-6, out=None, stream=None):
     """aecct_clip_gradients: scales the tensors `grads` by min(1, max_norm / (norm + eps)), norm the 2-norm over
     all of their elements, in place or into the tensors `out`.  They are contiguous float32, float16 and bfloat16
-    tensors on one GPU.  Returns norm, a float32 scalar there."""
+    tensors on the current CUDA device.  Returns norm, a float32 scalar there."""
     import torch
 
-    device = 0 if grads or stream is not None else torch.cuda.current_device()
+    device = 0 if grads else torch.cuda.current_device()
     return (_binding or _operators()).clip_gradients(grads, max_norm, eps, out, device, stream)

@@ -9,6 +9,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -80,10 +81,19 @@ void check_like(const char *name, const at::Tensor &t, const at::Tensor &x) {
     throw ValueError(std::string(name) + " must be a tensor of the type, shape " + shape_of(x.sizes()) + " and device of the other rows");
 }
 
+// Kernels are launched on the current device, whose SMs their plans count: tensors that lie on another one are refused (launched
+// there they would be read across devices, in no order to the work on their own).
+void check_current(const at::Device &on) {
+  c10::DeviceIndex current = -1;
+  if (c10::cuda::GetDevice(&current) != cudaSuccess || current != on.index())
+    throw ValueError("the tensors are on " + on.str() + ", which is not the current CUDA device");
+}
+
 // `t` holds rows of a known type on the GPU, and `gain` one float32 for each element of a row
 void check_rows(const char *name, const at::Tensor &t, const at::Tensor &gain) {
   if (!t.is_cuda() || element(t.scalar_type()) < 0 || t.dim() < 1)
     throw ValueError(std::string(name) + " must be a float32, float16 or bfloat16 CUDA tensor of rows");
+  check_current(t.device());
   if (gain.device() != t.device() || gain.scalar_type() != at::kFloat || gain.dim() != 1 || gain.size(0) != t.size(-1))
     throw ValueError("gain must be a float32 tensor of shape (" + std::to_string(t.size(-1)) + ",) on the rows' device");
 }
@@ -175,6 +185,7 @@ struct Linear {
       : codes(tensor(a[0], "codes")), scale(tensor(a[1], "scale")), packed(tensor(a[2], "packed")), w_scale(tensor(a[3], "w_scale")) {
     const at::Device dev = codes.device();
     if (!codes.is_cuda() || codes.scalar_type() != at::kChar || codes.dim() < 1) throw ValueError("codes must be an int8 CUDA tensor of rows");
+    check_current(dev);
     K = codes.size(-1);
     const at::IntArrayRef rows = codes.sizes().slice(0, codes.dim() - 1);
     if (scale.device() != dev || scale.scalar_type() != at::kFloat || scale.sizes() != rows)
@@ -249,7 +260,7 @@ PyObject *aap_linear_backward(PyObject *const *a) {
   return tuple({dx, dw, db});
 }
 
-// (list of gradients, max_norm, eps, list of outputs or None, device index where there are no gradients, stream)
+// (list of gradients, max_norm, eps, list of outputs or None, current device's index where there are no gradients, stream)
 PyObject *clip_gradients(PyObject *const *a) {
   THPObjectPtr grads(PySequence_Fast(a[0], "grads must be a sequence of tensors"));
   if (!grads) throw PythonError();
@@ -269,6 +280,7 @@ PyObject *clip_gradients(PyObject *const *a) {
     if (j == 0) {
       dev = g.device();
       if (!g.is_cuda()) throw ValueError("clip_gradients takes CUDA tensors");
+      check_current(dev);
     }
     if ((type[j] = element(g.scalar_type())) < 0 || g.device() != dev || !g.is_contiguous())
       throw ValueError("gradients must be contiguous float32, float16 or bfloat16 tensors on one device");
