@@ -367,7 +367,8 @@ __device__ __forceinline__ T *row_in(uint8_t *stage, const RowSource<T> &src, in
   if constexpr (ALIGNED) return reinterpret_cast<T *>(stage + k * row_bytes<T>(d));
   return reinterpret_cast<T *>(stage + k * row_bytes<T>(d) + (reinterpret_cast<uintptr_t>(src.p + row * src.ld) & 15));
 }
-// all threads: the elements of the first and last row that no copy takes
+// all threads: the elements of the first and last row that no copy takes.  The row's place is filled by a copy later: a fence
+// between the proxies orders these stores before its writes.
 template <typename T, int N>
 __device__ __forceinline__ void patch_rows(const RowSource<T> (&src)[N], int64_t row, int64_t rows, int d, uint8_t *stage) {
   if (row != 0 && row != rows - 1) return;
@@ -384,6 +385,7 @@ __device__ __forceinline__ void patch_rows(const RowSource<T> (&src)[N], int64_t
       for (int i = threadIdx.x; i < d; i += blockDim.x)
         if (i < from || i >= to) s[i] = p[i];
     }
+  fence_proxy_async_smem();
   __syncthreads();
 }
 // a wait for a copy, with an end: its rows are then wrong, and err says so
