@@ -11,7 +11,8 @@
 //
 // The gradients pass the rounding straight through (dy is that of q_i scale and of y_i):
 //   t_i = dy_i g_i,  dh_i = r t_i - h_i r^3 mean_j(t_j h_j) + dsum_i,  dg_i = sum over rows of dy_i h_i r
-// and dx = dres = dh.  Squares, products and sums are in 32 bits.
+// and dx = dres = dh.  Squares, products and sums are in 32 bits; the middle term is (h_i r) (mean_j(t_j h_j) r) r, whose
+// factors stay in range wherever the sum of squares does.
 #include <cuda_runtime.h>
 
 #include <atomic>
@@ -262,7 +263,7 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : kSmallThreads) rms_quant_grad_
       parity ^= 1;
     }
     const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(ss, static_cast<float>(d)) + a.eps));
-    const float c = r * r * r * (th * by);
+    const float c = th * r * by * r;  // (r^3 alone would leave the range for rows past 1e12 or under 1e-12)
     if (row < a.s.rows) {
 #pragma unroll
       for (int j = 0; j < C; ++j) {
@@ -274,9 +275,9 @@ __global__ void __launch_bounds__(BLOCK ? BLOCK : kSmallThreads) rms_quant_grad_
 #pragma unroll
           for (int e = 0; e < V; ++e) {
             const int k = j * V + e;
-            const float v = fmaf(-hv[k], c, r * tv[k]);
+            const float u = hv[k] * r, v = fmaf(-u, c, r * tv[k]);
             o[e] = a.dsum ? v + o[e] : v;
-            dg[k] = fmaf(y[e], hv[k] * r, dg[k]);
+            dg[k] = fmaf(y[e], u, dg[k]);
           }
           store_v<T, V>(a.dx + row * d + i, o);
         }
@@ -454,7 +455,7 @@ __global__ void __launch_bounds__(512, E == kFew ? 2 : 1) ring_grad_kernel(const
     uint8_t *stage = ring + s * stage_bytes;
     wait_copy(bar + 8 * s, parity, a.err);
     if constexpr (V == 1) patch_rows(a.src, row, a.rows, d, stage);
-    f32x2 h[H], t2[H], p[H];  // h, dy gain, dy h
+    f32x2 h[H], t2[H], y2[H];  // h, dy gain, dy
     f32x2 ss = 0, th = 0;
     {
       const T *hs = row_in<T, (V > 1)>(stage, a.src[0], 0, row, d), *ys = row_in<T, (V > 1)>(stage, a.src[1], 1, row, d);
@@ -471,10 +472,9 @@ __global__ void __launch_bounds__(512, E == kFew ? 2 : 1) ring_grad_kernel(const
       }
 #pragma unroll
       for (int k = 0; k < H; ++k) {
-        const f32x2 yy = pair(y[2 * k], y[2 * k + 1]);
-        h[k] = pair(x[2 * k], x[2 * k + 1]);
-        t2[k] = mul2(yy, g[k]), p[k] = mul2(yy, h[k]);
-        ss = fma2(h[k], h[k], ss), th = fma2(p[k], g[k], th);
+        h[k] = pair(x[2 * k], x[2 * k + 1]), y2[k] = pair(y[2 * k], y[2 * k + 1]);
+        t2[k] = mul2(y2[k], g[k]);
+        ss = fma2(h[k], h[k], ss), th = fma2(t2[k], h[k], th);
       }
     }
     // both sums side by side in a pair
@@ -493,11 +493,11 @@ __global__ void __launch_bounds__(512, E == kFew ? 2 : 1) ring_grad_kernel(const
     }
     float sq, dot;
     unpair(sum, sq, dot);
-    const float r = rsqrtf(fmaf(sq, by, a.eps)), c = -r * r * r * (dot * by);
+    const float r = rsqrtf(fmaf(sq, by, a.eps)), c = -(dot * r * by * r);  // (r^3 alone would leave the range)
     const f32x2 r2 = pair(r, r), c2 = pair(c, c);
     const T *ds = a.src[2].p ? row_in<T, (V > 1)>(stage, a.src[2], 2, row, d) : nullptr;
 #pragma unroll
-    for (int k = 0; k < H; ++k) dg[k] = fma2(p[k], r2, dg[k]);
+    for (int k = 0; k < H; ++k) h[k] = mul2(h[k], r2), dg[k] = fma2(y2[k], h[k], dg[k]);  // (h r from here on)
 #pragma unroll
     for (int j = 0; j < C; ++j) {
       const int i = (j * G + t) * V;
