@@ -311,7 +311,10 @@ int aecct_aap_linear(const int8_t *codes, int64_t ldc, const float *scale, const
  *   db[n]    = sum_m dy[m][n].
  *   dy  [M][N] of dtype, lddy apart;  dx  [M][K] of dtype;  dw  [N][K] of wdtype;  db  fp32 [N].
  * dx, dw and db may be NULL where they are not wanted.  Products are of dy's own values with the integers;
- * dy scale[m] is cut to 16 bits for a dw in AECCT_BF16 or AECCT_F16, and rounded to 24 for one in AECCT_F32.  Sums are in 32 bits.  M == 0 makes dw and db zero.  Errors: as above. */
+ * dy scale[m] is cut to 16 bits for a dw in AECCT_BF16 or AECCT_F16, and rounded to 24 for one in AECCT_F32.  Sums
+ * are in 32 bits, in parts: the tensor cores' additions cut off up to 2^-23 of what is there, so that a part is 28 of
+ * them at most for results in AECCT_F32, 1,024 for AECCT_F16 and 8,192 for AECCT_BF16, and parts are added
+ * rounded.  M == 0 makes dw and db zero.  Errors: as above. */
 int aecct_aap_linear_backward_workspace(int64_t M, int64_t K, int64_t N, int32_t dtype, int32_t wdtype, int64_t *bytes);
 int aecct_aap_linear_backward(const void *dy, int64_t lddy, const int8_t *codes, int64_t ldc, const float *scale,
                               const uint8_t *packed, const float *w_scale, int64_t M, int64_t K, int64_t N,

@@ -43,17 +43,17 @@ constexpr int64_t kFloat = sizeof(float);
 
 }  // namespace
 
-// the staged codes, and the splits' sums
+// the staged codes, and the splits' sums (of integers, so that they hang on no type)
 int64_t aap_linear_workspace(int64_t M, int64_t K, int64_t N) {
   const int sms = sm_count();
   if (M <= kIntegerTokens) return 0;
   if (pair_tiles(N, M, sms)) {
-    if (stages_codes(N)) return partial_floats<WeightsK, Staged, 256, 2>(N, M, K, sms) * kFloat + 2 * M * staged_k(K);
-    return partial_floats<WeightsK, CodesK<128>, 256, 2>(N, M, K, sms) * kFloat;
+    if (stages_codes(N)) return partial_floats<WeightsK, Staged, 256, 2>(N, M, K, sms, 0) * kFloat + 2 * M * staged_k(K);
+    return partial_floats<WeightsK, CodesK<128>, 256, 2>(N, M, K, sms, 0) * kFloat;
   }
   return with_forward_tile(M, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
-    return partial_floats<WeightsK, CodesK<TB>, TB, 1>(N, M, K, sms) * kFloat;
+    return partial_floats<WeightsK, CodesK<TB>, TB, 1>(N, M, K, sms, 0) * kFloat;
   });
 }
 

@@ -150,7 +150,7 @@ __device__ __forceinline__ void store_split8(const float (&v)[8], uint32_t addr,
 // or rows are not such, zeros beyond; aligned(): rows are; and store(thread, regs, step of the span, tile).
 // A row or column of the tile past the operand's last one reads that one again: its products are dropped.
 // A B also has kBf (bfloat16 or half) and P (pieces of an element), an A kMixed (its rows are in the order of
-// mix16).  The forward product's operands span two steps: the first takes k = 0 .. 3 and 8 .. 11 of every 16 k, the
+// mix16) and kExact (its sums are integers that 32 bits hold).  The forward product's operands span two steps: the first takes k = 0 .. 3 and 8 .. 11 of every 16 k, the
 // second the others, so that a load is 16 bytes of codes and a row's 128 bytes are one line.
 
 // 4 W bytes at any p, of which the first `left` are in range, the others zeros: aligned words that hold any of them, shifted.
@@ -194,7 +194,7 @@ __device__ __forceinline__ void load_weights(const uint8_t *p, int left, int uni
 
 // A(i = n, r = k): 2-bit weights, K-major, mixed order along k.  A thread holds 64 weights of one row.
 struct WeightsK {
-  static constexpr bool kMN = false, kMixed = false;
+  static constexpr bool kMN = false, kMixed = false, kExact = true;
   static constexpr int kSpan = 2, kRegs = 4;
   const uint8_t *packed;
   int64_t N, K;
@@ -233,7 +233,7 @@ struct WeightsK {
 // bits mixed.  A thread holds 32 k of one n.
 template <bool BF>
 struct WeightsT {
-  static constexpr bool kMN = true, kMixed = true;
+  static constexpr bool kMN = true, kMixed = true, kExact = false;
   static constexpr int kSpan = 1, kRegs = 2;
   const uint8_t *packed;
   int64_t N, K;
@@ -341,7 +341,7 @@ struct CodesK {
 // A(i = k, r = m): int8 codes as bfloat16, MN-major.  A thread holds 16 codes of each of 2 m, and stores their
 // two pieces in an order that gives eight lanes eight bank groups.
 struct CodesT {
-  static constexpr bool kMN = true, kMixed = false;
+  static constexpr bool kMN = true, kMixed = false, kExact = false;
   static constexpr int kSpan = 1, kRegs = 8;
   static_assert(2 * kPass == kStep, "two passes are a step's tokens");
   const int8_t *codes;
@@ -659,6 +659,10 @@ struct GemmShape {
   // added in registers: 28 additions to a part at most.
   static constexpr int kSets = B::P == 3 ? 4 : 1;
   static constexpr int kChunk = 20;  // a multiple of the producers' groups
+  // Results of 16 bits have one sum, of so many additions at most (four a step and piece) that it loses a quarter of what
+  // rounding it to its type does: 1,024 in half, 2^-13, and 8,192 in bfloat16, 2^-10.  Longer ones are split (gemm_plan: dW of
+  // 20,000 x 4,096 x 4,096 in half 895 us in three parts, in bfloat16 785 us whole).
+  static constexpr int most_steps(int dtype) { return (dtype == 2 ? 2048 : 256) / B::P; }
   // (Pairs wait for each other's tensor memory, so no mix of these products, of any streams, may run short of it: one of
   // more than half has an SM's shared memory to itself, and of the others a third CTA does not fit that.)
   static constexpr uint32_t kTmemCols = TB * kSets < 32 ? 32 : TB * kSets;
@@ -1069,14 +1073,17 @@ bool grads_vec(const void *dy, int64_t ld, int64_t N) {
 // (16 x 4,096 x 4,096: 8.4 and 9.4 us).  Wider tiles are slower so (64 x 4,096 x 4,096: 11.7 us in clusters, 11.1 us without;
 // 300 x 2,048 x 2,048: 17.7 and 13.2 us), and so are clusters of 8, which wait for 8 SMs of one kind
 // (16 x 16,384 x 2,048: 21.9 and 13.0 us).
+//
+// Sums that are not exact are split too where one accumulator would take more additions than it should (most_steps).
 struct GemmPlan {
   int64_t tiles_i, tiles_j;
   int splits, steps;
   bool cluster;
 };
 constexpr int kMinSteps = 8;
+constexpr int64_t kMaxSplits = 65535;  // of a grid (2^29 tokens, or outputs, and more have longer sums)
 template <class A, class B, int TB, int CG>
-GemmPlan gemm_plan(int64_t I, int64_t J, int64_t R, int sms) {
+GemmPlan gemm_plan(int64_t I, int64_t J, int64_t R, int sms, int dtype) {
   GemmPlan p;
   p.tiles_i = (I + CG * kTileI - 1) / (CG * kTileI) * CG, p.tiles_j = (J + TB - 1) / TB;
   const int64_t all = (R + kStep - 1) / kStep;
@@ -1086,6 +1093,10 @@ GemmPlan gemm_plan(int64_t I, int64_t J, int64_t R, int sms) {
   if (B::P == 3 && CG == 1 && all > S::kChunk * (splits < 1 ? 1 : splits)) splits = S::kCtasPerSm * static_cast<int64_t>(sms) / tiles;
   if (splits > all / (CG * kMinSteps)) splits = all / (CG * kMinSteps);
   if (splits < 1) splits = 1;
+  if (!A::kExact && B::P < 3) {
+    const int64_t least = (all + S::most_steps(dtype) - 1) / S::most_steps(dtype);
+    if (splits < least) splits = least < kMaxSplits ? least : kMaxSplits;
+  }
   p.cluster = S::kClusters && splits > 1 && splits < 8;
   if (p.cluster) splits = splits >= 4 ? 4 : 2;  // (a power of two, as it divides the tile's columns)
   const int64_t steps = (all + splits - 1) / splits;
@@ -1096,8 +1107,8 @@ GemmPlan gemm_plan(int64_t I, int64_t J, int64_t R, int sms) {
 }
 // floats of workspace that the splits' sums take, or those of their chunks
 template <class A, class B, int TB, int CG>
-int64_t partial_floats(int64_t I, int64_t J, int64_t R, int sms) {
-  const GemmPlan p = gemm_plan<A, B, TB, CG>(I, J, R, sms);
+int64_t partial_floats(int64_t I, int64_t J, int64_t R, int sms, int dtype) {
+  const GemmPlan p = gemm_plan<A, B, TB, CG>(I, J, R, sms, dtype);
   const bool carries = B::P == 3 && CG == 1 && p.steps > GemmShape<A, B, TB, CG>::kChunk;
   return (p.splits > 1 && !p.cluster) || carries ? p.splits * I * J : 0;
 }
@@ -1107,7 +1118,7 @@ template <class A, class B, class Out, int TB, int CG>
 cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b, const Out &out, float *partial, int sms, int *err,
                         Order order, cudaStream_t st) {
   using S = GemmShape<A, B, TB, CG>;
-  const GemmPlan p = gemm_plan<A, B, TB, CG>(I, J, R, sms);
+  const GemmPlan p = gemm_plan<A, B, TB, CG>(I, J, R, sms, out.dtype);
   const int64_t ctas = p.tiles_i * p.tiles_j * p.splits;
   const int stages = S::stages(S::kCtasPerSm == 2 && ctas > sms);
   const GemmArgs<A, B, Out> g = {I, J, R, a, b, out, static_cast<int>(p.tiles_i), p.steps,

@@ -72,17 +72,17 @@ cudaError_t input_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t s
 }
 
 template <typename T>
-int64_t input_grad_workspace(int64_t M, int64_t K, int64_t N) {
+int64_t input_grad_workspace(int64_t M, int64_t K, int64_t N, int dtype) {
   const int sms = sm_count();
-  if (grad_pairs(K, M, N, sms)) return partial_floats<Weights<T>, Staged<T>, kPairTile<kPieces<T>>, 2>(K, M, N, sms) * kFloat + 2 * kPieces<T> * M * padded(N);
+  if (grad_pairs(K, M, N, sms)) return partial_floats<Weights<T>, Staged<T>, kPairTile<kPieces<T>>, 2>(K, M, N, sms, dtype) * kFloat + 2 * kPieces<T> * M * padded(N);
   return with_single_tile<kPieces<T>>(M, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
-    return partial_floats<Weights<T>, GradK<T, TB>, TB, 1>(K, M, N, sms) * kFloat + (stages_rows<T>(K) ? up16(2 * M * padded(N)) : 0);
+    return partial_floats<Weights<T>, GradK<T, TB>, TB, 1>(K, M, N, sms, dtype) * kFloat + (stages_rows<T>(K) ? up16(2 * M * padded(N)) : 0);
   });
 }
 
 int64_t input_part(int64_t M, int64_t K, int64_t N, int dtype) {
-  return up16(dtype == 0 ? input_grad_workspace<float>(M, K, N) : input_grad_workspace<__half>(M, K, N));
+  return up16(dtype == 0 ? input_grad_workspace<float>(M, K, N, dtype) : input_grad_workspace<__half>(M, K, N, dtype));
 }
 
 }  // namespace

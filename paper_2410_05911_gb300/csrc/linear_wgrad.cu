@@ -55,12 +55,12 @@ cudaError_t weight_grad(const AapLinearGradCall &c, uint8_t *work, Order order, 
 }
 
 template <int P>
-int64_t workspace_of(int64_t M, int64_t K, int64_t N) {
+int64_t workspace_of(int64_t M, int64_t K, int64_t N, int wdtype) {
   const int sms = sm_count();
-  if (grad_pairs(K, N, M, sms)) return partial_floats<CodesT, Staged<P>, kPairTile<P>, 2>(K, N, M, sms) * kFloat + 2 * P * M * padded(N);
+  if (grad_pairs(K, N, M, sms)) return partial_floats<CodesT, Staged<P>, kPairTile<P>, 2>(K, N, M, sms, wdtype) * kFloat + 2 * P * M * padded(N);
   return with_single_tile<P>(N, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
-    return partial_floats<CodesT, GradT<float, TB, P>, TB, 1>(K, N, M, sms) * kFloat;
+    return partial_floats<CodesT, GradT<float, TB, P>, TB, 1>(K, N, M, sms, wdtype) * kFloat;
   });
 }
 
@@ -68,7 +68,7 @@ int64_t workspace_of(int64_t M, int64_t K, int64_t N) {
 
 // the column sums, and after them the staged pieces and the splits' sums
 int64_t weight_grad_workspace(int64_t M, int64_t K, int64_t N, int wdtype) {
-  return sums_bytes(M, N) + (pieces_of(wdtype) == 3 ? workspace_of<3>(M, K, N) : workspace_of<2>(M, K, N));
+  return sums_bytes(M, N) + (pieces_of(wdtype) == 3 ? workspace_of<3>(M, K, N, wdtype) : workspace_of<2>(M, K, N, wdtype));
 }
 
 cudaError_t launch_weight_grad(const AapLinearGradCall &c, uint8_t *work, bool beside, cudaStream_t st) {

@@ -50,3 +50,37 @@ def test_terms_alike(M, K, N):
     codes, scale = torch.ones((M, K), device="cuda", dtype=torch.int8), torch.full((M,), 1 + 0.9 / 256, device="cuda")
     dy = torch.ones((M, N), device="cuda", dtype=torch.bfloat16)
     check(dy, codes, scale, A.aap_linear_backward(dy, codes, scale, packed, w_scale, weight_dtype=torch.bfloat16)[1])
+
+
+# The longest sums, of one sign: a part of at most 1,024 additions (8,192 for bfloat16) loses 2^-23 of itself at each, however
+# long the whole is, and up to 64 parts are added with 2^-24 each.
+LONG = {torch.float16: 2.0 ** -13 + 64 * 2.0 ** -24, torch.bfloat16: 2.0 ** -10 + 64 * 2.0 ** -24}
+
+
+def check_long(got, w, factor):
+    own = (w.to(got.dtype).double() - w).abs()
+    assert ((got.double() - w).abs() <= own + 2 * (LONG[got.dtype] + factor) * w).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_sums_over_many_tokens(dtype):
+    M, K, N = 262149, 1536, 1792
+    g = torch.Generator(device="cuda").manual_seed(1)
+    dy = (torch.rand((M, N), device="cuda", generator=g) + 0.5).to(dtype)
+    q = torch.randint(1, 128, (K,), device="cuda", generator=g, dtype=torch.int8)
+    codes, scale = q.repeat(M, 1), torch.full((M,), 1.1e-3, device="cuda")
+    packed, w_scale = torch.zeros(N * K // 4, device="cuda", dtype=torch.uint8), torch.ones(1, device="cuda")
+    dw = A.aap_linear_backward(dy, codes, scale, packed, w_scale, weight_dtype=dtype, want=(False, True, False))[1]
+    sums = sum(part.double().sum(0) for part in dy.split(1 << 14)) * scale[0].double()
+    check_long(dw, sums[:, None] * q.double(), 2.0 ** -15)
+
+
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+def test_sums_over_many_outputs(dtype):
+    M, K, N = 1536, 1792, 262144
+    dy = (torch.rand((M, N), device="cuda", generator=torch.Generator(device="cuda").manual_seed(2)) + 0.5).to(dtype)
+    codes, scale = torch.zeros((M, K), device="cuda", dtype=torch.int8), torch.ones(M, device="cuda")
+    packed, w_scale = torch.full((N * K // 4,), 0x55, device="cuda", dtype=torch.uint8), torch.full((1,), 0.037, device="cuda")
+    dx = A.aap_linear_backward(dy, codes, scale, packed, w_scale, want=(True, False, False))[0]
+    sums = torch.stack([row.double().sum() for row in dy]) * w_scale.double()
+    check_long(dx, sums[:, None].expand(M, K), 0.0)
