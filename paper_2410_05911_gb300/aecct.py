@@ -452,7 +452,9 @@ def rms_quant(x, gain, residual=None, eps: float = 1e-6, want_values: bool = Fal
     row (the last dimension) at a time, on `stream` after what is queued on the current one.
 
     x and residual are float32, float16 or bfloat16, gain is float32 [d], all on the current CUDA device (as
-    are the tensors of the functions below; others are refused).  Returns (codes int8 like x, scale float32
+    are the tensors of the functions below; others are refused).  Nothing is recorded for autograd: tensors that
+    require a gradient are refused unless under torch.no_grad(), or in the forward or backward of an
+    autograd.Function (here and in the three functions below).  Returns (codes int8 like x, scale float32
     x.shape[:-1], total, values): codes * scale is the norm's output; total is h in x's type (x itself
     without a residual); values is codes * scale in x's type, or None."""
     return (_binding or _operators()).rms_quant(x, gain, residual, eps, bool(want_values), stream)

@@ -9,6 +9,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -89,6 +90,15 @@ void check_current(const at::Device &on) {
     throw ValueError("the tensors are on " + on.str() + ", which is not the current CUDA device");
 }
 
+// The operators record nothing for autograd (int8 codes stand between the norm and the product): where it would
+// record, a tensor that requires a gradient is refused, and does not lose it without a word.
+void check_no_graph(const char *call, std::initializer_list<const at::Tensor *> tensors) {
+  if (!c10::GradMode::is_enabled()) return;
+  for (const at::Tensor *t : tensors)
+    if (t && t->requires_grad())
+      throw ValueError(std::string(call) + " records nothing for autograd: call it under torch.no_grad(), in an autograd.Function, or on detached tensors");
+}
+
 // `t` holds rows of a known type on the GPU, and `gain` one float32 for each element of a row
 void check_rows(const char *name, const at::Tensor &t, const at::Tensor &gain) {
   if (!t.is_cuda() || element(t.scalar_type()) < 0 || t.dim() < 1)
@@ -142,6 +152,7 @@ PyObject *rms_quant(PyObject *const *a) {
   const at::Tensor *residual = optional_tensor(a[2], "residual");
   check_rows("x", x, gain);
   if (residual) check_like("residual", *residual, x);
+  check_no_graph("rms_quant", {&x, &gain, residual});
   const Rows src(x), res = residual ? Rows(*residual) : Rows();
   const at::Tensor g = gain.contiguous();
   const at::Tensor codes = make(x.sizes(), x, at::kChar), scale = make(x.sizes().slice(0, x.dim() - 1), x, at::kFloat);
@@ -163,6 +174,7 @@ PyObject *rms_quant_backward(PyObject *const *a) {
   check_rows("dy", dy, gain);
   check_like("total", total, dy);
   if (dtotal) check_like("dtotal", *dtotal, dy);
+  check_no_graph("rms_quant_backward", {&dy, &total, &gain, dtotal});
   const int64_t d = dy.size(-1), rows = d ? dy.numel() / d : 0;
   int64_t bytes = 0;
   check(aecct_rms_quant_backward_workspace(rows, static_cast<int32_t>(d), &bytes), "aecct_rms_quant_backward");
@@ -219,6 +231,7 @@ PyObject *aap_linear(PyObject *const *a) {
   const int32_t dtype = element_arg(a[5], "dtype");
   if (bias && (bias->device() != l.codes.device() || bias->scalar_type() != at::kFloat || bias->dim() != 1 || bias->size(0) != l.N))
     throw ValueError("bias must be a float32 tensor of shape (" + std::to_string(l.N) + ",) on the codes' device");
+  check_no_graph("aap_linear", {&l.scale, &l.w_scale, bias});
   int64_t bytes = 0;
   check(aecct_aap_linear_workspace(l.M, l.K, l.N, &bytes), "aecct_aap_linear");
   const Rows q(l.codes);
@@ -242,6 +255,7 @@ PyObject *aap_linear_backward(PyObject *const *a) {
   if (dy.device() != l.codes.device() || element(dy.scalar_type()) < 0 || dy.sizes() != at::IntArrayRef(shape))
     throw ValueError("dy must be a float32, float16 or bfloat16 tensor of shape " + shape_of(shape) + " on the codes' device");
   const int32_t dtype = element(dy.scalar_type());
+  check_no_graph("aap_linear_backward", {&dy, &l.scale, &l.w_scale});
   int64_t bytes = 0;
   check(aecct_aap_linear_backward_workspace(l.M, l.K, l.N, dtype, wdtype, &bytes), "aecct_aap_linear_backward");
   const Rows g(dy), q(l.codes);
