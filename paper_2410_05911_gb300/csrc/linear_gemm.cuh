@@ -1187,7 +1187,7 @@ struct StageGrads {
   void *out;           // [pieces][M][N up to a multiple of 8] 16-bit, or NULL
   float *db;           // [N] column sums, or NULL
   float *partial;      // [stage_parts(M, N)][N] with db
-  Order order;         // to the kernel before it on the stream
+  Order order;         // kFirst or kBeside: it reads nothing that a call writes
 };
 int stage_parts(int64_t M, int64_t N);
 cudaError_t launch_stage_codes(const int8_t *codes, int64_t ld, int64_t M, int64_t K, void *out, cudaStream_t st);

@@ -41,7 +41,6 @@ __global__ void __launch_bounds__(kStageThreads) stage_grads_kernel(const T *dy,
                                                                     const float *scale, uint16_t *out, float *partial, Order order) {
   __shared__ float sums[8][256];
   grid_trigger();
-  if (order == Order::kAfter) grid_wait();
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   const int64_t n = static_cast<int64_t>(blockIdx.x) * 256 + 8 * lane;
   const int left = static_cast<int>(N - n < 8 ? N - n : 8);
