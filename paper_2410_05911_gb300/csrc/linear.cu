@@ -23,12 +23,13 @@ namespace {
 
 using Staged = Tiled<128, false, false, 1, WeightsK::kSpan>;
 
-// Whether a pair's product reads staged codes: staging costs its bytes, and saves each tile along N the conversion
-// (8,192 x 4,096 codes: 15 us; their product with 1,024 weights 51 us converted, 40 us staged, with 4,096 207 and 162).
-bool stages_codes(int64_t N) { return N >= 1536; }
+// Whether a pair's product reads staged codes: staging costs its bytes, and saves each tile of 256 along N the conversion
+// (8,192 x 4,096 codes, with 512 weights 38.7 us converted, 39.4 us with 15 us of staging, with 768 67 and 58 us, with 4,096
+// 226 and 169).
+bool stages_codes(int64_t N) { return N > 512; }
 
-// The products of so few tokens that reading the weights is the work (linear_few.cu): 1 token 3.6 us, 8.4 us on the
-// tensor cores, 4 tokens 5.3 and 8.6 us at 4,096 x 4,096, 13.6 and 17 us at 16,384 x 4,096; a token more costs 1.5 us there,
+// The products of so few tokens that reading the weights is the work (linear_few.cu): 1 token 3.7 us, 8.4 us on the
+// tensor cores, 4 tokens 5.4 and 8.5 us at 4,096 x 4,096, 13.6 and 18.6 us at 16,384 x 4,096; a token more costs 1.5 us there,
 // and next to nothing on the tensor cores.
 constexpr int64_t kIntegerTokens = 4;
 

@@ -1064,13 +1064,13 @@ bool grads_vec(const void *dy, int64_t ld, int64_t N) {
 
 // How the sum over R is split where there are fewer tiles than SMs: into as many parts as SMs are left for, of at least
 // kMinSteps steps each (a pair's, with four times the sums of a single tile: twice as many; dX of 2,048 x 1,024 x 1,024
-// whole 11.4 us, in two parts of 8 steps 18.1 us), whose sums a second kernel joins.  Two CTAs to an SM for the parts'
-// sake lose more in the joining than they gain (8,192 x 4,096 x 512 46 us whole, 59 us in two parts; 37 x 4,096 x 16,384
-// 20 and 27 us), but not where parts of 32-bit sums are longer than a chunk and stop at its end (dX of 2,048 x 512 x
-// 16,384 in single tiles: 249 and 219 us; shorter parts, dW of 23,040 x 128 x 512: 23 us in 19, 26 us in 38).
+// whole 11.1 us, in two parts of 8 steps 18.3 us), whose sums a second kernel joins.  Two CTAs to an SM for the parts'
+// sake lose more in the joining than they gain (8,192 x 4,096 x 512 39 us whole, 59 us in two parts; 37 x 4,096 x 16,384
+// 20 and 25 us), but not where parts of 32-bit sums are longer than a chunk and stop at its end (dX of 2,048 x 512 x
+// 16,384 in single tiles: 249 and 219 us; shorter parts, dW of 23,040 x 128 x 512: 23 us in 19, 27 us in 38).
 //
 // Up to 4 parts of a tile of 16 j are a cluster, which joins them itself: there the second kernel would be an eighth of the time
-// (16 x 4,096 x 4,096: 8.4 and 9.4 us).  Wider tiles are slower so (64 x 4,096 x 4,096: 11.7 us in clusters, 11.1 us without;
+// (16 x 4,096 x 4,096: 8.6 and 9.7 us).  Wider tiles are slower so (64 x 4,096 x 4,096: 11.7 us in clusters, 11.1 us without;
 // 300 x 2,048 x 2,048: 17.7 and 13.2 us), and so are clusters of 8, which wait for 8 SMs of one kind
 // (16 x 16,384 x 2,048: 21.9 and 13.0 us).
 //
@@ -1153,7 +1153,7 @@ cudaError_t launch_gemm(int64_t I, int64_t J, int64_t R, const A &a, const B &b,
 }
 
 // The tile of a product.  A pair's 256 x 256 where those fill half of the SMs at least (2,048 x 1,024 x 1,024: 64 CTAs in
-// pairs 16.7 us, 128 single ones 12.7 us; 1,024 x 4,096 x 4,096: 128 in pairs 46 us, 256 single ones 58 us), else a
+// pairs 14.6 us, 128 single ones 9.8 us; 1,024 x 4,096 x 4,096: 128 in pairs 28 us, 256 single ones 50 us), else a
 // single CTA's, of 64 j at most where there are no more (the rest of a tile would be converted zeros) or three pieces of
 // more would leave an SM one CTA, of 128.
 template <int P>
@@ -1162,14 +1162,17 @@ inline bool pair_tiles(int64_t I, int64_t J, int sms) {
   return I > kTileI && J > kTileI && 2 * ((I + 255) / 256 * 2) * ((J + 255) / 256) >= sms;
 }
 // The gradients' products, of any R, also where single tiles would take each SM through many steps: they convert dy for
-// every 128 k, a pair's once for 256, from rows that lie there or are laid out once (kLongSteps single steps an SM: dW of
-// 20,000 x 1,088 x 784 (tokens, K, N) 130 steps, 102 us in single tiles, 65 us in pairs, in 32 bits 292 and 142 us; dX of
-// 1,500 x 1,088 x 784 9 steps, 12.8 and 10.1 us; dW of 5,000 x 512 x 512 8 steps, 13.5 and 17.6 us).  With up to 256 k dy is
-// not read often enough to be laid out (dW of 20,000 x 256 x 1,024: 28 us in single tiles, 36 us in pairs).
-constexpr int64_t kLongSteps = 9;
-inline bool grad_pairs(int64_t I, int64_t J, int64_t R, int sms) {
+// every 128 k, a pair's once for 256, from rows that lie there or are laid out once (long_steps single steps an SM: dW of
+// 20,000 x 1,088 x 784 (tokens, K, N) 130 steps, 151 us in single tiles, 88 us in pairs, in 32 bits 291 and 142 us; dX of
+// 1,500 x 1,088 x 784 9 steps, 12.7 and 9.9 us.  Of dW's two pieces there is the most to lay out for the least to convert: 3,000 x
+// 768 x 1,024 15 steps, 25.2 and 29.9 us; 6,000 x 512 x 1,024 20 steps, 31.7 and 29.4 us).  With up to 256 k dy is
+// not read often enough to be laid out (dW of 20,000 x 256 x 1,024: 40 us in single tiles, 47 us in pairs).
+template <int P>
+constexpr int64_t long_steps = P == 2 ? 16 : 9;
+template <int P>
+bool grad_pairs(int64_t I, int64_t J, int64_t R, int sms) {
   const int64_t steps = ((I + kTileI - 1) / kTileI) * ((J + 127) / 128) * ((R + kStep - 1) / kStep);
-  return pair_tiles(I, J, sms) || (I > 2 * kTileI && J > kTileI && steps >= kLongSteps * sms);
+  return pair_tiles(I, J, sms) || (I > 2 * kTileI && J > kTileI && steps >= long_steps<P> * sms);
 }
 template <int P, class F>
 auto with_single_tile(int64_t J, const F &f) {

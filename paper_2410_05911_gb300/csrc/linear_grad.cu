@@ -39,7 +39,7 @@ cudaError_t input_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t s
   const Weights<T> a = {c.packed, c.N, c.K, weights_unit(c.packed, c.K)};
   const OutX out = {c.dx, c.dtype, c.K, c.w_scale};
   const int sms = sm_count();
-  if (grad_pairs(c.K, c.M, c.N, sms)) {
+  if (grad_pairs<kPieces<T>>(c.K, c.M, c.N, sms)) {
     Staged<T> b;
     const void *rows = c.dy;
     int64_t ld = c.lddy;
@@ -74,7 +74,7 @@ cudaError_t input_grad(const AapLinearGradCall &c, uint8_t *work, cudaStream_t s
 template <typename T>
 int64_t input_grad_workspace(int64_t M, int64_t K, int64_t N, int dtype) {
   const int sms = sm_count();
-  if (grad_pairs(K, M, N, sms)) return partial_floats<Weights<T>, Staged<T>, kPairTile<kPieces<T>>, 2>(K, M, N, sms, dtype) * kFloat + 2 * kPieces<T> * M * padded(N);
+  if (grad_pairs<kPieces<T>>(K, M, N, sms)) return partial_floats<Weights<T>, Staged<T>, kPairTile<kPieces<T>>, 2>(K, M, N, sms, dtype) * kFloat + 2 * kPieces<T> * M * padded(N);
   return with_single_tile<kPieces<T>>(M, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
     return partial_floats<Weights<T>, GradK<T, TB>, TB, 1>(K, M, N, sms, dtype) * kFloat + (stages_rows<T>(K) ? up16(2 * M * padded(N)) : 0);

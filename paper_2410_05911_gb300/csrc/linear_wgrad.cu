@@ -57,7 +57,7 @@ cudaError_t weight_grad(const AapLinearGradCall &c, uint8_t *work, Order order, 
 template <int P>
 int64_t workspace_of(int64_t M, int64_t K, int64_t N, int wdtype) {
   const int sms = sm_count();
-  if (grad_pairs(K, N, M, sms)) return partial_floats<CodesT, Staged<P>, kPairTile<P>, 2>(K, N, M, sms, wdtype) * kFloat + 2 * P * M * padded(N);
+  if (grad_pairs<P>(K, N, M, sms)) return partial_floats<CodesT, Staged<P>, kPairTile<P>, 2>(K, N, M, sms, wdtype) * kFloat + 2 * P * M * padded(N);
   return with_single_tile<P>(N, [&](auto tb) {
     constexpr int TB = decltype(tb)::value;
     return partial_floats<CodesT, GradT<float, TB, P>, TB, 1>(K, N, M, sms, wdtype) * kFloat;
@@ -75,7 +75,8 @@ cudaError_t launch_weight_grad(const AapLinearGradCall &c, uint8_t *work, bool b
   Order order = beside ? Order::kBeside : Order::kFirst;
   const int p = pieces_of(c.wdtype);
   uint8_t *rest = work + sums_bytes(c.M, c.N);
-  const bool staged = c.dw && grad_pairs(c.K, c.N, c.M, sm_count());
+  const int sms = sm_count();
+  const bool staged = c.dw && (p == 3 ? grad_pairs<3>(c.K, c.N, c.M, sms) : grad_pairs<2>(c.K, c.N, c.M, sms));
   if (staged || c.db) {
     const StageGrads s = {c.dy, c.lddy, c.M, c.N, c.dtype, c.scale, staged ? p : 0, staged ? rest : nullptr, c.db,
                           reinterpret_cast<float *>(work), order};

@@ -20,7 +20,7 @@ def shifted(t, at, pad=0):
 
 @pytest.mark.parametrize("at,pad", [(1, 0), (3, 2), (4, 0), (15, 17)])
 @pytest.mark.parametrize("M,K,N", [(1, 64, 40), (2, 4, 1), (4, 4096, 33), (5, 100, 70), (16, 512, 128), (70, 1028, 130), (300, 256, 300),
-                                   (2300, 260, 1030), (2048, 100, 2500)])
+                                   (2300, 260, 1030), (2048, 100, 2500), (9800, 68, 300), (5000, 1100, 700)])
 def test_forward(M, K, N, at, pad):
     c, s, p, w, b = make(M, K, N, 1)
     c = shifted(c, at, pad)

@@ -13,8 +13,9 @@ from paper_2410_05911_gb300 import aecct as A
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-# single tiles (few tokens, few outputs, many of both), pairs from gradients laid out first
-SHAPES = [(64, 64, 40), (65, 64, 40), (300, 1100, 777), (513, 132, 2048), (3000, 128, 130), (1500, 2048, 1280), (2600, 2500, 2100)]
+# single tiles (few tokens, few outputs, many of both), pairs from gradients laid out first, few of them in parts
+SHAPES = [(64, 64, 40), (65, 64, 40), (300, 1100, 777), (513, 132, 2048), (3000, 128, 130), (1500, 2048, 1280), (2600, 2500, 2100),
+          (14000, 388, 261)]
 
 
 def layer(M, K, N, seed):
