@@ -489,8 +489,8 @@ def aap_linear_backward(dy, codes, scale, packed, w_scale, weight_dtype=None, wa
 
 def clip_gradients(grads, max_norm: float, eps: float = 1e-6, out=None, stream=None):
     """aecct_clip_gradients: scales the tensors `grads` by min(1, max_norm / (norm + eps)), norm the 2-norm over
-    all of their elements, in place or into the tensors `out`.  They are contiguous float32, float16 and bfloat16
-    tensors on the current CUDA device.  Returns norm, a float32 scalar there."""
+    all of their elements, in place or into the tensors `out`, no two of which share memory.  They are contiguous
+    float32, float16 and bfloat16 tensors on the current CUDA device.  Returns norm, a float32 scalar there."""
     import torch
 
     device = 0 if grads else torch.cuda.current_device()

@@ -338,7 +338,7 @@ cudaError_t launch_rms_quant_grad(const RmsQuantGradCall &c, cudaStream_t stream
 
 // linear.cu: the AAP linear layer on int8 codes and 2-bit weights, and its gradients
 constexpr int64_t kLinearMaxRows = int64_t(1) << 31;  // tokens; widths are 32-bit, K at most 65536
-constexpr int kLinearMaxK = 65536;                    // |sum of codes| <= 127 K < 2^24: exact in 32 bits
+constexpr int kLinearMaxK = 65536;                    // |sum of codes| <= 128 K < 2^24: exact in 32 bits
 struct AapLinearCall {
   int64_t M, K, N;
   int dtype;

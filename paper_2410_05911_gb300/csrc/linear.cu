@@ -8,7 +8,7 @@
 //
 // The three products run on the tensor cores (linear_gemm.cuh), a few tokens' forward product in integers
 // (linear_few.cu).  The forward sum is one of integers up to
-// 127 * 65536 < 2^23: exact in 32 bits, and the same however it is split.
+// 128 * 65536 = 2^23: exact in 32 bits, and the same however it is split.
 #include <cuda_runtime.h>
 
 #include <atomic>

@@ -2,11 +2,12 @@
 //
 //   out(j, i) = sum over r of A(i, r) B(j, r),   i < I, j < J, r < R
 //
-// with 16-bit operands that no memory holds: int8 codes, 2-bit weights and scaled gradients become half or
-// bfloat16 core matrices on their way from global to shared memory, in the registers of producer warps, and
-// tcgen05.mma multiplies them there (32-bit accumulators in tensor memory).  Reading 1 byte a code and
-// a quarter of one a weight keeps L2 traffic under what 16-bit operands would need, and no pass over memory
-// lays operands out before the product.
+// with 16-bit operands.  A (2-bit weights, or int8 codes) is in no memory as such: it becomes half or bfloat16 core
+// matrices on its way from global to shared memory, in the registers of producer warps, and tcgen05.mma multiplies them
+// there (32-bit accumulators in tensor memory).  Reading 1 byte a code and a quarter of one a weight keeps L2 traffic
+// under what 16-bit operands would need.  B (codes, or gradients) goes the same way in a single CTA's product; a pair's,
+// which many tiles read, is copied by TMA from 16-bit rows, where they lie or as a pass over memory has laid them out first
+// (linear_stage.cu).
 //
 // A CTA makes a tile of 128 i by TB j; from 256 of both on, a cluster of two makes 256 by 256 (cta_group::2),
 // each CTA with its own 128 rows of A and half of B in shared memory, so that a B is converted and stored by one
@@ -17,8 +18,8 @@
 // operands fit, one's epilogue behind the other's products.
 //
 // What it reaches, and what bounds it: 8,192 x 4,096 x 4,096 (tokens, K, N) the forward product 154 us after 15 us of
-// staging, dX 156 us, dW 178 us after 13 us: 1.78, 1.76 and 1.55 PFLOP/s, the tensor cores 65 to 73% busy, the rest the
-// filling of a tile's first stages and the last wave of tiles.  37 x 4,096 x 16,384 (few tokens: 128 single tiles) 20 us: the
+// staging, dX 156 us, dW 298 us (two products' work) after 31 us: 1.78, 1.76 and 1.85 PFLOP/s, the tensor cores 73 to 78% busy,
+// the rest the filling of a tile's first stages and the last wave of tiles.  37 x 4,096 x 16,384 (few tokens: 128 single tiles) 20 us: the
 // shared memory of an SM, which takes the weights as halves, twice their loads' wavefronts, and gives them to the tensor cores
 // (its pipe 88% busy on the SMs at work).  32-bit gradients, 23,040 x 128 x 512: dX 22 us, dW 23 us, 3 products each, bound
 // by the conversion to three pieces.

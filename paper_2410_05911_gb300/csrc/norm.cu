@@ -77,8 +77,9 @@ struct QuantArgs {
 // The forward pass of rows that start on 16 bytes (or have at most 256 elements).  A row is read once and stays in
 // registers: the sum of squares and the largest |z| come from one reduction, since the codes take no part of r, and the
 // codes, the scale and the values follow without a second look at memory.  Bound by memory, with 9 bytes an element for 16-bit
-// rows and all outputs: 8,192 rows of 4,096 in bfloat16 54 us (5.6 TB/s), 65,536 rows of 128 in float32 27 us (5.4 TB/s).
-// One row: 3.5 us, the launch and two trips to memory.
+// rows and all outputs: 8,192 rows of 4,096 in bfloat16 54 us (5.6 TB/s), 65,536 rows of 128 in float32 26 us (5.4 TB/s);
+// 2,048 rows of 16,384 in bfloat16, a CTA of 1,024 threads each, 74 us (4.1 TB/s).  One row: 3.3 us, the launch and two trips to
+// memory.
 template <typename T, int V, int E, int BLOCK>
 __global__ void __launch_bounds__(BLOCK ? BLOCK : kSmallThreads) rms_quant_kernel(const __grid_constant__ QuantArgs<T> a) {
   __shared__ float2 buf[2][32];
@@ -200,9 +201,10 @@ struct GradArgs {
 
 // A CTA takes every gridDim-th row (or group of rows) and holds the next one's elements, in flight, while it works
 // on one: the sums over a row and their barrier would otherwise stand between its loads and the next row's.
-// Rows of up to 256 elements, by groups of lanes (65,536 rows of 128 in float32: 27 us, 4.9 TB/s), and rows too wide for
-// two of them to fit shared memory (2,048 rows of 16,384 in bfloat16: 93 us, 2.9 TB/s); the others go through a ring
-// (ring_grad_kernel).
+// Rows of up to 256 elements, by groups of lanes (65,536 rows of 128 in float32: 26 us, 5.2 TB/s), and rows too wide for
+// the ring (ring_grad_kernel, which takes the others): past 16,384 elements, or two of them past its shared memory.  Those
+// are bound by registers: 32 elements a thread of a CTA of 1,024 spill 1.4 to 3.1 KB (2,048 rows of 32,768 in bfloat16: 605 us,
+// 0.9 TB/s).
 template <typename T, int V, int E, int BLOCK>
 __global__ void __launch_bounds__(BLOCK ? BLOCK : kSmallThreads) rms_quant_grad_kernel(const __grid_constant__ GradArgs<T> a) {
   __shared__ float2 buf[2][32];
@@ -416,7 +418,8 @@ struct RingGradArgs {
 // (V = 1 where a row or its outputs do not start on 16 bytes).  Bound by memory: 8,192 rows of 4,096 in bfloat16 with
 // `dsum` (8 bytes an element) 44 us and 6 us for dgain's join, 5.4 TB/s in all.  A row is read from shared memory once,
 // its products kept in pairs: with two passes over it in single operations (328 instructions of a thread for 8 elements
-// of 4,096) the instructions were the bound, 56 us for the same rows.
+// of 4,096) the instructions were the bound, 56 us for the same rows.  Rows past 8,192 elements, 32 of them a thread, spill
+// up to 0.5 KB: 2,048 of 16,384 in bfloat16 77 us, 3.5 TB/s.
 template <typename T, int V, int E>
 __global__ void __launch_bounds__(512, E == kFew ? 2 : 1) ring_grad_kernel(const __grid_constant__ RingGradArgs<T> a) {
   extern __shared__ __align__(16) uint8_t ring[];
