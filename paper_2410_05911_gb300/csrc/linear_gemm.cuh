@@ -5,9 +5,9 @@
 // with 16-bit operands.  A (2-bit weights, or int8 codes) is in no memory as such: it becomes half or bfloat16 core
 // matrices on its way from global to shared memory, in the registers of producer warps, and tcgen05.mma multiplies them
 // there (32-bit accumulators in tensor memory).  Reading 1 byte a code and a quarter of one a weight keeps L2 traffic
-// under what 16-bit operands would need.  B (codes, or gradients) goes the same way in a single CTA's product; a pair's,
-// which many tiles read, is copied by TMA from 16-bit rows, where they lie or as a pass over memory has laid them out first
-// (linear_stage.cu).
+// under what 16-bit operands would need.  B (codes, or gradients) goes the same way in a single CTA's product, and in a
+// pair's that few tiles read; where many do, it is copied by TMA from 16-bit rows, as they lie or as a pass over memory has
+// laid them out first (linear_stage.cu).
 //
 // A CTA makes a tile of 128 i by TB j; from 256 of both on, a cluster of two makes 256 by 256 (cta_group::2),
 // each CTA with its own 128 rows of A and half of B in shared memory, so that a B is converted and stored by one
