@@ -336,6 +336,98 @@ int aecct_clip_gradients(int32_t n_tensors, const void *const *grad, const int64
                          void *const *out, float max_norm, float eps, float *norm, void *workspace,
                          int64_t workspace_bytes, void *cuda_stream);
 
+/*
+ * A network of these layers served a token at a time: the keys and values of past tokens in a paged cache, the attention of
+ * one new token over them, and the choice of the next token.
+ */
+#define AECCT_I8 3 /* a cache's codes: the fourth element type, of the calls below alone */
+
+/* A cache of keys and values in pages of page_size tokens:
+ *   k, v              DEVICE [pages][heads][page_size][head_dim] of dtype, rows (of one token and head) ld elements
+ *                     apart; 16-byte aligned, and ld elements are a multiple of 16 bytes.  What lies between a row's
+ *                     end and the next one is never read or written.
+ *   k_scale, v_scale  DEVICE fp32 [pages][heads][page_size]: the scale of each row of codes (dtype AECCT_I8); NULL
+ *                     for rows of AECCT_F16 or AECCT_BF16, which are kept as they are.
+ * Sequence b's token at position p lies in page table[b][p / page_size], at place p % page_size.  A page whose number
+ * is not in [0, pages), and positions past the table's columns, hold nothing: nothing is written there, and what is read
+ * from there counts as absent.  Limits: head_dim <= 256, heads and page_size < 2^20. */
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;
+  int64_t pages;
+  int32_t page_size, heads, head_dim, ld, dtype;
+} aecct_kv_cache;
+
+/* The sequences of a call.  DEVICE arrays:
+ *   table    [batch][columns], ldt apart;  lengths  [batch]: the tokens of each sequence, the call's own new ones among
+ *            them (negative counts as 0; sequences may share pages that the call only reads). */
+typedef struct {
+  const int32_t *table, *lengths;
+  int64_t ldt;
+  int32_t batch, columns;
+} aecct_kv_sequences;
+
+/* New tokens' keys and values into the cache, by eq. Quant for each row x of head_dim elements (AECCT_I8):
+ *   alpha = max(max_i |x_i|, 2^-100); code_i = rint(x_i (127 / alpha)); scale = alpha / 127.
+ * rows[b] .. rows[b + 1] - 1 are the rows of k and v with sequence b's new tokens, which are its last:
+ * row r is position lengths[b] - (rows[b + 1] - r).  Positions below 0 and rows of no sequence are not written.
+ *   k, v  [total][heads][head_dim] of dtype, element (r, h, i) at r ld_row + h ld_head + i; of the cache's own type
+ *         where that is not AECCT_I8.
+ *   rows  DEVICE [batch + 1], ascending; NULL: one new token for each sequence (total = batch).
+ * Two sequences must not write to one page in a call.  A row that holds a NaN or an infinity gets a scale that is not finite, and
+ * codes without meaning.  Errors: INVALID_ARG (a size < 0, a NULL or misaligned pointer, a type that does not fit),
+ * UNSUPPORTED (a size past the limits above), CUDA. */
+int aecct_kv_append(const aecct_kv_cache *cache, const aecct_kv_sequences *seqs, const int32_t *rows, int64_t total,
+                    const void *k, int64_t k_ld_row, int64_t k_ld_head, const void *v, int64_t v_ld_row,
+                    int64_t v_ld_head, int32_t dtype, void *cuda_stream);
+
+/* The same rows read back, codes times scale: row r of k and v [total][heads][head_dim] of dtype (any of the three) is the token that
+ * aecct_kv_append puts at r's position; zeros for absent ones and for rows of no sequence.  Errors: as above. */
+int aecct_kv_read(const aecct_kv_cache *cache, const aecct_kv_sequences *seqs, const int32_t *rows, int64_t total,
+                  void *k, void *v, int32_t dtype, void *cuda_stream);
+
+/* Attention of one new token of each sequence over its cached ones, that is positions j with first[b] <= j < lengths[b]:
+ *   s_j = scale sum_i q_i k_ji;  out = sum_j exp(s_j - max) v_j / sum_j exp(s_j - max);  lse = ln sum_j exp(s_j).
+ * Query heads h G .. h G + G - 1, G = q_heads / heads, attend to the cache's head h.
+ *   q      [batch][q_heads][head_dim] of dtype, element (b, h, i) at b ld_row + h ld_head + i; of the cache's own type
+ *          where that is not AECCT_I8.
+ *   first  DEVICE [batch], or NULL: from position 0.
+ *   out    [batch][q_heads][head_dim] of dtype;  lse  fp32 [batch][q_heads] or NULL.
+ * A sequence with no position to attend to gets zeros, and an lse of minus infinity.  Scales of rows of codes are positive (those of
+ * aecct_kv_append are).  Sums, maxima and the softmax are in 32 bits, in an order that hangs on the lengths of the whole batch and
+ * on nothing else.
+ *   workspace  aecct_paged_attention_workspace bytes, 16-byte aligned; not read before it is written.
+ * Errors: as above, and INVALID_ARG where heads does not divide q_heads, scale is not finite or the workspace is too small. */
+int aecct_paged_attention_workspace(int32_t batch, int32_t q_heads, int32_t heads, int32_t head_dim, int32_t dtype,
+                                    int32_t cache_dtype, int64_t *bytes);
+int aecct_paged_attention(const aecct_kv_cache *cache, const aecct_kv_sequences *seqs, const int32_t *first,
+                          const void *q, int64_t ld_row, int64_t ld_head, int32_t q_heads, int32_t dtype, float scale,
+                          void *out, float *lse, void *workspace, int64_t workspace_bytes, void *cuda_stream);
+
+/* The settings of aecct_sample: a DEVICE array with one for each row, or (NULL) one value for all. */
+typedef struct {
+  const float *temperature_dev, *top_p_dev, *min_p_dev;
+  const int32_t *top_k_dev;
+  float temperature, top_p, min_p;
+  int32_t top_k;
+} aecct_sample_settings;
+
+/* The next token of each row of logits x, given a number u in [0, 1) for it:
+ *   w_i = exp((x_i - max x) / temperature); tokens in descending order of x, the lower index first among equal ones;
+ *   the first top_k of them stay (all for top_k <= 0); of these the shortest beginning whose weight is at least
+ *   top_p of theirs, and no less than one token (all for top_p >= 1); of these the tokens with w_i >= min_p;
+ *   token = the lowest index i among those that stay with sum over j <= i of w_j > u sum over all of w_j.
+ * A temperature of 0 (or less, or NaN) takes the largest logit, the lowest index among equal ones.  Logits of minus infinity
+ * and NaN never stay; a row with no other gets token -1.  Where logits of plus infinity occur only those stay, with equal
+ * weights.  u < 0 or NaN counts as 0, u >= 1 takes the last token that stays.
+ * Weights are fixed-point numbers of 44 bits behind the point and sums of them exact, so that a token hangs on nothing but its row
+ * and its settings.
+ *   logits  [rows][vocab] of dtype, ld apart;  u  fp32 [rows];  tokens  int64 [rows].
+ * Errors: INVALID_ARG (a size < 0, vocab < 1, ld < vocab, a NULL or misaligned pointer, temperature, top_p or min_p not
+ * finite or < 0 where given for all rows), UNSUPPORTED (vocab > 2^19, rows >= 2^31), CUDA. */
+int aecct_sample(const void *logits, int64_t ld, int64_t rows, int32_t vocab, int32_t dtype, const float *u,
+                 const aecct_sample_settings *settings, int64_t *tokens, void *cuda_stream);
+
 /* Wait for the handle's last decode and report whether its kernel stopped on a
  * device-side timeout (AECCT_ERR_TIMEOUT) or a CUDA error occurred. */
 int aecct_synchronize(aecct_handle *h);

@@ -8,7 +8,7 @@ from __future__ import annotations
 
 import ctypes
 import os
-from typing import Optional, Tuple
+from typing import Any, NamedTuple, Optional, Tuple
 
 import numpy as np
 
@@ -29,7 +29,8 @@ EXPORTED_SYMBOLS = (
     "aecct_aap_ternarize_list", "aecct_spe_table", "aecct_rms_quant", "aecct_rms_quant_backward",
     "aecct_rms_quant_backward_workspace", "aecct_clip_gradients", "aecct_clip_workspace",
     "aecct_aap_linear", "aecct_aap_linear_workspace", "aecct_aap_linear_backward",
-    "aecct_aap_linear_backward_workspace",
+    "aecct_aap_linear_backward_workspace", "aecct_kv_append", "aecct_kv_read", "aecct_paged_attention",
+    "aecct_paged_attention_workspace", "aecct_sample",
 )
 
 
@@ -101,6 +102,12 @@ def load(build_if_missing: bool = True):
     L.aecct_aap_linear_backward.argtypes = [P, I64, P, I64, P, P, P, I64, I64, I64, I32, I32, P, P, P, P, I64, P]
     L.aecct_clip_gradients.argtypes = [I32, P, P, P, P, F32, F32, P, P, I64, P]
     L.aecct_clip_workspace.argtypes = [I32, ctypes.POINTER(I64)]
+    K, S = ctypes.POINTER(KVPages), ctypes.POINTER(KVSequences)
+    L.aecct_kv_append.argtypes = [K, S, P, I64, P, I64, I64, P, I64, I64, I32, P]
+    L.aecct_kv_read.argtypes = [K, S, P, I64, P, P, I32, P]
+    L.aecct_paged_attention_workspace.argtypes = [I32, I32, I32, I32, I32, I32, ctypes.POINTER(I64)]
+    L.aecct_paged_attention.argtypes = [K, S, P, P, I64, I64, I32, I32, F32, P, P, P, I64, P]
+    L.aecct_sample.argtypes = [P, I64, I64, I32, I32, P, ctypes.POINTER(SampleSettings), P, P]
     for name in EXPORTED_SYMBOLS:
         fn = getattr(L, name)
         if fn.restype is None or fn.restype is ctypes.c_int:
@@ -134,6 +141,26 @@ def pack_ternary(t: np.ndarray) -> np.ndarray:
         raise ValueError("ternary weights must be in {-1, 0, 1}")
     c = code.reshape(rows, cols // 4, 4)
     return (c[..., 0] | (c[..., 1] << 2) | (c[..., 2] << 4) | (c[..., 3] << 6)).astype(np.uint8)
+
+
+class KVPages(ctypes.Structure):
+    """aecct_kv_cache"""
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("pages", ctypes.c_int64), ("page_size", ctypes.c_int32), ("heads", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("ld", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class KVSequences(ctypes.Structure):
+    """aecct_kv_sequences"""
+    _fields_ = [("table", ctypes.c_void_p), ("lengths", ctypes.c_void_p), ("ldt", ctypes.c_int64), ("batch", ctypes.c_int32),
+                ("columns", ctypes.c_int32)]
+
+
+class SampleSettings(ctypes.Structure):
+    """aecct_sample_settings"""
+    _fields_ = [("temperature_dev", ctypes.c_void_p), ("top_p_dev", ctypes.c_void_p), ("min_p_dev", ctypes.c_void_p),
+                ("top_k_dev", ctypes.c_void_p), ("temperature", ctypes.c_float), ("top_p", ctypes.c_float), ("min_p", ctypes.c_float),
+                ("top_k", ctypes.c_int32)]
 
 
 class _HostModel:
@@ -495,3 +522,69 @@ def clip_gradients(grads, max_norm: float, eps: float = 1e-6, out=None, stream=N
 
     device = 0 if grads else torch.cuda.current_device()
     return (_binding or _operators()).clip_gradients(grads, max_norm, eps, out, device, stream)
+
+
+# ------------------------------------------------------------------------------------------
+# operators of serving a token at a time: a paged cache of keys and values, attention over it, the next token
+# ------------------------------------------------------------------------------------------
+class KVCache(NamedTuple):
+    """A cache of keys and values in pages: k and v [pages, heads, page_size, head_dim] of int8, float16 or bfloat16
+    (rows of the last dimension on 16 bytes), and for int8 k_scale and v_scale float32 [pages, heads, page_size], else
+    None.  Position p of sequence b lies in page table[b, p // page_size], at place p % page_size."""
+    k: Any
+    v: Any
+    k_scale: Any
+    v_scale: Any
+
+
+def kv_cache(pages: int, heads: int, page_size: int, head_dim: int, dtype=None, device=None) -> KVCache:
+    """A KVCache on the current CUDA device (or `device`), int8 unless `dtype` says float16 or bfloat16.  Its memory is as it comes: what no
+    kv_append has written is never attended to."""
+    import torch
+
+    dtype = torch.int8 if dtype is None else dtype
+    if dtype not in (torch.int8, torch.float16, torch.bfloat16):
+        raise ValueError("a cache holds int8, float16 or bfloat16")
+    if min(pages, heads, page_size, head_dim) < 0 or not 1 <= head_dim <= 256:
+        raise ValueError("a cache has no negative size, and rows of 1 to 256 elements")
+    by = 16 if dtype is torch.int8 else 8
+    on = torch.device("cuda", torch.cuda.current_device()) if device is None else device
+    rows = [torch.empty((pages, heads, page_size, -(-head_dim // by) * by), dtype=dtype, device=on)[..., :head_dim] for _ in range(2)]
+    scales = [torch.empty((pages, heads, page_size), dtype=torch.float32, device=on) if dtype is torch.int8 else None for _ in range(2)]
+    return KVCache(*rows, *scales)
+
+
+def kv_append(k, v, cache, table, lengths, rows=None, stream=None) -> None:
+    """aecct_kv_append: new tokens' keys and values k, v [tokens, heads, head_dim] into `cache`, by eq. Quant where that is
+    int8, on `stream` after what is queued on the current one.  table int32 [batch, columns] names each sequence's pages; lengths int32
+    [batch] counts its tokens, the new ones among them, which are its last.  Rows rows[b] .. rows[b + 1] - 1 of k and v
+    (int32 [batch + 1]) are sequence b's; without `rows` each sequence has one new token.  k and v are float32, float16
+    or bfloat16, the cache's own type where it is not int8; slices of a wider tensor are read where they lie.  Tokens without a
+    page and rows of no sequence are not written; two sequences must not write to one page."""
+    (_binding or _operators()).kv_append(k, v, cache, table, lengths, rows, stream)
+
+
+def kv_read(cache, table, lengths, rows, total: int, dtype=None, stream=None):
+    """aecct_kv_read: what kv_append with the same arguments wrote: (k, v) [total, heads, head_dim] of `dtype` (float32 unless given), row by
+    row codes times scale.  Whole sequences where rows counts lengths.  Zeros for tokens without a page and rows of no
+    sequence."""
+    ops = _binding or _operators()
+    return ops.kv_read(cache, table, lengths, rows, total, 0 if dtype is None else _ELEMENT.get(dtype), stream)
+
+
+def paged_attention(q, cache, table, lengths, first=None, scale=None, want_lse: bool = False, stream=None):
+    """aecct_paged_attention: one new token's queries q [batch, q_heads, head_dim] over the keys and values of its sequence in
+    `cache`, positions first[b] .. lengths[b] - 1 (first int32 [batch], or None: from 0; lengths counts the new token, once
+    kv_append has written it).  q_heads is a multiple of the cache's heads, which serve as many query heads each.  scale is 1 / sqrt(head_dim)
+    unless given.  q is float32, float16 or bfloat16, the cache's own type where it is not int8.  Returns (out like q, lse):
+    lse float32 [batch, q_heads] is the log of the sum of exponentials where wanted, else None.  Zeros (and minus infinity) for a
+    sequence with nothing to attend to."""
+    return (_binding or _operators()).paged_attention(q, cache, table, lengths, first, scale, bool(want_lse), stream)
+
+
+def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, stream=None):
+    """aecct_sample: the next token (int64) of each row of `logits` [..., vocab] (float32, float16 or bfloat16), given a random
+    number u in [0, 1) for each (float32, logits.shape[:-1]).  temperature (0: the largest logit), top_k (0: all), top_p and min_p are
+    numbers, or CUDA tensors with one for each row (float32, top_k int32), which are not checked.  -1 for a row without a logit
+    above minus infinity."""
+    return (_binding or _operators()).sample(logits, u, temperature, top_k, top_p, min_p, stream)

@@ -382,6 +382,62 @@ int64_t clip_partials(int n_tensors);
 cudaError_t launch_clip_gradients(int n, const void *const *g, const int64_t *len, const int32_t *dtype, void *const *out,
                                   float max_norm, float eps, float *norm, float2 *partial, cudaStream_t stream);
 
+// kv_cache.cu: rows of a paged cache, written and read.  Element types: 0 = float, 1 = half, 2 = bfloat16, 3 = int8.
+constexpr int kCacheMaxDim = 256;
+constexpr int kCacheMaxCount = 1 << 20;  // heads, and tokens of a page
+struct KvPages {  // aecct_kv_cache
+  void *k, *v;
+  float *k_scale, *v_scale;
+  int64_t pages;
+  int page_size, heads, dim, ld;
+};
+struct KvSequences {  // aecct_kv_sequences, with the rows of their tokens in a call's tensors (NULL: one each)
+  const int32_t *table, *lengths, *rows;
+  int64_t ldt;
+  int batch, columns;
+};
+struct KvRowsCall {
+  KvPages cache;
+  KvSequences seqs;
+  int64_t total;
+  const void *k, *v;  // append: [total][heads][dim], ld apart
+  int64_t k_row, k_head, v_row, v_head;
+  void *k_out, *v_out;  // read: [total][heads][dim]
+  int dtype, cache_dtype;
+};
+cudaError_t launch_kv_append(const KvRowsCall &c, cudaStream_t stream);
+cudaError_t launch_kv_read(const KvRowsCall &c, cudaStream_t stream);
+
+// attend.cu: one new token of each sequence over a paged cache
+struct AttendCall {
+  KvPages cache;
+  KvSequences seqs;
+  const int32_t *first;  // or NULL
+  const void *q;
+  int64_t ld_row, ld_head;
+  int q_heads, dtype, cache_dtype;
+  float scale;
+  void *out;
+  float *lse;  // or NULL
+  void *workspace;
+};
+int64_t attend_workspace(int batch, int q_heads, int heads, int dim, int dtype, int cache_dtype);
+cudaError_t launch_attend(const AttendCall &c, cudaStream_t stream);
+
+// sample.cu: the next token of each row of logits
+constexpr int kSampleMaxVocab = 1 << 19;
+struct SampleCall {
+  const void *logits;
+  int64_t ld;
+  int rows, vocab, dtype;
+  const float *u, *temperature, *top_p, *min_p;  // the last three: NULL for the value below
+  const int32_t *top_k;
+  float temperature_all, top_p_all, min_p_all;
+  int top_k_all;
+  int64_t *tokens;
+};
+cudaError_t launch_sample(const SampleCall &c, cudaStream_t stream);
+
 // spe.cu: the spectral positional encoding (Sec. 4.3) on the GPU
 constexpr int kSpeMaxHeads = 8;
 constexpr int kSpeMaxTokens = 1024;

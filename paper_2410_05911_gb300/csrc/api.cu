@@ -46,6 +46,28 @@ int wait_gave_up() {
   g_last_error = "a device-side wait of an earlier call of an operator exceeded its limit";
   return AECCT_ERR_TIMEOUT;
 }
+// a cache and the sequences of a call on it (fills what the launchers take)
+int cache_of(const aecct_kv_cache *c, const aecct_kv_sequences *s, KvPages *pages, KvSequences *seqs) {
+  if (!c || !s || s->batch < 0 || s->columns < 0 || c->pages < 0 || c->page_size < 1 || c->heads < 1 || c->head_dim < 1) return AECCT_ERR_INVALID_ARG;
+  if (c->dtype != AECCT_I8 && c->dtype != AECCT_F16 && c->dtype != AECCT_BF16) return AECCT_ERR_INVALID_ARG;
+  if (c->head_dim > kCacheMaxDim || c->heads >= kCacheMaxCount || c->page_size >= kCacheMaxCount) return AECCT_ERR_UNSUPPORTED;
+  const int size = c->dtype == AECCT_I8 ? 1 : 2;
+  if (c->ld < c->head_dim || c->ld > (1 << 20) || c->ld * size % 16) return AECCT_ERR_INVALID_ARG;
+  if (c->pages > INT32_MAX) return AECCT_ERR_UNSUPPORTED;
+  if (c->pages > 0) {
+    const auto row = [](const void *p) { return p && (reinterpret_cast<uintptr_t>(p) & 15u) == 0; };
+    if (!row(c->k) || !row(c->v)) return AECCT_ERR_INVALID_ARG;
+    if (c->dtype == AECCT_I8 && (!is_array(c->k_scale, AECCT_F32) || !is_array(c->v_scale, AECCT_F32))) return AECCT_ERR_INVALID_ARG;
+  }
+  if (s->batch > 0 && (!is_array(s->lengths, AECCT_F32) || (s->columns > 0 && (!is_array(s->table, AECCT_F32) || s->ldt < s->columns))))
+    return AECCT_ERR_INVALID_ARG;
+  if (static_cast<int64_t>(s->columns) * c->page_size > INT32_MAX) return AECCT_ERR_UNSUPPORTED;
+  *pages = {c->k, c->v, c->k_scale, c->v_scale, c->pages, c->page_size, c->heads, c->head_dim, c->ld};
+  *seqs = {s->table, s->lengths, nullptr, s->ldt, s->batch, s->columns};
+  return AECCT_OK;
+}
+// rows of [tokens][heads][dim] with strides of their own
+bool is_rows(const void *p, int64_t ld_row, int64_t ld_head, int32_t dtype) { return is_array(p, dtype) && ld_row >= 0 && ld_head >= 0; }
 // the sizes of an AAP linear layer: M tokens, K inputs, N outputs
 int linear_sizes(int64_t M, int64_t K, int64_t N) {
   if (M < 0 || N < 0 || K < 4 || K % 4 != 0) return AECCT_ERR_INVALID_ARG;
@@ -1406,6 +1428,85 @@ int aecct_clip_gradients(int32_t n_tensors, const void *const *grad, const int64
   const cudaError_t e = launch_clip_gradients(n_tensors, grad, len, dtype, out, max_norm, eps, norm,
                                               static_cast<float2 *>(workspace), static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "clip_gradients launch");
+}
+
+int aecct_kv_append(const aecct_kv_cache *cache, const aecct_kv_sequences *seqs, const int32_t *rows, int64_t total, const void *k,
+                    int64_t k_ld_row, int64_t k_ld_head, const void *v, int64_t v_ld_row, int64_t v_ld_head, int32_t dtype,
+                    void *cuda_stream) {
+  KvRowsCall c = {};
+  const int bad = cache_of(cache, seqs, &c.cache, &c.seqs);
+  if (bad != AECCT_OK) return bad;
+  if (total < 0 || !element_type(dtype) || (cache->dtype != AECCT_I8 && cache->dtype != dtype)) return AECCT_ERR_INVALID_ARG;
+  if (total > INT32_MAX) return AECCT_ERR_UNSUPPORTED;
+  if (!rows && total != seqs->batch) return AECCT_ERR_INVALID_ARG;
+  if (total == 0 || seqs->batch == 0) return AECCT_OK;
+  if (!is_rows(k, k_ld_row, k_ld_head, dtype) || !is_rows(v, v_ld_row, v_ld_head, dtype) || (rows && !is_array(rows, AECCT_F32)))
+    return AECCT_ERR_INVALID_ARG;
+  c.seqs.rows = rows, c.total = total, c.k = k, c.v = v;
+  c.k_row = k_ld_row, c.k_head = k_ld_head, c.v_row = v_ld_row, c.v_head = v_ld_head, c.dtype = dtype, c.cache_dtype = cache->dtype;
+  const cudaError_t e = launch_kv_append(c, static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "kv_append launch");
+}
+
+int aecct_kv_read(const aecct_kv_cache *cache, const aecct_kv_sequences *seqs, const int32_t *rows, int64_t total, void *k, void *v,
+                  int32_t dtype, void *cuda_stream) {
+  KvRowsCall c = {};
+  const int bad = cache_of(cache, seqs, &c.cache, &c.seqs);
+  if (bad != AECCT_OK) return bad;
+  if (total < 0 || !element_type(dtype)) return AECCT_ERR_INVALID_ARG;
+  if (total > INT32_MAX) return AECCT_ERR_UNSUPPORTED;
+  if (!rows && total != seqs->batch) return AECCT_ERR_INVALID_ARG;
+  if (total == 0) return AECCT_OK;
+  if (!is_array(k, dtype) || !is_array(v, dtype) || (rows && !is_array(rows, AECCT_F32))) return AECCT_ERR_INVALID_ARG;
+  c.seqs.rows = rows, c.total = total, c.k_out = k, c.v_out = v, c.dtype = dtype, c.cache_dtype = cache->dtype;
+  const cudaError_t e = launch_kv_read(c, static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "kv_read launch");
+}
+
+int aecct_paged_attention_workspace(int32_t batch, int32_t q_heads, int32_t heads, int32_t head_dim, int32_t dtype, int32_t cache_dtype,
+                                    int64_t *bytes) {
+  if (!bytes || batch < 0 || heads < 1 || q_heads < 1 || q_heads % heads || head_dim < 1 || !element_type(dtype) ||
+      (cache_dtype != AECCT_I8 && (cache_dtype != dtype || dtype == AECCT_F32)))
+    return AECCT_ERR_INVALID_ARG;
+  if (head_dim > kCacheMaxDim || heads >= kCacheMaxCount || q_heads >= kCacheMaxCount) return AECCT_ERR_UNSUPPORTED;
+  *bytes = batch == 0 ? 0 : attend_workspace(batch, q_heads, heads, head_dim, dtype, cache_dtype);
+  return AECCT_OK;
+}
+
+int aecct_paged_attention(const aecct_kv_cache *cache, const aecct_kv_sequences *seqs, const int32_t *first, const void *q, int64_t ld_row,
+                          int64_t ld_head, int32_t q_heads, int32_t dtype, float scale, void *out, float *lse, void *workspace,
+                          int64_t workspace_bytes, void *cuda_stream) {
+  AttendCall c = {};
+  int bad = cache_of(cache, seqs, &c.cache, &c.seqs);
+  if (bad != AECCT_OK) return bad;
+  int64_t need = 0;
+  bad = aecct_paged_attention_workspace(seqs->batch, q_heads, cache->heads, cache->head_dim, dtype, cache->dtype, &need);
+  if (bad != AECCT_OK) return bad;
+  if (!std::isfinite(scale)) return AECCT_ERR_INVALID_ARG;
+  if (seqs->batch == 0) return AECCT_OK;
+  if (!is_rows(q, ld_row, ld_head, dtype) || !is_array(out, dtype) || (lse && !is_array(lse, AECCT_F32)) ||
+      (first && !is_array(first, AECCT_F32)) || !is_workspace(workspace, workspace_bytes, need))
+    return AECCT_ERR_INVALID_ARG;
+  c.first = first, c.q = q, c.ld_row = ld_row, c.ld_head = ld_head, c.q_heads = q_heads, c.dtype = dtype, c.cache_dtype = cache->dtype;
+  c.scale = scale, c.out = out, c.lse = lse, c.workspace = workspace;
+  const cudaError_t e = launch_attend(c, static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "paged_attention launch");
+}
+
+int aecct_sample(const void *logits, int64_t ld, int64_t rows, int32_t vocab, int32_t dtype, const float *u, const aecct_sample_settings *set,
+                 int64_t *tokens, void *cuda_stream) {
+  if (rows < 0 || vocab < 1 || ld < vocab || !element_type(dtype) || !set) return AECCT_ERR_INVALID_ARG;
+  if (vocab > kSampleMaxVocab || rows > INT32_MAX) return AECCT_ERR_UNSUPPORTED;
+  const auto fine = [](const float *each, float all) { return each ? is_array(each, AECCT_F32) : std::isfinite(all) && all >= 0.0f; };
+  if (!fine(set->temperature_dev, set->temperature) || !fine(set->top_p_dev, set->top_p) || !fine(set->min_p_dev, set->min_p) ||
+      (set->top_k_dev && !is_array(set->top_k_dev, AECCT_F32)))
+    return AECCT_ERR_INVALID_ARG;
+  if (rows == 0) return AECCT_OK;
+  if (!is_array(logits, dtype) || !is_array(u, AECCT_F32) || !tokens || (reinterpret_cast<uintptr_t>(tokens) & 7u)) return AECCT_ERR_INVALID_ARG;
+  const SampleCall c = {logits, ld, static_cast<int>(rows), vocab, dtype, u, set->temperature_dev, set->top_p_dev, set->min_p_dev, set->top_k_dev,
+                        set->temperature, set->top_p, set->min_p, set->top_k, tokens};
+  const cudaError_t e = launch_sample(c, static_cast<cudaStream_t>(cuda_stream));
+  return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "sample launch");
 }
 
 int aecct_selftest_fma_rate(int32_t paired, double *fma_per_s) {

@@ -16,6 +16,8 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/utils/object_ptr.h>
 
+#include <climits>
+#include <cmath>
 #include <initializer_list>
 #include <optional>
 #include <string>
@@ -320,6 +322,204 @@ PyObject *clip_gradients(PyObject *const *a) {
   return wrap(norm);
 }
 
+// ------------------------------------------------------------------------------------------
+// serving a token at a time
+// ------------------------------------------------------------------------------------------
+int cache_element(at::ScalarType t) { return t == at::kChar ? AECCT_I8 : t == at::kFloat ? -1 : element(t); }
+
+// a KVCache: its four tensors, checked
+struct Cache {
+  at::Tensor k, v, k_scale, v_scale;
+  aecct_kv_cache c = {};
+  explicit Cache(PyObject *o) {
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 4) throw ValueError("cache must be a KVCache");
+    k = tensor(PyTuple_GET_ITEM(o, 0), "cache.k"), v = tensor(PyTuple_GET_ITEM(o, 1), "cache.v");
+    if (!k.is_cuda() || cache_element(k.scalar_type()) < 0 || k.dim() != 4)
+      throw ValueError("cache.k must be an int8, float16 or bfloat16 CUDA tensor [pages, heads, page_size, head_dim]");
+    check_current(k.device());
+    const auto s = k.sizes();
+    if (v.device() != k.device() || v.scalar_type() != k.scalar_type() || v.sizes() != s) throw ValueError("cache.v must be a tensor like cache.k");
+    c.dtype = cache_element(k.scalar_type());
+    c.ld = row_stride(k);
+    if (row_stride(v) != c.ld) throw ValueError("cache.v must be laid out like cache.k");
+    const bool scaled = c.dtype == AECCT_I8;
+    for (int i = 2; i < 4; ++i) {
+      const at::Tensor *t = optional_tensor(PyTuple_GET_ITEM(o, i), "a cache's scale");
+      if (!scaled && t) throw ValueError("a cache of 16-bit rows has no scales");
+      if (scaled && (!t || t->device() != k.device() || t->scalar_type() != at::kFloat || t->sizes() != s.slice(0, 3) || !t->is_contiguous()))
+        throw ValueError("an int8 cache's scales must be contiguous float32 tensors of shape " + shape_of(s.slice(0, 3)));
+      if (scaled) (i == 2 ? k_scale : v_scale) = *t;
+    }
+    c.k = k.data_ptr(), c.v = v.data_ptr();
+    if (scaled) c.k_scale = static_cast<float *>(k_scale.data_ptr()), c.v_scale = static_cast<float *>(v_scale.data_ptr());
+    for (int i = 1; i < 4; ++i)
+      if (s[i] >= (1 << 20)) throw ValueError("cache.k has a size that is too large");
+    c.pages = s[0], c.heads = static_cast<int32_t>(s[1]), c.page_size = static_cast<int32_t>(s[2]), c.head_dim = static_cast<int32_t>(s[3]);
+  }
+
+ private:
+  // elements from one row to the next: pages, heads and places follow one another without a gap
+  static int32_t row_stride(const at::Tensor &t) {
+    const auto s = t.sizes(), st = t.strides();
+    const int64_t size = t.element_size();
+    int64_t ld = s[2] > 1 ? st[2] : s[1] > 1 ? st[1] : s[0] > 1 ? st[0] : (s[3] * size + 15) / 16 * 16 / size;
+    if (ld > (1 << 20) || ld < s[3] || ld * size % 16 || (t.numel() > 0 && (reinterpret_cast<uintptr_t>(t.data_ptr()) & 15u)) || (s[3] > 1 && st[3] != 1) ||
+        (s[1] > 1 && st[1] != s[2] * ld) || (s[0] > 1 && st[0] != s[1] * s[2] * ld))
+      throw ValueError("a cache's rows must lie an equal multiple of 16 bytes apart, as kv_cache makes them");
+    return static_cast<int32_t>(ld);
+  }
+};
+
+at::Tensor int_array(PyObject *o, const char *name, const at::Device &on, int64_t n) {
+  const at::Tensor &t = tensor(o, name);
+  if (t.device() != on || t.scalar_type() != at::kInt || t.dim() != 1 || t.size(0) != n)
+    throw ValueError(std::string(name) + " must be an int32 tensor of shape (" + std::to_string(n) + ",) on the cache's device");
+  return t.contiguous();
+}
+
+// table and lengths
+struct Sequences {
+  at::Tensor table, lengths;
+  aecct_kv_sequences s = {};
+  Sequences(PyObject *t, PyObject *l, const at::Device &on) {
+    table = tensor(t, "table");
+    if (table.device() != on || table.scalar_type() != at::kInt || table.dim() != 2 || table.size(0) > INT32_MAX || table.size(1) > INT32_MAX)
+      throw ValueError("table must be an int32 tensor [batch, columns] on the cache's device");
+    lengths = int_array(l, "lengths", on, table.size(0));
+    const Rows r(table);
+    table = r.t;
+    s.table = static_cast<const int32_t *>(r.p), s.ldt = r.ld, s.lengths = static_cast<const int32_t *>(lengths.data_ptr());
+    s.batch = static_cast<int32_t>(table.size(0)), s.columns = static_cast<int32_t>(table.size(1));
+  }
+};
+
+// [tokens][heads][dim], read where it lies if the elements of a row do
+struct Heads {
+  at::Tensor t;
+  int64_t row, head;
+  explicit Heads(const at::Tensor &x) : t(x.size(2) > 1 && x.stride(2) != 1 ? x.contiguous() : x), row(t.stride(0)), head(t.stride(1)) {}
+};
+
+// the arrays after the first, with the check that they are like it
+const at::Tensor &heads_of(PyObject *o, const char *name, const Cache &cache, bool same_heads) {
+  const at::Tensor &t = tensor(o, name);
+  if (t.device() != cache.k.device() || element(t.scalar_type()) < 0 || t.dim() != 3 || t.size(2) != cache.c.head_dim ||
+      (same_heads && t.size(1) != cache.c.heads))
+    throw ValueError(std::string(name) + " must be a float32, float16 or bfloat16 tensor [tokens, " + (same_heads ? "" : "q_") + "heads, head_dim] on the cache's device");
+  if (cache.c.dtype != AECCT_I8 && cache.c.dtype != element(t.scalar_type())) throw ValueError(std::string(name) + " must have the type of a 16-bit cache");
+  return t;
+}
+
+// (k, v, cache, table, lengths, rows, stream)
+PyObject *kv_append(PyObject *const *a) {
+  const Cache cache(a[2]);
+  const at::Device on = cache.k.device();
+  const at::Tensor &k = heads_of(a[0], "k", cache, true), &v = heads_of(a[1], "v", cache, true);
+  check_like("v", v, k);
+  const Sequences seqs(a[3], a[4], on);
+  const int64_t total = k.size(0);
+  const at::Tensor rows = a[5] == Py_None ? at::Tensor() : int_array(a[5], "rows", on, int64_t(seqs.s.batch) + 1);
+  if (!rows.defined() && total != seqs.s.batch) throw ValueError("without rows, k has one token for each of " + std::to_string(seqs.s.batch) + " sequences");
+  check_no_graph("kv_append", {&k, &v, &cache.k, &cache.v});
+  const Heads kh(k), vh(v);
+  void *s = launch_stream(a[6], cache.k, {&kh.t, &vh.t, &cache.k, &cache.v, &cache.k_scale, &cache.v_scale, &seqs.table, &seqs.lengths, &rows});
+  check(aecct_kv_append(&cache.c, &seqs.s, rows.defined() ? static_cast<const int32_t *>(rows.data_ptr()) : nullptr, total, kh.t.data_ptr(), kh.row, kh.head,
+                        vh.t.data_ptr(), vh.row, vh.head, element(k.scalar_type()), s),
+        "aecct_kv_append");
+  for (const at::Tensor *t : {&cache.k, &cache.v, &cache.k_scale, &cache.v_scale})  // (written in place, as autograd counts it)
+    if (t->defined() && !t->is_inference()) t->unsafeGetTensorImpl()->bump_version();
+  Py_RETURN_NONE;
+}
+
+// (cache, table, lengths, rows, total, dtype number, stream)
+PyObject *kv_read(PyObject *const *a) {
+  const Cache cache(a[0]);
+  const at::Device on = cache.k.device();
+  const Sequences seqs(a[1], a[2], on);
+  const at::Tensor rows = a[3] == Py_None ? at::Tensor() : int_array(a[3], "rows", on, int64_t(seqs.s.batch) + 1);
+  const int64_t total = PyLong_AsLongLong(a[4]);
+  if (total == -1 && PyErr_Occurred()) throw PythonError();
+  if (total < 0) throw ValueError("total must not be negative");
+  if (!rows.defined() && total != seqs.s.batch) throw ValueError("without rows, there is one token for each of " + std::to_string(seqs.s.batch) + " sequences");
+  const int32_t dtype = element_arg(a[5], "dtype");
+  check_no_graph("kv_read", {&cache.k, &cache.v});
+  const at::Tensor k = make({total, cache.c.heads, cache.c.head_dim}, on, type_of(dtype)), v = make({total, cache.c.heads, cache.c.head_dim}, on, type_of(dtype));
+  void *s = launch_stream(a[6], cache.k, {&k, &v, &cache.k, &cache.v, &cache.k_scale, &cache.v_scale, &seqs.table, &seqs.lengths, &rows});
+  check(aecct_kv_read(&cache.c, &seqs.s, rows.defined() ? static_cast<const int32_t *>(rows.data_ptr()) : nullptr, total, k.data_ptr(), v.data_ptr(), dtype, s),
+        "aecct_kv_read");
+  return tuple({k, v});
+}
+
+// (q, cache, table, lengths, first, scale, want_lse, stream)
+PyObject *paged_attention(PyObject *const *a) {
+  const Cache cache(a[1]);
+  const at::Device on = cache.k.device();
+  const at::Tensor &q = heads_of(a[0], "q", cache, false);
+  const Sequences seqs(a[2], a[3], on);
+  if (q.size(0) != seqs.s.batch) throw ValueError("q must have a token for each of " + std::to_string(seqs.s.batch) + " sequences");
+  if (cache.c.heads < 1 || q.size(1) < 1 || q.size(1) % cache.c.heads || q.size(1) >= (1 << 20))
+    throw ValueError("the heads of q must be a multiple of the cache's " + std::to_string(cache.c.heads));
+  const at::Tensor first = a[4] == Py_None ? at::Tensor() : int_array(a[4], "first", on, seqs.s.batch);
+  const double scale = a[5] == Py_None ? 1.0 / std::sqrt(static_cast<double>(cache.c.head_dim)) : number(a[5]);
+  check_no_graph("paged_attention", {&q, &cache.k, &cache.v});
+  const int32_t q_heads = static_cast<int32_t>(q.size(1)), dtype = element(q.scalar_type());
+  int64_t bytes = 0;
+  check(aecct_paged_attention_workspace(seqs.s.batch, q_heads, cache.c.heads, cache.c.head_dim, dtype, cache.c.dtype, &bytes), "aecct_paged_attention");
+  const Heads qh(q);
+  const at::Tensor out = make(q.sizes(), on, q.scalar_type()), lse = a[6] == Py_True ? make({seqs.s.batch, q_heads}, on, at::kFloat) : at::Tensor();
+  const at::Tensor work = bytes ? make({bytes}, on, at::kByte) : at::Tensor();
+  void *s = launch_stream(a[7], q, {&qh.t, &cache.k, &cache.v, &cache.k_scale, &cache.v_scale, &seqs.table, &seqs.lengths, &first, &out, &lse, &work});
+  check(aecct_paged_attention(&cache.c, &seqs.s, first.defined() ? static_cast<const int32_t *>(first.data_ptr()) : nullptr, qh.t.data_ptr(), qh.row, qh.head,
+                              q_heads, dtype, static_cast<float>(scale), out.data_ptr(), lse.defined() ? static_cast<float *>(lse.data_ptr()) : nullptr,
+                              bytes ? work.data_ptr() : nullptr, bytes, s),
+        "aecct_paged_attention");
+  return tuple({out, lse});
+}
+
+// a setting of sample: a tensor with one for each row, or a number
+at::Tensor setting(PyObject *o, const char *name, const at::Tensor &logits, at::ScalarType type, double *all) {
+  if (!THPVariable_Check(o)) {
+    *all = number(o);
+    return at::Tensor();
+  }
+  const at::Tensor &t = THPVariable_Unpack(o);
+  const at::IntArrayRef rows = logits.sizes().slice(0, logits.dim() - 1);
+  if (t.device() != logits.device() || t.scalar_type() != type || t.sizes() != rows)
+    throw ValueError(std::string(name) + " must be a number, or " + (type == at::kInt ? "an int32" : "a float32") + " tensor of shape " + shape_of(rows) +
+                     " on the logits' device");
+  return t.contiguous();
+}
+
+// (logits, u, temperature, top_k, top_p, min_p, stream)
+PyObject *sample(PyObject *const *a) {
+  const at::Tensor &logits = tensor(a[0], "logits"), &u = tensor(a[1], "u");
+  if (!logits.is_cuda() || element(logits.scalar_type()) < 0 || logits.dim() < 1)
+    throw ValueError("logits must be a float32, float16 or bfloat16 CUDA tensor of rows");
+  check_current(logits.device());
+  const at::IntArrayRef shape = logits.sizes().slice(0, logits.dim() - 1);
+  if (u.device() != logits.device() || u.scalar_type() != at::kFloat || u.sizes() != shape)
+    throw ValueError("u must be a float32 tensor of shape " + shape_of(shape) + " on the logits' device");
+  if (logits.size(-1) > INT32_MAX) throw ValueError("the rows of logits are too long");
+  double t = 0, k = 0, p = 0, m = 0;
+  const at::Tensor ts = setting(a[2], "temperature", logits, at::kFloat, &t), ks = setting(a[3], "top_k", logits, at::kInt, &k);
+  const at::Tensor ps = setting(a[4], "top_p", logits, at::kFloat, &p), ms = setting(a[5], "min_p", logits, at::kFloat, &m);
+  if (!(k >= 0) || k != std::floor(k)) throw ValueError("top_k must be a whole number that is not negative");
+  check_no_graph("sample", {&logits, &u, &ts, &ps, &ms});
+  const Rows x(logits);
+  const at::Tensor uc = u.contiguous(), tokens = make(shape, logits, at::kLong);
+  const auto floats = [](const at::Tensor &v) { return v.defined() ? static_cast<const float *>(v.data_ptr()) : nullptr; };
+  aecct_sample_settings set = {};
+  set.temperature_dev = floats(ts), set.top_p_dev = floats(ps), set.min_p_dev = floats(ms);
+  set.top_k_dev = ks.defined() ? static_cast<const int32_t *>(ks.data_ptr()) : nullptr;
+  set.temperature = static_cast<float>(t), set.top_p = static_cast<float>(p), set.min_p = static_cast<float>(m);
+  set.top_k = k >= INT32_MAX ? 0 : static_cast<int32_t>(k);
+  void *s = launch_stream(a[6], logits, {&x.t, &uc, &ts, &ks, &ps, &ms, &tokens});
+  check(aecct_sample(x.p, x.ld, uc.numel(), static_cast<int32_t>(logits.size(-1)), element(logits.scalar_type()), static_cast<const float *>(uc.data_ptr()), &set,
+                     static_cast<int64_t *>(tokens.data_ptr()), s),
+        "aecct_sample");
+  return wrap(tokens);
+}
+
 template <PyObject *(*F)(PyObject *const *), Py_ssize_t N>
 PyObject *entry(PyObject *, PyObject *const *args, Py_ssize_t n) {
   if (n != N) {
@@ -355,6 +555,10 @@ PyMethodDef g_methods[] = {method<setup, 2>("setup"),
                            method<aap_linear, 7>("aap_linear"),
                            method<aap_linear_backward, 10>("aap_linear_backward"),
                            method<clip_gradients, 6>("clip_gradients"),
+                           method<kv_append, 7>("kv_append"),
+                           method<kv_read, 7>("kv_read"),
+                           method<paged_attention, 8>("paged_attention"),
+                           method<sample, 7>("sample"),
                            {nullptr, nullptr, 0, nullptr}};
 PyModuleDef g_module = {PyModuleDef_HEAD_INIT, "aecct_torch", nullptr, -1, g_methods, nullptr, nullptr, nullptr, nullptr};
 
