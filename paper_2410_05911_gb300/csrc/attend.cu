@@ -1,81 +1,104 @@
-// attend.cu -- one new token of each sequence over its keys and values in a paged cache.
-//
-//   s_j = scale sum_i q_i k_ji,  out = sum_j exp(s_j - m) v_j / l,  m = max_j s_j,  l = sum_j exp(s_j - m)
-//
-// One pass over the keys with the running maximum and sum: where a new maximum m' comes, what was summed is multiplied by
-// exp(m - m').
+// attend.cu -- one new token of each sequence over its keys and values in a paged cache: the choice of a kernel (attend.cuh), and
+// the join of what passed a CTA's border.
 #include <cuda_runtime.h>
 
 #include <cmath>
 #include <cstdint>
 
-#include "aecct_internal.h"
-#include "kv_pages.cuh"
-#include "rowtypes.cuh"
+#include "attend.cuh"
 
 namespace aecct {
 
 namespace {
 
-template <typename C>
-__device__ __forceinline__ float element_of(const C *p) {
-  if constexpr (sizeof(C) == 1) return static_cast<float>(*p);
-  else return to_f32(*p);
+constexpr int kJoinThreads = 128;
+
+// Query head blockIdx.y of the piece that begins in CTA blockIdx.x and goes on in those after it.  And a row of zeros for
+// sequences that have no key: no tile of theirs is in the list.
+__global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const __grid_constant__ AttendArgs a, AttendPlan plan) {
+  grid_wait();
+  const int tid = threadIdx.x, lane = tid & 31, head = blockIdx.y;
+  if (head == 0) {
+    for (int base = (blockIdx.x * kJoinThreads + tid) & ~31; base < a.seqs.batch; base += gridDim.x * kJoinThreads) {
+      const int b = base + lane;
+      bool none = false;
+      if (b < a.seqs.batch) {
+        const int n = sequence_length(a.seqs, b, a.cache.page_size);
+        none = n == 0 || (a.first && a.first[b] >= n);
+      }
+      for (uint32_t left = __ballot_sync(0xffffffffu, none); left; left &= left - 1) {
+        const int64_t row = static_cast<int64_t>(base + __ffs(left) - 1) * a.q_heads;
+        for (int64_t i = lane; i < static_cast<int64_t>(a.q_heads) * a.cache.dim; i += 32) store_out(a, row * a.cache.dim + i, 0.0f);
+        if (a.lse)
+          for (int i = lane; i < a.q_heads; i += 32) a.lse[row + i] = -INFINITY;
+      }
+    }
+  }
+  const AttendPiece p = a.piece[blockIdx.x * 2 + 1];
+  if (p.b < 0) return;
+  const int part = p.j % a.parts;
+  if (head >= min(plan.heads, a.group - part * plan.heads)) return;
+  // the CTAs up to the one where it ends
+  int count = 1;
+  for (int c = blockIdx.x + 1;; c += 32) {
+    const bool ends = c + lane < static_cast<int>(gridDim.x) ? a.piece[(c + lane) * 2].ends != 0 : true;
+    const uint32_t found = __ballot_sync(0xffffffffu, ends);
+    if (found) {
+      count += c - static_cast<int>(blockIdx.x) - 1 + __ffs(found);
+      break;
+    }
+  }
+  const auto from = [&](int k) { return a.partial + ((blockIdx.x + k) * 2 + (k == 0 ? 1 : 0)) * static_cast<int64_t>(plan.part); };
+  float top = -INFINITY;
+  for (int k = lane; k < count; k += 32) top = fmaxf(top, from(k)[head]);
+  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const float base = top == -INFINITY ? 0.0f : top;
+  float l = 0.0f, v[2] = {0.0f, 0.0f};
+#pragma unroll 4
+  for (int k = 0; k < count; ++k) {
+    const float *f = from(k), by = exp2_fast(f[head] - base);
+    l = fmaf(f[plan.heads + head], by, l);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int e = tid + i * kJoinThreads;
+      if (e < plan.width) v[i] = fmaf(f[2 * plan.heads + head * plan.width + e], by, v[i]);
+    }
+  }
+  const int64_t at = static_cast<int64_t>(p.b) * a.q_heads + p.j / a.parts * a.group + part * plan.heads + head;
+  for (int i = 0; i < 2; ++i) {
+    const int e = tid + i * kJoinThreads;
+    if (e < a.cache.dim) store_out(a, at * a.cache.dim + e, share(v[i], l));
+  }
+  if (tid == 0 && a.lse) a.lse[at] = lse_of(top, l);
 }
 
-// a warp to a query head
-template <typename T, typename C>
-__global__ void attend_kernel(AttendCall c) {
-  constexpr int E = kCacheMaxDim / 32;
-  const int lane = threadIdx.x & 31, dim = c.cache.dim;
-  const int64_t i = blockIdx.x * int64_t(blockDim.x / 32) + threadIdx.x / 32;
-  if (i >= static_cast<int64_t>(c.seqs.batch) * c.q_heads) return;
-  const int b = static_cast<int>(i / c.q_heads), head = static_cast<int>(i % c.q_heads), h = head / (c.q_heads / c.cache.heads);
-  float q[E], acc[E], m = -INFINITY, l = 0.0f;
-  for (int e = 0; e < E; ++e) {
-    const int at = e * 32 + lane;
-    q[e] = at < dim ? to_f32((static_cast<const T *>(c.q) + b * c.ld_row + head * c.ld_head)[at]) : 0.0f, acc[e] = 0.0f;
-  }
-  const int n = sequence_length(c.seqs, b, c.cache.page_size);
-  for (int p = c.first && c.first[b] > 0 ? c.first[b] : 0; p < n; ++p) {
-    const int64_t place = token_place(c.cache, c.seqs, b, p);
-    if (place < 0) continue;
-    const int64_t row = cache_row(c.cache, place, h);
-    const C *k = static_cast<const C *>(c.cache.k) + row * c.cache.ld, *v = static_cast<const C *>(c.cache.v) + row * c.cache.ld;
-    float s = 0.0f;
-    for (int e = 0; e < E; ++e)
-      if (e * 32 + lane < dim) s = fmaf(q[e], element_of(k + e * 32 + lane), s);
-    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-    float vs = 1.0f;
-    if constexpr (sizeof(C) == 1) s *= c.cache.k_scale[row], vs = c.cache.v_scale[row];
-    s *= c.scale;
-    const float top = fmaxf(m, s), old = top == -INFINITY ? 1.0f : expf(m - top), w = top == -INFINITY ? 0.0f : expf(s - top);
-    m = top, l = fmaf(l, old, w);
-    for (int e = 0; e < E; ++e)
-      if (e * 32 + lane < dim) acc[e] = fmaf(acc[e], old, w * vs * element_of(v + e * 32 + lane));
-  }
-  T *out = static_cast<T *>(c.out) + i * dim;
-  for (int e = 0; e < E; ++e)
-    if (e * 32 + lane < dim) out[e * 32 + lane] = from_f32<T>(l == 0.0f ? 0.0f : __fdiv_rn(acc[e], l));
-  if (c.lse && lane == 0) c.lse[i] = m + logf(l);
+// One piece of 16 bits for a weight is under the rounding of a bfloat16 result (2^-12 of it and 2^-9, each at most half a step); a
+// half or float result takes two, and so does a cache in bfloat16, whose weights have that type's 8 bits.
+cudaError_t run(int dim, int group, int dtype, int cache_dtype, const AttendArgs *a, AttendPlan *plan, cudaStream_t st) {
+  if (cache_dtype == 1) return run_attend_half(dim, group, a, plan, st);
+  if (cache_dtype == 2) return run_attend_bf16(dim, group, a, plan, st);
+  return dtype == 2 ? run_attend_codes(dim, group, a, plan, st) : run_attend_pieces(dim, group, a, plan, st);
 }
 
-template <typename T, typename C>
-cudaError_t launch(const AttendCall &c, cudaStream_t st) {
-  attend_kernel<T, C><<<static_cast<unsigned>((static_cast<int64_t>(c.seqs.batch) * c.q_heads + 3) / 4), 128, 0, st>>>(c);
-  return cudaGetLastError();
-}
+int64_t piece_bytes(const AttendPlan &p) { return (2 * static_cast<int64_t>(p.ctas) * p.part * static_cast<int64_t>(sizeof(float)) + 15) / 16 * 16; }
 
 }  // namespace
 
-int64_t attend_workspace(int, int, int, int, int, int) { return 0; }
+int64_t attend_workspace(int, int q_heads, int heads, int dim, int dtype, int cache_dtype) {
+  AttendPlan p = {};
+  run(dim, q_heads / heads, dtype, cache_dtype, nullptr, &p, nullptr);
+  return piece_bytes(p) + 2 * static_cast<int64_t>(p.ctas) * static_cast<int64_t>(sizeof(AttendPiece));
+}
 
 cudaError_t launch_attend(const AttendCall &c, cudaStream_t st) {
-  if (c.cache_dtype == 1) return launch<__half, __half>(c, st);
-  if (c.cache_dtype == 2) return launch<__nv_bfloat16, __nv_bfloat16>(c, st);
-  if (c.dtype == 0) return launch<float, int8_t>(c, st);
-  if (c.dtype == 1) return launch<__half, int8_t>(c, st);
-  return launch<__nv_bfloat16, int8_t>(c, st);
+  const int group = c.q_heads / c.cache.heads;
+  AttendPlan p = {};
+  run(c.cache.dim, group, c.dtype, c.cache_dtype, nullptr, &p, st);
+  AttendArgs a = {c.cache, c.seqs, c.first, c.q, c.ld_row, c.ld_head, group, c.q_heads, c.dtype, (group + p.heads - 1) / p.heads, c.scale * kLog2e, c.out,
+                  c.lse, static_cast<float *>(c.workspace), reinterpret_cast<AttendPiece *>(static_cast<char *>(c.workspace) + piece_bytes(p))};
+  const cudaError_t e = run(c.cache.dim, group, c.dtype, c.cache_dtype, &a, &p, st);
+  if (e != cudaSuccess) return e;
+  return launch_dependent(attend_join_kernel, dim3(p.ctas, p.heads), kJoinThreads, 0, st, a, p);
 }
 
 }  // namespace aecct

@@ -1,0 +1,687 @@
+// attend.cuh -- the kernel of attend.cu: one new token's query heads over the paged keys and values of its sequence.
+//
+//   s_j = scale q . k_j,  out = sum_j 2^(x_j - m) v_j / l,  x_j = s_j log2 e,  m = max_j x_j,  l = sum_j 2^(x_j - m)
+//
+// Work.  The G query heads of a cache head read the same keys and values, so they are one operand of a matrix product: S^T = K q^T
+// and O^T = V^T P^T on the tensor cores, 16 keys (and 16 elements of a head) by 8 columns.  A column is a query head, or for P = 2
+// half of one: its numbers in two pieces of 16 bits (the number rounded, and what the rounding left), whose products are added up.
+// The positions of all sequences and cache heads are one list of tiles of TK keys, cut evenly over CTAs and
+// over their warps, whatever the lengths are: a warp takes several short sequences, or a part of a long one.  A warp needs no other
+// one while it works: it has a ring of stages in shared memory, filled by asynchronous copies that also put zeros where no
+// token is, and writes whole sequences out itself.  Parts are joined in shared memory, and those that pass a CTA's
+// border by the kernel in attend.cu.
+//
+// Operands.  The order of the contracted index is free, and so is that of the output's rows.  A lane's share of an
+// operand is therefore what it can read from shared memory in 16 bytes: of K, for key g of 8 (g = lane / 4), elements that follow one another
+// (the queries are loaded in the same order); of V, for four keys of 16 (2 t, 2 t + 1, 2 t + 8, 2 t + 9; t = lane % 4), elements that
+// follow one another, paired by key with byte permutes.  No transposed copy of V is made.  Codes become halves exactly:
+// 0x6400 + (code + 128) is the half 1152 + code.
+//
+// 32 bits: sums of products, maxima, exponents and sums.  What is rounded to 16: the weights, as the tensor cores' operand. With codes the scale of a value row belongs to the
+// weight: 2^(x_j - m) vs_j = 2^(y_j), y_j = x_j - m + log2 vs_j, has a running maximum of its own, so that the weights that
+// count use the whole range of a half.  Queries times codes are exact products: a bfloat16 or half query is scaled by a power of two to fit a half, a float one is cut in two.
+#pragma once
+#include <cuda_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+
+#include "aecct_internal.h"
+#include "kv_pages.cuh"
+#include "rowtypes.cuh"
+#include "sm103_ptx.cuh"
+
+namespace aecct {
+
+// a piece of a sequence's attention that passes a CTA's border
+struct AttendPiece {
+  int b, j;  // the sequence (-1: none), and the piece of its heads
+  int ends;  // the last tile is in it
+  int pad;
+};
+struct AttendArgs {
+  KvPages cache;
+  KvSequences seqs;
+  const int32_t *first;
+  const void *q;
+  int64_t ld_row, ld_head;
+  int group, q_heads, dtype;
+  int parts;    // pieces of at most kHeads query heads that the group is cut into
+  float scale;  // times log2 e
+  void *out;
+  float *lse;
+  float *partial;      // [2 CTAs][kHeads (DP + 2)]
+  AttendPiece *piece;  // [2 CTAs]
+};
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float exp2_fast(float x) {
+  float r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ float log2_fast(float x) {
+  float r;
+  asm("lg2.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+  return r;
+}
+__device__ __forceinline__ void copy16(uint32_t dst, const void *src, int bytes) {  // the rest of the 16 become zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void *src, int bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copies_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void copies_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+template <bool BF16>
+__device__ __forceinline__ void mma_16816(float *c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (BF16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+// an 8 x 8 matrix of 16-bit elements, transposed over the warp
+__device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
+  uint32_t r;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+  return r;
+}
+// bytes 0 and 1 (or 2 and 3) of codes + 128 as two halves
+__device__ __forceinline__ uint32_t halves_of(uint32_t codes, uint32_t select) {
+  const uint32_t w = __byte_perm(codes, 0x64646464u, select);
+  uint32_t r;
+  asm("sub.f16x2 %0, %1, %2;" : "=r"(r) : "r"(w), "r"(0x64806480u));
+  return r;
+}
+constexpr uint32_t kLow = 0x4140u, kHigh = 0x4342u;
+
+// The shapes of a kernel.  C: the cache's type; DP: the head's width, padded; NB: blocks of 8 columns; P: pieces of a number.
+template <typename C_, int DP_, int NB_, int P_>
+struct AttendShape {
+  using C = C_;
+  static constexpr int DP = DP_, NB = NB_, P = P_;
+  static constexpr int kSize = sizeof(C), kRow = DP * kSize;
+  static constexpr int kHeads = 8 * NB / P;
+  static constexpr int TK = kRow <= 128 ? 32 : 16;
+  static constexpr int kWarps = kRow <= 256 ? 8 : 4;
+  static constexpr int kCtas = kRow <= 64 ? 2 : 1;  // to an SM
+  static constexpr int kStage = 2 * TK * kRow + 2 * TK * 4 + 16;
+  static constexpr int kPart = kHeads * (DP + 2);  // floats of a piece: maxima, sums, rows
+  static constexpr int kFixed = 16 * kWarps + 8 * 32 * kWarps + 2 * kWarps * 16 + kWarps * kPart * 4;
+  static constexpr int kRoom = (227 * 1024 / kCtas - 1024 * (kCtas - 1) - kFixed) / (kWarps * kStage);
+  static constexpr int kStages = kRoom > 4 ? 4 : kRoom;
+  static constexpr int kSmem = kFixed + kWarps * kStages * kStage;
+  static_assert(kStages >= 2 && kStages * kStage >= kPart * 4, "a ring holds a piece");
+  static_assert(kStage % 16 == 0 && kFixed % 16 == 0, "copies of 16 bytes");
+};
+
+template <class S>
+struct AttendWarp {
+  using C = typename S::C;
+  static constexpr bool kCodes = sizeof(C) == 1;
+  static constexpr bool kBf16 = std::is_same_v<C, __nv_bfloat16>;
+  static constexpr int DP = S::DP, NB = S::NB, P = S::P, TK = S::TK, M = TK / 16, UPR = S::kRow / 16;
+  static constexpr int HC = NB * (3 - P);  // heads of a lane's columns
+  static constexpr float kOffset = kBf16 ? 0.0f : 15.0f;  // weights up to 2^15, so that halves reach down to 2^-39 of the largest
+
+  // where in the list of tiles
+  struct Cursor {
+    int b, j, tile, tiles, t0, lo, hi;
+  };
+
+  const AttendArgs &a;
+  const uint32_t ring;  // shared memory
+  const int lane, g, t;
+  const int all;  // pieces of heads of a sequence
+
+  uint32_t qf[DP / 16][NB][2];
+  float o[DP / 16][NB][4], top[HC], vtop[HC], l[HC], qs[HC];
+
+  __device__ AttendWarp(const AttendArgs &args, uint32_t ring_)
+      : a(args), ring(ring_), lane(threadIdx.x & 31), g((threadIdx.x & 31) >> 2), t(threadIdx.x & 3), all(args.cache.heads * args.parts) {}
+
+  static __device__ int tiles_of(const AttendArgs &a, int b, int &lo, int &hi) {
+    hi = sequence_length(a.seqs, b, a.cache.page_size);
+    lo = a.first ? a.first[b] : 0;
+    lo = lo < 0 ? 0 : lo;
+    return lo < hi ? (hi - 1) / TK - lo / TK + 1 : 0;
+  }
+  __device__ void sequence(Cursor &c) const {
+    c.tiles = tiles_of(a, c.b, c.lo, c.hi);
+    c.t0 = c.lo / TK;
+  }
+  // the next tile; the caller knows that there is one
+  __device__ void advance(Cursor &c) const {
+    if (++c.tile < c.tiles) return;
+    c.tile = 0;
+    if (++c.j < all) return;
+    c.j = 0;
+    do {
+      ++c.b;
+      sequence(c);
+    } while (c.tiles == 0);
+  }
+
+  // this lane's row of a tile: its page and place in it, -1 for none
+  __device__ void find(const Cursor &c, int &page, int &place) const {
+    const int p = (c.t0 + c.tile) * TK + lane;
+    page = -1, place = 0;
+    if (lane < TK && p >= c.lo && p < c.hi) {
+      const int column = p / a.cache.page_size;
+      place = p - column * a.cache.page_size;
+      page = a.seqs.table[static_cast<int64_t>(c.b) * a.seqs.ldt + column];
+    }
+  }
+  static __device__ __forceinline__ uint32_t k_unit(uint32_t row, uint32_t u) { return UPR >= 8 ? u ^ ((row & 1) << 2) : u; }
+  static __device__ __forceinline__ uint32_t v_unit(uint32_t row, uint32_t u) {
+    return UPR >= 8 ? u ^ (((row >> 1) & 3) << 1) : UPR == 4 ? u ^ (((row >> 1) & 1) << 1) : u;
+  }
+  // the copies of a tile into a stage; rows without a token and what is past a row's end become zeros
+  __device__ void fill(int stage, const Cursor &c, int page, int place) const {
+    const uint32_t at = ring + stage * S::kStage;
+    const bool fine = page >= 0 && page < a.cache.pages;
+    const int64_t row = fine ? (static_cast<int64_t>(page) * a.cache.heads + c.j / a.parts) * a.cache.page_size + place : 0;
+    const uint32_t mask = __ballot_sync(0xffffffffu, fine);
+    const int64_t from = row * (static_cast<int64_t>(a.cache.ld) * S::kSize);
+    const int width = a.cache.dim * S::kSize;
+#pragma unroll
+    for (int i = 0; i < TK * UPR / 32; ++i) {
+      const int r = (i * 32 + lane) / UPR, u = (i * 32 + lane) % UPR;
+      const int64_t off = __shfl_sync(0xffffffffu, from, r) + u * 16;
+      int bytes = width - u * 16;
+      bytes = (mask >> r) & 1 ? (bytes < 0 ? 0 : bytes < 16 ? bytes : 16) : 0;
+      const int64_t src = bytes > 0 ? off : 0;
+      copy16(at + r * S::kRow + k_unit(r, u) * 16, static_cast<const char *>(a.cache.k) + src, bytes);
+      copy16(at + TK * S::kRow + r * S::kRow + v_unit(r, u) * 16, static_cast<const char *>(a.cache.v) + src, bytes);
+    }
+    if constexpr (kCodes) {
+      if (lane < TK) {
+        copy4(at + 2 * TK * S::kRow + lane * 4, a.cache.k_scale + row, fine ? 4 : 0);
+        copy4(at + 2 * TK * S::kRow + TK * 4 + lane * 4, a.cache.v_scale + row, fine ? 4 : 0);
+      }
+    }
+    if (lane == 0) asm volatile("st.shared.u32 [%0], %1;" ::"r"(at + 2 * TK * S::kRow + 2 * TK * 4), "r"(mask) : "memory");
+  }
+
+  static __device__ __forceinline__ float lds(uint32_t p) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(p));
+    return v;
+  }
+  template <int N>
+  static __device__ __forceinline__ void lds_words(uint32_t p, uint32_t *w) {
+    if constexpr (N == 4) asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(p));
+    else if constexpr (N == 2) asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(p));
+    else asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(p));
+  }
+
+  // query head of a column of this piece (its number in the group's piece), and which piece of the number
+  static __device__ __forceinline__ int head_of(int column) { return column / P; }
+  __device__ float query(const void *row, int e) const {
+    if (e >= a.cache.dim) return 0.0f;
+    return a.dtype == 0 ? static_cast<const float *>(row)[e] : a.dtype == 1 ? to_f32(static_cast<const __half *>(row)[e]) : to_f32(static_cast<const __nv_bfloat16 *>(row)[e]);
+  }
+  // a sequence's or a head's first tile: the queries in the order of the keys' elements, and nothing summed yet
+  __device__ void begin(const Cursor &c) {
+    constexpr int EL = DP / 4 < 16 / S::kSize ? DP / 4 : 16 / S::kSize;  // elements of a lane's piece of a key
+    const int part = c.j % a.parts, heads = min(S::kHeads, a.group - part * S::kHeads), head0 = c.j / a.parts * a.group + part * S::kHeads;
+    const int size = a.dtype == 0 ? 4 : 2;
+    float by_column[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const int column = nb * 8 + g, head = head_of(column), which = column % P;
+      const bool on = head < heads;
+      const char *row = static_cast<const char *>(a.q) + (c.b * a.ld_row + (head0 + (on ? head : 0)) * a.ld_head) * size;
+      float v[DP / 4], most = 0.0f;
+#pragma unroll
+      for (int i = 0; i < DP / 4; ++i) {
+        v[i] = on ? query(row, 4 * EL * (i / EL) + EL * t + i % EL) : 0.0f;
+        most = fmaxf(most, fabsf(v[i]));
+      }
+      float by = 1.0f;
+      if constexpr (kCodes) {  // to 2^14 at most
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
+        most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 2));
+        const int e = (__float_as_uint(most) >> 23) - 127;  // (of a denormal: -127)
+        const int up = most > 0.0f && most < INFINITY ? 13 - e : 0;  // -114 .. 140, in two factors
+        const float f0 = __uint_as_float((127u + up / 2) << 23), f1 = __uint_as_float((127u + up - up / 2) << 23);
+#pragma unroll
+        for (int i = 0; i < DP / 4; ++i) v[i] = v[i] * f0 * f1;
+        by = __uint_as_float((127u - up / 2) << 23) * __uint_as_float((127u - (up - up / 2)) << 23);
+      }
+      by_column[nb] = by;
+#pragma unroll
+      for (int i = 0; i < DP / 4; i += 2) {
+        uint32_t w = 0;
+        if constexpr (kBf16) {
+          w = pack2<__nv_bfloat16>(v[i], v[i + 1]);
+          if (P == 2 && which == 1) w = 0;  // (a bfloat16 query has one piece)
+        } else {
+          w = pack2<__half>(v[i], v[i + 1]);
+          if (P == 2 && which == 1) {
+            float x, y;
+            unpack2<__half>(w, x, y);
+            w = pack2<__half>(v[i] - x, v[i + 1] - y);
+          }
+        }
+        qf[i / 4][nb][(i / 2) & 1] = w;
+      }
+    }
+#pragma unroll
+    for (int hc = 0; hc < HC; ++hc) {
+      const int nb = hc / (3 - P), column = P == 2 ? 2 * t : 2 * t + hc % 2;  // (within the block)
+      qs[hc] = a.scale;
+      if constexpr (kCodes) qs[hc] *= __shfl_sync(0xffffffffu, by_column[nb], column * 4);
+      top[hc] = vtop[hc] = -INFINITY, l[hc] = 0.0f;
+    }
+#pragma unroll
+    for (int m = 0; m < DP / 16; ++m)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) o[m][nb][i] = 0.0f;
+  }
+
+  __device__ __forceinline__ static float over_keys_max(float v) {
+    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 4));
+    v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 8));
+    return fmaxf(v, __shfl_xor_sync(0xffffffffu, v, 16));
+  }
+
+  // a tile in a stage
+  __device__ void tile(int stage) {
+    const uint32_t at = ring + stage * S::kStage, vat = at + TK * S::kRow, scales = vat + TK * S::kRow;
+    const uint32_t mask = __float_as_uint(lds(scales + 2 * TK * 4));
+    float s[M][NB][4];
+#pragma unroll
+    for (int mt = 0; mt < M; ++mt)
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[mt][nb][i] = 0.0f;
+    // S^T = K q^T
+    constexpr int KB = S::kRow / 4, KW = KB < 16 ? KB / 4 : 4, KP = KB < 16 ? 1 : KB / 16;  // a lane's bytes of a key, words of a piece, pieces
+#pragma unroll
+    for (int pc = 0; pc < KP; ++pc) {
+#pragma unroll
+      for (int mt = 0; mt < M; ++mt) {
+        uint32_t w[2][KW];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t r = mt * 16 + i * 8 + g;
+          lds_words<KW>(KB < 16 ? at + r * S::kRow + t * KB : at + r * S::kRow + k_unit(r, pc * 4 + t) * 16, w[i]);
+        }
+        if constexpr (kCodes) {
+#pragma unroll
+          for (int i = 0; i < KW; ++i) {
+            const uint32_t x = w[0][i] ^ 0x80808080u, y = w[1][i] ^ 0x80808080u;
+            const uint32_t a0 = halves_of(x, kLow), a1 = halves_of(y, kLow), a2 = halves_of(x, kHigh), a3 = halves_of(y, kHigh);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) mma_16816<false>(s[mt][nb], a0, a1, a2, a3, qf[pc * KW + i][nb][0], qf[pc * KW + i][nb][1]);
+          }
+        } else {
+#pragma unroll
+          for (int i = 0; i < KW / 2; ++i)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+              mma_16816<kBf16>(s[mt][nb], w[0][2 * i], w[1][2 * i], w[0][2 * i + 1], w[1][2 * i + 1], qf[pc * (KW / 2) + i][nb][0], qf[pc * (KW / 2) + i][nb][1]);
+        }
+      }
+    }
+    // scores in powers of two, maxima, weights
+    float x[M][2][HC], vs[M][2];
+    float most[HC], vmost[HC];
+#pragma unroll
+    for (int hc = 0; hc < HC; ++hc) most[hc] = top[hc], vmost[hc] = vtop[hc];
+#pragma unroll
+    for (int mt = 0; mt < M; ++mt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const uint32_t r = mt * 16 + i * 8 + g;
+        const bool on = (mask >> r) & 1;
+        float ks = 1.0f;
+        if constexpr (kCodes) ks = lds(scales + r * 4), vs[mt][i] = log2_fast(lds(scales + TK * 4 + r * 4));
+#pragma unroll
+        for (int hc = 0; hc < HC; ++hc) {
+          const int nb = hc / (3 - P);
+          float v = P == 2 ? s[mt][nb][2 * i] + s[mt][nb][2 * i + 1] : s[mt][nb][2 * i + hc % 2];
+          v = on ? v * (kCodes ? ks * qs[hc] : qs[hc]) : -INFINITY;  // (the factors first: queries and scales may be far from one)
+          x[mt][i][hc] = v;
+          most[hc] = fmaxf(most[hc], v);
+          if constexpr (kCodes) vmost[hc] = fmaxf(vmost[hc], v + vs[mt][i]);
+        }
+      }
+    float keep[HC];
+#pragma unroll
+    for (int hc = 0; hc < HC; ++hc) {
+      most[hc] = over_keys_max(most[hc]);
+      const float base = most[hc] == -INFINITY ? 0.0f : most[hc];  // (no key yet)
+      const float old = exp2_fast(top[hc] - base);
+      top[hc] = most[hc], most[hc] = base - (kCodes ? 0.0f : kOffset);
+      l[hc] *= old, keep[hc] = old;
+      if constexpr (kCodes) {
+        vmost[hc] = over_keys_max(vmost[hc]);
+        const float vbase = vmost[hc] == -INFINITY ? 0.0f : vmost[hc];
+        keep[hc] = exp2_fast(vtop[hc] - vbase);
+        vtop[hc] = vmost[hc], vmost[hc] = vbase - kOffset;
+      }
+    }
+    uint32_t pf[M][NB][2];
+#pragma unroll
+    for (int mt = 0; mt < M; ++mt)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        float w[HC];
+#pragma unroll
+        for (int hc = 0; hc < HC; ++hc) {
+          const float p = exp2_fast(x[mt][i][hc] - most[hc]);
+          l[hc] += p;
+          w[hc] = kCodes ? exp2_fast(x[mt][i][hc] + vs[mt][i] - vmost[hc]) : p;
+        }
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          using E = std::conditional_t<kBf16, __nv_bfloat16, __half>;
+          if constexpr (P == 2) pf[mt][nb][i] = transpose_8x8(pack2<E>(w[nb], w[nb] - to_f32(from_f32<E>(w[nb]))));
+          else pf[mt][nb][i] = transpose_8x8(pack2<E>(w[2 * nb], w[2 * nb + 1]));
+        }
+      }
+    // O^T += V^T P^T: the tile's part by itself, added to what there is in one rounded operation
+    constexpr int VB = S::kRow / 8, VW = VB < 16 ? VB / 4 : 4, VP = VB < 16 ? 1 : VB / 16;
+#pragma unroll
+    for (int pc = 0; pc < VP; ++pc) {
+      uint32_t w[M][4][VW];
+#pragma unroll
+      for (int mt = 0; mt < M; ++mt)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const uint32_t r = mt * 16 + 2 * t + (i & 1) + (i >> 1) * 8;
+          const uint32_t u = VB >= 16 ? pc * 8 + g : g * VB / 16;
+          lds_words<VW>(vat + r * S::kRow + v_unit(r, u) * 16 + (VB >= 16 ? 0 : g * VB % 16), w[mt][i]);
+        }
+#pragma unroll
+      for (int i = 0; i < VW; ++i) {
+        constexpr int kPairs = kCodes ? 2 : 1;  // pairs of elements in a word
+        float c[kPairs][NB][4];
+#pragma unroll
+        for (int h = 0; h < kPairs; ++h)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) c[h][nb][e] = 0.0f;
+#pragma unroll
+        for (int mt = 0; mt < M; ++mt) {
+          if constexpr (kCodes) {
+            const uint32_t x0 = w[mt][0][i] ^ 0x80808080u, x1 = w[mt][1][i] ^ 0x80808080u, x2 = w[mt][2][i] ^ 0x80808080u, x3 = w[mt][3][i] ^ 0x80808080u;
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {  // elements 2 h and 2 h + 1 of the word, each of two keys
+              const uint32_t y = __byte_perm(x0, x1, h == 0 ? 0x5140u : 0x7362u), z = __byte_perm(x2, x3, h == 0 ? 0x5140u : 0x7362u);
+              const uint32_t a0 = halves_of(y, kLow), a1 = halves_of(y, kHigh), a2 = halves_of(z, kLow), a3 = halves_of(z, kHigh);
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) mma_16816<false>(c[h][nb], a0, a1, a2, a3, pf[mt][nb][0], pf[mt][nb][1]);
+            }
+          } else {
+            const uint32_t a0 = __byte_perm(w[mt][0][i], w[mt][1][i], 0x5410u), a1 = __byte_perm(w[mt][0][i], w[mt][1][i], 0x7632u);
+            const uint32_t a2 = __byte_perm(w[mt][2][i], w[mt][3][i], 0x5410u), a3 = __byte_perm(w[mt][2][i], w[mt][3][i], 0x7632u);
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) mma_16816<kBf16>(c[0][nb], a0, a1, a2, a3, pf[mt][nb][0], pf[mt][nb][1]);
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < kPairs; ++h)
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              float &v = o[(pc * VW + i) * kPairs + h][nb][e];
+              v = fmaf(v, keep[P == 2 ? nb : 2 * nb + (e & 1)], c[h][nb][e]);
+            }
+      }
+    }
+  }
+
+  // The last tile of a piece: maxima, sums over the keys and rows that belong to them (in units of 2^top).  f(head, element, value of a
+  // row) takes the rows, s(head, top, l) the rest; l is the whole sum in every lane.
+  template <class F, class G>
+  __device__ void end(F &&f, G &&s) {
+    float by[HC];
+#pragma unroll
+    for (int hc = 0; hc < HC; ++hc) {
+      l[hc] += __shfl_xor_sync(0xffffffffu, l[hc], 4);
+      l[hc] += __shfl_xor_sync(0xffffffffu, l[hc], 8);
+      l[hc] += __shfl_xor_sync(0xffffffffu, l[hc], 16);
+      if constexpr (kCodes) by[hc] = vtop[hc] == -INFINITY ? 0.0f : exp2_fast(vtop[hc] - top[hc] - kOffset);
+      else by[hc] = exp2_fast(-kOffset), l[hc] *= by[hc];
+      const int head = P == 2 ? hc * 4 + t : hc / 2 * 8 + 2 * t + hc % 2;
+      s(head, hc, top[hc], l[hc]);
+    }
+    constexpr int EL = DP / 8 < 16 / S::kSize ? DP / 8 : 16 / S::kSize;  // elements of a lane's piece of a value
+#pragma unroll
+    for (int m = 0; m < DP / 16; ++m) {
+      const int e = 8 * EL * (2 * m / EL) + EL * g + 2 * m % EL;
+#pragma unroll
+      for (int hc = 0; hc < HC; ++hc) {
+        const int head = P == 2 ? hc * 4 + t : hc / 2 * 8 + 2 * t + hc % 2;
+        const float *v = o[m][hc / (3 - P)];
+        f(head, hc, e, (P == 2 ? v[0] + v[1] : v[hc % 2]) * by[hc]);
+        f(head, hc, e + 1, (P == 2 ? v[2] + v[3] : v[2 + hc % 2]) * by[hc]);
+      }
+    }
+  }
+};
+
+__device__ __forceinline__ void store_out(const AttendArgs &a, int64_t at, float v) {
+  if (a.dtype == 0) static_cast<float *>(a.out)[at] = v;
+  else if (a.dtype == 1) static_cast<__half *>(a.out)[at] = from_f32<__half>(v);
+  else static_cast<__nv_bfloat16 *>(a.out)[at] = from_f32<__nv_bfloat16>(v);
+}
+// a row's share, of what its keys' weights add up to: nothing where no key was there
+__device__ __forceinline__ float share(float v, float l) { return l == 0.0f ? 0.0f : __fdiv_rn(v, l); }
+__device__ __forceinline__ float lse_of(float top, float l) { return l == 0.0f ? -INFINITY : fmaf(top, kLn2, logf(l)); }
+
+template <class S>
+__global__ void __launch_bounds__(S::kWarps * 32, S::kCtas) attend_kernel(const __grid_constant__ AttendArgs a) {
+  constexpr int NT = S::kWarps * 32, W = S::kWarps, TK = S::TK, DP = S::DP, H = S::kHeads;
+  using Warp = AttendWarp<S>;
+  extern __shared__ __align__(16) unsigned char smem[];
+  long long *sums = reinterpret_cast<long long *>(smem);                      // [2 W]
+  long long *before = reinterpret_cast<long long *>(smem + 16 * W);           // [NT]
+  AttendPiece *pieces = reinterpret_cast<AttendPiece *>(smem + 16 * W + 8 * NT);  // [W][2]
+  float *heads_of_parts = reinterpret_cast<float *>(smem + 16 * W + 8 * NT + 2 * W * 16);  // [W][kPart]
+  unsigned char *rings = smem + S::kFixed;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  grid_trigger();
+
+  // the list of tiles: sequences one after the other, in each its pieces of heads, in each its tiles
+  const int all = a.cache.heads * a.parts;
+  const auto scan = [&](int b, long long &sum) {  // tiles of the sequences before b in its chunk, and of all of the chunk
+    int lo, hi;
+    long long n = b < a.seqs.batch ? Warp::tiles_of(a, b, lo, hi) : 0, s = n;
+    for (int d = 1; d < 32; d <<= 1) {
+      const long long v = __shfl_up_sync(0xffffffffu, s, d);
+      if (lane >= d) s += v;
+    }
+    __syncthreads();
+    if (lane == 31) sums[warp] = s;
+    __syncthreads();
+    long long earlier = 0;
+    sum = 0;
+    for (int w = 0; w < W; ++w) {
+      if (w < warp) earlier += sums[w];
+      sum += sums[w];
+    }
+    before[tid] = earlier + s - n;
+    __syncthreads();
+  };
+  long long total = 0, sum = 0;
+  for (int base = 0; base < a.seqs.batch; base += NT) scan(base + tid, sum), total += sum;
+  total *= all;
+  const long long per_cta = max((total + gridDim.x - 1) / gridDim.x, static_cast<long long>(W));
+  const long long from = min(total, blockIdx.x * per_cta), count = min(total, from + per_cta) - from;
+  const long long per = (count + W - 1) / W;
+  const long long mine = from + min(count, warp * per);
+  const int n = static_cast<int>(min(per, from + count - mine));  // this warp's tiles
+  typename Warp::Cursor at = {};
+  {
+    const long long want = mine / all;
+    long long passed = 0;
+    bool found = n <= 0;
+    for (int base = 0; base < a.seqs.batch; base += NT) {
+      if (a.seqs.batch > NT) scan(base + tid, sum);
+      if (!found && want < passed + sum) {
+        int i = -1;  // the last sequence of the chunk with no more than `want` tiles before it
+        for (int k = 0; k < W; ++k) i += __popc(__ballot_sync(0xffffffffu, passed + before[k * 32 + lane] <= want));
+        at.b = base + i;
+        const long long into = mine - (passed + before[i]) * all;
+        int lo, hi;
+        const int tiles = Warp::tiles_of(a, at.b, lo, hi);
+        at.j = static_cast<int>(into / tiles), at.tile = static_cast<int>(into % tiles);
+        found = true;
+      }
+      passed += sum;
+      if (a.seqs.batch > NT) __syncthreads();
+    }
+  }
+
+  Warp w(a, smem_u32(rings + warp * (S::kStages * S::kStage)));
+  if (lane < 2) pieces[warp * 2 + lane] = {-1, 0, 0, 0};
+  __syncwarp();
+  if (n > 0) {
+    w.sequence(at);
+    typename Warp::Cursor next = at;
+    int page, place, filled = 0;
+    w.find(next, page, place);
+    const auto fill = [&]() {
+      if (filled < n) {
+        w.fill(filled % S::kStages, next, page, place);
+        if (++filled < n) {
+          w.advance(next);
+          w.find(next, page, place);
+        }
+      }
+      copies_commit();
+    };
+    for (int i = 0; i < S::kStages - 1; ++i) fill();
+    bool starts = at.tile == 0, fresh = true;
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+      copies_wait<S::kStages - 2>();
+      __syncwarp();
+      fill();
+      if (fresh) w.begin(at);
+      w.tile(i % S::kStages);
+      fresh = at.tile == at.tiles - 1;
+      if (fresh || i == n - 1) {
+        const int part = at.j % a.parts, heads = min(H, a.group - part * H);
+        if (starts && fresh) {  // all of it
+          const int64_t head0 = static_cast<int64_t>(at.b) * a.q_heads + at.j / a.parts * a.group + part * H;
+          float inv[Warp::HC];
+          w.end(
+              [&](int head, int hc, int e, float v) {
+                if (head < heads && e < a.cache.dim) store_out(a, (head0 + head) * a.cache.dim + e, v * inv[hc]);
+              },
+              [&](int head, int hc, float top, float l) {
+                inv[hc] = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
+                if (a.lse && head < heads && w.g == 0) a.lse[head0 + head] = lse_of(top, l);
+              });
+        } else {
+          __syncwarp();
+          // (a piece that begins here lasts to the end of this warp's tiles: its place is the ring, where nothing is left to come)
+          float *to = starts ? reinterpret_cast<float *>(rings + warp * (S::kStages * S::kStage)) : heads_of_parts + warp * S::kPart;
+          w.end([&](int head, int, int e, float v) { to[2 * H + head * DP + e] = v; },
+                [&](int head, int, float top, float l) {
+                  if (w.g == 0) to[head] = top, to[H + head] = l;
+                });
+          if (lane == 0) pieces[warp * 2 + starts] = {at.b, at.j, fresh, 0};
+        }
+        starts = true;
+      }
+      if (i < n - 1) w.advance(at);
+    }
+  }
+  __syncthreads();
+
+  // The parts of a sequence's piece in this CTA, joined: one that goes on from the CTA before (slot 0 of warp 0), and those that begin in a
+  // warp (slot 1).  What is not whole goes out with a note.
+  bool noted[2] = {false, false};
+  for (int c = 0; c <= W; ++c) {
+    const int w0 = c == 0 ? 0 : c - 1, slot = c == 0 ? 0 : 1;
+    const AttendPiece p = pieces[w0 * 2 + slot];
+    if (p.b < 0) continue;
+    int last = w0, ends = p.ends;
+    while (!ends && last + 1 < W && pieces[(last + 1) * 2].b >= 0) ends = pieces[++last * 2].ends;
+    const bool whole = slot == 1 && ends;
+    const auto part_of = [&](int v) {
+      return v == w0 && slot == 1 ? reinterpret_cast<const float *>(rings + v * (S::kStages * S::kStage)) : heads_of_parts + v * S::kPart;
+    };
+    const int part = p.j % a.parts, heads = min(H, a.group - part * H);
+    const int64_t head0 = static_cast<int64_t>(p.b) * a.q_heads + p.j / a.parts * a.group + part * H;
+    float *to = a.partial + (blockIdx.x * 2 + slot) * static_cast<int64_t>(S::kPart);
+    for (int i = tid; i < heads * DP; i += NT) {
+      const int head = i / DP, e = i % DP;
+      float top = -INFINITY, l = 0.0f, v = 0.0f;
+      for (int k = w0; k <= last; ++k) top = fmaxf(top, part_of(k)[head]);
+      const float base = top == -INFINITY ? 0.0f : top;
+      for (int k = w0; k <= last; ++k) {
+        const float *from_part = part_of(k), by = exp2_fast(from_part[head] - base);
+        l = fmaf(from_part[H + head], by, l), v = fmaf(from_part[2 * H + i], by, v);
+      }
+      if (whole) {
+        if (e < a.cache.dim) store_out(a, (head0 + head) * a.cache.dim + e, share(v, l));
+        if (e == 0 && a.lse) a.lse[head0 + head] = lse_of(top, l);
+      } else {
+        to[2 * H + i] = v;
+        if (e == 0) to[head] = top, to[H + head] = l;
+      }
+    }
+    if (!whole) {
+      noted[slot] = true;
+      if (tid == 0) a.piece[blockIdx.x * 2 + slot] = {p.b, p.j, ends, 0};
+    }
+  }
+  if (tid < 2 && !noted[tid]) a.piece[blockIdx.x * 2 + tid] = {-1, 0, 0, 0};
+}
+
+// a launch of the kernel: the grid that fills the GPU
+struct AttendPlan {
+  int ctas, heads, width, part;  // CTAs, query heads of a piece, DP, floats of a piece
+};
+template <class S>
+cudaError_t run_attend(const AttendArgs *a, AttendPlan *plan, cudaStream_t st) {
+  plan->ctas = sm_count() * S::kCtas, plan->heads = S::kHeads, plan->width = S::DP, plan->part = S::kPart;
+  if (!a) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(attend_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+  if (e != cudaSuccess) return e;
+  attend_kernel<S><<<plan->ctas, S::kWarps * 32, S::kSmem, st>>>(*a);
+  return cudaGetLastError();
+}
+// two blocks of columns where one does not hold the group
+template <typename C, int DP, int P>
+cudaError_t run_columns(int group, const AttendArgs *a, AttendPlan *plan, cudaStream_t st) {
+  if constexpr (DP <= 128) {
+    if (group * P > 8) return run_attend<AttendShape<C, DP, 2, P>>(a, plan, st);
+  }
+  return run_attend<AttendShape<C, DP, 1, P>>(a, plan, st);
+}
+template <typename C, int P>
+cudaError_t run_width(int dim, int group, const AttendArgs *a, AttendPlan *plan, cudaStream_t st) {
+  if (dim <= 32) return run_columns<C, 32, P>(group, a, plan, st);
+  if (dim <= 64) return run_columns<C, 64, P>(group, a, plan, st);
+  if (dim <= 128) return run_columns<C, 128, P>(group, a, plan, st);
+  return run_columns<C, 256, P>(group, a, plan, st);
+}
+
+// by the cache's type (attend_codes.cu, attend_pieces.cu, attend_half.cu, attend_bf16.cu); a: NULL for the plan alone
+cudaError_t run_attend_codes(int dim, int group, const AttendArgs *a, AttendPlan *plan, cudaStream_t st);   // one piece
+cudaError_t run_attend_pieces(int dim, int group, const AttendArgs *a, AttendPlan *plan, cudaStream_t st);  // two
+cudaError_t run_attend_half(int dim, int group, const AttendArgs *a, AttendPlan *plan, cudaStream_t st);
+cudaError_t run_attend_bf16(int dim, int group, const AttendArgs *a, AttendPlan *plan, cudaStream_t st);
+
+}  // namespace aecct

@@ -6,7 +6,10 @@ head (a float32 q is cut into two pieces of 11 bits, 2^-22 of it, inside of that
 by its own rounding w: 2^-22 for exp2, and to the type that the tensor cores take: 2^-11 for bfloat16 queries on codes (one
 piece in half), 2^-16 for a cache in bfloat16 (two pieces), else 2^-22 (two pieces in half).  Weights change the output both in the sum and
 under the quotient: (2 e + 2 w) sum_j p_j |v_j|; its additions in 32 bits, one for 16 keys and some for the parts, add
-(n / 16 + 64) 2^-23 of it; the result is rounded once."""
+(n / 16 + 64) 2^-23 of it; the result is rounded once.
+Weights in half end at its smallest step, 2^-24: one that is less than 2^-29 of the largest, which is 2^14 to 2^15, is off by half
+a step, 2^-25, and not by a part of itself.  In units of the largest weight with its row's scale, max_j p_j vs_j, that is 2^-39 at most (vs = 1 for
+rows without a scale), and over the keys 2^-39 max_j (p_j vs_j) sum_j |c_jd|, c the codes (or a half cache's values)."""
 import math
 
 import pytest
@@ -51,13 +54,13 @@ def make(lens, heads, group, dim, page, dtype, cache_dtype, seed=0, spread=1.0, 
 
 
 def reference(q, cache, table, lengths, first=None, scale=None):
-    """Output and lse in 64 bits, with the largest absolute score and the weighted sum of |v| that the tolerances take."""
+    """Output and lse in 64 bits, and what the tolerances take: the largest absolute score, the weighted sum of |v|, the steps of small weights."""
     pages, heads, page, dim = cache.k.shape
     batch, hq = q.shape[:2]
     scale = dim ** -0.5 if scale is None else scale
     out = torch.zeros((batch, hq, dim), dtype=torch.float64, device="cuda")
     lse = torch.full((batch, hq), -math.inf, dtype=torch.float64, device="cuda")
-    big, mass = torch.zeros((batch, hq, 1), dtype=torch.float64, device="cuda"), torch.zeros_like(out)
+    big, mass, step = torch.zeros((batch, hq, 1), dtype=torch.float64, device="cuda"), torch.zeros_like(out), torch.zeros_like(out)
     for b in range(batch):
         n = min(max(0, int(lengths[b])), table.shape[1] * page)
         at = torch.arange(min(n, max(0, int(first[b]))) if first is not None else 0, n, device="cuda")
@@ -75,17 +78,21 @@ def reference(q, cache, table, lengths, first=None, scale=None):
         lse[b] = torch.logsumexp(s, 1)
         p = torch.softmax(s, 1)[:, None]
         out[b], mass[b] = (p @ v)[:, 0], (p @ v.abs())[:, 0]
-    return out, lse, big, mass
+        vs = torch.ones_like(p) if cache.v_scale is None else cache.v_scale[on, :, at % page].double().t().repeat_interleave(hq // heads, 0)[:, None]
+        step[b] = 2.0 ** -39 * (p * vs).amax(2) * (v.abs() / vs[:, 0, :, None]).sum(1)
+    return out, lse, big, mass, step
 
 
 def check(q, cache, table, lengths, first=None, scale=None, **kw):
     out, lse = A.paged_attention(q, cache, table, lengths, first=first, scale=scale, want_lse=True, **kw)
-    want, wl, big, mass = reference(q, cache, table, lengths, first, scale)
+    want, wl, big, mass, step = reference(q, cache, table, lengths, first, scale)
     assert out.dtype == q.dtype and out.shape == q.shape and lse.shape == q.shape[:2] and lse.dtype == F32
     n, dim = max(1, int(lengths.max())), q.shape[2]
     e = (dim + 8) * 2.0 ** -23 * big
     w = 2.0 ** -11 if q.dtype is BF16 and cache.k.dtype is I8 else 2.0 ** -16 if cache.k.dtype is BF16 else 2.0 ** -22
     tol = (2 * e + 2 * (w + 2.0 ** -22) + (n / 16 + 64) * 2.0 ** -23) * mass + HALF[q.dtype] * want.abs() + TINY[q.dtype]
+    if cache.k.dtype is not BF16:
+        tol = tol + step
     off = (out.double() - want).abs()
     assert (off <= tol).all(), (off / tol).max().item()
     empty = wl == -math.inf
