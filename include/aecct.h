@@ -417,7 +417,8 @@ typedef struct {
  *   the first top_k of them stay (all for top_k <= 0); of these the shortest beginning whose weight is at least
  *   top_p of theirs, and no less than one token (all for top_p >= 1); of these the tokens with w_i >= min_p;
  *   token = the lowest index i among those that stay with sum over j <= i of w_j > u sum over all of w_j.
- * A temperature of 0 (or less, or NaN) takes the largest logit, the lowest index among equal ones.  Logits of minus infinity
+ * A temperature of 0 (or less, or NaN) takes the largest logit, the lowest index among equal ones; others count as 2^-100 at
+ * least and 2^100 at most.  Logits of minus infinity
  * and NaN never stay; a row with no other gets token -1.  Where logits of plus infinity occur only those stay, with equal
  * weights.  u < 0 or NaN counts as 0, u >= 1 takes the last token that stays.
  * Weights are fixed-point numbers of 44 bits behind the point and sums of them exact, so that a token hangs on nothing but its row

@@ -435,6 +435,7 @@ struct SampleCall {
   float temperature_all, top_p_all, min_p_all;
   int top_k_all;
   int64_t *tokens;
+  int ctas;  // to a row: the launcher's choice
 };
 cudaError_t launch_sample(const SampleCall &c, cudaStream_t stream);
 

@@ -1504,7 +1504,7 @@ int aecct_sample(const void *logits, int64_t ld, int64_t rows, int32_t vocab, in
   if (rows == 0) return AECCT_OK;
   if (!is_array(logits, dtype) || !is_array(u, AECCT_F32) || !tokens || (reinterpret_cast<uintptr_t>(tokens) & 7u)) return AECCT_ERR_INVALID_ARG;
   const SampleCall c = {logits, ld, static_cast<int>(rows), vocab, dtype, u, set->temperature_dev, set->top_p_dev, set->min_p_dev, set->top_k_dev,
-                        set->temperature, set->top_p, set->min_p, set->top_k, tokens};
+                        set->temperature, set->top_p, set->min_p, set->top_k, tokens, 1};
   const cudaError_t e = launch_sample(c, static_cast<cudaStream_t>(cuda_stream));
   return e == cudaSuccess ? AECCT_OK : cuda_fail(e, "sample launch");
 }

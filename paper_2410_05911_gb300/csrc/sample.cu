@@ -1,7 +1,17 @@
 // sample.cu -- the next token of a row of logits: temperature, top-k, top-p, min-p, and a given random number.
 //
-//   w_i = exp((x_i - max x) / temperature), as a whole number of 2^-44: sums of up to 2^19 of them are exact in 64 bits, so that
-//   a cut or a choice hangs on no order of additions
+//   w_i = exp((x_i - top) / temperature) = 2^-(c (top - x_i)),  c = log2 e / temperature,  as a whole number of 2^-44
+//
+// Sums of up to 2^19 weights are exact in 64 bits, so that a cut or a choice hangs on no order of additions.  What stays is
+// always "every logit above `cut`, and the first `ties` of those equal to it": top-k, top-p and min-p each move the cut up.
+//
+// No sort.  A cut is found from histograms: first over equal steps of c (top - x) (2,048 of 2^-6, so that logits spread over the bins),
+// which bound the mass of a bin by its edges, to 1.1%, from its count alone; then over the keys (logits as ordered whole numbers) between the
+// bounds, until a bin is one key, whose mass is its count times its weight.  Weights are summed one by one only above the
+// bounds, and for the whole.  Each of these is a pass over the row, which L2 holds: the row is read from memory once.
+//
+// A cluster of 1 to 8 CTAs takes a row, each a part of it, and reads the others' histograms and sums through distributed
+// shared memory.
 #include <cuda_runtime.h>
 
 #include <cmath>
@@ -9,175 +19,574 @@
 
 #include "aecct_internal.h"
 #include "rowtypes.cuh"
+#include "sm103_ptx.cuh"
 
 namespace aecct {
 
 namespace {
 
-constexpr int kSampleThreads = 1024;
+using u64 = unsigned long long;
+constexpr int kSampleThreads = 1024, kSampleWarps = kSampleThreads / 32;
+constexpr int kBins = 2 * kSampleThreads;
+constexpr int kSteps = 256;  // of the table of powers of two
+constexpr int kStepsPerBin = 4;
+constexpr float kTemperatureMin = 0x1p-100f, kTemperatureMax = 0x1p100f;
 
-// logits in an order that whole numbers have; NaN below everything
-__device__ __forceinline__ uint32_t key_of(float x) {
-  const uint32_t b = __float_as_uint(x == 0.0f ? 0.0f : x);
-  return x != x ? 0u : (b & 0x80000000u) ? ~b : b | 0x80000000u;
-}
-__device__ __forceinline__ float logit_of(uint32_t key) { return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key); }
-constexpr uint32_t kNone = 0x007fffffu;  // the key of minus infinity: what is not above it never stays
-
-__device__ unsigned long long block_sum(unsigned long long v, unsigned long long *buf) {
-  for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
-  __syncthreads();
-  if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = v;
-  __syncthreads();
-  unsigned long long s = 0;
-  for (int i = 0; i < kSampleThreads / 32; ++i) s += buf[i];
-  return s;
-}
-
-__device__ __forceinline__ unsigned long long weight(uint32_t key, uint32_t top, double by) {
-  if (key == top) return 1ull << 44;
-  return __double2ull_rn(exp((static_cast<double>(logit_of(key)) - static_cast<double>(logit_of(top))) * by) * 0x1p44);
-}
-
-// a CTA to a row
-template <typename T>
-__global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall c) {
-  __shared__ unsigned long long buf[32];
-  __shared__ unsigned long long cut_u64;
-  const int row = blockIdx.x;
-  const T *x = static_cast<const T *>(c.logits) + row * c.ld;
-  const float t = c.temperature ? c.temperature[row] : c.temperature_all, p = c.top_p ? c.top_p[row] : c.top_p_all;
-  const float mp = c.min_p ? c.min_p[row] : c.min_p_all;
-  const int k = c.top_k ? c.top_k[row] : c.top_k_all;
-  const int per = (c.vocab + kSampleThreads - 1) / kSampleThreads, lo = threadIdx.x * per, hi = min(c.vocab, lo + per);  // a thread's tokens
-  uint32_t top = 0;
-  for (int i = lo; i < hi; ++i) top = max(top, key_of(to_f32(x[i])));
-  top = __reduce_max_sync(0xffffffffu, top);
-  if ((threadIdx.x & 31) == 0) buf[threadIdx.x >> 5] = top;
-  __syncthreads();
-  for (int i = 0; i < kSampleThreads / 32; ++i) top = max(top, static_cast<uint32_t>(buf[i]));
-  if (top <= kNone) {
-    if (threadIdx.x == 0) c.tokens[row] = -1;
-    return;
+// 2^-(j / 256), as a whole number of 2^-44 and as a float.  From square roots of 1/2, by Newton's iteration, and their products.
+struct PowerTable {
+  struct Entry {
+    u64 whole;
+    float value;
+    uint32_t pad;
+  } e[kSteps];
+  constexpr PowerTable() : e{} {
+    double root[8] = {};
+    double r = 0.5;
+    for (int i = 7; i >= 0; --i) {
+      double s = r;
+      for (int k = 0; k < 60; ++k) s = 0.5 * (s + r / s);
+      root[i] = r = s;  // 2^-(2^i / 256)
+    }
+    for (int j = 0; j < kSteps; ++j) {
+      double v = 1.0;
+      for (int i = 0; i < 8; ++i)
+        if (j >> i & 1) v *= root[i];
+      e[j].whole = static_cast<u64>(v * 0x1p44 + 0.5), e[j].value = static_cast<float>(v);
+    }
   }
-  const double by = 1.0 / static_cast<double>(t);
-  // the sum of f over the row's tokens
-  const auto total = [&](auto f) {
-    unsigned long long s = 0;
-    for (int i = lo; i < hi; ++i) s += f(key_of(to_f32(x[i])));
-    return block_sum(s, buf);
-  };
-  // A beginning of the descending order is "keys above `cut`, and the first `ties` of those that are the same".
-  uint32_t cut = t > 0.0f ? kNone : top;
-  int64_t ties = t > 0.0f ? 0 : 1;
-  // the shortest beginning with at least `want` of f, among the one at hand
-  const auto shorten = [&](auto f, auto enough) {
-    uint32_t a = cut, z = top;  // the largest key v with enough in keys >= v, or `cut` itself
-    while (a < z) {
-      const uint32_t mid = a + (z - a + 1) / 2;
-      if (enough(total([&](uint32_t key) { return key >= mid ? f(key) : 0ull; }))) a = mid;
-      else z = mid - 1;
-    }
-    if (a == cut && ties == 0) return;  // (all of them)
-    const unsigned long long above = total([&](uint32_t key) { return key > a ? f(key) : 0ull; }), one = f(a);
-    const int64_t have = a == cut ? ties : INT64_MAX;
-    int64_t n = 0, most = static_cast<int64_t>(total([&](uint32_t key) { return key == a ? 1ull : 0ull; }));
-    if (most > have) most = have;
-    int64_t l = 0, r = most;  // the fewest of the equal ones that are enough
-    while (l < r) {
-      const int64_t mid = (l + r) / 2;
-      if (enough(above + mid * one)) r = mid;
-      else l = mid + 1;
-    }
-    n = l;
-    cut = a, ties = n;
-  };
-  const auto mass = [&](uint32_t key) { return key > kNone ? weight(key, top, by) : 0ull; };
-  if (t > 0.0f) {
-    if (top == 0xff800000u) cut = top - 1;  // plus infinity: only those
-    if (k > 0) shorten([&](uint32_t key) { return 1ull; }, [&](unsigned long long n) { return n >= static_cast<unsigned long long>(k); });
-    if (p < 1.0f) {
-      // (the tokens at the cut: the first `ties` of them)
-      const unsigned long long above = total([&](uint32_t key) { return key > cut ? mass(key) : 0ull; });
-      const unsigned long long all = above + ties * mass(cut);
-      const double want = static_cast<double>(p) * static_cast<double>(all);
-      if (ties > 0) {
-        const uint32_t c0 = cut;
-        const int64_t t0 = ties;
-        if (static_cast<double>(above) >= want) {
-          cut = c0, ties = 0;
-          shorten(mass, [&](unsigned long long n) { return n > 0 && static_cast<double>(n) >= want; });
+};
+__device__ const PowerTable kPowers;
+
+// Logits in an order that whole numbers have, and back; no NaN comes here, and both zeros are one number.  A key has the bits that type T
+// has (a number between two of them gets the key of one of them).
+template <typename T>
+struct KeyOf {
+  static constexpr int kDrop = sizeof(T) == 4 ? 0 : std::is_same_v<T, __half> ? 13 : 16;
+  static __device__ __forceinline__ uint32_t key(float x) {
+    const uint32_t b = __float_as_uint(x == 0.0f ? 0.0f : x);
+    return ((b & 0x80000000u) ? ~b : b | 0x80000000u) >> kDrop;
+  }
+  static __device__ __forceinline__ float logit(uint32_t key) {
+    const uint32_t k = key << kDrop;
+    return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~(k | ((1u << kDrop) - 1)));
+  }
+};
+
+__device__ __forceinline__ u64 ld_cluster_u64(uint32_t addr) {
+  u64 v;
+  asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
+  return v;
+}
+__device__ __forceinline__ uint2 ld_cluster_u32x2(uint32_t addr) {
+  uint2 v;
+  asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "r"(addr) : "memory");
+  return v;
+}
+
+struct SampleShared {
+  PowerTable::Entry power[kSteps];
+  uint32_t count[2][kBins];
+  u64 warp[kSampleWarps][2];
+  u64 part[2][2];                // this CTA's sums, for the cluster
+  u64 segment[2][kSampleWarps];  // a number of each warp's part of the row
+  uint32_t found[2];
+  u64 found_sum[2];
+  double least;          // temperature ln min_p
+  float c, c_low, floor;  // log2 e / temperature, and the lowest logit that min_p leaves
+};
+
+// floor(f n) and whether something was cut off, for 0 < f < 1
+__device__ __forceinline__ u64 times(float f, u64 n, bool &more) {
+  const uint32_t b = __float_as_uint(f), e = b >> 23, m = e ? (b & 0x7fffffu) | 0x800000u : b & 0x7fffffu;
+  const int shift = 150 - static_cast<int>(e ? e : 1);  // f = m 2^-shift, 24 <= shift <= 149
+  const u64 low = m * n, high = __umul64hi(m, n);
+  if (shift >= 64) {
+    const int s = shift - 64;
+    more = low != 0 || (s < 64 ? (high & ((1ull << s) - 1)) : high) != 0;
+    return s < 64 ? high >> s : 0;
+  }
+  more = (low & ((1ull << shift) - 1)) != 0;
+  return (low >> shift) | (high << (64 - shift));
+}
+
+template <typename T>
+struct SampleRow {
+  static constexpr int V = 16 / sizeof(T);
+  const T *x;
+  int vocab, shift;         // shift: elements from the 16-byte border before x to x
+  int block, blocks;        // this warp's blocks of V elements: block, ..., block + blocks - 1
+  SampleShared &sh;
+  const int lane, warp;
+  const uint32_t rank, ctas;
+  int flip = 0, hist = 0;  // which of two places the next sum and the next histogram take
+
+  float top, c, c_low, bin_by;  // log2 e / temperature in two floats; bins per logit
+  float lowest;                 // logits below it never stay
+
+  __device__ SampleRow(SampleShared &s, uint32_t r, uint32_t n) : sh(s), lane(threadIdx.x & 31), warp(threadIdx.x >> 5), rank(r), ctas(n) {}
+
+  __device__ void sync() const {
+    if (ctas > 1) cluster_sync_all();
+    else __syncthreads();
+  }
+
+  // f(logit, index) for this lane's elements, a block of V at a time in ascending order of the warp's; g(block) after each
+  template <class F, class G>
+  __device__ __forceinline__ void blocks_of(F &&f, G &&g) const {
+    constexpr int kAhead = 4;
+    for (int b = 0; b < blocks; b += 32 * kAhead) {
+      float v[kAhead][V];
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) {
+        const int q = b + a * 32 + lane;
+        const int64_t i = static_cast<int64_t>(block + q) * V - shift;
+        if (q < blocks && i >= 0 && i + V <= vocab) {
+          load_v<T, V>(x + i, v[a]);
         } else {
-          int64_t l = 0, r = t0;
-          while (l < r) {
-            const int64_t mid = (l + r) / 2;
-            if (static_cast<double>(above + mid * mass(c0)) >= want) r = mid;
-            else l = mid + 1;
-          }
-          ties = l;
+#pragma unroll
+          for (int e = 0; e < V; ++e) v[a][e] = q < blocks && i + e >= 0 && i + e < vocab ? to_f32(x[i + e]) : NAN;
         }
-      } else {
-        shorten(mass, [&](unsigned long long n) { return n > 0 && static_cast<double>(n) >= want; });
+      }
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) {
+        const int i = (block + b + a * 32 + lane) * V - shift;
+#pragma unroll
+        for (int e = 0; e < V; ++e) f(v[a][e], i + e);
+        if (b + a * 32 < blocks) g();
       }
     }
   }
-  // rank among the equal ones at the cut
-  const auto scan = [&](unsigned long long v) {  // exclusive, over the threads
-    __shared__ unsigned long long part[kSampleThreads];
-    __syncthreads();
-    part[threadIdx.x] = v;
-    __syncthreads();
-    unsigned long long s = 0;
-    for (int i = 0; i < static_cast<int>(threadIdx.x); ++i) s += part[i];
-    return s;
-  };
-  unsigned long long mine = 0;
-  for (int i = lo; i < hi; ++i) mine += key_of(to_f32(x[i])) == cut;
-  const unsigned long long rank0 = scan(mine);
-  const double least = mp > 0.0f ? log(static_cast<double>(mp)) * static_cast<double>(t) : -INFINITY;
-  const auto stays = [&](uint32_t key, unsigned long long &rank) {
-    if (key <= kNone || key < cut) return false;
-    if (key == cut && rank++ >= static_cast<unsigned long long>(ties)) return false;
-    return key == top || static_cast<double>(logit_of(key)) - static_cast<double>(logit_of(top)) >= least;
-  };
-  const auto weight_of = [&](uint32_t key) { return t > 0.0f ? weight(key, top, by) : 1ull; };
-  unsigned long long sum = 0, rank = rank0;
-  int first = INT32_MAX, last = -1;
-  for (int i = lo; i < hi; ++i) {
-    const uint32_t key = key_of(to_f32(x[i]));
-    if (stays(key, rank)) sum += weight_of(key), first = min(first, i), last = i;
+  template <class F>
+  __device__ __forceinline__ void each(F &&f) const {
+    blocks_of([&](float v, int) { f(v); }, [] {});
   }
-  const unsigned long long all = block_sum(sum, buf), before = scan(sum);
-  const float u = c.u[row];
-  const unsigned long long target = u > 0.0f ? static_cast<unsigned long long>(static_cast<double>(u) * static_cast<double>(all)) : 0ull;
-  if (threadIdx.x == 0) cut_u64 = ~0ull;
+
+  __device__ __forceinline__ u64 weight(float v) const {
+    // c (top - v) in two floats; the difference is exact as a sum of two (Knuth)
+    const float d = top - v, t = d - top, d_low = (top - (d - t)) - (v + t);
+    float y = d * c;
+    float y_low = fmaf(d, c, -y);
+    y_low = fmaf(d, c_low, y_low);
+    y_low = fmaf(d_low, c, y_low);
+    if (!(y < 60.0f)) y = y_low = 0.0f, y = 60.0f;
+    const float j = fmaf(y, static_cast<float>(kSteps), 12582912.0f);  // (1.5 2^23: rounded to a whole number)
+    const uint32_t n = __float_as_uint(j) & 0xffffu;
+    const float r = (fmaf(j - 12582912.0f, -1.0f / kSteps, y) + y_low) * -0.6931471805599453f;  // |r| < 2^-9.5
+    const float q = fmaf(r * r, fmaf(r, 1.0f / 6.0f, 0.5f), r);                                 // e^r - 1, to 2^-42
+    const PowerTable::Entry e = sh.power[n % kSteps];
+    const int add = __float2int_rn(e.value * q * 0x1p39f);
+    return v == top ? 1ull << 44 : (e.whole + static_cast<u64>(static_cast<int64_t>(add) << 5)) >> (n / kSteps);
+  }
+  // an upper and a lower bound of what weight() says for all logits between (that of hi and that of lo are 2^-31 of themselves and a
+  // unit off at most)
+  static __device__ u64 above(u64 w) { return w + (w >> 30) + 2; }
+  static __device__ u64 below(u64 w) { return w < 4 ? 0 : w - (w >> 30) - 2; }
+
+  // sums over the row of two numbers
+  __device__ void sums(u64 &a, u64 &b) {
+    for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o), b += __shfl_xor_sync(0xffffffffu, b, o);
+    if (lane == 0) sh.warp[warp][0] = a, sh.warp[warp][1] = b;
+    __syncthreads();
+    if (warp == 0) {
+      a = sh.warp[lane][0], b = sh.warp[lane][1];
+      for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o), b += __shfl_xor_sync(0xffffffffu, b, o);
+      if (lane == 0) sh.part[flip][0] = a, sh.part[flip][1] = b;
+    }
+    sync();
+    a = b = 0;
+    const uint32_t at = smem_u32(sh.part[flip]);
+    for (uint32_t r = 0; r < ctas; ++r) a += ld_cluster_u64(mapa_cluster(at, r)), b += ld_cluster_u64(mapa_cluster(at + 8, r));
+    flip ^= 1;
+  }
+  __device__ float maximum(float v) {
+    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    if (lane == 0) sh.warp[warp][0] = __float_as_uint(v);
+    __syncthreads();
+    v = __uint_as_float(static_cast<uint32_t>(sh.warp[lane][0]));
+    for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
+    if (threadIdx.x == 0) sh.part[flip][0] = __float_as_uint(v);
+    sync();
+    for (uint32_t r = 0; r < ctas; ++r)
+      v = fmaxf(v, __uint_as_float(static_cast<uint32_t>(ld_cluster_u64(mapa_cluster(smem_u32(sh.part[flip]), r)))));
+    flip ^= 1;
+    return v;
+  }
+  // sum over the threads before this one, in its CTA, and over all (the row's bins lie in thread order in every CTA)
+  __device__ u64 before(u64 v, u64 &all) {
+    u64 s = v;
+    for (int d = 1; d < 32; d <<= 1) {
+      const u64 w = __shfl_up_sync(0xffffffffu, s, d);
+      if (lane >= d) s += w;
+    }
+    __syncthreads();
+    if (lane == 31) sh.warp[warp][0] = s;
+    __syncthreads();
+    u64 w = sh.warp[lane][0], e = w;
+    for (int d = 1; d < 32; d <<= 1) {
+      const u64 z = __shfl_up_sync(0xffffffffu, w, d);
+      if (lane >= d) w += z;
+    }
+    all = __shfl_sync(0xffffffffu, w, 31);
+    return __shfl_sync(0xffffffffu, w - e, warp) + s - v;
+  }
+
+  // counts of the row's logits by bin(logit) (negative: in none); this thread's are bins 2 i and 2 i + 1
+  template <class F>
+  __device__ uint2 histogram(F &&bin) {
+    uint32_t *count = sh.count[hist];
+    for (int i = threadIdx.x; i < kBins; i += kSampleThreads) count[i] = 0;
+    __syncthreads();
+    each([&](float v) {
+      const int b = bin(v);
+      if (b >= 0) atomicAdd(count + b, 1u);
+    });
+    sync();
+    uint2 n = {0, 0};
+    const uint32_t at = smem_u32(count + 2 * threadIdx.x);
+    for (uint32_t r = 0; r < ctas; ++r) {
+      const uint2 m = ld_cluster_u32x2(mapa_cluster(at, r));
+      n.x += m.x, n.y += m.y;
+    }
+    hist ^= 1;
+    return n;
+  }
+  // the bin of equal steps: off by less than 2^-11 of one (three roundings of a number below 2^11)
+  __device__ __forceinline__ int step_bin(float v) const {
+    return v >= lowest ? (v == top ? 0 : __float2int_rd(fminf((top - v) * bin_by, static_cast<float>(kBins - 1)))) : -1;
+  }
+  // a logit that no logit of a bin >= b is above, and one that none of a bin <= b is below
+  __device__ float bin_high(int b) const { return b <= 1 ? top : fminf(top, __fsub_ru(top, __fmul_rd(static_cast<float>(b - 1), __frcp_rd(bin_by)))); }
+  __device__ float bin_low(int b) const {
+    return b >= kBins - 2 ? lowest : fmaxf(lowest, __fsub_rd(top, __fmul_ru(static_cast<float>(b + 2), __frcp_ru(bin_by))));
+  }
+  __device__ u64 bin_power(int b) const { return sh.power[b * kStepsPerBin % kSteps].whole >> (b * kStepsPerBin / kSteps); }
+
+  // the bin that one thread has found, and the sum before it
+  __device__ void publish(uint32_t bin, u64 sum) { sh.found[0] = bin, sh.found_sum[0] = sum; }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call) {
+  __shared__ SampleShared sh;
+  const uint32_t ctas = call.ctas, rank = ctas > 1 ? cluster_ctarank() : 0;
+  const int row = blockIdx.x / ctas, tid = threadIdx.x;
+  SampleRow<T> r(sh, rank, ctas);
+  constexpr int V = SampleRow<T>::V;
+  using K = KeyOf<T>;
+  r.x = static_cast<const T *>(call.logits) + row * call.ld, r.vocab = call.vocab;
+  r.shift = static_cast<int>((reinterpret_cast<uintptr_t>(r.x) & 15u) / sizeof(T));
+  {
+    const int blocks = (call.vocab + r.shift + V - 1) / V, per = (blocks + ctas * kSampleWarps - 1) / (ctas * kSampleWarps);
+    r.block = static_cast<int>(rank * kSampleWarps + r.warp) * per;
+    r.blocks = max(0, min(per, blocks - r.block));
+  }
+  for (int i = tid; i < kSteps; i += kSampleThreads) sh.power[i] = kPowers.e[i];
+  const float t = call.temperature ? call.temperature[row] : call.temperature_all;
+  const float p = call.top_p ? call.top_p[row] : call.top_p_all, min_p = call.min_p ? call.min_p[row] : call.min_p_all, u = call.u[row];
+  const int k = call.top_k ? call.top_k[row] : call.top_k_all;
+
+  const bool greedy = !(t > 0.0f);
+  if (tid == 0) {  // (a double operation of all the threads takes as long as 300 others)
+    const float kept = fminf(fmaxf(t, kTemperatureMin), kTemperatureMax);
+    const double c = 1.4426950408889634074 / static_cast<double>(kept);
+    sh.c = static_cast<float>(c), sh.c_low = static_cast<float>(c - static_cast<double>(sh.c));
+    sh.least = min_p > 0.0f ? log(static_cast<double>(min_p)) * static_cast<double>(kept) : 0.0;
+  }
+  float most = -INFINITY;
+  r.each([&](float v) { most = fmaxf(most, v); });
+  r.top = most = r.maximum(most);
+  if (most == -INFINITY) {  // (the same in every CTA of the row)
+    if (rank == 0 && tid == 0) call.tokens[row] = -1;
+    if (ctas > 1) cluster_sync_all();
+    return;
+  }
+  if (tid == 0) {  // logits under top + temperature ln min_p go; the largest stays
+    const float v = __double2float_ru(static_cast<double>(most) + sh.least);
+    sh.floor = v < most ? v : most;
+  }
   __syncthreads();
-  if (!(u > 0.0f)) {
-    if (first < INT32_MAX) atomicMin(&cut_u64, static_cast<unsigned long long>(first));
-  } else if (!(u < 1.0f)) {
-    if (last >= 0) atomicMin(&cut_u64, ~1ull - static_cast<unsigned long long>(last));
-  } else {
-    unsigned long long s = before;
-    rank = rank0;
-    for (int i = lo; i < hi; ++i) {
-      const uint32_t key = key_of(to_f32(x[i]));
-      if (!stays(key, rank)) continue;
-      const unsigned long long w = weight_of(key);
-      if (s <= target && s + w > target) atomicMin(&cut_u64, static_cast<unsigned long long>(i));
-      s += w;
+  r.c = sh.c, r.c_low = sh.c_low;
+  r.bin_by = r.c * (kSteps / kStepsPerBin);
+  r.lowest = most == INFINITY ? INFINITY : -3.402823466e38f;
+
+  float cut = r.lowest;       // what stays: logits above it,
+  u64 ties = ~0ull;           // and the first of those equal to it
+  if (greedy) cut = most, ties = 1;
+  const bool by_count = !greedy && k > 0 && k < call.vocab, by_mass = !greedy && p < 1.0f;
+  if (by_count || by_mass) {
+    const uint2 n = r.histogram([&](float v) { return r.step_bin(v); });
+    const u64 m0 = n.x * r.bin_power(2 * tid), m1 = n.y * r.bin_power(2 * tid + 1);
+    u64 counts = 0, masses = 0;
+    const u64 n0 = r.before(static_cast<u64>(n.x) + n.y, counts);  // logits before this thread's bins
+    int last = kBins - 1;                                          // the bin of the k-th
+    if (by_count && counts > static_cast<u64>(k)) {
+      const u64 want = static_cast<u64>(k);
+      if (n0 < want && n0 + n.x + n.y >= want) r.publish(2 * tid + (n0 + n.x < want), 0);
+      __syncthreads();
+      last = static_cast<int>(sh.found[0]);
+      // down to one key
+      uint32_t high = K::key(r.bin_high(last)), low = K::key(r.bin_low(last));
+      bool first = true;
+      u64 passed = 0;
+      for (int step = 0; step < 3; ++step) {  // (each leaves a 2,048th of the keys)
+        int shift = 0;
+        while ((high - low) >> shift >= kBins) ++shift;
+        u64 over = 0, none = 0;
+        const uint2 m = r.histogram([&](float v) {
+          if (!(v >= r.lowest)) return -1;
+          const uint32_t key = K::key(v);
+          over += first && key > high;
+          return key <= high && key >= low ? static_cast<int>((high - key) >> shift) : -1;
+        });
+        if (first) r.sums(over, none), passed = over;
+        first = false;
+        u64 all;
+        const u64 at = passed + r.before(static_cast<u64>(m.x) + m.y, all);
+        if (at < want && at + m.x + m.y >= want) r.publish(2 * tid + (at + m.x < want), at + m.x < want ? at + m.x : at);
+        __syncthreads();
+        const uint32_t b = sh.found[0];
+        passed = sh.found_sum[0];
+        __syncthreads();
+        if (shift == 0) {
+          cut = K::logit(high - b), ties = want - passed;
+          break;
+        }
+        high -= b << shift;
+        low = max(low, high - ((1u << shift) - 1));
+      }
+    }
+    if (by_mass) {
+      const float kOver = 1.0f + 0x1p-14f;  // for the bins' own errors, and these roundings
+      const bool x0 = 2 * tid <= last, x1 = 2 * tid + 1 <= last;
+      const u64 before = r.before((x0 ? m0 : 0) + (x1 ? m1 : 0), masses);  // (upper bounds; a lower one is 2^(-1/64) of it)
+      // what the last bin holds may be anything from nothing to its bound
+      if (2 * tid == (last & ~1)) sh.found_sum[1] = last & 1 ? before + m0 : before;
+      if (tid == 0) sh.found[0] = sh.found[1] = static_cast<uint32_t>(last);
+      __syncthreads();
+      const float least = static_cast<float>(sh.found_sum[1]) * 0.98922f, all = static_cast<float>(masses);
+      const float want_low = p * fmaxf(least, 0x1p44f) / kOver, want_high = p * all * 1.0109f * kOver;  // (the largest logit alone has 2^44)
+      // the first bin whose upper bound, and the first whose lower bound reaches what is wanted
+      for (int i = 0; i < 2; ++i) {
+        const u64 lo = i == 0 ? before : before + m0, hi = lo + (i == 0 ? m0 : m1);
+        const int b = 2 * tid + i;
+        if (b < last && (b == 0 || static_cast<float>(lo) < want_low) && static_cast<float>(hi) >= want_low) sh.found[0] = b;
+        if (b < last && (b == 0 || static_cast<float>(lo) < want_high) && static_cast<float>(hi) >= want_high) sh.found[1] = b;
+      }
+      __syncthreads();
+      uint32_t high = K::key(r.bin_high(static_cast<int>(sh.found[0]))), low = max(K::key(r.bin_low(static_cast<int>(sh.found[1]))), K::key(cut));
+      // (46 steps of the logarithm under the largest logit, weights are 0)
+      low = max(low, K::key(fmaxf(r.lowest, __fsub_rd(most, __fmul_ru(46.0f, __frcp_ru(r.c))))));
+      high = max(high, low);
+      // the whole mass, and that above the bounds
+      u64 whole = 0, passed = 0;
+      const float over = K::logit(high);
+      r.each([&](float v) {
+        if (v > cut || (ties == ~0ull && v >= cut)) {
+          const u64 w = r.weight(v);
+          whole += w;
+          if (v > over) passed += w;
+        }
+      });
+      r.sums(whole, passed);
+      if (ties != ~0ull) whole += ties * r.weight(cut);
+      u64 want = 1;
+      if (p > 0.0f) {
+        bool cut_off;
+        want = times(p, whole, cut_off);
+        want += cut_off;
+      }
+      for (int step = 0; step < 33; ++step) {  // (each leaves half of the keys at most)
+        int shift = 0;
+        while ((high - low) >> shift >= kBins) ++shift;
+        const uint2 m = r.histogram([&](float v) {
+          if (!(v >= r.lowest)) return -1;
+          const uint32_t key = K::key(v);
+          return key <= high && key >= low ? static_cast<int>((high - key) >> shift) : -1;
+        });
+        u64 up[2], down[2];
+        for (int i = 0; i < 2; ++i) {
+          const uint32_t b = 2 * tid + i, off = b << shift;
+          const bool in = b <= (high - low) >> shift;
+          const uint32_t k1 = in ? high - off : high, k0 = in && k1 - low >= (1u << shift) - 1 ? k1 - ((1u << shift) - 1) : in ? low : high;
+          u64 count = in ? (i == 0 ? m.x : m.y) : 0;
+          if (shift == 0) {
+            if (K::logit(k1) == cut && count > ties) count = ties;
+            up[i] = down[i] = count ? count * r.weight(K::logit(k1)) : 0;
+          } else {
+            up[i] = count ? count * r.above(r.weight(K::logit(k1))) : 0, down[i] = count ? count * r.below(r.weight(K::logit(k0))) : 0;
+          }
+        }
+        u64 all;
+        const u64 a = passed + r.before(up[0] + up[1], all), d = shift == 0 ? a : passed + r.before(down[0] + down[1], all);
+        const uint32_t bins = ((high - low) >> shift);
+        if (tid == 0) sh.found[0] = sh.found[1] = bins, sh.found_sum[0] = passed;
+        __syncthreads();
+        if (a < want && a + up[0] + up[1] >= want) {
+          const bool second = a + up[0] < want;
+          r.publish(2 * tid + second, second ? a + up[0] : a);
+        }
+        if (d < want && d + down[0] + down[1] >= want) sh.found[1] = 2 * tid + (d + down[0] < want);
+        __syncthreads();
+        const uint32_t b0 = sh.found[0], b1 = sh.found[1];
+        const u64 sum = sh.found_sum[0];
+        __syncthreads();
+        if (shift == 0) {
+          const float v = K::logit(high - b0);
+          const u64 w = r.weight(v), n = (want - sum + w - 1) / w;
+          ties = v == cut && ties < n ? ties : n, cut = v;
+          break;
+        }
+        // between the bounds; where that is more than half of what it was (they may say little of a few wide bins), the half of it that the cut is in
+        const uint32_t range = high - low, next = high - (b0 << shift), least = b1 >= bins ? low : max(low, high - (((b1 + 1) << shift) - 1));
+        const bool halve = next - least > range / 2;
+        const uint32_t mid = least + (next - least) / 2;
+        if (b0 > 0 || halve) {
+          u64 more = 0, half = 0;
+          const float upto = K::logit(high), from = K::logit(next), middle = K::logit(mid);
+          r.each([&](float v) {
+            if (v <= upto && v > middle) {
+              if (v > from) more += r.weight(v);
+              else if (halve) half += r.weight(v);
+            }
+          });
+          r.sums(more, half);
+          passed += more;
+          high = next, low = least;
+          if (halve) {
+            if (passed + half >= want) low = mid + 1;
+            else passed += half, high = mid;
+          }
+        } else {
+          low = least;
+        }
+      }
     }
   }
-  __syncthreads();
-  if (threadIdx.x == 0) c.tokens[row] = static_cast<int64_t>(!(u > 0.0f) || u < 1.0f ? cut_u64 : ~1ull - cut_u64);
+  if (!greedy && min_p > 0.0f && sh.floor > cut) cut = sh.floor, ties = ~0ull;
+
+  // ranks among the equal ones where not all of them stay
+  u64 rank0 = 0;
+  const bool ranked = ties != ~0ull;
+  const auto segments = [&](u64 mine, u64 &all) {  // sum over the warps before this one in the row, and over all
+    __syncthreads();
+    if (r.lane == 0) sh.segment[r.flip][r.warp] = mine;
+    r.sync();
+    u64 s = 0;
+    all = 0;
+    for (uint32_t q = 0; q < ctas; ++q) {
+      u64 v = ld_cluster_u64(mapa_cluster(smem_u32(&sh.segment[r.flip][r.lane]), q)), w = v;
+      for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+      all += v;
+      if (q < rank) s += v;
+      if (q == rank) {
+        w = r.lane < r.warp ? w : 0;
+        for (int o = 16; o > 0; o >>= 1) w += __shfl_xor_sync(0xffffffffu, w, o);
+        s += w;
+      }
+    }
+    r.flip ^= 1;
+    return s;
+  };
+  const auto warp_sum = [&](u64 v) {
+    for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
+    return v;
+  };
+  if (ranked) {
+    u64 n = 0, all;
+    r.each([&](float v) { n += v == cut; });
+    rank0 = segments(warp_sum(n), all);
+    if (all <= ties) ties = ~0ull;
+  }
+  // This warp's mass, in the order of the row: equal ones up to the last that stays are the first of the row.  u at an end takes
+  // the first or the last that stays, whatever their weights are.
+  const bool ends = greedy || !(u > 0.0f) || !(u < 1.0f);
+  const auto weight = [&](float v) { return ends ? 1ull : r.weight(v); };
+  u64 mine = 0, equal = 0;
+  r.each([&](float v) {
+    if (v > cut) mine += weight(v);
+    equal += v == cut;
+  });
+  mine = warp_sum(mine), equal = warp_sum(equal);
+  const u64 left = ranked ? (ties > rank0 ? ties - rank0 : 0) : ~0ull;  // equal ones that stay from this warp on
+  mine += (equal < left ? equal : left) * (equal ? weight(cut) : 0);
+  u64 all;
+  const u64 passed = segments(mine, all);
+  u64 target = 0;
+  if (!(u < 1.0f) && u > 0.0f) target = all - 1;
+  else if (!ends) {
+    bool cut_off;
+    target = times(u, all, cut_off);
+  }
+  if (passed <= target && target < passed + mine) {  // in this warp
+    u64 s = passed, rank_here = rank0;
+    const u64 one = weight(cut);
+    int token = -1;
+    int e = 0, equals = 0, first = 0;
+    float v[V];
+    r.blocks_of(
+        [&](float x, int i) {
+          if (e == 0) first = i, equals = 0;
+          v[e] = x, equals += x == cut;
+          if (++e == V) e = 0;
+        },
+        [&] {
+          int q = equals;  // and those in the lanes before
+          for (int d = 1; d < 32; d <<= 1) {
+            const int o = __shfl_up_sync(0xffffffffu, q, d);
+            if (r.lane >= d) q += o;
+          }
+          // the equal ones that stay are the first `stay` of this block
+          const u64 rank = rank_here + static_cast<u64>(q - equals);
+          const int stay = rank >= ties ? 0 : ties - rank < V ? static_cast<int>(ties - rank) : V;
+          u64 sum = 0;
+          int met = 0;
+#pragma unroll
+          for (int i = 0; i < V; ++i) sum += v[i] > cut ? weight(v[i]) : v[i] == cut && met++ < stay ? one : 0;
+          u64 z = sum;
+          for (int d = 1; d < 32; d <<= 1) {
+            const u64 o = __shfl_up_sync(0xffffffffu, z, d);
+            if (r.lane >= d) z += o;
+          }
+          u64 at = s + z - sum;
+          if (at <= target && target < at + sum) {
+            met = 0;
+#pragma unroll
+            for (int i = 0; i < V; ++i) {
+              const u64 w = v[i] > cut ? weight(v[i]) : v[i] == cut && met++ < stay ? one : 0;
+              if (at <= target && target < at + w) token = first + i;
+              at += w;
+            }
+          }
+          s += __shfl_sync(0xffffffffu, z, 31), rank_here += __shfl_sync(0xffffffffu, q, 31);
+        });
+    if (token >= 0) call.tokens[row] = token;
+  }
+  if (ctas > 1) cluster_sync_all();  // (no CTA ends while another one reads its sums)
+}
+
+template <typename T>
+cudaError_t launch(const SampleCall &c, cudaStream_t st) {
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = static_cast<unsigned>(c.ctas), attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(c.rows) * static_cast<unsigned>(c.ctas));
+  cfg.blockDim = dim3(kSampleThreads);
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, sample_kernel<T>, c);
 }
 
 }  // namespace
 
-cudaError_t launch_sample(const SampleCall &c, cudaStream_t st) {
-  if (c.dtype == 0) sample_kernel<float><<<c.rows, kSampleThreads, 0, st>>>(c);
-  else if (c.dtype == 1) sample_kernel<__half><<<c.rows, kSampleThreads, 0, st>>>(c);
-  else sample_kernel<__nv_bfloat16><<<c.rows, kSampleThreads, 0, st>>>(c);
-  return cudaGetLastError();
+cudaError_t launch_sample(const SampleCall &call, cudaStream_t st) {
+  SampleCall c = call;
+  // CTAs to a row: as long as the GPU has SMs for them, and each has 4,096 logits
+  for (c.ctas = 1; c.ctas < 8 && int64_t(2) * c.ctas * c.rows <= sm_count() && c.vocab >= 2 * c.ctas * 4096;) c.ctas *= 2;
+  if (c.dtype == 0) return launch<float>(c, st);
+  if (c.dtype == 1) return launch<__half>(c, st);
+  return launch<__nv_bfloat16>(c, st);
 }
 
 }  // namespace aecct
