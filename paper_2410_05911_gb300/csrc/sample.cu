@@ -32,13 +32,10 @@ constexpr int kSteps = 256;  // of the table of powers of two
 constexpr int kStepsPerBin = 4;
 constexpr float kTemperatureMin = 0x1p-100f, kTemperatureMax = 0x1p100f;
 
-// 2^-(j / 256), as a whole number of 2^-44 and as a float.  From square roots of 1/2, by Newton's iteration, and their products.
+// 2^-(j / 256) as a whole number of 2^-30.  From square roots of 1/2, by Newton's iteration, and their products.  (Entries of 32 bits: lanes
+// read any of them, and 16-byte ones took most of a pass.)
 struct PowerTable {
-  struct Entry {
-    u64 whole;
-    float value;
-    uint32_t pad;
-  } e[kSteps];
+  uint32_t e[kSteps];
   constexpr PowerTable() : e{} {
     double root[8] = {};
     double r = 0.5;
@@ -51,7 +48,7 @@ struct PowerTable {
       double v = 1.0;
       for (int i = 0; i < 8; ++i)
         if (j >> i & 1) v *= root[i];
-      e[j].whole = static_cast<u64>(v * 0x1p44 + 0.5), e[j].value = static_cast<float>(v);
+      e[j] = static_cast<uint32_t>(v * 0x1p30 + 0.5);
     }
   }
 };
@@ -84,11 +81,15 @@ __device__ __forceinline__ uint2 ld_cluster_u32x2(uint32_t addr) {
 }
 
 struct SampleShared {
-  PowerTable::Entry power[kSteps];
+  uint32_t power[kSteps];
   uint32_t count[2][kBins];
   u64 warp[kSampleWarps][2];
   u64 part[2][2];                // this CTA's sums, for the cluster
   u64 segment[2][kSampleWarps];  // a number of each warp's part of the row
+  struct Hand {
+    u64 passed, rank;
+    int block, blocks;
+  } hand;  // the part of the row that holds the token
   uint32_t found[2];
   u64 found_sum[2];
   double least;          // temperature ln min_p
@@ -130,57 +131,85 @@ struct SampleRow {
     else __syncthreads();
   }
 
-  // f(logit, index) for this lane's elements, a block of V at a time in ascending order of the warp's; g(block) after each
-  template <class F, class G>
-  __device__ __forceinline__ void blocks_of(F &&f, G &&g) const {
-    constexpr int kAhead = 4;
-    for (int b = 0; b < blocks; b += 32 * kAhead) {
-      float v[kAhead][V];
+  // a block of V elements, NaN where the row has none
+  __device__ __forceinline__ uint4 block_of(int q) const {
+    const int64_t i = static_cast<int64_t>(q) * V - shift;
+    if (i >= 0 && i + V <= vocab) return *reinterpret_cast<const uint4 *>(x + i);
+    uint32_t w[4];
 #pragma unroll
-      for (int a = 0; a < kAhead; ++a) {
-        const int q = b + a * 32 + lane;
-        const int64_t i = static_cast<int64_t>(block + q) * V - shift;
-        if (q < blocks && i >= 0 && i + V <= vocab) {
-          load_v<T, V>(x + i, v[a]);
-        } else {
+    for (int k = 0; k < 4; ++k) {
+      w[k] = 0;
 #pragma unroll
-          for (int e = 0; e < V; ++e) v[a][e] = q < blocks && i + e >= 0 && i + e < vocab ? to_f32(x[i + e]) : NAN;
+      for (int h = 0; h < V / 4; ++h) {
+        const int64_t at = i + k * (V / 4) + h;
+        uint32_t bits = sizeof(T) == 4 ? 0x7fffffffu : 0x7fffu;
+        if (at >= 0 && at < vocab) {
+          if constexpr (sizeof(T) == 4) bits = reinterpret_cast<const uint32_t *>(x)[at];
+          else bits = reinterpret_cast<const uint16_t *>(x)[at];
         }
+        w[k] |= bits << (h * 16);
       }
+    }
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ void numbers(const uint4 &w, float (&v)[V]) {
+    if constexpr (sizeof(T) == 4) {
+      v[0] = __uint_as_float(w.x), v[1] = __uint_as_float(w.y), v[2] = __uint_as_float(w.z), v[3] = __uint_as_float(w.w);
+    } else {
+      unpack2<T>(w.x, v[0], v[1]), unpack2<T>(w.y, v[2], v[3]), unpack2<T>(w.z, v[4], v[5]), unpack2<T>(w.w, v[6], v[7]);
+    }
+  }
+  // f(v, block) for blocks from, ..., from + n - 1 of V logits, 32 lanes' at once and in ascending order; blocks past the end hold NaN
+  template <class F>
+  __device__ __forceinline__ void blocks_of(int from, int n, F &&f) const {
+    constexpr int kAhead = 4;
+    for (int b = 0; b < n; b += 32 * kAhead) {
+      uint4 w[kAhead];
+#pragma unroll
+      for (int a = 0; a < kAhead; ++a) w[a] = b + a * 32 + lane < n ? block_of(from + b + a * 32 + lane) : make_uint4(~0u, ~0u, ~0u, ~0u);
 #pragma unroll
       for (int a = 0; a < kAhead; ++a) {
-        const int i = (block + b + a * 32 + lane) * V - shift;
-#pragma unroll
-        for (int e = 0; e < V; ++e) f(v[a][e], i + e);
-        if (b + a * 32 < blocks) g();
+        if (b + a * 32 >= n) break;
+        float v[V];
+        numbers(w[a], v);
+        f(v, from + b + a * 32 + lane);
       }
     }
   }
+  // f(logit) for this warp's logits, those at or above `from` among them: blocks of the warp with none of these are left out
   template <class F>
-  __device__ __forceinline__ void each(F &&f) const {
-    blocks_of([&](float v, int) { f(v); }, [] {});
+  __device__ __forceinline__ void each(float from, F &&f) const {
+    blocks_of(block, blocks, [&](const float (&v)[V], int) {
+      float most = v[0];
+#pragma unroll
+      for (int e = 1; e < V; ++e) most = fmaxf(most, v[e]);
+      if (!__any_sync(0xffffffffu, most >= from)) return;
+#pragma unroll
+      for (int e = 0; e < V; ++e) f(v[e]);
+    });
   }
 
   __device__ __forceinline__ u64 weight(float v) const {
-    // c (top - v) in two floats; the difference is exact as a sum of two (Knuth)
-    const float d = top - v, t = d - top, d_low = (top - (d - t)) - (v + t);
-    float y = d * c;
-    float y_low = fmaf(d, c, -y);
-    y_low = fmaf(d, c_low, y_low);
-    y_low = fmaf(d_low, c, y_low);
-    if (!(y < 60.0f)) y = y_low = 0.0f, y = 60.0f;
+    // y = c (top - v) in two floats.  The difference of floats is one as a sum of two (Knuth); that of 16-bit numbers is rounded only where
+    // one is 2^16 times the other.
+    const float d = top - v;
+    float y = d * c, y_low = fmaf(d, c_low, fmaf(d, c, -y));
+    if constexpr (sizeof(T) == 4) {
+      const float t = d - top;
+      y_low = fmaf((top - (d - t)) - (v + t), c, y_low);
+    }
+    if (!(y < 60.0f)) y_low = 0.0f, y = 60.0f;
     const float j = fmaf(y, static_cast<float>(kSteps), 12582912.0f);  // (1.5 2^23: rounded to a whole number)
     const uint32_t n = __float_as_uint(j) & 0xffffu;
     const float r = (fmaf(j - 12582912.0f, -1.0f / kSteps, y) + y_low) * -0.6931471805599453f;  // |r| < 2^-9.5
-    const float q = fmaf(r * r, fmaf(r, 1.0f / 6.0f, 0.5f), r);                                 // e^r - 1, to 2^-42
-    const PowerTable::Entry e = sh.power[n % kSteps];
-    const int add = __float2int_rn(e.value * q * 0x1p39f);
-    return v == top ? 1ull << 44 : (e.whole + static_cast<u64>(static_cast<int64_t>(add) << 5)) >> (n / kSteps);
+    const float q = fmaf(r * r, fmaf(r, 1.0f / 6.0f, 0.5f), r);                                 // e^r - 1, to 2^-33
+    const uint32_t e = sh.power[n % kSteps];
+    const uint32_t m = e + __mulhi(static_cast<int>(e), __float2int_rn(q * 0x1p32f));
+    return v == top ? 1ull << 44 : (static_cast<u64>(m) << 14) >> (n / kSteps);
   }
-  // an upper and a lower bound of what weight() says for all logits between (that of hi and that of lo are 2^-31 of themselves and a
-  // unit off at most)
-  static __device__ u64 above(u64 w) { return w + (w >> 30) + 2; }
-  static __device__ u64 below(u64 w) { return w < 4 ? 0 : w - (w >> 30) - 2; }
+  // bounds of what weight() says of logits up to (from) one of which it says w: each is off by less than 2^-29 of itself and a unit
+  static __device__ u64 above(u64 w) { return w + (w >> 27) + 2; }
+  static __device__ u64 below(u64 w) { return w < 4 ? 0 : w - (w >> 27) - 2; }
 
   // sums over the row of two numbers
   __device__ void sums(u64 &a, u64 &b) {
@@ -211,32 +240,32 @@ struct SampleRow {
     flip ^= 1;
     return v;
   }
-  // sum over the threads before this one, in its CTA, and over all (the row's bins lie in thread order in every CTA)
-  __device__ u64 before(u64 v, u64 &all) {
+  __device__ u64 lanes_before(u64 v) const {
     u64 s = v;
     for (int d = 1; d < 32; d <<= 1) {
       const u64 w = __shfl_up_sync(0xffffffffu, s, d);
       if (lane >= d) s += w;
     }
+    return s - v;
+  }
+  // sum over the threads before this one, in its CTA, and over all (the row's bins lie in thread order in every CTA)
+  __device__ u64 before(u64 v, u64 &all) {
+    const u64 s = lanes_before(v) + v;
     __syncthreads();
     if (lane == 31) sh.warp[warp][0] = s;
     __syncthreads();
-    u64 w = sh.warp[lane][0], e = w;
-    for (int d = 1; d < 32; d <<= 1) {
-      const u64 z = __shfl_up_sync(0xffffffffu, w, d);
-      if (lane >= d) w += z;
-    }
-    all = __shfl_sync(0xffffffffu, w, 31);
-    return __shfl_sync(0xffffffffu, w - e, warp) + s - v;
+    const u64 w = sh.warp[lane][0], e = lanes_before(w);
+    all = __shfl_sync(0xffffffffu, e + w, 31);
+    return __shfl_sync(0xffffffffu, e, warp) + s - v;
   }
 
   // counts of the row's logits by bin(logit) (negative: in none); this thread's are bins 2 i and 2 i + 1
   template <class F>
-  __device__ uint2 histogram(F &&bin) {
+  __device__ uint2 histogram(float from, F &&bin) {
     uint32_t *count = sh.count[hist];
     for (int i = threadIdx.x; i < kBins; i += kSampleThreads) count[i] = 0;
     __syncthreads();
-    each([&](float v) {
+    each(from, [&](float v) {
       const int b = bin(v);
       if (b >= 0) atomicAdd(count + b, 1u);
     });
@@ -259,7 +288,7 @@ struct SampleRow {
   __device__ float bin_low(int b) const {
     return b >= kBins - 2 ? lowest : fmaxf(lowest, __fsub_rd(top, __fmul_ru(static_cast<float>(b + 2), __frcp_ru(bin_by))));
   }
-  __device__ u64 bin_power(int b) const { return sh.power[b * kStepsPerBin % kSteps].whole >> (b * kStepsPerBin / kSteps); }
+  __device__ u64 bin_power(int b) const { return (static_cast<u64>(sh.power[b * kStepsPerBin % kSteps]) << 14) >> (b * kStepsPerBin / kSteps); }
 
   // the bin that one thread has found, and the sum before it
   __device__ void publish(uint32_t bin, u64 sum) { sh.found[0] = bin, sh.found_sum[0] = sum; }
@@ -286,6 +315,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
   const int k = call.top_k ? call.top_k[row] : call.top_k_all;
 
   const bool greedy = !(t > 0.0f);
+  if (tid == 0) sh.hand.blocks = 0;
   if (tid == 0) {  // (a double operation of all the threads takes as long as 300 others)
     const float kept = fminf(fmaxf(t, kTemperatureMin), kTemperatureMax);
     const double c = 1.4426950408889634074 / static_cast<double>(kept);
@@ -293,7 +323,10 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
     sh.least = min_p > 0.0f ? log(static_cast<double>(min_p)) * static_cast<double>(kept) : 0.0;
   }
   float most = -INFINITY;
-  r.each([&](float v) { most = fmaxf(most, v); });
+  r.blocks_of(r.block, r.blocks, [&](const float (&v)[V], int) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) most = fmaxf(most, v[e]);
+  });
   r.top = most = r.maximum(most);
   if (most == -INFINITY) {  // (the same in every CTA of the row)
     if (rank == 0 && tid == 0) call.tokens[row] = -1;
@@ -312,9 +345,12 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
   float cut = r.lowest;       // what stays: logits above it,
   u64 ties = ~0ull;           // and the first of those equal to it
   if (greedy) cut = most, ties = 1;
+  // this lane's mass of the logits above `known`, where a pass has summed it
+  u64 above = 0;
+  float known = INFINITY;
   const bool by_count = !greedy && k > 0 && k < call.vocab, by_mass = !greedy && p < 1.0f;
   if (by_count || by_mass) {
-    const uint2 n = r.histogram([&](float v) { return r.step_bin(v); });
+    const uint2 n = r.histogram(r.lowest, [&](float v) { return r.step_bin(v); });
     const u64 m0 = n.x * r.bin_power(2 * tid), m1 = n.y * r.bin_power(2 * tid + 1);
     u64 counts = 0, masses = 0;
     const u64 n0 = r.before(static_cast<u64>(n.x) + n.y, counts);  // logits before this thread's bins
@@ -332,11 +368,10 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
         int shift = 0;
         while ((high - low) >> shift >= kBins) ++shift;
         u64 over = 0, none = 0;
-        const uint2 m = r.histogram([&](float v) {
-          if (!(v >= r.lowest)) return -1;
-          const uint32_t key = K::key(v);
-          over += first && key > high;
-          return key <= high && key >= low ? static_cast<int>((high - key) >> shift) : -1;
+        const float upto = K::logit(high), from = fmaxf(r.lowest, K::logit(low));
+        const uint2 m = r.histogram(from, [&](float v) {
+          over += v > upto;
+          return v <= upto && v >= from ? static_cast<int>((high - K::key(v)) >> shift) : -1;
         });
         if (first) r.sums(over, none), passed = over;
         first = false;
@@ -380,13 +415,14 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
       // the whole mass, and that above the bounds
       u64 whole = 0, passed = 0;
       const float over = K::logit(high);
-      r.each([&](float v) {
+      r.each(cut, [&](float v) {
         if (v > cut || (ties == ~0ull && v >= cut)) {
           const u64 w = r.weight(v);
           whole += w;
           if (v > over) passed += w;
         }
       });
+      above = passed;
       r.sums(whole, passed);
       if (ties != ~0ull) whole += ties * r.weight(cut);
       u64 want = 1;
@@ -398,11 +434,8 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
       for (int step = 0; step < 33; ++step) {  // (each leaves half of the keys at most)
         int shift = 0;
         while ((high - low) >> shift >= kBins) ++shift;
-        const uint2 m = r.histogram([&](float v) {
-          if (!(v >= r.lowest)) return -1;
-          const uint32_t key = K::key(v);
-          return key <= high && key >= low ? static_cast<int>((high - key) >> shift) : -1;
-        });
+        const float upto = K::logit(high), from = fmaxf(r.lowest, K::logit(low));
+        const uint2 m = r.histogram(from, [&](float v) { return v <= upto && v >= from ? static_cast<int>((high - K::key(v)) >> shift) : -1; });
         u64 up[2], down[2];
         for (int i = 0; i < 2; ++i) {
           const uint32_t b = 2 * tid + i, off = b << shift;
@@ -434,6 +467,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
           const float v = K::logit(high - b0);
           const u64 w = r.weight(v), n = (want - sum + w - 1) / w;
           ties = v == cut && ties < n ? ties : n, cut = v;
+          known = upto;
           break;
         }
         // between the bounds; where that is more than half of what it was (they may say little of a few wide bins), the half of it that the cut is in
@@ -442,19 +476,21 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
         const uint32_t mid = least + (next - least) / 2;
         if (b0 > 0 || halve) {
           u64 more = 0, half = 0;
-          const float upto = K::logit(high), from = K::logit(next), middle = K::logit(mid);
-          r.each([&](float v) {
+          const float border = K::logit(next), middle = K::logit(halve ? mid : next);
+          r.each(middle, [&](float v) {
             if (v <= upto && v > middle) {
-              if (v > from) more += r.weight(v);
-              else if (halve) half += r.weight(v);
+              if (v > border) more += r.weight(v);
+              else half += r.weight(v);
             }
           });
+          above += more;
+          const u64 half_here = half;
           r.sums(more, half);
           passed += more;
           high = next, low = least;
           if (halve) {
             if (passed + half >= want) low = mid + 1;
-            else passed += half, high = mid;
+            else passed += half, above += half_here, high = mid;
           }
         } else {
           low = least;
@@ -463,10 +499,8 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
     }
   }
   if (!greedy && min_p > 0.0f && sh.floor > cut) cut = sh.floor, ties = ~0ull;
+  if (known < cut) known = INFINITY;
 
-  // ranks among the equal ones where not all of them stay
-  u64 rank0 = 0;
-  const bool ranked = ties != ~0ull;
   const auto segments = [&](u64 mine, u64 &all) {  // sum over the warps before this one in the row, and over all
     __syncthreads();
     if (r.lane == 0) sh.segment[r.flip][r.warp] = mine;
@@ -491,75 +525,74 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
     for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(0xffffffffu, v, o);
     return v;
   };
-  if (ranked) {
-    u64 n = 0, all;
-    r.each([&](float v) { n += v == cut; });
-    rank0 = segments(warp_sum(n), all);
-    if (all <= ties) ties = ~0ull;
-  }
-  // This warp's mass, in the order of the row: equal ones up to the last that stays are the first of the row.  u at an end takes
-  // the first or the last that stays, whatever their weights are.
+  // This warp's mass, in the order of the row: the equal ones that stay are the first of the row.  u at an end takes the first or the last
+  // that stays, whatever their weights are.
   const bool ends = greedy || !(u > 0.0f) || !(u < 1.0f);
   const auto weight = [&](float v) { return ends ? 1ull : r.weight(v); };
-  u64 mine = 0, equal = 0;
-  r.each([&](float v) {
-    if (v > cut) mine += weight(v);
+  if (ends) known = INFINITY;
+  u64 mine = known < INFINITY ? above : 0, equal = 0, all;
+  r.each(cut, [&](float v) {
+    if (v > cut && v <= known) mine += weight(v);
     equal += v == cut;
   });
   mine = warp_sum(mine), equal = warp_sum(equal);
-  const u64 left = ranked ? (ties > rank0 ? ties - rank0 : 0) : ~0ull;  // equal ones that stay from this warp on
-  mine += (equal < left ? equal : left) * (equal ? weight(cut) : 0);
-  u64 all;
-  const u64 passed = segments(mine, all);
-  u64 target = 0;
-  if (!(u < 1.0f) && u > 0.0f) target = all - 1;
-  else if (!ends) {
+  const u64 one = weight(cut);
+  u64 earlier = 0;  // equal ones before this warp
+  if (ties != ~0ull) {
+    earlier = segments(equal, all);
+    if (all <= ties) ties = ~0ull;
+  }
+  const u64 left = ties > earlier ? ties - earlier : 0;  // equal ones that stay from this warp on
+  mine += (equal < left ? equal : left) * one;
+  u64 passed = segments(mine, all), target = 0;
+  if (!(u < 1.0f) && u > 0.0f) {
+    target = all - 1;
+  } else if (!ends) {
     bool cut_off;
     target = times(u, all, cut_off);
   }
-  if (passed <= target && target < passed + mine) {  // in this warp
-    u64 s = passed, rank_here = rank0;
-    const u64 one = weight(cut);
-    int token = -1;
-    int e = 0, equals = 0, first = 0;
-    float v[V];
-    r.blocks_of(
-        [&](float x, int i) {
-          if (e == 0) first = i, equals = 0;
-          v[e] = x, equals += x == cut;
-          if (++e == V) e = 0;
-        },
-        [&] {
-          int q = equals;  // and those in the lanes before
-          for (int d = 1; d < 32; d <<= 1) {
-            const int o = __shfl_up_sync(0xffffffffu, q, d);
-            if (r.lane >= d) q += o;
-          }
-          // the equal ones that stay are the first `stay` of this block
-          const u64 rank = rank_here + static_cast<u64>(q - equals);
-          const int stay = rank >= ties ? 0 : ties - rank < V ? static_cast<int>(ties - rank) : V;
-          u64 sum = 0;
-          int met = 0;
+  // The warp with the token's place hands its part of the row to all warps of its CTA.
+  if (r.lane == 0 && passed <= target && target < passed + mine) sh.hand = {passed, earlier, r.block, r.blocks};
+  __syncthreads();
+  if (sh.hand.blocks > 0) {
+    const int per = (sh.hand.blocks + 32 * kSampleWarps - 1) / (32 * kSampleWarps) * 32, from = sh.hand.block + r.warp * per;
+    const int blocks = max(0, min(per, sh.hand.blocks - r.warp * per));
+    mine = equal = 0;
+    r.blocks_of(from, blocks, [&](const float (&v)[V], int) {
 #pragma unroll
-          for (int i = 0; i < V; ++i) sum += v[i] > cut ? weight(v[i]) : v[i] == cut && met++ < stay ? one : 0;
-          u64 z = sum;
-          for (int d = 1; d < 32; d <<= 1) {
-            const u64 o = __shfl_up_sync(0xffffffffu, z, d);
-            if (r.lane >= d) z += o;
-          }
-          u64 at = s + z - sum;
-          if (at <= target && target < at + sum) {
-            met = 0;
+      for (int e = 0; e < V; ++e) mine += v[e] > cut ? weight(v[e]) : 0, equal += v[e] == cut;
+    });
+    mine = warp_sum(mine), equal = warp_sum(equal);
+    if (r.lane == 0) sh.warp[r.warp][0] = mine, sh.warp[r.warp][1] = equal;
+    __syncthreads();
+    // (lane i for warp i)
+    equal = sh.warp[r.lane][1];
+    const u64 ranks = sh.hand.rank + r.lanes_before(equal), stay = ties > ranks ? ties - ranks : 0;
+    mine = sh.warp[r.lane][0] + (equal < stay ? equal : stay) * one;
+    const u64 masses = sh.hand.passed + r.lanes_before(mine);
+    if (__shfl_sync(0xffffffffu, masses <= target && target < masses + mine, r.warp)) {
+      passed = __shfl_sync(0xffffffffu, masses, r.warp), earlier = __shfl_sync(0xffffffffu, ranks, r.warp);
+      r.blocks_of(from, blocks, [&](const float (&v)[V], int block) {
+        uint32_t equals = 0;
 #pragma unroll
-            for (int i = 0; i < V; ++i) {
-              const u64 w = v[i] > cut ? weight(v[i]) : v[i] == cut && met++ < stay ? one : 0;
-              if (at <= target && target < at + w) token = first + i;
-              at += w;
-            }
-          }
-          s += __shfl_sync(0xffffffffu, z, 31), rank_here += __shfl_sync(0xffffffffu, q, 31);
-        });
-    if (token >= 0) call.tokens[row] = token;
+        for (int e = 0; e < V; ++e) equals += v[e] == cut;
+        const u64 here = earlier + r.lanes_before(equals);
+        // the equal ones that stay are the first of this block
+        const int first = here >= ties ? 0 : ties - here < V ? static_cast<int>(ties - here) : V;
+        u64 w[V], sum = 0;
+        int met = 0;
+#pragma unroll
+        for (int e = 0; e < V; ++e) w[e] = v[e] > cut ? weight(v[e]) : v[e] == cut && met++ < first ? one : 0, sum += w[e];
+        u64 at = passed + r.lanes_before(sum);
+        const u64 next = at + sum, next_rank = here + equals;
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+          if (at <= target && target < at + w[e]) call.tokens[row] = static_cast<int64_t>(block) * V - r.shift + e;
+          at += w[e];
+        }
+        passed = __shfl_sync(0xffffffffu, next, 31), earlier = __shfl_sync(0xffffffffu, next_rank, 31);
+      });
+    }
   }
   if (ctas > 1) cluster_sync_all();  // (no CTA ends while another one reads its sums)
 }
