@@ -30,6 +30,7 @@ constexpr int kSampleThreads = 1024, kSampleWarps = kSampleThreads / 32;
 constexpr int kBins = 2 * kSampleThreads;
 constexpr int kSteps = 256;  // of the table of powers of two
 constexpr int kStepsPerBin = 4;
+constexpr int kList = 512;  // candidates that one CTA takes
 constexpr float kTemperatureMin = 0x1p-100f, kTemperatureMax = 0x1p100f;
 
 // 2^-(j / 256) as a whole number of 2^-30.  From square roots of 1/2, by Newton's iteration, and their products.  (Entries of 32 bits: lanes
@@ -80,6 +81,15 @@ __device__ __forceinline__ uint2 ld_cluster_u32x2(uint32_t addr) {
   return v;
 }
 
+__device__ __forceinline__ uint32_t atom_cluster_add(uint32_t addr, uint32_t v) {
+  uint32_t old;
+  asm volatile("atom.shared::cluster.add.u32 %0, [%1], %2;" : "=r"(old) : "r"(addr), "r"(v) : "memory");
+  return old;
+}
+__device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) {
+  asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
+
 struct SampleShared {
   uint32_t power[kSteps];
   uint32_t count[2][kBins];
@@ -90,6 +100,9 @@ struct SampleShared {
     u64 passed, rank;
     int block, blocks;
   } hand;  // the part of the row that holds the token
+  float list_logit[kList];
+  uint32_t list_index[kList], listed;
+  u64 list_weight[kList];
   uint32_t found[2];
   u64 found_sum[2];
   double least;          // temperature ln min_p
@@ -123,6 +136,7 @@ struct SampleRow {
 
   float top, c, c_low, bin_by;  // log2 e / temperature in two floats; bins per logit
   float lowest;                 // logits below it never stay
+  float most_off;               // 45 / c; 0 where the largest logit is infinity
 
   __device__ SampleRow(SampleShared &s, uint32_t r, uint32_t n) : sh(s), lane(threadIdx.x & 31), warp(threadIdx.x >> 5), rank(r), ctas(n) {}
 
@@ -162,7 +176,7 @@ struct SampleRow {
   // f(v, block) for blocks from, ..., from + n - 1 of V logits, 32 lanes' at once and in ascending order; blocks past the end hold NaN
   template <class F>
   __device__ __forceinline__ void blocks_of(int from, int n, F &&f) const {
-    constexpr int kAhead = 4;
+    constexpr int kAhead = 2;
     for (int b = 0; b < n; b += 32 * kAhead) {
       uint4 w[kAhead];
 #pragma unroll
@@ -188,26 +202,42 @@ struct SampleRow {
       for (int e = 0; e < V; ++e) f(v[e]);
     });
   }
+  // f(logit, index) for those from `from` to `upto`, which are few: 32 lanes with none of them are left out
+  template <class F>
+  __device__ __forceinline__ void between(float from, float upto, F &&f) const {
+    blocks_of(block, blocks, [&](const float (&v)[V], int b) {
+      float most = v[0];
+#pragma unroll
+      for (int e = 1; e < V; ++e) most = fmaxf(most, v[e]);
+      if (!__any_sync(0xffffffffu, most >= from)) return;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const bool in = v[e] >= from && v[e] <= upto;
+        if (__any_sync(0xffffffffu, in))
+          if (in) f(v[e], b * V - shift + e);
+      }
+    });
+  }
 
   __device__ __forceinline__ u64 weight(float v) const {
-    // y = c (top - v) in two floats.  The difference of floats is one as a sum of two (Knuth); that of 16-bit numbers is rounded only where
-    // one is 2^16 times the other.
-    const float d = top - v;
+    // y = c (top - v) in two floats, up to 45 (where the weight ends).  The difference of floats is one as a sum of two (Knuth); that of 16-bit
+    // numbers is rounded only where one is 2^16 times the other.
+    const float d = fminf(top - v, most_off);
     float y = d * c, y_low = fmaf(d, c_low, fmaf(d, c, -y));
     if constexpr (sizeof(T) == 4) {
       const float t = d - top;
-      y_low = fmaf((top - (d - t)) - (v + t), c, y_low);
+      y_low = fmaf(d < most_off ? (top - (d - t)) - (v + t) : 0.0f, c, y_low);
     }
-    if (!(y < 60.0f)) y_low = 0.0f, y = 60.0f;
     const float j = fmaf(y, static_cast<float>(kSteps), 12582912.0f);  // (1.5 2^23: rounded to a whole number)
-    const uint32_t n = __float_as_uint(j) & 0xffffu;
-    const float r = (fmaf(j - 12582912.0f, -1.0f / kSteps, y) + y_low) * -0.6931471805599453f;  // |r| < 2^-9.5
-    const float q = fmaf(r * r, fmaf(r, 1.0f / 6.0f, 0.5f), r);                                 // e^r - 1, to 2^-33
-    const uint32_t e = sh.power[n % kSteps];
-    const uint32_t m = e + __mulhi(static_cast<int>(e), __float2int_rn(q * 0x1p32f));
-    return v == top ? 1ull << 44 : (static_cast<u64>(m) << 14) >> (n / kSteps);
+    const uint32_t n = __float_as_uint(j);
+    const float r = fmaf(j - 12582912.0f, -1.0f / kSteps, y) + y_low;  // |r| < 2^-9 and a little
+    // 2^-r - 1 by its series, to 2^-33, in units of 2^-30, as a whole number
+    constexpr float kC1 = -0.6931471805599453f * 0x1p30f, kC2 = 0.2402265069591007f * 0x1p30f, kC3 = -0.0555041086648216f * 0x1p30f;
+    const uint32_t q = __float_as_uint(fmaf(r, fmaf(r, fmaf(r, kC3, kC2), kC1), 12582912.0f)) - 0x4b400000u;
+    const uint32_t e = sh.power[n % kSteps], m = e + __mulhi(static_cast<int>(e), static_cast<int>(q << 2));
+    return (static_cast<u64>(m) << 32) >> ((n / kSteps & 63) + 18);  // (n / kSteps <= 45)
   }
-  // bounds of what weight() says of logits up to (from) one of which it says w: each is off by less than 2^-29 of itself and a unit
+  // bounds of what weight() says of logits up to (from) one of which it says w: each is off by less than 2^-28 of itself and a unit
   static __device__ u64 above(u64 w) { return w + (w >> 27) + 2; }
   static __device__ u64 below(u64 w) { return w < 4 ? 0 : w - (w >> 27) - 2; }
 
@@ -259,16 +289,13 @@ struct SampleRow {
     return __shfl_sync(0xffffffffu, e, warp) + s - v;
   }
 
-  // counts of the row's logits by bin(logit) (negative: in none); this thread's are bins 2 i and 2 i + 1
+  // counts of the row's logits by bin, which count_all(counts) adds for this warp's part; this thread's are bins 2 i and 2 i + 1
   template <class F>
-  __device__ uint2 histogram(float from, F &&bin) {
+  __device__ uint2 histogram(F &&count_all) {
     uint32_t *count = sh.count[hist];
     for (int i = threadIdx.x; i < kBins; i += kSampleThreads) count[i] = 0;
     __syncthreads();
-    each(from, [&](float v) {
-      const int b = bin(v);
-      if (b >= 0) atomicAdd(count + b, 1u);
-    });
+    count_all(count);
     sync();
     uint2 n = {0, 0};
     const uint32_t at = smem_u32(count + 2 * threadIdx.x);
@@ -290,6 +317,53 @@ struct SampleRow {
   }
   __device__ u64 bin_power(int b) const { return (static_cast<u64>(sh.power[b * kStepsPerBin % kSteps]) << 14) >> (b * kStepsPerBin / kSteps); }
 
+  // The whole choice among the listed candidates, which hold the first k: a thread to each, in the descending order that counting gives.
+  __device__ void choose(int k, float p, float min_p, float u, int64_t *token) {
+    const int n = static_cast<int>(sh.listed), i = threadIdx.x;
+    int rank_here = 0;
+    const float v0 = i < n ? sh.list_logit[i] : 0.0f;
+    const uint32_t i0 = i < n ? sh.list_index[i] : 0;
+    if ((i & ~31) < n)
+      for (int j = 0; j < n; ++j) {
+        const float v = sh.list_logit[j];
+        rank_here += v > v0 || (v == v0 && sh.list_index[j] < i0);
+      }
+    __syncthreads();
+    if (i < n) sh.list_logit[rank_here] = v0, sh.list_index[rank_here] = i0;
+    __syncthreads();
+    const int most = min(n, k);
+    const float v = i < most ? sh.list_logit[i] : -INFINITY;
+    u64 w = i < most ? weight(v) : 0, all, want = ~0ull;
+    const u64 passed = before(w, all);
+    if (p < 1.0f) {
+      want = 1;
+      if (p > 0.0f) {
+        bool cut_off;
+        want = times(p, all, cut_off);
+        want += cut_off;
+      }
+    }
+    const bool stays = i < most && (i == 0 || passed < want) && !(min_p > 0.0f && v < sh.floor);
+    const bool ends = !(u > 0.0f) || !(u < 1.0f);
+    w = !stays ? 0 : ends ? 1 : w;
+    before(w, all);
+    u64 target = 0;
+    if (!(u < 1.0f) && u > 0.0f) {
+      target = all - 1;
+    } else if (!ends) {
+      bool cut_off;
+      target = times(u, all, cut_off);
+    }
+    // the same in the order of the row
+    if (i < most) sh.list_weight[i] = w;
+    __syncthreads();
+    if ((i & ~31) < most) {
+      const uint32_t index = i < most ? sh.list_index[i] : 0;
+      u64 at = 0;
+      for (int j = 0; j < most; ++j) at += sh.list_index[j] < index ? sh.list_weight[j] : 0;
+      if (stays && at <= target && target < at + w) *token = index;
+    }
+  }
   // the bin that one thread has found, and the sum before it
   __device__ void publish(uint32_t bin, u64 sum) { sh.found[0] = bin, sh.found_sum[0] = sum; }
 };
@@ -315,7 +389,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
   const int k = call.top_k ? call.top_k[row] : call.top_k_all;
 
   const bool greedy = !(t > 0.0f);
-  if (tid == 0) sh.hand.blocks = 0;
+  if (tid == 0) sh.hand.blocks = 0, sh.listed = 0;
   if (tid == 0) {  // (a double operation of all the threads takes as long as 300 others)
     const float kept = fminf(fmaxf(t, kTemperatureMin), kTemperatureMax);
     const double c = 1.4426950408889634074 / static_cast<double>(kept);
@@ -339,6 +413,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
   }
   __syncthreads();
   r.c = sh.c, r.c_low = sh.c_low;
+  r.most_off = most == INFINITY ? 0.0f : __fdiv_rd(45.0f, r.c);
   r.bin_by = r.c * (kSteps / kStepsPerBin);
   r.lowest = most == INFINITY ? INFINITY : -3.402823466e38f;
 
@@ -350,7 +425,12 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
   float known = INFINITY;
   const bool by_count = !greedy && k > 0 && k < call.vocab, by_mass = !greedy && p < 1.0f;
   if (by_count || by_mass) {
-    const uint2 n = r.histogram(r.lowest, [&](float v) { return r.step_bin(v); });
+    const uint2 n = r.histogram([&](uint32_t *count) {
+      r.each(r.lowest, [&](float v) {
+        const int b = r.step_bin(v);
+        if (b >= 0) atomicAdd(count + b, 1u);
+      });
+    });
     const u64 m0 = n.x * r.bin_power(2 * tid), m1 = n.y * r.bin_power(2 * tid + 1);
     u64 counts = 0, masses = 0;
     const u64 n0 = r.before(static_cast<u64>(n.x) + n.y, counts);  // logits before this thread's bins
@@ -360,6 +440,20 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
       if (n0 < want && n0 + n.x + n.y >= want) r.publish(2 * tid + (n0 + n.x < want), 0);
       __syncthreads();
       last = static_cast<int>(sh.found[0]);
+      // few candidates (the logits up to that bin): to one CTA, and through
+      if (2 * tid == (last & ~1)) sh.found_sum[1] = n0 + n.x + (last & 1 ? n.y : 0);
+      __syncthreads();
+      if (sh.found_sum[1] <= kList) {
+        r.between(r.bin_low(last), INFINITY, [&](float v, int i) {
+          if (r.step_bin(v) > last) return;
+          const uint32_t at = atom_cluster_add(mapa_cluster(smem_u32(&sh.listed), 0), 1u);
+          st_cluster_f32(mapa_cluster(smem_u32(sh.list_logit + at), 0), v);
+          st_cluster_u32(mapa_cluster(smem_u32(sh.list_index + at), 0), static_cast<uint32_t>(i));
+        });
+        r.sync();
+        if (rank == 0) r.choose(k, p, min_p, u, call.tokens + row);
+        return;
+      }
       // down to one key
       uint32_t high = K::key(r.bin_high(last)), low = K::key(r.bin_low(last));
       bool first = true;
@@ -369,9 +463,11 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
         while ((high - low) >> shift >= kBins) ++shift;
         u64 over = 0, none = 0;
         const float upto = K::logit(high), from = fmaxf(r.lowest, K::logit(low));
-        const uint2 m = r.histogram(from, [&](float v) {
-          over += v > upto;
-          return v <= upto && v >= from ? static_cast<int>((high - K::key(v)) >> shift) : -1;
+        const uint2 m = r.histogram([&](uint32_t *count) {
+          r.between(from, first ? INFINITY : upto, [&](float v, int) {
+            if (v > upto) ++over;
+            else atomicAdd(count + ((high - K::key(v)) >> shift), 1u);
+          });
         });
         if (first) r.sums(over, none), passed = over;
         first = false;
@@ -435,7 +531,8 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
         int shift = 0;
         while ((high - low) >> shift >= kBins) ++shift;
         const float upto = K::logit(high), from = fmaxf(r.lowest, K::logit(low));
-        const uint2 m = r.histogram(from, [&](float v) { return v <= upto && v >= from ? static_cast<int>((high - K::key(v)) >> shift) : -1; });
+        const uint2 m = r.histogram(
+            [&](uint32_t *count) { r.between(from, upto, [&](float v, int) { atomicAdd(count + ((high - K::key(v)) >> shift), 1u); }); });
         u64 up[2], down[2];
         for (int i = 0; i < 2; ++i) {
           const uint32_t b = 2 * tid + i, off = b << shift;
@@ -477,11 +574,8 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
         if (b0 > 0 || halve) {
           u64 more = 0, half = 0;
           const float border = K::logit(next), middle = K::logit(halve ? mid : next);
-          r.each(middle, [&](float v) {
-            if (v <= upto && v > middle) {
-              if (v > border) more += r.weight(v);
-              else half += r.weight(v);
-            }
+          r.between(middle, upto, [&](float v, int) {
+            if (v > middle) (v > border ? more : half) += r.weight(v);
           });
           above += more;
           const u64 half_here = half;
@@ -530,11 +624,19 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
   const bool ends = greedy || !(u > 0.0f) || !(u < 1.0f);
   const auto weight = [&](float v) { return ends ? 1ull : r.weight(v); };
   if (ends) known = INFINITY;
-  u64 mine = known < INFINITY ? above : 0, equal = 0, all;
-  r.each(cut, [&](float v) {
-    if (v > cut && v <= known) mine += weight(v);
-    equal += v == cut;
-  });
+  u64 mine = 0, equal = 0, all;
+  if (known < INFINITY) {
+    mine = above;
+    r.between(cut, known, [&](float v, int) {
+      if (v > cut) mine += r.weight(v);
+      else ++equal;
+    });
+  } else {
+    r.each(cut, [&](float v) {
+      if (v > cut) mine += weight(v);
+      equal += v == cut;
+    });
+  }
   mine = warp_sum(mine), equal = warp_sum(equal);
   const u64 one = weight(cut);
   u64 earlier = 0;  // equal ones before this warp

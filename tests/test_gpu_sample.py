@@ -1,5 +1,7 @@
-"""sample on the GPU against its definition in 64 bits.  Tokens are equal, but where u lies within 1e-8 of the border between two
-(weights are off by 2^-34 of themselves and 2^-45 at most, so that borders, of up to 2^19 of them, are off by less than 1e-8)."""
+"""sample on the GPU against its definition in 64 bits.  Tokens are equal, but where u lies next to the border between two.
+A weight is off by less than 2^-28 of itself (its table, the series and the product are whole numbers of 2^-30) and by less than its unit,
+2^-44; the sum of all is 1 at least, as the largest logit's is 1: borders between n tokens, as parts of the sum, are off by less than
+2^-28 + n 2^-44."""
 import math
 
 import numpy as np
@@ -11,7 +13,6 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 DTYPES = [torch.float32, torch.float16, torch.bfloat16]
-NEAR = 1e-8
 
 
 def kept_weights(x, t, k, p, mp):
@@ -57,7 +58,8 @@ def expected(x, u, t, k, p, mp):
         return pick(0.0), {pick(0.0)}
     if u >= 1:
         return last, {last}
-    return pick(u), {pick(u), pick(max(0.0, u - NEAR)), last if u + NEAR >= 1 else pick(u + NEAR)}
+    near = 2.0 ** -28 + len(x) * 2.0 ** -44
+    return pick(u), {pick(u), pick(max(0.0, u - near)), last if u + near >= 1 else pick(u + near)}
 
 
 def column(v, n):
