@@ -28,26 +28,26 @@ namespace {
 using u64 = unsigned long long;
 constexpr int kSampleThreads = 1024, kSampleWarps = kSampleThreads / 32;
 constexpr int kBins = 2 * kSampleThreads;
-constexpr int kSteps = 256;  // of the table of powers of two
-constexpr int kStepsPerBin = 4;
-constexpr int kList = 512;  // candidates that one CTA takes
+constexpr int kSteps = 128;  // of the table of powers of two
+constexpr int kStepsPerBin = 2;
+constexpr int kList = 256;   // candidates of top-k that one CTA takes
+constexpr int kNotes = 1024;  // logits between the bounds of a cut that a warp puts down
 constexpr float kTemperatureMin = 0x1p-100f, kTemperatureMax = 0x1p100f;
 
-// 2^-(j / 256) as a whole number of 2^-30.  From square roots of 1/2, by Newton's iteration, and their products.  (Entries of 32 bits: lanes
-// read any of them, and 16-byte ones took most of a pass.)
+// 2^-(j / kSteps) as a whole number of 2^-30.  From square roots of 1/2, by Newton's iteration, and their products.
 struct PowerTable {
   uint32_t e[kSteps];
   constexpr PowerTable() : e{} {
-    double root[8] = {};
+    double root[7] = {};
     double r = 0.5;
-    for (int i = 7; i >= 0; --i) {
+    for (int i = 6; i >= 0; --i) {
       double s = r;
       for (int k = 0; k < 60; ++k) s = 0.5 * (s + r / s);
-      root[i] = r = s;  // 2^-(2^i / 256)
+      root[i] = r = s;  // 2^-(2^i / 128)
     }
     for (int j = 0; j < kSteps; ++j) {
       double v = 1.0;
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < 7; ++i)
         if (j >> i & 1) v *= root[i];
       e[j] = static_cast<uint32_t>(v * 0x1p30 + 0.5);
     }
@@ -91,7 +91,7 @@ __device__ __forceinline__ void st_cluster_u32(uint32_t addr, uint32_t v) {
 }
 
 struct SampleShared {
-  uint32_t power[kSteps];
+  uint32_t power[kSteps][32];  // a copy to each lane's bank (with one, random entries took 3 to 4 reads)
   uint32_t count[2][kBins];
   u64 warp[kSampleWarps][2];
   u64 part[2][2];                // this CTA's sums, for the cluster
@@ -100,6 +100,7 @@ struct SampleShared {
     u64 passed, rank;
     int block, blocks;
   } hand;  // the part of the row that holds the token
+  float notes[kSampleWarps][kNotes];
   float list_logit[kList];
   uint32_t list_index[kList], listed;
   u64 list_weight[kList];
@@ -132,11 +133,12 @@ struct SampleRow {
   SampleShared &sh;
   const int lane, warp;
   const uint32_t rank, ctas;
+  int noted = 0;           // logits put down by this warp
   int flip = 0, hist = 0;  // which of two places the next sum and the next histogram take
 
   float top, c, c_low, bin_by;  // log2 e / temperature in two floats; bins per logit
   float lowest;                 // logits below it never stay
-  float most_off;               // 45 / c; 0 where the largest logit is infinity
+  float most_off, bins_off;     // logits under the largest where weights end, and where bins end
 
   __device__ SampleRow(SampleShared &s, uint32_t r, uint32_t n) : sh(s), lane(threadIdx.x & 31), warp(threadIdx.x >> 5), rank(r), ctas(n) {}
 
@@ -222,7 +224,7 @@ struct SampleRow {
   __device__ __forceinline__ u64 weight(float v) const {
     // y = c (top - v) in two floats, up to 45 (where the weight ends).  The difference of floats is one as a sum of two (Knuth); that of 16-bit
     // numbers is rounded only where one is 2^16 times the other.
-    const float d = fminf(top - v, most_off);
+    const float d = fminf(fmaxf(top - v, 0.0f), most_off);  // (infinity under itself: 0)
     float y = d * c, y_low = fmaf(d, c_low, fmaf(d, c, -y));
     if constexpr (sizeof(T) == 4) {
       const float t = d - top;
@@ -230,13 +232,36 @@ struct SampleRow {
     }
     const float j = fmaf(y, static_cast<float>(kSteps), 12582912.0f);  // (1.5 2^23: rounded to a whole number)
     const uint32_t n = __float_as_uint(j);
-    const float r = fmaf(j - 12582912.0f, -1.0f / kSteps, y) + y_low;  // |r| < 2^-9 and a little
-    // 2^-r - 1 by its series, to 2^-33, in units of 2^-30, as a whole number
+    const float r = fmaf(j - 12582912.0f, -1.0f / kSteps, y) + y_low;  // |r| < 2^-8 and a little
+    // e (2^-r - 1) by the series (to 2^-39), in units of 2^-30, rounded to a whole number; e as a float from its upper 24 bits
     constexpr float kC1 = -0.6931471805599453f * 0x1p30f, kC2 = 0.2402265069591007f * 0x1p30f, kC3 = -0.0555041086648216f * 0x1p30f;
-    const uint32_t q = __float_as_uint(fmaf(r, fmaf(r, fmaf(r, kC3, kC2), kC1), 12582912.0f)) - 0x4b400000u;
-    const uint32_t e = sh.power[n % kSteps], m = e + __mulhi(static_cast<int>(e), static_cast<int>(q << 2));
+    const uint32_t e = sh.power[n % kSteps][lane];
+    const float q = r * fmaf(r, fmaf(r, kC3, kC2), kC1);
+    const uint32_t m = e + __float_as_uint(fmaf(__uint_as_float((e >> 6) + (125u << 23)), q, 12582912.0f)) - 0x4b400000u;
     return (static_cast<u64>(m) << 32) >> ((n / kSteps & 63) + 18);  // (n / kSteps <= 45)
   }
+  // puts down a logit between the bounds of a cut for the passes that follow: each warp its own
+  __device__ __forceinline__ void note(bool in, float v) {
+    const uint32_t who = __ballot_sync(0xffffffffu, in);
+    if (who == 0) return;
+    const int at = noted + __popc(who & ((1u << lane) - 1));
+    if (in && at < kNotes) sh.notes[warp][at] = v;
+    noted += __popc(who);
+  }
+  // f(logit) for the warp's logits from `from` to `upto`, all of which note() has seen
+  template <class F>
+  __device__ __forceinline__ void noted_between(float from, float upto, F &&f) const {
+    if (noted > kNotes) {  // (too many to put down)
+      between(from, upto, [&](float v, int) { f(v); });
+      return;
+    }
+    __syncwarp();
+    for (int i = lane; i < noted; i += 32) {
+      const float v = sh.notes[warp][i];
+      if (v >= from && v <= upto) f(v);
+    }
+  }
+
   // bounds of what weight() says of logits up to (from) one of which it says w: each is off by less than 2^-28 of itself and a unit
   static __device__ u64 above(u64 w) { return w + (w >> 27) + 2; }
   static __device__ u64 below(u64 w) { return w < 4 ? 0 : w - (w >> 27) - 2; }
@@ -306,16 +331,21 @@ struct SampleRow {
     hist ^= 1;
     return n;
   }
-  // the bin of equal steps: off by less than 2^-11 of one (three roundings of a number below 2^11)
+  // The bin of equal steps of a logit that is not below `lowest`: the nearest whole number of steps, off by less than 2^-11 of one (three
+  // roundings of a number below 2^11).
   __device__ __forceinline__ int step_bin(float v) const {
-    return v >= lowest ? (v == top ? 0 : __float2int_rd(fminf((top - v) * bin_by, static_cast<float>(kBins - 1)))) : -1;
+    return static_cast<int>(__float_as_uint(fmaf(fminf(fmaxf(top - v, 0.0f), bins_off), bin_by, 12582912.0f)) - 0x4b400000u);
   }
   // a logit that no logit of a bin >= b is above, and one that none of a bin <= b is below
   __device__ float bin_high(int b) const { return b <= 1 ? top : fminf(top, __fsub_ru(top, __fmul_rd(static_cast<float>(b - 1), __frcp_rd(bin_by)))); }
   __device__ float bin_low(int b) const {
     return b >= kBins - 2 ? lowest : fmaxf(lowest, __fsub_rd(top, __fmul_ru(static_cast<float>(b + 2), __frcp_ru(bin_by))));
   }
-  __device__ u64 bin_power(int b) const { return (static_cast<u64>(sh.power[b * kStepsPerBin % kSteps]) << 14) >> (b * kStepsPerBin / kSteps); }
+  // the weight of its upper edge
+  __device__ u64 bin_power(int b) const {
+    const int j = b == 0 ? 0 : b * kStepsPerBin - kStepsPerBin / 2;
+    return (static_cast<u64>(sh.power[j % kSteps][lane]) << 14) >> (j / kSteps);
+  }
 
   // The whole choice among the listed candidates, which hold the first k: a thread to each, in the descending order that counting gives.
   __device__ void choose(int k, float p, float min_p, float u, int64_t *token) {
@@ -370,7 +400,8 @@ struct SampleRow {
 
 template <typename T>
 __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call) {
-  __shared__ SampleShared sh;
+  extern __shared__ __align__(16) unsigned char smem[];
+  SampleShared &sh = *reinterpret_cast<SampleShared *>(smem);
   const uint32_t ctas = call.ctas, rank = ctas > 1 ? cluster_ctarank() : 0;
   const int row = blockIdx.x / ctas, tid = threadIdx.x;
   SampleRow<T> r(sh, rank, ctas);
@@ -383,7 +414,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
     r.block = static_cast<int>(rank * kSampleWarps + r.warp) * per;
     r.blocks = max(0, min(per, blocks - r.block));
   }
-  for (int i = tid; i < kSteps; i += kSampleThreads) sh.power[i] = kPowers.e[i];
+  for (int i = r.warp; i < kSteps; i += kSampleWarps) sh.power[i][r.lane] = kPowers.e[i];
   const float t = call.temperature ? call.temperature[row] : call.temperature_all;
   const float p = call.top_p ? call.top_p[row] : call.top_p_all, min_p = call.min_p ? call.min_p[row] : call.min_p_all, u = call.u[row];
   const int k = call.top_k ? call.top_k[row] : call.top_k_all;
@@ -413,8 +444,9 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
   }
   __syncthreads();
   r.c = sh.c, r.c_low = sh.c_low;
-  r.most_off = most == INFINITY ? 0.0f : __fdiv_rd(45.0f, r.c);
+  r.most_off = __fdiv_rd(45.0f, r.c);
   r.bin_by = r.c * (kSteps / kStepsPerBin);
+  r.bins_off = __fdiv_rd(kBins - 0.75f, r.bin_by);
   r.lowest = most == INFINITY ? INFINITY : -3.402823466e38f;
 
   float cut = r.lowest;       // what stays: logits above it,
@@ -427,8 +459,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
   if (by_count || by_mass) {
     const uint2 n = r.histogram([&](uint32_t *count) {
       r.each(r.lowest, [&](float v) {
-        const int b = r.step_bin(v);
-        if (b >= 0) atomicAdd(count + b, 1u);
+        if (v >= r.lowest) atomicAdd(count + r.step_bin(v), 1u);
       });
     });
     const u64 m0 = n.x * r.bin_power(2 * tid), m1 = n.y * r.bin_power(2 * tid + 1);
@@ -511,12 +542,13 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
       // the whole mass, and that above the bounds
       u64 whole = 0, passed = 0;
       const float over = K::logit(high);
+      const float under = K::logit(low);
+      const bool some = ties != ~0ull;  // (of those at the cut)
       r.each(cut, [&](float v) {
-        if (v > cut || (ties == ~0ull && v >= cut)) {
-          const u64 w = r.weight(v);
-          whole += w;
-          if (v > over) passed += w;
-        }
+        const u64 w = r.weight(some ? v > cut ? v : -INFINITY : v >= cut ? v : -INFINITY);
+        whole += w;
+        if (v > over) passed += w;
+        r.note(v <= over && v >= under, v);
       });
       above = passed;
       r.sums(whole, passed);
@@ -532,7 +564,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
         while ((high - low) >> shift >= kBins) ++shift;
         const float upto = K::logit(high), from = fmaxf(r.lowest, K::logit(low));
         const uint2 m = r.histogram(
-            [&](uint32_t *count) { r.between(from, upto, [&](float v, int) { atomicAdd(count + ((high - K::key(v)) >> shift), 1u); }); });
+            [&](uint32_t *count) { r.noted_between(from, upto, [&](float v) { atomicAdd(count + ((high - K::key(v)) >> shift), 1u); }); });
         u64 up[2], down[2];
         for (int i = 0; i < 2; ++i) {
           const uint32_t b = 2 * tid + i, off = b << shift;
@@ -574,7 +606,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
         if (b0 > 0 || halve) {
           u64 more = 0, half = 0;
           const float border = K::logit(next), middle = K::logit(halve ? mid : next);
-          r.between(middle, upto, [&](float v, int) {
+          r.noted_between(middle, upto, [&](float v) {
             if (v > middle) (v > border ? more : half) += r.weight(v);
           });
           above += more;
@@ -627,7 +659,7 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
   u64 mine = 0, equal = 0, all;
   if (known < INFINITY) {
     mine = above;
-    r.between(cut, known, [&](float v, int) {
+    r.noted_between(cut, known, [&](float v) {
       if (v > cut) mine += r.weight(v);
       else ++equal;
     });
@@ -701,12 +733,15 @@ __global__ void __launch_bounds__(kSampleThreads) sample_kernel(SampleCall call)
 
 template <typename T>
 cudaError_t launch(const SampleCall &c, cudaStream_t st) {
+  const cudaError_t e = cudaFuncSetAttribute(sample_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, sizeof(SampleShared));
+  if (e != cudaSuccess) return e;
   cudaLaunchAttribute attr[1];
   attr[0].id = cudaLaunchAttributeClusterDimension;
   attr[0].val.clusterDim.x = static_cast<unsigned>(c.ctas), attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3(static_cast<unsigned>(c.rows) * static_cast<unsigned>(c.ctas));
   cfg.blockDim = dim3(kSampleThreads);
+  cfg.dynamicSmemBytes = sizeof(SampleShared);
   cfg.stream = st;
   cfg.attrs = attr;
   cfg.numAttrs = 1;
