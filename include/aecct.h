@@ -350,7 +350,7 @@ int aecct_clip_gradients(int32_t n_tensors, const void *const *grad, const int64
  *                     for rows of AECCT_F16 or AECCT_BF16, which are kept as they are.
  * Sequence b's token at position p lies in page table[b][p / page_size], at place p % page_size.  A page whose number
  * is not in [0, pages), and positions past the table's columns, hold nothing: nothing is written there, and what is read
- * from there counts as absent.  Limits: head_dim <= 256, heads and page_size < 2^20. */
+ * from there counts as absent.  Limits: head_dim <= 256, heads and page_size < 2^20, batch < 2^24. */
 typedef struct {
   void *k, *v;
   float *k_scale, *v_scale;

@@ -385,6 +385,7 @@ cudaError_t launch_clip_gradients(int n, const void *const *g, const int64_t *le
 // kv_cache.cu: rows of a paged cache, written and read.  Element types: 0 = float, 1 = half, 2 = bfloat16, 3 = int8.
 constexpr int kCacheMaxDim = 256;
 constexpr int kCacheMaxCount = 1 << 20;  // heads, and tokens of a page
+constexpr int kCacheMaxBatch = 1 << 24;  // sequences of a call
 struct KvPages {  // aecct_kv_cache
   void *k, *v;
   float *k_scale, *v_scale;

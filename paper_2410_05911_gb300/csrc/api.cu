@@ -53,7 +53,7 @@ int cache_of(const aecct_kv_cache *c, const aecct_kv_sequences *s, KvPages *page
   if (c->head_dim > kCacheMaxDim || c->heads >= kCacheMaxCount || c->page_size >= kCacheMaxCount) return AECCT_ERR_UNSUPPORTED;
   const int size = c->dtype == AECCT_I8 ? 1 : 2;
   if (c->ld < c->head_dim || c->ld > (1 << 20) || c->ld * size % 16) return AECCT_ERR_INVALID_ARG;
-  if (c->pages > INT32_MAX) return AECCT_ERR_UNSUPPORTED;
+  if (c->pages > INT32_MAX || s->batch >= kCacheMaxBatch) return AECCT_ERR_UNSUPPORTED;
   if (c->pages > 0) {
     const auto row = [](const void *p) { return p && (reinterpret_cast<uintptr_t>(p) & 15u) == 0; };
     if (!row(c->k) || !row(c->v)) return AECCT_ERR_INVALID_ARG;

@@ -34,34 +34,51 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const __grid_
       }
     }
   }
+  const auto ends_at = [&](int c) { return c < static_cast<int>(gridDim.x) ? a.piece[c * 2].ends != 0 : true; };
   const AttendPiece p = a.piece[blockIdx.x * 2 + 1];
+  bool ends = ends_at(blockIdx.x + 1 + lane);
   if (p.b < 0) return;
   const int part = p.j % a.parts;
   if (head >= min(plan.heads, a.group - part * plan.heads)) return;
   // the CTAs up to the one where it ends
   int count = 1;
-  for (int c = blockIdx.x + 1;; c += 32) {
-    const bool ends = c + lane < static_cast<int>(gridDim.x) ? a.piece[(c + lane) * 2].ends != 0 : true;
+  for (int c = blockIdx.x + 1;;) {
     const uint32_t found = __ballot_sync(0xffffffffu, ends);
     if (found) {
       count += c - static_cast<int>(blockIdx.x) - 1 + __ffs(found);
       break;
     }
+    c += 32;
+    ends = ends_at(c + lane);
   }
   const auto from = [&](int k) { return a.partial + ((blockIdx.x + k) * 2 + (k == 0 ? 1 : 0)) * static_cast<int64_t>(plan.part); };
-  float top = -INFINITY;
-  for (int k = lane; k < count; k += 32) top = fmaxf(top, from(k)[head]);
-  for (int o = 16; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
-  const float base = top == -INFINITY ? 0.0f : top;
-  float l = 0.0f, v[2] = {0.0f, 0.0f};
-#pragma unroll 4
-  for (int k = 0; k < count; ++k) {
-    const float *f = from(k), by = exp2_fast(f[head] - base);
-    l = fmaf(f[plan.heads + head], by, l);
+  const int row = 2 * plan.heads + head * plan.width;
+  float top = -INFINITY, l = 0.0f, v[2] = {0.0f, 0.0f};
+  // 32 parts at a time, a lane to each for what it is scaled by; 8 parts' rows on their way at once
+  for (int k0 = 0; k0 < count; k0 += 32) {
+    const int parts = min(32, count - k0);
+    float mine = lane < parts ? from(k0 + lane)[head] : -INFINITY;
+    const float sum = lane < parts ? from(k0 + lane)[plan.heads + head] : 0.0f;
+    for (int k1 = 0; k1 < parts; k1 += 8) {
+      float x[8][2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int e = tid + i * kJoinThreads;
-      if (e < plan.width) v[i] = fmaf(f[2 * plan.heads + head * plan.width + e], by, v[i]);
+      for (int k = 0; k < 8; ++k)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) x[k][i] = k1 + k < parts && tid + i * kJoinThreads < plan.width ? from(k0 + k1 + k)[row + tid + i * kJoinThreads] : 0.0f;
+      if (k1 == 0) {
+        float most = fmaxf(top, mine);
+        for (int o = 16; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+        const float base = most == -INFINITY ? 0.0f : most, old = exp2_fast(top - base);
+        mine = exp2_fast(mine - base);
+        float s = sum * mine;
+        for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+        l = fmaf(l, old, s), v[0] *= old, v[1] *= old, top = most;
+      }
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        const float by = __shfl_sync(0xffffffffu, mine, k1 + k);
+        v[0] = fmaf(x[k][0], by, v[0]), v[1] = fmaf(x[k][1], by, v[1]);
+      }
     }
   }
   const int64_t at = static_cast<int64_t>(p.b) * a.q_heads + p.j / a.parts * a.group + part * plan.heads + head;

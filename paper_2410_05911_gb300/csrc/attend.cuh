@@ -37,7 +37,7 @@ namespace aecct {
 struct AttendPiece {
   int b, j;  // the sequence (-1: none), and the piece of its heads
   int ends;  // the last tile is in it
-  int pad;
+  int last;  // (within a CTA) the warp that it ends in
 };
 struct AttendArgs {
   KvPages cache;
@@ -50,8 +50,8 @@ struct AttendArgs {
   float scale;  // times log2 e
   void *out;
   float *lse;
-  float *partial;      // [2 CTAs][kHeads (DP + 2)]
-  AttendPiece *piece;  // [2 CTAs]
+  float *partial;      // [CTAs][2][kPart]
+  AttendPiece *piece;  // [CTAs][2]
 };
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -115,7 +115,7 @@ struct AttendShape {
   static constexpr int kCtas = kRow <= 64 ? 2 : 1;  // to an SM
   static constexpr int kStage = 2 * TK * kRow + 2 * TK * 4 + 16;
   static constexpr int kPart = kHeads * (DP + 2);  // floats of a piece: maxima, sums, rows
-  static constexpr int kFixed = 16 * kWarps + 8 * 32 * kWarps + 2 * kWarps * 16 + kWarps * kPart * 4;
+  static constexpr int kFixed = 16 * kWarps + 8 * 32 * kWarps + (3 * kWarps + 1) * 16 + (kWarps + kWarps + 1) * 2 * kHeads * 4 + kWarps * kPart * 4;
   static constexpr int kRoom = (227 * 1024 / kCtas - 1024 * (kCtas - 1) - kFixed) / (kWarps * kStage);
   static constexpr int kStages = kRoom > 4 ? 4 : kRoom;
   static constexpr int kSmem = kFixed + kWarps * kStages * kStage;
@@ -225,27 +225,53 @@ struct AttendWarp {
 
   // query head of a column of this piece (its number in the group's piece), and which piece of the number
   static __device__ __forceinline__ int head_of(int column) { return column / P; }
-  __device__ float query(const void *row, int e) const {
-    if (e >= a.cache.dim) return 0.0f;
-    return a.dtype == 0 ? static_cast<const float *>(row)[e] : a.dtype == 1 ? to_f32(static_cast<const __half *>(row)[e]) : to_f32(static_cast<const __nv_bfloat16 *>(row)[e]);
+  // EL elements of a row of queries from e on, zeros past its end
+  template <typename T, int EL>
+  __device__ __forceinline__ void queries(const T *row, int e, bool vectors, float *v) const {
+    constexpr int V = kVec<T> < EL ? kVec<T> : EL;
+    if (V == kVec<T> && vectors) {
+#pragma unroll
+      for (int i = 0; i < EL; i += V) {
+        if (e + i < a.cache.dim) {
+          load_v<T, V>(row + e + i, v + i);
+        } else {
+#pragma unroll
+          for (int k = 0; k < V; ++k) v[i + k] = 0.0f;
+        }
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < EL; ++i) v[i] = e + i < a.cache.dim ? to_f32(row[e + i]) : 0.0f;
+    }
+  }
+  template <typename T, int EL>
+  __device__ __forceinline__ void query_row(int64_t at, bool on, float (&v)[DP / 4]) const {
+    const T *row = static_cast<const T *>(a.q) + at;
+    // rows that all start on 16 bytes, and end on them
+    const bool vectors = ((reinterpret_cast<uintptr_t>(a.q) | (a.ld_row * sizeof(T)) | (a.ld_head * sizeof(T)) | (a.cache.dim * sizeof(T))) & 15u) == 0;
+#pragma unroll
+    for (int i = 0; i < DP / 4; ++i) v[i] = 0.0f;
+    if (on) {
+#pragma unroll
+      for (int i = 0; i < DP / 4; i += EL) queries<T, EL>(row, 4 * i + EL * t, vectors, v + i);
+    }
   }
   // a sequence's or a head's first tile: the queries in the order of the keys' elements, and nothing summed yet
   __device__ void begin(const Cursor &c) {
     constexpr int EL = DP / 4 < 16 / S::kSize ? DP / 4 : 16 / S::kSize;  // elements of a lane's piece of a key
     const int part = c.j % a.parts, heads = min(S::kHeads, a.group - part * S::kHeads), head0 = c.j / a.parts * a.group + part * S::kHeads;
-    const int size = a.dtype == 0 ? 4 : 2;
     float by_column[NB];
 #pragma unroll
     for (int nb = 0; nb < NB; ++nb) {
       const int column = nb * 8 + g, head = head_of(column), which = column % P;
       const bool on = head < heads;
-      const char *row = static_cast<const char *>(a.q) + (c.b * a.ld_row + (head0 + (on ? head : 0)) * a.ld_head) * size;
+      const int64_t from = c.b * a.ld_row + (head0 + (on ? head : 0)) * a.ld_head;
       float v[DP / 4], most = 0.0f;
+      if constexpr (kBf16 || (kCodes && P == 1)) query_row<__nv_bfloat16, EL>(from, on, v);
+      else if (kCodes && a.dtype == 0) query_row<float, EL>(from, on, v);
+      else query_row<__half, EL>(from, on, v);
 #pragma unroll
-      for (int i = 0; i < DP / 4; ++i) {
-        v[i] = on ? query(row, 4 * EL * (i / EL) + EL * t + i % EL) : 0.0f;
-        most = fmaxf(most, fabsf(v[i]));
-      }
+      for (int i = 0; i < DP / 4; ++i) most = fmaxf(most, fabsf(v[i]));
       float by = 1.0f;
       if constexpr (kCodes) {  // to 2^14 at most
         most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, 1));
@@ -491,62 +517,79 @@ __global__ void __launch_bounds__(S::kWarps * 32, S::kCtas) attend_kernel(const 
   constexpr int NT = S::kWarps * 32, W = S::kWarps, TK = S::TK, DP = S::DP, H = S::kHeads;
   using Warp = AttendWarp<S>;
   extern __shared__ __align__(16) unsigned char smem[];
-  long long *sums = reinterpret_cast<long long *>(smem);                      // [2 W]
-  long long *before = reinterpret_cast<long long *>(smem + 16 * W);           // [NT]
-  AttendPiece *pieces = reinterpret_cast<AttendPiece *>(smem + 16 * W + 8 * NT);  // [W][2]
-  float *heads_of_parts = reinterpret_cast<float *>(smem + 16 * W + 8 * NT + 2 * W * 16);  // [W][kPart]
+  long long *sums = reinterpret_cast<long long *>(smem);  // [2 W]
+  long long *before = sums + 2 * W;                       // [NT]
+  AttendPiece *pieces = reinterpret_cast<AttendPiece *>(before + NT);    // [W][2]: what a warp leaves
+  AttendPiece *chains = pieces + 2 * W;                                  // [W + 1]: what belongs together
+  float *factors = reinterpret_cast<float *>(chains + W + 1);            // [W][2][H]
+  float *totals = factors + 2 * W * H;                                   // [W + 1][2][H]: maxima and sums of the chains
+  float *heads_of_parts = totals + 2 * (W + 1) * H;                      // [W][kPart]
   unsigned char *rings = smem + S::kFixed;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   grid_trigger();
 
-  // the list of tiles: sequences one after the other, in each its pieces of heads, in each its tiles
+  // the list of tiles: sequences one after the other, in each its pieces of heads, in each its tiles.  Lane i of every warp adds up the i-th of 32
+  // runs of sequences (each warp for itself: no barrier, and the lengths are in L2 or nearer); where there are many, thread i the i-th of NT.
   const int all = a.cache.heads * a.parts;
-  const auto scan = [&](int b, long long &sum) {  // tiles of the sequences before b in its chunk, and of all of the chunk
-    int lo, hi;
-    long long n = b < a.seqs.batch ? Warp::tiles_of(a, b, lo, hi) : 0, s = n;
+  const bool wide = a.seqs.batch > 32 * 32;
+  const int runs = wide ? NT : 32, run = (a.seqs.batch + runs - 1) / runs, mine_run = wide ? tid : lane;
+  const auto lanes_before = [&](long long v) {
+    long long s = v;
     for (int d = 1; d < 32; d <<= 1) {
-      const long long v = __shfl_up_sync(0xffffffffu, s, d);
-      if (lane >= d) s += v;
+      const long long o = __shfl_up_sync(0xffffffffu, s, d);
+      if (lane >= d) s += o;
     }
-    __syncthreads();
-    if (lane == 31) sums[warp] = s;
-    __syncthreads();
-    long long earlier = 0;
-    sum = 0;
-    for (int w = 0; w < W; ++w) {
-      if (w < warp) earlier += sums[w];
-      sum += sums[w];
-    }
-    before[tid] = earlier + s - n;
-    __syncthreads();
+    return s - v;
   };
-  long long total = 0, sum = 0;
-  for (int base = 0; base < a.seqs.batch; base += NT) scan(base + tid, sum), total += sum;
-  total *= all;
-  const long long per_cta = max((total + gridDim.x - 1) / gridDim.x, static_cast<long long>(W));
-  const long long from = min(total, blockIdx.x * per_cta), count = min(total, from + per_cta) - from;
+  const auto tiles_in = [&](int b) {
+    int lo, hi;
+    return b < a.seqs.batch ? static_cast<long long>(Warp::tiles_of(a, b, lo, hi)) : 0ll;
+  };
+  long long sum = 0;
+#pragma unroll 4
+  for (int i = 0; i < run; ++i) sum += tiles_in(mine_run * run + i);
+  long long earlier = lanes_before(sum), total = __shfl_sync(0xffffffffu, earlier + sum, 31);
+  if (wide) {
+    if (lane == 0) sums[warp] = total;
+    __syncthreads();
+    total = 0;
+    for (int v = 0; v < W; ++v) {
+      if (v < warp) earlier += sums[v];
+      total += sums[v];
+    }
+    before[tid] = earlier;
+    __syncthreads();
+  }
+  const long long tiles = total * all, per_cta = max((tiles + gridDim.x - 1) / gridDim.x, static_cast<long long>(W));
+  const long long from = min(tiles, blockIdx.x * per_cta), count = min(tiles, from + per_cta) - from;
   const long long per = (count + W - 1) / W;
   const long long mine = from + min(count, warp * per);
   const int n = static_cast<int>(min(per, from + count - mine));  // this warp's tiles
   typename Warp::Cursor at = {};
-  {
+  if (n > 0) {
+    // the last run, and in it the last sequence, with no more than `want` tiles before it
     const long long want = mine / all;
-    long long passed = 0;
-    bool found = n <= 0;
-    for (int base = 0; base < a.seqs.batch; base += NT) {
-      if (a.seqs.batch > NT) scan(base + tid, sum);
-      if (!found && want < passed + sum) {
-        int i = -1;  // the last sequence of the chunk with no more than `want` tiles before it
-        for (int k = 0; k < W; ++k) i += __popc(__ballot_sync(0xffffffffu, passed + before[k * 32 + lane] <= want));
-        at.b = base + i;
-        const long long into = mine - (passed + before[i]) * all;
-        int lo, hi;
-        const int tiles = Warp::tiles_of(a, at.b, lo, hi);
-        at.j = static_cast<int>(into / tiles), at.tile = static_cast<int>(into % tiles);
-        found = true;
+    int i = -1;
+    if (wide) {
+      for (int k = 0; k < W; ++k) i += __popc(__ballot_sync(0xffffffffu, before[k * 32 + lane] <= want));
+      earlier = before[i];
+    } else {
+      i += __popc(__ballot_sync(0xffffffffu, earlier <= want));
+      earlier = __shfl_sync(0xffffffffu, earlier, i);
+    }
+    long long passed = earlier;
+    for (int b = i * run;; b += 32) {
+      const long long here = b + lane < (i + 1) * run ? tiles_in(b + lane) : 0, first = passed + lanes_before(here);
+      const uint32_t who = __ballot_sync(0xffffffffu, here > 0 && first <= want);
+      const int k = 31 - __clz(who);
+      const long long end = __shfl_sync(0xffffffffu, first + here, 31);
+      if (want < end || b + 32 >= (i + 1) * run) {
+        at.b = b + k;
+        const long long into = mine - __shfl_sync(0xffffffffu, first, k) * all, len = __shfl_sync(0xffffffffu, here, k);
+        at.j = static_cast<int>(into / len), at.tile = static_cast<int>(into % len);
+        break;
       }
-      passed += sum;
-      if (a.seqs.batch > NT) __syncthreads();
+      passed = end;
     }
   }
 
@@ -572,10 +615,10 @@ __global__ void __launch_bounds__(S::kWarps * 32, S::kCtas) attend_kernel(const 
     bool starts = at.tile == 0, fresh = true;
 #pragma unroll 1
     for (int i = 0; i < n; ++i) {
+      if (fresh) w.begin(at);  // (its loads, while the first copies are under way)
       copies_wait<S::kStages - 2>();
       __syncwarp();
       fill();
-      if (fresh) w.begin(at);
       w.tile(i % S::kStages);
       fresh = at.tile == at.tiles - 1;
       if (fresh || i == n - 1) {
@@ -608,42 +651,82 @@ __global__ void __launch_bounds__(S::kWarps * 32, S::kCtas) attend_kernel(const 
   }
   __syncthreads();
 
-  // The parts of a sequence's piece in this CTA, joined: one that goes on from the CTA before (slot 0 of warp 0), and those that begin in a
-  // warp (slot 1).  What is not whole goes out with a note.
-  bool noted[2] = {false, false};
-  for (int c = 0; c <= W; ++c) {
+  // The parts of a sequence's piece in this CTA, joined.  A chain of them begins in slot 0 of warp 0 (it goes on from the CTA before), or in
+  // slot 1 of a warp, and goes on in slot 0 of the warps after it.
+  const auto part_of = [&](int v, int slot) -> const float * {
+    return slot == 1 ? reinterpret_cast<const float *>(rings + v * (S::kStages * S::kStage)) : heads_of_parts + v * S::kPart;
+  };
+  const int most_heads = min(H, a.group);
+  for (int c = warp; c <= W; c += W) {
     const int w0 = c == 0 ? 0 : c - 1, slot = c == 0 ? 0 : 1;
-    const AttendPiece p = pieces[w0 * 2 + slot];
-    if (p.b < 0) continue;
-    int last = w0, ends = p.ends;
-    while (!ends && last + 1 < W && pieces[(last + 1) * 2].b >= 0) ends = pieces[++last * 2].ends;
-    const bool whole = slot == 1 && ends;
-    const auto part_of = [&](int v) {
-      return v == w0 && slot == 1 ? reinterpret_cast<const float *>(rings + v * (S::kStages * S::kStage)) : heads_of_parts + v * S::kPart;
-    };
-    const int part = p.j % a.parts, heads = min(H, a.group - part * H);
-    const int64_t head0 = static_cast<int64_t>(p.b) * a.q_heads + p.j / a.parts * a.group + part * H;
-    float *to = a.partial + (blockIdx.x * 2 + slot) * static_cast<int64_t>(S::kPart);
-    for (int i = tid; i < heads * DP; i += NT) {
-      const int head = i / DP, e = i % DP;
-      float top = -INFINITY, l = 0.0f, v = 0.0f;
-      for (int k = w0; k <= last; ++k) top = fmaxf(top, part_of(k)[head]);
-      const float base = top == -INFINITY ? 0.0f : top;
-      for (int k = w0; k <= last; ++k) {
-        const float *from_part = part_of(k), by = exp2_fast(from_part[head] - base);
-        l = fmaf(from_part[H + head], by, l), v = fmaf(from_part[2 * H + i], by, v);
-      }
-      if (whole) {
-        if (e < a.cache.dim) store_out(a, (head0 + head) * a.cache.dim + e, share(v, l));
-        if (e == 0 && a.lse) a.lse[head0 + head] = lse_of(top, l);
-      } else {
-        to[2 * H + i] = v;
-        if (e == 0) to[head] = top, to[H + head] = l;
+    AttendPiece p = pieces[w0 * 2 + slot];
+    p.last = w0;
+    if (p.b >= 0) {
+      while (!p.ends && p.last + 1 < W && pieces[(p.last + 1) * 2].b >= 0) p.ends = pieces[++p.last * 2].ends;
+      // W lanes to a head, one to each part
+      const int v = w0 + lane % W;
+      const bool in = v <= p.last;
+      const float *from_part = part_of(in ? v : w0, v == w0 ? slot : 0);
+      for (int h = lane / W; h < most_heads + lane / W; h += 32 / W) {  // (all lanes take part in each round)
+        const bool on = in && h < H;
+        const float mine = on ? from_part[h] : -INFINITY;
+        float top = mine;
+        for (int o = W / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+        const float by = on ? exp2_fast(mine - (top == -INFINITY ? 0.0f : top)) : 0.0f;
+        float l = on ? from_part[H + h] * by : 0.0f;
+        for (int o = W / 2; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+        if (on) factors[(v * 2 + (v == w0 ? slot : 0)) * H + h] = by;
+        if (on && v == w0) totals[c * 2 * H + h] = top, totals[(c * 2 + 1) * H + h] = l;
       }
     }
-    if (!whole) {
+    if (lane == 0) chains[c] = p;
+  }
+  __syncthreads();
+  // the chains that there are, and four elements of a head of one of them to a thread
+  int chain_of[W + 1], count_of_chains = 0;
+  bool noted[2] = {false, false};
+#pragma unroll
+  for (int c = 0; c <= W; ++c) {
+    chain_of[c] = 0;
+    const AttendPiece p = chains[c];
+    if (p.b < 0) continue;
+    const int slot = c == 0 ? 0 : 1;
+#pragma unroll
+    for (int i = 0; i <= c; ++i)
+      if (i == count_of_chains) chain_of[i] = c;
+    ++count_of_chains;
+    if (slot == 0 || !p.ends) {  // out with a note
       noted[slot] = true;
-      if (tid == 0) a.piece[blockIdx.x * 2 + slot] = {p.b, p.j, ends, 0};
+      if (tid == 0) a.piece[blockIdx.x * 2 + slot] = {p.b, p.j, p.ends, 0};
+    }
+  }
+  for (int i = tid; i < count_of_chains * most_heads * (DP / 4); i += NT) {
+    const int n = i / (most_heads * (DP / 4)), head = i / (DP / 4) % most_heads, e = i % (DP / 4) * 4;
+    int c = chain_of[0];
+#pragma unroll
+    for (int k = 1; k <= W; ++k) c = k == n ? chain_of[k] : c;
+    const AttendPiece p = chains[c];
+    const int w0 = c == 0 ? 0 : c - 1, slot = c == 0 ? 0 : 1, part = p.j % a.parts;
+    if (head >= a.group - part * H) continue;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int k = w0; k <= p.last; ++k) {
+      const int s = k == w0 ? slot : 0;
+      const float by = factors[(k * 2 + s) * H + head];
+      const float4 x = *reinterpret_cast<const float4 *>(part_of(k, s) + 2 * H + head * DP + e);
+      v[0] = fmaf(x.x, by, v[0]), v[1] = fmaf(x.y, by, v[1]), v[2] = fmaf(x.z, by, v[2]), v[3] = fmaf(x.w, by, v[3]);
+    }
+    const float top = totals[c * 2 * H + head], l = totals[(c * 2 + 1) * H + head];
+    if (slot == 1 && p.ends) {
+      const int64_t at = static_cast<int64_t>(p.b) * a.q_heads + p.j / a.parts * a.group + part * H + head;
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        if (e + k < a.cache.dim) store_out(a, at * a.cache.dim + e + k, share(v[k], l));
+      if (e == 0 && a.lse) a.lse[at] = lse_of(top, l);
+    } else {
+      float *to = a.partial + (blockIdx.x * 2 + slot) * static_cast<int64_t>(S::kPart);
+      *reinterpret_cast<float4 *>(to + 2 * H + head * DP + e) = make_float4(v[0], v[1], v[2], v[3]);
+      if (e == 0) to[head] = top, to[H + head] = l;
     }
   }
   if (tid < 2 && !noted[tid]) a.piece[blockIdx.x * 2 + tid] = {-1, 0, 0, 0};

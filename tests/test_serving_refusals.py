@@ -22,7 +22,7 @@ CACHES = [(dict(k=None), BAD), (dict(v=P + 8), BAD), (dict(k_scale=None), BAD), 
           (dict(heads=0), BAD), (dict(head_dim=0), BAD), (dict(ld=63), BAD), (dict(ld=72), BAD), (dict(dtype=0), BAD), (dict(dtype=4), BAD), (dict(head_dim=257, ld=272), FAR),
           (dict(heads=1 << 20), FAR), (dict(page_size=1 << 20), FAR), (dict(pages=1 << 31), FAR), (dict(ld=(1 << 20) + 16), BAD), (dict(dtype=2, ld=68), BAD)]
 SEQS = [(dict(table=None), BAD), (dict(lengths=None), BAD), (dict(lengths=P + 1), BAD), (dict(ldt=3), BAD), (dict(batch=-1), BAD), (dict(columns=-1), BAD),
-        (dict(columns=1 << 28, ldt=1 << 28), FAR)]
+        (dict(columns=1 << 28, ldt=1 << 28), FAR), (dict(batch=1 << 24), FAR)]
 
 
 def append(c=None, s=None, rows=P, total=5, k=P, kr=128, kh=64, v=P, vr=128, vh=64, dtype=2):
