@@ -88,6 +88,18 @@ __device__ __forceinline__ void mma_16816(float *c, uint32_t a0, uint32_t a1, ui
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+// the same on nothing
+template <bool BF16>
+__device__ __forceinline__ void mma_16816_first(float *c, uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  if constexpr (BF16)
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+  else
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(c[0]), "=f"(c[1]), "=f"(c[2]), "=f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.0f));
+}
 // an 8 x 8 matrix of 16-bit elements, transposed over the warp
 __device__ __forceinline__ uint32_t transpose_8x8(uint32_t v) {
   uint32_t r;
@@ -140,13 +152,14 @@ struct AttendWarp {
   const AttendArgs &a;
   const uint32_t ring;  // shared memory
   const int lane, g, t;
-  const int all;  // pieces of heads of a sequence
+  const int all;    // pieces of heads of a sequence
+  const bool even;  // a tile lies in one page, and its rows follow one another without a gap
 
   uint32_t qf[DP / 16][NB][2];
   float o[DP / 16][NB][4], top[HC], vtop[HC], l[HC], qs[HC];
 
   __device__ AttendWarp(const AttendArgs &args, uint32_t ring_)
-      : a(args), ring(ring_), lane(threadIdx.x & 31), g((threadIdx.x & 31) >> 2), t(threadIdx.x & 3), all(args.cache.heads * args.parts) {}
+      : a(args), ring(ring_), lane(threadIdx.x & 31), g((threadIdx.x & 31) >> 2), t(threadIdx.x & 3), all(args.cache.heads * args.parts), even(args.cache.page_size % TK == 0 && args.cache.ld == DP && args.cache.dim == DP) {}
 
   static __device__ int tiles_of(const AttendArgs &a, int b, int &lo, int &hi) {
     hi = sequence_length(a.seqs, b, a.cache.page_size);
@@ -172,14 +185,15 @@ struct AttendWarp {
 
   // this lane's row of a tile: its page and place in it, -1 for none
   __device__ void find(const Cursor &c, int &page, int &place) const {
-    const int p = (c.t0 + c.tile) * TK + lane;
+    const int p0 = (c.t0 + c.tile) * TK, p = p0 + lane;
     page = -1, place = 0;
     if (lane < TK && p >= c.lo && p < c.hi) {
-      const int column = p / a.cache.page_size;
+      const int of = even ? p0 : p, column = of / a.cache.page_size;  // (a tile in one page: the same for all)
       place = p - column * a.cache.page_size;
       page = a.seqs.table[static_cast<int64_t>(c.b) * a.seqs.ldt + column];
     }
   }
+  // the 16-byte unit of a row that a row's unit u is kept in, so that the 8 lanes of a read lie in 8 groups of banks
   static __device__ __forceinline__ uint32_t k_unit(uint32_t row, uint32_t u) { return UPR >= 8 ? u ^ ((row & 1) << 2) : u; }
   static __device__ __forceinline__ uint32_t v_unit(uint32_t row, uint32_t u) {
     return UPR >= 8 ? u ^ (((row >> 1) & 3) << 1) : UPR == 4 ? u ^ (((row >> 1) & 1) << 1) : u;
@@ -191,16 +205,29 @@ struct AttendWarp {
     const int64_t row = fine ? (static_cast<int64_t>(page) * a.cache.heads + c.j / a.parts) * a.cache.page_size + place : 0;
     const uint32_t mask = __ballot_sync(0xffffffffu, fine);
     const int64_t from = row * (static_cast<int64_t>(a.cache.ld) * S::kSize);
-    const int width = a.cache.dim * S::kSize;
+    constexpr uint32_t kWhole = TK == 32 ? 0xffffffffu : (1u << TK) - 1;
+    constexpr int kRows = 32 / UPR > 0 ? 32 / UPR : 1;  // of 32 units
+    if (even && mask == kWhole) {  // rows that follow one another, all of them: a copy is one instruction
+      const int64_t first = __shfl_sync(0xffffffffu, from, 0) + lane * 16;
+      const char *k = static_cast<const char *>(a.cache.k) + first, *v = static_cast<const char *>(a.cache.v) + first;
+      const uint32_t r0 = lane / UPR, u = lane % UPR, ku = at + r0 * S::kRow, vu = ku + TK * S::kRow;
 #pragma unroll
-    for (int i = 0; i < TK * UPR / 32; ++i) {
-      const int r = (i * 32 + lane) / UPR, u = (i * 32 + lane) % UPR;
-      const int64_t off = __shfl_sync(0xffffffffu, from, r) + u * 16;
-      int bytes = width - u * 16;
-      bytes = (mask >> r) & 1 ? (bytes < 0 ? 0 : bytes < 16 ? bytes : 16) : 0;
-      const int64_t src = bytes > 0 ? off : 0;
-      copy16(at + r * S::kRow + k_unit(r, u) * 16, static_cast<const char *>(a.cache.k) + src, bytes);
-      copy16(at + TK * S::kRow + r * S::kRow + v_unit(r, u) * 16, static_cast<const char *>(a.cache.v) + src, bytes);
+      for (int i = 0; i < TK * UPR / 32; ++i) {  // (a row is r0 and i kRows in disjoint bits, and so are their parts of a unit's number)
+        copy16(ku + i * kRows * S::kRow + (k_unit(r0, u) ^ k_unit(i * kRows, 0)) * 16, k + i * 512, 16);
+        copy16(vu + i * kRows * S::kRow + (v_unit(r0, u) ^ v_unit(i * kRows, 0)) * 16, v + i * 512, 16);
+      }
+    } else {
+      const int width = a.cache.dim * S::kSize;
+#pragma unroll
+      for (int i = 0; i < TK * UPR / 32; ++i) {
+        const int r = (i * 32 + lane) / UPR, u = (i * 32 + lane) % UPR;
+        const int64_t off = __shfl_sync(0xffffffffu, from, r) + u * 16;
+        int bytes = width - u * 16;
+        bytes = (mask >> r) & 1 ? (bytes < 0 ? 0 : bytes < 16 ? bytes : 16) : 0;
+        const int64_t src = bytes > 0 ? off : 0;
+        copy16(at + r * S::kRow + k_unit(r, u) * 16, static_cast<const char *>(a.cache.k) + src, bytes);
+        copy16(at + TK * S::kRow + r * S::kRow + v_unit(r, u) * 16, static_cast<const char *>(a.cache.v) + src, bytes);
+      }
     }
     if constexpr (kCodes) {
       if (lane < TK) {
@@ -327,12 +354,6 @@ struct AttendWarp {
     const uint32_t at = ring + stage * S::kStage, vat = at + TK * S::kRow, scales = vat + TK * S::kRow;
     const uint32_t mask = __float_as_uint(lds(scales + 2 * TK * 4));
     float s[M][NB][4];
-#pragma unroll
-    for (int mt = 0; mt < M; ++mt)
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[mt][nb][i] = 0.0f;
     // S^T = K q^T
     constexpr int KB = S::kRow / 4, KW = KB < 16 ? KB / 4 : 4, KP = KB < 16 ? 1 : KB / 16;  // a lane's bytes of a key, words of a piece, pieces
 #pragma unroll
@@ -351,14 +372,21 @@ struct AttendWarp {
             const uint32_t x = w[0][i] ^ 0x80808080u, y = w[1][i] ^ 0x80808080u;
             const uint32_t a0 = halves_of(x, kLow), a1 = halves_of(y, kLow), a2 = halves_of(x, kHigh), a3 = halves_of(y, kHigh);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) mma_16816<false>(s[mt][nb], a0, a1, a2, a3, qf[pc * KW + i][nb][0], qf[pc * KW + i][nb][1]);
+            for (int nb = 0; nb < NB; ++nb) {
+              const uint32_t *b = qf[pc * KW + i][nb];
+              if (pc == 0 && i == 0) mma_16816_first<false>(s[mt][nb], a0, a1, a2, a3, b[0], b[1]);
+              else mma_16816<false>(s[mt][nb], a0, a1, a2, a3, b[0], b[1]);
+            }
           }
         } else {
 #pragma unroll
           for (int i = 0; i < KW / 2; ++i)
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
-              mma_16816<kBf16>(s[mt][nb], w[0][2 * i], w[1][2 * i], w[0][2 * i + 1], w[1][2 * i + 1], qf[pc * (KW / 2) + i][nb][0], qf[pc * (KW / 2) + i][nb][1]);
+            for (int nb = 0; nb < NB; ++nb) {
+              const uint32_t *b = qf[pc * (KW / 2) + i][nb];
+              if (pc == 0 && i == 0) mma_16816_first<kBf16>(s[mt][nb], w[0][2 * i], w[1][2 * i], w[0][2 * i + 1], w[1][2 * i + 1], b[0], b[1]);
+              else mma_16816<kBf16>(s[mt][nb], w[0][2 * i], w[1][2 * i], w[0][2 * i + 1], w[1][2 * i + 1], b[0], b[1]);
+            }
         }
       }
     }
@@ -385,20 +413,28 @@ struct AttendWarp {
           if constexpr (kCodes) vmost[hc] = fmaxf(vmost[hc], v + vs[mt][i]);
         }
       }
+    // (most tiles of a long sequence have no new maximum: one vote instead of its 6 shuffles a head)
     float keep[HC];
+    bool higher = false;
 #pragma unroll
-    for (int hc = 0; hc < HC; ++hc) {
-      most[hc] = over_keys_max(most[hc]);
-      const float base = most[hc] == -INFINITY ? 0.0f : most[hc];  // (no key yet)
-      const float old = exp2_fast(top[hc] - base);
-      top[hc] = most[hc], most[hc] = base - (kCodes ? 0.0f : kOffset);
-      l[hc] *= old, keep[hc] = old;
-      if constexpr (kCodes) {
-        vmost[hc] = over_keys_max(vmost[hc]);
-        const float vbase = vmost[hc] == -INFINITY ? 0.0f : vmost[hc];
-        keep[hc] = exp2_fast(vtop[hc] - vbase);
-        vtop[hc] = vmost[hc], vmost[hc] = vbase - kOffset;
+    for (int hc = 0; hc < HC; ++hc) higher |= most[hc] > top[hc] || (kCodes && vmost[hc] > vtop[hc]), keep[hc] = 1.0f;
+    if (__any_sync(0xffffffffu, higher)) {
+#pragma unroll
+      for (int hc = 0; hc < HC; ++hc) {
+        most[hc] = over_keys_max(most[hc]);
+        keep[hc] = exp2_fast(top[hc] - (most[hc] == -INFINITY ? 0.0f : most[hc]));
+        top[hc] = most[hc], l[hc] *= keep[hc];
+        if constexpr (kCodes) {
+          vmost[hc] = over_keys_max(vmost[hc]);
+          keep[hc] = exp2_fast(vtop[hc] - (vmost[hc] == -INFINITY ? 0.0f : vmost[hc]));
+          vtop[hc] = vmost[hc];
+        }
       }
+    }
+#pragma unroll
+    for (int hc = 0; hc < HC; ++hc) {  // (0 where no key has been)
+      most[hc] = (top[hc] == -INFINITY ? 0.0f : top[hc]) - (kCodes ? 0.0f : kOffset);
+      vmost[hc] = (vtop[hc] == -INFINITY ? 0.0f : vtop[hc]) - kOffset;
     }
     uint32_t pf[M][NB][2];
 #pragma unroll
@@ -437,12 +473,6 @@ struct AttendWarp {
         constexpr int kPairs = kCodes ? 2 : 1;  // pairs of elements in a word
         float c[kPairs][NB][4];
 #pragma unroll
-        for (int h = 0; h < kPairs; ++h)
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int e = 0; e < 4; ++e) c[h][nb][e] = 0.0f;
-#pragma unroll
         for (int mt = 0; mt < M; ++mt) {
           if constexpr (kCodes) {
             const uint32_t x0 = w[mt][0][i] ^ 0x80808080u, x1 = w[mt][1][i] ^ 0x80808080u, x2 = w[mt][2][i] ^ 0x80808080u, x3 = w[mt][3][i] ^ 0x80808080u;
@@ -451,13 +481,19 @@ struct AttendWarp {
               const uint32_t y = __byte_perm(x0, x1, h == 0 ? 0x5140u : 0x7362u), z = __byte_perm(x2, x3, h == 0 ? 0x5140u : 0x7362u);
               const uint32_t a0 = halves_of(y, kLow), a1 = halves_of(y, kHigh), a2 = halves_of(z, kLow), a3 = halves_of(z, kHigh);
 #pragma unroll
-              for (int nb = 0; nb < NB; ++nb) mma_16816<false>(c[h][nb], a0, a1, a2, a3, pf[mt][nb][0], pf[mt][nb][1]);
+              for (int nb = 0; nb < NB; ++nb) {
+                if (mt == 0) mma_16816_first<false>(c[h][nb], a0, a1, a2, a3, pf[mt][nb][0], pf[mt][nb][1]);
+                else mma_16816<false>(c[h][nb], a0, a1, a2, a3, pf[mt][nb][0], pf[mt][nb][1]);
+              }
             }
           } else {
             const uint32_t a0 = __byte_perm(w[mt][0][i], w[mt][1][i], 0x5410u), a1 = __byte_perm(w[mt][0][i], w[mt][1][i], 0x7632u);
             const uint32_t a2 = __byte_perm(w[mt][2][i], w[mt][3][i], 0x5410u), a3 = __byte_perm(w[mt][2][i], w[mt][3][i], 0x7632u);
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb) mma_16816<kBf16>(c[0][nb], a0, a1, a2, a3, pf[mt][nb][0], pf[mt][nb][1]);
+            for (int nb = 0; nb < NB; ++nb) {
+              if (mt == 0) mma_16816_first<kBf16>(c[0][nb], a0, a1, a2, a3, pf[mt][nb][0], pf[mt][nb][1]);
+              else mma_16816<kBf16>(c[0][nb], a0, a1, a2, a3, pf[mt][nb][0], pf[mt][nb][1]);
+            }
           }
         }
 #pragma unroll
