@@ -3,6 +3,10 @@
 //
 //   alpha = max(max_i |x_i|, 2^-100),  code_i = rint(x_i (127 / alpha)),  scale = alpha / 127    (a row of one token and head)
 //   value_i = code_i scale
+//
+// Bound by memory: a row is read and written once.  A row has G lanes of a warp (a power of two, 8 elements each), which take its maximum
+// by shuffles; a thread has kAhead rows on their way at once.  Where a row of tensors that lie anyhow has no 16-byte
+// pieces, its elements are read one by one, by the same lanes.
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -16,103 +20,204 @@ namespace aecct {
 namespace {
 
 constexpr float kAlphaMin = 0x1p-100f;
+constexpr int kRowsThreads = 256;
+constexpr int E = 8;  // elements of a row to a lane
+constexpr int kSearched = 1024, kMaxTokens = 512;  // of a CTA
 
-__device__ __forceinline__ float warp_max(float v) {
-  for (int o = 16; o > 0; o >>= 1) {
-    const float w = __shfl_xor_sync(0xffffffffu, v, o);
-    v = (w > v || w != w) ? w : v;  // (a NaN stays)
+struct RowsPlan {
+  int lanes, tokens;  // lanes to a row; tokens of a CTA at most
+  bool wide;          // rows of the call's tensors in pieces of 16 bytes
+};
+
+template <typename T>
+__device__ __forceinline__ void load_row(const T *x, int n, bool wide, float (&v)[E]) {
+  if (wide && n >= E) {
+#pragma unroll
+    for (int i = 0; i < E; i += kVec<T>) load_v<T, kVec<T>>(x + i, v + i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = i < n ? to_f32(x[i]) : 0.0f;
   }
-  return v;
+}
+template <typename T>
+__device__ __forceinline__ void store_row(T *x, int n, bool wide, const float (&v)[E]) {
+  if (wide && n >= E) {
+#pragma unroll
+    for (int i = 0; i < E; i += kVec<T>) store_v<T, kVec<T>>(x + i, v + i);
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+      if (i < n) x[i] = from_f32<T>(v[i]);
+  }
+}
+__device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d) {  // (values of -127 .. 127; a NaN becomes 0)
+  return (__float2int_rn(a) & 0xff) | (__float2int_rn(b) & 0xff) << 8 | (__float2int_rn(c) & 0xff) << 16 | static_cast<uint32_t>(__float2int_rn(d)) << 24;
 }
 
-// a warp to a row (of one token, one head, keys or values)
+// the places of a CTA's tokens; the search over the sequences in shared memory where they fit (a step in L2 takes 0.3 us)
+__device__ __forceinline__ void find_places(const KvRowsCall &c, int64_t token0, int tokens, int64_t *place) {
+  __shared__ int32_t rows[kSearched + 1];
+  const bool near = c.seqs.rows && c.seqs.batch <= kSearched;
+  if (near) {
+    for (int i = threadIdx.x; i <= c.seqs.batch; i += kRowsThreads) rows[i] = c.seqs.rows[i];
+    __syncthreads();
+  }
+  for (int i = threadIdx.x; i < tokens; i += kRowsThreads) place[i] = token_row(c.cache, c.seqs, near ? rows : c.seqs.rows, static_cast<int>(token0) + i);
+  __syncthreads();
+}
+
+// A CTA takes `tokens` tokens, all heads, keys and values.
+template <typename T, typename C, int AHEAD>
+__global__ void __launch_bounds__(kRowsThreads) append_kernel(const __grid_constant__ KvRowsCall c, RowsPlan p) {
+  extern __shared__ int64_t place[];
+  const int64_t token0 = static_cast<int64_t>(blockIdx.x) * p.tokens;
+  const int lane = threadIdx.x % p.lanes, step = kRowsThreads / p.lanes, e = lane * E, n = c.cache.dim - e;
+  const int tokens = static_cast<int>(min(static_cast<int64_t>(p.tokens), c.total - token0)), rows = tokens * 2 * c.cache.heads;
+  const auto row_of = [&](int i, int &token, int &which, int &head) {
+    token = i / (2 * c.cache.heads);
+    const int h = i - token * 2 * c.cache.heads;
+    which = h >= c.cache.heads, head = h - which * c.cache.heads;
+  };
+  bool found = false;
+  for (int i0 = threadIdx.x / p.lanes; i0 - static_cast<int>(threadIdx.x / p.lanes) < rows; i0 += AHEAD * step) {
+    float v[AHEAD][E];
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      const int i = i0 + a * step;
+      int token, which, head;
+      row_of(i < rows ? i : 0, token, which, head);
+      const int64_t r = token0 + token;
+      const T *x = static_cast<const T *>(which ? c.v : c.k) + (which ? r * c.v_row + head * c.v_head : r * c.k_row + head * c.k_head);
+      load_row<T>(x + e, i < rows ? n : 0, p.wide, v[a]);
+    }
+    if (!found) find_places(c, token0, tokens, place), found = true;  // (beside the first rows' loads)
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      const int i = i0 + a * step;
+      int token, which, head;
+      row_of(i < rows ? i : 0, token, which, head);
+      const int64_t at = i < rows ? place[token] : -1, row = at < 0 ? -1 : at + static_cast<int64_t>(head) * c.cache.page_size;
+      C *out = static_cast<C *>(which ? c.cache.v : c.cache.k) + (row < 0 ? 0 : row * c.cache.ld + e);
+      if constexpr (sizeof(C) == 1) {
+        float m = 0.0f;
+#pragma unroll
+        for (int k = 0; k < E; ++k) {
+          const float w = fabsf(v[a][k]);
+          m = (w > m || w != w) ? w : m;  // (a NaN stays)
+        }
+        for (int o = p.lanes / 2; o > 0; o >>= 1) {
+          const float w = __shfl_xor_sync(0xffffffffu, m, o);
+          m = (w > m || w != w) ? w : m;
+        }
+        const float alpha = m < kAlphaMin ? kAlphaMin : m, by = __fdiv_rn(127.0f, alpha);
+        if (row < 0) continue;
+#pragma unroll
+        for (int k = 0; k < E; ++k) v[a][k] = __fmul_rn(v[a][k], by);
+        const uint2 w = make_uint2(codes_of(v[a][0], v[a][1], v[a][2], v[a][3]), codes_of(v[a][4], v[a][5], v[a][6], v[a][7]));
+        if (n >= E) {
+          *reinterpret_cast<uint2 *>(out) = w;  // (rows start on 16 bytes)
+        } else {
+#pragma unroll
+          for (int k = 0; k < E; ++k)
+            if (k < n) out[k] = static_cast<int8_t>((k < 4 ? w.x : w.y) >> (k % 4 * 8));
+        }
+        if (lane == 0) (which ? c.cache.v_scale : c.cache.k_scale)[row] = __fdiv_rn(alpha, 127.0f);
+      } else {
+        if (row >= 0) store_row<C>(out, n, true, v[a]);
+      }
+    }
+  }
+}
+
+template <typename C, typename T, int AHEAD>
+__global__ void __launch_bounds__(kRowsThreads) read_kernel(const __grid_constant__ KvRowsCall c, RowsPlan p) {
+  extern __shared__ int64_t place[];
+  const int64_t token0 = static_cast<int64_t>(blockIdx.x) * p.tokens;
+  const int lane = threadIdx.x % p.lanes, step = kRowsThreads / p.lanes, e = lane * E, n = c.cache.dim - e;
+  const int tokens = static_cast<int>(min(static_cast<int64_t>(p.tokens), c.total - token0)), rows = tokens * 2 * c.cache.heads;
+  find_places(c, token0, tokens, place);
+  for (int i0 = threadIdx.x / p.lanes; i0 < rows; i0 += AHEAD * step) {
+    float v[AHEAD][E];
+    T *out[AHEAD];
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      const int i = i0 + a * step;
+      if (i >= rows) break;
+      // values after all of the keys: each tensor is written in order
+      const int which = i >= tokens * c.cache.heads, j = i - which * tokens * c.cache.heads, token = j / c.cache.heads, head = j - token * c.cache.heads;
+      const int64_t at = place[token], row = at < 0 ? -1 : at + static_cast<int64_t>(head) * c.cache.page_size;
+      out[a] = static_cast<T *>(which ? c.v_out : c.k_out) + ((token0 + token) * c.cache.heads + head) * c.cache.dim + e;
+      const C *x = static_cast<const C *>(which ? c.cache.v : c.cache.k) + (row < 0 ? 0 : row * c.cache.ld + e);
+      if constexpr (sizeof(C) == 1) {
+        const float scale = row < 0 ? 0.0f : (which ? c.cache.v_scale : c.cache.k_scale)[row];
+        uint2 w = make_uint2(0, 0);
+        if (row >= 0 && n >= E) {
+          w = *reinterpret_cast<const uint2 *>(x);
+        } else if (row >= 0) {
+#pragma unroll
+          for (int k = 0; k < E; ++k)
+            if (k < n) (k < 4 ? w.x : w.y) |= static_cast<uint32_t>(static_cast<uint8_t>(x[k])) << (k % 4 * 8);
+        }
+#pragma unroll
+        for (int k = 0; k < E; ++k) v[a][k] = __fmul_rn(static_cast<float>(static_cast<int8_t>((k < 4 ? w.x : w.y) >> (k % 4 * 8))), scale);
+      } else {
+        load_row<C>(x, row < 0 ? 0 : n, true, v[a]);
+      }
+    }
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a)
+      if (i0 + a * step < rows) store_row<T>(out[a], n, p.wide, v[a]);
+  }
+}
+
+// One wave of four CTAs to an SM, each with a share of the tokens: finding their places is a chain of three trips to L2 (with 4 tokens to a CTA, 4,500 CTAs
+// of them, 18,000 prompt tokens took 77 us).  Few tokens: a CTA to each pass over its lanes.
+template <class F>
+cudaError_t plan_rows(const KvRowsCall &c, bool wide, F &&launch) {
+  RowsPlan p = {1, 1, wide};
+  while (p.lanes * E < c.cache.dim) p.lanes *= 2;
+  const int64_t groups = kRowsThreads / p.lanes, rows = 2 * static_cast<int64_t>(c.cache.heads), ctas = 4 * static_cast<int64_t>(sm_count());
+  int64_t tokens = (c.total + ctas - 1) / ctas;
+  if (tokens * rows < groups) tokens = groups / rows;
+  p.tokens = static_cast<int>(tokens < 1 ? 1 : tokens > kMaxTokens ? kMaxTokens : tokens);
+  launch(static_cast<unsigned>((c.total + p.tokens - 1) / p.tokens), p, static_cast<size_t>(p.tokens) * sizeof(int64_t), p.tokens * rows >= 4 * groups);
+  return cudaGetLastError();
+}
+
+// whether rows of these tensors (dim elements, their places so many elements apart) are pieces of 16 bytes
+bool in_pieces(const void *k, const void *v, int64_t a, int64_t b, int64_t x, int64_t y, int dim, int size) {
+  return ((reinterpret_cast<uintptr_t>(k) | reinterpret_cast<uintptr_t>(v) | static_cast<uintptr_t>((a | b | x | y | dim) * size)) & 15u) == 0;
+}
+
 template <typename T, typename C>
-__global__ void append_kernel(KvRowsCall c) {
-  const int lane = threadIdx.x & 31;
-  const int64_t n = c.total * c.cache.heads * 2;
-  for (int64_t i = blockIdx.x * int64_t(blockDim.x / 32) + threadIdx.x / 32; i < n; i += int64_t(gridDim.x) * (blockDim.x / 32)) {
-    const int which = static_cast<int>(i & 1), h = static_cast<int>((i >> 1) % c.cache.heads);
-    const int64_t r = (i >> 1) / c.cache.heads, place = row_place(c.cache, c.seqs, static_cast<int>(r));
-    if (place < 0) continue;
-    const T *x = static_cast<const T *>(which ? c.v : c.k) + (which ? r * c.v_row + h * c.v_head : r * c.k_row + h * c.k_head);
-    const int64_t row = cache_row(c.cache, place, h);
-    C *out = static_cast<C *>(which ? c.cache.v : c.cache.k) + row * c.cache.ld;
-    if constexpr (sizeof(C) == 1) {
-      float m = 0.0f;
-      for (int e = lane; e < c.cache.dim; e += 32) {
-        const float v = fabsf(to_f32(x[e]));
-        m = (v > m || v != v) ? v : m;
-      }
-      m = warp_max(m);
-      const float alpha = m < kAlphaMin ? kAlphaMin : m, by = __fdiv_rn(127.0f, alpha);
-      for (int e = lane; e < c.cache.dim; e += 32) out[e] = static_cast<int8_t>(__float2int_rn(__fmul_rn(to_f32(x[e]), by)));
-      if (lane == 0) (which ? c.cache.v_scale : c.cache.k_scale)[row] = __fdiv_rn(alpha, 127.0f);
-    } else {
-      for (int e = lane; e < c.cache.dim; e += 32) out[e] = from_f32<C>(to_f32(x[e]));
-    }
-  }
+cudaError_t append_of(const KvRowsCall &c, cudaStream_t st) {
+  return plan_rows(c, in_pieces(c.k, c.v, c.k_row, c.k_head, c.v_row, c.v_head, 0, sizeof(T)), [&](unsigned grid, const RowsPlan &p, size_t smem, bool many) {
+    if (many) append_kernel<T, C, 4><<<grid, kRowsThreads, smem, st>>>(c, p);
+    else append_kernel<T, C, 1><<<grid, kRowsThreads, smem, st>>>(c, p);
+  });
 }
-
 template <typename C, typename T>
-__global__ void read_kernel(KvRowsCall c) {
-  const int lane = threadIdx.x & 31;
-  const int64_t n = c.total * c.cache.heads * 2;
-  for (int64_t i = blockIdx.x * int64_t(blockDim.x / 32) + threadIdx.x / 32; i < n; i += int64_t(gridDim.x) * (blockDim.x / 32)) {
-    const int which = static_cast<int>(i & 1), h = static_cast<int>((i >> 1) % c.cache.heads);
-    const int64_t r = (i >> 1) / c.cache.heads, place = row_place(c.cache, c.seqs, static_cast<int>(r));
-    T *out = static_cast<T *>(which ? c.v_out : c.k_out) + (r * c.cache.heads + h) * c.cache.dim;
-    const int64_t row = place < 0 ? 0 : cache_row(c.cache, place, h);
-    const C *x = static_cast<const C *>(which ? c.cache.v : c.cache.k) + row * c.cache.ld;
-    float scale = 1.0f;
-    if constexpr (sizeof(C) == 1) scale = place < 0 ? 0.0f : (which ? c.cache.v_scale : c.cache.k_scale)[row];
-    for (int e = lane; e < c.cache.dim; e += 32) {
-      float v = 0.0f;
-      if (place >= 0) {
-        if constexpr (sizeof(C) == 1) v = __fmul_rn(static_cast<float>(x[e]), scale);
-        else v = to_f32(x[e]);
-      }
-      out[e] = from_f32<T>(v);
-    }
-  }
+cudaError_t read_of(const KvRowsCall &c, cudaStream_t st) {
+  return plan_rows(c, in_pieces(c.k_out, c.v_out, 0, 0, 0, 0, c.cache.dim, sizeof(T)), [&](unsigned grid, const RowsPlan &p, size_t smem, bool many) {
+    if (many) read_kernel<C, T, 4><<<grid, kRowsThreads, smem, st>>>(c, p);
+    else read_kernel<C, T, 1><<<grid, kRowsThreads, smem, st>>>(c, p);
+  });
 }
-
-int grid_of(const KvRowsCall &c) {
-  const int64_t n = (c.total * c.cache.heads * 2 + 7) / 8, most = 16 * static_cast<int64_t>(sm_count());
-  return static_cast<int>(n < most ? n : most);
+template <typename C>
+cudaError_t read_from(const KvRowsCall &c, cudaStream_t st) {
+  return c.dtype == 0 ? read_of<C, float>(c, st) : c.dtype == 1 ? read_of<C, __half>(c, st) : read_of<C, __nv_bfloat16>(c, st);
 }
 
 }  // namespace
 
 cudaError_t launch_kv_append(const KvRowsCall &c, cudaStream_t st) {
-  const int g = grid_of(c);
-  if (c.cache_dtype != 3) {
-    if (c.dtype == 1) append_kernel<__half, __half><<<g, 256, 0, st>>>(c);
-    else append_kernel<__nv_bfloat16, __nv_bfloat16><<<g, 256, 0, st>>>(c);
-  } else if (c.dtype == 0) {
-    append_kernel<float, int8_t><<<g, 256, 0, st>>>(c);
-  } else if (c.dtype == 1) {
-    append_kernel<__half, int8_t><<<g, 256, 0, st>>>(c);
-  } else {
-    append_kernel<__nv_bfloat16, int8_t><<<g, 256, 0, st>>>(c);
-  }
-  return cudaGetLastError();
+  if (c.cache_dtype == 1) return append_of<__half, __half>(c, st);
+  if (c.cache_dtype == 2) return append_of<__nv_bfloat16, __nv_bfloat16>(c, st);
+  return c.dtype == 0 ? append_of<float, int8_t>(c, st) : c.dtype == 1 ? append_of<__half, int8_t>(c, st) : append_of<__nv_bfloat16, int8_t>(c, st);
 }
-
-namespace {
-template <typename C>
-void read_as(const KvRowsCall &c, int g, cudaStream_t st) {
-  if (c.dtype == 0) read_kernel<C, float><<<g, 256, 0, st>>>(c);
-  else if (c.dtype == 1) read_kernel<C, __half><<<g, 256, 0, st>>>(c);
-  else read_kernel<C, __nv_bfloat16><<<g, 256, 0, st>>>(c);
-}
-}  // namespace
 
 cudaError_t launch_kv_read(const KvRowsCall &c, cudaStream_t st) {
-  const int g = grid_of(c);
-  if (c.cache_dtype == 3) read_as<int8_t>(c, g, st);
-  else if (c.cache_dtype == 1) read_as<__half>(c, g, st);
-  else read_as<__nv_bfloat16>(c, g, st);
-  return cudaGetLastError();
+  return c.cache_dtype == 3 ? read_from<int8_t>(c, st) : c.cache_dtype == 1 ? read_from<__half>(c, st) : read_from<__nv_bfloat16>(c, st);
 }
 
 }  // namespace aecct
