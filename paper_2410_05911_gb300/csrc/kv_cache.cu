@@ -4,9 +4,8 @@
 //   alpha = max(max_i |x_i|, 2^-100),  code_i = rint(x_i (127 / alpha)),  scale = alpha / 127    (a row of one token and head)
 //   value_i = code_i scale
 //
-// Bound by memory: a row is read and written once.  A row has G lanes of a warp (a power of two, 8 elements each), which take its maximum
-// by shuffles; a thread has kAhead rows on their way at once.  Where a row of tensors that lie anyhow has no 16-byte
-// pieces, its elements are read one by one, by the same lanes.
+// Bound by memory: a row is read and written once.  A row has G lanes of a warp (a power of two, 16 elements each), which take its maximum
+// by shuffles; a thread has kAhead rows on their way at once.
 #include <cuda_runtime.h>
 
 #include <cstdint>
@@ -21,38 +20,65 @@ namespace {
 
 constexpr float kAlphaMin = 0x1p-100f;
 constexpr int kRowsThreads = 256;
-constexpr int E = 8;  // elements of a row to a lane
+constexpr int E = 16;  // elements of a row to a lane
 constexpr int kSearched = 1024, kMaxTokens = 512;  // of a CTA
+constexpr int kAhead = 2;  // rows that a lane group has on their way at once, where it has several
 
 struct RowsPlan {
   int lanes, tokens;  // lanes to a row; tokens of a CTA at most
-  bool wide;          // rows of the call's tensors in pieces of 16 bytes
 };
 
+// n of E elements (none for n <= 0, all for n >= E) from a 16-byte border, the others 0
 template <typename T>
-__device__ __forceinline__ void load_row(const T *x, int n, bool wide, float (&v)[E]) {
-  if (wide && n >= E) {
+__device__ __forceinline__ void load_row(const T *x, int n, float (&v)[E]) {
 #pragma unroll
-    for (int i = 0; i < E; i += kVec<T>) load_v<T, kVec<T>>(x + i, v + i);
-  } else {
+  for (int i = 0; i < E; i += kVec<T>) {
+    if (n >= i + kVec<T>) {
+      load_v<T, kVec<T>>(x + i, v + i);
+    } else {
 #pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = i < n ? to_f32(x[i]) : 0.0f;
+      for (int k = 0; k < kVec<T>; ++k) v[i + k] = i + k < n ? to_f32(x[i + k]) : 0.0f;
+    }
   }
 }
 template <typename T>
-__device__ __forceinline__ void store_row(T *x, int n, bool wide, const float (&v)[E]) {
-  if (wide && n >= E) {
+__device__ __forceinline__ void store_row(T *x, int n, const float (&v)[E]) {
 #pragma unroll
-    for (int i = 0; i < E; i += kVec<T>) store_v<T, kVec<T>>(x + i, v + i);
-  } else {
+  for (int i = 0; i < E; i += kVec<T>) {
+    if (n >= i + kVec<T>) {
+      store_v<T, kVec<T>>(x + i, v + i);
+    } else {
 #pragma unroll
-    for (int i = 0; i < E; ++i)
-      if (i < n) x[i] = from_f32<T>(v[i]);
+      for (int k = 0; k < kVec<T>; ++k)
+        if (i + k < n) x[i + k] = from_f32<T>(v[i + k]);
+    }
   }
 }
-__device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d) {  // (values of -127 .. 127; a NaN becomes 0)
-  return (__float2int_rn(a) & 0xff) | (__float2int_rn(b) & 0xff) << 8 | (__float2int_rn(c) & 0xff) << 16 | static_cast<uint32_t>(__float2int_rn(d)) << 24;
+// Four numbers of up to 127 as codes, each rounded to a whole number by adding 1.5 2^23, whose last byte it then is.
+__device__ __forceinline__ uint32_t codes_of(const float *v) {
+  const auto b = [&](int i) { return __float_as_uint(v[i] + 12582912.0f); };
+  return __byte_perm(__byte_perm(b(0), b(1), 0x0040u), __byte_perm(b(2), b(3), 0x0040u), 0x5410u);
 }
+// and back: 2^23 + 128 + code, less 2^23 + 128
+__device__ __forceinline__ float code_value(uint32_t biased, int i) {
+  return __uint_as_float(__byte_perm(biased, 0x4b000000u, 0x7440u | static_cast<uint32_t>(i))) - 8388736.0f;
+}
+
+// alpha / 127: the product with 1 / 127, and what it leaves of alpha (the rounded quotient, for every mantissa)
+__device__ __forceinline__ float scale_of(float alpha) {
+  const float by = 1.0f / 127.0f, q = __fmul_rn(alpha, by);
+  return fmaf(fmaf(-q, 127.0f, alpha), by, q);
+}
+
+// the rows of a CTA that a lane group takes: every step-th, as a token and one of its `per` rows
+struct RowsWalk {
+  int token, at, per, tokens_on, on;
+  __device__ RowsWalk(int first, int step, int per_) : token(first / per_), at(first - first / per_ * per_), per(per_), tokens_on(step / per_), on(step - step / per_ * per_) {}
+  __device__ __forceinline__ void next() {
+    token += tokens_on, at += on;
+    if (at >= per) at -= per, ++token;
+  }
+};
 
 // the places of a CTA's tokens; the search over the sequences in shared memory where they fit (a step in L2 takes 0.3 us)
 __device__ __forceinline__ void find_places(const KvRowsCall &c, int64_t token0, int tokens, int64_t *place) {
@@ -73,61 +99,95 @@ __global__ void __launch_bounds__(kRowsThreads) append_kernel(const __grid_const
   const int64_t token0 = static_cast<int64_t>(blockIdx.x) * p.tokens;
   const int lane = threadIdx.x % p.lanes, step = kRowsThreads / p.lanes, e = lane * E, n = c.cache.dim - e;
   const int tokens = static_cast<int>(min(static_cast<int64_t>(p.tokens), c.total - token0)), rows = tokens * 2 * c.cache.heads;
-  const auto row_of = [&](int i, int &token, int &which, int &head) {
-    token = i / (2 * c.cache.heads);
-    const int h = i - token * 2 * c.cache.heads;
-    which = h >= c.cache.heads, head = h - which * c.cache.heads;
-  };
-  bool found = false;
-  for (int i0 = threadIdx.x / p.lanes; i0 - static_cast<int>(threadIdx.x / p.lanes) < rows; i0 += AHEAD * step) {
+  RowsWalk w(threadIdx.x / p.lanes, step, 2 * c.cache.heads);
+  for (int i = 0; i < rows; i += AHEAD * step) {
     float v[AHEAD][E];
+    int token[AHEAD], at[AHEAD];
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
-      const int i = i0 + a * step;
-      int token, which, head;
-      row_of(i < rows ? i : 0, token, which, head);
-      const int64_t r = token0 + token;
-      const T *x = static_cast<const T *>(which ? c.v : c.k) + (which ? r * c.v_row + head * c.v_head : r * c.k_row + head * c.k_head);
-      load_row<T>(x + e, i < rows ? n : 0, p.wide, v[a]);
+      token[a] = w.token, at[a] = w.at;
+      w.next();
+      const bool values = at[a] >= c.cache.heads;
+      const int64_t r = token0 + token[a];
+      const T *x = values ? static_cast<const T *>(c.v) + (r * c.v_row + (at[a] - c.cache.heads) * c.v_head) : static_cast<const T *>(c.k) + (r * c.k_row + at[a] * c.k_head);
+      load_row<T>(x + e, token[a] < tokens ? n : 0, v[a]);
     }
-    if (!found) find_places(c, token0, tokens, place), found = true;  // (beside the first rows' loads)
+    if (i == 0) find_places(c, token0, tokens, place);  // (beside the first rows' loads)
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
-      const int i = i0 + a * step;
-      int token, which, head;
-      row_of(i < rows ? i : 0, token, which, head);
-      const int64_t at = i < rows ? place[token] : -1, row = at < 0 ? -1 : at + static_cast<int64_t>(head) * c.cache.page_size;
-      C *out = static_cast<C *>(which ? c.cache.v : c.cache.k) + (row < 0 ? 0 : row * c.cache.ld + e);
+      const bool values = at[a] >= c.cache.heads;
+      const int head = values ? at[a] - c.cache.heads : at[a];
+      const int64_t first = token[a] < tokens ? place[token[a]] : -1, row = first + static_cast<int64_t>(head) * c.cache.page_size;
+      C *out = static_cast<C *>(values ? c.cache.v : c.cache.k) + (row * c.cache.ld + e);
       if constexpr (sizeof(C) == 1) {
-        float m = 0.0f;
+        uint32_t m = 0;  // (as whole numbers, magnitudes keep their order, and a NaN is the largest)
 #pragma unroll
-        for (int k = 0; k < E; ++k) {
-          const float w = fabsf(v[a][k]);
-          m = (w > m || w != w) ? w : m;  // (a NaN stays)
-        }
-        for (int o = p.lanes / 2; o > 0; o >>= 1) {
-          const float w = __shfl_xor_sync(0xffffffffu, m, o);
-          m = (w > m || w != w) ? w : m;
-        }
-        const float alpha = m < kAlphaMin ? kAlphaMin : m, by = __fdiv_rn(127.0f, alpha);
-        if (row < 0) continue;
+        for (int k = 0; k < E; ++k) m = max(m, __float_as_uint(v[a][k]) & 0x7fffffffu);
+        for (int o = p.lanes / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+        const float alpha = __uint_as_float(max(m, __float_as_uint(kAlphaMin))), by = __fdiv_rn(127.0f, alpha);
+        if (first < 0) continue;
 #pragma unroll
         for (int k = 0; k < E; ++k) v[a][k] = __fmul_rn(v[a][k], by);
-        const uint2 w = make_uint2(codes_of(v[a][0], v[a][1], v[a][2], v[a][3]), codes_of(v[a][4], v[a][5], v[a][6], v[a][7]));
+        const uint4 w4 = make_uint4(codes_of(v[a]), codes_of(v[a] + 4), codes_of(v[a] + 8), codes_of(v[a] + 12));
         if (n >= E) {
-          *reinterpret_cast<uint2 *>(out) = w;  // (rows start on 16 bytes)
+          *reinterpret_cast<uint4 *>(out) = w4;  // (rows start on 16 bytes)
         } else {
+          const uint32_t words[4] = {w4.x, w4.y, w4.z, w4.w};
 #pragma unroll
           for (int k = 0; k < E; ++k)
-            if (k < n) out[k] = static_cast<int8_t>((k < 4 ? w.x : w.y) >> (k % 4 * 8));
+            if (k < n) out[k] = static_cast<int8_t>(words[k / 4] >> (k % 4 * 8));
         }
-        if (lane == 0) (which ? c.cache.v_scale : c.cache.k_scale)[row] = __fdiv_rn(alpha, 127.0f);
+        if (lane == 0) (values ? c.cache.v_scale : c.cache.k_scale)[row] = scale_of(alpha);
       } else {
-        if (row >= 0) store_row<C>(out, n, true, v[a]);
+        if (first >= 0) store_row<C>(out, n, v[a]);
       }
     }
   }
 }
+
+// E elements of a cached row (`have` of them, 0 for the others) as they lie there, and as numbers
+template <typename C>
+struct CachedRow {
+  uint4 raw[sizeof(C)];
+  float scale;
+  __device__ __forceinline__ void load(const C *x, int have, const float *scales) {
+    scale = sizeof(C) == 1 && have > 0 ? *scales : 0.0f;
+#pragma unroll
+    for (int k = 0; k < static_cast<int>(sizeof(C)); ++k) {  // (16 bytes each; a row's last ones element by element)
+      constexpr int V = 16 / sizeof(C);
+      raw[k] = make_uint4(0, 0, 0, 0);
+      if (have >= (k + 1) * V) {
+        raw[k] = reinterpret_cast<const uint4 *>(x)[k];
+      } else if (have > k * V) {
+        uint32_t words[4] = {0, 0, 0, 0};
+#pragma unroll
+        for (int h = 0; h < V; ++h) {
+          uint32_t bits = 0;
+          if (k * V + h < have) {
+            if constexpr (sizeof(C) == 1) bits = reinterpret_cast<const uint8_t *>(x)[k * V + h];
+            else bits = reinterpret_cast<const uint16_t *>(x)[k * V + h];
+          }
+          words[h * sizeof(C) / 4] |= bits << (h * sizeof(C) % 4 * 8);
+        }
+        raw[k] = make_uint4(words[0], words[1], words[2], words[3]);
+      }
+    }
+  }
+  __device__ __forceinline__ void numbers(float (&v)[E]) const {
+    if constexpr (sizeof(C) == 1) {
+      const uint32_t words[4] = {raw[0].x, raw[0].y, raw[0].z, raw[0].w};
+#pragma unroll
+      for (int k = 0; k < E; ++k) v[k] = __fmul_rn(code_value(words[k / 4] ^ 0x80808080u, k % 4), scale);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 2; ++k) {
+        const uint32_t words[4] = {raw[k].x, raw[k].y, raw[k].z, raw[k].w};
+#pragma unroll
+        for (int h = 0; h < 4; ++h) unpack2<C>(words[h], v[k * 8 + 2 * h], v[k * 8 + 2 * h + 1]);
+      }
+    }
+  }
+};
 
 template <typename C, typename T, int AHEAD>
 __global__ void __launch_bounds__(kRowsThreads) read_kernel(const __grid_constant__ KvRowsCall c, RowsPlan p) {
@@ -136,51 +196,138 @@ __global__ void __launch_bounds__(kRowsThreads) read_kernel(const __grid_constan
   const int lane = threadIdx.x % p.lanes, step = kRowsThreads / p.lanes, e = lane * E, n = c.cache.dim - e;
   const int tokens = static_cast<int>(min(static_cast<int64_t>(p.tokens), c.total - token0)), rows = tokens * 2 * c.cache.heads;
   find_places(c, token0, tokens, place);
-  for (int i0 = threadIdx.x / p.lanes; i0 < rows; i0 += AHEAD * step) {
-    float v[AHEAD][E];
-    T *out[AHEAD];
+  RowsWalk w(threadIdx.x / p.lanes, step, 2 * c.cache.heads);
+  for (int i = threadIdx.x / p.lanes; i < rows; i += AHEAD * step) {
+    CachedRow<C> x[AHEAD];
+    int token[AHEAD], at[AHEAD];
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
-      const int i = i0 + a * step;
-      if (i >= rows) break;
-      // values after all of the keys: each tensor is written in order
-      const int which = i >= tokens * c.cache.heads, j = i - which * tokens * c.cache.heads, token = j / c.cache.heads, head = j - token * c.cache.heads;
-      const int64_t at = place[token], row = at < 0 ? -1 : at + static_cast<int64_t>(head) * c.cache.page_size;
-      out[a] = static_cast<T *>(which ? c.v_out : c.k_out) + ((token0 + token) * c.cache.heads + head) * c.cache.dim + e;
-      const C *x = static_cast<const C *>(which ? c.cache.v : c.cache.k) + (row < 0 ? 0 : row * c.cache.ld + e);
-      if constexpr (sizeof(C) == 1) {
-        const float scale = row < 0 ? 0.0f : (which ? c.cache.v_scale : c.cache.k_scale)[row];
-        uint2 w = make_uint2(0, 0);
-        if (row >= 0 && n >= E) {
-          w = *reinterpret_cast<const uint2 *>(x);
-        } else if (row >= 0) {
-#pragma unroll
-          for (int k = 0; k < E; ++k)
-            if (k < n) (k < 4 ? w.x : w.y) |= static_cast<uint32_t>(static_cast<uint8_t>(x[k])) << (k % 4 * 8);
-        }
-#pragma unroll
-        for (int k = 0; k < E; ++k) v[a][k] = __fmul_rn(static_cast<float>(static_cast<int8_t>((k < 4 ? w.x : w.y) >> (k % 4 * 8))), scale);
-      } else {
-        load_row<C>(x, row < 0 ? 0 : n, true, v[a]);
-      }
+      token[a] = w.token, at[a] = w.at;
+      w.next();
+      const bool values = at[a] >= c.cache.heads;
+      const int64_t first = token[a] < tokens ? place[token[a]] : -1, row = first + static_cast<int64_t>(values ? at[a] - c.cache.heads : at[a]) * c.cache.page_size;
+      x[a].load(static_cast<const C *>(values ? c.cache.v : c.cache.k) + (row * c.cache.ld + e), first < 0 ? 0 : n, (values ? c.cache.v_scale : c.cache.k_scale) + row);
     }
 #pragma unroll
-    for (int a = 0; a < AHEAD; ++a)
-      if (i0 + a * step < rows) store_row<T>(out[a], n, p.wide, v[a]);
+    for (int a = 0; a < AHEAD; ++a) {
+      if (token[a] >= tokens) break;
+      const bool values = at[a] >= c.cache.heads;
+      T *out = static_cast<T *>(values ? c.v_out : c.k_out) + (((token0 + token[a]) * c.cache.heads + (values ? at[a] - c.cache.heads : at[a])) * c.cache.dim + e);
+      float v[E];
+      x[a].numbers(v);
+      store_row<T>(out, n, v);
+    }
   }
 }
 
+// The same where the rows that come out do not lie on 16 bytes: they follow one another, so that those of a pass go through shared memory, kept there as far
+// from a 16-byte border as in the output, and out in pieces of 16 bytes (one element at a time: 61 us for 70 MB).
+template <typename C, typename T, int AHEAD>
+__global__ void __launch_bounds__(kRowsThreads) read_through_kernel(const __grid_constant__ KvRowsCall c, RowsPlan p) {
+  extern __shared__ int64_t place[];
+  __shared__ __align__(16) T buf[AHEAD * kRowsThreads * E + kVec<T>];  // (a lane's E elements, and the border)
+  const int64_t token0 = static_cast<int64_t>(blockIdx.x) * p.tokens;
+  const int lane = threadIdx.x % p.lanes, group = threadIdx.x / p.lanes, step = kRowsThreads / p.lanes, e = lane * E, n = c.cache.dim - e;
+  const int tokens = static_cast<int>(min(static_cast<int64_t>(p.tokens), c.total - token0)), rows = tokens * c.cache.heads;
+  find_places(c, token0, tokens, place);
+  for (int values = 0; values < 2; ++values) {
+    const C *from = static_cast<const C *>(values ? c.cache.v : c.cache.k);
+    const float *scales = values ? c.cache.v_scale : c.cache.k_scale;
+    for (int i = 0; i < rows; i += AHEAD * step) {
+      CachedRow<C> x[AHEAD];
+#pragma unroll
+      for (int a = 0; a < AHEAD; ++a) {
+        const int r = i + group + a * step, token = r / c.cache.heads, head = r - token * c.cache.heads;
+        const int64_t first = r < rows ? place[token] : -1, row = first + static_cast<int64_t>(head) * c.cache.page_size;
+        x[a].load(from + (row * c.cache.ld + e), first < 0 ? 0 : n, scales + row);
+      }
+      T *out = static_cast<T *>(values ? c.v_out : c.k_out) + (token0 * c.cache.heads + i) * c.cache.dim;
+      const int off = static_cast<int>((reinterpret_cast<uintptr_t>(out) & 15u) / sizeof(T)), count = min(rows - i, AHEAD * step) * c.cache.dim;
+#pragma unroll
+      for (int a = 0; a < AHEAD; ++a) {
+        float v[E];
+        x[a].numbers(v);
+        T *to = buf + off + (group + a * step) * c.cache.dim + e;
+#pragma unroll
+        for (int k = 0; k < E; ++k)
+          if (k < n) to[k] = from_f32<T>(v[k]);
+      }
+      __syncthreads();
+      constexpr int V = kVec<T>;
+      for (int q = threadIdx.x * V; q < off + count; q += kRowsThreads * V) {
+        if (q >= off && q + V <= off + count) {
+          *reinterpret_cast<uint4 *>(out + (q - off)) = *reinterpret_cast<const uint4 *>(buf + q);
+        } else {
+#pragma unroll
+          for (int k = 0; k < V; ++k)
+            if (q + k >= off && q + k < off + count) out[q - off + k] = buf[q + k];
+        }
+      }
+      __syncthreads();
+    }
+  }
+}
+
+// kv_append where the rows that come in do not lie on 16 bytes: a warp to a row, lanes take neighbouring elements.
+constexpr int kStrided = kCacheMaxDim / 32;  // elements of a row to a lane
+template <typename T, typename C, int AHEAD>
+__global__ void __launch_bounds__(kRowsThreads) append_strided_kernel(const __grid_constant__ KvRowsCall c, RowsPlan p) {
+  extern __shared__ int64_t place[];
+  const int64_t token0 = static_cast<int64_t>(blockIdx.x) * p.tokens;
+  constexpr int step = kRowsThreads / 32;
+  const int lane = threadIdx.x % 32, steps = (c.cache.dim + 31) / 32;
+  const int tokens = static_cast<int>(min(static_cast<int64_t>(p.tokens), c.total - token0)), rows = tokens * 2 * c.cache.heads;
+  RowsWalk w(threadIdx.x / 32, step, 2 * c.cache.heads);
+  for (int i = 0; i < rows; i += AHEAD * step) {
+    float v[AHEAD][kStrided];
+    int token[AHEAD], at[AHEAD];
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      token[a] = w.token, at[a] = w.at;
+      w.next();
+      const bool values = at[a] >= c.cache.heads;
+      const int64_t r = token0 + token[a];
+      const T *x = values ? static_cast<const T *>(c.v) + (r * c.v_row + (at[a] - c.cache.heads) * c.v_head) : static_cast<const T *>(c.k) + (r * c.k_row + at[a] * c.k_head);
+#pragma unroll
+      for (int k = 0; k < kStrided; ++k) v[a][k] = k < steps && token[a] < tokens && lane + k * 32 < c.cache.dim ? to_f32(x[lane + k * 32]) : 0.0f;
+    }
+    if (i == 0) find_places(c, token0, tokens, place);
+#pragma unroll
+    for (int a = 0; a < AHEAD; ++a) {
+      const bool values = at[a] >= c.cache.heads;
+      const int64_t first = token[a] < tokens ? place[token[a]] : -1, row = first + static_cast<int64_t>(values ? at[a] - c.cache.heads : at[a]) * c.cache.page_size;
+      C *out = static_cast<C *>(values ? c.cache.v : c.cache.k) + row * c.cache.ld;
+      float by = 1.0f;
+      if constexpr (sizeof(C) == 1) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int k = 0; k < kStrided; ++k) m = max(m, __float_as_uint(v[a][k]) & 0x7fffffffu);
+        for (int o = 16; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
+        const float alpha = __uint_as_float(max(m, __float_as_uint(kAlphaMin)));
+        by = __fdiv_rn(127.0f, alpha);
+        if (lane == 0 && first >= 0) (values ? c.cache.v_scale : c.cache.k_scale)[row] = scale_of(alpha);
+      }
+#pragma unroll
+      for (int k = 0; k < kStrided; ++k) {
+        if (k >= steps) break;
+        if (first < 0 || lane + k * 32 >= c.cache.dim) continue;
+        if constexpr (sizeof(C) == 1) out[lane + k * 32] = static_cast<int8_t>(__float_as_uint(__fmul_rn(v[a][k], by) + 12582912.0f));
+        else out[lane + k * 32] = from_f32<C>(v[a][k]);
+      }
+    }
+  }
+}
 // One wave of four CTAs to an SM, each with a share of the tokens: finding their places is a chain of three trips to L2 (with 4 tokens to a CTA, 4,500 CTAs
 // of them, 18,000 prompt tokens took 77 us).  Few tokens: a CTA to each pass over its lanes.
 template <class F>
 cudaError_t plan_rows(const KvRowsCall &c, bool wide, F &&launch) {
-  RowsPlan p = {1, 1, wide};
-  while (p.lanes * E < c.cache.dim) p.lanes *= 2;
+  RowsPlan p = {1, 1};
+  while (p.lanes < 32 && (!wide || p.lanes * E < c.cache.dim)) p.lanes *= 2;
   const int64_t groups = kRowsThreads / p.lanes, rows = 2 * static_cast<int64_t>(c.cache.heads), ctas = 4 * static_cast<int64_t>(sm_count());
   int64_t tokens = (c.total + ctas - 1) / ctas;
   if (tokens * rows < groups) tokens = groups / rows;
   p.tokens = static_cast<int>(tokens < 1 ? 1 : tokens > kMaxTokens ? kMaxTokens : tokens);
-  launch(static_cast<unsigned>((c.total + p.tokens - 1) / p.tokens), p, static_cast<size_t>(p.tokens) * sizeof(int64_t), p.tokens * rows >= 4 * groups);
+  launch(static_cast<unsigned>((c.total + p.tokens - 1) / p.tokens), p, static_cast<size_t>(p.tokens) * sizeof(int64_t), p.tokens * rows >= kAhead * groups);
   return cudaGetLastError();
 }
 
@@ -191,16 +338,18 @@ bool in_pieces(const void *k, const void *v, int64_t a, int64_t b, int64_t x, in
 
 template <typename T, typename C>
 cudaError_t append_of(const KvRowsCall &c, cudaStream_t st) {
-  return plan_rows(c, in_pieces(c.k, c.v, c.k_row, c.k_head, c.v_row, c.v_head, 0, sizeof(T)), [&](unsigned grid, const RowsPlan &p, size_t smem, bool many) {
-    if (many) append_kernel<T, C, 4><<<grid, kRowsThreads, smem, st>>>(c, p);
-    else append_kernel<T, C, 1><<<grid, kRowsThreads, smem, st>>>(c, p);
+  const bool wide = in_pieces(c.k, c.v, c.k_row, c.k_head, c.v_row, c.v_head, 0, sizeof(T));
+  return plan_rows(c, wide, [&](unsigned grid, const RowsPlan &p, size_t smem, bool many) {
+    const auto kernel = wide ? (many ? append_kernel<T, C, kAhead> : append_kernel<T, C, 1>) : many ? append_strided_kernel<T, C, 2 * kAhead> : append_strided_kernel<T, C, 1>;
+    kernel<<<grid, kRowsThreads, smem, st>>>(c, p);
   });
 }
 template <typename C, typename T>
 cudaError_t read_of(const KvRowsCall &c, cudaStream_t st) {
-  return plan_rows(c, in_pieces(c.k_out, c.v_out, 0, 0, 0, 0, c.cache.dim, sizeof(T)), [&](unsigned grid, const RowsPlan &p, size_t smem, bool many) {
-    if (many) read_kernel<C, T, 4><<<grid, kRowsThreads, smem, st>>>(c, p);
-    else read_kernel<C, T, 1><<<grid, kRowsThreads, smem, st>>>(c, p);
+  const bool wide = in_pieces(c.k_out, c.v_out, 0, 0, 0, 0, c.cache.dim, sizeof(T));
+  return plan_rows(c, true, [&](unsigned grid, const RowsPlan &p, size_t smem, bool many) {
+    const auto kernel = wide ? (many ? read_kernel<C, T, kAhead> : read_kernel<C, T, 1>) : many ? read_through_kernel<C, T, kAhead> : read_through_kernel<C, T, 1>;
+    kernel<<<grid, kRowsThreads, smem, st>>>(c, p);
   });
 }
 template <typename C>
