@@ -509,8 +509,9 @@ struct AttendWarp {
     }
   }
 
-  // The last tile of a piece: maxima, sums over the keys and rows that belong to them (in units of 2^top).  f(head, element, value of a
-  // row) takes the rows, s(head, top, l) the rest; l is the whole sum in every lane.
+  static constexpr int EL = DP / 8 < 16 / S::kSize ? DP / 8 : 16 / S::kSize;  // elements that a lane has of a row side by side
+  // The last tile of a piece: maxima, sums over the keys and rows that belong to them (in units of 2^top).  f(head, number of the lane's head,
+  // element, EL values from there on) takes the rows, s(head, number, top, l) the rest; l is the whole sum in every lane.
   template <class F, class G>
   __device__ void end(F &&f, G &&s) {
     float by[HC];
@@ -524,16 +525,19 @@ struct AttendWarp {
       const int head = P == 2 ? hc * 4 + t : hc / 2 * 8 + 2 * t + hc % 2;
       s(head, hc, top[hc], l[hc]);
     }
-    constexpr int EL = DP / 8 < 16 / S::kSize ? DP / 8 : 16 / S::kSize;  // elements of a lane's piece of a value
 #pragma unroll
-    for (int m = 0; m < DP / 16; ++m) {
-      const int e = 8 * EL * (2 * m / EL) + EL * g + 2 * m % EL;
+    for (int hc = 0; hc < HC; ++hc) {
+      const int head = P == 2 ? hc * 4 + t : hc / 2 * 8 + 2 * t + hc % 2;
 #pragma unroll
-      for (int hc = 0; hc < HC; ++hc) {
-        const int head = P == 2 ? hc * 4 + t : hc / 2 * 8 + 2 * t + hc % 2;
-        const float *v = o[m][hc / (3 - P)];
-        f(head, hc, e, (P == 2 ? v[0] + v[1] : v[hc % 2]) * by[hc]);
-        f(head, hc, e + 1, (P == 2 ? v[2] + v[3] : v[2 + hc % 2]) * by[hc]);
+      for (int m0 = 0; m0 < DP / 16; m0 += EL / 2) {
+        float row[EL];
+#pragma unroll
+        for (int i = 0; i < EL / 2; ++i) {
+          const float *v = o[m0 + i][hc / (3 - P)];
+          row[2 * i] = (P == 2 ? v[0] + v[1] : v[hc % 2]) * by[hc];
+          row[2 * i + 1] = (P == 2 ? v[2] + v[3] : v[2 + hc % 2]) * by[hc];
+        }
+        f(head, hc, 16 * m0 + EL * g, row);
       }
     }
   }
@@ -543,6 +547,28 @@ __device__ __forceinline__ void store_out(const AttendArgs &a, int64_t at, float
   if (a.dtype == 0) static_cast<float *>(a.out)[at] = v;
   else if (a.dtype == 1) static_cast<__half *>(a.out)[at] = from_f32<__half>(v);
   else static_cast<__nv_bfloat16 *>(a.out)[at] = from_f32<__nv_bfloat16>(v);
+}
+// N results side by side, in pieces of 16 bytes where rows of the output lie on them (single stores of 32 lanes' results, none of them next to each other,
+// were most of the time of short sequences)
+template <int N>
+__device__ __forceinline__ void store_outs(const AttendArgs &a, int64_t row, int e, const float (&v)[N]) {
+  const int64_t at = row * a.cache.dim + e;
+  const auto pieces = [&](auto *p) {
+    using T = std::remove_reference_t<decltype(*p)>;
+    if constexpr (N % kVec<T> == 0) {
+      if (((reinterpret_cast<uintptr_t>(p) | a.cache.dim * sizeof(T)) & 15u) == 0 && e + N <= a.cache.dim) {
+#pragma unroll
+        for (int i = 0; i < N; i += kVec<T>) store_v<T, kVec<T>>(p + at + i, v + i);
+        return;
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (e + i < a.cache.dim) p[at + i] = from_f32<T>(v[i]);
+  };
+  if (a.dtype == 0) pieces(static_cast<float *>(a.out));
+  else if (a.dtype == 1) pieces(static_cast<__half *>(a.out));
+  else pieces(static_cast<__nv_bfloat16 *>(a.out));
 }
 // a row's share, of what its keys' weights add up to: nothing where no key was there
 __device__ __forceinline__ float share(float v, float l) { return l == 0.0f ? 0.0f : __fdiv_rn(v, l); }
@@ -663,8 +689,10 @@ __global__ void __launch_bounds__(S::kWarps * 32, S::kCtas) attend_kernel(const 
           const int64_t head0 = static_cast<int64_t>(at.b) * a.q_heads + at.j / a.parts * a.group + part * H;
           float inv[Warp::HC];
           w.end(
-              [&](int head, int hc, int e, float v) {
-                if (head < heads && e < a.cache.dim) store_out(a, (head0 + head) * a.cache.dim + e, v * inv[hc]);
+              [&](int head, int hc, int e, float (&v)[Warp::EL]) {
+#pragma unroll
+                for (int k = 0; k < Warp::EL; ++k) v[k] *= inv[hc];
+                if (head < heads) store_outs(a, head0 + head, e, v);
               },
               [&](int head, int hc, float top, float l) {
                 inv[hc] = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
@@ -674,7 +702,11 @@ __global__ void __launch_bounds__(S::kWarps * 32, S::kCtas) attend_kernel(const 
           __syncwarp();
           // (a piece that begins here lasts to the end of this warp's tiles: its place is the ring, where nothing is left to come)
           float *to = starts ? reinterpret_cast<float *>(rings + warp * (S::kStages * S::kStage)) : heads_of_parts + warp * S::kPart;
-          w.end([&](int head, int, int e, float v) { to[2 * H + head * DP + e] = v; },
+          w.end(
+              [&](int head, int, int e, const float (&v)[Warp::EL]) {
+#pragma unroll
+                for (int k = 0; k < Warp::EL; k += 4) *reinterpret_cast<float4 *>(to + 2 * H + head * DP + e + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+              },
                 [&](int head, int, float top, float l) {
                   if (w.g == 0) to[head] = top, to[H + head] = l;
                 });
@@ -756,8 +788,8 @@ __global__ void __launch_bounds__(S::kWarps * 32, S::kCtas) attend_kernel(const 
     if (slot == 1 && p.ends) {
       const int64_t at = static_cast<int64_t>(p.b) * a.q_heads + p.j / a.parts * a.group + part * H + head;
 #pragma unroll
-      for (int k = 0; k < 4; ++k)
-        if (e + k < a.cache.dim) store_out(a, at * a.cache.dim + e + k, share(v[k], l));
+      for (int k = 0; k < 4; ++k) v[k] = share(v[k], l);
+      store_outs(a, at, e, v);
       if (e == 0 && a.lse) a.lse[at] = lse_of(top, l);
     } else {
       float *to = a.partial + (blockIdx.x * 2 + slot) * static_cast<int64_t>(S::kPart);
