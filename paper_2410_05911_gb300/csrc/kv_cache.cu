@@ -41,6 +41,27 @@ __device__ __forceinline__ void load_row(const T *x, int n, float (&v)[E]) {
     }
   }
 }
+// the same from anywhere: by whole words, two 16-bit elements each, shifted into place where the first is the second of its word (single
+// elements, a warp to a row: 65 us for 18,000 tokens of 8 heads of 77)
+template <typename T>
+__device__ __forceinline__ void load_row_anywhere(const T *x, int n, float (&v)[E]) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < E; ++i) v[i] = i < n ? x[i] : 0.0f;
+  } else {
+    const int odd = static_cast<int>(reinterpret_cast<uintptr_t>(x) >> 1 & 1);
+    const uint32_t *from = reinterpret_cast<const uint32_t *>(reinterpret_cast<uintptr_t>(x) & ~uintptr_t(3));
+    uint32_t w[E / 2 + 1];
+#pragma unroll
+    for (int i = 0; i <= E / 2; ++i) w[i] = 2 * i - odd < n && (i < E / 2 || odd) ? from[i] : 0;  // (words with an element of the row)
+#pragma unroll
+    for (int i = 0; i < E / 2; ++i) {
+      float a, b;
+      unpack2<T>(__funnelshift_r(w[i], w[i + 1], odd * 16), a, b);
+      v[2 * i] = 2 * i < n ? a : 0.0f, v[2 * i + 1] = 2 * i + 1 < n ? b : 0.0f;
+    }
+  }
+}
 template <typename T>
 __device__ __forceinline__ void store_row(T *x, int n, const float (&v)[E]) {
 #pragma unroll
@@ -93,7 +114,7 @@ __device__ __forceinline__ void find_places(const KvRowsCall &c, int64_t token0,
 }
 
 // A CTA takes `tokens` tokens, all heads, keys and values.
-template <typename T, typename C, int AHEAD>
+template <typename T, typename C, int AHEAD, bool WIDE>
 __global__ void __launch_bounds__(kRowsThreads) append_kernel(const __grid_constant__ KvRowsCall c, RowsPlan p) {
   extern __shared__ int64_t place[];
   const int64_t token0 = static_cast<int64_t>(blockIdx.x) * p.tokens;
@@ -110,7 +131,8 @@ __global__ void __launch_bounds__(kRowsThreads) append_kernel(const __grid_const
       const bool values = at[a] >= c.cache.heads;
       const int64_t r = token0 + token[a];
       const T *x = values ? static_cast<const T *>(c.v) + (r * c.v_row + (at[a] - c.cache.heads) * c.v_head) : static_cast<const T *>(c.k) + (r * c.k_row + at[a] * c.k_head);
-      load_row<T>(x + e, token[a] < tokens ? n : 0, v[a]);
+      if constexpr (WIDE) load_row<T>(x + e, token[a] < tokens ? n : 0, v[a]);
+      else load_row_anywhere<T>(x + e, token[a] < tokens ? n : 0, v[a]);
     }
     if (i == 0) find_places(c, token0, tokens, place);  // (beside the first rows' loads)
 #pragma unroll
@@ -268,61 +290,12 @@ __global__ void __launch_bounds__(kRowsThreads) read_through_kernel(const __grid
   }
 }
 
-// kv_append where the rows that come in do not lie on 16 bytes: a warp to a row, lanes take neighbouring elements.
-constexpr int kStrided = kCacheMaxDim / 32;  // elements of a row to a lane
-template <typename T, typename C, int AHEAD>
-__global__ void __launch_bounds__(kRowsThreads) append_strided_kernel(const __grid_constant__ KvRowsCall c, RowsPlan p) {
-  extern __shared__ int64_t place[];
-  const int64_t token0 = static_cast<int64_t>(blockIdx.x) * p.tokens;
-  constexpr int step = kRowsThreads / 32;
-  const int lane = threadIdx.x % 32, steps = (c.cache.dim + 31) / 32;
-  const int tokens = static_cast<int>(min(static_cast<int64_t>(p.tokens), c.total - token0)), rows = tokens * 2 * c.cache.heads;
-  RowsWalk w(threadIdx.x / 32, step, 2 * c.cache.heads);
-  for (int i = 0; i < rows; i += AHEAD * step) {
-    float v[AHEAD][kStrided];
-    int token[AHEAD], at[AHEAD];
-#pragma unroll
-    for (int a = 0; a < AHEAD; ++a) {
-      token[a] = w.token, at[a] = w.at;
-      w.next();
-      const bool values = at[a] >= c.cache.heads;
-      const int64_t r = token0 + token[a];
-      const T *x = values ? static_cast<const T *>(c.v) + (r * c.v_row + (at[a] - c.cache.heads) * c.v_head) : static_cast<const T *>(c.k) + (r * c.k_row + at[a] * c.k_head);
-#pragma unroll
-      for (int k = 0; k < kStrided; ++k) v[a][k] = k < steps && token[a] < tokens && lane + k * 32 < c.cache.dim ? to_f32(x[lane + k * 32]) : 0.0f;
-    }
-    if (i == 0) find_places(c, token0, tokens, place);
-#pragma unroll
-    for (int a = 0; a < AHEAD; ++a) {
-      const bool values = at[a] >= c.cache.heads;
-      const int64_t first = token[a] < tokens ? place[token[a]] : -1, row = first + static_cast<int64_t>(values ? at[a] - c.cache.heads : at[a]) * c.cache.page_size;
-      C *out = static_cast<C *>(values ? c.cache.v : c.cache.k) + row * c.cache.ld;
-      float by = 1.0f;
-      if constexpr (sizeof(C) == 1) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int k = 0; k < kStrided; ++k) m = max(m, __float_as_uint(v[a][k]) & 0x7fffffffu);
-        for (int o = 16; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
-        const float alpha = __uint_as_float(max(m, __float_as_uint(kAlphaMin)));
-        by = __fdiv_rn(127.0f, alpha);
-        if (lane == 0 && first >= 0) (values ? c.cache.v_scale : c.cache.k_scale)[row] = scale_of(alpha);
-      }
-#pragma unroll
-      for (int k = 0; k < kStrided; ++k) {
-        if (k >= steps) break;
-        if (first < 0 || lane + k * 32 >= c.cache.dim) continue;
-        if constexpr (sizeof(C) == 1) out[lane + k * 32] = static_cast<int8_t>(__float_as_uint(__fmul_rn(v[a][k], by) + 12582912.0f));
-        else out[lane + k * 32] = from_f32<C>(v[a][k]);
-      }
-    }
-  }
-}
 // One wave of four CTAs to an SM, each with a share of the tokens: finding their places is a chain of three trips to L2 (with 4 tokens to a CTA, 4,500 CTAs
 // of them, 18,000 prompt tokens took 77 us).  Few tokens: a CTA to each pass over its lanes.
 template <class F>
-cudaError_t plan_rows(const KvRowsCall &c, bool wide, F &&launch) {
+cudaError_t plan_rows(const KvRowsCall &c, F &&launch) {
   RowsPlan p = {1, 1};
-  while (p.lanes < 32 && (!wide || p.lanes * E < c.cache.dim)) p.lanes *= 2;
+  while (p.lanes * E < c.cache.dim) p.lanes *= 2;
   const int64_t groups = kRowsThreads / p.lanes, rows = 2 * static_cast<int64_t>(c.cache.heads), ctas = 4 * static_cast<int64_t>(sm_count());
   int64_t tokens = (c.total + ctas - 1) / ctas;
   if (tokens * rows < groups) tokens = groups / rows;
@@ -339,15 +312,16 @@ bool in_pieces(const void *k, const void *v, int64_t a, int64_t b, int64_t x, in
 template <typename T, typename C>
 cudaError_t append_of(const KvRowsCall &c, cudaStream_t st) {
   const bool wide = in_pieces(c.k, c.v, c.k_row, c.k_head, c.v_row, c.v_head, 0, sizeof(T));
-  return plan_rows(c, wide, [&](unsigned grid, const RowsPlan &p, size_t smem, bool many) {
-    const auto kernel = wide ? (many ? append_kernel<T, C, kAhead> : append_kernel<T, C, 1>) : many ? append_strided_kernel<T, C, 2 * kAhead> : append_strided_kernel<T, C, 1>;
+  return plan_rows(c, [&](unsigned grid, const RowsPlan &p, size_t smem, bool many) {
+    const auto kernel = wide ? (many ? append_kernel<T, C, kAhead, true> : append_kernel<T, C, 1, true>)
+                             : many ? append_kernel<T, C, kAhead, false> : append_kernel<T, C, 1, false>;
     kernel<<<grid, kRowsThreads, smem, st>>>(c, p);
   });
 }
 template <typename C, typename T>
 cudaError_t read_of(const KvRowsCall &c, cudaStream_t st) {
   const bool wide = in_pieces(c.k_out, c.v_out, 0, 0, 0, 0, c.cache.dim, sizeof(T));
-  return plan_rows(c, true, [&](unsigned grid, const RowsPlan &p, size_t smem, bool many) {
+  return plan_rows(c, [&](unsigned grid, const RowsPlan &p, size_t smem, bool many) {
     const auto kernel = wide ? (many ? read_kernel<C, T, kAhead> : read_kernel<C, T, 1>) : many ? read_through_kernel<C, T, kAhead> : read_through_kernel<C, T, 1>;
     kernel<<<grid, kRowsThreads, smem, st>>>(c, p);
   });
