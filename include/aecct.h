@@ -394,8 +394,8 @@ int aecct_kv_read(const aecct_kv_cache *cache, const aecct_kv_sequences *seqs, c
  *   first  DEVICE [batch], or NULL: from position 0.
  *   out    [batch][q_heads][head_dim] of dtype;  lse  fp32 [batch][q_heads] or NULL.
  * A sequence with no position to attend to gets zeros, and an lse of minus infinity.  Scales of rows of codes are positive (those of
- * aecct_kv_append are).  Sums, maxima and the softmax are in 32 bits, in an order that hangs on the lengths of the whole batch and
- * on nothing else.
+ * aecct_kv_append are).  Sums, maxima and the softmax are in 32 bits, in an order that hangs on the sizes of the call and on the
+ * lengths of the whole batch, and on nothing else.
  *   workspace  aecct_paged_attention_workspace bytes, 16-byte aligned; not read before it is written.
  * Errors: as above, and INVALID_ARG where heads does not divide q_heads, scale is not finite or the workspace is too small. */
 int aecct_paged_attention_workspace(int32_t batch, int32_t q_heads, int32_t heads, int32_t head_dim, int32_t dtype,

@@ -89,7 +89,7 @@ __global__ void __launch_bounds__(kJoinThreads) attend_join_kernel(const __grid_
   if (tid == 0 && a.lse) a.lse[at] = lse_of(top, l);
 }
 
-// One piece of 16 bits for a weight is under the rounding of a bfloat16 result (2^-12 of it and 2^-9, each at most half a step); a
+// One piece of 16 bits for a weight is under the rounding of a bfloat16 result (2^-11 of it and 2^-8, each at most half a step); a
 // half or float result takes two, and so does a cache in bfloat16, whose weights have that type's 8 bits.
 cudaError_t run(int dim, int group, int dtype, int cache_dtype, const AttendArgs *a, AttendPlan *plan, cudaStream_t st) {
   if (cache_dtype == 1) return run_attend_half(dim, group, a, plan, st);
@@ -112,9 +112,15 @@ cudaError_t launch_attend(const AttendCall &c, cudaStream_t st) {
   AttendPlan p = {};
   run(c.cache.dim, group, c.dtype, c.cache_dtype, nullptr, &p, st);
   AttendArgs a = {c.cache, c.seqs, c.first, c.q, c.ld_row, c.ld_head, group, c.q_heads, c.dtype, (group + p.heads - 1) / p.heads, c.scale * kLog2e, c.out,
-                  c.lse, static_cast<float *>(c.workspace), reinterpret_cast<AttendPiece *>(static_cast<char *>(c.workspace) + piece_bytes(p))};
+                  c.lse, static_cast<float *>(c.workspace), reinterpret_cast<AttendPiece *>(static_cast<char *>(c.workspace) + piece_bytes(p)), 0};
+  // A cluster to each piece where all run at once and no warp has more than 4 tiles, as far as the table says: the most CTAs that have a tile for
+  // each warp.  (Beyond that, the longest sequence would have its cluster work while others are done.)
+  const int64_t pieces = static_cast<int64_t>(c.seqs.batch) * c.cache.heads * a.parts;
+  const int64_t tiles = (static_cast<int64_t>(c.seqs.columns) * c.cache.page_size + p.tile - 1) / p.tile;
+  for (int i = 0; i < 4; ++i)
+    if (pieces <= p.at_once[i] && tiles <= 4 * static_cast<int64_t>(p.warps << i) && (i == 0 || tiles > p.warps << (i - 1))) a.ctas = 1 << i;
   const cudaError_t e = run(c.cache.dim, group, c.dtype, c.cache_dtype, &a, &p, st);
-  if (e != cudaSuccess) return e;
+  if (e != cudaSuccess || a.ctas > 0) return e;
   return launch_dependent(attend_join_kernel, dim3(p.ctas, p.heads), kJoinThreads, 0, st, a, p);
 }
 

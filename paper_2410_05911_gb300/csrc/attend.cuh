@@ -27,6 +27,7 @@
 #pragma once
 #include <cuda_runtime.h>
 
+#include <atomic>
 #include <cmath>
 #include <cstdint>
 
@@ -56,6 +57,7 @@ struct AttendArgs {
   float *lse;
   float *partial;      // [CTAs][2][kPart]
   AttendPiece *piece;  // [CTAs][2]
+  int ctas;            // of a cluster that takes one piece of heads of one sequence; 0: tiles are dealt out
 };
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -806,14 +808,155 @@ __global__ void __launch_bounds__(S::kWarps * 32, S::kCtas) attend_kernel(const 
   if (tid < 2 && !noted[tid]) a.piece[blockIdx.x * 2 + tid] = {-1, 0, 0, 0};
 }
 
+// Few and short sequences: a cluster of CTAs to each piece of heads of each of them, whose parts are joined through distributed shared memory.  No list, no
+// second kernel: one request of 500 tokens 8 us instead of 11.
+template <class S>
+__global__ void __launch_bounds__(S::kWarps * 32, S::kCtas) attend_whole_kernel(const __grid_constant__ AttendArgs a) {
+  constexpr int NT = S::kWarps * 32, W = S::kWarps, DP = S::DP, H = S::kHeads;
+  using Warp = AttendWarp<S>;
+  extern __shared__ __align__(16) unsigned char smem[];
+  float *factors = reinterpret_cast<float *>(smem);  // [W][H]
+  float *sum = factors + W * H;                      // [kPart]: maxima, sums and rows of this CTA's parts together
+  unsigned char *rings = smem + S::kFixed;
+  static_assert((W * H + S::kPart) * 4 <= S::kFixed, "room before the rings");
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int ctas = a.ctas, rank = ctas > 1 ? static_cast<int>(cluster_ctarank()) : 0, all = a.cache.heads * a.parts;
+  typename Warp::Cursor at = {};
+  at.b = blockIdx.x / ctas / all, at.j = blockIdx.x / ctas % all;
+  Warp w(a, smem_u32(rings + warp * (S::kStages * S::kStage)));
+  w.sequence(at);
+  const int per_cta = (at.tiles + ctas - 1) / ctas, from = min(at.tiles, rank * per_cta), count = min(at.tiles, from + per_cta) - from;
+  const int per = (count + W - 1) / W, used = per > 0 ? (count + per - 1) / per : 0;  // tiles of a warp, and warps that have some
+  const int n = warp < used ? min(per, count - warp * per) : 0;
+  at.tile = from + warp * per;
+  const int part = at.j % a.parts, heads = min(H, a.group - part * H);
+  const int64_t head0 = static_cast<int64_t>(at.b) * a.q_heads + at.j / a.parts * a.group + part * H;
+  if (n > 0) {
+    typename Warp::Cursor next = at;
+    int page, place, filled = 0;
+    w.find(next, page, place);
+    const auto fill = [&]() {
+      if (filled < n) {
+        w.fill(filled % S::kStages, next, page, place);
+        if (++filled < n) ++next.tile, w.find(next, page, place);
+      }
+      copies_commit();
+    };
+    for (int i = 0; i < S::kStages - 1; ++i) fill();
+    w.begin(at);
+#pragma unroll 1
+    for (int i = 0; i < n; ++i) {
+      copies_wait<S::kStages - 2>();
+      __syncwarp();
+      fill();
+      w.tile(i % S::kStages);
+    }
+    __syncwarp();
+    float *to = reinterpret_cast<float *>(rings + warp * (S::kStages * S::kStage));  // (nothing is left to come there)
+    w.end(
+        [&](int head, int, int e, const float (&v)[Warp::EL]) {
+#pragma unroll
+          for (int k = 0; k < Warp::EL; k += 4) *reinterpret_cast<float4 *>(to + 2 * H + head * DP + e + k) = make_float4(v[k], v[k + 1], v[k + 2], v[k + 3]);
+        },
+        [&](int head, int, float top, float l) {
+          if (w.g == 0) to[head] = top, to[H + head] = l;
+        });
+  }
+  __syncthreads();
+  const auto part_of = [&](int v) { return reinterpret_cast<const float *>(rings + v * (S::kStages * S::kStage)); };
+  for (int h0 = warp * (32 / W); h0 < heads; h0 += 32) {  // W lanes to a head, one to each part
+    const int h = h0 + lane / W, v = lane % W;
+    const bool on = v < used && h < H;
+    const float mine = on ? part_of(v)[h] : -INFINITY;
+    float top = mine;
+    for (int o = W / 2; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, o));
+    const float by = on ? exp2_fast(mine - (top == -INFINITY ? 0.0f : top)) : 0.0f;
+    float l = on ? part_of(v)[H + h] * by : 0.0f;
+    for (int o = W / 2; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    if (h < H) factors[v * H + h] = by;
+    if (h < H && v == 0) sum[h] = top, sum[H + h] = l;
+  }
+  __syncthreads();
+  const auto out = [&](int head, int e, float (&v)[4], float top, float l) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) v[k] = share(v[k], l);
+    store_outs(a, head0 + head, e, v);
+    if (e == 0 && a.lse) a.lse[head0 + head] = lse_of(top, l);
+  };
+  for (int i = tid; i < heads * (DP / 4); i += NT) {
+    const int head = i / (DP / 4), e = i % (DP / 4) * 4;
+    float v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 4
+    for (int k = 0; k < used; ++k) {
+      const float by = factors[k * H + head];
+      const float4 x = *reinterpret_cast<const float4 *>(part_of(k) + 2 * H + head * DP + e);
+      v[0] = fmaf(x.x, by, v[0]), v[1] = fmaf(x.y, by, v[1]), v[2] = fmaf(x.z, by, v[2]), v[3] = fmaf(x.w, by, v[3]);
+    }
+    if (ctas == 1) out(head, e, v, sum[head], sum[H + head]);
+    else *reinterpret_cast<float4 *>(sum + 2 * H + head * DP + e) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+  if (ctas == 1) return;
+  cluster_sync_all();
+  const uint32_t sums = smem_u32(sum);
+  for (int i = rank * NT + tid; i < heads * (DP / 4); i += ctas * NT) {
+    const int head = i / (DP / 4), e = i % (DP / 4) * 4;
+    float top = -INFINITY, l = 0.0f, v[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+    for (int r = 0; r < ctas; ++r) top = fmaxf(top, ld_cluster_f32(mapa_cluster(sums + head * 4, r)));
+    const float base = top == -INFINITY ? 0.0f : top;
+    for (int r = 0; r < ctas; ++r) {
+      const float by = exp2_fast(ld_cluster_f32(mapa_cluster(sums + head * 4, r)) - base);
+      const float4 x = ld_cluster_f32x4(mapa_cluster(sums + (2 * H + head * DP + e) * 4, r));
+      l = fmaf(ld_cluster_f32(mapa_cluster(sums + (H + head) * 4, r)), by, l);
+      v[0] = fmaf(x.x, by, v[0]), v[1] = fmaf(x.y, by, v[1]), v[2] = fmaf(x.z, by, v[2]), v[3] = fmaf(x.w, by, v[3]);
+    }
+    out(head, e, v, top, l);
+  }
+  cluster_sync_all();  // (no CTA ends while another one reads its sums)
+}
+
 // a launch of the kernel: the grid that fills the GPU
 struct AttendPlan {
   int ctas, heads, width, part;  // CTAs, query heads of a piece, DP, floats of a piece
+  int tile, warps;               // keys of a tile, warps of a CTA
+  int at_once[4];                // clusters of 1, 2, 4 and 8 CTAs that the GPU holds
 };
 template <class S>
+cudaError_t launch_whole(const AttendArgs &a, int pieces, cudaStream_t st, int *at_once = nullptr) {
+  const cudaError_t e = cudaFuncSetAttribute(attend_whole_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
+  if (e != cudaSuccess) return e;
+  cudaLaunchAttribute attr[1];
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = static_cast<unsigned>(a.ctas), attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+  cudaLaunchConfig_t cfg = {};
+  cfg.gridDim = dim3(static_cast<unsigned>(pieces * a.ctas));
+  cfg.blockDim = dim3(S::kWarps * 32);
+  cfg.dynamicSmemBytes = S::kSmem;
+  cfg.stream = st;
+  cfg.attrs = attr;
+  cfg.numAttrs = 1;
+  if (at_once) return cudaOccupancyMaxActiveClusters(at_once, attend_whole_kernel<S>, &cfg);
+  return cudaLaunchKernelEx(&cfg, attend_whole_kernel<S>, a);
+}
+template <class S>
 cudaError_t run_attend(const AttendArgs *a, AttendPlan *plan, cudaStream_t st) {
-  plan->ctas = sm_count() * S::kCtas, plan->heads = S::kHeads, plan->width = S::DP, plan->part = S::kPart;
-  if (!a) return cudaSuccess;
+  if (!a) {
+    static std::atomic<int> known[64][4];  // by device
+    *plan = {sm_count() * S::kCtas, S::kHeads, S::DP, S::kPart, S::TK, S::kWarps, {}};
+    int device = 0;
+    if (cudaGetDevice(&device) != cudaSuccess || device < 0 || device >= 64) return cudaSuccess;
+    for (int i = 0; i < 4; ++i) {
+      int n = known[device][i].load(std::memory_order_relaxed);
+      if (n == 0) {
+        AttendArgs one = {};
+        one.ctas = 1 << i;
+        if (launch_whole<S>(one, 1, nullptr, &n) != cudaSuccess) n = 0;
+        known[device][i].store(n, std::memory_order_relaxed);
+      }
+      plan->at_once[i] = n;
+    }
+    return cudaSuccess;
+  }
+  if (a->ctas > 0) return launch_whole<S>(*a, a->seqs.batch * a->cache.heads * a->parts, st);
   const cudaError_t e = cudaFuncSetAttribute(attend_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
   if (e != cudaSuccess) return e;
   attend_kernel<S><<<plan->ctas, S::kWarps * 32, S::kSmem, st>>>(*a);
