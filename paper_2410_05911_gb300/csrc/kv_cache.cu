@@ -23,47 +23,71 @@ constexpr float kAlphaMin = 0x1p-100f;
 constexpr int kRowsThreads = 256, kCtas = 4;  // of a CTA; CTAs to an SM
 constexpr int E = 16;  // elements of a row to a lane
 constexpr int kSearched = 1024, kMaxTokens = 512;  // of a CTA
-constexpr int kAhead = 2;  // rows that a lane group has on their way at once, where it has several
+constexpr int kAhead = 2;  // rows that a lane group has on their way at once, where it has several (4 new ones of 16 bits)
 
 struct RowsPlan {
   int lanes, tokens;  // lanes to a row; tokens of a CTA at most
 };
 
-// E elements of a row of dim, from element e on; those past its end are 0.  Rows of 16-byte pieces:
-template <typename T>
-__device__ __forceinline__ void load_row(const T *x, int e, int dim, float (&v)[E]) {
-  constexpr int V = kVec<T>;
+// E elements of a row, of which it has n (none for n <= 0; the others are 0), as they lie there, so that rows on their way take few registers, and as numbers.
+// WIDE: rows of 16-byte pieces.  Else by whole words, two 16-bit elements each, shifted into place where the first is the second of its word (single
+// elements, a warp to a row: 65 us for 19,400 tokens of 8 heads of 77).
+template <typename T, bool WIDE>
+struct NewRow {
+  static constexpr int kWords = E * sizeof(T) / 4 + (!WIDE && sizeof(T) == 2);
+  uint32_t w[kWords];
+  bool odd;
+  __device__ __forceinline__ void load(const T *x, int n) {
+    odd = false;
+    if constexpr (WIDE) {
+      constexpr int V = kVec<T>;
 #pragma unroll
-  for (int i = 0; i < E; i += V) {
-    if (e + i + V <= dim) {
-      load_v<T, V>(x + e + i, v + i);
+      for (int i = 0; i < E / V; ++i) {
+        uint4 q = make_uint4(0, 0, 0, 0);
+        if (n >= (i + 1) * V) {
+          q = reinterpret_cast<const uint4 *>(x)[i];
+        } else if (n > i * V) {  // (a row's last elements)
+          uint32_t part[4] = {0, 0, 0, 0};
+#pragma unroll
+          for (int k = 0; k < V; ++k) {
+            uint32_t bits = 0;
+            if (i * V + k < n) {
+              if constexpr (sizeof(T) == 4) bits = reinterpret_cast<const uint32_t *>(x)[i * V + k];
+              else bits = reinterpret_cast<const uint16_t *>(x)[i * V + k];
+            }
+            part[k * sizeof(T) / 4] |= bits << (k * sizeof(T) % 4 * 8);
+          }
+          q = make_uint4(part[0], part[1], part[2], part[3]);
+        }
+        w[4 * i] = q.x, w[4 * i + 1] = q.y, w[4 * i + 2] = q.z, w[4 * i + 3] = q.w;
+      }
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) w[i] = i < n ? reinterpret_cast<const uint32_t *>(x)[i] : 0;
+    } else {
+      odd = reinterpret_cast<uintptr_t>(x) >> 1 & 1;
+      const uint32_t *from = reinterpret_cast<const uint32_t *>(reinterpret_cast<uintptr_t>(x) & ~uintptr_t(3));
+#pragma unroll
+      for (int i = 0; i < kWords; ++i) w[i] = 2 * i - odd < n && (i < E / 2 || odd) ? from[i] : 0;  // (words with an element of the row)
+    }
+  }
+  __device__ __forceinline__ void numbers(int n, float (&v)[E]) const {
+    if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < E; ++i) v[i] = __uint_as_float(w[i]);
+    } else if constexpr (WIDE) {
+#pragma unroll
+      for (int i = 0; i < E / 2; ++i) unpack2<T>(w[i], v[2 * i], v[2 * i + 1]);
     } else {
 #pragma unroll
-      for (int k = 0; k < V; ++k) v[i + k] = e + i + k < dim ? to_f32(x[e + i + k]) : 0.0f;
+      for (int i = 0; i < E / 2; ++i) {
+        float a, b;
+        unpack2<T>(__funnelshift_r(w[i], w[i + 1], odd * 16), a, b);
+        v[2 * i] = 2 * i < n ? a : 0.0f, v[2 * i + 1] = 2 * i + 1 < n ? b : 0.0f;
+      }
     }
   }
-}
-// the same from anywhere: by whole words, two 16-bit elements each, shifted into place where the first is the second of its word (single
-// elements, a warp to a row: 65 us for 19,400 tokens of 8 heads of 77)
-template <typename T>
-__device__ __forceinline__ void load_row_anywhere(const T *x, int n, float (&v)[E]) {
-  if constexpr (sizeof(T) == 4) {
-#pragma unroll
-    for (int i = 0; i < E; ++i) v[i] = i < n ? x[i] : 0.0f;
-  } else {
-    const int odd = static_cast<int>(reinterpret_cast<uintptr_t>(x) >> 1 & 1);
-    const uint32_t *from = reinterpret_cast<const uint32_t *>(reinterpret_cast<uintptr_t>(x) & ~uintptr_t(3));
-    uint32_t w[E / 2 + 1];
-#pragma unroll
-    for (int i = 0; i <= E / 2; ++i) w[i] = 2 * i - odd < n && (i < E / 2 || odd) ? from[i] : 0;  // (words with an element of the row)
-#pragma unroll
-    for (int i = 0; i < E / 2; ++i) {
-      float a, b;
-      unpack2<T>(__funnelshift_r(w[i], w[i + 1], odd * 16), a, b);
-      v[2 * i] = 2 * i < n ? a : 0.0f, v[2 * i + 1] = 2 * i + 1 < n ? b : 0.0f;
-    }
-  }
-}
+};
 template <typename T>
 __device__ __forceinline__ void store_piece(T *x, int e, int dim, const float *v) {
   if (e + kVec<T> <= dim) {
@@ -145,7 +169,7 @@ __global__ void __launch_bounds__(kRowsThreads, kCtas) append_kernel(const __gri
   const int tokens = static_cast<int>(min(static_cast<int64_t>(p.tokens), c.total - token0)), rows = tokens * 2 * c.cache.heads;
   RowsWalk w(threadIdx.x / p.lanes, step, 2 * c.cache.heads);
   for (int i = 0; i < rows; i += AHEAD * step) {
-    float v[AHEAD][E];
+    NewRow<T, WIDE> x[AHEAD];
     int token[AHEAD], at[AHEAD];
 #pragma unroll
     for (int a = 0; a < AHEAD; ++a) {
@@ -153,10 +177,8 @@ __global__ void __launch_bounds__(kRowsThreads, kCtas) append_kernel(const __gri
       w.next();
       const bool values = at[a] >= c.cache.heads;
       const int64_t r = token0 + token[a];
-      const T *x = values ? static_cast<const T *>(c.v) + (r * c.v_row + (at[a] - c.cache.heads) * c.v_head) : static_cast<const T *>(c.k) + (r * c.k_row + at[a] * c.k_head);
-      const int have = token[a] < tokens ? dim : 0;
-      if constexpr (WIDE) load_row<T>(x, lane * E, have, v[a]);
-      else load_row_anywhere<T>(x + lane * E, have - lane * E, v[a]);
+      const T *from = values ? static_cast<const T *>(c.v) + (r * c.v_row + (at[a] - c.cache.heads) * c.v_head) : static_cast<const T *>(c.k) + (r * c.k_row + at[a] * c.k_head);
+      x[a].load(from + lane * E, token[a] < tokens ? dim - lane * E : 0);
     }
     if (i == 0) find_places(c, token0, tokens, place);  // (beside the first rows' loads)
 #pragma unroll
@@ -165,16 +187,18 @@ __global__ void __launch_bounds__(kRowsThreads, kCtas) append_kernel(const __gri
       const int head = values ? at[a] - c.cache.heads : at[a];
       const int64_t first = token[a] < tokens ? place[token[a]] : -1, row = first + static_cast<int64_t>(head) * c.cache.page_size;
       C *out = static_cast<C *>(values ? c.cache.v : c.cache.k) + row * c.cache.ld;
+      float v[E];
+      x[a].numbers(dim - lane * E, v);
       if constexpr (sizeof(C) == 1) {
         uint32_t m = 0;  // (as whole numbers, magnitudes keep their order, and a NaN is the largest)
 #pragma unroll
-        for (int k = 0; k < E; ++k) m = max(m, __float_as_uint(v[a][k]) & 0x7fffffffu);
+        for (int k = 0; k < E; ++k) m = max(m, __float_as_uint(v[k]) & 0x7fffffffu);
         for (int o = p.lanes / 2; o > 0; o >>= 1) m = max(m, __shfl_xor_sync(0xffffffffu, m, o));
         const float alpha = __uint_as_float(max(m, __float_as_uint(kAlphaMin))), by = __fdiv_rn(127.0f, alpha);
         if (first < 0) continue;
 #pragma unroll
-        for (int k = 0; k < E; ++k) v[a][k] = __fmul_rn(v[a][k], by);
-        const uint4 w4 = make_uint4(codes_of(v[a]), codes_of(v[a] + 4), codes_of(v[a] + 8), codes_of(v[a] + 12));
+        for (int k = 0; k < E; ++k) v[k] = __fmul_rn(v[k], by);
+        const uint4 w4 = make_uint4(codes_of(v), codes_of(v + 4), codes_of(v + 8), codes_of(v + 12));
         const int e = lane * E;
         if (e + E <= dim) {
           *reinterpret_cast<uint4 *>(out + e) = w4;  // (rows start on 16 bytes)
@@ -186,7 +210,7 @@ __global__ void __launch_bounds__(kRowsThreads, kCtas) append_kernel(const __gri
       } else {
         if (first < 0) continue;
 #pragma unroll
-        for (int k = 0; k < E; k += kVec<C>) store_piece<C>(out, lane * E + k, dim, v[a] + k);
+        for (int k = 0; k < E; k += kVec<C>) store_piece<C>(out, lane * E + k, dim, v + k);
       }
     }
   }
@@ -368,7 +392,7 @@ template <typename T, typename C>
 cudaError_t append_of(const KvRowsCall &c, cudaStream_t st) {
   const bool wide = in_pieces(c.k, c.v, c.k_row, c.k_head, c.v_row, c.v_head, 0, sizeof(T));
   return plan_rows(c, [&](unsigned grid, const RowsPlan &p, size_t smem, bool many) {
-    const auto kernel = wide ? (many ? append_kernel<T, C, kAhead, true> : append_kernel<T, C, 1, true>)
+    const auto kernel = wide ? (many ? append_kernel<T, C, 8 / sizeof(T), true> : append_kernel<T, C, 1, true>)
                              : many ? append_kernel<T, C, kAhead, false> : append_kernel<T, C, 1, false>;
     kernel<<<grid, kRowsThreads, smem, st>>>(c, p);
   });
