@@ -29,31 +29,36 @@ struct RowsPlan {
   int lanes, tokens;  // lanes to a row; tokens of a CTA at most
 };
 
-// E elements of a row, of which it has n (none for n <= 0; the others are 0), as they lie there, so that rows on their way take few registers, and as numbers.
+// A lane's E elements of a row of dim (those past its end are 0) as they lie there, so that rows on their way take few registers, and as numbers.
 // WIDE: rows of 16-byte pieces.  Else by whole words, two 16-bit elements each, shifted into place where the first is the second of its word (single
-// elements, a warp to a row: 65 us for 19,400 tokens of 8 heads of 77).
+// elements, a warp to a row: 65 us for 19,400 tokens of 8 heads of 77).  Elements side by side, but wide rows of floats, of which a lane takes every
+// lanes-th piece: with 64 bytes to a lane, lanes read a quarter of a line each (12,300 tokens of 12 heads of 100 35 us, 33 so).
 template <typename T, bool WIDE>
 struct NewRow {
   static constexpr int kWords = E * sizeof(T) / 4 + (!WIDE && sizeof(T) == 2);
+  static constexpr bool kApart = WIDE && sizeof(T) == 4;
   uint32_t w[kWords];
   bool odd;
-  __device__ __forceinline__ void load(const T *x, int n) {
+  // the first of the i-th four elements
+  static __device__ __forceinline__ int four(int i, int lane, int lanes) { return kApart ? (i * lanes + lane) * 4 : lane * E + i * 4; }
+  __device__ __forceinline__ void load(const T *row, int lane, int lanes, int dim) {
     odd = false;
     if constexpr (WIDE) {
       constexpr int V = kVec<T>;
 #pragma unroll
       for (int i = 0; i < E / V; ++i) {
+        const int e = four(i * V / 4, lane, lanes);
         uint4 q = make_uint4(0, 0, 0, 0);
-        if (n >= (i + 1) * V) {
-          q = reinterpret_cast<const uint4 *>(x)[i];
-        } else if (n > i * V) {  // (a row's last elements)
+        if (e + V <= dim) {
+          q = *reinterpret_cast<const uint4 *>(row + e);
+        } else if (e < dim) {  // (a row's last elements)
           uint32_t part[4] = {0, 0, 0, 0};
 #pragma unroll
           for (int k = 0; k < V; ++k) {
             uint32_t bits = 0;
-            if (i * V + k < n) {
-              if constexpr (sizeof(T) == 4) bits = reinterpret_cast<const uint32_t *>(x)[i * V + k];
-              else bits = reinterpret_cast<const uint16_t *>(x)[i * V + k];
+            if (e + k < dim) {
+              if constexpr (sizeof(T) == 4) bits = reinterpret_cast<const uint32_t *>(row)[e + k];
+              else bits = reinterpret_cast<const uint16_t *>(row)[e + k];
             }
             part[k * sizeof(T) / 4] |= bits << (k * sizeof(T) % 4 * 8);
           }
@@ -63,8 +68,10 @@ struct NewRow {
       }
     } else if constexpr (sizeof(T) == 4) {
 #pragma unroll
-      for (int i = 0; i < E; ++i) w[i] = i < n ? reinterpret_cast<const uint32_t *>(x)[i] : 0;
+      for (int i = 0; i < E; ++i) w[i] = lane * E + i < dim ? reinterpret_cast<const uint32_t *>(row)[lane * E + i] : 0;
     } else {
+      const T *x = row + lane * E;
+      const int n = dim - lane * E;
       odd = reinterpret_cast<uintptr_t>(x) >> 1 & 1;
       const uint32_t *from = reinterpret_cast<const uint32_t *>(reinterpret_cast<uintptr_t>(x) & ~uintptr_t(3));
 #pragma unroll
@@ -114,14 +121,14 @@ __device__ __forceinline__ float scale_of(float alpha) {
   return fmaf(fmaf(-q, 127.0f, alpha), by, q);
 }
 
-// 8 codes of a row of dim, from element e on, or V (4 or 8) of them: words of four
-__device__ __forceinline__ void store_codes(int8_t *row, int e, int dim, uint32_t a, uint32_t b) {
-  if (e + 8 <= dim) {
-    *reinterpret_cast<uint2 *>(row + e) = make_uint2(a, b);
+// four codes of a row of dim, from element e on; and V (4 or 8) of them back
+__device__ __forceinline__ void store_codes(int8_t *row, int e, int dim, uint32_t w) {
+  if (e + 4 <= dim) {
+    *reinterpret_cast<uint32_t *>(row + e) = w;
   } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k)
-      if (e + k < dim) row[e + k] = static_cast<int8_t>((k < 4 ? a : b) >> (k % 4 * 8));
+    for (int k = 0; k < 3; ++k)
+      if (e + k < dim) row[e + k] = static_cast<int8_t>(w >> (k * 8));
   }
 }
 template <int V>
@@ -178,7 +185,7 @@ __global__ void __launch_bounds__(kRowsThreads, kCtas) append_kernel(const __gri
       const bool values = at[a] >= c.cache.heads;
       const int64_t r = token0 + token[a];
       const T *from = values ? static_cast<const T *>(c.v) + (r * c.v_row + (at[a] - c.cache.heads) * c.v_head) : static_cast<const T *>(c.k) + (r * c.k_row + at[a] * c.k_head);
-      x[a].load(from + lane * E, token[a] < tokens ? dim - lane * E : 0);
+      x[a].load(from, lane, p.lanes, token[a] < tokens ? dim : 0);
     }
     if (i == 0) find_places(c, token0, tokens, place);  // (beside the first rows' loads)
 #pragma unroll
@@ -200,11 +207,12 @@ __global__ void __launch_bounds__(kRowsThreads, kCtas) append_kernel(const __gri
         for (int k = 0; k < E; ++k) v[k] = __fmul_rn(v[k], by);
         const uint4 w4 = make_uint4(codes_of(v), codes_of(v + 4), codes_of(v + 8), codes_of(v + 12));
         const int e = lane * E;
-        if (e + E <= dim) {
+        if (!NewRow<T, WIDE>::kApart && e + E <= dim) {
           *reinterpret_cast<uint4 *>(out + e) = w4;  // (rows start on 16 bytes)
         } else {
-          store_codes(out, e, dim, w4.x, w4.y);
-          store_codes(out, e + 8, dim, w4.z, w4.w);
+          const uint32_t words[4] = {w4.x, w4.y, w4.z, w4.w};
+#pragma unroll
+          for (int k = 0; k < 4; ++k) store_codes(out, NewRow<T, WIDE>::four(k, lane, p.lanes), dim, words[k]);
         }
         if (lane == 0) (values ? c.cache.v_scale : c.cache.k_scale)[row] = scale_of(alpha);
       } else {
