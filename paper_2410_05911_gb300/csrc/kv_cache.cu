@@ -75,7 +75,7 @@ struct NewRow {
       odd = reinterpret_cast<uintptr_t>(x) >> 1 & 1;
       const uint32_t *from = reinterpret_cast<const uint32_t *>(reinterpret_cast<uintptr_t>(x) & ~uintptr_t(3));
 #pragma unroll
-      for (int i = 0; i < kWords; ++i) w[i] = 2 * i - odd < n && (i < E / 2 || odd) ? from[i] : 0;  // (words with an element of the row)
+      for (int i = 0; i < kWords; ++i) w[i] = n > 0 && 2 * i - odd < n && (i < E / 2 || odd) ? from[i] : 0;  // (words with an element of the row)
     }
   }
   __device__ __forceinline__ void numbers(int n, float (&v)[E]) const {

@@ -176,6 +176,22 @@ def test_strides_and_a_cache_of_the_users_own():
         assert torch.equal(got.cpu(), torch.tensor(codes.astype(np.float32) * scale[..., None]))
 
 
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("off", [0, 1])
+@pytest.mark.parametrize("dim,heads", [(8, 1), (16, 1), (48, 2), (77, 3), (128, 8)])
+def test_nothing_is_read_past_the_last_token(dim, heads, off, dtype):
+    """Rows that would lie 2^36 bytes and more after the last token's, where no memory is."""
+    x = torch.randn(heads * dim + off, device="cuda").to(dtype)[off:].as_strided((1, heads, dim), (2 ** 35, dim, 1))
+    table, pages = pages_for([3], 4)
+    cache = marked(pages, heads, 4, dim, torch.int8)
+    lengths = torch.tensor([3], **I32)
+    A.kv_append(x, x, cache, table, lengths)
+    A.kv_append(x, x, cache, table, lengths, rows=torch.tensor([0, 1], **I32))
+    codes, scale = quant(x[0])
+    for got in A.kv_read(cache, table, lengths, None, 1):
+        assert torch.equal(got[0].cpu(), torch.tensor(codes.astype(np.float32) * scale[..., None]))
+
+
 def test_on_another_stream_and_in_a_graph():
     lens = [40, 17]
     table, pages = pages_for(lens, 16)
