@@ -19,7 +19,7 @@
 //
 // Bound by memory where sequences are long: a million tokens of 8 cache heads of 128, 8 query heads to each, take 346 us, 6.1 TB/s (a copy of the
 // same bytes 313).  Where they are short, by a piece's start and end and by what a warp alone waits for: 512 sequences of up to 180 tokens, 8 heads
-// of 16, 24 us.
+// of 16, 16 us.
 //
 // 32 bits: sums of products, maxima, exponents and sums.  What is rounded to 16: the weights, as the tensor cores' operand. With codes the scale of a value row belongs to the
 // weight: 2^(x_j - m) vs_j = 2^(y_j), y_j = x_j - m + log2 vs_j, has a running maximum of its own, so that the weights that
@@ -57,7 +57,7 @@ struct AttendArgs {
   float *lse;
   float *partial;      // [CTAs][2][kPart]
   AttendPiece *piece;  // [CTAs][2]
-  int ctas;            // of a cluster that takes one piece of heads of one sequence; 0: tiles are dealt out
+  int ctas;            // of a cluster that takes one piece of heads of one sequence; 0: tiles are dealt out; -1: a warp to each piece
 };
 
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
@@ -809,7 +809,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, S::kCtas) attend_kernel(const 
 }
 
 // Few and short sequences: a cluster of CTAs to each piece of heads of each of them, whose parts are joined through distributed shared memory.  No list, no
-// second kernel: one request of 500 tokens 8 us instead of 11.
+// second kernel: one request of 500 tokens 7.2 us instead of 11.3.
 template <class S>
 __global__ void __launch_bounds__(S::kWarps * 32, S::kCtas) attend_whole_kernel(const __grid_constant__ AttendArgs a) {
   constexpr int NT = S::kWarps * 32, W = S::kWarps, DP = S::DP, H = S::kHeads;
@@ -914,6 +914,54 @@ __global__ void __launch_bounds__(S::kWarps * 32, S::kCtas) attend_whole_kernel(
   cluster_sync_all();  // (no CTA ends while another one reads its sums)
 }
 
+// Many short sequences: a warp to each piece of heads of each of them, and nothing to join (512 of up to 180 tokens, 8 heads of 16, 16 us, 24 dealt
+// out).
+template <class S>
+__global__ void __launch_bounds__(S::kWarps * 32, S::kCtas) attend_lone_kernel(const __grid_constant__ AttendArgs a, int pieces) {
+  constexpr int H = S::kHeads;
+  using Warp = AttendWarp<S>;
+  extern __shared__ __align__(16) unsigned char smem[];
+  const int warp = threadIdx.x >> 5, all = a.cache.heads * a.parts, piece = blockIdx.x * S::kWarps + warp;
+  if (piece >= pieces) return;
+  typename Warp::Cursor at = {};
+  at.b = piece / all, at.j = piece % all;
+  Warp w(a, smem_u32(smem + warp * (S::kStages * S::kStage)));
+  w.sequence(at);
+  typename Warp::Cursor next = at;
+  const int n = at.tiles;
+  int page = -1, place = 0, filled = 0;
+  if (n > 0) w.find(next, page, place);
+  const auto fill = [&]() {
+    if (filled < n) {
+      w.fill(filled % S::kStages, next, page, place);
+      if (++filled < n) ++next.tile, w.find(next, page, place);
+    }
+    copies_commit();
+  };
+  for (int i = 0; i < S::kStages - 1; ++i) fill();
+  w.begin(at);
+#pragma unroll 1
+  for (int i = 0; i < n; ++i) {
+    copies_wait<S::kStages - 2>();
+    __syncwarp();
+    fill();
+    w.tile(i % S::kStages);
+  }
+  const int part = at.j % a.parts, heads = min(H, a.group - part * H);
+  const int64_t head0 = static_cast<int64_t>(at.b) * a.q_heads + at.j / a.parts * a.group + part * H;
+  float inv[Warp::HC];
+  w.end(
+      [&](int head, int hc, int e, float (&v)[Warp::EL]) {
+#pragma unroll
+        for (int k = 0; k < Warp::EL; ++k) v[k] *= inv[hc];
+        if (head < heads) store_outs(a, head0 + head, e, v);
+      },
+      [&](int head, int hc, float top, float l) {
+        inv[hc] = l == 0.0f ? 0.0f : __fdiv_rn(1.0f, l);
+        if (a.lse && head < heads && w.g == 0) a.lse[head0 + head] = lse_of(top, l);
+      });
+}
+
 // a launch of the kernel: the grid that fills the GPU
 struct AttendPlan {
   int ctas, heads, width, part;  // CTAs, query heads of a piece, DP, floats of a piece
@@ -956,7 +1004,15 @@ cudaError_t run_attend(const AttendArgs *a, AttendPlan *plan, cudaStream_t st) {
     }
     return cudaSuccess;
   }
-  if (a->ctas > 0) return launch_whole<S>(*a, a->seqs.batch * a->cache.heads * a->parts, st);
+  const int64_t pieces = static_cast<int64_t>(a->seqs.batch) * a->cache.heads * a->parts;
+  if (a->ctas > 0) return launch_whole<S>(*a, static_cast<int>(pieces), st);
+  if (a->ctas < 0) {
+    constexpr int kSmem = S::kWarps * S::kStages * S::kStage;
+    const cudaError_t e = cudaFuncSetAttribute(attend_lone_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, kSmem);
+    if (e != cudaSuccess) return e;
+    attend_lone_kernel<S><<<static_cast<unsigned>((pieces + S::kWarps - 1) / S::kWarps), S::kWarps * 32, kSmem, st>>>(*a, static_cast<int>(pieces));
+    return cudaGetLastError();
+  }
   const cudaError_t e = cudaFuncSetAttribute(attend_kernel<S>, cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
   if (e != cudaSuccess) return e;
   attend_kernel<S><<<plan->ctas, S::kWarps * 32, S::kSmem, st>>>(*a);
