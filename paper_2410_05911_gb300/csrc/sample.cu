@@ -32,6 +32,7 @@ namespace {
 using u64 = unsigned long long;
 constexpr int kSteps = 128;  // of the table of powers of two
 constexpr int kList = 256;   // candidates of top-k that one CTA takes
+constexpr int kFew = 128;    // logits between the bounds of a cut that one CTA puts in order
 constexpr int kOctaves = 32;  // of weights that bins of equal steps cover
 constexpr float kTemperatureMin = 0x1p-100f, kTemperatureMax = 0x1p100f;
 
@@ -97,8 +98,8 @@ struct SampleShared {
   static constexpr int kNotes = NT == 1024 ? 1024 : 512;  // logits between the bounds of a cut that a warp puts down
   uint32_t power[kSteps][32];  // a copy to each lane's bank (with one, random entries took 3 to 4 reads)
   uint32_t count[2][kBins];
-  u64 warp[32][2];  // (all 32 are read)
-  u64 part[2][2];                // this CTA's sums, for the cluster
+  u64 warp[32][3];  // (all 32 are read)
+  u64 part[2][3];                // this CTA's sums, for the cluster
   u64 segment[2][32];  // a number of each warp's part of the row
   struct Hand {
     u64 passed, rank;
@@ -109,6 +110,7 @@ struct SampleShared {
   uint32_t list_index[kList], listed;
   u64 list_weight[kList];
   uint32_t found[2];
+  float settled;
   u64 found_sum[2];
   double least;          // temperature ln min_p
   float c, c_low, floor;  // log2 e / temperature, and the lowest logit that min_p leaves
@@ -246,6 +248,7 @@ struct SampleRow {
     const uint32_t m = e + __float_as_uint(fmaf(__uint_as_float((e >> 6) + (125u << 23)), q, 12582912.0f)) - 0x4b400000u;
     return (static_cast<u64>(m) << 32) >> ((n / kSteps & 63) + 18);  // (n / kSteps <= 45)
   }
+
   // puts down a logit between the bounds of a cut for the passes that follow: each warp its own
   __device__ __forceinline__ void note(bool in, float v) {
     const uint32_t who = __ballot_sync(0xffffffffu, in);
@@ -272,21 +275,29 @@ struct SampleRow {
   static __device__ u64 above(u64 w) { return w + (w >> 27) + 2; }
   static __device__ u64 below(u64 w) { return w < 4 ? 0 : w - (w >> 27) - 2; }
 
-  // sums over the row of two numbers
-  __device__ void sums(u64 &a, u64 &b) {
-    for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o), b += __shfl_xor_sync(0xffffffffu, b, o);
-    if (lane == 0) sh.warp[warp][0] = a, sh.warp[warp][1] = b;
+  // sums over the row of three numbers
+  __device__ void sums(u64 &a, u64 &b, u64 &c3) {
+    for (int o = 16; o > 0; o >>= 1)
+      a += __shfl_xor_sync(0xffffffffu, a, o), b += __shfl_xor_sync(0xffffffffu, b, o), c3 += __shfl_xor_sync(0xffffffffu, c3, o);
+    if (lane == 0) sh.warp[warp][0] = a, sh.warp[warp][1] = b, sh.warp[warp][2] = c3;
     __syncthreads();
     if (warp == 0) {
-      a = lane < kWarps ? sh.warp[lane][0] : 0, b = lane < kWarps ? sh.warp[lane][1] : 0;
-      for (int o = 16; o > 0; o >>= 1) a += __shfl_xor_sync(0xffffffffu, a, o), b += __shfl_xor_sync(0xffffffffu, b, o);
-      if (lane == 0) sh.part[flip][0] = a, sh.part[flip][1] = b;
+      const bool in = lane < kWarps;
+      a = in ? sh.warp[lane][0] : 0, b = in ? sh.warp[lane][1] : 0, c3 = in ? sh.warp[lane][2] : 0;
+      for (int o = 16; o > 0; o >>= 1)
+        a += __shfl_xor_sync(0xffffffffu, a, o), b += __shfl_xor_sync(0xffffffffu, b, o), c3 += __shfl_xor_sync(0xffffffffu, c3, o);
+      if (lane == 0) sh.part[flip][0] = a, sh.part[flip][1] = b, sh.part[flip][2] = c3;
     }
     sync();
-    a = b = 0;
+    a = b = c3 = 0;
     const uint32_t at = smem_u32(sh.part[flip]);
-    for (uint32_t r = 0; r < ctas; ++r) a += ld_cluster_u64(mapa_cluster(at, r)), b += ld_cluster_u64(mapa_cluster(at + 8, r));
+    for (uint32_t r = 0; r < ctas; ++r)
+      a += ld_cluster_u64(mapa_cluster(at, r)), b += ld_cluster_u64(mapa_cluster(at + 8, r)), c3 += ld_cluster_u64(mapa_cluster(at + 16, r));
     flip ^= 1;
+  }
+  __device__ void sums(u64 &a, u64 &b) {
+    u64 none = 0;
+    sums(a, b, none);
   }
   __device__ float maximum(float v) {
     for (int o = 16; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, o));
@@ -399,6 +410,32 @@ struct SampleRow {
       u64 at = 0;
       for (int j = 0; j < most; ++j) at += sh.list_index[j] < index ? sh.list_weight[j] : 0;
       if (stays && at <= target && target < at + w) *token = index;
+    }
+  }
+  // The cut of the mass among the listed logits, one of which it is, `passed` being that of the logits above them: to every CTA of the row.
+  __device__ void settle(u64 passed, u64 want) {
+    const int n = static_cast<int>(sh.listed), i = threadIdx.x;
+    const float v0 = i < n ? sh.list_logit[i] : 0.0f;
+    int rank_here = 0;
+    if ((i & ~31) < n)
+      for (int j = 0; j < n; ++j) {
+        const float v = sh.list_logit[j];
+        rank_here += v > v0 || (v == v0 && j < i);
+      }
+    __syncthreads();
+    if (i < n) sh.list_logit[rank_here] = v0;
+    __syncthreads();
+    const float v = i < n ? sh.list_logit[i] : 0.0f;
+    const u64 w = i < n ? weight(v) : 0;
+    u64 all;
+    const u64 at = passed + before(w, all);
+    if (i < n && (i == 0 || at < want) && (at + w >= want || i == n - 1)) {  // (one of them)
+      uint32_t ties = 1;
+      while (ties <= static_cast<uint32_t>(i) && sh.list_logit[i - ties] == v) ++ties;
+      for (uint32_t r = 0; r < ctas; ++r) {
+        st_cluster_f32(mapa_cluster(smem_u32(&sh.settled), r), v);
+        st_cluster_u32(mapa_cluster(smem_u32(sh.found), r), ties);
+      }
     }
   }
   // the bin that one thread has found, and the sum before it
@@ -566,7 +603,8 @@ __global__ void __launch_bounds__(NT, NT == 1024 ? 1 : 4) sample_kernel(SampleCa
         r.note(v <= over && v >= under, v);
       });
       above = passed;
-      r.sums(whole, passed);
+      u64 notes = r.lane == 0 ? r.noted : 0;
+      r.sums(whole, passed, notes);
       if (ties != ~0ull) whole += ties * r.weight(cut);
       u64 want = 1;
       if (p > 0.0f) {
@@ -574,7 +612,27 @@ __global__ void __launch_bounds__(NT, NT == 1024 ? 1 : 4) sample_kernel(SampleCa
         want = times(p, whole, cut_off);
         want += cut_off;
       }
-      for (int step = 0; step < 33; ++step) {  // (each leaves half of the keys at most)
+      // Few logits between the bounds: one CTA puts them in order instead of histograms of their keys, of which logits of 32 bits take up to four (one
+      // row of 50,021 28 us for 33, 512 rows of 1,000 21 for 24.5; with up to 256 of them, rows of 131,072 took 64 for 62).
+      const bool few = notes > 0 && notes <= kFew;  // (the same in every CTA)
+      static_assert(kFew <= SampleRow<T, NT>::kNotes && kFew <= kList && kFew <= NT, "all of them were put down, and a thread takes each");
+      if (few) {
+        if (r.noted > 0) {
+          uint32_t at = 0;
+          if (r.lane == 0) at = atom_cluster_add(mapa_cluster(smem_u32(&sh.listed), 0), static_cast<uint32_t>(r.noted));
+          at = __shfl_sync(0xffffffffu, at, 0);
+          __syncwarp();
+          for (int i = r.lane; i < r.noted; i += 32) st_cluster_f32(mapa_cluster(smem_u32(sh.list_logit + at + i), 0), sh.notes[r.warp][i]);
+        }
+        r.sync();
+        if (rank == 0) r.settle(passed, want);
+        r.sync();
+        const float v = sh.settled;
+        const u64 n = sh.found[0];
+        ties = v == cut && ties < n ? ties : n, cut = v;
+        known = over;
+      }
+      for (int step = 0; step < 33 && !few; ++step) {  // (each leaves half of the keys at most)
         int shift = 0;
         while ((high - low) >> shift >= kBins) ++shift;
         const float upto = K::logit(high), from = fmaxf(r.lowest, K::logit(low));
