@@ -97,7 +97,7 @@ void check_current(const at::Device &on) {
 void check_no_graph(const char *call, std::initializer_list<const at::Tensor *> tensors) {
   if (!c10::GradMode::is_enabled()) return;
   for (const at::Tensor *t : tensors)
-    if (t && t->requires_grad())
+    if (t && t->defined() && t->requires_grad())
       throw ValueError(std::string(call) + " records nothing for autograd: call it under torch.no_grad(), in an autograd.Function, or on detached tensors");
 }
 
@@ -420,7 +420,7 @@ PyObject *kv_append(PyObject *const *a) {
   const int64_t total = k.size(0);
   const at::Tensor rows = a[5] == Py_None ? at::Tensor() : int_array(a[5], "rows", on, int64_t(seqs.s.batch) + 1);
   if (!rows.defined() && total != seqs.s.batch) throw ValueError("without rows, k has one token for each of " + std::to_string(seqs.s.batch) + " sequences");
-  check_no_graph("kv_append", {&k, &v, &cache.k, &cache.v});
+  check_no_graph("kv_append", {&k, &v, &cache.k, &cache.v, &cache.k_scale, &cache.v_scale});
   const Heads kh(k), vh(v);
   void *s = launch_stream(a[6], cache.k, {&kh.t, &vh.t, &cache.k, &cache.v, &cache.k_scale, &cache.v_scale, &seqs.table, &seqs.lengths, &rows});
   check(aecct_kv_append(&cache.c, &seqs.s, rows.defined() ? static_cast<const int32_t *>(rows.data_ptr()) : nullptr, total, kh.t.data_ptr(), kh.row, kh.head,
@@ -442,7 +442,7 @@ PyObject *kv_read(PyObject *const *a) {
   if (total < 0) throw ValueError("total must not be negative");
   if (!rows.defined() && total != seqs.s.batch) throw ValueError("without rows, there is one token for each of " + std::to_string(seqs.s.batch) + " sequences");
   const int32_t dtype = element_arg(a[5], "dtype");
-  check_no_graph("kv_read", {&cache.k, &cache.v});
+  check_no_graph("kv_read", {&cache.k, &cache.v, &cache.k_scale, &cache.v_scale});
   const at::Tensor k = make({total, cache.c.heads, cache.c.head_dim}, on, type_of(dtype)), v = make({total, cache.c.heads, cache.c.head_dim}, on, type_of(dtype));
   void *s = launch_stream(a[6], cache.k, {&k, &v, &cache.k, &cache.v, &cache.k_scale, &cache.v_scale, &seqs.table, &seqs.lengths, &rows});
   check(aecct_kv_read(&cache.c, &seqs.s, rows.defined() ? static_cast<const int32_t *>(rows.data_ptr()) : nullptr, total, k.data_ptr(), v.data_ptr(), dtype, s),
@@ -461,7 +461,7 @@ PyObject *paged_attention(PyObject *const *a) {
     throw ValueError("the heads of q must be a multiple of the cache's " + std::to_string(cache.c.heads));
   const at::Tensor first = a[4] == Py_None ? at::Tensor() : int_array(a[4], "first", on, seqs.s.batch);
   const double scale = a[5] == Py_None ? 1.0 / std::sqrt(static_cast<double>(cache.c.head_dim)) : number(a[5]);
-  check_no_graph("paged_attention", {&q, &cache.k, &cache.v});
+  check_no_graph("paged_attention", {&q, &cache.k, &cache.v, &cache.k_scale, &cache.v_scale});
   const int32_t q_heads = static_cast<int32_t>(q.size(1)), dtype = element(q.scalar_type());
   int64_t bytes = 0;
   check(aecct_paged_attention_workspace(seqs.s.batch, q_heads, cache.c.heads, cache.c.head_dim, dtype, cache.c.dtype, &bytes), "aecct_paged_attention");

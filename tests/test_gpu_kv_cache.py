@@ -249,6 +249,22 @@ def test_refusals():
     assert (cache.k == 77).all()
 
 
+def test_scales_that_autograd_records_are_refused():
+    table, pages = pages_for([8], 4)
+    plain = marked(pages, 2, 4, 16, torch.int8)
+    k, v = tokens(1, 2, 16, torch.float32, 1)
+    n = torch.tensor([8], **I32)
+    for name in ("k_scale", "v_scale"):
+        cache = plain._replace(**{name: getattr(plain, name).clone().requires_grad_()})
+        for call in (lambda: A.kv_append(k, v, cache, table, n), lambda: A.kv_read(cache, table, n, None, 1), lambda: A.paged_attention(k, cache, table, n)):
+            with pytest.raises(ValueError):
+                call()
+        with torch.no_grad():
+            A.kv_append(k, v, cache, table, n)
+    half = marked(pages, 2, 4, 16, torch.float16)  # (has no scales)
+    A.kv_append(k.half(), v.half(), half, table, n)
+
+
 def test_nothing_to_do():
     table, pages = pages_for([8], 4)
     cache = marked(pages, 2, 4, 16, torch.int8)
