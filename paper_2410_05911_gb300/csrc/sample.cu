@@ -13,7 +13,7 @@
 // A cluster of 1 to 8 CTAs takes a row, each a part of it, and reads the others' histograms and sums through distributed
 // shared memory.
 //
-// Bound by instructions where rows are many and flat (128 rows of 131,072 logits, top-p 0.9: 67 us, of them 28 for the weights of all logits, 11 for
+// Bound by instructions where rows are many and flat (128 rows of 131,072 logits, top-p 0.9: 68 us, of them 28 for the weights of all logits, 11 for
 // the histogram of steps, 5 for the trip to memory), by the phases' trips and barriers where they are few (one row of 50,021, every filter: 17 us).
 #include <cuda_runtime.h>
 
@@ -840,8 +840,8 @@ int rows_at_once(int i) {
   return n;
 }
 
-// CTAs to a row: as long as all rows' run at once, and each has 8 logits to a thread (one row of 50,021: 34 us with 4 CTAs and 38 with 8 at top-p
-// alone, 43 with one; 15 with either, 21 with one, at top-k)
+// CTAs to a row: as long as all rows' run at once, and each has 8 logits to a thread (one row of 50,021: 27.5 us with 4 CTAs and 31 with 8 at
+// top-p alone, 37 with one; 16 with either, 22 with one, at top-k; of 131,072 41, 44 and 73)
 template <int NT>
 int ctas_of(const SampleCall &c) {
   int i = 0;
