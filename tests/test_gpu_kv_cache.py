@@ -1,5 +1,7 @@
 """kv_append and kv_read on the GPU, bit for bit against eq. Quant in numpy's 32-bit arithmetic (each operation is rounded
 once there and here: the quotient 127 / alpha, the product with it, the rounding to a whole number, alpha / 127)."""
+import math
+
 import numpy as np
 import pytest
 
@@ -247,6 +249,33 @@ def test_refusals():
             call()
             pytest.fail(f"call {i} was not refused")
     assert (cache.k == 77).all()
+
+
+@pytest.mark.parametrize("dtype,size", [(torch.int8, 80), (torch.float16, 80), (torch.float16, 8)])
+def test_memory_that_ends_with_the_last_row(dtype, size):
+    """Rows `size` elements apart, of which the last has nothing behind it, and what is behind the others is no number or 100."""
+    dim, page, heads = size - 3, 4, 2
+    table, pages = pages_for([12, 8], page, spare=0)  # (every row of every page)
+    n = torch.tensor([12, 8], **I32)
+    rows = pages * heads * page
+
+    def cut_short():
+        flat = torch.full(((rows - 1) * size + dim,), 100 if dtype is torch.int8 else math.nan, device="cuda", dtype=dtype)
+        return flat.as_strided((pages, heads, page, dim), (heads * page * size, page * size, size, 1))
+
+    plain = A.kv_cache(pages, heads, page, dim, dtype=dtype)
+    cache = plain._replace(k=cut_short(), v=cut_short())
+    if dtype is torch.int8:
+        cache = cache._replace(k_scale=torch.zeros_like(plain.k_scale), v_scale=torch.zeros_like(plain.v_scale))
+    k, v = tokens(20, heads, dim, torch.float16, 3)
+    first = torch.tensor([0, 12, 20], **I32)
+    for c in (plain, cache):
+        A.kv_append(k, v, c, table, n, rows=first)
+    for out in (torch.float16, torch.float32):
+        got, want = A.kv_read(cache, table, n, first, 20, dtype=out), A.kv_read(plain, table, n, first, 20, dtype=out)
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+        if dtype is torch.float16:
+            assert torch.equal(got[0].half(), k) and torch.equal(got[1].half(), v)
 
 
 def test_scales_that_autograd_records_are_refused():
