@@ -224,3 +224,20 @@ def test_refusals():
         A.sample(x[:, :0], u)
     with pytest.raises(A.AecctError):
         A.sample(torch.zeros((1, 2 ** 19 + 1), device="cuda"), u[:1])
+
+
+@pytest.mark.parametrize("vocab", [1000, 50021])
+@pytest.mark.parametrize("near", [1, 3, 127, 128, 129, 300])
+@pytest.mark.parametrize("p", [0.5, 0.95])
+def test_a_cut_among_logits_close_to_each_other(p, near, vocab):
+    """The mass is that of `near` logits 1e-6 apart, and the cut lies among them: 1e-5 at least from the next border, where 300 weights are off by
+    300 2^-28 = 1.2e-6 together."""
+    g = torch.Generator(device="cuda").manual_seed(near)
+    x = torch.full((6, vocab), -20.0, device="cuda")
+    for r in range(6):
+        x[r, torch.randperm(vocab, device="cuda", generator=g)[:near]] = -1e-6 * torch.arange(near, device="cuda", dtype=torch.float32)
+    x[3:] = (x[3:] * 1e4).round() / 1e4  # (ties, in the order of the row)
+    u = torch.rand((6,), device="cuda", generator=g)
+    check(x, u, top_p=p)
+    check(x, u, top_p=p, top_k=near)
+    check(x, u, top_p=p, min_p=0.5)
