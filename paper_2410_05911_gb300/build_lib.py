@@ -21,7 +21,7 @@ SOURCES = ["api.cu", "decoder_kernel.cu", "decoder_kernel_gelu.cu", "decoder_ker
            "norm.cu", "clip.cu", "linear.cu", "linear_grad.cu", "linear_wgrad.cu",
            "linear_stage.cu", "linear_few.cu", "kv_cache.cu", "attend.cu", "attend_codes.cu", "attend_pieces.cu",
            "attend_half.cu", "attend_bf16.cu", "sample.cu"]
-HEADERS = ["aecct_internal.h", "sm103_ptx.cuh", "rowtypes.cuh", "linear_gemm.cuh", "kv_pages.cuh", "attend.cuh", "decoder_kernel.cuh", os.path.join("..", "..", "include", "aecct.h")]
+HEADERS = ["aecct_internal.h", "sm103_ptx.cuh", "rowtypes.cuh", "linear_gemm.cuh", "kv_pages.cuh", "attend.cuh", "sample_weight.cuh", "decoder_kernel.cuh", os.path.join("..", "..", "include", "aecct.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 NVCC_FLAGS = ARCH + ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "--fmad=false",
                      "-Xcompiler", "-fno-strict-aliasing"]

@@ -23,6 +23,7 @@
 
 #include "aecct_internal.h"
 #include "rowtypes.cuh"
+#include "sample_weight.cuh"
 #include "sm103_ptx.cuh"
 
 namespace aecct {
@@ -30,31 +31,11 @@ namespace aecct {
 namespace {
 
 using u64 = unsigned long long;
-constexpr int kSteps = 128;  // of the table of powers of two
 constexpr int kList = 256;   // candidates of top-k that one CTA takes
 constexpr int kFew = 128;    // logits between the bounds of a cut that one CTA puts in order
 constexpr int kOctaves = 32;  // of weights that bins of equal steps cover
 constexpr float kTemperatureMin = 0x1p-100f, kTemperatureMax = 0x1p100f;
 
-// 2^-(j / kSteps) as a whole number of 2^-30.  From square roots of 1/2, by Newton's iteration, and their products.
-struct PowerTable {
-  uint32_t e[kSteps];
-  constexpr PowerTable() : e{} {
-    double root[7] = {};
-    double r = 0.5;
-    for (int i = 6; i >= 0; --i) {
-      double s = r;
-      for (int k = 0; k < 60; ++k) s = 0.5 * (s + r / s);
-      root[i] = r = s;  // 2^-(2^i / 128)
-    }
-    for (int j = 0; j < kSteps; ++j) {
-      double v = 1.0;
-      for (int i = 0; i < 7; ++i)
-        if (j >> i & 1) v *= root[i];
-      e[j] = static_cast<uint32_t>(v * 0x1p30 + 0.5);
-    }
-  }
-};
 __device__ const PowerTable kPowers;
 
 // Logits in an order that whole numbers have, and back; no NaN comes here, and both zeros are one number.  A key has the bits that type T
@@ -230,23 +211,7 @@ struct SampleRow {
   }
 
   __device__ __forceinline__ u64 weight(float v) const {
-    // y = c (top - v) in two floats, up to 45 (where the weight ends).  The difference of floats is one as a sum of two (Knuth); that of 16-bit
-    // numbers is rounded only where one is 2^16 times the other.
-    const float d = fminf(fmaxf(top - v, 0.0f), most_off);  // (infinity under itself: 0)
-    float y = d * c, y_low = fmaf(d, c_low, fmaf(d, c, -y));
-    if constexpr (sizeof(T) == 4) {
-      const float t = d - top;
-      y_low = fmaf(d < most_off ? (top - (d - t)) - (v + t) : 0.0f, c, y_low);
-    }
-    const float j = fmaf(y, static_cast<float>(kSteps), 12582912.0f);  // (1.5 2^23: rounded to a whole number)
-    const uint32_t n = __float_as_uint(j);
-    const float r = fmaf(j - 12582912.0f, -1.0f / kSteps, y) + y_low;  // |r| < 2^-8 and a little
-    // e (2^-r - 1) by the series (to 2^-39), in units of 2^-30, rounded to a whole number; e as a float from its upper 24 bits
-    constexpr float kC1 = -0.6931471805599453f * 0x1p30f, kC2 = 0.2402265069591007f * 0x1p30f, kC3 = -0.0555041086648216f * 0x1p30f;
-    const uint32_t e = sh.power[n % kSteps][lane];
-    const float q = r * fmaf(r, fmaf(r, kC3, kC2), kC1);
-    const uint32_t m = e + __float_as_uint(fmaf(__uint_as_float((e >> 6) + (125u << 23)), q, 12582912.0f)) - 0x4b400000u;
-    return (static_cast<u64>(m) << 32) >> ((n / kSteps & 63) + 18);  // (n / kSteps <= 45)
+    return weight_of(v, top, c, c_low, most_off, [&](uint32_t j) { return sh.power[j][lane]; });
   }
 
   // puts down a logit between the bounds of a cut for the passes that follow: each warp its own
