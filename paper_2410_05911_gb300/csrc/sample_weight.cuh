@@ -59,9 +59,9 @@ template <class F>
 AECCT_BOTH uint64_t weight_of(float v, float top, float c, float c_low, float most_off, F &&power) {
   // y = c (top - v) in two floats, up to 45 (where the weight ends).  The difference of floats is one as a sum of two (Knuth), for logits of 16 bits
   // too: without what its rounding leaves out, those of 1e-7 under one of 8 would be off by 2^-22.
-  const float d = fminf(fmaxf(top - v, 0.0f), most_off);  // (infinity under itself: 0)
+  const float off = top - v, d = fminf(fmaxf(off, 0.0f), most_off);  // (of infinity under itself, no number: 0, and nothing left out)
   const float y = d * c, t = d - top;
-  const float y_low = fmaf(d < most_off ? (top - (d - t)) - (v + t) : 0.0f, c, fmaf(d, c_low, fmaf(d, c, -y)));
+  const float y_low = fmaf(off < most_off ? (top - (d - t)) - (v + t) : 0.0f, c, fmaf(d, c_low, fmaf(d, c, -y)));
   const float j = fmaf(y, static_cast<float>(kSteps), 12582912.0f);  // (1.5 2^23: rounded to a whole number)
   const uint32_t n = float_bits(j);
   const float r = fmaf(j - 12582912.0f, -1.0f / kSteps, y) + y_low;  // |r| < 2^-8 and a little

@@ -33,3 +33,19 @@ def test_borders_between_small_logits_under_a_large_one(n, dtype):
     got = A.sample(x.expand(len(u), n), torch.tensor(u).cuda()).cpu().numpy()
     want = np.searchsorted(upto, u.astype(np.float64), side="right")
     assert (got == want)[far].all(), int((got != want)[far].sum())
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+@pytest.mark.parametrize("vocab,many", [(4001, 3000), (50_021, 20_000), (2 ** 19, 2 ** 19)])
+def test_many_logits_of_plus_infinity(vocab, many, dtype):
+    """They share the row equally: what stays of them are the first, and u counts them."""
+    g = torch.Generator(device="cuda").manual_seed(many)
+    x = torch.randn((vocab,), device="cuda", generator=g)
+    at = torch.randperm(vocab, device="cuda", generator=g)[:many].sort().values
+    x[at] = float("inf")
+    u = ((torch.arange(64, device="cuda", dtype=torch.float64) + 0.5) / 64).float()  # (whole sixty-fourths of a half: exact)
+    rows = x.to(dtype).expand(64, vocab)
+    for settings, stay in ((dict(), many), (dict(top_p=0.5), -(-many // 2)), (dict(top_k=7), 7), (dict(min_p=0.9), many), (dict(top_k=many - 1, top_p=0.25), -(-(many - 1) // 4)),
+                           (dict(temperature=50.0), many), (dict(temperature=0.0), 1)):
+        want = at[(u.double() * stay).long()]  # the lowest with (rank + 1) > u stay
+        assert torch.equal(A.sample(rows, u, **settings), want), settings

@@ -118,3 +118,11 @@ def test_the_largest_logit_weighs_one(harness, dtype):
         assert (got == 2.0 ** 44).all()
     got, _ = weights(harness, 1.0, -np.inf, [0.3, 1.0, 7.0])
     assert not got.any()
+
+
+def test_infinity_under_itself_weighs_one(harness):
+    got, _ = weights(harness, np.inf, np.inf, [2.0 ** -100, 0.3, 1.0, 7.0, 2.0 ** 100])
+    assert (got == 2.0 ** 44).all(), got / 2.0 ** 44
+    for v in (-np.inf, -3e38, 0.0, 3e38):
+        got, _ = weights(harness, np.inf, v, [2.0 ** -100, 0.3, 1.0, 7.0, 2.0 ** 100])
+        assert not got.any()
