@@ -9,6 +9,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/cuda/EmptyTensor.h>
+#include <c10/core/AutogradState.h>
 #include <c10/core/GradMode.h>
 #include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
@@ -93,12 +94,18 @@ void check_current(const at::Device &on) {
 }
 
 // The operators record nothing for autograd (int8 codes stand between the norm and the product): where it would
-// record, a tensor that requires a gradient is refused, and does not lose it without a word.
+// record, a tensor that requires a gradient is refused, and does not lose it without a word.  Nor does one with a tangent (forward mode, which
+// torch.no_grad() leaves on and an autograd.Function turns off) lose that.
 void check_no_graph(const char *call, std::initializer_list<const at::Tensor *> tensors) {
-  if (!c10::GradMode::is_enabled()) return;
-  for (const at::Tensor *t : tensors)
-    if (t && t->defined() && t->requires_grad())
+  const bool reverse = c10::GradMode::is_enabled(), forward = c10::AutogradState::get_tls_state().get_fw_grad_mode();
+  if (!reverse && !forward) return;
+  for (const at::Tensor *t : tensors) {
+    if (!t || !t->defined()) continue;
+    if (reverse && t->requires_grad())
       throw ValueError(std::string(call) + " records nothing for autograd: call it under torch.no_grad(), in an autograd.Function, or on detached tensors");
+    if (forward && t->_fw_grad(0).defined())
+      throw ValueError(std::string(call) + " carries no tangents of forward mode: call it in an autograd.Function, or on the primal of a dual tensor");
+  }
 }
 
 // `t` holds rows of a known type on the GPU, and `gain` one float32 for each element of a row

@@ -61,3 +61,56 @@ def test_in_a_function_of_autograd():
     dx, dgain = A.rms_quant_backward(dn, total, gain)
     for got, want in zip(inputs, (dx, dgain, dw, db)):
         assert torch.equal(got.grad, want)
+
+
+def test_tensors_with_a_tangent_are_refused():
+    import torch.autograd.forward_ad as fw
+
+    x, r, gain, w, b, dy = tensors()
+    (t,), ws, _ = A.aap_ternarize([w])
+    codes, scale, total, _ = A.rms_quant(x, gain, residual=r)
+    cache = A.kv_cache(2, 2, 4, 16)
+    half = A.kv_cache(2, 2, 4, 16, dtype=torch.float16)
+    for c in (cache, half):
+        for s in c:
+            if s is not None:
+                s.zero_()
+    table, n = torch.tensor([[0, 1]], dtype=torch.int32, device="cuda"), torch.tensor([5], dtype=torch.int32, device="cuda")
+    k = torch.randn((1, 2, 16), device="cuda")
+    u = torch.rand((12,), device="cuda")
+    each = torch.ones((12,), device="cuda")
+    calls = [lambda d: A.rms_quant(d(x), gain), lambda d: A.rms_quant(x, d(gain)), lambda d: A.rms_quant(x, gain, residual=d(r)),
+             lambda d: A.rms_quant_backward(d(x), total, gain), lambda d: A.rms_quant_backward(x, total, gain, dtotal=d(r)),
+             lambda d: A.aap_linear(codes, d(scale), t, ws), lambda d: A.aap_linear(codes, scale, t, ws, bias=d(b)),
+             lambda d: A.aap_linear_backward(d(dy), codes, scale, t, ws), lambda d: A.kv_append(d(k), k, cache, table, n),
+             lambda d: A.kv_append(k, d(k), cache, table, n), lambda d: A.kv_append(k, k, cache._replace(v_scale=d(cache.v_scale)), table, n),
+             lambda d: A.kv_read(cache._replace(k_scale=d(cache.k_scale)), table, n, None, 1), lambda d: A.kv_read(half._replace(v=d(half.v)), table, n, None, 1),
+             lambda d: A.paged_attention(d(k), cache, table, n), lambda d: A.paged_attention(k.half(), half._replace(k=d(half.k)), table, n),
+             lambda d: A.sample(d(x), u), lambda d: A.sample(x, d(u)), lambda d: A.sample(x, u, temperature=d(each))]
+    with fw.dual_level():
+        dual = lambda v: fw.make_dual(v, torch.ones_like(v))  # noqa: E731
+        for i, call in enumerate(calls):
+            for on in (True, False):
+                with torch.set_grad_enabled(on), pytest.raises(ValueError, match="tangents"):
+                    call(dual)
+                    pytest.fail(f"call {i} was not refused")
+            call(lambda v: fw.unpack_dual(dual(v)).primal)
+        # in a function that says what its tangents are, forward mode is off
+        class Norm(torch.autograd.Function):
+            @staticmethod
+            def forward(v):
+                codes, scale, _, _ = A.rms_quant(v, gain)
+                return codes.float() * scale.reshape(-1, 1)
+
+            @staticmethod
+            def setup_context(ctx, inputs, output):
+                pass
+
+            @staticmethod
+            def jvp(ctx, tangent):
+                return 2 * tangent
+
+        y = fw.unpack_dual(Norm.apply(dual(x)))
+        assert (y.tangent == 2).all() and (y.primal - x * gain).isfinite().all()
+    for call in calls:
+        call(lambda v: v)
