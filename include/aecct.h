@@ -345,7 +345,8 @@ int aecct_clip_gradients(int32_t n_tensors, const void *const *grad, const int64
 /* A cache of keys and values in pages of page_size tokens:
  *   k, v              DEVICE [pages][heads][page_size][head_dim] of dtype, rows (of one token and head) ld elements
  *                     apart; 16-byte aligned, and ld elements are a multiple of 16 bytes.  What lies between a row's
- *                     end and the next one is never read or written.
+ *                     end and the next one is never written and never used; the rest of a row's last 16 bytes may be
+ *                     read (not behind the last row, where the memory may end).
  *   k_scale, v_scale  DEVICE fp32 [pages][heads][page_size]: the scale of each row of codes (dtype AECCT_I8); NULL
  *                     for rows of AECCT_F16 or AECCT_BF16, which are kept as they are.
  * Sequence b's token at position p lies in page table[b][p / page_size], at place p % page_size.  A page whose number

@@ -406,6 +406,16 @@ struct KvRowsCall {
   void *k_out, *v_out;  // read: [total][heads][dim]
   int dtype, cache_dtype;
 };
+// What a lane reads of rows that may lie anywhere.  Of a new token's row of 16-bit elements, `left` of them from the lane's `elements` first ones on (0 or
+// less: the row ends before them, or there is no row): whether the i-th 4-byte word from the one with the first element on, which is the second of that
+// word where `odd`.  A word without an element of the row may lie in no memory.
+__host__ __device__ constexpr bool reads_new_word(int left, int i, bool odd, int elements) {
+  return left > 0 && 2 * i - odd < left && (i < elements / 2 || odd);
+}
+// Of a cached row, `left` elements of `size` bytes: all of them, and where another row follows the rest of its last 16 bytes, which belong to no row.
+__host__ __device__ constexpr int reads_cached(int left, int size, bool follows) {
+  return left <= 0 ? 0 : follows ? (left + 16 / size - 1) / (16 / size) * (16 / size) : left;
+}
 cudaError_t launch_kv_append(const KvRowsCall &c, cudaStream_t stream);
 cudaError_t launch_kv_read(const KvRowsCall &c, cudaStream_t stream);
 

@@ -75,7 +75,7 @@ struct NewRow {
       odd = reinterpret_cast<uintptr_t>(x) >> 1 & 1;
       const uint32_t *from = reinterpret_cast<const uint32_t *>(reinterpret_cast<uintptr_t>(x) & ~uintptr_t(3));
 #pragma unroll
-      for (int i = 0; i < kWords; ++i) w[i] = n > 0 && 2 * i - odd < n && (i < E / 2 || odd) ? from[i] : 0;  // (words with an element of the row)
+      for (int i = 0; i < kWords; ++i) w[i] = reads_new_word(n, i, odd, E) ? from[i] : 0;
     }
   }
   __device__ __forceinline__ void numbers(int n, float (&v)[E]) const {
@@ -341,7 +341,7 @@ __global__ void __launch_bounds__(kRowsThreads, kCtas) read_through_kernel(const
   // A row's last 16 bytes are read whole, what lies behind its end with them, which goes no further (one by one: 19.2 us for 16.4 from 16 bits, 26 for 19.5
   // from codes); but not the cache's last row's, behind which its memory may end.
   const int64_t last = c.cache.pages * c.cache.heads * c.cache.page_size - 1;
-  const int whole = n > 0 ? (n + 15 / static_cast<int>(sizeof(C))) & -(16 / static_cast<int>(sizeof(C))) : 0;
+  const int whole = reads_cached(n, sizeof(C), true), exact = reads_cached(n, sizeof(C), false);
   find_places(c, token0, tokens, place);
   for (int values = 0; values < 2; ++values) {
     const C *from = static_cast<const C *>(values ? c.cache.v : c.cache.k);
@@ -352,7 +352,7 @@ __global__ void __launch_bounds__(kRowsThreads, kCtas) read_through_kernel(const
       for (int a = 0; a < AHEAD; ++a) {
         const int r = i + group + a * step, token = r / c.cache.heads, head = r - token * c.cache.heads;
         const int64_t first = r < rows ? place[token] : -1, row = first + static_cast<int64_t>(head) * c.cache.page_size;
-        x[a].load(from + (row * c.cache.ld + e), first < 0 ? 0 : row < last ? whole : n, scales + row);
+        x[a].load(from + (row * c.cache.ld + e), first < 0 ? 0 : row < last ? whole : exact, scales + row);
       }
       T *out = static_cast<T *>(values ? c.v_out : c.k_out) + (token0 * c.cache.heads + i) * c.cache.dim;
       const int off = static_cast<int>((reinterpret_cast<uintptr_t>(out) & 15u) / sizeof(T)), count = min(rows - i, AHEAD * step) * c.cache.dim;
