@@ -3,6 +3,8 @@ example that writes sequences."""
 import importlib.util
 import math
 import os
+import subprocess
+import sys
 
 import pytest
 
@@ -109,3 +111,43 @@ def test_example():
     assert m.generate(model, prompts, new=12) == together
     greedy = m.generate(model, prompts[:1], new=8, temperature=0.0)
     assert greedy[0][:3] == prompts[0] and len(greedy[0]) == 11
+
+
+FIRST_CALLS = r"""
+import torch
+from paper_2410_05911_gb300 import aecct as A
+A.load()
+g = torch.Generator(device="cuda").manual_seed(1)
+rand = lambda *s: torch.randn(s, device="cuda", generator=g)
+def arrays(batch, length):
+    columns = -(-length // 16)
+    table = torch.arange(batch * columns, device="cuda", dtype=torch.int32).view(batch, columns)
+    cache = A.kv_cache(batch * columns, 2, 16, 64)
+    for t in cache:
+        t.zero_()
+    n = torch.full((batch,), length, device="cuda", dtype=torch.int32)
+    rows = torch.arange(batch + 1, device="cuda", dtype=torch.int32) * length
+    return cache, table, n, rows, rand(batch * length, 2, 64), rand(batch, 8, 64)
+few, many, long = arrays(2, 100), arrays(400, 50), arrays(3, 5000)
+logits, u = rand(4, 50021), torch.rand((4,), device="cuda", generator=g)
+def step():
+    out = []
+    for cache, table, n, rows, x, q in (few, many, long):
+        A.kv_append(x, x, cache, table, n, rows=rows)
+        out += [*A.paged_attention(q, cache, table, n, want_lse=True), *A.kv_read(cache, table, n, rows, len(x))]
+    return out + [A.sample(logits, u, top_p=0.9), A.sample(logits[:, :1000], u, top_k=20)]
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    got = step()
+graph.replay()
+got = [t.clone() for t in got]
+assert all(torch.equal(a, b) for a, b in zip(got, step())) and got[0].any()
+print("same")
+"""
+
+
+def test_first_calls_of_a_process_in_a_capture():
+    """Nothing of a call needs one before it outside of the graph."""
+    r = subprocess.run([sys.executable, "-c", FIRST_CALLS], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True, timeout=300)
+    assert r.returncode == 0 and r.stdout.strip() == "same", r.stderr[-2000:]
