@@ -398,7 +398,8 @@ int aecct_kv_read(const aecct_kv_cache *cache, const aecct_kv_sequences *seqs, c
  * aecct_kv_append are).  Sums, maxima and the softmax are in 32 bits, in an order that hangs on the sizes of the call and on the
  * lengths of the whole batch, and on nothing else.
  *   workspace  aecct_paged_attention_workspace bytes, 16-byte aligned; not read before it is written.
- * Errors: as above, and INVALID_ARG where heads does not divide q_heads, scale is not finite or the workspace is too small. */
+ * Errors: as above, and INVALID_ARG where heads does not divide q_heads, scale log2 e is not finite in 32 bits or the workspace is too
+ * small. */
 int aecct_paged_attention_workspace(int32_t batch, int32_t q_heads, int32_t heads, int32_t head_dim, int32_t dtype,
                                     int32_t cache_dtype, int64_t *bytes);
 int aecct_paged_attention(const aecct_kv_cache *cache, const aecct_kv_sequences *seqs, const int32_t *first,

@@ -1482,7 +1482,7 @@ int aecct_paged_attention(const aecct_kv_cache *cache, const aecct_kv_sequences 
   int64_t need = 0;
   bad = aecct_paged_attention_workspace(seqs->batch, q_heads, cache->heads, cache->head_dim, dtype, cache->dtype, &need);
   if (bad != AECCT_OK) return bad;
-  if (!std::isfinite(scale)) return AECCT_ERR_INVALID_ARG;
+  if (!std::isfinite(scale * 1.4426950408889634f)) return AECCT_ERR_INVALID_ARG;  // (scores are taken in powers of two)
   if (seqs->batch == 0) return AECCT_OK;
   if (!is_rows(q, ld_row, ld_head, dtype) || !is_array(out, dtype) || (lse && !is_array(lse, AECCT_F32)) ||
       (first && !is_array(first, AECCT_F32)) || !is_workspace(workspace, workspace_bytes, need))

@@ -101,3 +101,9 @@ def test_tensors_of_another_device_are_refused():
                  lambda: A.sample(Elsewhere((3, 100), torch.float32), Elsewhere((3,), torch.float32))):
         with pytest.raises(ValueError, match="cuda:63, which is not the current CUDA device"):
             call()
+
+
+def test_a_scale_that_overflows_in_powers_of_two():
+    """Scores are taken in powers of two: scale log2 e has to be finite too."""
+    for scale in (2.4e38, -2.4e38, 3.4e38, -math.inf):
+        assert attend(scale=scale) == BAD, scale
