@@ -395,8 +395,10 @@ int aecct_kv_read(const aecct_kv_cache *cache, const aecct_kv_sequences *seqs, c
  *   first  DEVICE [batch], or NULL: from position 0.
  *   out    [batch][q_heads][head_dim] of dtype;  lse  fp32 [batch][q_heads] or NULL.
  * A sequence with no position to attend to gets zeros, and an lse of minus infinity.  Scales of rows of codes are positive (those of
- * aecct_kv_append are).  Sums, maxima and the softmax are in 32 bits, in an order that hangs on the sizes of the call and on the
- * lengths of the whole batch, and on nothing else.
+ * aecct_kv_append are).  Sums, maxima and exponentials (to 2^-22) are in 32 bits, in an order that hangs on the sizes of the call and on the
+ * lengths of the whole batch, and on nothing else.  The factors of the products are rounded: a weight exp(s_j - max) to 11 bits for AECCT_BF16
+ * queries over codes, to 16 for a cache of AECCT_BF16 and to 22 else, AECCT_F32 queries to 22; weights under 2^-29 of the largest (with codes: times
+ * their rows' scales) to 2^-39 of it, but for a cache of AECCT_BF16.
  *   workspace  aecct_paged_attention_workspace bytes, 16-byte aligned; not read before it is written.
  * Errors: as above, and INVALID_ARG where heads does not divide q_heads, scale log2 e is not finite in 32 bits or the workspace is too
  * small. */
@@ -417,7 +419,8 @@ typedef struct {
 /* The next token of each row of logits x, given a number u in [0, 1) for it:
  *   w_i = exp((x_i - max x) / temperature); tokens in descending order of x, the lower index first among equal ones;
  *   the first top_k of them stay (all for top_k <= 0); of these the shortest beginning whose weight is at least
- *   top_p of theirs, and no less than one token (all for top_p >= 1); of these the tokens with w_i >= min_p;
+ *   top_p of theirs, and no less than one token (all for top_p >= 1); of these the tokens with w_i >= min_p (and the largest
+ *   logits whatever min_p is);
  *   token = the lowest index i among those that stay with sum over j <= i of w_j > u sum over all of w_j.
  * A temperature of 0 (or less, or NaN) takes the largest logit, the lowest index among equal ones; others count as 2^-100 at
  * least and 2^100 at most.  Logits of minus infinity

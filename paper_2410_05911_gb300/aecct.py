@@ -576,7 +576,8 @@ def paged_attention(q, cache, table, lengths, first=None, scale=None, want_lse: 
     """aecct_paged_attention: one new token's queries q [batch, q_heads, head_dim] over the keys and values of its sequence in
     `cache`, positions first[b] .. lengths[b] - 1 (first int32 [batch], or None: from 0; lengths counts the new token, once
     kv_append has written it).  q_heads is a multiple of the cache's heads, which serve as many query heads each.  scale is 1 / sqrt(head_dim)
-    unless given.  q is float32, float16 or bfloat16, the cache's own type where it is not int8.  Returns (out like q, lse):
+    unless given.  q is float32, float16 or bfloat16, the cache's own type where it is not int8.  Sums are in 32 bits; the weights, as the tensor cores
+    take them, have 22 bits, for a bfloat16 cache 16, for bfloat16 queries on int8 codes 11 (float32 queries 22).  Returns (out like q, lse):
     lse float32 [batch, q_heads] is the log of the sum of exponentials where wanted, else None.  Zeros (and minus infinity) for a
     sequence with nothing to attend to."""
     return (_binding or _operators()).paged_attention(q, cache, table, lengths, first, scale, bool(want_lse), stream)

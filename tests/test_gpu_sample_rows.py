@@ -128,3 +128,13 @@ def test_logits_that_are_not_finite_in_rows_of_several_ctas(vocab, dtype):
         for r, token in enumerate(got):
             assert token in tokens(rows[r], float(u[r]), t, s["top_k"], p, mp), (r, settings, token)
         assert got[1] == got[2] == got[9] == -1 and got[5] == vocab // 2 and got[10] == 0
+
+
+def test_the_largest_logits_stay_whatever_min_p_is():
+    g = torch.Generator(device="cuda").manual_seed(2)
+    x = torch.randint(0, 9, (8, 5000), device="cuda", generator=g).float()
+    u = torch.rand((8,), device="cuda", generator=g)
+    for kw in (dict(), dict(top_p=0.01), dict(top_k=300), dict(top_k=300, top_p=0.01)):
+        want = A.sample(x, u, min_p=1.0, **kw)
+        assert torch.equal(A.sample(x, u, min_p=1.5, **kw), want) and torch.equal(A.sample(x, u, min_p=3e38, **kw), want)
+        assert (x[torch.arange(8), want] == 8).all()
