@@ -5,6 +5,9 @@
 // Work.  The G query heads of a cache head read the same keys and values, so they are one operand of a matrix product: S^T = K q^T
 // and O^T = V^T P^T on the tensor cores, 16 keys (and 16 elements of a head) by 8 columns.  A column is a query head, or for P = 2
 // half of one: its numbers in two pieces of 16 bits (the number rounded, and what the rounding left), whose products are added up.
+// A warp has 8 columns, or 16 where heads are up to 128 wide.  Query heads that do not fit (more than 16 / P, or 8 / P of wider heads) are a piece
+// of heads of their own, whose tiles read the same keys and values again: 64 contexts of up to 8,000 tokens, 8 heads of 128 in bfloat16, 193 us for
+// 8 query heads to each and 353 for 16; of 256 388 for 4, 710 for 8 and 1,436 for 16.
 // The positions of all sequences and cache heads are one list of tiles of TK keys, cut evenly over CTAs and
 // over their warps, whatever the lengths are: a warp takes several short sequences, or a part of a long one.  A warp needs no other
 // one while it works: it has a ring of stages in shared memory, filled by asynchronous copies that also put zeros where no
@@ -17,11 +20,17 @@
 // follow one another, paired by key with byte permutes.  No transposed copy of V is made.  Codes become halves exactly:
 // 0x6400 + (code + 128) is the half 1152 + code.
 //
+// The forms with 16 columns over codes spill: attend_kernel 70 bytes of its 128 registers at 64 wide, 28 of its 255 at 128 (64 contexts as above
+// 116 us for 8 query heads in 8 columns, 167 for 16 in 16); attend_whole_kernel 36 and 20, attend_lone_kernel 4 at 64; the others 4 at most.
+//
 // Bound by memory where sequences are long: a million tokens of 8 cache heads of 128, 8 query heads to each, take 346 us, 6.1 TB/s (a copy of the
 // same bytes 313).  Where they are short, by a piece's start and end and by what a warp alone waits for: 512 sequences of up to 180 tokens, 8 heads
 // of 16, 16 us.
 //
-// 32 bits: sums of products, maxima, exponents and sums.  What is rounded to 16: the weights, as the tensor cores' operand. With codes the scale of a value row belongs to the
+// 32 bits: sums of products, maxima, exponents and sums (exponentials and the scales' logarithms by the hardware's, to 2^-22).  What is rounded: the
+// weights, as the tensor cores' operand, to 11 bits in one half for bfloat16 results over codes, else to two pieces (22 bits in halves, 16 in
+// bfloat16); float queries over codes, to 22.  A float result is 2.4 times as far from 64 bits as the plain form (5.1e-7 and 2.1e-7), a result in 16
+// bits as far.  With codes the scale of a value row belongs to the
 // weight: 2^(x_j - m) vs_j = 2^(y_j), y_j = x_j - m + log2 vs_j, has a running maximum of its own, so that the weights that
 // count use the whole range of a half.  Queries times codes are exact products: a bfloat16 or half query is scaled by a power of two to fit a half, a float one is cut in two.
 #pragma once
@@ -914,7 +923,7 @@ __global__ void __launch_bounds__(S::kWarps * 32, S::kCtas) attend_whole_kernel(
   cluster_sync_all();  // (no CTA ends while another one reads its sums)
 }
 
-// Many short sequences: a warp to each piece of heads of each of them, and nothing to join (512 of up to 180 tokens, 8 heads of 16, 16 us, 24 dealt
+// Many short sequences: a warp to each piece of heads of each of them, and nothing to join (512 of up to 180 tokens, 8 heads of 16, 16 us, 25 dealt
 // out).
 template <class S>
 __global__ void __launch_bounds__(S::kWarps * 32, S::kCtas) attend_lone_kernel(const __grid_constant__ AttendArgs a, int pieces) {
@@ -1018,7 +1027,7 @@ cudaError_t run_attend(const AttendArgs *a, AttendPlan *plan, cudaStream_t st) {
   attend_kernel<S><<<plan->ctas, S::kWarps * 32, S::kSmem, st>>>(*a);
   return cudaGetLastError();
 }
-// two blocks of columns where one does not hold the group
+// two blocks of columns where one does not hold the group; 256 wide, their queries and rows would not fit the registers
 template <typename C, int DP, int P>
 cudaError_t run_columns(int group, const AttendArgs *a, AttendPlan *plan, cudaStream_t st) {
   if constexpr (DP <= 128) {

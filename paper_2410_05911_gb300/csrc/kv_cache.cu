@@ -6,7 +6,8 @@
 //
 // A row is read and written once.  It has some lanes of a warp (a power of two, 16 elements each), which take its maximum by shuffles; a thread has kAhead
 // rows on their way at once.  Reading back is bound by memory (67,700 tokens of 8 heads of 128 into bfloat16 74 us, 5.7 TB/s), writing by its
-// instructions too, some 60 for a row of 128 in each of its 8 lanes' warps (19,400 tokens 27 us, 4.4 TB/s).
+// instructions too, some 60 for a row of 128 in each of its 8 lanes' warps (19,400 tokens 24 us, 5.0 TB/s; into a 16-bit cache 31.5 us, 5.0 TB/s).  A row
+// takes the lanes and the time of the next power of two: 12,300 tokens of 12 float heads of 100 33 to 34 us, of 128 34.
 #include <cuda_runtime.h>
 
 #include <cstdint>

@@ -13,8 +13,10 @@
 // A cluster of 1 to 8 CTAs takes a row, each a part of it, and reads the others' histograms and sums through distributed
 // shared memory.
 //
-// Bound by instructions where rows are many and flat (128 rows of 131,072 logits, top-p 0.9: 68 us, of them 28 for the weights of all logits, 11 for
-// the histogram of steps, 5 for the trip to memory), by the phases' trips and barriers where they are few (one row of 50,021, every filter: 17 us).
+// Bound by instructions where rows are many and flat (128 rows of 131,072 logits, top-p 0.9: 72 us, of them some 32 for the weights of all logits, 11
+// for the histogram of steps, 5 for the trip to memory; 4 of the 32 for what rounding takes from the difference to the largest logit), by the phases'
+// trips and barriers where they are few (one row of 50,021, every filter: 17 us).  An exact weight of every logit is this design's choice: the
+// definition needs exact sums next to a border only.  The kernels for 16-bit logits spill 4 bytes of their 64 registers.
 #include <cuda_runtime.h>
 
 #include <atomic>
@@ -805,8 +807,8 @@ int rows_at_once(int i) {
   return n;
 }
 
-// CTAs to a row: as long as all rows' run at once, and each has 8 logits to a thread (one row of 50,021: 27.5 us with 4 CTAs and 31 with 8 at
-// top-p alone, 37 with one; 16 with either, 22 with one, at top-k; of 131,072 41, 44 and 73)
+// CTAs to a row: as long as all rows' run at once, and each has 8 logits to a thread (one row of 50,021: 27.3 us with 4 CTAs and 30.6 with 8 at
+// top-p alone, 36.5 with one; 15.6 with either, 20.7 with one, at top-k; of 131,072 in 16 bits 36.7, 38.5 and 67)
 template <int NT>
 int ctas_of(const SampleCall &c) {
   int i = 0;
@@ -826,7 +828,8 @@ cudaError_t launch_of(SampleCall c, cudaStream_t st) {
 
 cudaError_t launch_sample(const SampleCall &c, cudaStream_t st) {
   // Short rows, and rows that CTAs of 1,024 threads, one to an SM, would take in three rounds or more: CTAs of 256 threads, of which an SM holds
-  // four (512 rows of 1,000 logits 24 us, 82 in the long ones; of 30,000 78 and 118; but 160 rows of 131,072 160 and 127).
+  // four (512 rows of 1,000 logits 18 us, 62 in the long ones; of 30,000 85 and 118; but 160 rows of 131,072 168 and 131, and 305 of them 315 and 195,
+  // where the rule takes the slower side).
   if (c.vocab <= 4 * kLong || c.rows > 2 * sm_count()) return launch_of<kShort>(c, st);
   return launch_of<kLong>(c, st);
 }
